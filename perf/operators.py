@@ -268,7 +268,7 @@ def run(state):
 
 def _handle(s):
     import paper_2606_02955_gb300 as fd
-    return fd, fd.Kv4Cache(s["k_codes"], s["v_codes"], s["k_affine"], s["v_affine"])
+    return fd, fd.KvCache(s["k_codes"], s["v_codes"], s["k_affine"], s["v_affine"])
 
 
 def _own_qk(s):
@@ -281,14 +281,14 @@ def _own_qk(s):
 
 def _own_store(s):
     fd, cache = _handle(s)
-    fd.fdllm_kv4_append(cache, s["table"], s["start"], s["k"], s["v"])
-    k, v = fd.fdllm_kv4_read(cache, s["table"], s["start"], s["case"]["n"], s["k"].dtype)
+    fd.fdllm_cache_append(cache, s["table"], s["start"], s["k"], s["v"])
+    k, v = fd.fdllm_cache_read(cache, s["table"], s["start"], s["case"]["n"], s["k"].dtype)
     return {"k": k, "v": v}
 
 
 def _own_attn(s):
     fd, cache = _handle(s)
-    out, lse = fd.fdllm_kv4_attention(s["q"], cache, s["table"], s["lens"], s["k_new"], s["v_new"],
+    out, lse = fd.fdllm_cache_attention(s["q"], cache, s["table"], s["lens"], s["k_new"], s["v_new"],
                                       new_lens=s["new_lens"], causal=s["case"]["causal"],
                                       scale=s["scale"], return_lse=True)
     return {"out": out, "lse": lse}
@@ -296,16 +296,16 @@ def _own_attn(s):
 
 def _own_weigh(s):
     fd, cache = _handle(s)
-    return {"weights": fd.fdllm_kv4_key_weights(s["q"], s["lse"], cache, s["table"], s["lens"],
+    return {"weights": fd.fdllm_cache_key_weights(s["q"], s["lse"], cache, s["table"], s["lens"],
                                                 weights=s["weights"], scale=s["scale"])}
 
 
 def _own_evict(s):
     fd, cache = _handle(s)
     c = s["case"]
-    lens, weights, index = fd.fdllm_kv4_evict(cache, s["table"], s["lens"], s["weights"], c["budget"],
+    lens, weights, index = fd.fdllm_cache_evict(cache, s["table"], s["lens"], s["weights"], c["budget"],
                                               s["to"], keep_first=c["first"], keep_last=c["last"])
-    k, v = fd.fdllm_kv4_read(cache, s["to"], None, c["budget"], DTYPES[c["dtype"]], count=lens)
+    k, v = fd.fdllm_cache_read(cache, s["to"], None, c["budget"], DTYPES[c["dtype"]], count=lens)
     return {"lens": lens, "weights": weights, "index": index, "k": k, "v": v}
 
 
