@@ -352,6 +352,166 @@ fdllm_status fdllm_profile_terms(const float *conf, const uint8_t *mask, int B, 
                                  double delta, double *out_G, double *out_F, double *out_B,
                                  double *out_feff, int32_t *out_order, void *stream);
 
+/* ------------------------------------------------------------ the 4-bit prefix cache --- */
+/* The paper's decoding keeps the keys and values of the finished prefix and lets the active
+ * block's queries attend to them at every step (PrefixCache, Sec. 5); the cache itself is
+ * the model's side of the step, which the paper takes as given.  The entry points below hold
+ * such a cache in 4 bits, in pages, for one layer: write (fdllm_cache_append), read back
+ * (fdllm_cache_read), attend (fdllm_cache_attention), measure how much attention each key
+ * receives (fdllm_cache_key_weights) and drop the keys that receive little
+ * (fdllm_cache_evict).  fdllm_qk_norm_rope makes the queries and keys that enter it.  All of
+ * them are asynchronous on `stream`, allocate nothing, use no library workspace and may be
+ * captured into a CUDA graph (the forward pass of fdllm_decode_loop, for instance).  They are
+ * forms for inference and have no gradients.
+ *
+ * A row of D values (one token's keys, or values, of one head) is held as 4-bit codes with
+ * two bfloat16 numbers, value = offset + scale * code:
+ *   offset = bf16(min), scale = bf16((max - min) / 15),
+ *   code   = clamp(rint((x - offset) / scale), 0, 15), 0 when scale is 0,
+ * computed in fp32 (bf16(): round to nearest even; rint(): half to even).  A row with a NaN or
+ * an infinity, or whose range overflows, is held as NaN (all of its values read as NaN).
+ *
+ * Pages are found through block_table [B, max_pages] int32 (device): slot j of sequence b is
+ * slot j % page_size of page block_table[b][j / page_size].  Slots keep the order of the
+ * tokens; attention does not depend on it.  Offsets into the cache are 64-bit.
+ */
+typedef struct {
+    void *k_codes;   /* uint8 [pages, heads, page_size, D/2]: channel 2i in the low half of
+                        byte i                                                            */
+    void *v_codes;   /* uint8 [pages, heads, D, page_size/2]: slot 2i in the low half of
+                        byte i (channel-major, as the attention's products read it)       */
+    void *k_affine;  /* bfloat16 [pages, heads, page_size, 2]: (scale, offset)            */
+    void *v_affine;  /* bfloat16 [pages, heads, page_size, 2]: (scale, offset)            */
+    int pages;
+    int heads;       /* key/value heads                                                   */
+    int page_size;   /* 32, 64, 128 or 256                                                */
+    int head_dim;    /* D: 64 or 128                                                      */
+} fdllm_cache;
+/* The four arrays are device memory of the caller, 16-byte aligned, of any content before
+ * the slots are written (they need not be cleared).  The struct itself is host memory, read
+ * during the call.  Every entry point checks it: FDLLM_ERR_ARG for a null pointer or a size
+ * out of range, FDLLM_ERR_ALIGN for a base that is not 16-byte aligned. */
+
+/* Per-head RMS norm of queries and keys and their rotary positions in one pass:
+ *   y = x / sqrt(mean(x^2) + eps) * weight        (skipped for a tensor whose weight is NULL)
+ *   pair p of y turned by the angle positions[axis(p)][t] * inv_freq[p].
+ * All arithmetic in fp32, rounded once; the angle is reduced exactly (64-bit fixed point, in
+ * turns), so positions up to 2^31 keep their full accuracy.
+ *   q, k         [T, Hq, D], [T, Hk, D] in dtype, the channels of a row contiguous;
+ *                q_strides / k_strides: {token, head} strides in elements, host (rows of a
+ *                packed projection, for instance).  k may be NULL with Hk = 0.
+ *   D            2 to 512, even.
+ *   q_weight, k_weight  [D] in dtype, or NULL.
+ *   positions    [axes, T] int32 device, any sign; axes 1 to 4 (time, height, width, ...).
+ *   sections     host, axes ints summing to pairs: the first sections[0] pairs follow axis
+ *                0, and so on; NULL with axes = 1.
+ *   inv_freq     host, `pairs` finite doubles (radians per position), pairs <= D / 2; channels
+ *                from 2 * pairs on are normed but not turned.
+ *   interleaved  0: pair p is channels (p, p + pairs); 1: channels (2p, 2p + 1).
+ *   out_q, out_k contiguous [T, Hq, D], [T, Hk, D] in dtype; out_q may be q itself where q is
+ *                contiguous (likewise k).
+ * T = 0 is a no-op.  Errors: FDLLM_ERR_ARG. */
+fdllm_status fdllm_qk_norm_rope(const void *q, const int64_t *q_strides, const void *k,
+                                const int64_t *k_strides, int dtype, int T, int Hq, int Hk,
+                                int D, const void *q_weight, const void *k_weight, double eps,
+                                const int32_t *positions, int axes, const int32_t *sections,
+                                const double *inv_freq, int pairs, int interleaved, void *out_q,
+                                void *out_k, void *stream);
+
+/* Writes n tokens' keys and values into slots start[b] .. start[b] + count[b] - 1.
+ *   k, v   [B, n, heads, D] in dtype (bf16, fp16 or fp32), channels contiguous; strides
+ *          {batch, token, head} in elements, host; base and strides 16-byte multiples
+ *          (FDLLM_ERR_ALIGN).
+ *   start  [B] int32 device, or NULL: 0.      count  [B] int32 device, or NULL: n; tokens from
+ *          count[b] on are padding and not written.
+ * A token whose slot is negative, past the table or in a page out of range is not written
+ * (device data, not checked on the host; attention over such a slot reports NaN).  Two slots
+ * share a byte of v_codes: calls writing one sequence must be ordered on the GPU. */
+fdllm_status fdllm_cache_append(const fdllm_cache *cache, const int32_t *block_table, int B,
+                                int max_pages, const int32_t *start, const int32_t *count,
+                                const void *k, const int64_t *k_strides, const void *v,
+                                const int64_t *v_strides, int dtype, int n, void *stream);
+
+/* Reads slots start[b] .. start[b] + n - 1 back as dense rows: out_k, out_v contiguous
+ * [B, n, heads, D] in dtype (offset + scale * code in fp32, rounded once).  Rows from count[b]
+ * on (count NULL: n) are zero; a slot that does not exist reads as NaN.  start, count as in
+ * fdllm_cache_append. */
+fdllm_status fdllm_cache_read(const fdllm_cache *cache, const int32_t *block_table, int B,
+                              int max_pages, const int32_t *start, const int32_t *count,
+                              void *out_k, void *out_v, int dtype, int n, void *stream);
+
+/* Attention of Lq queries of each sequence over its cached keys and the block's own:
+ *   s_ij = scale * (q_i . k_j),   out_i = sum_j softmax_j(s_ij) v_j,
+ *   out_lse_i = log sum_j exp(s_ij).
+ * Query head h reads key/value head h / (Hq / heads).
+ *   q            [B, Lq, Hq, D] bf16 or fp16, Hq a multiple of the cache's heads; strides
+ *                {batch, token, head} in elements, host.
+ *   cache_lens   [B] int32 device: slots 0 .. cache_lens[b] - 1 are attended to.
+ *   k_new, v_new [B, Ln, heads, D] in q's dtype: the block's own keys and values, not in the
+ *                cache, strides as q's; NULL with Ln = 0.
+ *   new_lens     [B] int32 device, or NULL: Ln.  Own keys from new_lens[b] on are not seen.
+ *   causal       1: query i sees own keys j <= i only (all cached keys always).
+ *   out          [B, Lq, Hq, D] in q's dtype, contiguous.   out_lse [B, Lq, Hq] fp32 or NULL.
+ *   workspace    device, 256-byte aligned, fdllm_cache_attention_workspace_bytes() bytes, of
+ *                any content; calls that may overlap on the GPU need their own.
+ * A query that sees no key gets out = 0 and out_lse = -inf.  A sequence whose cache_lens or
+ * new_lens is out of range (negative, past the table, past Ln) or that meets a page out of
+ * range among its first cache_lens slots gets NaN, for all its rows where the lengths are
+ * wrong and for the heads and rows that meet the page otherwise.  Non-finite values behind
+ * the lengths or the causal bound change nothing.  Scores and sums are fp32; the weights enter
+ * the second product as fp16 with the scale of the cached row folded in (own values: as a sum
+ * of two numbers of q's dtype).
+ * q, k_new and v_new: 16-byte aligned bases and strides (FDLLM_ERR_ALIGN). */
+fdllm_status fdllm_cache_attention(const void *q, const int64_t *q_strides, int dtype, int B,
+                                   int Lq, int Hq, const fdllm_cache *cache,
+                                   const int32_t *block_table, int max_pages,
+                                   const int32_t *cache_lens, const void *k_new,
+                                   const int64_t *k_strides, const void *v_new,
+                                   const int64_t *v_strides, int Ln, const int32_t *new_lens,
+                                   int causal, double scale, void *out, float *out_lse,
+                                   void *workspace, size_t workspace_bytes, void *stream);
+
+/* Bytes of workspace fdllm_cache_attention needs for these sizes (a host function; it asks
+ * the current device for its number of SMs).  0 for sizes out of range. */
+size_t fdllm_cache_attention_workspace_bytes(int B, int Lq, int Hq, int heads, int head_dim);
+
+/* The attention each cached key receives, summed over the queries and the heads that read it:
+ *   weights_out[b][h][j] = weights_in[b][h][j] + sum_{i, g} exp(scale * q_ig . k_j - lse_ig)
+ * for j < cache_lens[b], and 0 from there to max_len - 1.
+ *   q, cache, block_table, cache_lens, scale   as in fdllm_cache_attention.
+ *   lse          [B, Lq, Hq] fp32, contiguous: fdllm_cache_attention's out_lse (a row of -inf
+ *                counts as 0: it saw no key).
+ *   weights_in   [B, heads, max_len] fp32 or NULL (0); weights_out the same shape, may be
+ *                weights_in.
+ * Deterministic (no atomics).  A sequence whose length is negative, past the table or past
+ * max_len gets NaN in all its weights, a key in a page out of range NaN in its own. */
+fdllm_status fdllm_cache_key_weights(const void *q, const int64_t *q_strides, int dtype, int B,
+                                     int Lq, int Hq, const fdllm_cache *cache,
+                                     const int32_t *block_table, int max_pages,
+                                     const int32_t *cache_lens, const float *lse, double scale,
+                                     const float *weights_in, float *weights_out, int max_len,
+                                     void *stream);
+
+/* Keeps `budget` keys of each sequence and head: the first keep_first slots, the last
+ * keep_last, and of the rest those with the largest weights (equal weights: the lower slot; a
+ * NaN weighs less than any number).  The kept rows are copied in slot order into the pages of
+ * dst_table [B, dst_max_pages], slots 0, 1, ...; each head keeps its own set.  A sequence of
+ * at most `budget` slots keeps all of them.
+ *   weights      [B, heads, max_len] fp32 (fdllm_cache_key_weights).
+ *   out_lens     [B] int32: min(cache_lens[b], budget); -1 for a sequence whose length is
+ *                negative, past the table or past max_len (nothing else is written for it but
+ *                the padding).
+ *   out_weights  [B, heads, budget] fp32: the kept keys' weights, 0 behind out_lens.
+ *   out_index    [B, heads, budget] int32: the slots they came from, -1 behind out_lens.
+ * The source is not modified; dst_table's pages must not be among the source's, and
+ * dst_max_pages * page_size >= budget (FDLLM_ERR_ARG).  Rows whose source or destination page
+ * is out of range are not copied.  budget >= 1, keep_first + keep_last <= budget. */
+fdllm_status fdllm_cache_evict(const fdllm_cache *cache, const int32_t *block_table, int B,
+                               int max_pages, const int32_t *cache_lens, const float *weights,
+                               int max_len, int budget, int keep_first, int keep_last,
+                               const int32_t *dst_table, int dst_max_pages, int32_t *out_lens,
+                               float *out_weights, int32_t *out_index, void *stream);
+
 /* Health check of the library's failure detection: every wait inside the kernels is
  * bounded, and a wait that runs out records a device error and lets the kernel return
  * instead of hanging.  This launches one thread that waits on a barrier nobody completes,
