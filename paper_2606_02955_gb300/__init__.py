@@ -27,6 +27,9 @@ __all__ = [
     "fdllm_lmhead_select", "fdllm_lmhead_confidence", "fdllm_lmhead_logits",
     "fdllm_gather_masked_rows", "fdllm_decode_loop_lmhead", "fdllm_vocab_reduce",
     "fdllm_select_host",
+    "KvCache", "fdllm_qk_norm_rope", "fdllm_cache_append", "fdllm_cache_read",
+    "fdllm_cache_attention", "fdllm_cache_attention_workspace_bytes",
+    "fdllm_cache_key_weights", "fdllm_cache_evict",
 ]
 
 BF16, FP32, FP16 = 0, 1, 2
@@ -85,6 +88,22 @@ def _load():
     lib.fdllm_decode_loop_lmhead.argtypes = [i, i, i, i, i, p, d, i, FORWARD_FN, p, p, p, p, i,
                                              ctypes.POINTER(ctypes.c_int), p]
     lib.fdllm_decode_loop_lmhead.restype = i
+    lib.fdllm_qk_norm_rope.argtypes = [p, p, p, p, i, i, i, i, i, p, p, d, p, i, p, p, i, i, p,
+                                       p, p]
+    lib.fdllm_qk_norm_rope.restype = i
+    lib.fdllm_cache_append.argtypes = [p, p, i, i, p, p, p, p, p, p, i, i, p]
+    lib.fdllm_cache_append.restype = i
+    lib.fdllm_cache_read.argtypes = [p, p, i, i, p, p, p, p, i, i, p]
+    lib.fdllm_cache_read.restype = i
+    lib.fdllm_cache_attention.argtypes = [p, p, i, i, i, i, p, p, i, p, p, p, p, p, i, p, i, d, p,
+                                          p, p, sz, p]
+    lib.fdllm_cache_attention.restype = i
+    lib.fdllm_cache_attention_workspace_bytes.argtypes = [i, i, i, i, i]
+    lib.fdllm_cache_attention_workspace_bytes.restype = sz
+    lib.fdllm_cache_key_weights.argtypes = [p, p, i, i, i, i, p, p, i, p, p, d, p, p, i, p]
+    lib.fdllm_cache_key_weights.restype = i
+    lib.fdllm_cache_evict.argtypes = [p, p, i, i, p, p, i, i, i, i, p, i, p, p, p, p]
+    lib.fdllm_cache_evict.restype = i
     lib.fdllm_check_bounded_wait.argtypes = [d, p]
     lib.fdllm_check_bounded_wait.restype = i
     lib.fdllm_device_status.argtypes = [p]
@@ -523,6 +542,332 @@ def fdllm_decode_loop_lmhead(forward, hidden: torch.Tensor, w_vocab: torch.Tenso
         ctypes.byref(steps), _stream(stream))
     _check(st, "fdllm_decode_loop_lmhead")
     return seq, nfe, steps.value
+
+
+class _CacheStruct(ctypes.Structure):
+    _fields_ = [("k_codes", ctypes.c_void_p), ("v_codes", ctypes.c_void_p),
+                ("k_affine", ctypes.c_void_p), ("v_affine", ctypes.c_void_p),
+                ("pages", ctypes.c_int), ("heads", ctypes.c_int), ("page_size", ctypes.c_int),
+                ("head_dim", ctypes.c_int)]
+
+
+class KvCache:
+    """The 4-bit prefix cache of one layer (fdllm_cache): four CUDA tensors and their sizes.
+
+    ``k_codes`` uint8 [pages, heads, page_size, D/2], ``v_codes`` uint8 [pages, heads, D,
+    page_size/2], ``k_affine`` and ``v_affine`` bfloat16 [pages, heads, page_size, 2] (scale,
+    offset).  ``KvCache.empty`` allocates them."""
+
+    __slots__ = ("k_codes", "v_codes", "k_affine", "v_affine", "pages", "heads", "page_size",
+                 "head_dim", "device", "_struct", "_ref")
+
+    def __init__(self, k_codes, v_codes, k_affine, v_affine):
+        if k_codes.dim() != 4:
+            raise ValueError("k_codes must be [pages, heads, page_size, D/2]")
+        pages, heads, page, half = k_codes.shape
+        _dev(k_codes, "k_codes", torch.uint8)
+        _dev(v_codes, "v_codes", torch.uint8, (pages, heads, 2 * half, page // 2))
+        _dev(k_affine, "k_affine", torch.bfloat16, (pages, heads, page, 2))
+        _dev(v_affine, "v_affine", torch.bfloat16, (pages, heads, page, 2))
+        self.device = k_codes.device
+        for t in (v_codes, k_affine, v_affine):
+            if t.device != self.device:
+                raise ValueError("the cache's tensors must share a device")
+        self.k_codes, self.v_codes = k_codes, v_codes
+        self.k_affine, self.v_affine = k_affine, v_affine
+        self.pages, self.heads, self.page_size, self.head_dim = pages, heads, page, 2 * half
+        self._struct = _CacheStruct(k_codes.data_ptr(), v_codes.data_ptr(), k_affine.data_ptr(),
+                                    v_affine.data_ptr(), pages, heads, page, 2 * half)
+        self._ref = ctypes.addressof(self._struct)
+
+    @classmethod
+    def empty(cls, pages: int, heads: int, page_size: int, head_dim: int, device="cuda"):
+        affine = (pages, heads, page_size, 2)
+        return cls(torch.empty((pages, heads, page_size, head_dim // 2), dtype=torch.uint8,
+                               device=device),
+                   torch.empty((pages, heads, head_dim, page_size // 2), dtype=torch.uint8,
+                               device=device),
+                   torch.empty(affine, dtype=torch.bfloat16, device=device),
+                   torch.empty(affine, dtype=torch.bfloat16, device=device))
+
+
+_Two, _Three, _Four = ctypes.c_int64 * 2, ctypes.c_int64 * 3, ctypes.c_int * 4
+
+
+class _Call:
+    """The device and stream of one call on the cache's operators: makes the device of the
+    arguments current where it is not, checks that they share it, and tells the allocator when
+    a tensor made for the call is used on another stream than the current one."""
+
+    __slots__ = ("device", "stream", "_other", "_back")
+
+    def __init__(self, device, stream):
+        self.device = device
+        self._back = None
+        if device.index != torch.cuda.current_device():
+            self._back = torch.cuda.current_device()
+            torch.cuda.set_device(device)
+        current = torch.cuda.current_stream().cuda_stream
+        self._other = None
+        if stream is None:
+            self.stream = current
+        else:
+            self.stream = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+            if self.stream != current:
+                self._other = (stream if hasattr(stream, "cuda_stream")
+                               else torch.cuda.ExternalStream(self.stream))
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        if self._back is not None:
+            torch.cuda.set_device(self._back)
+
+    def ptr(self, t, name, dtype=None, shape=None):
+        """A contiguous CUDA tensor of the call's device (None: a null pointer)."""
+        if t is None:
+            return None
+        p = _dev(t, name, dtype, shape)
+        if t.device != self.device:
+            raise ValueError("the CUDA tensors of one call must share a device (%s, %s)"
+                             % (self.device, t.device))
+        return p
+
+    def rows(self, t, name, dtype, shape, kind):
+        """A CUDA tensor whose last axis is contiguous: (pointer, leading strides)."""
+        if not t.is_cuda or t.device != self.device:
+            raise ValueError("%s must be a CUDA tensor on %s" % (name, self.device))
+        if t.dtype != dtype:
+            raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+        if tuple(t.shape) != tuple(shape):
+            raise ValueError("%s must have shape %s, got %s"
+                             % (name, tuple(shape), tuple(t.shape)))
+        st = t.stride()
+        if st[-1] != 1:
+            raise ValueError("the channels of %s must be contiguous" % name)
+        # the stride of an axis of one is never taken
+        return t.data_ptr(), kind(*[x if m > 1 else 0 for x, m in zip(st, t.shape[:-1])])
+
+    def made(self, shape, dtype):
+        t = torch.empty(shape, dtype=dtype, device=self.device)
+        if self._other is not None:
+            # The memory may still be in use by work queued on the current stream.
+            self._other.wait_stream(torch.cuda.current_stream())
+            t.record_stream(self._other)
+        return t
+
+
+def _cuda_device(t, name):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError("%s must be a CUDA tensor" % name)
+    return t.device
+
+
+def fdllm_qk_norm_rope(q: torch.Tensor, k: torch.Tensor | None, positions: torch.Tensor,
+                       inv_freq: torch.Tensor, q_weight=None, k_weight=None, eps: float = 1e-6,
+                       sections=None, interleaved: bool = False, out_q=None, out_k=None,
+                       stream=None):
+    """Per-head RMS norm and rotary positions of queries and keys in one pass.
+
+    ``q`` [T, Hq, D] and ``k`` [T, Hk, D] (or None), bf16/fp16/fp32, channels contiguous (rows
+    of a packed projection are taken where they lie); ``positions`` int32 [T] or [axes, T];
+    ``inv_freq`` a CPU float64 tensor of the pairs' frequencies in radians per position;
+    ``sections`` the pairs of each axis; a weight of None skips that tensor's norm.
+    ``out_q`` / ``out_k`` may be q / k themselves where those are contiguous.  Returns
+    (out_q, out_k)."""
+    with _Call(_cuda_device(q, "q"), stream) as c:
+        if q.dim() != 3:
+            raise ValueError("q must be [T, Hq, D]")
+        T, Hq, D = q.shape
+        qp, qs = c.rows(q, "q", q.dtype, (T, Hq, D), _Two)
+        Hk, kp, ks = 0, None, None
+        if k is not None:
+            Hk = k.shape[1] if k.dim() == 3 else -1
+            kp, ks = c.rows(k, "k", q.dtype, (T, Hk, D), _Two)
+        axes = 1 if positions.dim() == 1 else positions.shape[0]
+        pp = c.ptr(positions, "positions", torch.int32, (T,) if positions.dim() == 1 else (axes, T))
+        if inv_freq.is_cuda or inv_freq.dtype != torch.float64 or not inv_freq.is_contiguous():
+            raise ValueError("inv_freq must be a contiguous CPU float64 tensor")
+        if sections is not None and (len(sections) != axes or axes > 4):
+            raise ValueError("sections must name the pairs of each of %d axes (at most 4)" % axes)
+        if out_q is None:
+            out_q = c.made((T, Hq, D), q.dtype)
+        if out_k is None and k is not None:
+            out_k = c.made((T, Hk, D), q.dtype)
+        st = _load().fdllm_qk_norm_rope(
+            qp, qs, kp, ks, _dtype_code(q), T, Hq, Hk, D,
+            c.ptr(q_weight, "q_weight", q.dtype, (D,)), c.ptr(k_weight, "k_weight", q.dtype, (D,)),
+            eps, pp, axes, None if sections is None else _Four(*sections), inv_freq.data_ptr(),
+            inv_freq.numel(), 1 if interleaved else 0, c.ptr(out_q, "out_q", q.dtype, (T, Hq, D)),
+            None if k is None else c.ptr(out_k, "out_k", q.dtype, (T, Hk, D)), c.stream)
+        _check(st, "fdllm_qk_norm_rope")
+        return out_q, out_k
+
+
+def _table(c, cache, table, name="block_table"):
+    if table.dim() != 2:
+        raise ValueError("%s must be [B, max_pages]" % name)
+    if cache.device != c.device:
+        raise ValueError("the cache must be on %s" % c.device)
+    return c.ptr(table, name, torch.int32), table.shape[0], table.shape[1]
+
+
+def fdllm_cache_append(cache: KvCache, block_table: torch.Tensor, start, k: torch.Tensor,
+                       v: torch.Tensor, count=None, stream=None):
+    """Write k, v [B, n, heads, D] (bf16/fp16/fp32, channels contiguous) into slots
+    start[b] .. start[b] + count[b] - 1 (int32 [B] each; None: 0 and n)."""
+    with _Call(_cuda_device(k, "k"), stream) as c:
+        tp, B, mp = _table(c, cache, block_table)
+        n = k.shape[1] if k.dim() == 4 else -1
+        shape = (B, n, cache.heads, cache.head_dim)
+        kp, ks = c.rows(k, "k", k.dtype, shape, _Three)
+        vp, vs = c.rows(v, "v", k.dtype, shape, _Three)
+        st = _load().fdllm_cache_append(cache._ref, tp, B, mp,
+                                        c.ptr(start, "start", torch.int32, (B,)),
+                                        c.ptr(count, "count", torch.int32, (B,)), kp, ks, vp, vs,
+                                        _dtype_code(k), n, c.stream)
+        _check(st, "fdllm_cache_append")
+
+
+def fdllm_cache_read(cache: KvCache, block_table: torch.Tensor, start, n: int,
+                     dtype=torch.bfloat16, count=None, out_k=None, out_v=None, stream=None):
+    """Slots start[b] .. start[b] + n - 1 as dense rows (out_k, out_v) [B, n, heads, D] of
+    ``dtype``; rows from count[b] on are zero."""
+    with _Call(_cuda_device(block_table, "block_table"), stream) as c:
+        tp, B, mp = _table(c, cache, block_table)
+        shape = (B, n, cache.heads, cache.head_dim)
+        if out_k is None:
+            out_k = c.made(shape, dtype)
+        if out_v is None:
+            out_v = c.made(shape, dtype)
+        st = _load().fdllm_cache_read(cache._ref, tp, B, mp,
+                                      c.ptr(start, "start", torch.int32, (B,)),
+                                      c.ptr(count, "count", torch.int32, (B,)),
+                                      c.ptr(out_k, "out_k", dtype, shape),
+                                      c.ptr(out_v, "out_v", dtype, shape), _dtype_code(out_k), n,
+                                      c.stream)
+        _check(st, "fdllm_cache_read")
+        return out_k, out_v
+
+
+def fdllm_cache_attention_workspace_bytes(B: int, Lq: int, Hq: int, heads: int,
+                                          head_dim: int) -> int:
+    return int(_load().fdllm_cache_attention_workspace_bytes(B, Lq, Hq, heads, head_dim))
+
+
+def _queries(c, q, cache):
+    if q.dim() != 4:
+        raise ValueError("q must be [B, Lq, Hq, D]")
+    if q.dtype not in (torch.bfloat16, torch.float16):
+        raise TypeError("q must be bfloat16 or float16, got %s" % q.dtype)
+    B, Lq, Hq, D = q.shape
+    qp, qs = c.rows(q, "q", q.dtype, (B, Lq, Hq, cache.head_dim), _Three)
+    return qp, qs, B, Lq, Hq
+
+
+def fdllm_cache_attention(q: torch.Tensor, cache: KvCache, block_table: torch.Tensor,
+                          cache_lens: torch.Tensor, k_new=None, v_new=None, new_lens=None,
+                          causal: bool = False, scale: float | None = None, out=None,
+                          return_lse: bool = False, out_lse=None, workspace=None, stream=None):
+    """Attention of ``q`` [B, Lq, Hq, D] (bf16/fp16) over the first cache_lens[b] slots of the
+    cache and the block's own ``k_new``, ``v_new`` [B, Ln, heads, D].  ``scale`` None: D^-0.5.
+    ``workspace`` a uint8 CUDA tensor of fdllm_cache_attention_workspace_bytes bytes (None:
+    allocated for the call; pass one under stream capture by another library).  Returns out, or
+    (out, lse fp32 [B, Lq, Hq]) with ``return_lse``."""
+    with _Call(_cuda_device(q, "q"), stream) as c:
+        tp, tb, mp = _table(c, cache, block_table)
+        qp, qs, B, Lq, Hq = _queries(c, q, cache)
+        if tb != B:
+            raise ValueError("block_table must have %d rows, got %d" % (B, tb))
+        Ln, kp, ks, vp, vs = 0, None, None, None, None
+        if (k_new is None) != (v_new is None):
+            raise ValueError("k_new and v_new go together")
+        if k_new is not None:
+            Ln = k_new.shape[1] if k_new.dim() == 4 else -1
+            shape = (B, Ln, cache.heads, cache.head_dim)
+            kp, ks = c.rows(k_new, "k_new", q.dtype, shape, _Three)
+            vp, vs = c.rows(v_new, "v_new", q.dtype, shape, _Three)
+        if out is None:
+            out = c.made((B, Lq, Hq, cache.head_dim), q.dtype)
+        if out_lse is None and return_lse:
+            out_lse = c.made((B, Lq, Hq), torch.float32)
+        lib = _load()
+        if workspace is None:
+            need = lib.fdllm_cache_attention_workspace_bytes(B, Lq, Hq, cache.heads,
+                                                             cache.head_dim)
+            workspace = c.made((max(need, 256),), torch.uint8)
+        st = lib.fdllm_cache_attention(
+            qp, qs, _dtype_code(q), B, Lq, Hq, cache._ref, tp, mp,
+            c.ptr(cache_lens, "cache_lens", torch.int32, (B,)), kp, ks, vp, vs, Ln,
+            c.ptr(new_lens, "new_lens", torch.int32, (B,)), 1 if causal else 0,
+            cache.head_dim ** -0.5 if scale is None else scale,
+            c.ptr(out, "out", q.dtype, (B, Lq, Hq, cache.head_dim)),
+            c.ptr(out_lse, "out_lse", torch.float32, (B, Lq, Hq)),
+            c.ptr(workspace, "workspace", torch.uint8), workspace.numel(), c.stream)
+        _check(st, "fdllm_cache_attention")
+        return (out, out_lse) if return_lse else out
+
+
+def fdllm_cache_key_weights(q: torch.Tensor, lse: torch.Tensor, cache: KvCache,
+                            block_table: torch.Tensor, cache_lens: torch.Tensor, weights=None,
+                            scale: float | None = None, max_len: int | None = None, out=None,
+                            stream=None):
+    """The attention each cached key receives from ``q`` given attention's ``lse`` [B, Lq, Hq],
+    added to ``weights`` fp32 [B, heads, max_len] (None: from zero, ``max_len`` slots or the
+    table's).  ``out`` may be ``weights``.  Returns the sums (0 behind cache_lens)."""
+    with _Call(_cuda_device(q, "q"), stream) as c:
+        tp, tb, mp = _table(c, cache, block_table)
+        qp, qs, B, Lq, Hq = _queries(c, q, cache)
+        if tb != B:
+            raise ValueError("block_table must have %d rows, got %d" % (B, tb))
+        if weights is not None:
+            max_len = weights.shape[-1]
+        elif max_len is None:
+            max_len = mp * cache.page_size
+        shape = (B, cache.heads, max_len)
+        if out is None:
+            out = c.made(shape, torch.float32)
+        st = _load().fdllm_cache_key_weights(
+            qp, qs, _dtype_code(q), B, Lq, Hq, cache._ref, tp, mp,
+            c.ptr(cache_lens, "cache_lens", torch.int32, (B,)),
+            c.ptr(lse, "lse", torch.float32, (B, Lq, Hq)),
+            cache.head_dim ** -0.5 if scale is None else scale,
+            c.ptr(weights, "weights", torch.float32, shape),
+            c.ptr(out, "out", torch.float32, shape), max_len, c.stream)
+        _check(st, "fdllm_cache_key_weights")
+        return out
+
+
+def fdllm_cache_evict(cache: KvCache, block_table: torch.Tensor, cache_lens: torch.Tensor,
+                      weights: torch.Tensor, budget: int, dst_table: torch.Tensor,
+                      keep_first: int = 0, keep_last: int = 0, out_lens=None, out_weights=None,
+                      out_index=None, stream=None):
+    """Copy the ``budget`` heaviest keys of each sequence and head (the first ``keep_first`` and
+    the last ``keep_last`` slots always) into the pages of ``dst_table`` [B, dst_max_pages],
+    in slot order.  Returns (lens int32 [B], weights fp32 [B, heads, budget], the slots they
+    came from int32 [B, heads, budget])."""
+    with _Call(_cuda_device(weights, "weights"), stream) as c:
+        tp, B, mp = _table(c, cache, block_table)
+        dp, db, dmp = _table(c, cache, dst_table, "dst_table")
+        if db != B:
+            raise ValueError("dst_table must have %d rows, got %d" % (B, db))
+        max_len = weights.shape[-1]
+        shape = (B, cache.heads, budget)
+        if out_lens is None:
+            out_lens = c.made((B,), torch.int32)
+        if out_weights is None:
+            out_weights = c.made(shape, torch.float32)
+        if out_index is None:
+            out_index = c.made(shape, torch.int32)
+        st = _load().fdllm_cache_evict(
+            cache._ref, tp, B, mp, c.ptr(cache_lens, "cache_lens", torch.int32, (B,)),
+            c.ptr(weights, "weights", torch.float32, (B, cache.heads, max_len)), max_len, budget,
+            keep_first, keep_last, dp, dmp, c.ptr(out_lens, "out_lens", torch.int32, (B,)),
+            c.ptr(out_weights, "out_weights", torch.float32, shape),
+            c.ptr(out_index, "out_index", torch.int32, shape), c.stream)
+        _check(st, "fdllm_cache_evict")
+        return out_lens, out_weights, out_index
 
 
 def fdllm_check_bounded_wait(seconds: float = 0.01, stream=None) -> int:
