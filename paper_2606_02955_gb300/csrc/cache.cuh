@@ -63,6 +63,10 @@ inline bool check_table(const int32_t *table, int B, int max_pages, int page_shi
            ((int64_t)max_pages << page_shift) < ((int64_t)1 << 30);
 }
 
+// fdllm_cache_attention's and fdllm_cache_key_weights' queries (defined with the former).
+bool check_queries(const void *q, const int64_t *strides, int dtype, int B, int Lq, int Hq,
+                   int heads);
+
 // A base and its strides as 16-byte vectors need them.
 inline bool aligned16(const void *p, const int64_t *strides, int n, int esize)
 {

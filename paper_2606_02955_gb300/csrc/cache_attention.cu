@@ -1,11 +1,45 @@
-// cache_attention.cu -- fdllm_cache_attention and fdllm_cache_key_weights: a block's queries
-// over the 4-bit prefix cache and the block's own keys.
+// cache_attention.cu -- fdllm_cache_attention: a block's queries over the 4-bit prefix cache
+// and the block's own keys, on the fifth-generation tensor cores.
+//
+// Mathematics.  With k_j = ko_j + ks_j u_j (u_j the codes minus 8, ko_j the middle of the range)
+// and likewise v_j, for the rows r of one key/value head (queries x heads of the group):
+//   s_rj = scale (ks_j (q_r . u_j) + ko_j sum(q_r)),
+//   out_r = (sum_j p_rj vs_j w_j + sum_j p_rj vo_j) / sum_j p_rj,   p_rj = e^(s_rj - m_r).
+// The tensor cores see the codes themselves, exact in bf16 and fp16; scales and offsets act on
+// the scores and the weights.
+//
+// Layout.  A tile is 128 keys.  Both products are taken transposed, with the unpacked codes as
+// the A operand in tensor memory, so that the codes go from registers straight to the tensor
+// core and never back through shared memory:
+//   S^T [128 keys x N rows]      = K [keys x D] . Q^T       (a thread holds one key's scores)
+//   O^T [128 channels x N rows] += V^T [channels x keys] . P^T
+// A key's scale and offset are then scalars of the thread that holds its scores, and V's codes
+// are stored channel-major so that a thread unpacks one channel.  P^T is the only operand
+// written to shared memory by threads (16-byte stores, rows contiguous).
+//
+// A row's running maximum lags: the reference of a row moves only when a weight leaves the
+// range that fp16 and fp32 hold (kTopWeight), which one vote a tile decides.  Weights are
+// scaled by the cached row's scale before they are rounded to fp16; c[r] keeps their largest
+// near 1 whatever the scales are.
+//
+// Split.  The tiles of all (sequence, head, row tile) units in order are cut into equal ranges,
+// one to a CTA (the lengths are read on the device); a unit that crosses a CTA's end leaves
+// fp32 partials, joined by combine_kernel in tile order.
 #include <cuda_runtime.h>
 
+#include <type_traits>
+
 #include "cache.cuh"
+#include "cache_tc.cuh"
 
 namespace fdllm {
 namespace {
+
+constexpr int kKeys = 128;                // keys of a tile
+constexpr float kFar = -1e30f;            // reference of a row that has seen no key
+constexpr float kTopWeight = 16384.0f;    // largest weight (fp16 holds 65504)
+constexpr float kTopShift = 90.0f;        // a score this far above its reference may overflow
+constexpr float kMaxShift = 120.0f;       // c = 2^(ref - refz) stays below 2^120
 
 struct AttnArgs {
     CacheView c;
@@ -14,19 +48,53 @@ struct AttnArgs {
     const int32_t *lens;      // [B]
     const void *q;            // [B, Lq, Hq, D]
     Strides3 qs;
-    int Lq, Hq, group;        // group = Hq / heads
+    int B, Lq, Hq, group;     // group = Hq / heads
     const void *k_new;        // [B, Ln, heads, D]
     const void *v_new;
     Strides3 ks, vs;
     int Ln;
     const int32_t *new_lens;  // [B] or null
     int causal;
-    float scale;
+    float scale;              // times log2(e)
     void *out;                // [B, Lq, Hq, D]
     float *lse;               // [B, Lq, Hq] or null
+    int rows;                 // Lq * group
+    int row_tiles;            // ceil(rows / N)
+    float *parts;             // [grid][2][N][D] accumulators, at the row's reference
+    float *part_refs;         // [grid][2][N][2] (reference, sum)
+    int32_t *meta;            // [grid][kMeta]
 };
 
-// A sequence's cached length, or -1 where it is out of range.
+// meta of a CTA: whether it starts a unit that it does not finish (slot 1) and which, whether
+// it continues a unit begun before (slot 0) and whether that ends here.
+enum { kOpen = 0, kOpenB, kOpenUnit, kCont, kContEnds, kMeta = 8 };
+
+template <int D_, int N_>
+struct Shape {
+    static constexpr int D = D_;
+    static constexpr int N = N_;                       // rows of a row tile
+    static constexpr int C = N >= 64 ? 4 : 2;          // warpgroups sharing a tile's columns
+    static constexpr int cols = N / C;                 // columns (rows of the problem) a thread
+    static constexpr int warps = 4 * C;                // worker warps
+    static constexpr int workers = 32 * warps;
+    static constexpr int threads = workers + 64;       // the loading and the issuing warp
+    static constexpr int ctas = N >= 64 ? 1 : 2;       // CTAs an SM holds
+    static constexpr int stages = N >= 64 ? 6 : 4;
+    static constexpr int code_bytes = kKeys * D / 2;   // of keys, or of values
+    static constexpr int stage_bytes = 2 * code_bytes + 1024;
+    static constexpr int q_bytes = N * D * 2;
+    static constexpr int q_off = stages * stage_bytes;
+    static constexpr int p_off = q_off + 2 * q_bytes;
+    static constexpr int lo_off = p_off + kKeys * N * 2;
+    static constexpr int smem = lo_off + kKeys * N * 2 + 1024;  // and room to align the base
+    // tensor memory columns
+    static constexpr int tK = 0, tV = 64, tS = 128, tO = 128 + 2 * N;
+    static constexpr int tmem = tO + N <= 256 ? 256 : 512;
+    static_assert(tO + N <= tmem && ctas * tmem <= 512, "tensor memory");
+};
+
+__device__ uint32_t g_status;  // sticky: a bounded wait gave up
+
 __device__ __forceinline__ int cached_len(const CacheView &c, const int32_t *lens, int max_pages,
                                           int b)
 {
@@ -34,176 +102,937 @@ __device__ __forceinline__ int cached_len(const CacheView &c, const int32_t *len
     return n >= 0 && n <= (max_pages << c.page_shift) ? n : -1;
 }
 
-constexpr int kKeys = 128;  // keys of a step: one thread to a key
-
-__device__ __forceinline__ float block_max(float x, float *red)
-{
-#pragma unroll
-    for (int m = 16; m > 0; m >>= 1)
-        x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, m));
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0)
-        red[threadIdx.x >> 5] = x;
-    __syncthreads();
-    return fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-}
-
-// One CTA to a query row: thread = key for the scores, thread = channel for the sum.
-template <typename T, int D>
-__global__ void __launch_bounds__(kKeys) attention_kernel(const __grid_constant__ AttnArgs a)
-{
-    __shared__ float q[D], p[kKeys], red[4];
-    __shared__ int bad;
-    pdl_wait();
-    const int i = blockIdx.x, hq = blockIdx.y, b = blockIdx.z, h = hq / a.group;
-    const T *qr = static_cast<const T *>(a.q) + b * a.qs.batch + i * a.qs.token + hq * a.qs.head;
-    if (threadIdx.x < D)
-        q[threadIdx.x] = to_float(qr[threadIdx.x]);
-    if (threadIdx.x == 0)
-        bad = 0;
-    __syncthreads();
-    const int n = cached_len(a.c, a.lens, a.max_pages, b);
-    const int own = a.new_lens ? a.new_lens[b] : a.Ln;
-    const bool wrong = n < 0 || own < 0 || own > a.Ln;
-    const int seen = wrong ? 0 : (a.causal ? min(own, i + 1) : own);
-    const int cached = max(n, 0);
-    const int pieces = (cached + kKeys - 1) / kKeys;
-    const int total = wrong ? 0 : pieces + (seen + kKeys - 1) / kKeys;
-    float m = neg_inf_f(), l = 0.0f, o = 0.0f;
-    const int d = threadIdx.x;
-    for (int t = 0; t < total; ++t) {
-        const bool in_cache = t < pieces;
-        const int j0 = in_cache ? t * kKeys : (t - pieces) * kKeys;
-        const int j = j0 + threadIdx.x;
-        const int end = in_cache ? cached : seen;
-        float s = neg_inf_f();
-        if (j < end) {
-            float x = 0.0f;
-            if (in_cache) {
-                const int pg = page_of(a.c, a.table, a.max_pages, b, j);
-                if (pg < 0) {
-                    bad = 1;
-                } else {
-                    const int64_t at = slot_index(a.c, pg, h, j);
-                    const uint8_t *k = a.c.kc + at * (D / 2);
-                    const uint32_t f = a.c.ka[at];
-                    for (int e = 0; e < D / 2; ++e) {
-                        x += q[2 * e] * fmaf(bf16_low(f), (float)(k[e] & 15), bf16_high(f));
-                        x += q[2 * e + 1] * fmaf(bf16_low(f), (float)(k[e] >> 4), bf16_high(f));
-                    }
-                }
-            } else {
-                const T *k = static_cast<const T *>(a.k_new) + b * a.ks.batch + j * a.ks.token +
-                             h * a.ks.head;
-                for (int e = 0; e < D; ++e)
-                    x += q[e] * to_float(k[e]);
-            }
-            s = x * a.scale;
-        }
-        const float top = fmaxf(m, block_max(s, red));
-        const float w = j < end ? exp2f((s - top) * kLog2e) : 0.0f;
-        __syncthreads();
-        p[threadIdx.x] = w;
-        __syncthreads();
-        const float c = m == neg_inf_f() ? 0.0f : exp2f((m - top) * kLog2e);
-        m = top;
-        l *= c;
-        o *= c;
-        const int cnt = min(end - j0, kKeys);
-        for (int e = 0; e < cnt; ++e) {
-            l += p[e];
-            if (d < D) {
-                float v = 0.0f;
-                if (in_cache) {
-                    const int pg = page_of(a.c, a.table, a.max_pages, b, j0 + e);
-                    if (pg >= 0) {
-                        const uint32_t f = a.c.va[slot_index(a.c, pg, h, j0 + e)];
-                        const uint32_t byte = a.c.vc[v_byte(a.c, pg, h, d, j0 + e)];
-                        v = fmaf(bf16_low(f), (float)((byte >> (4 * ((j0 + e) & 1))) & 15u),
-                                 bf16_high(f));
-                    }
-                } else {
-                    v = to_float(static_cast<const T *>(a.v_new)[b * a.vs.batch +
-                                                                 (j0 + e) * a.vs.token +
-                                                                 h * a.vs.head + d]);
-                }
-                o = fmaf(p[e], v, o);
-            }
-        }
-    }
-    __syncthreads();
-    const bool poison = wrong || bad != 0;
-    const int64_t row = ((int64_t)b * a.Lq + i) * a.Hq + hq;
-    if (d < D)
-        static_cast<T *>(a.out)[row * D + d] =
-            from_float<T>(poison ? nan_f() : (total ? o / l : 0.0f));
-    if (d == 0 && a.lse)
-        a.lse[row] = poison ? nan_f() : (total ? m + logf(l) : neg_inf_f());
-}
-
-struct WeighArgs {
-    CacheView c;
-    const int32_t *table;
-    int max_pages;
-    const int32_t *lens;
-    const void *q;
-    Strides3 qs;
-    int Lq, Hq, group;
-    const float *lse;         // [B, Lq, Hq]
-    float scale;
-    const float *in;          // [B, heads, max_len] or null
-    float *out;
-    int max_len;
+// One sequence's share of the work.
+struct Sequence {
+    int cached;    // cached keys
+    int own;       // own keys
+    int ct;        // tiles of cached keys
+    int tiles;     // all tiles, at least 1
+    bool wrong;    // a length out of range
 };
 
-// One thread to a key.
-template <typename T, int D>
-__global__ void __launch_bounds__(kKeys) weigh_kernel(const __grid_constant__ WeighArgs a)
+__device__ __forceinline__ Sequence sequence_of(const AttnArgs &a, int b)
 {
-    __shared__ float q[D];
-    pdl_wait();
-    const int j = blockIdx.x * kKeys + threadIdx.x, h = blockIdx.y, b = blockIdx.z;
-    int n = cached_len(a.c, a.lens, a.max_pages, b);
-    if (n > a.max_len)
-        n = -1;
-    const int pg = j < n ? page_of(a.c, a.table, a.max_pages, b, j) : -1;
-    float k[D];
-    if (pg >= 0) {
-        const int64_t at = slot_index(a.c, pg, h, j);
-        const uint32_t f = a.c.ka[at];
-        for (int e = 0; e < D / 2; ++e) {
-            const uint32_t w = a.c.kc[at * (D / 2) + e];
-            k[2 * e] = fmaf(bf16_low(f), (float)(w & 15), bf16_high(f));
-            k[2 * e + 1] = fmaf(bf16_low(f), (float)(w >> 4), bf16_high(f));
-        }
-    }
-    float sum = 0.0f;
-    for (int r = 0; r < a.Lq * a.group; ++r) {
-        const int i = r / a.group, hq = h * a.group + r % a.group;
-        __syncthreads();
-        if (threadIdx.x < D)
-            q[threadIdx.x] = to_float(static_cast<const T *>(
-                a.q)[b * a.qs.batch + i * a.qs.token + hq * a.qs.head + threadIdx.x]);
-        __syncthreads();
-        const float lse = a.lse[((int64_t)b * a.Lq + i) * a.Hq + hq];
-        if (pg >= 0 && lse != neg_inf_f()) {
-            float x = 0.0f;
+    Sequence s;
+    const int n = cached_len(a.c, a.lens, a.max_pages, b);
+    const int own = a.new_lens ? a.new_lens[b] : a.Ln;
+    s.wrong = n < 0 || own < 0 || own > a.Ln;
+    s.cached = s.wrong ? 0 : n;
+    s.own = s.wrong ? 0 : own;
+    s.ct = (s.cached + kKeys - 1) / kKeys;
+    s.tiles = max(1, s.ct + (s.own + kKeys - 1) / kKeys);
+    return s;
+}
+
+// 32 own values of one channel, keys x0 .. x0 + 31, as pairs in the operand's order; keys from
+// `end` on are 0.  A non-finite value must not meet the zero weights of the rows that do not
+// see it: it is taken out, and the first such key returned for the rows that do.
+template <typename T>
+__device__ __noinline__ int own_values(const uint16_t *v, int64_t step, int x0, int end,
+                                       uint32_t (&y)[16])
+{
+    constexpr uint32_t kExp = std::is_same<T, __half>::value ? 0x7C00u : 0x7F80u;
+    int bad = 0x7FFFFFFF;
 #pragma unroll
-            for (int e = 0; e < D; ++e)
-                x += q[e] * k[e];
-            sum += exp2f((x * a.scale - lse) * kLog2e);
+    for (int e = 0; e < 16; ++e) {
+        const int x = x0 + (e >> 2) * 8 + (e & 3);  // and four further on
+        uint32_t lo = x < end ? v[(int64_t)x * step] : 0u;
+        uint32_t hi = x + 4 < end ? v[(int64_t)(x + 4) * step] : 0u;
+        if ((lo & kExp) == kExp)
+            bad = min(bad, x), lo = 0;
+        if ((hi & kExp) == kExp)
+            bad = min(bad, x + 4), hi = 0;
+        y[e] = lo | (hi << 16);
+    }
+    return bad;
+}
+
+// A CTA's walk over its range of tiles, segment by segment (a segment: tiles of one unit).
+struct Walk {
+    int64_t at, end;    // tiles of the whole call
+    int64_t base;       // first tile of sequence b
+    int b;
+    Sequence s;
+    int unit;           // head * row_tiles + row tile
+    int first, last;    // the segment's tiles [first, last) of the unit
+
+    __device__ bool next(const AttnArgs &a, int units)
+    {
+        if (at >= end)
+            return false;
+        while (at >= base + (int64_t)s.tiles * units) {
+            base += (int64_t)s.tiles * units;
+            s = sequence_of(a, ++b);
+        }
+        const int64_t local = at - base;
+        unit = (int)(local / s.tiles);
+        first = (int)(local - (int64_t)unit * s.tiles);
+        last = (int)min((int64_t)s.tiles, first + (end - at));
+        at += last - first;
+        return true;
+    }
+};
+
+// What a segment's warps need to know of it, left in shared memory by the loading warp.
+struct Segment {
+    int b, unit, h, r0, rows;  // sequence; head * row_tiles + row tile; head; rows r0 ...
+    int first, last;           // tiles of the unit that hold keys, [first, last)
+    int ct, cached, own;
+    int starts, ends;          // the unit's first tile, its last
+    int wrong;
+    int done;                  // no segment: the walk is over
+};
+
+template <typename S, typename T>
+__global__ void __launch_bounds__(S::threads, S::ctas)
+    attention_kernel(const __grid_constant__ AttnArgs a,
+                     const __grid_constant__ CUtensorMap k_map,
+                     const __grid_constant__ CUtensorMap v_map)
+{
+    constexpr int D = S::D, N = S::N, kCols = S::cols;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
+    __shared__ __align__(8) uint64_t full[S::stages], empty[S::stages];  // the ring of codes
+    __shared__ __align__(8) uint64_t q_full[2], q_empty[2];              // queries, segments
+    __shared__ __align__(8) uint64_t k_ready, s_done, p_ready, o_done, voted;
+    __shared__ uint32_t tmem_base;
+    __shared__ uint8_t stage_bad[S::stages];
+    __shared__ int64_t scan[S::threads / 32];
+    __shared__ int64_t find_base;
+    __shared__ int find_b;
+    __shared__ Segment segs[2];
+    __shared__ uint32_t vote[2];
+    __shared__ __align__(16) float sumq[2][N];  // of the queries' channels
+    // per row: the reference (negated), 2^(ref - refz), the reference of the scaled weights
+    __shared__ __align__(16) float nref[N], cmul[N], refz[N];
+    __shared__ __align__(16) float fl[N], fo[N], redo[N];
+    __shared__ float wred[S::warps][2][kCols];
+    __shared__ int first_bad[D];  // first own key of the segment with a non-finite value
+    __shared__ int any_bad;
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (tid == 0) {
+        for (int i = 0; i < S::stages; ++i) {
+            mbar_init(&full[i], 1);
+            mbar_init(&empty[i], S::warps);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&q_full[i], 1);
+            mbar_init(&q_empty[i], S::warps + 1);
+            vote[i] = 0;
+        }
+        mbar_init(&k_ready, S::warps);
+        mbar_init(&s_done, 1);
+        mbar_init(&p_ready, S::warps);
+        mbar_init(&o_done, 1);
+        mbar_init(&voted, S::warps);
+        fence_mbar_init();
+    }
+    if (warp == S::warps)
+        tc::tmem_alloc(&tmem_base, S::tmem);
+    if (tid == S::workers + 32) {
+        tc::prefetch_tensormap(&k_map);
+        tc::prefetch_tensormap(&v_map);
+    }
+    pdl_wait();
+
+    // The call's tiles, and the sequence in which this CTA's range begins: every thread sums a
+    // run of sequences, a scan over the CTA gives the runs' places.
+    const int units = a.c.heads * a.row_tiles;
+    Walk w;
+    {
+        const int run = (a.B + S::threads - 1) / S::threads;
+        const int b0 = min(a.B, tid * run), b1 = min(a.B, b0 + run);
+        int64_t mine = 0;
+        for (int b = b0; b < b1; ++b)
+            mine += sequence_of(a, b).tiles;
+        int64_t upto = mine;
+#pragma unroll
+        for (int m = 1; m < 32; m <<= 1) {
+            const int64_t o = __shfl_up_sync(0xFFFFFFFFu, upto, m);
+            upto += lane >= m ? o : 0;
+        }
+        if (lane == 31)
+            scan[warp] = upto;
+        __syncthreads();
+        int64_t before = 0, total = 0;
+        for (int i = 0; i < S::threads / 32; ++i) {
+            before += i < warp ? scan[i] : 0;
+            total += scan[i];
+        }
+        total *= units;
+        const int64_t p0 = (before + upto - mine) * units;
+        w.at = total * blockIdx.x / gridDim.x;
+        w.end = total * (blockIdx.x + 1) / gridDim.x;
+        if (b0 < b1 && w.at >= p0 && w.at < p0 + mine * units) {
+            find_base = p0;
+            find_b = b0;
         }
     }
-    if (j < a.max_len) {
-        const int64_t at = ((int64_t)b * a.c.heads + h) * a.max_len + j;
-        float y = 0.0f;
-        if (n < 0 || (j < n && pg < 0))
-            y = nan_f();
-        else if (j < n)
-            y = (a.in ? a.in[at] : 0.0f) + sum;
-        a.out[at] = y;
+    int32_t *meta = a.meta + (int64_t)blockIdx.x * kMeta;
+    if (tid < kMeta)
+        meta[tid] = 0;
+    tc::fence_before_sync();
+    __syncthreads();
+    tc::fence_after_sync();
+    const uint32_t tmem = tmem_base;
+    pdl_launch_dependents();
+
+    bool dead = false;  // a wait gave up: no further wait, the walk goes on to its end
+    auto wait = [&](uint64_t *bar, uint32_t parity) {
+        if (!dead && !mbar_wait_short(bar, parity, &g_status))
+            dead = true;
+    };
+
+    if (warp == S::warps) {
+        // ---------------------------------------------------------------- the loading warp
+        if (w.at < w.end) {
+            w.b = find_b;
+            w.base = find_base;
+            w.s = sequence_of(a, w.b);
+        }
+        uint32_t ring = 0;  // cached tiles so far: stage ring % stages, phase ring / stages
+        for (uint32_t seg = 0;; ++seg) {
+            const uint32_t sb = seg & 1;
+            const bool more = w.next(a, units);
+            wait(&q_empty[sb], ((seg >> 1) & 1) ^ 1);
+            const int h = more ? w.unit / a.row_tiles : 0;
+            const int r0 = more ? (w.unit - h * a.row_tiles) * N : 0;
+            const int rows = min(N, a.rows - r0);
+            if (lane == 0) {
+                Segment &g = segs[sb];
+                g.done = !more;
+                if (more) {
+                    g.b = w.b, g.unit = w.unit, g.h = h, g.r0 = r0, g.rows = rows;
+                    // an empty unit's one tile holds no key
+                    g.first = w.first;
+                    g.last = min(w.last, w.s.ct + (w.s.own + kKeys - 1) / kKeys);
+                    g.ct = w.s.ct, g.cached = w.s.cached, g.own = w.s.own;
+                    g.starts = w.first == 0, g.ends = w.last == w.s.tiles;
+                    g.wrong = w.s.wrong;
+                }
+            }
+            if (!more) {
+                __syncwarp();
+                if (lane == 0)
+                    mbar_arrive(&q_full[sb]);
+                break;
+            }
+            // Queries into shared memory (K-major, 128-byte swizzle), and their sums.
+            uint8_t *q_smem = smem + S::q_off + sb * S::q_bytes;
+#pragma unroll 4
+            for (int i = lane; i < N * (D / 8); i += 32) {
+                const int n = i / (D / 8), c8 = i % (D / 8);
+                uint4 x = make_uint4(0, 0, 0, 0);
+                if (n < rows) {
+                    const int qi = (r0 + n) / a.group, g = (r0 + n) - qi * a.group;
+                    x = *reinterpret_cast<const uint4 *>(
+                        static_cast<const T *>(a.q) + w.b * a.qs.batch + qi * a.qs.token +
+                        (int64_t)(h * a.group + g) * a.qs.head + 8 * c8);
+                }
+                const uint32_t xw[4] = {x.x, x.y, x.z, x.w};
+                float sum = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float lo, hi;
+                    unpack2<T>(xw[e], lo, hi);
+                    sum += lo + hi;
+                }
+#pragma unroll
+                for (int m = D / 16; m > 0; m >>= 1)
+                    sum += __shfl_xor_sync(0xFFFFFFFFu, sum, m);
+                if (c8 == 0)
+                    sumq[sb][n] = sum;
+                *reinterpret_cast<uint4 *>(q_smem + (c8 >> 3) * (N * 128) + n * 128 +
+                                           (((c8 & 7) ^ (n & 7)) << 4)) = interleave8(x);
+            }
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(&q_full[sb]);
+                const int page = 1 << a.c.page_shift;
+                const int span = min(page, kKeys);  // slots of a page in a tile
+                for (int t = w.first; t < min(w.last, w.s.ct); ++t, ++ring) {
+                    const uint32_t st = ring % S::stages;
+                    wait(&empty[st], ((ring / S::stages) & 1) ^ 1);
+                    uint8_t *buf = smem + st * S::stage_bytes;
+                    uint32_t bytes = 0;
+                    int pg[4];
+                    bool bad = false;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int slot = t * kKeys + i * span;
+                        pg[i] = -1;
+                        if (i * span < kKeys && slot < w.s.cached) {
+                            pg[i] = page_of(a.c, a.table, a.max_pages, w.b, slot);
+                            bad |= pg[i] < 0;
+                        }
+                        if (pg[i] >= 0)
+                            bytes += (uint32_t)span * (D + 8);
+                    }
+                    stage_bad[st] = bad;
+                    if (dead)
+                        continue;
+                    if (bytes)
+                        mbar_arrive_expect_tx(&full[st], bytes);
+                    else
+                        mbar_arrive(&full[st]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if (pg[i] < 0)
+                            continue;
+                        const int in_page = (t * kKeys + i * span) & (page - 1);
+                        const int64_t ph = (int64_t)pg[i] * a.c.heads + h;
+                        tc::tma_load_2d(buf + i * span * (D / 2), &k_map, 0,
+                                        (int)(ph * page + in_page), &full[st]);
+                        tc::tma_load_2d(buf + S::code_bytes + i * (span / 2) * D, &v_map,
+                                        in_page / 2, (int)(ph * D), &full[st]);
+                        uint8_t *aff = buf + 2 * S::code_bytes + i * span * 4;
+                        bulk_copy_g2s(aff, a.c.ka + ph * page + in_page, span * 4, &full[st]);
+                        bulk_copy_g2s(aff + 512, a.c.va + ph * page + in_page, span * 4,
+                                      &full[st]);
+                    }
+                }
+            }
+            __syncwarp();
+        }
+        // Nothing may land in this CTA's memory after it has gone: the last copies of every
+        // stage (at most one each) are waited for, with a limit.
+        if (lane == 0)
+            for (uint32_t i = 0; i < min(ring, (uint32_t)S::stages); ++i) {
+                const uint32_t r = ring - 1 - i;
+                mbar_wait_short(&full[r % S::stages], (r / S::stages) & 1, &g_status,
+                                dead ? kDrainLimitNs : kWaitLimitNs);
+            }
+    } else if (warp == S::warps + 1) {
+        // ---------------------------------------------------------------- the issuing warp
+        // S of a tile before the sums of the tile before it, so that the tensor core works on
+        // scores while the workers make weights.
+        uint32_t scores = 0, sums = 0;  // products issued so far
+        for (uint32_t seg = 0;; ++seg) {
+            const uint32_t sb = seg & 1;
+            wait(&q_full[sb], (seg >> 1) & 1);
+            const Segment g = segs[sb];
+            if (g.done)
+                break;
+            const uint8_t *q_smem = smem + S::q_off + sb * S::q_bytes;
+            const uint64_t q_desc = tc::sw128_kmajor_desc(q_smem);
+            const uint64_t p_desc = mn_desc(smem + S::p_off, 128, N * 16);
+            const uint64_t lo_desc = mn_desc(smem + S::lo_off, 128, N * 16);
+            for (int t = g.first; t <= g.last; ++t) {
+                if (t < g.last) {
+                    wait(&k_ready, scores & 1);
+                    tc::fence_after_sync();
+                    if (lane == 0) {
+#pragma unroll
+                        for (int k = 0; k < D / 16; ++k)
+                            mma_ts(tmem + S::tS + (scores & 1) * N, tmem + S::tK + 8 * k,
+                                   q_desc + (k >> 2) * ((N * 128) >> 4) + 2 * (k & 3),
+                                   idesc_f16<T>(128, N, false), k > 0);
+                        tc::commit(&s_done);
+                    }
+                    __syncwarp();
+                    ++scores;
+                }
+                if (t > g.first) {
+                    const bool own = t - 1 >= g.ct;
+                    const bool split = own || !std::is_same<T, __nv_bfloat16>::value;
+                    const uint32_t idesc =
+                        own ? idesc_f16<T>(128, N, true) : idesc_f16<__half>(128, N, true);
+                    wait(&p_ready, sums & 1);
+                    tc::fence_after_sync();
+                    if (lane == 0) {
+#pragma unroll
+                        for (int k = 0; k < kKeys / 16; ++k)
+                            mma_ts(tmem + S::tO, tmem + S::tV + 8 * k,
+                                   p_desc + k * ((2 * N * 16) >> 4), idesc,
+                                   t - 1 > g.first || k > 0);
+                        if (split)
+#pragma unroll
+                            for (int k = 0; k < kKeys / 16; ++k)
+                                mma_ts(tmem + S::tO, tmem + S::tV + 8 * k,
+                                       lo_desc + k * ((2 * N * 16) >> 4), idesc, 1);
+                        tc::commit(&o_done);
+                    }
+                    __syncwarp();
+                    ++sums;
+                }
+            }
+            if (lane == 0)
+                tc::commit(&q_empty[sb]);  // the queries are read
+            __syncwarp();
+        }
+    } else {
+        // ---------------------------------------------------------------- the workers
+        const int wg = warp >> 2, key = tid & 127;
+        const int col0 = wg * kCols;  // this thread's columns
+        const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);
+        uint8_t *p_smem = smem + S::p_off, *lo_smem = smem + S::lo_off;
+        uint32_t ring = 0;             // cached tiles so far
+        uint32_t seen = 0, summed = 0; // tiles whose scores, whose sums were taken
+        uint32_t given = 0;            // tiles whose weights were given
+        auto arrive = [&](uint64_t *bar) {
+            __syncwarp();
+            if (lane == 0)
+                mbar_arrive(bar);
+        };
+        auto sync = [&] { named_sync(1, S::workers); };
+
+        for (uint32_t seg = 0;; ++seg) {
+            const uint32_t sb = seg & 1;
+            wait(&q_full[sb], (seg >> 1) & 1);
+            const Segment &g = segs[sb];
+            if (g.done)
+                break;
+            bool poison = g.wrong != 0;
+            if (tid < D)
+                first_bad[tid] = 0x7FFFFFFF;
+            if (tid == 0)
+                any_bad = 0;
+            if (tid < N) {
+                nref[tid] = -kFar;
+                refz[tid] = kFar;
+                cmul[tid] = 1.0f;
+            }
+            sync();
+            uint64_t l2[kCols / 2], pm2[kCols / 2];
+#pragma unroll
+            for (int j = 0; j < kCols / 2; ++j)
+                l2[j] = pm2[j] = 0;
+            const int begin = g.first;
+
+            // Tiles [from, to) of the unit, all of them cached or all of them own.  A turn loads
+            // the keys of tile t + 1, whose scores are computed while the weights of tile t are
+            // made; the first turn only loads.
+            auto tiles = [&](auto own_tag, int from, int to) {
+                constexpr bool kOwn = decltype(own_tag)::value;
+                // own values: weights as a sum of two numbers of T; cached ones need a second
+                // number only for results of 11 bits
+                constexpr bool kSplit = kOwn || !std::is_same<T, __nv_bfloat16>::value;
+                using W = std::conditional_t<kOwn, T, __half>;  // weights and values
+                const int end = kOwn ? g.own : g.cached;
+                const int base = kOwn ? g.ct : 0;
+#pragma unroll 1
+                for (int t = from - 1; t < to; ++t) {
+                    const bool cur = t >= from;
+                    if (cur) {
+                        wait(&s_done, seen & 1);
+                        tc::fence_after_sync();
+                    }
+                    // tile t's scores being there, the keys' place in tensor memory is free
+                    if (t + 1 < to) {
+                        const uint32_t tK = lanes + S::tK;
+                        if constexpr (!kOwn) {
+                            const uint32_t r = ring + (cur ? 1 : 0), s1 = r % S::stages;
+                            wait(&full[s1], (r / S::stages) & 1);
+                            poison |= stage_bad[s1] != 0;
+                            const uint8_t *row = smem + s1 * S::stage_bytes + key * (D / 2);
+#pragma unroll
+                            for (int i = 0; i < D / 32; ++i)
+                                if (i * S::C / (D / 32) == wg) {
+                                    const int sw = D == 128 ? (i ^ ((key >> 1) & 3))
+                                                            : (i ^ ((key >> 2) & 1));
+                                    uint32_t y[16];
+                                    unpack32<T>(*reinterpret_cast<const uint4 *>(row + 16 * sw), y);
+                                    tmem_st16(tK + 16 * i, y);
+                                }
+                        } else {
+                            const int j = (t + 1 - base) * kKeys + key;
+                            const bool live = j < end;
+                            const T *row = static_cast<const T *>(a.k_new) + g.b * a.ks.batch +
+                                           (int64_t)(live ? j : 0) * a.ks.token +
+                                           (int64_t)g.h * a.ks.head;
+#pragma unroll
+                            for (int i = 0; i < D / 32; ++i)
+                                if (i * S::C / (D / 32) == wg) {
+                                    uint32_t y[16];
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) {
+                                        uint4 x = make_uint4(0, 0, 0, 0);
+                                        if (live)
+                                            x = *reinterpret_cast<const uint4 *>(row + 32 * i +
+                                                                                 8 * e);
+                                        x = interleave8(x);
+                                        y[4 * e] = x.x, y[4 * e + 1] = x.y;
+                                        y[4 * e + 2] = x.z, y[4 * e + 3] = x.w;
+                                    }
+                                    tmem_st16(tK + 16 * i, y);
+                                }
+                        }
+                        tmem_wait_st();
+                        tc::fence_before_sync();
+                        arrive(&k_ready);
+                    }
+                    if (!cur)
+                        continue;
+                    const uint32_t st = ring % S::stages;
+                    const uint8_t *buf = smem + st * S::stage_bytes;
+                    const uint32_t tS = lanes + S::tS + (seen & 1) * N + col0;
+                    // this thread's key: scale and middle of its range, for scores and weights
+                    const int j0 = (t - base) * kKeys, j = j0 + key;
+                    const bool masked = j0 + kKeys > end || (kOwn && a.causal);
+                    const bool valid = j < end;
+                    float ks = a.scale, ko = 0.0f, vs = 1.0f, vo = 0.0f;
+                    if constexpr (!kOwn) {
+                        const uint32_t *f =
+                            reinterpret_cast<const uint32_t *>(buf + 2 * S::code_bytes) + key;
+                        const uint32_t fk = f[0], fv = f[kKeys];
+                        ks = bf16_low(fk) * a.scale;
+                        ko = fmaf(8.0f, bf16_low(fk), bf16_high(fk)) * a.scale;
+                        vs = bf16_low(fv);
+                        vo = fmaf(8.0f, vs, bf16_high(fv));
+                        if (!valid)
+                            ks = ko = vs = vo = 0.0f;
+                    }
+                    // the rows of this thread that see its key: those from first_col on
+                    const int first_col = !valid || (kOwn && a.causal && j >= a.Lq) ? kCols
+                                          : kOwn && a.causal ? j * a.group - (g.r0 + col0)
+                                                             : 0;
+                    uint32_t ph[kCols / 2], pl[kSplit ? kCols / 2 : 1];
+                    // Weights of this thread's columns, and their sums.  The second time (after
+                    // the references moved) only the rows of `redo` are summed again.
+                    auto weights = [&](auto again) -> float {
+                        constexpr bool kAgain = decltype(again)::value;
+                        const float4 *sq4 = reinterpret_cast<const float4 *>(sumq[sb] + col0);
+                        const float4 *nr4 = reinterpret_cast<const float4 *>(nref + col0);
+                        const float4 *cm4 = reinterpret_cast<const float4 *>(cmul + col0);
+                        const float4 *rd4 = reinterpret_cast<const float4 *>(redo + col0);
+                        const uint64_t ks2 = f2(ks, ks), ko2 = f2(ko, ko);
+                        const uint64_t vs2 = f2(vs, vs), vo2 = f2(vo, vo);
+                        float top = 0.0f;
+#pragma unroll
+                        for (int c8 = 0; c8 < kCols; c8 += 8) {
+                            uint32_t s[8];
+                            tmem_ld<8>(tS + c8, s);
+#pragma unroll
+                            for (int c = c8; c < c8 + 8; c += 4) {
+                                const float4 nr = nr4[c / 4], cm = cm4[c / 4];
+                                uint64_t y[2] = {f2(nr.x, nr.y), f2(nr.z, nr.w)};
+                                if constexpr (!kOwn) {
+                                    const float4 sq = sq4[c / 4];
+                                    y[0] = fma2(ko2, f2(sq.x, sq.y), y[0]);
+                                    y[1] = fma2(ko2, f2(sq.z, sq.w), y[1]);
+                                }
+                                const uint64_t cm2[2] = {f2(cm.x, cm.y), f2(cm.z, cm.w)};
+                                uint64_t rd2[2];
+                                if constexpr (kAgain) {
+                                    const float4 rd = rd4[c / 4];
+                                    rd2[0] = f2(rd.x, rd.y), rd2[1] = f2(rd.z, rd.w);
+                                }
+#pragma unroll
+                                for (int e = 0; e < 2; ++e) {
+                                    const int i = c / 2 + e;
+                                    float y0, y1, z0, z1;
+                                    un2(fma2(f2(__uint_as_float(s[2 * i - c8]),
+                                                __uint_as_float(s[2 * i + 1 - c8])),
+                                             ks2, y[e]),
+                                        y0, y1);
+                                    if (masked) {
+                                        y0 = 2 * i >= first_col ? y0 : neg_inf_f();
+                                        y1 = 2 * i + 1 >= first_col ? y1 : neg_inf_f();
+                                    }
+                                    y0 = ex2_mufu(y0);
+                                    y1 = ex2_mufu(y1);
+                                    const uint64_t p = f2(y0, y1);
+                                    if constexpr (kAgain) {
+                                        const uint64_t pr = mul2(p, rd2[e]);
+                                        l2[i] = add2(l2[i], pr);
+                                        if constexpr (!kOwn)
+                                            pm2[i] = fma2(pr, vo2, pm2[i]);
+                                    } else {
+                                        l2[i] = add2(l2[i], p);
+                                        if constexpr (!kOwn)
+                                            pm2[i] = fma2(p, vo2, pm2[i]);
+                                    }
+                                    un2(mul2(p, kOwn ? cm2[e] : mul2(vs2, cm2[e])), z0, z1);
+                                    top = fmaxf(top, fmaxf(fmaxf(y0, y1), fmaxf(z0, z1)));
+                                    ph[i] = pack2<W>(z0, z1);
+                                    if constexpr (kSplit) {
+                                        float h0, h1;
+                                        unpack2<W>(ph[i], h0, h1);
+                                        pl[i] = pack2<W>(z0 - h0, z1 - h1);
+                                    }
+                                }
+                            }
+                        }
+                        return top;
+                    };
+                    const bool over =
+                        __any_sync(0xFFFFFFFFu, weights(std::false_type{}) > kTopWeight);
+                    if (lane == 0) {
+                        if (over)
+                            *reinterpret_cast<volatile uint32_t *>(&vote[seen & 1]) = seen + 1;
+                        mbar_arrive(&voted);
+                    }
+                    __syncwarp();
+                    // ---- the values; the sums of the tile before must have read theirs
+                    if (given > summed) {
+                        wait(&o_done, summed & 1);
+                        ++summed;
+                        tc::fence_after_sync();
+                    }
+                    if (D == 128 || key < D) {
+                        const uint32_t tV = lanes + S::tV;
+                        const int d = key;
+                        if constexpr (!kOwn) {
+#pragma unroll
+                            for (int q = 0; q < 4 / S::C; ++q) {
+                                const int i = wg * (4 / S::C) + q;  // 32 slots
+                                int off;
+                                if (a.c.page_shift == 5)
+                                    off = i * (16 * D) + d * 16;
+                                else if (a.c.page_shift == 6)
+                                    off = (i >> 1) * (32 * D) + d * 32 +
+                                          (((i & 1) ^ ((d >> 2) & 1)) << 4);
+                                else
+                                    off = d * 64 + ((i ^ ((d >> 1) & 3)) << 4);
+                                uint32_t y[16];
+                                unpack32<__half>(*reinterpret_cast<const uint4 *>(
+                                                     buf + S::code_bytes + off),
+                                                 y);
+                                tmem_st16(tV + 16 * i, y);
+                            }
+                        } else {
+#pragma unroll 1
+                            for (int q = 0; q < 4 / S::C; ++q) {
+                                const int i = wg * (4 / S::C) + q;
+                                const uint16_t *v = static_cast<const uint16_t *>(a.v_new) +
+                                                    g.b * a.vs.batch + (int64_t)g.h * a.vs.head + d;
+                                uint32_t y[16];
+                                const int bad =
+                                    own_values<T>(v, a.vs.token, j0 + 32 * i, end, y);
+                                if (bad < end) {
+                                    atomicMin(&first_bad[d], bad);
+                                    any_bad = 1;
+                                }
+                                tmem_st16(tV + 16 * i, y);
+                            }
+                        }
+                    }
+                    wait(&voted, seen & 1);
+                    if (*reinterpret_cast<volatile uint32_t *>(&vote[seen & 1]) == seen + 1) {
+                        // ---- the references move: per row, the running maxima of the scores
+                        // and of the scores with the values' scale
+                        const float lv = vs > 0.0f ? log2f(vs) : neg_inf_f();
+#pragma unroll 1
+                        for (int z = 0; z < 2; ++z) {
+                            float m[kCols];
+#pragma unroll
+                            for (int c8 = 0; c8 < kCols; c8 += 8) {
+                                uint32_t s[8];
+                                tmem_ld<8>(tS + c8, s);
+#pragma unroll
+                                for (int c = 0; c < 8; ++c) {
+                                    const float x = fmaf(__uint_as_float(s[c]), ks,
+                                                         ko * sumq[sb][col0 + c8 + c]);
+                                    m[c8 + c] = c8 + c >= first_col ? x + (z ? lv : 0.0f)
+                                                                    : neg_inf_f();
+                                }
+                            }
+                            warp_columns<kCols>(m, [](float x, float y) { return fmaxf(x, y); });
+                            if (lane < kCols)
+                                wred[warp][z][lane] = m[0];
+                        }
+                        sync();
+                        if (tid < N) {
+                            const int w4 = tid / kCols * 4, c = tid % kCols;
+                            float s4 = wred[w4][0][c], z4 = wred[w4][1][c];
+#pragma unroll
+                            for (int i = 1; i < 4; ++i) {
+                                s4 = fmaxf(s4, wred[w4 + i][0][c]);
+                                z4 = fmaxf(z4, wred[w4 + i][1][c]);
+                            }
+                            const float ref = -nref[tid];
+                            const float to_ref = fmaxf(ref, s4);
+                            // where no value has a scale yet, refz follows at a distance
+                            const float z_old = refz[tid];
+                            const float to_z = fmaxf(fmaxf(z_old, z4), to_ref - kMaxShift);
+                            // a row whose weights may have overflowed starts anew with this
+                            // tile: what it held weighs less than 2^-60 of what it gets
+                            const bool anew = to_ref - ref > kTopShift;
+                            redo[tid] = anew ? 1.0f : 0.0f;
+                            fl[tid] = anew ? 0.0f : exp2f(ref - to_ref);
+                            fo[tid] = exp2f(z_old - to_z);
+                            nref[tid] = -to_ref;
+                            refz[tid] = to_z;
+                            cmul[tid] = exp2f(to_ref - to_z);
+                        }
+                        sync();
+                        if (t > begin) {  // the sums of the tiles before (waited for above)
+                            const uint32_t tO = lanes + S::tO + col0;
+#pragma unroll 1
+                            for (int c8 = 0; c8 < kCols; c8 += 8) {
+                                uint32_t s[8];
+                                tmem_ld<8>(tO + c8, s);
+#pragma unroll
+                                for (int c = 0; c < 8; ++c)
+                                    s[c] = __float_as_uint(__uint_as_float(s[c]) *
+                                                           fo[col0 + c8 + c]);
+                                tmem_st<8>(tO + c8, s);
+                            }
+                        }
+#pragma unroll
+                        for (int c = 0; c < kCols / 2; ++c) {
+                            float x0, x1, m0, m1;
+                            un2(l2[c], x0, x1);
+                            un2(pm2[c], m0, m1);
+                            const float f0 = fl[col0 + 2 * c], f1 = fl[col0 + 2 * c + 1];
+                            // (a sum that is NaN stays)
+                            x0 = f0 == 0.0f && x0 == x0 ? 0.0f : x0 * f0;
+                            x1 = f1 == 0.0f && x1 == x1 ? 0.0f : x1 * f1;
+                            m0 = f0 == 0.0f ? 0.0f : m0 * f0;
+                            m1 = f1 == 0.0f ? 0.0f : m1 * f1;
+                            l2[c] = f2(x0, x1);
+                            pm2[c] = f2(m0, m1);
+                        }
+                        weights(std::true_type{});
+                    }
+                    // ---- the weights
+                    const int kappa = (key & ~7) | ((key & 3) << 1) | ((key >> 2) & 1);
+                    const int at = (kappa >> 3) * (N * 16) + (col0 >> 3) * 128 + (kappa & 7) * 16;
+#pragma unroll
+                    for (int q = 0; q < kCols / 8; ++q) {
+                        *reinterpret_cast<uint4 *>(p_smem + at + 128 * q) =
+                            make_uint4(ph[4 * q], ph[4 * q + 1], ph[4 * q + 2], ph[4 * q + 3]);
+                        if constexpr (kSplit)
+                            *reinterpret_cast<uint4 *>(lo_smem + at + 128 * q) =
+                                make_uint4(pl[4 * q], pl[4 * q + 1], pl[4 * q + 2], pl[4 * q + 3]);
+                    }
+                    tmem_wait_st();
+                    fence_async_smem();
+                    tc::fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive(&p_ready);
+                        if (!kOwn)
+                            mbar_arrive(&empty[st]);
+                    }
+                    ++seen;
+                    ++given;
+                    ring += kOwn ? 0 : 1;
+                }
+            };
+            tiles(std::false_type{}, min(g.first, g.ct), min(g.last, g.ct));
+            tiles(std::true_type{}, max(g.first, g.ct), max(g.last, g.ct));
+
+            // ---- the end of the segment: sums over the keys, then the channels' results
+#pragma unroll 1
+            for (int z = 0; z < 2; ++z) {
+                float x[kCols];
+#pragma unroll
+                for (int c = 0; c < kCols / 2; ++c)
+                    un2(z ? pm2[c] : l2[c], x[2 * c], x[2 * c + 1]);
+                warp_columns<kCols>(x, [](float u, float v) { return u + v; });
+                if (lane < kCols)
+                    wred[warp][z][lane] = x[0];
+            }
+            const bool some = g.first < g.last;
+            if (given > summed) {
+                wait(&o_done, summed & 1);
+                ++summed;
+            }
+            tc::fence_after_sync();
+            sync();
+            const bool whole = g.starts && g.ends;
+            const int64_t part = ((int64_t)blockIdx.x * 2 + (g.starts ? 1 : 0)) * N;
+            if (tid < g.rows) {
+                const int w4 = tid / kCols * 4, c = tid % kCols;
+                float sum = 0.0f, off = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    sum += wred[w4 + i][0][c];
+                    off += wred[w4 + i][1][c];
+                }
+                if (poison)
+                    sum = nan_f();
+                const float ref = -nref[tid];
+                const float f = some ? exp2f(refz[tid] - ref) : 0.0f;
+                if (whole) {
+                    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+                    fl[tid] = off * inv;
+                    fo[tid] = f * inv;
+                    if (a.lse) {
+                        const int r = g.r0 + tid, qi = r / a.group;
+                        a.lse[((int64_t)g.b * a.Lq + qi) * a.Hq + g.h * a.group + r - qi * a.group] =
+                            sum == 0.0f ? neg_inf_f() : (ref + log2f(sum)) * 0.6931471805599453f;
+                    }
+                } else {
+                    fl[tid] = off;
+                    fo[tid] = f;
+                    a.part_refs[2 * (part + tid)] = ref;
+                    a.part_refs[2 * (part + tid) + 1] = sum;
+                }
+            }
+            if (tid == 0 && !whole) {
+                if (g.starts) {
+                    meta[kOpen] = 1;
+                    meta[kOpenB] = g.b;
+                    meta[kOpenUnit] = g.unit;
+                } else {
+                    meta[kCont] = 1;
+                    meta[kContEnds] = g.ends;
+                }
+            }
+            sync();
+            const int d = key;
+            int qi = (g.r0 + col0) / a.group, gi = g.r0 + col0 - qi * a.group;
+#pragma unroll 1
+            for (int c8 = 0; c8 < kCols; c8 += 8) {
+                uint32_t o[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+                if (some)
+                    tmem_ld<8>(lanes + S::tO + col0 + c8, o);
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    const int n = col0 + c8 + c;
+                    if (n < g.rows && d < D) {
+                        float x = fmaf(__uint_as_float(o[c]), fo[n], fl[n]);
+                        if (any_bad && first_bad[d] <= (a.causal ? qi : 0x7FFFFFFE))
+                            x = nan_f();
+                        if (whole)
+                            static_cast<T *>(
+                                a.out)[(((int64_t)g.b * a.Lq + qi) * a.Hq + g.h * a.group + gi) * D +
+                                       d] = from_float<T>(x);
+                        else
+                            a.parts[(part + n) * D + d] = x;
+                    }
+                    if (++gi == a.group) {
+                        gi = 0;
+                        ++qi;
+                    }
+                }
+            }
+            tc::fence_before_sync();
+            sync();  // the next segment overwrites the references and its sums
+            tc::fence_after_sync();
+            arrive(&q_empty[sb]);
+        }
+    }
+    tc::fence_before_sync();
+    __syncthreads();
+    tc::fence_after_sync();
+    if (warp == S::warps)
+        tc::tmem_dealloc(tmem, S::tmem);
+}
+
+// Joins the partials of the unit that CTA blockIdx.x of the attention began and did not finish:
+// its slot 1, then slot 0 of the CTAs after it up to the one where the unit ends.  A block takes
+// kJoinRows rows, a thread a channel.
+constexpr int kJoinRows = 8;
+
+template <typename T>
+__global__ void __launch_bounds__(128) combine_kernel(const __grid_constant__ AttnArgs a, int N,
+                                                      int grid)
+{
+    pdl_wait();
+    const int first = blockIdx.x;
+    const int32_t *meta = a.meta + (int64_t)first * kMeta;
+    if (!meta[kOpen])
+        return;
+    const int b = meta[kOpenB], unit = meta[kOpenUnit], D = a.c.D;
+    const int h = unit / a.row_tiles, r0 = (unit - h * a.row_tiles) * N;
+    const int n0 = blockIdx.y * kJoinRows;
+    const int n1 = min(n0 + kJoinRows, min(N, a.rows - r0));
+    int last = first;  // the CTA where the unit ends
+    for (int i = first + 1; i < grid; ++i) {
+        const int32_t *m = a.meta + (int64_t)i * kMeta;
+        if (m[kCont]) {
+            last = i;
+            if (m[kContEnds])
+                break;
+        }
+    }
+    const int d = threadIdx.x;
+    for (int n = n0; n < n1; ++n) {
+        float top = kFar;
+        for (int i = first; i <= last; ++i) {
+            const int64_t at = ((int64_t)i * 2 + (i == first)) * N + n;
+            if (i == first || a.meta[(int64_t)i * kMeta + kCont])
+                top = fmaxf(top, a.part_refs[2 * at]);
+        }
+        float sum = 0.0f, x = 0.0f;
+        for (int i = first; i <= last; ++i) {
+            const int64_t at = ((int64_t)i * 2 + (i == first)) * N + n;
+            if (i != first && !a.meta[(int64_t)i * kMeta + kCont])
+                continue;
+            const float f = exp2f(a.part_refs[2 * at] - top);
+            sum = fmaf(a.part_refs[2 * at + 1], f, sum);
+            if (d < D)
+                x = fmaf(a.parts[at * D + d], f, x);
+        }
+        const int qi = (r0 + n) / a.group, g = (r0 + n) - qi * a.group;
+        const int64_t row = ((int64_t)b * a.Lq + qi) * a.Hq + h * a.group + g;
+        if (d < D)
+            static_cast<T *>(a.out)[row * D + d] = from_float<T>(sum == 0.0f ? 0.0f : x / sum);
+        if (d == 0 && a.lse)
+            a.lse[row] =
+                sum == 0.0f ? neg_inf_f() : (top + log2f(sum)) * 0.6931471805599453f;
     }
 }
+
+// Rows of a row tile: the smallest width that holds a head's rows, 64 beyond that.
+int tile_rows(int64_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
+
+int sm_count()
+{
+    static int cached[64] = {0};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
+        cudaGetLastError();
+        return 152;
+    }
+    if (cached[dev] == 0) {
+        int n = 0;
+        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) {
+            cudaGetLastError();
+            return 152;
+        }
+        cached[dev] = n;
+    }
+    return cached[dev];
+}
+
+struct Workspace {
+    size_t meta, refs, parts, total;
+};
+
+Workspace workspace_of(int grid, int N, int D)
+{
+    Workspace w;
+    w.meta = 0;
+    w.refs = ((size_t)grid * kMeta * 4 + 255) / 256 * 256;
+    w.parts = (w.refs + (size_t)grid * 2 * N * 8 + 255) / 256 * 256;
+    w.total = (w.parts + (size_t)grid * 2 * N * D * 4 + 255) / 256 * 256;
+    return w;
+}
+
+int full_grid(int N) { return sm_count() * (N >= 64 ? 1 : 2); }
+
+template <typename S, typename T>
+cudaError_t run(const AttnArgs &a, int grid, const CUtensorMap &k_map, const CUtensorMap &v_map,
+                cudaStream_t s)
+{
+    static const cudaError_t ready = cudaFuncSetAttribute(
+        attention_kernel<S, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::smem);
+    if (ready != cudaSuccess)
+        return ready;
+    cudaError_t e = launch(attention_kernel<S, T>, dim3(grid), dim3(S::threads), S::smem, s, true,
+                           a, k_map, v_map);
+    if (e != cudaSuccess)
+        return e;
+    return launch(combine_kernel<T>, dim3(grid, S::N / kJoinRows), dim3(128), 0, s, true, a, S::N,
+                  grid);
+}
+
+template <int D, typename T>
+cudaError_t run_rows(const AttnArgs &a, int N, int grid, const CUtensorMap &k, const CUtensorMap &v,
+                     cudaStream_t s)
+{
+    return N == 16   ? run<Shape<D, 16>, T>(a, grid, k, v, s)
+           : N == 32 ? run<Shape<D, 32>, T>(a, grid, k, v, s)
+                     : run<Shape<D, 64>, T>(a, grid, k, v, s);
+}
+
+}  // namespace
 
 bool check_queries(const void *q, const int64_t *strides, int dtype, int B, int Lq, int Hq,
                    int heads)
@@ -213,7 +1042,6 @@ bool check_queries(const void *q, const int64_t *strides, int dtype, int B, int 
            (int64_t)Lq * (Hq / heads) < ((int64_t)1 << 30);
 }
 
-}  // namespace
 }  // namespace fdllm
 
 using namespace fdllm;
@@ -225,7 +1053,8 @@ size_t fdllm_cache_attention_workspace_bytes(int B, int Lq, int Hq, int heads, i
     if (B < 1 || Lq < 1 || Hq < 1 || heads < 1 || Hq % heads != 0 ||
         (head_dim != 64 && head_dim != 128))
         return 0;
-    return 256;
+    const int N = tile_rows((int64_t)Lq * (Hq / heads));
+    return workspace_of(full_grid(N), N, head_dim).total;
 }
 
 fdllm_status fdllm_cache_attention(const void *q, const int64_t *q_strides, int dtype, int B,
@@ -250,15 +1079,19 @@ fdllm_status fdllm_cache_attention(const void *q, const int64_t *q_strides, int 
     if (!aligned16(q, q_strides, 3, 2) || !aligned16(out, none, 0, 2) ||
         (Ln > 0 && (!aligned16(k_new, k_strides, 3, 2) || !aligned16(v_new, v_strides, 3, 2))))
         return FDLLM_ERR_ALIGN;
+    const int64_t rows = (int64_t)Lq * (Hq / a.c.heads);
+    const int N = tile_rows(rows), D = a.c.D;
+    const int most = full_grid(N);
+    const Workspace ws = workspace_of(most, N, D);
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 ||
-        workspace_bytes <
-            fdllm_cache_attention_workspace_bytes(B, Lq, Hq, a.c.heads, a.c.D))
+        workspace_bytes < ws.total)
         return FDLLM_ERR_WORKSPACE;
     a.table = block_table;
     a.max_pages = max_pages;
     a.lens = cache_lens;
     a.q = q;
     a.qs = strides3(q_strides);
+    a.B = B;
     a.Lq = Lq;
     a.Hq = Hq;
     a.group = Hq / a.c.heads;
@@ -271,58 +1104,34 @@ fdllm_status fdllm_cache_attention(const void *q, const int64_t *q_strides, int 
     a.Ln = Ln;
     a.new_lens = new_lens;
     a.causal = causal;
-    a.scale = (float)scale;
+    a.scale = (float)(scale * 1.4426950408889634);
     a.out = out;
     a.lse = out_lse;
-    cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const dim3 grid(Lq, Hq, B);
-    const bool bf = dtype == FDLLM_BF16, wide = a.c.D == 128;
-    const cudaError_t e =
-        bf ? (wide ? launch(attention_kernel<__nv_bfloat16, 128>, grid, dim3(kKeys), 0, s, true, a)
-                   : launch(attention_kernel<__nv_bfloat16, 64>, grid, dim3(kKeys), 0, s, true, a))
-           : (wide ? launch(attention_kernel<__half, 128>, grid, dim3(kKeys), 0, s, true, a)
-                   : launch(attention_kernel<__half, 64>, grid, dim3(kKeys), 0, s, true, a));
-    return e == cudaSuccess ? FDLLM_OK : FDLLM_ERR_CUDA;
-}
-
-fdllm_status fdllm_cache_key_weights(const void *q, const int64_t *q_strides, int dtype, int B,
-                                     int Lq, int Hq, const fdllm_cache *cache,
-                                     const int32_t *block_table, int max_pages,
-                                     const int32_t *cache_lens, const float *lse, double scale,
-                                     const float *weights_in, float *weights_out, int max_len,
-                                     void *stream)
-{
-    WeighArgs a = {};
-    const fdllm_status st = check_cache(cache, a.c);
-    if (st != FDLLM_OK)
-        return st;
-    if (!check_table(block_table, B, max_pages, a.c.page_shift, a.c.heads) || !cache_lens ||
-        !check_queries(q, q_strides, dtype, B, Lq, Hq, a.c.heads) || !lse ||
-        !std::isfinite(scale) || !weights_out || max_len < 1 || max_len >= (1 << 30))
+    a.rows = (int)rows;
+    a.row_tiles = (int)((rows + N - 1) / N);
+    if ((int64_t)a.c.heads * a.row_tiles >= ((int64_t)1 << 31))
         return FDLLM_ERR_ARG;
-    if (!aligned16(q, q_strides, 3, 2))
-        return FDLLM_ERR_ALIGN;
-    a.table = block_table;
-    a.max_pages = max_pages;
-    a.lens = cache_lens;
-    a.q = q;
-    a.qs = strides3(q_strides);
-    a.Lq = Lq;
-    a.Hq = Hq;
-    a.group = Hq / a.c.heads;
-    a.lse = lse;
-    a.scale = (float)scale;
-    a.in = weights_in;
-    a.out = weights_out;
-    a.max_len = max_len;
+    uint8_t *w = static_cast<uint8_t *>(workspace);
+    a.meta = reinterpret_cast<int32_t *>(w + ws.meta);
+    a.part_refs = reinterpret_cast<float *>(w + ws.refs);
+    a.parts = reinterpret_cast<float *>(w + ws.parts);
+    // No more CTAs than the call can have tiles.
+    const int64_t slots = (int64_t)max_pages << a.c.page_shift;
+    const int64_t tiles = (slots + kKeys - 1) / kKeys + ((int64_t)Ln + kKeys - 1) / kKeys;
+    int64_t bound = most;
+    if ((int64_t)a.c.heads * a.row_tiles < most && (int64_t)a.c.heads * a.row_tiles * B < most)
+        bound = (int64_t)a.c.heads * a.row_tiles * B * tiles;
+    const int grid = (int)(bound < most ? bound : most);
+    CUtensorMap k_map, v_map;
+    if (!make_cache_maps(a.c, &k_map, &v_map))
+        return FDLLM_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const dim3 grid((max_len + kKeys - 1) / kKeys, a.c.heads, B);
-    const bool bf = dtype == FDLLM_BF16, wide = a.c.D == 128;
+    const bool bf = dtype == FDLLM_BF16;
     const cudaError_t e =
-        bf ? (wide ? launch(weigh_kernel<__nv_bfloat16, 128>, grid, dim3(kKeys), 0, s, true, a)
-                   : launch(weigh_kernel<__nv_bfloat16, 64>, grid, dim3(kKeys), 0, s, true, a))
-           : (wide ? launch(weigh_kernel<__half, 128>, grid, dim3(kKeys), 0, s, true, a)
-                   : launch(weigh_kernel<__half, 64>, grid, dim3(kKeys), 0, s, true, a));
+        D == 128 ? (bf ? run_rows<128, __nv_bfloat16>(a, N, grid, k_map, v_map, s)
+                       : run_rows<128, __half>(a, N, grid, k_map, v_map, s))
+                 : (bf ? run_rows<64, __nv_bfloat16>(a, N, grid, k_map, v_map, s)
+                       : run_rows<64, __half>(a, N, grid, k_map, v_map, s));
     return e == cudaSuccess ? FDLLM_OK : FDLLM_ERR_CUDA;
 }
 

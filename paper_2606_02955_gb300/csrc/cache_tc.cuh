@@ -1,0 +1,307 @@
+// cache_tc.cuh -- tensor-core building blocks of the prefix cache's kernels: codes to matrix
+// operands, the A operand in tensor memory, descriptors, packed arithmetic, column reductions
+// and the tensor maps of a cache.
+#pragma once
+
+#include <cuda.h>
+
+#include "cache.cuh"
+#include "ptx.cuh"
+#include "tcgen05.cuh"
+
+namespace fdllm {
+
+// Tensor maps of a cache's codes: keys as rows of D/2 bytes, one box a page's (or a tile's)
+// slots; values as rows of page/2 bytes, one box D channels of up to 128 slots.  The swizzle
+// follows the box's row, so that 16-byte reads of one row a thread meet no bank twice.
+inline bool make_cache_maps(const CacheView &c, CUtensorMap *k, CUtensorMap *v)
+{
+    using Fn = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *,
+                            const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                            const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                            CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static const Fn encode = [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000,
+                                             cudaEnableDefault, &q) != cudaSuccess ||
+            q != cudaDriverEntryPointSuccess)
+            return (Fn) nullptr;
+        return reinterpret_cast<Fn>(p);
+    }();
+    if (!encode)
+        return false;
+    const int page = 1 << c.page_shift, span = page < 128 ? page : 128;
+    const auto map = [&](CUtensorMap *m, void *base, int64_t inner, int64_t outer, int box_inner,
+                         int box_outer) {
+        const cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)outer};
+        const cuuint64_t strides[1] = {(cuuint64_t)inner};
+        const cuuint32_t box[2] = {(cuuint32_t)box_inner, (cuuint32_t)box_outer};
+        const cuuint32_t unit[2] = {1, 1};
+        const CUtensorMapSwizzle sw = box_inner == 64   ? CU_TENSOR_MAP_SWIZZLE_64B
+                                      : box_inner == 32 ? CU_TENSOR_MAP_SWIZZLE_32B
+                                                        : CU_TENSOR_MAP_SWIZZLE_NONE;
+        return encode(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, base, dims, strides, box, unit,
+                      CU_TENSOR_MAP_INTERLEAVE_NONE, sw, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    };
+    const int64_t ph = (int64_t)c.pages * c.heads;
+    if (ph * page >= ((int64_t)1 << 31) || ph * c.D >= ((int64_t)1 << 31))
+        return false;  // box coordinates are 32-bit; such a pool exceeds the GPU's memory
+    return map(k, c.kc, c.D / 2, ph * page, c.D / 2, span) &&
+           (!v || map(v, c.vc, page / 2, ph * c.D, span / 2, c.D));
+}
+
+#ifdef __CUDACC__
+
+// ---------------------------------------------------------------- packed fp32 pairs
+__device__ __forceinline__ uint64_t f2(float lo, float hi)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void un2(uint64_t v, float &lo, float &hi)
+{
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+
+template <typename T>
+__device__ __forceinline__ void unpack2(uint32_t w, float &lo, float &hi)
+{
+    if constexpr (__is_same(T, __nv_bfloat16)) {
+        lo = bf16_low(w);
+        hi = bf16_high(w);
+    } else {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w));
+        lo = f.x;
+        hi = f.y;
+    }
+}
+
+// ---------------------------------------------------------------- codes -> matrix operands
+// Inside every group of eight, the contraction runs over elements 0 4 1 5 2 6 3 7: the order in
+// which masking a word of eight 4-bit codes yields pairs.
+//
+// A word's codes minus 8 as four pairs of T.  A code is put into the low bits of a number whose
+// last place is 1 (128 in bf16, 1024 in fp16; 1024 with last place 16 for the code's upper
+// position) and the constant taken off again: exact.
+template <typename T>
+__device__ __forceinline__ void unpack8(uint32_t w, uint32_t *y)
+{
+    if constexpr (__is_same(T, __nv_bfloat16)) {
+        const uint32_t minus = 0xC308C308u;  // -136
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t x = ((w >> (4 * j)) & 0x000F000Fu) | 0x43004300u;
+            asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(y[j]) : "r"(x), "r"(minus));
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const uint32_t v = w >> (8 * j);
+            const uint32_t lo = (v & 0x000F000Fu) | 0x64006400u;
+            const uint32_t hi = (v & 0x00F000F0u) | 0x64006400u;
+            asm("add.rn.f16x2 %0, %1, %2;" : "=r"(y[2 * j]) : "r"(lo), "r"(0xE408E408u));  // -1032
+            asm("fma.rn.f16x2 %0, %1, %2, %3;"                                  // / 16 - 72
+                : "=r"(y[2 * j + 1])
+                : "r"(hi), "r"(0x2C002C00u), "r"(0xD480D480u));
+        }
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void unpack32(const uint4 x, uint32_t (&y)[16])
+{
+    unpack8<T>(x.x, y);
+    unpack8<T>(x.y, y + 4);
+    unpack8<T>(x.z, y + 8);
+    unpack8<T>(x.w, y + 12);
+}
+
+// Eight 16-bit values in the same order.
+__device__ __forceinline__ uint4 interleave8(const uint4 x)
+{
+    return make_uint4(__byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632),
+                      __byte_perm(x.y, x.w, 0x5410), __byte_perm(x.y, x.w, 0x7632));
+}
+
+// ---------------------------------------------------------------- tensor memory
+// Columns of this warp's 32 lanes, one 32-bit word a column.
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, "
+        "%11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]),
+        "r"(r[15])
+        : "memory");
+}
+
+template <int NC>
+__device__ __forceinline__ void tmem_st(uint32_t taddr, const uint32_t (&r)[NC])
+{
+    if constexpr (NC == 16) {
+        tmem_st16(taddr, r);
+    } else {
+        static_assert(NC == 8, "columns");
+        asm volatile(
+            "tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(
+                taddr),
+            "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]),
+            "r"(r[7])
+            : "memory");
+    }
+}
+
+__device__ __forceinline__ void tmem_wait_st()
+{
+    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+
+template <int NC>
+__device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&r)[NC])
+{
+    if constexpr (NC == 16) {
+        asm volatile(
+            "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, "
+            "%11, %12, %13, %14, %15}, [%16];"
+            : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+              "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]),
+              "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+            : "r"(taddr)
+            : "memory");
+        asm volatile("tcgen05.wait::ld.sync.aligned;"
+                     : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]),
+                       "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]),
+                       "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+                     :
+                     : "memory");
+    } else {
+        static_assert(NC == 8, "columns");
+        asm volatile(
+            "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+            : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+              "=r"(r[7])
+            : "r"(taddr)
+            : "memory");
+        asm volatile("tcgen05.wait::ld.sync.aligned;"
+                     : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]),
+                       "+r"(r[6]), "+r"(r[7])
+                     :
+                     : "memory");
+    }
+}
+
+// ---------------------------------------------------------------- tcgen05.mma, A in tensor memory
+// kind::f16 with fp32 accumulation: formats of A and B (both T), B K-major or (b_mn) with its
+// rows contiguous (bit 16), N >> 3, M >> 4.
+template <typename T>
+__device__ __forceinline__ constexpr uint32_t idesc_f16(int M, int N, bool b_mn)
+{
+    const uint32_t f = __is_same(T, __nv_bfloat16) ? 1u : 0u;
+    return (1u << 4) | (f << 7) | (f << 10) | (b_mn ? 1u << 16 : 0u) | (uint32_t(N >> 3) << 17) |
+           (uint32_t(M >> 4) << 24);
+}
+
+// D[tmem] (+)= A[tmem] * B[smem] for one K = 16 slice; issued by one thread.
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc,
+                                       uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
+// Descriptor of an unswizzled operand with contiguous rows (MN-major): blocks of 8 rows x 8 k
+// (a 16-byte line of 8 rows for each k, 128 bytes), `rows_step` bytes from a block to the next
+// 8 rows, `k_step` bytes to the next 8 k.
+__device__ __forceinline__ uint64_t mn_desc(const void *tile, uint32_t rows_step, uint32_t k_step)
+{
+    return (uint64_t)((smem_addr(tile) & 0x3FFFFu) >> 4) | ((uint64_t)(k_step >> 4) << 16) |
+           ((uint64_t)(rows_step >> 4) << 32) | (1ull << 46);
+}
+
+// Shared-memory writes of this thread made visible to the tensor core.
+__device__ __forceinline__ void fence_async_smem()
+{
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+}
+
+// mbar_wait for waits that are short as a rule: the timer (whose reading alone costs about as
+// much as a tile) is looked at only after many tries.
+__device__ __forceinline__ bool mbar_wait_short(uint64_t *bar, uint32_t parity, uint32_t *status,
+                                                uint64_t limit_ns = kWaitLimitNs)
+{
+#pragma unroll 1
+    for (int i = 0; i < 4096; ++i)
+        if (mbar_try_wait(bar, parity))
+            return true;
+    return mbar_wait(bar, parity, status, limit_ns);
+}
+
+// ---------------------------------------------------------------- barriers of some of a CTA's warps
+__device__ __forceinline__ void named_sync(int id, int threads)
+{
+    asm volatile("barrier.cta.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+
+__device__ __forceinline__ bool named_sync_or(int id, int threads, bool x)
+{
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.u32 p, %3, 0;\n\t"
+        "barrier.cta.red.or.pred q, %1, %2, p;\n\t"
+        "selp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(r)
+        : "r"(id), "r"(threads), "r"((uint32_t)x)
+        : "memory");
+    return r != 0;
+}
+
+// Reduces each of NC columns over the warp's lanes: afterwards v[0] of lane c holds column
+// c % NC.  NC - 1 shuffles, then one for each further halving of the lanes.
+template <int NC, typename Op>
+__device__ __forceinline__ void warp_columns(float (&v)[NC], Op op)
+{
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int h = NC / 2; h > 0; h >>= 1) {
+#pragma unroll
+        for (int i = 0; i < h; ++i) {
+            const float send = (lane & h) ? v[i] : v[i + h];
+            const float keep = (lane & h) ? v[i + h] : v[i];
+            v[i] = op(keep, __shfl_xor_sync(0xFFFFFFFFu, send, h));
+        }
+    }
+#pragma unroll
+    for (int m = NC; m < 32; m <<= 1)
+        v[0] = op(v[0], __shfl_xor_sync(0xFFFFFFFFu, v[0], m));
+}
+
+#endif  // __CUDACC__
+
+}  // namespace fdllm
