@@ -1,12 +1,13 @@
 // cache_attention.cu -- fdllm_cache_attention: a block's queries over the 4-bit prefix cache
 // and the block's own keys, on the fifth-generation tensor cores.
 //
-// Mathematics.  With k_j = ko_j + ks_j u_j (u_j the codes minus 8, ko_j the middle of the range)
-// and likewise v_j, for the rows r of one key/value head (queries x heads of the group):
+// Mathematics.  With k_j = ko_j + ks_j u_j (u_j the codes) and likewise v_j, for the rows r of
+// one key/value head (queries x heads of the group):
 //   s_rj = scale (ks_j (q_r . u_j) + ko_j sum(q_r)),
 //   out_r = (sum_j p_rj vs_j w_j + sum_j p_rj vo_j) / sum_j p_rj,   p_rj = e^(s_rj - m_r).
-// The tensor cores see the codes themselves, exact in bf16 and fp16; scales and offsets act on
-// the scores and the weights.
+// The tensor cores see the codes themselves, exact in fp16; scales and offsets act on the
+// scores and the weights.  Queries enter the first product as fp16 too, times a power of two
+// that brings the tile's largest to 2^13: exact but for elements below 2^-23 of it.
 //
 // Layout.  A tile is 128 keys.  Both products are taken transposed, with the unpacked codes as
 // the A operand in tensor memory, so that the codes go from registers straight to the tensor
@@ -17,14 +18,18 @@
 // are stored channel-major so that a thread unpacks one channel.  P^T is the only operand
 // written to shared memory by threads (16-byte stores, rows contiguous).
 //
-// A row's running maximum lags: the reference of a row moves only when a weight leaves the
-// range that fp16 and fp32 hold (kTopWeight), which one vote a tile decides.  Weights are
-// scaled by the cached row's scale before they are rounded to fp16; c[r] keeps their largest
-// near 1 whatever the scales are.
+// A row's reference (the running maximum of a softmax) is the score of the first key it meets,
+// and moves only when a weight leaves the range that fp16 and fp32 hold (kTopWeight), which one
+// vote a tile decides.  Weights are scaled by the cached row's scale before they are rounded to
+// fp16; a second reference of the row keeps their largest near 1 whatever the scales are.
 //
-// Split.  The tiles of all (sequence, head, row tile) units in order are cut into equal ranges,
-// one to a CTA (the lengths are read on the device); a unit that crosses a CTA's end leaves
-// fp32 partials, joined by combine_kernel in tile order.
+// Warps.  One loads (queries, codes, own keys and values, through one ring of shared-memory
+// stages), one issues the products, the others unpack and make weights.
+//
+// Split.  The tiles of all (sequence, head, row tile) units in order, with a charge of
+// kUnitCost tiles for each unit's beginning and end, are cut into equal ranges, one to a CTA
+// (the lengths are read on the device); a unit that crosses a CTA's end leaves fp32 partials,
+// joined by combine_kernel in tile order.
 #include <cuda_runtime.h>
 
 #include <type_traits>
@@ -40,6 +45,7 @@ constexpr float kFar = -1e30f;            // reference of a row that has seen no
 constexpr float kTopWeight = 16384.0f;    // largest weight (fp16 holds 65504)
 constexpr float kTopShift = 90.0f;        // a score this far above its reference may overflow
 constexpr float kMaxShift = 120.0f;       // c = 2^(ref - refz) stays below 2^120
+constexpr float kSumUnit = 1048576.0f;    // sums over codes come in units of 2^-20
 
 struct AttnArgs {
     CacheView c;
@@ -79,28 +85,69 @@ struct Shape {
     static constexpr int workers = 32 * warps;
     static constexpr int threads = workers + 64;       // the loading and the issuing warp
     static constexpr int ctas = N >= 64 ? 1 : 2;       // CTAs an SM holds
-    static constexpr int stages = N >= 64 ? 6 : 4;
+    static constexpr int stages = N >= 64 ? 8 : 4;
+    // own keys come 32 to a stage; a block's 32 fill one tile, long prompts whole ones
+    static constexpr int own_keys = N >= 64 ? 128 : 32;
     static constexpr int code_bytes = kKeys * D / 2;   // of keys, or of values
     static constexpr int stage_bytes = 2 * code_bytes + 1024;
+    static constexpr int own_row = 2 * D + 16;         // a stage's own keys: rows apart in banks
+    static constexpr int own_v = 32 * own_row;
     static constexpr int q_bytes = N * D * 2;
-    static constexpr int q_off = stages * stage_bytes;
-    static constexpr int p_off = q_off + 2 * q_bytes;
+    static constexpr int q16_off = stages * stage_bytes;  // queries for codes, in fp16
+    static constexpr int qt_off = q16_off + q_bytes;      // queries for own keys, as they are
+    static constexpr int p_off = qt_off + q_bytes;
     static constexpr int lo_off = p_off + kKeys * N * 2;
     static constexpr int smem = lo_off + kKeys * N * 2 + 1024;  // and room to align the base
     // tensor memory columns
     static constexpr int tK = 0, tV = 64, tS = 128, tO = 128 + 2 * N;
     static constexpr int tmem = tO + N <= 256 ? 256 : 512;
     static_assert(tO + N <= tmem && ctas * tmem <= 512, "tensor memory");
+    static_assert(q_bytes <= stage_bytes && own_v + 64 * D <= stage_bytes, "a stage holds them");
+    static_assert(stages >= 2 * own_keys / 32, "two own tiles are in flight");
 };
 
 __device__ uint32_t g_status;  // sticky: a bounded wait gave up
 
-__device__ __forceinline__ int cached_len(const CacheView &c, const int32_t *lens, int max_pages,
-                                          int b)
+// 32 own values of one channel (rows `step` apart in shared memory), as pairs in the operand's
+// order; keys from `n` on are 0.  A non-finite value must not meet the zero weights of the rows
+// that do not see it: it is taken out, and the first such key returned for the rows that do.
+template <typename T>
+__device__ __forceinline__ int own_values(const T *v, int step, int n, uint32_t (&y)[16])
 {
-    const int n = lens[b];
-    return n >= 0 && n <= (max_pages << c.page_shift) ? n : -1;
+    constexpr uint32_t kExp = std::is_same<T, __half>::value ? 0x7C00u : 0x7F80u;
+    const uint16_t *u = reinterpret_cast<const uint16_t *>(v);
+    int bad = 32;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        const int x = (e >> 2) * 8 + (e & 3);  // and four further on
+        uint32_t lo = x < n ? u[x * step] : 0u;
+        uint32_t hi = x + 4 < n ? u[(x + 4) * step] : 0u;
+        if ((lo & kExp) == kExp)
+            bad = min(bad, x), lo = 0;
+        if ((hi & kExp) == kExp)
+            bad = min(bad, x + 4), hi = 0;
+        y[e] = lo | (hi << 16);
+    }
+    return bad;
 }
+
+// Sums in tensor memory times a factor for each column (f) or for all (u).
+template <int NC>
+__device__ __forceinline__ void scale_sums(uint32_t taddr, const float *f, float u)
+{
+#pragma unroll 1
+    for (int c8 = 0; c8 < NC; c8 += 8) {
+        uint32_t s[8];
+        tmem_ld<8>(taddr + c8, s);
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+            s[c] = __float_as_uint(__uint_as_float(s[c]) * (f ? f[c8 + c] : u));
+        tmem_st<8>(taddr + c8, s);
+    }
+}
+
+// A unit's beginning and end cost about as much as this many tiles.
+constexpr int kUnitCost = 3;
 
 // One sequence's share of the work.
 struct Sequence {
@@ -111,46 +158,25 @@ struct Sequence {
     bool wrong;    // a length out of range
 };
 
+template <int OwnKeys>
 __device__ __forceinline__ Sequence sequence_of(const AttnArgs &a, int b)
 {
     Sequence s;
-    const int n = cached_len(a.c, a.lens, a.max_pages, b);
+    const int n = a.lens[b];
     const int own = a.new_lens ? a.new_lens[b] : a.Ln;
-    s.wrong = n < 0 || own < 0 || own > a.Ln;
+    s.wrong = n < 0 || n > (a.max_pages << a.c.page_shift) || own < 0 || own > a.Ln;
     s.cached = s.wrong ? 0 : n;
     s.own = s.wrong ? 0 : own;
     s.ct = (s.cached + kKeys - 1) / kKeys;
-    s.tiles = max(1, s.ct + (s.own + kKeys - 1) / kKeys);
+    s.tiles = max(1, s.ct + (s.own + OwnKeys - 1) / OwnKeys);
     return s;
 }
 
-// 32 own values of one channel, keys x0 .. x0 + 31, as pairs in the operand's order; keys from
-// `end` on are 0.  A non-finite value must not meet the zero weights of the rows that do not
-// see it: it is taken out, and the first such key returned for the rows that do.
-template <typename T>
-__device__ __noinline__ int own_values(const uint16_t *v, int64_t step, int x0, int end,
-                                       uint32_t (&y)[16])
-{
-    constexpr uint32_t kExp = std::is_same<T, __half>::value ? 0x7C00u : 0x7F80u;
-    int bad = 0x7FFFFFFF;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-        const int x = x0 + (e >> 2) * 8 + (e & 3);  // and four further on
-        uint32_t lo = x < end ? v[(int64_t)x * step] : 0u;
-        uint32_t hi = x + 4 < end ? v[(int64_t)(x + 4) * step] : 0u;
-        if ((lo & kExp) == kExp)
-            bad = min(bad, x), lo = 0;
-        if ((hi & kExp) == kExp)
-            bad = min(bad, x + 4), hi = 0;
-        y[e] = lo | (hi << 16);
-    }
-    return bad;
-}
-
-// A CTA's walk over its range of tiles, segment by segment (a segment: tiles of one unit).
+// A CTA's walk over its range, segment by segment (a segment: tiles of one unit).
+template <int OwnKeys>
 struct Walk {
-    int64_t at, end;    // tiles of the whole call
-    int64_t base;       // first tile of sequence b
+    int64_t at, end;    // places in the whole call
+    int64_t base;       // first place of sequence b
     int b;
     Sequence s;
     int unit;           // head * row_tiles + row tile
@@ -158,18 +184,23 @@ struct Walk {
 
     __device__ bool next(const AttnArgs &a, int units)
     {
-        if (at >= end)
-            return false;
-        while (at >= base + (int64_t)s.tiles * units) {
-            base += (int64_t)s.tiles * units;
-            s = sequence_of(a, ++b);
+        while (at < end) {
+            while (at >= base + (int64_t)(s.tiles + kUnitCost) * units) {
+                base += (int64_t)(s.tiles + kUnitCost) * units;
+                s = sequence_of<OwnKeys>(a, ++b);
+            }
+            const int64_t local = at - base;
+            const int length = s.tiles + kUnitCost;
+            unit = (int)(local / length);
+            const int from = (int)(local - (int64_t)unit * length);
+            const int to = (int)min((int64_t)length, from + (end - at));
+            at += to - from;
+            first = min(from, s.tiles);
+            last = min(to, s.tiles);
+            if (first < last)
+                return true;
         }
-        const int64_t local = at - base;
-        unit = (int)(local / s.tiles);
-        first = (int)(local - (int64_t)unit * s.tiles);
-        last = (int)min((int64_t)s.tiles, first + (end - at));
-        at += last - first;
-        return true;
+        return false;
     }
 };
 
@@ -189,11 +220,11 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                      const __grid_constant__ CUtensorMap k_map,
                      const __grid_constant__ CUtensorMap v_map)
 {
-    constexpr int D = S::D, N = S::N, kCols = S::cols;
+    constexpr int D = S::D, N = S::N, kCols = S::cols, kOwnKeys = S::own_keys;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
-    __shared__ __align__(8) uint64_t full[S::stages], empty[S::stages];  // the ring of codes
-    __shared__ __align__(8) uint64_t q_full[2], q_empty[2];              // queries, segments
+    __shared__ __align__(8) uint64_t full[S::stages], empty[S::stages];  // the ring
+    __shared__ __align__(8) uint64_t seg_full[2], seg_empty[2];
     __shared__ __align__(8) uint64_t k_ready, s_done, p_ready, o_done, voted;
     __shared__ uint32_t tmem_base;
     __shared__ uint8_t stage_bad[S::stages];
@@ -202,23 +233,24 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
     __shared__ int find_b;
     __shared__ Segment segs[2];
     __shared__ uint32_t vote[2];
-    __shared__ __align__(16) float sumq[2][N];  // of the queries' channels
-    // per row: the reference (negated), 2^(ref - refz), the reference of the scaled weights
-    __shared__ __align__(16) float nref[N], cmul[N], refz[N];
+    // per row: sum of the query's channels; the reference (negated), 2^(ref - refz), the
+    // reference of the scaled weights
+    __shared__ __align__(16) float sumq[N], nref[N], cmul[N], refz[N];
     __shared__ __align__(16) float fl[N], fo[N], redo[N];
+    __shared__ int64_t row_at[N];
     __shared__ float wred[S::warps][2][kCols];
     __shared__ int first_bad[D];  // first own key of the segment with a non-finite value
     __shared__ int any_bad;
 
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31;
     if (tid == 0) {
         for (int i = 0; i < S::stages; ++i) {
             mbar_init(&full[i], 1);
             mbar_init(&empty[i], S::warps);
         }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&q_full[i], 1);
-            mbar_init(&q_empty[i], S::warps + 1);
+            mbar_init(&seg_full[i], 1);
+            mbar_init(&seg_empty[i], S::warps + 1);
             vote[i] = 0;
         }
         mbar_init(&k_ready, S::warps);
@@ -236,16 +268,16 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
     }
     pdl_wait();
 
-    // The call's tiles, and the sequence in which this CTA's range begins: every thread sums a
+    // The call's places, and the sequence in which this CTA's range begins: every thread sums a
     // run of sequences, a scan over the CTA gives the runs' places.
     const int units = a.c.heads * a.row_tiles;
-    Walk w;
+    Walk<kOwnKeys> w;
     {
         const int run = (a.B + S::threads - 1) / S::threads;
         const int b0 = min(a.B, tid * run), b1 = min(a.B, b0 + run);
         int64_t mine = 0;
         for (int b = b0; b < b1; ++b)
-            mine += sequence_of(a, b).tiles;
+            mine += sequence_of<kOwnKeys>(a, b).tiles + kUnitCost;
         int64_t upto = mine;
 #pragma unroll
         for (int m = 1; m < 32; m <<= 1) {
@@ -275,7 +307,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
     tc::fence_before_sync();
     __syncthreads();
     tc::fence_after_sync();
-    const uint32_t tmem = tmem_base;
+    const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, tmem_base, 0);
     pdl_launch_dependents();
 
     bool dead = false;  // a wait gave up: no further wait, the walk goes on to its end
@@ -284,222 +316,311 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
             dead = true;
     };
 
+    // the same for a whole warp
+    auto wait_warp = [&](uint64_t *bar, uint32_t parity) {
+        wait(bar, parity);
+        dead = __any_sync(0xFFFFFFFFu, dead);
+    };
+
     if (warp == S::warps) {
         // ---------------------------------------------------------------- the loading warp
         if (w.at < w.end) {
             w.b = find_b;
             w.base = find_base;
-            w.s = sequence_of(a, w.b);
+            w.s = sequence_of<kOwnKeys>(a, w.b);
         }
-        uint32_t ring = 0;  // cached tiles so far: stage ring % stages, phase ring / stages
+        uint32_t ring = 0;  // stages filled so far: stage ring % stages, phase ring / stages
+        const int page = 1 << a.c.page_shift;
+        const int span = min(page, kKeys);  // slots of a page in a tile
+        const int pieces = kKeys / span;
         for (uint32_t seg = 0;; ++seg) {
             const uint32_t sb = seg & 1;
             const bool more = w.next(a, units);
-            wait(&q_empty[sb], ((seg >> 1) & 1) ^ 1);
+            wait_warp(&seg_empty[sb], ((seg >> 1) & 1) ^ 1);
             const int h = more ? w.unit / a.row_tiles : 0;
             const int r0 = more ? (w.unit - h * a.row_tiles) * N : 0;
             const int rows = min(N, a.rows - r0);
+            int own_tiles = more ? (w.s.own + kOwnKeys - 1) / kOwnKeys : 0;
+            if (a.causal)  // own keys that the last row sees
+                own_tiles = min(own_tiles, (r0 + rows - 1) / a.group / kOwnKeys + 1);
+            const int last = more ? min(w.last, w.s.ct + own_tiles) : 0;
             if (lane == 0) {
                 Segment &g = segs[sb];
                 g.done = !more;
                 if (more) {
                     g.b = w.b, g.unit = w.unit, g.h = h, g.r0 = r0, g.rows = rows;
-                    // an empty unit's one tile holds no key
-                    g.first = w.first;
-                    g.last = min(w.last, w.s.ct + (w.s.own + kKeys - 1) / kKeys);
+                    g.first = w.first, g.last = last;
                     g.ct = w.s.ct, g.cached = w.s.cached, g.own = w.s.own;
                     g.starts = w.first == 0, g.ends = w.last == w.s.tiles;
                     g.wrong = w.s.wrong;
                 }
+                mbar_arrive(&seg_full[sb]);
             }
-            if (!more) {
-                __syncwarp();
-                if (lane == 0)
-                    mbar_arrive(&q_full[sb]);
-                break;
-            }
-            // Queries into shared memory (K-major, 128-byte swizzle), and their sums.
-            uint8_t *q_smem = smem + S::q_off + sb * S::q_bytes;
-#pragma unroll 4
-            for (int i = lane; i < N * (D / 8); i += 32) {
-                const int n = i / (D / 8), c8 = i % (D / 8);
-                uint4 x = make_uint4(0, 0, 0, 0);
-                if (n < rows) {
-                    const int qi = (r0 + n) / a.group, g = (r0 + n) - qi * a.group;
-                    x = *reinterpret_cast<const uint4 *>(
-                        static_cast<const T *>(a.q) + w.b * a.qs.batch + qi * a.qs.token +
-                        (int64_t)(h * a.group + g) * a.qs.head + 8 * c8);
-                }
-                const uint32_t xw[4] = {x.x, x.y, x.z, x.w};
-                float sum = 0.0f;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float lo, hi;
-                    unpack2<T>(xw[e], lo, hi);
-                    sum += lo + hi;
-                }
-#pragma unroll
-                for (int m = D / 16; m > 0; m >>= 1)
-                    sum += __shfl_xor_sync(0xFFFFFFFFu, sum, m);
-                if (c8 == 0)
-                    sumq[sb][n] = sum;
-                *reinterpret_cast<uint4 *>(q_smem + (c8 >> 3) * (N * 128) + n * 128 +
-                                           (((c8 & 7) ^ (n & 7)) << 4)) = interleave8(x);
-            }
-            fence_async_smem();
             __syncwarp();
-            if (lane == 0) {
-                mbar_arrive(&q_full[sb]);
-                const int page = 1 << a.c.page_shift;
-                const int span = min(page, kKeys);  // slots of a page in a tile
-                for (int t = w.first; t < min(w.last, w.s.ct); ++t, ++ring) {
-                    const uint32_t st = ring % S::stages;
-                    wait(&empty[st], ((ring / S::stages) & 1) ^ 1);
-                    uint8_t *buf = smem + st * S::stage_bytes;
-                    uint32_t bytes = 0;
-                    int pg[4];
-                    bool bad = false;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int slot = t * kKeys + i * span;
-                        pg[i] = -1;
-                        if (i * span < kKeys && slot < w.s.cached) {
-                            pg[i] = page_of(a.c, a.table, a.max_pages, w.b, slot);
-                            bad |= pg[i] < 0;
-                        }
-                        if (pg[i] >= 0)
-                            bytes += (uint32_t)span * (D + 8);
+            if (!more)
+                break;
+            if (w.first >= last)
+                continue;
+            // The queries' rows.
+            {
+                const uint32_t st = ring % S::stages;
+                wait_warp(&empty[st], ((ring / S::stages) & 1) ^ 1);
+                uint8_t *buf = smem + st * S::stage_bytes;
+                if (!dead) {
+                    if (lane == 0)
+                        mbar_arrive_expect_tx(&full[st], (uint32_t)rows * D * 2);
+                    __syncwarp();
+                    for (int n = lane; n < rows; n += 32) {
+                        const int qi = (r0 + n) / a.group, g = (r0 + n) - qi * a.group;
+                        bulk_copy_g2s(buf + n * (D * 2),
+                                      static_cast<const T *>(a.q) + w.b * a.qs.batch +
+                                          qi * a.qs.token + (int64_t)(h * a.group + g) * a.qs.head,
+                                      D * 2, &full[st]);
                     }
+                }
+                ++ring;
+            }
+            // Cached tiles; a lane looks up one page of the next 32.
+            const int cached_end = min(last, w.s.ct);
+            int pg_lane = -1;
+            for (int t = w.first; t < cached_end; ++t, ++ring) {
+                const int batch = (t - w.first) * pieces;  // pieces since the segment began
+                if ((batch & 31) == 0) {
+                    const int slot = t * kKeys + lane * span;
+                    pg_lane = slot < w.s.cached
+                                  ? page_of(a.c, a.table, a.max_pages, w.b, slot)
+                                  : -2;
+                }
+                const uint32_t st = ring % S::stages;
+                wait_warp(&empty[st], ((ring / S::stages) & 1) ^ 1);
+                uint8_t *buf = smem + st * S::stage_bytes;
+                // lane i < pieces copies piece i
+                const int pg = __shfl_sync(0xFFFFFFFFu, pg_lane, (batch & 31) + (lane & 3));
+                const bool mine = lane < pieces && pg >= 0;
+                const uint32_t there = __ballot_sync(0xFFFFFFFFu, mine);
+                const bool bad = __any_sync(0xFFFFFFFFu, lane < pieces && pg == -1);
+                if (lane == 0) {
                     stage_bad[st] = bad;
+                    if (!dead && there)
+                        mbar_arrive_expect_tx(&full[st],
+                                              (uint32_t)__popc(there) * span * (D + 8));
+                    else if (!dead)
+                        mbar_arrive(&full[st]);
+                }
+                __syncwarp();
+                if (mine && !dead) {
+                    const int i = lane;
+                    const int in_page = (t * kKeys + i * span) & (page - 1);
+                    const int64_t ph = (int64_t)pg * a.c.heads + h;
+                    tc::tma_load_2d(buf + i * span * (D / 2), &k_map, 0, (int)(ph * page + in_page),
+                                    &full[st]);
+                    tc::tma_load_2d(buf + S::code_bytes + i * (span / 2) * D, &v_map, in_page / 2,
+                                    (int)(ph * D), &full[st]);
+                    uint8_t *aff = buf + 2 * S::code_bytes + i * span * 4;
+                    bulk_copy_g2s(aff, a.c.ka + ph * page + in_page, span * 4, &full[st]);
+                    bulk_copy_g2s(aff + 512, a.c.va + ph * page + in_page, span * 4, &full[st]);
+                }
+                __syncwarp();
+            }
+            // Own tiles, 32 keys and values to a stage.
+            for (int t = max(w.first, w.s.ct); t < last; ++t) {
+                const int j1 = min(w.s.own, (t - w.s.ct + 1) * kOwnKeys);
+                for (int j0 = (t - w.s.ct) * kOwnKeys; j0 < j1; j0 += 32, ++ring) {
+                    const uint32_t st = ring % S::stages;
+                    wait_warp(&empty[st], ((ring / S::stages) & 1) ^ 1);
+                    uint8_t *buf = smem + st * S::stage_bytes;
+                    const int n = min(32, j1 - j0);
                     if (dead)
                         continue;
-                    if (bytes)
-                        mbar_arrive_expect_tx(&full[st], bytes);
-                    else
-                        mbar_arrive(&full[st]);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if (pg[i] < 0)
-                            continue;
-                        const int in_page = (t * kKeys + i * span) & (page - 1);
-                        const int64_t ph = (int64_t)pg[i] * a.c.heads + h;
-                        tc::tma_load_2d(buf + i * span * (D / 2), &k_map, 0,
-                                        (int)(ph * page + in_page), &full[st]);
-                        tc::tma_load_2d(buf + S::code_bytes + i * (span / 2) * D, &v_map,
-                                        in_page / 2, (int)(ph * D), &full[st]);
-                        uint8_t *aff = buf + 2 * S::code_bytes + i * span * 4;
-                        bulk_copy_g2s(aff, a.c.ka + ph * page + in_page, span * 4, &full[st]);
-                        bulk_copy_g2s(aff + 512, a.c.va + ph * page + in_page, span * 4,
-                                      &full[st]);
+                    if (lane == 0)
+                        mbar_arrive_expect_tx(&full[st], (uint32_t)n * D * 4);
+                    __syncwarp();
+                    if (lane < n) {
+                        bulk_copy_g2s(buf + lane * S::own_row,
+                                      static_cast<const T *>(a.k_new) + w.b * a.ks.batch +
+                                          (int64_t)(j0 + lane) * a.ks.token + (int64_t)h * a.ks.head,
+                                      D * 2, &full[st]);
+                        bulk_copy_g2s(buf + S::own_v + lane * (D * 2),
+                                      static_cast<const T *>(a.v_new) + w.b * a.vs.batch +
+                                          (int64_t)(j0 + lane) * a.vs.token + (int64_t)h * a.vs.head,
+                                      D * 2, &full[st]);
                     }
+                    __syncwarp();
                 }
             }
-            __syncwarp();
         }
         // Nothing may land in this CTA's memory after it has gone: the last copies of every
-        // stage (at most one each) are waited for, with a limit.
-        if (lane == 0)
-            for (uint32_t i = 0; i < min(ring, (uint32_t)S::stages); ++i) {
-                const uint32_t r = ring - 1 - i;
-                mbar_wait_short(&full[r % S::stages], (r / S::stages) & 1, &g_status,
-                                dead ? kDrainLimitNs : kWaitLimitNs);
-            }
+        // stage (at most one round each) are waited for, with a limit.
+        __syncwarp();
+        for (uint32_t i = 0; i < min(ring, (uint32_t)S::stages); ++i) {
+            const uint32_t r = ring - 1 - i;
+            mbar_wait_short(&full[r % S::stages], (r / S::stages) & 1, &g_status,
+                            dead ? kDrainLimitNs : kWaitLimitNs);
+        }
     } else if (warp == S::warps + 1) {
         // ---------------------------------------------------------------- the issuing warp
         // S of a tile before the sums of the tile before it, so that the tensor core works on
         // scores while the workers make weights.
+        const uint64_t q16_desc = tc::sw128_kmajor_desc(smem + S::q16_off);
+        const uint64_t qt_desc = tc::sw128_kmajor_desc(smem + S::qt_off);
+        const uint64_t p_desc = mn_desc(smem + S::p_off, 128, N * 16);
+        const uint64_t lo_desc = mn_desc(smem + S::lo_off, 128, N * 16);
         uint32_t scores = 0, sums = 0;  // products issued so far
         for (uint32_t seg = 0;; ++seg) {
             const uint32_t sb = seg & 1;
-            wait(&q_full[sb], (seg >> 1) & 1);
-            const Segment g = segs[sb];
-            if (g.done)
+            wait_warp(&seg_full[sb], (seg >> 1) & 1);
+            const int done = segs[sb].done, first = segs[sb].first, last = segs[sb].last;
+            const int ct = segs[sb].ct, own_total = segs[sb].own;
+            __syncwarp();
+            if (lane == 0)
+                mbar_arrive(&seg_empty[sb]);
+            if (done)
                 break;
-            const uint8_t *q_smem = smem + S::q_off + sb * S::q_bytes;
-            const uint64_t q_desc = tc::sw128_kmajor_desc(q_smem);
-            const uint64_t p_desc = mn_desc(smem + S::p_off, 128, N * 16);
-            const uint64_t lo_desc = mn_desc(smem + S::lo_off, 128, N * 16);
-            for (int t = g.first; t <= g.last; ++t) {
-                if (t < g.last) {
-                    wait(&k_ready, scores & 1);
+            for (int t = first; t <= last; ++t) {
+                if (t < last) {
+                    wait_warp(&k_ready, scores & 1);
                     tc::fence_after_sync();
-                    if (lane == 0) {
+                    const uint64_t q_desc = t < ct ? q16_desc : qt_desc;
+                    const uint32_t idesc =
+                        t < ct ? idesc_f16<__half>(128, N, false) : idesc_f16<T>(128, N, false);
 #pragma unroll
-                        for (int k = 0; k < D / 16; ++k)
-                            mma_ts(tmem + S::tS + (scores & 1) * N, tmem + S::tK + 8 * k,
-                                   q_desc + (k >> 2) * ((N * 128) >> 4) + 2 * (k & 3),
-                                   idesc_f16<T>(128, N, false), k > 0);
-                        tc::commit(&s_done);
-                    }
-                    __syncwarp();
+                    for (int k = 0; k < D / 16; ++k)
+                        mma_ts(tmem + S::tS + (scores & 1) * N, tmem + S::tK + 8 * k,
+                               q_desc + (k >> 2) * ((N * 128) >> 4) + 2 * (k & 3), idesc, k > 0);
+                    mma_commit(&s_done);
                     ++scores;
                 }
-                if (t > g.first) {
-                    const bool own = t - 1 >= g.ct;
-                    const bool split = own || !std::is_same<T, __nv_bfloat16>::value;
-                    const uint32_t idesc =
-                        own ? idesc_f16<T>(128, N, true) : idesc_f16<__half>(128, N, true);
-                    wait(&p_ready, sums & 1);
+                if (t > first) {
+                    wait_warp(&p_ready, sums & 1);
                     tc::fence_after_sync();
-                    if (lane == 0) {
+                    const uint32_t more = t - 1 > first;
+                    if (t - 1 < ct) {
+                        constexpr uint32_t idesc = idesc_f16<__half>(128, N, true);
 #pragma unroll
                         for (int k = 0; k < kKeys / 16; ++k)
                             mma_ts(tmem + S::tO, tmem + S::tV + 8 * k,
-                                   p_desc + k * ((2 * N * 16) >> 4), idesc,
-                                   t - 1 > g.first || k > 0);
-                        if (split)
+                                   p_desc + k * ((2 * N * 16) >> 4), idesc, k > 0 ? 1u : more);
+                        if (!std::is_same<T, __nv_bfloat16>::value)
 #pragma unroll
                             for (int k = 0; k < kKeys / 16; ++k)
                                 mma_ts(tmem + S::tO, tmem + S::tV + 8 * k,
                                        lo_desc + k * ((2 * N * 16) >> 4), idesc, 1);
-                        tc::commit(&o_done);
+                    } else {
+                        constexpr uint32_t idesc = idesc_f16<T>(128, N, true);
+                        const int keys = min(kOwnKeys, own_total - (t - 1 - ct) * kOwnKeys);
+                        const int steps = (keys + 31) / 32 * 2;
+                        for (int k = 0; k < steps; ++k) {
+                            mma_ts(tmem + S::tO, tmem + S::tV + 8 * k,
+                                   p_desc + k * ((2 * N * 16) >> 4), idesc, k > 0 ? 1u : more);
+                            mma_ts(tmem + S::tO, tmem + S::tV + 8 * k,
+                                   lo_desc + k * ((2 * N * 16) >> 4), idesc, 1);
+                        }
                     }
-                    __syncwarp();
+                    mma_commit(&o_done);
                     ++sums;
                 }
             }
-            if (lane == 0)
-                tc::commit(&q_empty[sb]);  // the queries are read
-            __syncwarp();
         }
     } else {
         // ---------------------------------------------------------------- the workers
-        const int wg = warp >> 2, key = tid & 127;
+        const int wg = warp >> 2, quarter = warp & 3, key = tid & 127;
         const int col0 = wg * kCols;  // this thread's columns
-        const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);
+        const uint32_t lanes = tmem + ((uint32_t)quarter << 21);
         uint8_t *p_smem = smem + S::p_off, *lo_smem = smem + S::lo_off;
-        uint32_t ring = 0;             // cached tiles so far
-        uint32_t seen = 0, summed = 0; // tiles whose scores, whose sums were taken
-        uint32_t given = 0;            // tiles whose weights were given
-        auto arrive = [&](uint64_t *bar) {
-            __syncwarp();
-            if (lane == 0)
-                mbar_arrive(bar);
-        };
+        uint32_t ring = 0;    // stages used so far
+        uint32_t seen = 0;    // tiles whose scores were taken and whose weights were given
+        uint32_t summed = 0;  // tiles whose sums were waited for
         auto sync = [&] { named_sync(1, S::workers); };
 
         for (uint32_t seg = 0;; ++seg) {
             const uint32_t sb = seg & 1;
-            wait(&q_full[sb], (seg >> 1) & 1);
+            wait(&seg_full[sb], (seg >> 1) & 1);
             const Segment &g = segs[sb];
             if (g.done)
                 break;
             bool poison = g.wrong != 0;
-            if (tid < D)
-                first_bad[tid] = 0x7FFFFFFF;
-            if (tid == 0)
-                any_bad = 0;
-            if (tid < N) {
-                nref[tid] = -kFar;
-                refz[tid] = kFar;
-                cmul[tid] = 1.0f;
-            }
-            sync();
+            const int begin = g.first;
+            const bool some = begin < g.last;
             uint64_t l2[kCols / 2], pm2[kCols / 2];
 #pragma unroll
             for (int j = 0; j < kCols / 2; ++j)
                 l2[j] = pm2[j] = 0;
-            const int begin = g.first;
+            float k_unit = 1.0f;  // a score's factor for the queries' power of two and the codes'
+            if (some) {
+                // ---- the queries: their sums, and both operands (K-major, 128-byte swizzle)
+                const uint32_t st = ring % S::stages;
+                wait(&full[st], (ring / S::stages) & 1);
+                const uint8_t *raw = smem + st * S::stage_bytes;
+                constexpr int kChunks = N * (D / 8);
+                constexpr int kMine = (kChunks + S::workers - 1) / S::workers;
+                uint4 x[kMine];
+                float big = 0.0f;
+#pragma unroll
+                for (int m = 0; m < kMine; ++m) {
+                    const int i = tid + m * S::workers, n = i / (D / 8), c8 = i % (D / 8);
+                    x[m] = make_uint4(0, 0, 0, 0);
+                    if (i < kChunks && n < g.rows)
+                        x[m] = *reinterpret_cast<const uint4 *>(raw + 16 * i);
+                    float f[8], sum = 0.0f;
+                    const uint32_t xw[4] = {x[m].x, x[m].y, x[m].z, x[m].w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        unpack2<T>(xw[e], f[2 * e], f[2 * e + 1]);
+                        sum += f[2 * e] + f[2 * e + 1];
+                    }
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (fabsf(f[e]) <= 3.4e38f)
+                            big = fmaxf(big, fabsf(f[e]));
+#pragma unroll
+                    for (int s = D / 16; s > 0; s >>= 1)
+                        sum += __shfl_xor_sync(0xFFFFFFFFu, sum, s);
+                    if (i < kChunks && c8 == 0)
+                        sumq[n] = sum;
+                }
+                const uint32_t wbig = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(big));
+                if (lane == 0)
+                    wred[warp][0][0] = __uint_as_float(wbig);
+                if (tid < D)
+                    first_bad[tid] = 0x7FFFFFFF;
+                if (tid == 0)
+                    any_bad = 0;
+                sync();
+#pragma unroll
+                for (int i = 0; i < S::warps; ++i)
+                    big = fmaxf(big, wred[i][0][0]);
+                // 2^-e with e the exponent of the largest, less 13; 0 stays 0
+                const int e = big > 0.0f ? (int)((__float_as_uint(big) >> 23) & 255u) - 127 - 13 : 0;
+                const int e0 = min(max(e, -100), 100);
+                const float q_unit = __uint_as_float((uint32_t)(127 - e0) << 23);
+                k_unit = kCodeUnit * __uint_as_float((uint32_t)(127 + e0) << 23);
+#pragma unroll
+                for (int m = 0; m < kMine; ++m) {
+                    const int i = tid + m * S::workers, n = i / (D / 8), c8 = i % (D / 8);
+                    if (i >= kChunks)
+                        continue;
+                    float f[8];
+                    const uint32_t xw[4] = {x[m].x, x[m].y, x[m].z, x[m].w};
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+                        unpack2<T>(xw[v], f[2 * v], f[2 * v + 1]);
+                    // pairs (c, c + 4); the codes of odd channels are 16 times as large
+                    const float q_odd = q_unit * 0.0625f;
+                    const int at = (c8 >> 3) * (N * 128) + n * 128 + (((c8 & 7) ^ (n & 7)) << 4);
+                    *reinterpret_cast<uint4 *>(smem + S::q16_off + at) =
+                        make_uint4(pack2<__half>(f[0] * q_unit, f[4] * q_unit),
+                                   pack2<__half>(f[1] * q_odd, f[5] * q_odd),
+                                   pack2<__half>(f[2] * q_unit, f[6] * q_unit),
+                                   pack2<__half>(f[3] * q_odd, f[7] * q_odd));
+                    if (g.last > g.ct)
+                        *reinterpret_cast<uint4 *>(smem + S::qt_off + at) = interleave8(x[m]);
+                }
+                fence_async_smem();  // for the first tile's product
+                __syncwarp();
+                if (lane == 0)
+                    mbar_arrive(&empty[st]);
+                ++ring;
+            }
 
             // Tiles [from, to) of the unit, all of them cached or all of them own.  A turn loads
             // the keys of tile t + 1, whose scores are computed while the weights of tile t are
@@ -512,6 +633,9 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 using W = std::conditional_t<kOwn, T, __half>;  // weights and values
                 const int end = kOwn ? g.own : g.cached;
                 const int base = kOwn ? g.ct : 0;
+                const int step = kOwn ? kOwnKeys : kKeys;
+                const float k_factor = kOwn ? a.scale : a.scale * k_unit;
+                int used = 0;  // stages of tile t
 #pragma unroll 1
                 for (int t = from - 1; t < to; ++t) {
                     const bool cur = t >= from;
@@ -522,83 +646,110 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     // tile t's scores being there, the keys' place in tensor memory is free
                     if (t + 1 < to) {
                         const uint32_t tK = lanes + S::tK;
-                        if constexpr (!kOwn) {
-                            const uint32_t r = ring + (cur ? 1 : 0), s1 = r % S::stages;
+                        const uint32_t r0 = ring + (cur ? used : 0);
+                        const int left = end - (t + 1 - base) * step;  // keys from there on
+                        if (!kOwn || 32 * quarter < min(left, kOwnKeys)) {
+                            const uint32_t r = kOwn ? r0 + quarter : r0, s1 = r % S::stages;
                             wait(&full[s1], (r / S::stages) & 1);
-                            poison |= stage_bad[s1] != 0;
-                            const uint8_t *row = smem + s1 * S::stage_bytes + key * (D / 2);
-#pragma unroll
-                            for (int i = 0; i < D / 32; ++i)
-                                if (i * S::C / (D / 32) == wg) {
-                                    const int sw = D == 128 ? (i ^ ((key >> 1) & 3))
-                                                            : (i ^ ((key >> 2) & 1));
-                                    uint32_t y[16];
-                                    unpack32<T>(*reinterpret_cast<const uint4 *>(row + 16 * sw), y);
-                                    tmem_st16(tK + 16 * i, y);
-                                }
-                        } else {
-                            const int j = (t + 1 - base) * kKeys + key;
-                            const bool live = j < end;
-                            const T *row = static_cast<const T *>(a.k_new) + g.b * a.ks.batch +
-                                           (int64_t)(live ? j : 0) * a.ks.token +
-                                           (int64_t)g.h * a.ks.head;
+                            if (!kOwn)
+                                poison |= stage_bad[s1] != 0;
+                            const uint8_t *row = smem + s1 * S::stage_bytes +
+                                                 (kOwn ? lane * S::own_row : key * (D / 2));
 #pragma unroll
                             for (int i = 0; i < D / 32; ++i)
                                 if (i * S::C / (D / 32) == wg) {
                                     uint32_t y[16];
+                                    if constexpr (!kOwn) {
+                                        const int sw = D == 128 ? (i ^ ((key >> 1) & 3))
+                                                                : (i ^ ((key >> 2) & 1));
+                                        unpack32(*reinterpret_cast<const uint4 *>(row + 16 * sw), y);
+                                    } else {
 #pragma unroll
-                                    for (int e = 0; e < 4; ++e) {
-                                        uint4 x = make_uint4(0, 0, 0, 0);
-                                        if (live)
-                                            x = *reinterpret_cast<const uint4 *>(row + 32 * i +
-                                                                                 8 * e);
-                                        x = interleave8(x);
-                                        y[4 * e] = x.x, y[4 * e + 1] = x.y;
-                                        y[4 * e + 2] = x.z, y[4 * e + 3] = x.w;
+                                        for (int v = 0; v < 4; ++v) {
+                                            const uint4 x = interleave8(
+                                                *reinterpret_cast<const uint4 *>(row + 64 * i +
+                                                                                 16 * v));
+                                            y[4 * v] = x.x, y[4 * v + 1] = x.y;
+                                            y[4 * v + 2] = x.z, y[4 * v + 3] = x.w;
+                                        }
                                     }
                                     tmem_st16(tK + 16 * i, y);
                                 }
+                            tmem_wait_st();
                         }
-                        tmem_wait_st();
                         tc::fence_before_sync();
-                        arrive(&k_ready);
+                        __syncwarp();
+                        if (lane == 0)
+                            mbar_arrive(&k_ready);
                     }
-                    if (!cur)
+                    const int keys = min(step, end - (t - base) * step);  // of tile t
+                    if (!cur) {
+                        used = kOwn ? (min(step, end - (t + 1 - base) * step) + 31) / 32 : 1;
                         continue;
+                    }
                     const uint32_t st = ring % S::stages;
                     const uint8_t *buf = smem + st * S::stage_bytes;
                     const uint32_t tS = lanes + S::tS + (seen & 1) * N + col0;
-                    // this thread's key: scale and middle of its range, for scores and weights
-                    const int j0 = (t - base) * kKeys, j = j0 + key;
-                    const bool masked = j0 + kKeys > end || (kOwn && a.causal);
-                    const bool valid = j < end;
-                    float ks = a.scale, ko = 0.0f, vs = 1.0f, vo = 0.0f;
+                    // this thread's key: scale and offset, for scores and weights
+                    const int j = (t - base) * step + key;
+                    const bool masked = keys < kKeys || (kOwn && a.causal);
+                    const bool valid = key < keys;
+                    float ks = k_factor, ko = 0.0f, vs = 1.0f, vo = 0.0f;
                     if constexpr (!kOwn) {
                         const uint32_t *f =
                             reinterpret_cast<const uint32_t *>(buf + 2 * S::code_bytes) + key;
                         const uint32_t fk = f[0], fv = f[kKeys];
-                        ks = bf16_low(fk) * a.scale;
-                        ko = fmaf(8.0f, bf16_low(fk), bf16_high(fk)) * a.scale;
+                        ks = bf16_low(fk) * k_factor;
+                        ko = bf16_high(fk) * a.scale;
                         vs = bf16_low(fv);
-                        vo = fmaf(8.0f, vs, bf16_high(fv));
+                        vo = bf16_high(fv);
                         if (!valid)
                             ks = ko = vs = vo = 0.0f;
                     }
+                    // values' codes of odd slots are 16 times as large: their weights are not
+                    const float vw = kOwn || (key & 1) ? vs : 16.0f * vs;
                     // the rows of this thread that see its key: those from first_col on
                     const int first_col = !valid || (kOwn && a.causal && j >= a.Lq) ? kCols
                                           : kOwn && a.causal ? j * a.group - (g.r0 + col0)
                                                              : 0;
+                    if (t == begin) {
+                        // ---- the references: the score of the tile's first key, where the row
+                        // sees it
+                        if (quarter == 0) {
+                            const float lv = vs > 0.0f ? log2f(vs) : kFar;
+#pragma unroll
+                            for (int c8 = 0; c8 < kCols; c8 += 8) {
+                                uint32_t s[8];
+                                tmem_ld<8>(tS + c8, s);
+                                if (lane != 0)
+                                    continue;
+#pragma unroll
+                                for (int c = 0; c < 8; ++c) {
+                                    const int n = col0 + c8 + c;
+                                    const float x = fmaf(__uint_as_float(s[c]), ks, ko * sumq[n]);
+                                    const float ref = c8 + c < first_col ? kFar
+                                                      : fabsf(x) < 1e30f ? x
+                                                                         : 0.0f;
+                                    const float z = fmaxf(ref + lv, ref - kMaxShift);
+                                    nref[n] = -ref;
+                                    refz[n] = z;
+                                    cmul[n] = ref == kFar ? 1.0f : exp2f(ref - z);
+                                }
+                            }
+                        }
+                        sync();
+                    }
                     uint32_t ph[kCols / 2], pl[kSplit ? kCols / 2 : 1];
                     // Weights of this thread's columns, and their sums.  The second time (after
                     // the references moved) only the rows of `redo` are summed again.
                     auto weights = [&](auto again) -> float {
                         constexpr bool kAgain = decltype(again)::value;
-                        const float4 *sq4 = reinterpret_cast<const float4 *>(sumq[sb] + col0);
+                        const float4 *sq4 = reinterpret_cast<const float4 *>(sumq + col0);
                         const float4 *nr4 = reinterpret_cast<const float4 *>(nref + col0);
                         const float4 *cm4 = reinterpret_cast<const float4 *>(cmul + col0);
                         const float4 *rd4 = reinterpret_cast<const float4 *>(redo + col0);
                         const uint64_t ks2 = f2(ks, ks), ko2 = f2(ko, ko);
-                        const uint64_t vs2 = f2(vs, vs), vo2 = f2(vo, vo);
+                        const uint64_t vw2 = f2(vw, vw), vo2 = f2(vo, vo);
                         float top = 0.0f;
 #pragma unroll
                         for (int c8 = 0; c8 < kCols; c8 += 8) {
@@ -644,7 +795,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                                         if constexpr (!kOwn)
                                             pm2[i] = fma2(p, vo2, pm2[i]);
                                     }
-                                    un2(mul2(p, kOwn ? cm2[e] : mul2(vs2, cm2[e])), z0, z1);
+                                    un2(mul2(p, kOwn ? cm2[e] : mul2(vw2, cm2[e])), z0, z1);
                                     top = fmaxf(top, fmaxf(fmaxf(y0, y1), fmaxf(z0, z1)));
                                     ph[i] = pack2<W>(z0, z1);
                                     if constexpr (kSplit) {
@@ -657,8 +808,18 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                         }
                         return top;
                     };
-                    const bool over =
-                        __any_sync(0xFFFFFFFFu, weights(std::false_type{}) > kTopWeight);
+                    const bool busy = 32 * quarter < keys;  // some key of this warp exists
+                    bool over = false;
+                    if (busy) {
+                        over = __any_sync(0xFFFFFFFFu, weights(std::false_type{}) > kTopWeight);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < kCols / 2; ++i) {
+                            ph[i] = 0;
+                            if constexpr (kSplit)
+                                pl[i] = 0;
+                        }
+                    }
                     if (lane == 0) {
                         if (over)
                             *reinterpret_cast<volatile uint32_t *>(&vote[seen & 1]) = seen + 1;
@@ -666,18 +827,21 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     }
                     __syncwarp();
                     // ---- the values; the sums of the tile before must have read theirs
-                    if (given > summed) {
+                    if (seen > summed) {
                         wait(&o_done, summed & 1);
                         ++summed;
                         tc::fence_after_sync();
                     }
+                    if (kOwn && t == from && from > begin)
+                        scale_sums<kCols>(lanes + S::tO + col0, nullptr, kSumUnit);
                     if (D == 128 || key < D) {
                         const uint32_t tV = lanes + S::tV;
                         const int d = key;
-                        if constexpr (!kOwn) {
-#pragma unroll
-                            for (int q = 0; q < 4 / S::C; ++q) {
-                                const int i = wg * (4 / S::C) + q;  // 32 slots
+#pragma unroll(kOwn ? 1 : 4 / S::C)
+                        for (int q = 0; q < 4 / S::C; ++q) {
+                            const int i = wg * (4 / S::C) + q;  // 32 slots
+                            uint32_t y[16];
+                            if constexpr (!kOwn) {
                                 int off;
                                 if (a.c.page_shift == 5)
                                     off = i * (16 * D) + d * 16;
@@ -686,27 +850,24 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                                           (((i & 1) ^ ((d >> 2) & 1)) << 4);
                                 else
                                     off = d * 64 + ((i ^ ((d >> 1) & 3)) << 4);
-                                uint32_t y[16];
-                                unpack32<__half>(*reinterpret_cast<const uint4 *>(
-                                                     buf + S::code_bytes + off),
-                                                 y);
-                                tmem_st16(tV + 16 * i, y);
-                            }
-                        } else {
-#pragma unroll 1
-                            for (int q = 0; q < 4 / S::C; ++q) {
-                                const int i = wg * (4 / S::C) + q;
-                                const uint16_t *v = static_cast<const uint16_t *>(a.v_new) +
-                                                    g.b * a.vs.batch + (int64_t)g.h * a.vs.head + d;
-                                uint32_t y[16];
-                                const int bad =
-                                    own_values<T>(v, a.vs.token, j0 + 32 * i, end, y);
-                                if (bad < end) {
-                                    atomicMin(&first_bad[d], bad);
+                                unpack32(*reinterpret_cast<const uint4 *>(buf + S::code_bytes + off),
+                                         y);
+                            } else {
+                                if (32 * i >= keys)
+                                    break;
+                                const uint32_t r = ring + i, s1 = r % S::stages;
+                                wait(&full[s1], (r / S::stages) & 1);
+                                const int bad = own_values<T>(
+                                    reinterpret_cast<const T *>(smem + s1 * S::stage_bytes +
+                                                                S::own_v) +
+                                        d,
+                                    D, keys - 32 * i, y);
+                                if (bad < 32) {
+                                    atomicMin(&first_bad[d], (t - base) * step + 32 * i + bad);
                                     any_bad = 1;
                                 }
-                                tmem_st16(tV + 16 * i, y);
                             }
+                            tmem_st16(tV + 16 * i, y);
                         }
                     }
                     wait(&voted, seen & 1);
@@ -724,7 +885,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
 #pragma unroll
                                 for (int c = 0; c < 8; ++c) {
                                     const float x = fmaf(__uint_as_float(s[c]), ks,
-                                                         ko * sumq[sb][col0 + c8 + c]);
+                                                         ko * sumq[col0 + c8 + c]);
                                     m[c8 + c] = c8 + c >= first_col ? x + (z ? lv : 0.0f)
                                                                     : neg_inf_f();
                                 }
@@ -758,19 +919,8 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                             cmul[tid] = exp2f(to_ref - to_z);
                         }
                         sync();
-                        if (t > begin) {  // the sums of the tiles before (waited for above)
-                            const uint32_t tO = lanes + S::tO + col0;
-#pragma unroll 1
-                            for (int c8 = 0; c8 < kCols; c8 += 8) {
-                                uint32_t s[8];
-                                tmem_ld<8>(tO + c8, s);
-#pragma unroll
-                                for (int c = 0; c < 8; ++c)
-                                    s[c] = __float_as_uint(__uint_as_float(s[c]) *
-                                                           fo[col0 + c8 + c]);
-                                tmem_st<8>(tO + c8, s);
-                            }
-                        }
+                        if (t > begin)  // the sums of the tiles before (waited for above)
+                            scale_sums<kCols>(lanes + S::tO + col0, fo + col0, 1.0f);
 #pragma unroll
                         for (int c = 0; c < kCols / 2; ++c) {
                             float x0, x1, m0, m1;
@@ -785,18 +935,22 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                             l2[c] = f2(x0, x1);
                             pm2[c] = f2(m0, m1);
                         }
-                        weights(std::true_type{});
+                        if (busy)
+                            weights(std::true_type{});
                     }
-                    // ---- the weights
-                    const int kappa = (key & ~7) | ((key & 3) << 1) | ((key >> 2) & 1);
-                    const int at = (kappa >> 3) * (N * 16) + (col0 >> 3) * 128 + (kappa & 7) * 16;
+                    // ---- the weights (own tiles: the rows of absent stages are not read)
+                    if (!kOwn || busy) {
+                        const int kappa = (key & ~7) | ((key & 3) << 1) | ((key >> 2) & 1);
+                        const int at =
+                            (kappa >> 3) * (N * 16) + (col0 >> 3) * 128 + (kappa & 7) * 16;
 #pragma unroll
-                    for (int q = 0; q < kCols / 8; ++q) {
-                        *reinterpret_cast<uint4 *>(p_smem + at + 128 * q) =
-                            make_uint4(ph[4 * q], ph[4 * q + 1], ph[4 * q + 2], ph[4 * q + 3]);
-                        if constexpr (kSplit)
-                            *reinterpret_cast<uint4 *>(lo_smem + at + 128 * q) =
-                                make_uint4(pl[4 * q], pl[4 * q + 1], pl[4 * q + 2], pl[4 * q + 3]);
+                        for (int q = 0; q < kCols / 8; ++q) {
+                            *reinterpret_cast<uint4 *>(p_smem + at + 128 * q) =
+                                make_uint4(ph[4 * q], ph[4 * q + 1], ph[4 * q + 2], ph[4 * q + 3]);
+                            if constexpr (kSplit)
+                                *reinterpret_cast<uint4 *>(lo_smem + at + 128 * q) = make_uint4(
+                                    pl[4 * q], pl[4 * q + 1], pl[4 * q + 2], pl[4 * q + 3]);
+                        }
                     }
                     tmem_wait_st();
                     fence_async_smem();
@@ -804,16 +958,17 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     __syncwarp();
                     if (lane == 0) {
                         mbar_arrive(&p_ready);
-                        if (!kOwn)
-                            mbar_arrive(&empty[st]);
+                        for (int i = 0; i < used; ++i)
+                            mbar_arrive(&empty[(ring + i) % S::stages]);
                     }
                     ++seen;
-                    ++given;
-                    ring += kOwn ? 0 : 1;
+                    ring += used;
+                    if (kOwn)
+                        used = (min(step, end - (t + 1 - base) * step) + 31) / 32;
                 }
             };
-            tiles(std::false_type{}, min(g.first, g.ct), min(g.last, g.ct));
-            tiles(std::true_type{}, max(g.first, g.ct), max(g.last, g.ct));
+            tiles(std::false_type{}, min(begin, g.ct), min(g.last, g.ct));
+            tiles(std::true_type{}, max(begin, g.ct), max(g.last, g.ct));
 
             // ---- the end of the segment: sums over the keys, then the channels' results
 #pragma unroll 1
@@ -826,15 +981,8 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 if (lane < kCols)
                     wred[warp][z][lane] = x[0];
             }
-            const bool some = g.first < g.last;
-            if (given > summed) {
-                wait(&o_done, summed & 1);
-                ++summed;
-            }
-            tc::fence_after_sync();
             sync();
             const bool whole = g.starts && g.ends;
-            const int64_t part = ((int64_t)blockIdx.x * 2 + (g.starts ? 1 : 0)) * N;
             if (tid < g.rows) {
                 const int w4 = tid / kCols * 4, c = tid % kCols;
                 float sum = 0.0f, off = 0.0f;
@@ -845,22 +993,30 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 }
                 if (poison)
                     sum = nan_f();
-                const float ref = -nref[tid];
-                const float f = some ? exp2f(refz[tid] - ref) : 0.0f;
+                const bool none = !some || sum == 0.0f;
+                const float ref = none ? kFar : -nref[tid];
+                const float f =
+                    none ? 0.0f : exp2f(refz[tid] - ref) * (g.last > g.ct ? 1.0f : kSumUnit);
                 if (whole) {
-                    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+                    const int r = g.r0 + tid, qi = r / a.group;
+                    const int64_t row =
+                        ((int64_t)g.b * a.Lq + qi) * a.Hq + g.h * a.group + r - qi * a.group;
+                    const float inv = none ? 0.0f : 1.0f / sum;
+                    row_at[tid] = row * D;
                     fl[tid] = off * inv;
                     fo[tid] = f * inv;
-                    if (a.lse) {
-                        const int r = g.r0 + tid, qi = r / a.group;
-                        a.lse[((int64_t)g.b * a.Lq + qi) * a.Hq + g.h * a.group + r - qi * a.group] =
-                            sum == 0.0f ? neg_inf_f() : (ref + log2f(sum)) * 0.6931471805599453f;
-                    }
+                    if (a.lse)
+                        a.lse[row] = none ? (poison ? nan_f() : neg_inf_f())
+                                          : (ref + log2f(sum)) * 0.6931471805599453f;
+                    if (poison)
+                        fl[tid] = nan_f();
                 } else {
+                    const int64_t at = ((int64_t)blockIdx.x * 2 + (g.starts ? 1 : 0)) * N + tid;
+                    row_at[tid] = at * D;
                     fl[tid] = off;
                     fo[tid] = f;
-                    a.part_refs[2 * (part + tid)] = ref;
-                    a.part_refs[2 * (part + tid) + 1] = sum;
+                    a.part_refs[2 * at] = ref;
+                    a.part_refs[2 * at + 1] = sum;
                 }
             }
             if (tid == 0 && !whole) {
@@ -873,38 +1029,39 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     meta[kContEnds] = g.ends;
                 }
             }
+            if (seen > summed) {
+                wait(&o_done, summed & 1);
+                ++summed;
+            }
+            tc::fence_after_sync();
             sync();
             const int d = key;
-            int qi = (g.r0 + col0) / a.group, gi = g.r0 + col0 - qi * a.group;
+            const int bad = some && any_bad ? first_bad[min(d, D - 1)] : 0x7FFFFFFF;
 #pragma unroll 1
             for (int c8 = 0; c8 < kCols; c8 += 8) {
                 uint32_t o[8] = {0, 0, 0, 0, 0, 0, 0, 0};
                 if (some)
                     tmem_ld<8>(lanes + S::tO + col0 + c8, o);
+                if (D == 128 || d < D)
 #pragma unroll
-                for (int c = 0; c < 8; ++c) {
-                    const int n = col0 + c8 + c;
-                    if (n < g.rows && d < D) {
-                        float x = fmaf(__uint_as_float(o[c]), fo[n], fl[n]);
-                        if (any_bad && first_bad[d] <= (a.causal ? qi : 0x7FFFFFFE))
-                            x = nan_f();
-                        if (whole)
-                            static_cast<T *>(
-                                a.out)[(((int64_t)g.b * a.Lq + qi) * a.Hq + g.h * a.group + gi) * D +
-                                       d] = from_float<T>(x);
-                        else
-                            a.parts[(part + n) * D + d] = x;
+                    for (int c = 0; c < 8; ++c) {
+                        const int n = col0 + c8 + c;
+                        if (n < g.rows) {
+                            float x = fmaf(__uint_as_float(o[c]), fo[n], fl[n]);
+                            if (bad != 0x7FFFFFFF && (!a.causal || bad <= (g.r0 + n) / a.group))
+                                x = nan_f();
+                            if (whole)
+                                static_cast<T *>(a.out)[row_at[n] + d] = from_float<T>(x);
+                            else
+                                a.parts[row_at[n] + d] = x;
+                        }
                     }
-                    if (++gi == a.group) {
-                        gi = 0;
-                        ++qi;
-                    }
-                }
             }
             tc::fence_before_sync();
             sync();  // the next segment overwrites the references and its sums
             tc::fence_after_sync();
-            arrive(&q_empty[sb]);
+            if (lane == 0)
+                mbar_arrive(&seg_empty[sb]);
         }
     }
     tc::fence_before_sync();

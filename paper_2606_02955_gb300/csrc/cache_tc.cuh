@@ -101,40 +101,21 @@ __device__ __forceinline__ void unpack2(uint32_t w, float &lo, float &hi)
 // Inside every group of eight, the contraction runs over elements 0 4 1 5 2 6 3 7: the order in
 // which masking a word of eight 4-bit codes yields pairs.
 //
-// A word's codes minus 8 as four pairs of T.  A code is put into the low bits of a number whose
-// last place is 1 (128 in bf16, 1024 in fp16; 1024 with last place 16 for the code's upper
-// position) and the constant taken off again: exact.
-template <typename T>
-__device__ __forceinline__ void unpack8(uint32_t w, uint32_t *y)
-{
-    if constexpr (__is_same(T, __nv_bfloat16)) {
-        const uint32_t minus = 0xC308C308u;  // -136
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t x = ((w >> (4 * j)) & 0x000F000Fu) | 0x43004300u;
-            asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(y[j]) : "r"(x), "r"(minus));
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const uint32_t v = w >> (8 * j);
-            const uint32_t lo = (v & 0x000F000Fu) | 0x64006400u;
-            const uint32_t hi = (v & 0x00F000F0u) | 0x64006400u;
-            asm("add.rn.f16x2 %0, %1, %2;" : "=r"(y[2 * j]) : "r"(lo), "r"(0xE408E408u));  // -1032
-            asm("fma.rn.f16x2 %0, %1, %2, %3;"                                  // / 16 - 72
-                : "=r"(y[2 * j + 1])
-                : "r"(hi), "r"(0x2C002C00u), "r"(0xD480D480u));
-        }
-    }
-}
-
-template <typename T>
+// A word's codes as four fp16 pairs, unconverted: four bits in a number's lowest places are the
+// subnormal code * 2^-24, exactly.  The codes of odd place are left in the next four bits, 16
+// times as much; the other operand makes up for both (a mask a pair, one shift a word; taking
+// the constant off a number with the code in its last places took twice as many instructions).
+constexpr float kCodeUnit = 16777216.0f;  // 2^24
 __device__ __forceinline__ void unpack32(const uint4 x, uint32_t (&y)[16])
 {
-    unpack8<T>(x.x, y);
-    unpack8<T>(x.y, y + 4);
-    unpack8<T>(x.z, y + 8);
-    unpack8<T>(x.w, y + 12);
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        y[4 * i] = w[i] & 0x000F000Fu;
+        y[4 * i + 1] = w[i] & 0x00F000F0u;
+        y[4 * i + 2] = (w[i] >> 8) & 0x000F000Fu;
+        y[4 * i + 3] = (w[i] >> 8) & 0x00F000F0u;
+    }
 }
 
 // Eight 16-bit values in the same order.
@@ -223,15 +204,29 @@ __device__ __forceinline__ constexpr uint32_t idesc_f16(int M, int N, bool b_mn)
            (uint32_t(M >> 4) << 24);
 }
 
-// D[tmem] (+)= A[tmem] * B[smem] for one K = 16 slice; issued by one thread.
+// D[tmem] (+)= A[tmem] * B[smem] for one K = 16 slice, and a commit of all of them.  The whole
+// warp calls these with the same operands and one lane of it issues: operands that the compiler
+// knows to be uniform need no move of registers (N = 32: 17 cycles a product; issued under
+// `if (lane == 0)` 47, whatever N).
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc,
                                        uint32_t accumulate)
 {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
+        "{\n\t.reg .pred p, e;\n\t.reg .b32 x;\n\t"
+        "elect.sync x|e, 0xffffffff;\n\t"
         "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
         "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
+__device__ __forceinline__ void mma_commit(uint64_t *bar)
+{
+    asm volatile(
+        "{\n\t.reg .pred e;\n\t.reg .b32 x;\n\t"
+        "elect.sync x|e, 0xffffffff;\n\t"
+        "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(
+            smem_addr(bar))
         : "memory");
 }
 

@@ -5,10 +5,11 @@ shared with the library's code.  Tolerances used with them (fixed before the fir
 
   * attention output: half an ulp of the output type (its unit roundoff: 2^-8 for bfloat16's 8
     significant bits, 2^-11 for fp16's 11); the weights' rounding to fp16 (2^-11) times what
-    they multiply (codes about the middle of the row's range: up to 8 scales; own values: |v|);
-    scores off by `d` change a weight by at most a factor e^(2 d).
-    Scores are fp32 sums of D products: d = 2^-19 * scale * max_j sum_c |q_c k_c|, which leaves
-    the sum 32 roundings of its largest partial sum.
+    they multiply (codes: up to 15 scales of the row; own values: |v|); scores off by `d` change
+    a weight by at most a factor e^(2 d).
+    Scores are fp32 sums of products of queries with codes, up to 15 scales, and of the row's
+    offset: d = 2^-21 * scale * max_j sum_c |q_c| (|offset_j| + 15 scale_j), which leaves the sum
+    8 roundings of its largest partial sum (own keys: |k| in the bracket's place).
   * lse: d, and four fp32 roundings of the result.
   * key weights: the same 2 d on every term, and n fp32 roundings of the sum.
 """
@@ -57,11 +58,18 @@ def sequence(dense, table_row, page, n):
     return x.reshape(dense.shape[1], -1, dense.shape[3])[:, :n]
 
 
+def row_reach(affine, D):
+    """|offset| + 15 scale of every cached row, as [pages, heads, page, D]."""
+    f = affine.cpu().double()
+    return (f[..., 1:].abs() + 15 * f[..., :1]).expand(-1, -1, -1, D)
+
+
 def attention(q, cache, table, lens, k_new=None, v_new=None, new_lens=None, causal=False,
               scale=None):
     """(out, lse, tolerance of out, tolerance of lse), fp64 on the CPU."""
     kd, vd = unpack_cache(cache)
-    half = (8 * cache.v_affine[..., :1].cpu().double()).expand(-1, -1, -1, cache.head_dim)
+    k_reach = row_reach(cache.k_affine, cache.head_dim)
+    v_reach = (15 * cache.v_affine[..., :1].cpu().double()).expand(-1, -1, -1, cache.head_dim)
     q64 = q.cpu().double()
     B, Lq, Hq, D = q64.shape
     group = Hq // cache.heads
@@ -72,26 +80,26 @@ def attention(q, cache, table, lens, k_new=None, v_new=None, new_lens=None, caus
     tol_lse = torch.zeros_like(lse)
     for b in range(B):
         n = int(lens[b])
-        k, v = sequence(kd, table[b], cache.page_size, n), sequence(vd, table[b], cache.page_size, n)
-        size = torch.maximum(v.abs(), sequence(half, table[b], cache.page_size, n))
+        k, v, kr, vr = (sequence(x, table[b], cache.page_size, n) for x in (kd, vd, k_reach, v_reach))
+        vr = torch.maximum(v.abs(), vr)
         m = 0
         if k_new is not None:
             m = k_new.shape[1] if new_lens is None else int(new_lens[b])
-            k = torch.cat((k, k_new[b, :m].cpu().double().transpose(0, 1)), 1)
-            v = torch.cat((v, v_new[b, :m].cpu().double().transpose(0, 1)), 1)
-            size = torch.cat((size, v_new[b, :m].cpu().double().abs().transpose(0, 1)), 1)
+            own_k, own_v = (x[b, :m].cpu().double().transpose(0, 1) for x in (k_new, v_new))
+            k, v = torch.cat((k, own_k), 1), torch.cat((v, own_v), 1)
+            kr, vr = torch.cat((kr, own_k.abs()), 1), torch.cat((vr, own_v.abs()), 1)
         for h in range(Hq):
-            kh, vh = k[h // group], v[h // group]
+            kh, vh, krh, vrh = (x[h // group] for x in (k, v, kr, vr))
             for i in range(Lq):
                 seen = n + (min(m, i + 1) if causal else m)
                 if seen == 0:
                     continue
                 x = kh[:seen] @ q64[b, i, h] * scale
-                d = 2.0 ** -19 * abs(scale) * float((kh[:seen].abs() @ q64[b, i, h].abs()).max())
+                d = 2.0 ** -21 * abs(scale) * float((krh[:seen] @ q64[b, i, h].abs()).max())
                 lse[b, i, h] = torch.logsumexp(x, 0)
                 p = torch.softmax(x, 0)
                 out[b, i, h] = p @ vh[:seen]
-                spread = p @ size[h // group, :seen]
+                spread = p @ vrh[:seen]
                 tol[b, i, h] = EPS[q.dtype] * out[b, i, h].abs() + (2.0 ** -11 + 2 * d) * spread + 1e-30
                 tol_lse[b, i, h] = d + 4 * 2.0 ** -24 * max(1.0, abs(float(lse[b, i, h]))) + 1e-6
     return out, lse, tol, tol_lse
@@ -100,6 +108,7 @@ def attention(q, cache, table, lens, k_new=None, v_new=None, new_lens=None, caus
 def key_weights(q, lse, cache, table, lens, weights, scale=None):
     """(weights, tolerance) fp64 [B, heads, max_len]."""
     kd, _ = unpack_cache(cache)
+    k_reach = row_reach(cache.k_affine, cache.head_dim)
     q64, lse64 = q.cpu().double(), lse.cpu().double()
     B, Lq, Hq, D = q64.shape
     group = Hq // cache.heads
@@ -109,12 +118,13 @@ def key_weights(q, lse, cache, table, lens, weights, scale=None):
     for b in range(B):
         n = int(lens[b])
         k = sequence(kd, table[b], cache.page_size, n)
+        kr = sequence(k_reach, table[b], cache.page_size, n)
         for h in range(cache.heads):
             qh = q64[b, :, h * group:(h + 1) * group].reshape(-1, D)
             ls = lse64[b, :, h * group:(h + 1) * group].reshape(-1, 1)
             p = torch.exp(qh @ k[h].t() * scale - ls)
             p = torch.where(torch.isinf(ls) & (ls < 0), torch.zeros_like(p), p)
-            d = 2.0 ** -19 * abs(scale) * (qh.abs() @ k[h].abs().t())
+            d = 2.0 ** -21 * abs(scale) * (qh.abs() @ kr[h].t())
             # exp's argument, in base 2: two roundings of it and of the exponential
             d = d + 2.0 ** -22 * (2 + torch.nan_to_num(ls, neginf=0.0).abs() + (qh @ k[h].t() * scale).abs())
             w[b, h, :n] = weights[b, h, :n].cpu().double() + p.sum(0)
