@@ -227,7 +227,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
     __shared__ __align__(8) uint64_t seg_full[2], seg_empty[2];
     __shared__ __align__(8) uint64_t k_ready, s_done, p_ready, o_done, voted;
     __shared__ uint32_t tmem_base;
-    __shared__ uint8_t stage_bad[S::stages];
+    __shared__ int bad_page[2];                                 // a segment met one
     __shared__ int64_t scan[S::threads / 32];
     __shared__ int64_t find_base;
     __shared__ int find_b;
@@ -237,6 +237,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
     // reference of the scaled weights
     __shared__ __align__(16) float sumq[N], nref[N], cmul[N], refz[N];
     __shared__ __align__(16) float fl[N], fo[N], redo[N];
+    __shared__ __align__(16) float none_row[S::cols];  // -inf: the references of absent keys
     __shared__ int64_t row_at[N];
     __shared__ float wred[S::warps][2][kCols];
     __shared__ int first_bad[D];  // first own key of the segment with a non-finite value
@@ -260,6 +261,8 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
         mbar_init(&voted, S::warps);
         fence_mbar_init();
     }
+    if (tid < S::cols)
+        none_row[tid] = neg_inf_f();
     if (warp == S::warps)
         tc::tmem_alloc(&tmem_base, S::tmem);
     if (tid == S::workers + 32) {
@@ -353,6 +356,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     g.ct = w.s.ct, g.cached = w.s.cached, g.own = w.s.own;
                     g.starts = w.first == 0, g.ends = w.last == w.s.tiles;
                     g.wrong = w.s.wrong;
+                    bad_page[sb] = 0;
                 }
                 mbar_arrive(&seg_full[sb]);
             }
@@ -400,7 +404,8 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 const uint32_t there = __ballot_sync(0xFFFFFFFFu, mine);
                 const bool bad = __any_sync(0xFFFFFFFFu, lane < pieces && pg == -1);
                 if (lane == 0) {
-                    stage_bad[st] = bad;
+                    if (bad)
+                        bad_page[sb] = 1;
                     if (!dead && there)
                         mbar_arrive_expect_tx(&full[st],
                                               (uint32_t)__popc(there) * span * (D + 8));
@@ -538,7 +543,6 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
             const Segment &g = segs[sb];
             if (g.done)
                 break;
-            bool poison = g.wrong != 0;
             const int begin = g.first;
             const bool some = begin < g.last;
             uint64_t l2[kCols / 2], pm2[kCols / 2];
@@ -646,13 +650,11 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     // tile t's scores being there, the keys' place in tensor memory is free
                     if (t + 1 < to) {
                         const uint32_t tK = lanes + S::tK;
-                        const uint32_t r0 = ring + (cur ? used : 0);
+                        const uint32_t r0 = ring + (cur ? (kOwn ? used : 1) : 0);
                         const int left = end - (t + 1 - base) * step;  // keys from there on
                         if (!kOwn || 32 * quarter < min(left, kOwnKeys)) {
                             const uint32_t r = kOwn ? r0 + quarter : r0, s1 = r % S::stages;
                             wait(&full[s1], (r / S::stages) & 1);
-                            if (!kOwn)
-                                poison |= stage_bad[s1] != 0;
                             const uint8_t *row = smem + s1 * S::stage_bytes +
                                                  (kOwn ? lane * S::own_row : key * (D / 2));
 #pragma unroll
@@ -666,9 +668,10 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                                     } else {
 #pragma unroll
                                         for (int v = 0; v < 4; ++v) {
-                                            const uint4 x = interleave8(
-                                                *reinterpret_cast<const uint4 *>(row + 64 * i +
-                                                                                 16 * v));
+                                            uint4 x = make_uint4(0, 0, 0, 0);
+                                            if (key < left)
+                                                x = interleave8(*reinterpret_cast<const uint4 *>(
+                                                    row + 64 * i + 16 * v));
                                             y[4 * v] = x.x, y[4 * v + 1] = x.y;
                                             y[4 * v + 2] = x.z, y[4 * v + 3] = x.w;
                                         }
@@ -692,7 +695,6 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     const uint32_t tS = lanes + S::tS + (seen & 1) * N + col0;
                     // this thread's key: scale and offset, for scores and weights
                     const int j = (t - base) * step + key;
-                    const bool masked = keys < kKeys || (kOwn && a.causal);
                     const bool valid = key < keys;
                     float ks = k_factor, ko = 0.0f, vs = 1.0f, vo = 0.0f;
                     if constexpr (!kOwn) {
@@ -716,25 +718,33 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                         // ---- the references: the score of the tile's first key, where the row
                         // sees it
                         if (quarter == 0) {
-                            const float lv = vs > 0.0f ? log2f(vs) : kFar;
+                            // lane c takes column c of lane 0's key
+                            float x = 0.0f;
 #pragma unroll
                             for (int c8 = 0; c8 < kCols; c8 += 8) {
                                 uint32_t s[8];
                                 tmem_ld<8>(tS + c8, s);
-                                if (lane != 0)
-                                    continue;
 #pragma unroll
                                 for (int c = 0; c < 8; ++c) {
-                                    const int n = col0 + c8 + c;
-                                    const float x = fmaf(__uint_as_float(s[c]), ks, ko * sumq[n]);
-                                    const float ref = c8 + c < first_col ? kFar
-                                                      : fabsf(x) < 1e30f ? x
-                                                                         : 0.0f;
-                                    const float z = fmaxf(ref + lv, ref - kMaxShift);
-                                    nref[n] = -ref;
-                                    refz[n] = z;
-                                    cmul[n] = ref == kFar ? 1.0f : exp2f(ref - z);
+                                    const uint32_t o = __shfl_sync(0xFFFFFFFFu, s[c], 0);
+                                    x = lane == c8 + c ? __uint_as_float(o) : x;
                                 }
+                            }
+                            const float ks_0 = __shfl_sync(0xFFFFFFFFu, ks, 0);
+                            const float ko_0 = __shfl_sync(0xFFFFFFFFu, ko, 0);
+                            const float vs_0 = __shfl_sync(0xFFFFFFFFu, vs, 0);
+                            const int col_0 = __shfl_sync(0xFFFFFFFFu, first_col, 0);
+                            if (lane < kCols) {
+                                const int n = col0 + lane;
+                                x = fmaf(x, ks_0, ko_0 * sumq[n]);
+                                const float lv = vs_0 > 0.0f ? log2f(vs_0) : kFar;
+                                const float ref = lane < col_0        ? kFar
+                                                  : fabsf(x) < 1e30f ? x
+                                                                     : 0.0f;
+                                const float z = fmaxf(ref + lv, ref - kMaxShift);
+                                nref[n] = -ref;
+                                refz[n] = z;
+                                cmul[n] = ref == kFar ? 1.0f : exp2f(ref - z);
                             }
                         }
                         sync();
@@ -745,7 +755,8 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     auto weights = [&](auto again) -> float {
                         constexpr bool kAgain = decltype(again)::value;
                         const float4 *sq4 = reinterpret_cast<const float4 *>(sumq + col0);
-                        const float4 *nr4 = reinterpret_cast<const float4 *>(nref + col0);
+                        const float4 *nr4 =
+                            reinterpret_cast<const float4 *>(valid ? nref + col0 : none_row);
                         const float4 *cm4 = reinterpret_cast<const float4 *>(cmul + col0);
                         const float4 *rd4 = reinterpret_cast<const float4 *>(redo + col0);
                         const uint64_t ks2 = f2(ks, ks), ko2 = f2(ko, ko);
@@ -778,7 +789,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                                                 __uint_as_float(s[2 * i + 1 - c8])),
                                              ks2, y[e]),
                                         y0, y1);
-                                    if (masked) {
+                                    if constexpr (kOwn) {
                                         y0 = 2 * i >= first_col ? y0 : neg_inf_f();
                                         y1 = 2 * i + 1 >= first_col ? y1 : neg_inf_f();
                                     }
@@ -796,7 +807,8 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                                             pm2[i] = fma2(p, vo2, pm2[i]);
                                     }
                                     un2(mul2(p, kOwn ? cm2[e] : mul2(vw2, cm2[e])), z0, z1);
-                                    top = fmaxf(top, fmaxf(fmaxf(y0, y1), fmaxf(z0, z1)));
+                                    top = max3(top, y0, y1);
+                                    top = max3(top, z0, z1);
                                     ph[i] = pack2<W>(z0, z1);
                                     if constexpr (kSplit) {
                                         float h0, h1;
@@ -958,11 +970,14 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     __syncwarp();
                     if (lane == 0) {
                         mbar_arrive(&p_ready);
-                        for (int i = 0; i < used; ++i)
-                            mbar_arrive(&empty[(ring + i) % S::stages]);
+                        if constexpr (!kOwn)
+                            mbar_arrive(&empty[st]);
+                        else
+                            for (int i = 0; i < used; ++i)
+                                mbar_arrive(&empty[(ring + i) % S::stages]);
                     }
                     ++seen;
-                    ring += used;
+                    ring += kOwn ? used : 1;
                     if (kOwn)
                         used = (min(step, end - (t + 1 - base) * step) + 31) / 32;
                 }
@@ -983,6 +998,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
             }
             sync();
             const bool whole = g.starts && g.ends;
+            const bool poison = g.wrong || bad_page[sb];
             if (tid < g.rows) {
                 const int w4 = tid / kCols * 4, c = tid % kCols;
                 float sum = 0.0f, off = 0.0f;
@@ -1072,58 +1088,91 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
 }
 
 // Joins the partials of the unit that CTA blockIdx.x of the attention began and did not finish:
-// its slot 1, then slot 0 of the CTAs after it up to the one where the unit ends.  A block takes
-// kJoinRows rows, a thread a channel.
-constexpr int kJoinRows = 8;
+// its slot 1, then slot 0 of the CTAs after it up to the one where the unit ends.  A warp takes a
+// row, a lane D / 32 channels; the parts' factors are computed a lane each.
+constexpr int kJoinWarps = 8;
 
-template <typename T>
-__global__ void __launch_bounds__(128) combine_kernel(const __grid_constant__ AttnArgs a, int N,
-                                                      int grid)
+template <typename T, int D>
+__global__ void __launch_bounds__(32 * kJoinWarps)
+    combine_kernel(const __grid_constant__ AttnArgs a, int N, int grid)
 {
+    constexpr int kV = D / 32;
+    using V = std::conditional_t<kV == 4, float4, float2>;
     pdl_wait();
-    const int first = blockIdx.x;
+    const int first = blockIdx.x, lane = threadIdx.x & 31;
     const int32_t *meta = a.meta + (int64_t)first * kMeta;
-    if (!meta[kOpen])
+    const int open = meta[kOpen], b = meta[kOpenB], unit = meta[kOpenUnit];
+    if (!open)
         return;
-    const int b = meta[kOpenB], unit = meta[kOpenUnit], D = a.c.D;
     const int h = unit / a.row_tiles, r0 = (unit - h * a.row_tiles) * N;
-    const int n0 = blockIdx.y * kJoinRows;
-    const int n1 = min(n0 + kJoinRows, min(N, a.rows - r0));
-    int last = first;  // the CTA where the unit ends
-    for (int i = first + 1; i < grid; ++i) {
-        const int32_t *m = a.meta + (int64_t)i * kMeta;
-        if (m[kCont]) {
-            last = i;
-            if (m[kContEnds])
-                break;
+    const int n = blockIdx.y * kJoinWarps + (threadIdx.x >> 5);
+    if (n >= N || r0 + n >= a.rows)
+        return;
+    float top = kFar, sum = 0.0f, x[kV] = {};
+    // 32 CTAs a turn, lane i looking at the i-th: the parts up to the one where the unit ends.
+    bool more = true;
+    for (int i0 = first; more && i0 < grid; i0 += 32) {
+        const int i = i0 + lane;
+        const int32_t *m = a.meta + (int64_t)min(i, grid - 1) * kMeta;
+        const bool cont = i < grid && i > first && m[kCont];
+        const uint32_t ends = __ballot_sync(0xFFFFFFFFu, cont && m[kContEnds]);
+        const uint32_t upto = ends ? (2u << (__ffs(ends) - 1)) - 1u : 0xFFFFFFFFu;
+        uint32_t parts = __ballot_sync(0xFFFFFFFFu, cont || i == first) & upto;
+        more = ends == 0;
+        const int64_t at = ((int64_t)i * 2 + (i == first)) * N + n;
+        const bool mine = (parts >> lane) & 1u;
+        const float ref = mine ? a.part_refs[2 * at] : kFar;
+        const float part = mine ? a.part_refs[2 * at + 1] : 0.0f;
+        float t = fmaxf(top, ref);
+#pragma unroll
+        for (int s = 16; s > 0; s >>= 1)
+            t = fmaxf(t, __shfl_xor_sync(0xFFFFFFFFu, t, s));
+        const float old = exp2f(top - t), f = exp2f(ref - t);
+        top = t;
+        sum *= old;
+#pragma unroll
+        for (int c = 0; c < kV; ++c)
+            x[c] *= old;
+        while (parts) {  // four parts' channels in flight
+            V v[4];
+            float pf[4], ps[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int s = parts ? __ffs(parts) - 1 : -1;
+                parts &= parts - 1;
+                pf[e] = __shfl_sync(0xFFFFFFFFu, f, s & 31);
+                ps[e] = __shfl_sync(0xFFFFFFFFu, part, s & 31);
+                const int j = i0 + s;
+                v[e] = V{};
+                if (s >= 0)
+                    v[e] = *reinterpret_cast<const V *>(
+                        a.parts + (((int64_t)j * 2 + (j == first)) * N + n) * D + kV * lane);
+                else
+                    pf[e] = ps[e] = 0.0f;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                sum = fmaf(ps[e], pf[e], sum);
+                const float *ve = reinterpret_cast<const float *>(&v[e]);
+#pragma unroll
+                for (int c = 0; c < kV; ++c)
+                    x[c] = fmaf(ve[c], pf[e], x[c]);
+            }
         }
     }
-    const int d = threadIdx.x;
-    for (int n = n0; n < n1; ++n) {
-        float top = kFar;
-        for (int i = first; i <= last; ++i) {
-            const int64_t at = ((int64_t)i * 2 + (i == first)) * N + n;
-            if (i == first || a.meta[(int64_t)i * kMeta + kCont])
-                top = fmaxf(top, a.part_refs[2 * at]);
-        }
-        float sum = 0.0f, x = 0.0f;
-        for (int i = first; i <= last; ++i) {
-            const int64_t at = ((int64_t)i * 2 + (i == first)) * N + n;
-            if (i != first && !a.meta[(int64_t)i * kMeta + kCont])
-                continue;
-            const float f = exp2f(a.part_refs[2 * at] - top);
-            sum = fmaf(a.part_refs[2 * at + 1], f, sum);
-            if (d < D)
-                x = fmaf(a.parts[at * D + d], f, x);
-        }
-        const int qi = (r0 + n) / a.group, g = (r0 + n) - qi * a.group;
-        const int64_t row = ((int64_t)b * a.Lq + qi) * a.Hq + h * a.group + g;
-        if (d < D)
-            static_cast<T *>(a.out)[row * D + d] = from_float<T>(sum == 0.0f ? 0.0f : x / sum);
-        if (d == 0 && a.lse)
-            a.lse[row] =
-                sum == 0.0f ? neg_inf_f() : (top + log2f(sum)) * 0.6931471805599453f;
-    }
+    const int qi = (r0 + n) / a.group, g = (r0 + n) - qi * a.group;
+    const int64_t row = ((int64_t)b * a.Lq + qi) * a.Hq + h * a.group + g;
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    uint32_t y[kV / 2];
+#pragma unroll
+    for (int c = 0; c < kV / 2; ++c)
+        y[c] = pack2<T>(x[2 * c] * inv, x[2 * c + 1] * inv);
+    uint32_t *o = reinterpret_cast<uint32_t *>(static_cast<T *>(a.out) + row * D) + kV / 2 * lane;
+#pragma unroll
+    for (int c = 0; c < kV / 2; ++c)
+        o[c] = y[c];
+    if (lane == 0 && a.lse)
+        a.lse[row] = sum == 0.0f ? neg_inf_f() : (top + log2f(sum)) * 0.6931471805599453f;
 }
 
 // Rows of a row tile: the smallest width that holds a head's rows, 64 beyond that.
@@ -1176,8 +1225,8 @@ cudaError_t run(const AttnArgs &a, int grid, const CUtensorMap &k_map, const CUt
                            a, k_map, v_map);
     if (e != cudaSuccess)
         return e;
-    return launch(combine_kernel<T>, dim3(grid, S::N / kJoinRows), dim3(128), 0, s, true, a, S::N,
-                  grid);
+    return launch(combine_kernel<T, S::D>, dim3(grid, (S::N + kJoinWarps - 1) / kJoinWarps),
+                  dim3(32 * kJoinWarps), 0, s, true, a, S::N, grid);
 }
 
 template <int D, typename T>
