@@ -18,13 +18,14 @@
 // are stored channel-major so that a thread unpacks one channel.  P^T is the only operand
 // written to shared memory by threads (16-byte stores, rows contiguous).
 //
-// A row's reference (the running maximum of a softmax) is the score of the first key it meets,
-// and moves only when a weight leaves the range that fp16 and fp32 hold (kTopWeight), which one
+// A row's reference (the running maximum of a softmax) is the largest score of the first 32 keys
+// it meets, and moves only when a weight leaves the range that fp16 and fp32 hold (kTopWeight), which one
 // vote a tile decides.  Weights are scaled by the cached row's scale before they are rounded to
 // fp16; a second reference of the row keeps their largest near 1 whatever the scales are.
 //
 // Warps.  One loads (queries, codes, own keys and values, through one ring of shared-memory
-// stages), one issues the products, the others unpack and make weights.
+// stages), one issues the products, four unpack, four to sixteen make weights: an unpacking
+// warp is tiles ahead, in the next unit's queries while the weights' warps write a unit's end.
 //
 // Split.  The tiles of all (sequence, head, row tile) units in order, with a charge of
 // kUnitCost tiles for each unit's beginning and end, are cut into equal ranges, one to a CTA
@@ -79,12 +80,16 @@ template <int D_, int N_>
 struct Shape {
     static constexpr int D = D_;
     static constexpr int N = N_;                       // rows of a row tile
-    static constexpr int C = N >= 64 ? 4 : 2;          // warpgroups sharing a tile's columns
+    static constexpr int C = N >= 64 ? 4 : N / 16;     // warpgroups sharing a tile's columns
     static constexpr int cols = N / C;                 // columns (rows of the problem) a thread
-    static constexpr int warps = 4 * C;                // worker warps
-    static constexpr int workers = 32 * warps;
-    static constexpr int threads = workers + 64;       // the loading and the issuing warp
+    static constexpr int w_warps = 4 * C;              // warps that make weights
+    static constexpr int w_threads = 32 * w_warps;
+    static constexpr int w_first = 4;                  // (warps 0 to 3 unpack)
+    static constexpr int loader = w_first + w_warps;
+    static constexpr int issuer = loader + 1;
+    static constexpr int threads = 32 * (issuer + 1);
     static constexpr int ctas = N >= 64 ? 1 : 2;       // CTAs an SM holds
+    static constexpr int bufs = N >= 64 ? 2 : 1;       // of unpacked keys, and of values
     static constexpr int stages = N >= 64 ? 8 : 4;
     // own keys come 32 to a stage; a block's 32 fill one tile, long prompts whole ones
     static constexpr int own_keys = N >= 64 ? 128 : 32;
@@ -99,7 +104,7 @@ struct Shape {
     static constexpr int lo_off = p_off + kKeys * N * 2;
     static constexpr int smem = lo_off + kKeys * N * 2 + 1024;  // and room to align the base
     // tensor memory columns
-    static constexpr int tK = 0, tV = 64, tS = 128, tO = 128 + 2 * N;
+    static constexpr int tK = 0, tV = 64 * bufs, tS = 128 * bufs, tO = tS + 2 * N;
     static constexpr int tmem = tO + N <= 256 ? 256 : 512;
     static_assert(tO + N <= tmem && ctas * tmem <= 512, "tensor memory");
     static_assert(q_bytes <= stage_bytes && own_v + 64 * D <= stage_bytes, "a stage holds them");
@@ -225,47 +230,52 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
     uint8_t *smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
     __shared__ __align__(8) uint64_t full[S::stages], empty[S::stages];  // the ring
     __shared__ __align__(8) uint64_t seg_full[2], seg_empty[2];
-    __shared__ __align__(8) uint64_t k_ready, s_done, p_ready, o_done, voted;
+    // of a tile, by its parity: keys and values unpacked, scores and sums done
+    __shared__ __align__(8) uint64_t k_ready[2], v_ready[2], s_done[2], o_done[2];
+    __shared__ __align__(8) uint64_t p_ready, voted;
     __shared__ uint32_t tmem_base;
-    __shared__ int bad_page[2];                                 // a segment met one
     __shared__ int64_t scan[S::threads / 32];
     __shared__ int64_t find_base;
     __shared__ int find_b;
-    __shared__ Segment segs[2];
     __shared__ uint32_t vote[2];
-    // per row: sum of the query's channels; the reference (negated), 2^(ref - refz), the
-    // reference of the scaled weights
-    __shared__ __align__(16) float sumq[N], nref[N], cmul[N], refz[N];
+    // of a segment, by its parity: what it is, whether it met a page out of range, the queries'
+    // sums and a score's unit, the first own key with a non-finite value (by channel)
+    __shared__ Segment segs[2];
+    __shared__ int bad_page[2], any_bad[2];
+    __shared__ __align__(16) float sumq[2][N];
+    __shared__ float q_unit[2], q_big[4];
+    __shared__ int first_bad[2][D];
+    // per row: the reference (negated), 2^(ref - refz), the reference of the scaled weights
+    __shared__ __align__(16) float nref[N], cmul[N], refz[N];
     __shared__ __align__(16) float fl[N], fo[N], redo[N];
     __shared__ __align__(16) float none_row[S::cols];  // -inf: the references of absent keys
     __shared__ int64_t row_at[N];
-    __shared__ float wred[S::warps][2][kCols];
-    __shared__ int first_bad[D];  // first own key of the segment with a non-finite value
-    __shared__ int any_bad;
+    __shared__ float wred[S::w_warps][2][kCols];
 
     const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31;
     if (tid == 0) {
         for (int i = 0; i < S::stages; ++i) {
             mbar_init(&full[i], 1);
-            mbar_init(&empty[i], S::warps);
+            mbar_init(&empty[i], 4 + S::w_warps);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&seg_full[i], 1);
-            mbar_init(&seg_empty[i], S::warps + 1);
+            mbar_init(&seg_empty[i], 4 + S::w_warps + 1);
+            mbar_init(&k_ready[i], 4);
+            mbar_init(&v_ready[i], 4);
+            mbar_init(&s_done[i], 1);
+            mbar_init(&o_done[i], 1);
             vote[i] = 0;
         }
-        mbar_init(&k_ready, S::warps);
-        mbar_init(&s_done, 1);
-        mbar_init(&p_ready, S::warps);
-        mbar_init(&o_done, 1);
-        mbar_init(&voted, S::warps);
+        mbar_init(&p_ready, S::w_warps);
+        mbar_init(&voted, S::w_warps);
         fence_mbar_init();
     }
     if (tid < S::cols)
         none_row[tid] = neg_inf_f();
-    if (warp == S::warps)
+    if (warp == S::issuer)
         tc::tmem_alloc(&tmem_base, S::tmem);
-    if (tid == S::workers + 32) {
+    if (warp == S::loader && lane == 0) {
         tc::prefetch_tensormap(&k_map);
         tc::prefetch_tensormap(&v_map);
     }
@@ -325,7 +335,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
         dead = __any_sync(0xFFFFFFFFu, dead);
     };
 
-    if (warp == S::warps) {
+    if (warp == S::loader) {
         // ---------------------------------------------------------------- the loading warp
         if (w.at < w.end) {
             w.b = find_b;
@@ -462,15 +472,15 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
             mbar_wait_short(&full[r % S::stages], (r / S::stages) & 1, &g_status,
                             dead ? kDrainLimitNs : kWaitLimitNs);
         }
-    } else if (warp == S::warps + 1) {
+    } else if (warp == S::issuer) {
         // ---------------------------------------------------------------- the issuing warp
         // S of a tile before the sums of the tile before it, so that the tensor core works on
-        // scores while the workers make weights.
+        // scores while the others make weights.
         const uint64_t q16_desc = tc::sw128_kmajor_desc(smem + S::q16_off);
         const uint64_t qt_desc = tc::sw128_kmajor_desc(smem + S::qt_off);
         const uint64_t p_desc = mn_desc(smem + S::p_off, 128, N * 16);
         const uint64_t lo_desc = mn_desc(smem + S::lo_off, 128, N * 16);
-        uint32_t scores = 0, sums = 0;  // products issued so far
+        uint32_t scores = 0, sums = 0;  // tiles issued so far
         for (uint32_t seg = 0;; ++seg) {
             const uint32_t sb = seg & 1;
             wait_warp(&seg_full[sb], (seg >> 1) & 1);
@@ -483,59 +493,261 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 break;
             for (int t = first; t <= last; ++t) {
                 if (t < last) {
-                    wait_warp(&k_ready, scores & 1);
+                    const uint32_t par = scores & 1;
+                    wait_warp(&k_ready[par], (scores >> 1) & 1);
                     tc::fence_after_sync();
                     const uint64_t q_desc = t < ct ? q16_desc : qt_desc;
                     const uint32_t idesc =
                         t < ct ? idesc_f16<__half>(128, N, false) : idesc_f16<T>(128, N, false);
+                    const uint32_t tK = tmem + S::tK + (S::bufs > 1 ? par * 64 : 0);
 #pragma unroll
                     for (int k = 0; k < D / 16; ++k)
-                        mma_ts(tmem + S::tS + (scores & 1) * N, tmem + S::tK + 8 * k,
+                        mma_ts(tmem + S::tS + par * N, tK + 8 * k,
                                q_desc + (k >> 2) * ((N * 128) >> 4) + 2 * (k & 3), idesc, k > 0);
-                    mma_commit(&s_done);
+                    mma_commit(&s_done[par]);
                     ++scores;
                 }
                 if (t > first) {
+                    const uint32_t par = sums & 1;
+                    wait_warp(&v_ready[par], (sums >> 1) & 1);
                     wait_warp(&p_ready, sums & 1);
                     tc::fence_after_sync();
+                    const uint32_t tV = tmem + S::tV + (S::bufs > 1 ? par * 64 : 0);
                     const uint32_t more = t - 1 > first;
                     if (t - 1 < ct) {
                         constexpr uint32_t idesc = idesc_f16<__half>(128, N, true);
 #pragma unroll
                         for (int k = 0; k < kKeys / 16; ++k)
-                            mma_ts(tmem + S::tO, tmem + S::tV + 8 * k,
-                                   p_desc + k * ((2 * N * 16) >> 4), idesc, k > 0 ? 1u : more);
+                            mma_ts(tmem + S::tO, tV + 8 * k, p_desc + k * ((2 * N * 16) >> 4),
+                                   idesc, k > 0 ? 1u : more);
                         if (!std::is_same<T, __nv_bfloat16>::value)
 #pragma unroll
                             for (int k = 0; k < kKeys / 16; ++k)
-                                mma_ts(tmem + S::tO, tmem + S::tV + 8 * k,
-                                       lo_desc + k * ((2 * N * 16) >> 4), idesc, 1);
+                                mma_ts(tmem + S::tO, tV + 8 * k, lo_desc + k * ((2 * N * 16) >> 4),
+                                       idesc, 1);
                     } else {
                         constexpr uint32_t idesc = idesc_f16<T>(128, N, true);
                         const int keys = min(kOwnKeys, own_total - (t - 1 - ct) * kOwnKeys);
                         const int steps = (keys + 31) / 32 * 2;
                         for (int k = 0; k < steps; ++k) {
-                            mma_ts(tmem + S::tO, tmem + S::tV + 8 * k,
-                                   p_desc + k * ((2 * N * 16) >> 4), idesc, k > 0 ? 1u : more);
-                            mma_ts(tmem + S::tO, tmem + S::tV + 8 * k,
-                                   lo_desc + k * ((2 * N * 16) >> 4), idesc, 1);
+                            mma_ts(tmem + S::tO, tV + 8 * k, p_desc + k * ((2 * N * 16) >> 4),
+                                   idesc, k > 0 ? 1u : more);
+                            mma_ts(tmem + S::tO, tV + 8 * k, lo_desc + k * ((2 * N * 16) >> 4),
+                                   idesc, 1);
                         }
                     }
-                    mma_commit(&o_done);
+                    mma_commit(&o_done[par]);
                     ++sums;
                 }
             }
         }
+    } else if (warp < S::w_first) {
+        // ---------------------------------------------------------------- the unpacking warps
+        // Queries, keys and values into the tensor core's operands; a thread is a key of K and
+        // a channel of V^T.
+        const int key = tid;
+        const uint32_t lanes = tmem + ((uint32_t)warp << 21);
+        uint32_t ring = 0, tile = 0;  // stages used, tiles unpacked so far
+        auto arrive = [&](uint64_t *bar, uint32_t n) {
+            __syncwarp();
+            if (lane == 0)
+                mbar_arrive_n(bar, n);
+        };
+        // Stages that only these warps read are given back for all.
+        constexpr uint32_t kForAll = 1 + S::C;
+        for (uint32_t seg = 0;; ++seg) {
+            const uint32_t sb = seg & 1;
+            wait(&seg_full[sb], (seg >> 1) & 1);
+            const Segment &g = segs[sb];
+            if (g.done)
+                break;
+            const int first = g.first, last = g.last, ct = g.ct, own = g.own;
+            if (first < last) {
+                // ---- the queries: their sums, and both operands (K-major, 128-byte swizzle)
+                const uint32_t st = ring % S::stages;
+                wait(&full[st], (ring / S::stages) & 1);
+                const uint8_t *raw = smem + st * S::stage_bytes;
+                constexpr int kMine = N * (D / 8) / 128;
+                float big = 0.0f;
+#pragma unroll 2
+                for (int m = 0; m < kMine; ++m) {
+                    const int i = tid + m * 128, n = i / (D / 8), c8 = i % (D / 8);
+                    uint4 x = make_uint4(0, 0, 0, 0);
+                    if (n < g.rows)
+                        x = *reinterpret_cast<const uint4 *>(raw + 16 * i);
+                    float f[8], sum = 0.0f;
+                    const uint32_t xw[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        unpack2<T>(xw[e], f[2 * e], f[2 * e + 1]);
+                        sum += f[2 * e] + f[2 * e + 1];
+                    }
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        big = fmaxf(big, fabsf(f[e]) <= 3.4e38f ? fabsf(f[e]) : 0.0f);
+#pragma unroll
+                    for (int s = D / 16; s > 0; s >>= 1)
+                        sum += __shfl_xor_sync(0xFFFFFFFFu, sum, s);
+                    if (c8 == 0)
+                        sumq[sb][n] = sum;
+                }
+                const uint32_t wbig = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(big));
+                named_sync(2, 128);  // (the segment before has read its own)
+                if (lane == 0)
+                    q_big[warp] = __uint_as_float(wbig);
+                if (tid < D)
+                    first_bad[sb][tid] = 0x7FFFFFFF;
+                if (tid == 0)
+                    any_bad[sb] = 0;
+                named_sync(2, 128);
+                big = fmaxf(fmaxf(q_big[0], q_big[1]), fmaxf(q_big[2], q_big[3]));
+                // 2^-e with e the exponent of the largest, less 13; 0 stays 0
+                const int e = big > 0.0f ? (int)(__float_as_uint(big) >> 23) - 127 - 13 : 0;
+                const int e0 = min(max(e, -100), 100);
+                const float unit = __uint_as_float((uint32_t)(127 - e0) << 23);
+                const float odd = unit * 0.0625f;  // the codes of odd channels are 16 times as large
+                if (tid == 0)
+                    q_unit[sb] = kCodeUnit * __uint_as_float((uint32_t)(127 + e0) << 23);
+                // the operands' last readers are done: the scores of the tile before
+                if (tile > 0)
+                    wait(&s_done[(tile - 1) & 1], ((tile - 1) >> 1) & 1);
+#pragma unroll 2
+                for (int m = 0; m < kMine; ++m) {
+                    const int i = tid + m * 128, n = i / (D / 8), c8 = i % (D / 8);
+                    uint4 x = make_uint4(0, 0, 0, 0);
+                    if (n < g.rows)
+                        x = *reinterpret_cast<const uint4 *>(raw + 16 * i);
+                    float f[8];
+                    const uint32_t xw[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+                        unpack2<T>(xw[v], f[2 * v], f[2 * v + 1]);
+                    const int at = (c8 >> 3) * (N * 128) + n * 128 + (((c8 & 7) ^ (n & 7)) << 4);
+                    // pairs (c, c + 4)
+                    *reinterpret_cast<uint4 *>(smem + S::q16_off + at) =
+                        make_uint4(pack2<__half>(f[0] * unit, f[4] * unit),
+                                   pack2<__half>(f[1] * odd, f[5] * odd),
+                                   pack2<__half>(f[2] * unit, f[6] * unit),
+                                   pack2<__half>(f[3] * odd, f[7] * odd));
+                    if (last > ct)
+                        *reinterpret_cast<uint4 *>(smem + S::qt_off + at) = interleave8(x);
+                }
+                fence_async_smem();  // for the first tile's product
+                arrive(&empty[st], kForAll);
+                ++ring;
+            }
+            for (int t = first; t < last; ++t, ++tile) {
+                const uint32_t par = tile & 1;
+                const bool cached = t < ct;
+                const int keys = cached ? kKeys : min(kOwnKeys, own - (t - ct) * kOwnKeys);
+                const int used = cached ? 1 : (keys + 31) / 32;
+                const uint32_t tK = lanes + S::tK + (S::bufs > 1 ? par * 64 : 0);
+                const uint32_t tV = lanes + S::tV + (S::bufs > 1 ? par * 64 : 0);
+                // ---- keys; their place is free when the scores of `bufs` tiles before are done
+                if (tile >= S::bufs)
+                    wait(&s_done[(tile - S::bufs) & 1], ((tile - S::bufs) >> 1) & 1);
+                if (cached) {
+                    const uint32_t s1 = ring % S::stages;
+                    wait(&full[s1], (ring / S::stages) & 1);
+                    tc::fence_after_sync();
+                    const uint8_t *row = smem + s1 * S::stage_bytes + key * (D / 2);
+#pragma unroll
+                    for (int i = 0; i < D / 32; ++i) {
+                        const int sw = D == 128 ? (i ^ ((key >> 1) & 3)) : (i ^ ((key >> 2) & 1));
+                        uint32_t y[16];
+                        unpack32(*reinterpret_cast<const uint4 *>(row + 16 * sw), y);
+                        tmem_st16(tK + 16 * i, y);
+                    }
+                } else if (32 * warp < keys) {
+                    const uint32_t r = ring + warp, s1 = r % S::stages;
+                    wait(&full[s1], (r / S::stages) & 1);
+                    tc::fence_after_sync();
+                    const uint8_t *row = smem + s1 * S::stage_bytes + lane * S::own_row;
+#pragma unroll 1
+                    for (int i = 0; i < D / 32; ++i) {
+                        uint32_t y[16];
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) {
+                            uint4 x = make_uint4(0, 0, 0, 0);
+                            if (key < keys)
+                                x = interleave8(
+                                    *reinterpret_cast<const uint4 *>(row + 64 * i + 16 * v));
+                            y[4 * v] = x.x, y[4 * v + 1] = x.y;
+                            y[4 * v + 2] = x.z, y[4 * v + 3] = x.w;
+                        }
+                        tmem_st16(tK + 16 * i, y);
+                    }
+                }
+                tmem_wait_st();
+                tc::fence_before_sync();
+                arrive(&k_ready[par], 1);
+                // ---- values; their place is free when the sums of `bufs` tiles before are done
+                if (tile >= S::bufs) {
+                    wait(&o_done[(tile - S::bufs) & 1], ((tile - S::bufs) >> 1) & 1);
+                    tc::fence_after_sync();
+                }
+                const int d = key;
+                if (cached) {
+                    const uint8_t *v = smem + (ring % S::stages) * S::stage_bytes + S::code_bytes;
+                    if (D == 128 || d < D)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {  // 32 slots
+                            int off;
+                            if (a.c.page_shift == 5)
+                                off = i * (16 * D) + d * 16;
+                            else if (a.c.page_shift == 6)
+                                off = (i >> 1) * (32 * D) + d * 32 +
+                                      (((i & 1) ^ ((d >> 2) & 1)) << 4);
+                            else
+                                off = d * 64 + ((i ^ ((d >> 1) & 3)) << 4);
+                            uint32_t y[16];
+                            unpack32(*reinterpret_cast<const uint4 *>(v + off), y);
+                            tmem_st16(tV + 16 * i, y);
+                        }
+                } else {
+#pragma unroll 1
+                    for (int i = 0; i < used; ++i) {
+                        const uint32_t r = ring + i, s1 = r % S::stages;
+                        wait(&full[s1], (r / S::stages) & 1);
+                        if (D == 128 || d < D) {
+                            uint32_t y[16];
+                            const int bad = own_values<T>(
+                                reinterpret_cast<const T *>(smem + s1 * S::stage_bytes + S::own_v) +
+                                    d,
+                                D, keys - 32 * i, y);
+                            if (bad < 32) {
+                                first_bad[sb][d] =
+                                    min(first_bad[sb][d], (t - ct) * kOwnKeys + 32 * i + bad);
+                                any_bad[sb] = 1;
+                            }
+                            tmem_st16(tV + 16 * i, y);
+                        }
+                    }
+                }
+                tmem_wait_st();
+                tc::fence_before_sync();
+                arrive(&v_ready[par], 1);
+                if (cached)
+                    arrive(&empty[ring % S::stages], 1);
+                else
+                    for (int i = 0; i < used; ++i)
+                        arrive(&empty[(ring + i) % S::stages], kForAll);
+                ring += used;
+            }
+            arrive(&seg_empty[sb], 1);
+        }
     } else {
-        // ---------------------------------------------------------------- the workers
-        const int wg = warp >> 2, quarter = warp & 3, key = tid & 127;
+        // ---------------------------------------------------------------- the weights
+        // A thread holds one key's scores of its columns.
+        const int wt = tid - 32 * S::w_first, ww = warp - S::w_first;  // thread, warp among these
+        const int wg = ww >> 2, quarter = ww & 3, key = wt & 127;
         const int col0 = wg * kCols;  // this thread's columns
         const uint32_t lanes = tmem + ((uint32_t)quarter << 21);
         uint8_t *p_smem = smem + S::p_off, *lo_smem = smem + S::lo_off;
         uint32_t ring = 0;    // stages used so far
-        uint32_t seen = 0;    // tiles whose scores were taken and whose weights were given
+        uint32_t seen = 0;    // tiles whose weights were given
         uint32_t summed = 0;  // tiles whose sums were waited for
-        auto sync = [&] { named_sync(1, S::workers); };
+        auto sync = [&] { named_sync(1, S::w_threads); };
 
         for (uint32_t seg = 0;; ++seg) {
             const uint32_t sb = seg & 1;
@@ -545,90 +757,13 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 break;
             const int begin = g.first;
             const bool some = begin < g.last;
+            ring += some ? 1 : 0;  // the queries'
             uint64_t l2[kCols / 2], pm2[kCols / 2];
 #pragma unroll
             for (int j = 0; j < kCols / 2; ++j)
                 l2[j] = pm2[j] = 0;
-            float k_unit = 1.0f;  // a score's factor for the queries' power of two and the codes'
-            if (some) {
-                // ---- the queries: their sums, and both operands (K-major, 128-byte swizzle)
-                const uint32_t st = ring % S::stages;
-                wait(&full[st], (ring / S::stages) & 1);
-                const uint8_t *raw = smem + st * S::stage_bytes;
-                constexpr int kChunks = N * (D / 8);
-                constexpr int kMine = (kChunks + S::workers - 1) / S::workers;
-                uint4 x[kMine];
-                float big = 0.0f;
-#pragma unroll
-                for (int m = 0; m < kMine; ++m) {
-                    const int i = tid + m * S::workers, n = i / (D / 8), c8 = i % (D / 8);
-                    x[m] = make_uint4(0, 0, 0, 0);
-                    if (i < kChunks && n < g.rows)
-                        x[m] = *reinterpret_cast<const uint4 *>(raw + 16 * i);
-                    float f[8], sum = 0.0f;
-                    const uint32_t xw[4] = {x[m].x, x[m].y, x[m].z, x[m].w};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        unpack2<T>(xw[e], f[2 * e], f[2 * e + 1]);
-                        sum += f[2 * e] + f[2 * e + 1];
-                    }
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (fabsf(f[e]) <= 3.4e38f)
-                            big = fmaxf(big, fabsf(f[e]));
-#pragma unroll
-                    for (int s = D / 16; s > 0; s >>= 1)
-                        sum += __shfl_xor_sync(0xFFFFFFFFu, sum, s);
-                    if (i < kChunks && c8 == 0)
-                        sumq[n] = sum;
-                }
-                const uint32_t wbig = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(big));
-                if (lane == 0)
-                    wred[warp][0][0] = __uint_as_float(wbig);
-                if (tid < D)
-                    first_bad[tid] = 0x7FFFFFFF;
-                if (tid == 0)
-                    any_bad = 0;
-                sync();
-#pragma unroll
-                for (int i = 0; i < S::warps; ++i)
-                    big = fmaxf(big, wred[i][0][0]);
-                // 2^-e with e the exponent of the largest, less 13; 0 stays 0
-                const int e = big > 0.0f ? (int)((__float_as_uint(big) >> 23) & 255u) - 127 - 13 : 0;
-                const int e0 = min(max(e, -100), 100);
-                const float q_unit = __uint_as_float((uint32_t)(127 - e0) << 23);
-                k_unit = kCodeUnit * __uint_as_float((uint32_t)(127 + e0) << 23);
-#pragma unroll
-                for (int m = 0; m < kMine; ++m) {
-                    const int i = tid + m * S::workers, n = i / (D / 8), c8 = i % (D / 8);
-                    if (i >= kChunks)
-                        continue;
-                    float f[8];
-                    const uint32_t xw[4] = {x[m].x, x[m].y, x[m].z, x[m].w};
-#pragma unroll
-                    for (int v = 0; v < 4; ++v)
-                        unpack2<T>(xw[v], f[2 * v], f[2 * v + 1]);
-                    // pairs (c, c + 4); the codes of odd channels are 16 times as large
-                    const float q_odd = q_unit * 0.0625f;
-                    const int at = (c8 >> 3) * (N * 128) + n * 128 + (((c8 & 7) ^ (n & 7)) << 4);
-                    *reinterpret_cast<uint4 *>(smem + S::q16_off + at) =
-                        make_uint4(pack2<__half>(f[0] * q_unit, f[4] * q_unit),
-                                   pack2<__half>(f[1] * q_odd, f[5] * q_odd),
-                                   pack2<__half>(f[2] * q_unit, f[6] * q_unit),
-                                   pack2<__half>(f[3] * q_odd, f[7] * q_odd));
-                    if (g.last > g.ct)
-                        *reinterpret_cast<uint4 *>(smem + S::qt_off + at) = interleave8(x[m]);
-                }
-                fence_async_smem();  // for the first tile's product
-                __syncwarp();
-                if (lane == 0)
-                    mbar_arrive(&empty[st]);
-                ++ring;
-            }
 
-            // Tiles [from, to) of the unit, all of them cached or all of them own.  A turn loads
-            // the keys of tile t + 1, whose scores are computed while the weights of tile t are
-            // made; the first turn only loads.
+            // Tiles [from, to) of the unit, all of them cached or all of them own.
             auto tiles = [&](auto own_tag, int from, int to) {
                 constexpr bool kOwn = decltype(own_tag)::value;
                 // own values: weights as a sum of two numbers of T; cached ones need a second
@@ -637,71 +772,25 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 using W = std::conditional_t<kOwn, T, __half>;  // weights and values
                 const int end = kOwn ? g.own : g.cached;
                 const int base = kOwn ? g.ct : 0;
-                const int step = kOwn ? kOwnKeys : kKeys;
-                const float k_factor = kOwn ? a.scale : a.scale * k_unit;
-                int used = 0;  // stages of tile t
+                constexpr int step = kOwn ? kOwnKeys : kKeys;
 #pragma unroll 1
-                for (int t = from - 1; t < to; ++t) {
-                    const bool cur = t >= from;
-                    if (cur) {
-                        wait(&s_done, seen & 1);
-                        tc::fence_after_sync();
-                    }
-                    // tile t's scores being there, the keys' place in tensor memory is free
-                    if (t + 1 < to) {
-                        const uint32_t tK = lanes + S::tK;
-                        const uint32_t r0 = ring + (cur ? (kOwn ? used : 1) : 0);
-                        const int left = end - (t + 1 - base) * step;  // keys from there on
-                        if (!kOwn || 32 * quarter < min(left, kOwnKeys)) {
-                            const uint32_t r = kOwn ? r0 + quarter : r0, s1 = r % S::stages;
-                            wait(&full[s1], (r / S::stages) & 1);
-                            const uint8_t *row = smem + s1 * S::stage_bytes +
-                                                 (kOwn ? lane * S::own_row : key * (D / 2));
-#pragma unroll
-                            for (int i = 0; i < D / 32; ++i)
-                                if (i * S::C / (D / 32) == wg) {
-                                    uint32_t y[16];
-                                    if constexpr (!kOwn) {
-                                        const int sw = D == 128 ? (i ^ ((key >> 1) & 3))
-                                                                : (i ^ ((key >> 2) & 1));
-                                        unpack32(*reinterpret_cast<const uint4 *>(row + 16 * sw), y);
-                                    } else {
-#pragma unroll
-                                        for (int v = 0; v < 4; ++v) {
-                                            uint4 x = make_uint4(0, 0, 0, 0);
-                                            if (key < left)
-                                                x = interleave8(*reinterpret_cast<const uint4 *>(
-                                                    row + 64 * i + 16 * v));
-                                            y[4 * v] = x.x, y[4 * v + 1] = x.y;
-                                            y[4 * v + 2] = x.z, y[4 * v + 3] = x.w;
-                                        }
-                                    }
-                                    tmem_st16(tK + 16 * i, y);
-                                }
-                            tmem_wait_st();
-                        }
-                        tc::fence_before_sync();
-                        __syncwarp();
-                        if (lane == 0)
-                            mbar_arrive(&k_ready);
-                    }
-                    const int keys = min(step, end - (t - base) * step);  // of tile t
-                    if (!cur) {
-                        used = kOwn ? (min(step, end - (t + 1 - base) * step) + 31) / 32 : 1;
-                        continue;
-                    }
+                for (int t = from; t < to; ++t) {
+                    const int keys = min(step, end - (t - base) * step);
                     const uint32_t st = ring % S::stages;
-                    const uint8_t *buf = smem + st * S::stage_bytes;
                     const uint32_t tS = lanes + S::tS + (seen & 1) * N + col0;
+                    wait(&s_done[seen & 1], (seen >> 1) & 1);
+                    tc::fence_after_sync();
                     // this thread's key: scale and offset, for scores and weights
                     const int j = (t - base) * step + key;
                     const bool valid = key < keys;
-                    float ks = k_factor, ko = 0.0f, vs = 1.0f, vo = 0.0f;
+                    float ks = a.scale, ko = 0.0f, vs = 1.0f, vo = 0.0f;
                     if constexpr (!kOwn) {
                         const uint32_t *f =
-                            reinterpret_cast<const uint32_t *>(buf + 2 * S::code_bytes) + key;
+                            reinterpret_cast<const uint32_t *>(smem + st * S::stage_bytes +
+                                                               2 * S::code_bytes) +
+                            key;
                         const uint32_t fk = f[0], fv = f[kKeys];
-                        ks = bf16_low(fk) * k_factor;
+                        ks = bf16_low(fk) * (a.scale * q_unit[sb]);
                         ko = bf16_high(fk) * a.scale;
                         vs = bf16_low(fv);
                         vo = bf16_high(fv);
@@ -715,33 +804,46 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                                           : kOwn && a.causal ? j * a.group - (g.r0 + col0)
                                                              : 0;
                     if (t == begin) {
-                        // ---- the references: the score of the tile's first key, where the row
-                        // sees it
+                        // ---- the references: the largest score of the tile's first 32 keys
+                        // that the row sees, with the largest scale of their values
                         if (quarter == 0) {
-                            // lane c takes column c of lane 0's key
-                            float x = 0.0f;
+                            const float big = __uint_as_float(
+                                __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(fmaxf(vs, 0.0f))));
+                            const float small = __uint_as_float(__reduce_min_sync(
+                                0xFFFFFFFFu, vs > 0.0f ? __float_as_uint(vs) : 0x7F800000u));
+                            // scales within a factor of 2^8: the largest stands for all
+                            const bool alike = !(big > 256.0f * small);
+                            float ref = kFar, z = kFar;
+#pragma unroll 1
+                            for (int pass = 0; pass < (alike ? 1 : 2); ++pass) {
+                                const float lv = pass == 0 ? 0.0f : vs > 0.0f ? log2f(vs) : neg_inf_f();
+                                float x[kCols];
 #pragma unroll
-                            for (int c8 = 0; c8 < kCols; c8 += 8) {
-                                uint32_t s[8];
-                                tmem_ld<8>(tS + c8, s);
+                                for (int c8 = 0; c8 < kCols; c8 += 8) {
+                                    uint32_t s[8];
+                                    tmem_ld<8>(tS + c8, s);
 #pragma unroll
-                                for (int c = 0; c < 8; ++c) {
-                                    const uint32_t o = __shfl_sync(0xFFFFFFFFu, s[c], 0);
-                                    x = lane == c8 + c ? __uint_as_float(o) : x;
+                                    for (int c = 0; c < 8; ++c) {
+                                        const float y = fmaf(__uint_as_float(s[c]), ks,
+                                                             ko * sumq[sb][col0 + c8 + c]);
+                                        x[c8 + c] = c8 + c >= first_col ? y + lv : neg_inf_f();
+                                    }
                                 }
+                                warp_columns<kCols>(x,
+                                                    [](float u, float v) { return fmaxf(u, v); });
+                                const float m = x[0] == neg_inf_f()    ? kFar
+                                                : fabsf(x[0]) < 1e30f ? x[0]
+                                                                      : 0.0f;
+                                if (pass == 0)
+                                    ref = m;
+                                else
+                                    z = m;
                             }
-                            const float ks_0 = __shfl_sync(0xFFFFFFFFu, ks, 0);
-                            const float ko_0 = __shfl_sync(0xFFFFFFFFu, ko, 0);
-                            const float vs_0 = __shfl_sync(0xFFFFFFFFu, vs, 0);
-                            const int col_0 = __shfl_sync(0xFFFFFFFFu, first_col, 0);
+                            if (alike && big > 0.0f)
+                                z = ref + log2f(big);
                             if (lane < kCols) {
                                 const int n = col0 + lane;
-                                x = fmaf(x, ks_0, ko_0 * sumq[n]);
-                                const float lv = vs_0 > 0.0f ? log2f(vs_0) : kFar;
-                                const float ref = lane < col_0        ? kFar
-                                                  : fabsf(x) < 1e30f ? x
-                                                                     : 0.0f;
-                                const float z = fmaxf(ref + lv, ref - kMaxShift);
+                                z = fmaxf(z, ref - kMaxShift);
                                 nref[n] = -ref;
                                 refz[n] = z;
                                 cmul[n] = ref == kFar ? 1.0f : exp2f(ref - z);
@@ -754,7 +856,6 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     // the references moved) only the rows of `redo` are summed again.
                     auto weights = [&](auto again) -> float {
                         constexpr bool kAgain = decltype(again)::value;
-                        const float4 *sq4 = reinterpret_cast<const float4 *>(sumq + col0);
                         const float4 *nr4 =
                             reinterpret_cast<const float4 *>(valid ? nref + col0 : none_row);
                         const float4 *cm4 = reinterpret_cast<const float4 *>(cmul + col0);
@@ -771,7 +872,8 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                                 const float4 nr = nr4[c / 4], cm = cm4[c / 4];
                                 uint64_t y[2] = {f2(nr.x, nr.y), f2(nr.z, nr.w)};
                                 if constexpr (!kOwn) {
-                                    const float4 sq = sq4[c / 4];
+                                    const float4 sq =
+                                        reinterpret_cast<const float4 *>(sumq[sb] + col0)[c / 4];
                                     y[0] = fma2(ko2, f2(sq.x, sq.y), y[0]);
                                     y[1] = fma2(ko2, f2(sq.z, sq.w), y[1]);
                                 }
@@ -838,50 +940,14 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                         mbar_arrive(&voted);
                     }
                     __syncwarp();
-                    // ---- the values; the sums of the tile before must have read theirs
+                    // the sums of the tile before must have read its weights
                     if (seen > summed) {
-                        wait(&o_done, summed & 1);
+                        wait(&o_done[summed & 1], (summed >> 1) & 1);
                         ++summed;
                         tc::fence_after_sync();
                     }
                     if (kOwn && t == from && from > begin)
                         scale_sums<kCols>(lanes + S::tO + col0, nullptr, kSumUnit);
-                    if (D == 128 || key < D) {
-                        const uint32_t tV = lanes + S::tV;
-                        const int d = key;
-#pragma unroll(kOwn ? 1 : 4 / S::C)
-                        for (int q = 0; q < 4 / S::C; ++q) {
-                            const int i = wg * (4 / S::C) + q;  // 32 slots
-                            uint32_t y[16];
-                            if constexpr (!kOwn) {
-                                int off;
-                                if (a.c.page_shift == 5)
-                                    off = i * (16 * D) + d * 16;
-                                else if (a.c.page_shift == 6)
-                                    off = (i >> 1) * (32 * D) + d * 32 +
-                                          (((i & 1) ^ ((d >> 2) & 1)) << 4);
-                                else
-                                    off = d * 64 + ((i ^ ((d >> 1) & 3)) << 4);
-                                unpack32(*reinterpret_cast<const uint4 *>(buf + S::code_bytes + off),
-                                         y);
-                            } else {
-                                if (32 * i >= keys)
-                                    break;
-                                const uint32_t r = ring + i, s1 = r % S::stages;
-                                wait(&full[s1], (r / S::stages) & 1);
-                                const int bad = own_values<T>(
-                                    reinterpret_cast<const T *>(smem + s1 * S::stage_bytes +
-                                                                S::own_v) +
-                                        d,
-                                    D, keys - 32 * i, y);
-                                if (bad < 32) {
-                                    atomicMin(&first_bad[d], (t - base) * step + 32 * i + bad);
-                                    any_bad = 1;
-                                }
-                            }
-                            tmem_st16(tV + 16 * i, y);
-                        }
-                    }
                     wait(&voted, seen & 1);
                     if (*reinterpret_cast<volatile uint32_t *>(&vote[seen & 1]) == seen + 1) {
                         // ---- the references move: per row, the running maxima of the scores
@@ -897,38 +963,38 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
 #pragma unroll
                                 for (int c = 0; c < 8; ++c) {
                                     const float x = fmaf(__uint_as_float(s[c]), ks,
-                                                         ko * sumq[col0 + c8 + c]);
+                                                         ko * sumq[sb][col0 + c8 + c]);
                                     m[c8 + c] = c8 + c >= first_col ? x + (z ? lv : 0.0f)
                                                                     : neg_inf_f();
                                 }
                             }
                             warp_columns<kCols>(m, [](float x, float y) { return fmaxf(x, y); });
                             if (lane < kCols)
-                                wred[warp][z][lane] = m[0];
+                                wred[ww][z][lane] = m[0];
                         }
                         sync();
-                        if (tid < N) {
-                            const int w4 = tid / kCols * 4, c = tid % kCols;
+                        if (wt < N) {
+                            const int w4 = wt / kCols * 4, c = wt % kCols;
                             float s4 = wred[w4][0][c], z4 = wred[w4][1][c];
 #pragma unroll
                             for (int i = 1; i < 4; ++i) {
                                 s4 = fmaxf(s4, wred[w4 + i][0][c]);
                                 z4 = fmaxf(z4, wred[w4 + i][1][c]);
                             }
-                            const float ref = -nref[tid];
+                            const float ref = -nref[wt];
                             const float to_ref = fmaxf(ref, s4);
                             // where no value has a scale yet, refz follows at a distance
-                            const float z_old = refz[tid];
+                            const float z_old = refz[wt];
                             const float to_z = fmaxf(fmaxf(z_old, z4), to_ref - kMaxShift);
                             // a row whose weights may have overflowed starts anew with this
                             // tile: what it held weighs less than 2^-60 of what it gets
                             const bool anew = to_ref - ref > kTopShift;
-                            redo[tid] = anew ? 1.0f : 0.0f;
-                            fl[tid] = anew ? 0.0f : exp2f(ref - to_ref);
-                            fo[tid] = exp2f(z_old - to_z);
-                            nref[tid] = -to_ref;
-                            refz[tid] = to_z;
-                            cmul[tid] = exp2f(to_ref - to_z);
+                            redo[wt] = anew ? 1.0f : 0.0f;
+                            fl[wt] = anew ? 0.0f : exp2f(ref - to_ref);
+                            fo[wt] = exp2f(z_old - to_z);
+                            nref[wt] = -to_ref;
+                            refz[wt] = to_z;
+                            cmul[wt] = exp2f(to_ref - to_z);
                         }
                         sync();
                         if (t > begin)  // the sums of the tiles before (waited for above)
@@ -964,22 +1030,17 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                                     pl[4 * q], pl[4 * q + 1], pl[4 * q + 2], pl[4 * q + 3]);
                         }
                     }
-                    tmem_wait_st();
+                    tmem_wait_st();  // (sums that were scaled)
                     fence_async_smem();
                     tc::fence_before_sync();
                     __syncwarp();
                     if (lane == 0) {
                         mbar_arrive(&p_ready);
-                        if constexpr (!kOwn)
+                        if (!kOwn)
                             mbar_arrive(&empty[st]);
-                        else
-                            for (int i = 0; i < used; ++i)
-                                mbar_arrive(&empty[(ring + i) % S::stages]);
                     }
                     ++seen;
-                    ring += kOwn ? used : 1;
-                    if (kOwn)
-                        used = (min(step, end - (t + 1 - base) * step) + 31) / 32;
+                    ring += kOwn ? (keys + 31) / 32 : 1;
                 }
             };
             tiles(std::false_type{}, min(begin, g.ct), min(g.last, g.ct));
@@ -994,13 +1055,13 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     un2(z ? pm2[c] : l2[c], x[2 * c], x[2 * c + 1]);
                 warp_columns<kCols>(x, [](float u, float v) { return u + v; });
                 if (lane < kCols)
-                    wred[warp][z][lane] = x[0];
+                    wred[ww][z][lane] = x[0];
             }
             sync();
             const bool whole = g.starts && g.ends;
             const bool poison = g.wrong || bad_page[sb];
-            if (tid < g.rows) {
-                const int w4 = tid / kCols * 4, c = tid % kCols;
+            if (wt < g.rows) {
+                const int w4 = wt / kCols * 4, c = wt % kCols;
                 float sum = 0.0f, off = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -1010,32 +1071,32 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 if (poison)
                     sum = nan_f();
                 const bool none = !some || sum == 0.0f;
-                const float ref = none ? kFar : -nref[tid];
+                const float ref = none ? kFar : -nref[wt];
                 const float f =
-                    none ? 0.0f : exp2f(refz[tid] - ref) * (g.last > g.ct ? 1.0f : kSumUnit);
+                    none ? 0.0f : exp2f(refz[wt] - ref) * (g.last > g.ct ? 1.0f : kSumUnit);
                 if (whole) {
-                    const int r = g.r0 + tid, qi = r / a.group;
+                    const int r = g.r0 + wt, qi = r / a.group;
                     const int64_t row =
                         ((int64_t)g.b * a.Lq + qi) * a.Hq + g.h * a.group + r - qi * a.group;
                     const float inv = none ? 0.0f : 1.0f / sum;
-                    row_at[tid] = row * D;
-                    fl[tid] = off * inv;
-                    fo[tid] = f * inv;
+                    row_at[wt] = row * D;
+                    fl[wt] = off * inv;
+                    fo[wt] = f * inv;
                     if (a.lse)
                         a.lse[row] = none ? (poison ? nan_f() : neg_inf_f())
                                           : (ref + log2f(sum)) * 0.6931471805599453f;
                     if (poison)
-                        fl[tid] = nan_f();
+                        fl[wt] = nan_f();
                 } else {
-                    const int64_t at = ((int64_t)blockIdx.x * 2 + (g.starts ? 1 : 0)) * N + tid;
-                    row_at[tid] = at * D;
-                    fl[tid] = off;
-                    fo[tid] = f;
+                    const int64_t at = ((int64_t)blockIdx.x * 2 + (g.starts ? 1 : 0)) * N + wt;
+                    row_at[wt] = at * D;
+                    fl[wt] = off;
+                    fo[wt] = f;
                     a.part_refs[2 * at] = ref;
                     a.part_refs[2 * at + 1] = sum;
                 }
             }
-            if (tid == 0 && !whole) {
+            if (wt == 0 && !whole) {
                 if (g.starts) {
                     meta[kOpen] = 1;
                     meta[kOpenB] = g.b;
@@ -1046,13 +1107,13 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 }
             }
             if (seen > summed) {
-                wait(&o_done, summed & 1);
+                wait(&o_done[summed & 1], (summed >> 1) & 1);
                 ++summed;
             }
             tc::fence_after_sync();
             sync();
             const int d = key;
-            const int bad = some && any_bad ? first_bad[min(d, D - 1)] : 0x7FFFFFFF;
+            const int bad = some && any_bad[sb] ? first_bad[sb][min(d, D - 1)] : 0x7FFFFFFF;
 #pragma unroll 1
             for (int c8 = 0; c8 < kCols; c8 += 8) {
                 uint32_t o[8] = {0, 0, 0, 0, 0, 0, 0, 0};
@@ -1083,7 +1144,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
     tc::fence_before_sync();
     __syncthreads();
     tc::fence_after_sync();
-    if (warp == S::warps)
+    if (warp == S::issuer)
         tc::tmem_dealloc(tmem, S::tmem);
 }
 

@@ -245,27 +245,23 @@ __device__ __forceinline__ void fence_async_smem()
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
 }
 
-// mbar_wait for waits that are short as a rule.  The thread is suspended by the hardware for up
-// to kSuspendNs a try (tries in a loop take issue slots from the warps that work); the timer,
-// whose reading alone costs about as much as a tile, is looked at only after many.
-constexpr uint32_t kSuspendNs = 20000;
+// mbar_wait for waits that are short as a rule: the timer, whose reading alone costs about as
+// much as a tile, is looked at only after many tries.
 __device__ __forceinline__ bool mbar_wait_short(uint64_t *bar, uint32_t parity, uint32_t *status,
                                                 uint64_t limit_ns = kWaitLimitNs)
 {
 #pragma unroll 1
-    for (int i = 0; i < 64; ++i) {
-        uint32_t done;
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t"
-            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
-            "selp.u32 %0, 1, 0, p;\n\t}"
-            : "=r"(done)
-            : "r"(smem_addr(bar)), "r"(parity), "r"(kSuspendNs)
-            : "memory");
-        if (done)
+    for (int i = 0; i < 4096; ++i)
+        if (mbar_try_wait(bar, parity))
             return true;
-    }
     return mbar_wait(bar, parity, status, limit_ns);
+}
+
+// n arrivals at once.
+__device__ __forceinline__ void mbar_arrive_n(uint64_t *bar, uint32_t n)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(smem_addr(bar)), "r"(n)
+                 : "memory");
 }
 
 __device__ __forceinline__ float max3(float a, float b, float c)
