@@ -149,6 +149,7 @@ __device__ __forceinline__ void scale_sums(uint32_t taddr, const float *f, float
             s[c] = __float_as_uint(__uint_as_float(s[c]) * (f ? f[c8 + c] : u));
         tmem_st<8>(taddr + c8, s);
     }
+    tmem_wait_st();
 }
 
 // A unit's beginning and end cost about as much as this many tiles.
@@ -228,51 +229,51 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
     constexpr int D = S::D, N = S::N, kCols = S::cols, kOwnKeys = S::own_keys;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
-    __shared__ __align__(8) uint64_t full[S::stages], empty[S::stages];  // the ring
-    __shared__ __align__(8) uint64_t seg_full[2], seg_empty[2];
-    // of a tile, by its parity: keys and values unpacked, scores and sums done
-    __shared__ __align__(8) uint64_t k_ready[2], v_ready[2], s_done[2], o_done[2];
-    __shared__ __align__(8) uint64_t p_ready, voted;
+    // Barriers: the ring's stages full and empty; of a segment, by its parity, published and done
+    // with; of a tile, by its parity, keys and values unpacked, scores and sums done; weights
+    // given; the vote cast.
+    enum {
+        kFull = 0, kEmpty = kFull + S::stages, kSegFull = kEmpty + S::stages, kSegEmpty = kSegFull + 2,
+        kKReady = kSegEmpty + 2, kVReady = kKReady + 2, kSDone = kVReady + 2, kODone = kSDone + 2,
+        kPReady = kODone + 2, kVoted, kBars
+    };
+    __shared__ __align__(8) uint64_t bars[kBars];
     __shared__ uint32_t tmem_base;
     __shared__ int64_t scan[S::threads / 32];
     __shared__ int64_t find_base;
     __shared__ int find_b;
     __shared__ uint32_t vote[2];
-    // of a segment, by its parity: what it is, whether it met a page out of range, the queries'
-    // sums and a score's unit, the first own key with a non-finite value (by channel)
+    // of a segment, by its parity: what it is, whether it met a page out of range, a score's
+    // unit, the first own key with a non-finite value (by channel)
     __shared__ Segment segs[2];
     __shared__ int bad_page[2], any_bad[2];
-    __shared__ __align__(16) float sumq[2][N];
     __shared__ float q_unit[2], q_big[4];
     __shared__ int first_bad[2][D];
-    // per row: the reference (negated), 2^(ref - refz), the reference of the scaled weights
-    __shared__ __align__(16) float nref[N], cmul[N], refz[N];
-    __shared__ __align__(16) float fl[N], fo[N], redo[N];
-    __shared__ __align__(16) float none_row[S::cols];  // -inf: the references of absent keys
+    // per row: the reference (negated), 2^(ref - refz), the queries' sums (by the segment's
+    // parity); -inf, the references of absent keys; the reference of the scaled weights; factors
+    enum { kNref = 0, kCmul = N, kSumq = 2 * N, kNone = 4 * N, kRefz = 5 * N, kFl = 6 * N,
+           kFo = 7 * N, kRedo = 8 * N, kRowFloats = 9 * N };
+    __shared__ __align__(16) float rowf[kRowFloats];
+    float *const nref = rowf + kNref, *const cmul = rowf + kCmul, *const refz = rowf + kRefz;
+    float *const fl = rowf + kFl, *const fo = rowf + kFo, *const redo = rowf + kRedo;
     __shared__ int64_t row_at[N];
     __shared__ float wred[S::w_warps][2][kCols];
 
     const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31;
     if (tid == 0) {
-        for (int i = 0; i < S::stages; ++i) {
-            mbar_init(&full[i], 1);
-            mbar_init(&empty[i], 4 + S::w_warps);
+        for (int i = 0; i < kBars; ++i) {
+            const int n = i >= kEmpty && i < kSegFull        ? 4 + S::w_warps
+                          : i >= kSegEmpty && i < kKReady    ? 4 + S::w_warps + 1
+                          : i >= kKReady && i < kSDone       ? 4
+                          : i == kPReady || i == kVoted      ? S::w_warps
+                                                             : 1;
+            mbar_init(&bars[i], n);
         }
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(&seg_full[i], 1);
-            mbar_init(&seg_empty[i], 4 + S::w_warps + 1);
-            mbar_init(&k_ready[i], 4);
-            mbar_init(&v_ready[i], 4);
-            mbar_init(&s_done[i], 1);
-            mbar_init(&o_done[i], 1);
-            vote[i] = 0;
-        }
-        mbar_init(&p_ready, S::w_warps);
-        mbar_init(&voted, S::w_warps);
+        vote[0] = vote[1] = 0;
         fence_mbar_init();
     }
-    if (tid < S::cols)
-        none_row[tid] = neg_inf_f();
+    if (tid < N)
+        rowf[kNone + tid] = neg_inf_f();
     if (warp == S::issuer)
         tc::tmem_alloc(&tmem_base, S::tmem);
     if (warp == S::loader && lane == 0) {
@@ -323,17 +324,23 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
     const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, tmem_base, 0);
     pdl_launch_dependents();
 
+    // Addresses of the barriers and of the dynamic memory, kept rather than rebuilt.
+    uint32_t bar0 = smem_addr(bars), buf0 = smem_addr(smem), row0 = smem_addr(rowf);
+    asm volatile("" : "+r"(bar0), "+r"(buf0), "+r"(row0));
+    auto bar = [&](int i) { return bar0 + 8u * i; };
     bool dead = false;  // a wait gave up: no further wait, the walk goes on to its end
-    auto wait = [&](uint64_t *bar, uint32_t parity) {
-        if (!dead && !mbar_wait_short(bar, parity, &g_status))
+    auto wait = [&](int i, uint32_t parity) {
+        if (!dead && !mbar_wait_at<0>(bar(i), parity, &g_status))
             dead = true;
     };
-
-    // the same for a whole warp
-    auto wait_warp = [&](uint64_t *bar, uint32_t parity) {
-        wait(bar, parity);
+    // the same for a whole warp that waits most of its time
+    auto wait_warp = [&](auto sleep, int i, uint32_t parity) {
+        if (!dead && !mbar_wait_at<decltype(sleep)::value>(bar(i), parity, &g_status))
+            dead = true;
         dead = __any_sync(0xFFFFFFFFu, dead);
     };
+    using Long = std::integral_constant<int, 100>;
+    using Short = std::integral_constant<int, 20>;
 
     if (warp == S::loader) {
         // ---------------------------------------------------------------- the loading warp
@@ -349,7 +356,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
         for (uint32_t seg = 0;; ++seg) {
             const uint32_t sb = seg & 1;
             const bool more = w.next(a, units);
-            wait_warp(&seg_empty[sb], ((seg >> 1) & 1) ^ 1);
+            wait_warp(Long{}, kSegEmpty + (sb), ((seg >> 1) & 1) ^ 1);
             const int h = more ? w.unit / a.row_tiles : 0;
             const int r0 = more ? (w.unit - h * a.row_tiles) * N : 0;
             const int rows = min(N, a.rows - r0);
@@ -368,7 +375,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     g.wrong = w.s.wrong;
                     bad_page[sb] = 0;
                 }
-                mbar_arrive(&seg_full[sb]);
+                mbar_arrive(&bars[kSegFull + (sb)]);
             }
             __syncwarp();
             if (!more)
@@ -378,18 +385,18 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
             // The queries' rows.
             {
                 const uint32_t st = ring % S::stages;
-                wait_warp(&empty[st], ((ring / S::stages) & 1) ^ 1);
+                wait_warp(Long{}, kEmpty + (st), ((ring / S::stages) & 1) ^ 1);
                 uint8_t *buf = smem + st * S::stage_bytes;
                 if (!dead) {
                     if (lane == 0)
-                        mbar_arrive_expect_tx(&full[st], (uint32_t)rows * D * 2);
+                        mbar_arrive_expect_tx(&bars[kFull + st], (uint32_t)rows * D * 2);
                     __syncwarp();
                     for (int n = lane; n < rows; n += 32) {
                         const int qi = (r0 + n) / a.group, g = (r0 + n) - qi * a.group;
                         bulk_copy_g2s(buf + n * (D * 2),
                                       static_cast<const T *>(a.q) + w.b * a.qs.batch +
                                           qi * a.qs.token + (int64_t)(h * a.group + g) * a.qs.head,
-                                      D * 2, &full[st]);
+                                      D * 2, &bars[kFull + st]);
                     }
                 }
                 ++ring;
@@ -406,7 +413,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                                   : -2;
                 }
                 const uint32_t st = ring % S::stages;
-                wait_warp(&empty[st], ((ring / S::stages) & 1) ^ 1);
+                wait_warp(Long{}, kEmpty + (st), ((ring / S::stages) & 1) ^ 1);
                 uint8_t *buf = smem + st * S::stage_bytes;
                 // lane i < pieces copies piece i
                 const int pg = __shfl_sync(0xFFFFFFFFu, pg_lane, (batch & 31) + (lane & 3));
@@ -417,10 +424,10 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     if (bad)
                         bad_page[sb] = 1;
                     if (!dead && there)
-                        mbar_arrive_expect_tx(&full[st],
+                        mbar_arrive_expect_tx(&bars[kFull + st],
                                               (uint32_t)__popc(there) * span * (D + 8));
                     else if (!dead)
-                        mbar_arrive(&full[st]);
+                        mbar_arrive(&bars[kFull + (st)]);
                 }
                 __syncwarp();
                 if (mine && !dead) {
@@ -428,12 +435,12 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     const int in_page = (t * kKeys + i * span) & (page - 1);
                     const int64_t ph = (int64_t)pg * a.c.heads + h;
                     tc::tma_load_2d(buf + i * span * (D / 2), &k_map, 0, (int)(ph * page + in_page),
-                                    &full[st]);
+                                    &bars[kFull + st]);
                     tc::tma_load_2d(buf + S::code_bytes + i * (span / 2) * D, &v_map, in_page / 2,
-                                    (int)(ph * D), &full[st]);
+                                    (int)(ph * D), &bars[kFull + st]);
                     uint8_t *aff = buf + 2 * S::code_bytes + i * span * 4;
-                    bulk_copy_g2s(aff, a.c.ka + ph * page + in_page, span * 4, &full[st]);
-                    bulk_copy_g2s(aff + 512, a.c.va + ph * page + in_page, span * 4, &full[st]);
+                    bulk_copy_g2s(aff, a.c.ka + ph * page + in_page, span * 4, &bars[kFull + st]);
+                    bulk_copy_g2s(aff + 512, a.c.va + ph * page + in_page, span * 4, &bars[kFull + st]);
                 }
                 __syncwarp();
             }
@@ -442,23 +449,23 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 const int j1 = min(w.s.own, (t - w.s.ct + 1) * kOwnKeys);
                 for (int j0 = (t - w.s.ct) * kOwnKeys; j0 < j1; j0 += 32, ++ring) {
                     const uint32_t st = ring % S::stages;
-                    wait_warp(&empty[st], ((ring / S::stages) & 1) ^ 1);
+                    wait_warp(Long{}, kEmpty + (st), ((ring / S::stages) & 1) ^ 1);
                     uint8_t *buf = smem + st * S::stage_bytes;
                     const int n = min(32, j1 - j0);
                     if (dead)
                         continue;
                     if (lane == 0)
-                        mbar_arrive_expect_tx(&full[st], (uint32_t)n * D * 4);
+                        mbar_arrive_expect_tx(&bars[kFull + st], (uint32_t)n * D * 4);
                     __syncwarp();
                     if (lane < n) {
                         bulk_copy_g2s(buf + lane * S::own_row,
                                       static_cast<const T *>(a.k_new) + w.b * a.ks.batch +
                                           (int64_t)(j0 + lane) * a.ks.token + (int64_t)h * a.ks.head,
-                                      D * 2, &full[st]);
+                                      D * 2, &bars[kFull + st]);
                         bulk_copy_g2s(buf + S::own_v + lane * (D * 2),
                                       static_cast<const T *>(a.v_new) + w.b * a.vs.batch +
                                           (int64_t)(j0 + lane) * a.vs.token + (int64_t)h * a.vs.head,
-                                      D * 2, &full[st]);
+                                      D * 2, &bars[kFull + st]);
                     }
                     __syncwarp();
                 }
@@ -469,8 +476,8 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
         __syncwarp();
         for (uint32_t i = 0; i < min(ring, (uint32_t)S::stages); ++i) {
             const uint32_t r = ring - 1 - i;
-            mbar_wait_short(&full[r % S::stages], (r / S::stages) & 1, &g_status,
-                            dead ? kDrainLimitNs : kWaitLimitNs);
+            mbar_wait_at<100>(bar(kFull + r % S::stages), (r / S::stages) & 1, &g_status,
+                              dead ? kDrainLimitNs : kWaitLimitNs);
         }
     } else if (warp == S::issuer) {
         // ---------------------------------------------------------------- the issuing warp
@@ -483,18 +490,18 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
         uint32_t scores = 0, sums = 0;  // tiles issued so far
         for (uint32_t seg = 0;; ++seg) {
             const uint32_t sb = seg & 1;
-            wait_warp(&seg_full[sb], (seg >> 1) & 1);
+            wait_warp(Short{}, kSegFull + (sb), (seg >> 1) & 1);
             const int done = segs[sb].done, first = segs[sb].first, last = segs[sb].last;
             const int ct = segs[sb].ct, own_total = segs[sb].own;
             __syncwarp();
             if (lane == 0)
-                mbar_arrive(&seg_empty[sb]);
+                mbar_arrive(&bars[kSegEmpty + (sb)]);
             if (done)
                 break;
             for (int t = first; t <= last; ++t) {
                 if (t < last) {
                     const uint32_t par = scores & 1;
-                    wait_warp(&k_ready[par], (scores >> 1) & 1);
+                    wait_warp(Short{}, kKReady + (par), (scores >> 1) & 1);
                     tc::fence_after_sync();
                     const uint64_t q_desc = t < ct ? q16_desc : qt_desc;
                     const uint32_t idesc =
@@ -504,13 +511,13 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     for (int k = 0; k < D / 16; ++k)
                         mma_ts(tmem + S::tS + par * N, tK + 8 * k,
                                q_desc + (k >> 2) * ((N * 128) >> 4) + 2 * (k & 3), idesc, k > 0);
-                    mma_commit(&s_done[par]);
+                    mma_commit(&bars[kSDone + par]);
                     ++scores;
                 }
                 if (t > first) {
                     const uint32_t par = sums & 1;
-                    wait_warp(&v_ready[par], (sums >> 1) & 1);
-                    wait_warp(&p_ready, sums & 1);
+                    wait_warp(Short{}, kVReady + (par), (sums >> 1) & 1);
+                    wait_warp(Short{}, kPReady, sums & 1);
                     tc::fence_after_sync();
                     const uint32_t tV = tmem + S::tV + (S::bufs > 1 ? par * 64 : 0);
                     const uint32_t more = t - 1 > first;
@@ -536,7 +543,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                                    idesc, 1);
                         }
                     }
-                    mma_commit(&o_done[par]);
+                    mma_commit(&bars[kODone + par]);
                     ++sums;
                 }
             }
@@ -548,16 +555,30 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
         const int key = tid;
         const uint32_t lanes = tmem + ((uint32_t)warp << 21);
         uint32_t ring = 0, tile = 0;  // stages used, tiles unpacked so far
-        auto arrive = [&](uint64_t *bar, uint32_t n) {
+        auto arrive = [&](int i, uint32_t n) {
             __syncwarp();
-            if (lane == 0)
-                mbar_arrive_n(bar, n);
+            mbar_arrive_if(bar(i), lane == 0, n);
         };
+        // Where this thread's row of codes lies in a stage: 16-byte pieces, swizzled as the
+        // tensor maps say.
+        const uint32_t k_row = key * (D / 2) + ((D == 128 ? (key >> 1) & 3 : (key >> 2) & 1) << 4);
+        uint32_t v_piece[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int d = key;
+            v_piece[i] = S::code_bytes;
+            if (a.c.page_shift == 5)
+                v_piece[i] += i * (16 * D) + d * 16;
+            else if (a.c.page_shift == 6)
+                v_piece[i] += (i >> 1) * (32 * D) + d * 32 + (((i & 1) ^ ((d >> 2) & 1)) << 4);
+            else
+                v_piece[i] += d * 64 + ((i ^ ((d >> 1) & 3)) << 4);
+        }
         // Stages that only these warps read are given back for all.
         constexpr uint32_t kForAll = 1 + S::C;
         for (uint32_t seg = 0;; ++seg) {
             const uint32_t sb = seg & 1;
-            wait(&seg_full[sb], (seg >> 1) & 1);
+            wait(kSegFull + (sb), (seg >> 1) & 1);
             const Segment &g = segs[sb];
             if (g.done)
                 break;
@@ -565,7 +586,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
             if (first < last) {
                 // ---- the queries: their sums, and both operands (K-major, 128-byte swizzle)
                 const uint32_t st = ring % S::stages;
-                wait(&full[st], (ring / S::stages) & 1);
+                wait(kFull + (st), (ring / S::stages) & 1);
                 const uint8_t *raw = smem + st * S::stage_bytes;
                 constexpr int kMine = N * (D / 8) / 128;
                 float big = 0.0f;
@@ -589,7 +610,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     for (int s = D / 16; s > 0; s >>= 1)
                         sum += __shfl_xor_sync(0xFFFFFFFFu, sum, s);
                     if (c8 == 0)
-                        sumq[sb][n] = sum;
+                        rowf[kSumq + sb * N + n] = sum;
                 }
                 const uint32_t wbig = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(big));
                 named_sync(2, 128);  // (the segment before has read its own)
@@ -610,7 +631,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     q_unit[sb] = kCodeUnit * __uint_as_float((uint32_t)(127 + e0) << 23);
                 // the operands' last readers are done: the scores of the tile before
                 if (tile > 0)
-                    wait(&s_done[(tile - 1) & 1], ((tile - 1) >> 1) & 1);
+                    wait(kSDone + ((tile - 1) & 1), ((tile - 1) >> 1) & 1);
 #pragma unroll 2
                 for (int m = 0; m < kMine; ++m) {
                     const int i = tid + m * 128, n = i / (D / 8), c8 = i % (D / 8);
@@ -633,7 +654,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                         *reinterpret_cast<uint4 *>(smem + S::qt_off + at) = interleave8(x);
                 }
                 fence_async_smem();  // for the first tile's product
-                arrive(&empty[st], kForAll);
+                arrive(kEmpty + st, kForAll);
                 ++ring;
             }
             for (int t = first; t < last; ++t, ++tile) {
@@ -645,22 +666,21 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 const uint32_t tV = lanes + S::tV + (S::bufs > 1 ? par * 64 : 0);
                 // ---- keys; their place is free when the scores of `bufs` tiles before are done
                 if (tile >= S::bufs)
-                    wait(&s_done[(tile - S::bufs) & 1], ((tile - S::bufs) >> 1) & 1);
+                    wait(kSDone + ((tile - S::bufs) & 1), ((tile - S::bufs) >> 1) & 1);
                 if (cached) {
                     const uint32_t s1 = ring % S::stages;
-                    wait(&full[s1], (ring / S::stages) & 1);
+                    wait(kFull + (s1), (ring / S::stages) & 1);
                     tc::fence_after_sync();
-                    const uint8_t *row = smem + s1 * S::stage_bytes + key * (D / 2);
+                    const uint32_t row = buf0 + s1 * S::stage_bytes;
 #pragma unroll
                     for (int i = 0; i < D / 32; ++i) {
-                        const int sw = D == 128 ? (i ^ ((key >> 1) & 3)) : (i ^ ((key >> 2) & 1));
                         uint32_t y[16];
-                        unpack32(*reinterpret_cast<const uint4 *>(row + 16 * sw), y);
+                        unpack32(lds4(row + (k_row ^ (i << 4))), y);
                         tmem_st16(tK + 16 * i, y);
                     }
                 } else if (32 * warp < keys) {
                     const uint32_t r = ring + warp, s1 = r % S::stages;
-                    wait(&full[s1], (r / S::stages) & 1);
+                    wait(kFull + (s1), (r / S::stages) & 1);
                     tc::fence_after_sync();
                     const uint8_t *row = smem + s1 * S::stage_bytes + lane * S::own_row;
 #pragma unroll 1
@@ -680,35 +700,27 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 }
                 tmem_wait_st();
                 tc::fence_before_sync();
-                arrive(&k_ready[par], 1);
+                arrive(kKReady + (par), 1);
                 // ---- values; their place is free when the sums of `bufs` tiles before are done
                 if (tile >= S::bufs) {
-                    wait(&o_done[(tile - S::bufs) & 1], ((tile - S::bufs) >> 1) & 1);
+                    wait(kODone + ((tile - S::bufs) & 1), ((tile - S::bufs) >> 1) & 1);
                     tc::fence_after_sync();
                 }
                 const int d = key;
                 if (cached) {
-                    const uint8_t *v = smem + (ring % S::stages) * S::stage_bytes + S::code_bytes;
+                    const uint32_t at = buf0 + (ring % S::stages) * S::stage_bytes;
                     if (D == 128 || d < D)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {  // 32 slots
-                            int off;
-                            if (a.c.page_shift == 5)
-                                off = i * (16 * D) + d * 16;
-                            else if (a.c.page_shift == 6)
-                                off = (i >> 1) * (32 * D) + d * 32 +
-                                      (((i & 1) ^ ((d >> 2) & 1)) << 4);
-                            else
-                                off = d * 64 + ((i ^ ((d >> 1) & 3)) << 4);
                             uint32_t y[16];
-                            unpack32(*reinterpret_cast<const uint4 *>(v + off), y);
+                            unpack32(lds4(at + v_piece[i]), y);
                             tmem_st16(tV + 16 * i, y);
                         }
                 } else {
 #pragma unroll 1
                     for (int i = 0; i < used; ++i) {
                         const uint32_t r = ring + i, s1 = r % S::stages;
-                        wait(&full[s1], (r / S::stages) & 1);
+                        wait(kFull + (s1), (r / S::stages) & 1);
                         if (D == 128 || d < D) {
                             uint32_t y[16];
                             const int bad = own_values<T>(
@@ -726,15 +738,15 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 }
                 tmem_wait_st();
                 tc::fence_before_sync();
-                arrive(&v_ready[par], 1);
+                arrive(kVReady + (par), 1);
                 if (cached)
-                    arrive(&empty[ring % S::stages], 1);
+                    arrive(kEmpty + (ring % S::stages), 1);
                 else
                     for (int i = 0; i < used; ++i)
-                        arrive(&empty[(ring + i) % S::stages], kForAll);
+                        arrive(kEmpty + ((ring + i) % S::stages), kForAll);
                 ring += used;
             }
-            arrive(&seg_empty[sb], 1);
+            arrive(kSegEmpty + (sb), 1);
         }
     } else {
         // ---------------------------------------------------------------- the weights
@@ -743,7 +755,11 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
         const int wg = ww >> 2, quarter = ww & 3, key = wt & 127;
         const int col0 = wg * kCols;  // this thread's columns
         const uint32_t lanes = tmem + ((uint32_t)quarter << 21);
-        uint8_t *p_smem = smem + S::p_off, *lo_smem = smem + S::lo_off;
+        // where this thread's weights go: 16 bytes (8 rows of its key) a column group
+        const int kappa = (key & ~7) | ((key & 3) << 1) | ((key >> 2) & 1);
+        const uint32_t p_at = buf0 + S::p_off + (kappa >> 3) * (N * 16) + (col0 >> 3) * 128 +
+                              (kappa & 7) * 16;
+        const uint32_t cols_at = row0 + 4 * col0;
         uint32_t ring = 0;    // stages used so far
         uint32_t seen = 0;    // tiles whose weights were given
         uint32_t summed = 0;  // tiles whose sums were waited for
@@ -751,7 +767,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
 
         for (uint32_t seg = 0;; ++seg) {
             const uint32_t sb = seg & 1;
-            wait(&seg_full[sb], (seg >> 1) & 1);
+            wait(kSegFull + (sb), (seg >> 1) & 1);
             const Segment &g = segs[sb];
             if (g.done)
                 break;
@@ -778,18 +794,15 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     const int keys = min(step, end - (t - base) * step);
                     const uint32_t st = ring % S::stages;
                     const uint32_t tS = lanes + S::tS + (seen & 1) * N + col0;
-                    wait(&s_done[seen & 1], (seen >> 1) & 1);
+                    wait(kSDone + (seen & 1), (seen >> 1) & 1);
                     tc::fence_after_sync();
                     // this thread's key: scale and offset, for scores and weights
                     const int j = (t - base) * step + key;
                     const bool valid = key < keys;
                     float ks = a.scale, ko = 0.0f, vs = 1.0f, vo = 0.0f;
                     if constexpr (!kOwn) {
-                        const uint32_t *f =
-                            reinterpret_cast<const uint32_t *>(smem + st * S::stage_bytes +
-                                                               2 * S::code_bytes) +
-                            key;
-                        const uint32_t fk = f[0], fv = f[kKeys];
+                        const uint32_t f = buf0 + st * S::stage_bytes + 2 * S::code_bytes + 4 * key;
+                        const uint32_t fk = lds1(f), fv = lds1(f + 4 * kKeys);
                         ks = bf16_low(fk) * (a.scale * q_unit[sb]);
                         ko = bf16_high(fk) * a.scale;
                         vs = bf16_low(fv);
@@ -825,7 +838,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
 #pragma unroll
                                     for (int c = 0; c < 8; ++c) {
                                         const float y = fmaf(__uint_as_float(s[c]), ks,
-                                                             ko * sumq[sb][col0 + c8 + c]);
+                                                             ko * rowf[kSumq + sb * N + col0 + c8 + c]);
                                         x[c8 + c] = c8 + c >= first_col ? y + lv : neg_inf_f();
                                     }
                                 }
@@ -856,10 +869,8 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     // the references moved) only the rows of `redo` are summed again.
                     auto weights = [&](auto again) -> float {
                         constexpr bool kAgain = decltype(again)::value;
-                        const float4 *nr4 =
-                            reinterpret_cast<const float4 *>(valid ? nref + col0 : none_row);
-                        const float4 *cm4 = reinterpret_cast<const float4 *>(cmul + col0);
-                        const float4 *rd4 = reinterpret_cast<const float4 *>(redo + col0);
+                        const uint32_t nr_at = valid ? cols_at + 4 * kNref : cols_at + 4 * kNone;
+                        const uint32_t sq_at = cols_at + 4 * (kSumq + sb * N);
                         const uint64_t ks2 = f2(ks, ks), ko2 = f2(ko, ko);
                         const uint64_t vw2 = f2(vw, vw), vo2 = f2(vo, vo);
                         float top = 0.0f;
@@ -869,18 +880,18 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                             tmem_ld<8>(tS + c8, s);
 #pragma unroll
                             for (int c = c8; c < c8 + 8; c += 4) {
-                                const float4 nr = nr4[c / 4], cm = cm4[c / 4];
+                                const float4 nr = lds4f(nr_at + 4 * c);
+                                const float4 cm = lds4f(cols_at + 4 * (kCmul + c));
                                 uint64_t y[2] = {f2(nr.x, nr.y), f2(nr.z, nr.w)};
                                 if constexpr (!kOwn) {
-                                    const float4 sq =
-                                        reinterpret_cast<const float4 *>(sumq[sb] + col0)[c / 4];
+                                    const float4 sq = lds4f(sq_at + 4 * c);
                                     y[0] = fma2(ko2, f2(sq.x, sq.y), y[0]);
                                     y[1] = fma2(ko2, f2(sq.z, sq.w), y[1]);
                                 }
                                 const uint64_t cm2[2] = {f2(cm.x, cm.y), f2(cm.z, cm.w)};
                                 uint64_t rd2[2];
                                 if constexpr (kAgain) {
-                                    const float4 rd = rd4[c / 4];
+                                    const float4 rd = lds4f(cols_at + 4 * (kRedo + c));
                                     rd2[0] = f2(rd.x, rd.y), rd2[1] = f2(rd.z, rd.w);
                                 }
 #pragma unroll
@@ -934,21 +945,21 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                                 pl[i] = 0;
                         }
                     }
-                    if (lane == 0) {
-                        if (over)
+                    if (over) {
+                        if (lane == 0)
                             *reinterpret_cast<volatile uint32_t *>(&vote[seen & 1]) = seen + 1;
-                        mbar_arrive(&voted);
+                        __syncwarp();
                     }
-                    __syncwarp();
+                    mbar_arrive_if(bar(kVoted), lane == 0);
                     // the sums of the tile before must have read its weights
                     if (seen > summed) {
-                        wait(&o_done[summed & 1], (summed >> 1) & 1);
+                        wait(kODone + (summed & 1), (summed >> 1) & 1);
                         ++summed;
                         tc::fence_after_sync();
                     }
                     if (kOwn && t == from && from > begin)
                         scale_sums<kCols>(lanes + S::tO + col0, nullptr, kSumUnit);
-                    wait(&voted, seen & 1);
+                    wait(kVoted, seen & 1);
                     if (*reinterpret_cast<volatile uint32_t *>(&vote[seen & 1]) == seen + 1) {
                         // ---- the references move: per row, the running maxima of the scores
                         // and of the scores with the values' scale
@@ -963,7 +974,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
 #pragma unroll
                                 for (int c = 0; c < 8; ++c) {
                                     const float x = fmaf(__uint_as_float(s[c]), ks,
-                                                         ko * sumq[sb][col0 + c8 + c]);
+                                                         ko * rowf[kSumq + sb * N + col0 + c8 + c]);
                                     m[c8 + c] = c8 + c >= first_col ? x + (z ? lv : 0.0f)
                                                                     : neg_inf_f();
                                 }
@@ -1018,27 +1029,21 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     }
                     // ---- the weights (own tiles: the rows of absent stages are not read)
                     if (!kOwn || busy) {
-                        const int kappa = (key & ~7) | ((key & 3) << 1) | ((key >> 2) & 1);
-                        const int at =
-                            (kappa >> 3) * (N * 16) + (col0 >> 3) * 128 + (kappa & 7) * 16;
 #pragma unroll
                         for (int q = 0; q < kCols / 8; ++q) {
-                            *reinterpret_cast<uint4 *>(p_smem + at + 128 * q) =
-                                make_uint4(ph[4 * q], ph[4 * q + 1], ph[4 * q + 2], ph[4 * q + 3]);
+                            sts4(p_at + 128 * q, ph[4 * q], ph[4 * q + 1], ph[4 * q + 2],
+                                 ph[4 * q + 3]);
                             if constexpr (kSplit)
-                                *reinterpret_cast<uint4 *>(lo_smem + at + 128 * q) = make_uint4(
-                                    pl[4 * q], pl[4 * q + 1], pl[4 * q + 2], pl[4 * q + 3]);
+                                sts4(p_at + (S::lo_off - S::p_off) + 128 * q, pl[4 * q],
+                                     pl[4 * q + 1], pl[4 * q + 2], pl[4 * q + 3]);
                         }
                     }
-                    tmem_wait_st();  // (sums that were scaled)
                     fence_async_smem();
                     tc::fence_before_sync();
                     __syncwarp();
-                    if (lane == 0) {
-                        mbar_arrive(&p_ready);
-                        if (!kOwn)
-                            mbar_arrive(&empty[st]);
-                    }
+                    mbar_arrive_if(bar(kPReady), lane == 0);
+                    if (!kOwn)
+                        mbar_arrive_if(bar(kEmpty + st), lane == 0);
                     ++seen;
                     ring += kOwn ? (keys + 31) / 32 : 1;
                 }
@@ -1107,7 +1112,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 }
             }
             if (seen > summed) {
-                wait(&o_done[summed & 1], (summed >> 1) & 1);
+                wait(kODone + (summed & 1), (summed >> 1) & 1);
                 ++summed;
             }
             tc::fence_after_sync();
@@ -1138,7 +1143,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
             sync();  // the next segment overwrites the references and its sums
             tc::fence_after_sync();
             if (lane == 0)
-                mbar_arrive(&seg_empty[sb]);
+                mbar_arrive(&bars[kSegEmpty + (sb)]);
         }
     }
     tc::fence_before_sync();

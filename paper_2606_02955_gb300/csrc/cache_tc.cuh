@@ -245,22 +245,80 @@ __device__ __forceinline__ void fence_async_smem()
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
 }
 
-// mbar_wait for waits that are short as a rule: the timer, whose reading alone costs about as
-// much as a tile, is looked at only after many tries.
-__device__ __forceinline__ bool mbar_wait_short(uint64_t *bar, uint32_t parity, uint32_t *status,
-                                                uint64_t limit_ns = kWaitLimitNs)
+// mbar_wait on a shared-memory address, for waits that are short as a rule: the timer, whose
+// reading alone costs about as much as a tile, is looked at only after many tries.  kSleepNs: a
+// warp that waits most of its time sleeps between tries, which would take issue slots from the
+// warps that work.
+template <int kSleepNs>
+__device__ __forceinline__ bool mbar_wait_at(uint32_t bar, uint32_t parity, uint32_t *status,
+                                             uint64_t limit_ns = kWaitLimitNs)
 {
+    uint64_t t0 = 0;
 #pragma unroll 1
-    for (int i = 0; i < 4096; ++i)
-        if (mbar_try_wait(bar, parity))
+    for (uint32_t i = 1;; ++i) {
+        uint32_t done;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(done)
+            : "r"(bar), "r"(parity)
+            : "memory");
+        if (done)
             return true;
-    return mbar_wait(bar, parity, status, limit_ns);
+        if constexpr (kSleepNs > 0)
+            __nanosleep(kSleepNs);
+        if ((i & 1023u) == 0) {
+            const uint64_t t = global_timer_ns();
+            if (t0 == 0) {
+                t0 = t;
+            } else if (t - t0 > limit_ns) {
+                atomicOr(status, kDevStatTimeout);
+                return false;
+            }
+        }
+    }
 }
 
-// n arrivals at once.
-__device__ __forceinline__ void mbar_arrive_n(uint64_t *bar, uint32_t n)
+// An arrival by the lanes where `who` holds (a predicate, not a branch).
+__device__ __forceinline__ void mbar_arrive_if(uint32_t bar, bool who, uint32_t n = 1)
 {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(smem_addr(bar)), "r"(n)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.u32 p, %1, 0;\n\t"
+        "@p mbarrier.arrive.shared::cta.b64 _, [%0], %2;\n\t}" ::"r"(bar),
+        "r"((uint32_t)who), "r"(n)
+        : "memory");
+}
+
+// Shared memory by address (a base kept in a register, not rebuilt at each use).
+__device__ __forceinline__ float4 lds4f(uint32_t at)
+{
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                 : "r"(at)
+                 : "memory");
+    return v;
+}
+__device__ __forceinline__ uint4 lds4(uint32_t at)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                 : "r"(at)
+                 : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t lds1(uint32_t at)
+{
+    uint32_t v;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ void sts4(uint32_t at, uint32_t x, uint32_t y, uint32_t z, uint32_t w)
+{
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x), "r"(y), "r"(z), "r"(w)
                  : "memory");
 }
 
