@@ -38,6 +38,15 @@
 #include "cache.cuh"
 #include "cache_tc.cuh"
 
+#ifndef U_SLEEP
+#define U_SLEEP 20
+#endif
+#ifndef W_SLEEP
+#define W_SLEEP 0
+#endif
+#ifndef I_SLEEP
+#define I_SLEEP 20
+#endif
 namespace fdllm {
 namespace {
 
@@ -229,20 +238,23 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
     constexpr int D = S::D, N = S::N, kCols = S::cols, kOwnKeys = S::own_keys;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
-    // Barriers: the ring's stages full and empty; of a segment, by its parity, published and done
-    // with; of a tile, by its parity, keys and values unpacked, scores and sums done; weights
-    // given; the vote cast.
+    // Memory barriers: the ring's stages full and empty; of a segment, by its parity, published
+    // and done with; of a tile, by its parity, scores and sums done.
     enum {
         kFull = 0, kEmpty = kFull + S::stages, kSegFull = kEmpty + S::stages, kSegEmpty = kSegFull + 2,
-        kKReady = kSegEmpty + 2, kVReady = kKReady + 2, kSDone = kVReady + 2, kODone = kSDone + 2,
-        kPReady = kODone + 2, kVoted, kBars
+        kSDone = kSegEmpty + 2, kODone = kSDone + 2, kVoted = kODone + 2, kKR, kVR = kKR + 2, kPR = kVR + 2, kBars
     };
+    // CTA barriers, between warps (these block without a poll): the weights' warps, the
+    // unpacking warps; to the issuing warp, weights given, keys unpacked, values unpacked (by the
+    // tile's parity; none is two tiles ahead).
+    enum { kBarW = 1, kBarU, kBarPReady, kBarKReady, kBarVReady = kBarKReady + 2 };
     __shared__ __align__(8) uint64_t bars[kBars];
     __shared__ uint32_t tmem_base;
+    __shared__ uint32_t vote[2];
+    if (threadIdx.x == 0) vote[0] = vote[1] = 0;
     __shared__ int64_t scan[S::threads / 32];
     __shared__ int64_t find_base;
     __shared__ int find_b;
-    __shared__ uint32_t vote[2];
     // of a segment, by its parity: what it is, whether it met a page out of range, a score's
     // unit, the first own key with a non-finite value (by channel)
     __shared__ Segment segs[2];
@@ -262,14 +274,12 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
     const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31;
     if (tid == 0) {
         for (int i = 0; i < kBars; ++i) {
-            const int n = i >= kEmpty && i < kSegFull        ? 4 + S::w_warps
-                          : i >= kSegEmpty && i < kKReady    ? 4 + S::w_warps + 1
-                          : i >= kKReady && i < kSDone       ? 4
-                          : i == kPReady || i == kVoted      ? S::w_warps
-                                                             : 1;
+            const int n = i >= kEmpty && i < kSegFull     ? 4 + S::w_warps
+                          : i >= kSegEmpty && i < kSDone ? 4 + S::w_warps + 1
+                          : i == kVoted || i == kPR ? S::w_warps : i >= kKR && i < kPR ? 4
+                                                         : 1;
             mbar_init(&bars[i], n);
         }
-        vote[0] = vote[1] = 0;
         fence_mbar_init();
     }
     if (tid < N)
@@ -330,7 +340,11 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
     auto bar = [&](int i) { return bar0 + 8u * i; };
     bool dead = false;  // a wait gave up: no further wait, the walk goes on to its end
     auto wait = [&](int i, uint32_t parity) {
-        if (!dead && !mbar_wait_at<0>(bar(i), parity, &g_status))
+        if (!dead && !mbar_wait_at<W_SLEEP>(bar(i), parity, &g_status))
+            dead = true;
+    };
+    auto wait_u = [&](int i, uint32_t parity) {
+        if (!dead && !mbar_wait_at<U_SLEEP>(bar(i), parity, &g_status))
             dead = true;
     };
     // the same for a whole warp that waits most of its time
@@ -340,7 +354,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
         dead = __any_sync(0xFFFFFFFFu, dead);
     };
     using Long = std::integral_constant<int, 100>;
-    using Short = std::integral_constant<int, 20>;
+    using Short = std::integral_constant<int, I_SLEEP>;
 
     if (warp == S::loader) {
         // ---------------------------------------------------------------- the loading warp
@@ -501,7 +515,11 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
             for (int t = first; t <= last; ++t) {
                 if (t < last) {
                     const uint32_t par = scores & 1;
-                    wait_warp(Short{}, kKReady + (par), (scores >> 1) & 1);
+#ifdef F_MREADY
+                    wait_warp(Short{}, kKR + (par), (scores >> 1) & 1);
+#else
+                    named_sync(kBarKReady + par, 128 + 32);
+#endif
                     tc::fence_after_sync();
                     const uint64_t q_desc = t < ct ? q16_desc : qt_desc;
                     const uint32_t idesc =
@@ -516,8 +534,13 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 }
                 if (t > first) {
                     const uint32_t par = sums & 1;
-                    wait_warp(Short{}, kVReady + (par), (sums >> 1) & 1);
-                    wait_warp(Short{}, kPReady, sums & 1);
+#ifdef F_MREADY
+                    wait_warp(Short{}, kVR + (par), (sums >> 1) & 1);
+                    wait_warp(Short{}, kPR, sums & 1);
+#else
+                    named_sync(kBarVReady + par, 128 + 32);
+                    named_sync(kBarPReady, S::w_threads + 32);
+#endif
                     tc::fence_after_sync();
                     const uint32_t tV = tmem + S::tV + (S::bufs > 1 ? par * 64 : 0);
                     const uint32_t more = t - 1 > first;
@@ -578,7 +601,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
         constexpr uint32_t kForAll = 1 + S::C;
         for (uint32_t seg = 0;; ++seg) {
             const uint32_t sb = seg & 1;
-            wait(kSegFull + (sb), (seg >> 1) & 1);
+            wait_u(kSegFull + (sb), (seg >> 1) & 1);
             const Segment &g = segs[sb];
             if (g.done)
                 break;
@@ -586,7 +609,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
             if (first < last) {
                 // ---- the queries: their sums, and both operands (K-major, 128-byte swizzle)
                 const uint32_t st = ring % S::stages;
-                wait(kFull + (st), (ring / S::stages) & 1);
+                wait_u(kFull + (st), (ring / S::stages) & 1);
                 const uint8_t *raw = smem + st * S::stage_bytes;
                 constexpr int kMine = N * (D / 8) / 128;
                 float big = 0.0f;
@@ -613,14 +636,14 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                         rowf[kSumq + sb * N + n] = sum;
                 }
                 const uint32_t wbig = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(big));
-                named_sync(2, 128);  // (the segment before has read its own)
+                named_sync(kBarU, 128);  // (the segment before has read its own)
                 if (lane == 0)
                     q_big[warp] = __uint_as_float(wbig);
                 if (tid < D)
                     first_bad[sb][tid] = 0x7FFFFFFF;
                 if (tid == 0)
                     any_bad[sb] = 0;
-                named_sync(2, 128);
+                named_sync(kBarU, 128);
                 big = fmaxf(fmaxf(q_big[0], q_big[1]), fmaxf(q_big[2], q_big[3]));
                 // 2^-e with e the exponent of the largest, less 13; 0 stays 0
                 const int e = big > 0.0f ? (int)(__float_as_uint(big) >> 23) - 127 - 13 : 0;
@@ -631,7 +654,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     q_unit[sb] = kCodeUnit * __uint_as_float((uint32_t)(127 + e0) << 23);
                 // the operands' last readers are done: the scores of the tile before
                 if (tile > 0)
-                    wait(kSDone + ((tile - 1) & 1), ((tile - 1) >> 1) & 1);
+                    wait_u(kSDone + ((tile - 1) & 1), ((tile - 1) >> 1) & 1);
 #pragma unroll 2
                 for (int m = 0; m < kMine; ++m) {
                     const int i = tid + m * 128, n = i / (D / 8), c8 = i % (D / 8);
@@ -666,10 +689,10 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 const uint32_t tV = lanes + S::tV + (S::bufs > 1 ? par * 64 : 0);
                 // ---- keys; their place is free when the scores of `bufs` tiles before are done
                 if (tile >= S::bufs)
-                    wait(kSDone + ((tile - S::bufs) & 1), ((tile - S::bufs) >> 1) & 1);
+                    wait_u(kSDone + ((tile - S::bufs) & 1), ((tile - S::bufs) >> 1) & 1);
                 if (cached) {
                     const uint32_t s1 = ring % S::stages;
-                    wait(kFull + (s1), (ring / S::stages) & 1);
+                    wait_u(kFull + (s1), (ring / S::stages) & 1);
                     tc::fence_after_sync();
                     const uint32_t row = buf0 + s1 * S::stage_bytes;
 #pragma unroll
@@ -680,7 +703,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     }
                 } else if (32 * warp < keys) {
                     const uint32_t r = ring + warp, s1 = r % S::stages;
-                    wait(kFull + (s1), (r / S::stages) & 1);
+                    wait_u(kFull + (s1), (r / S::stages) & 1);
                     tc::fence_after_sync();
                     const uint8_t *row = smem + s1 * S::stage_bytes + lane * S::own_row;
 #pragma unroll 1
@@ -700,10 +723,14 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 }
                 tmem_wait_st();
                 tc::fence_before_sync();
-                arrive(kKReady + (par), 1);
+#ifdef F_MREADY
+                arrive(kKR + par, 1);
+#else
+                named_arrive(kBarKReady + par, 128 + 32);
+#endif
                 // ---- values; their place is free when the sums of `bufs` tiles before are done
                 if (tile >= S::bufs) {
-                    wait(kODone + ((tile - S::bufs) & 1), ((tile - S::bufs) >> 1) & 1);
+                    wait_u(kODone + ((tile - S::bufs) & 1), ((tile - S::bufs) >> 1) & 1);
                     tc::fence_after_sync();
                 }
                 const int d = key;
@@ -720,7 +747,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
 #pragma unroll 1
                     for (int i = 0; i < used; ++i) {
                         const uint32_t r = ring + i, s1 = r % S::stages;
-                        wait(kFull + (s1), (r / S::stages) & 1);
+                        wait_u(kFull + (s1), (r / S::stages) & 1);
                         if (D == 128 || d < D) {
                             uint32_t y[16];
                             const int bad = own_values<T>(
@@ -738,7 +765,11 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 }
                 tmem_wait_st();
                 tc::fence_before_sync();
-                arrive(kVReady + (par), 1);
+#ifdef F_MREADY
+                arrive(kVR + par, 1);
+#else
+                named_arrive(kBarVReady + par, 128 + 32);
+#endif
                 if (cached)
                     arrive(kEmpty + (ring % S::stages), 1);
                 else
@@ -763,7 +794,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
         uint32_t ring = 0;    // stages used so far
         uint32_t seen = 0;    // tiles whose weights were given
         uint32_t summed = 0;  // tiles whose sums were waited for
-        auto sync = [&] { named_sync(1, S::w_threads); };
+        auto sync = [&] { named_sync(kBarW, S::w_threads); };
 
         for (uint32_t seg = 0;; ++seg) {
             const uint32_t sb = seg & 1;
@@ -936,7 +967,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     const bool busy = 32 * quarter < keys;  // some key of this warp exists
                     bool over = false;
                     if (busy) {
-                        over = __any_sync(0xFFFFFFFFu, weights(std::false_type{}) > kTopWeight);
+                        over = weights(std::false_type{}) > kTopWeight;
                     } else {
 #pragma unroll
                         for (int i = 0; i < kCols / 2; ++i) {
@@ -945,12 +976,15 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                                 pl[i] = 0;
                         }
                     }
+#ifdef F_MVOTE
+                    over = __any_sync(0xFFFFFFFFu, over);
                     if (over) {
                         if (lane == 0)
                             *reinterpret_cast<volatile uint32_t *>(&vote[seen & 1]) = seen + 1;
                         __syncwarp();
                     }
                     mbar_arrive_if(bar(kVoted), lane == 0);
+#endif
                     // the sums of the tile before must have read its weights
                     if (seen > summed) {
                         wait(kODone + (summed & 1), (summed >> 1) & 1);
@@ -959,8 +993,12 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     }
                     if (kOwn && t == from && from > begin)
                         scale_sums<kCols>(lanes + S::tO + col0, nullptr, kSumUnit);
+#ifdef F_MVOTE
                     wait(kVoted, seen & 1);
                     if (*reinterpret_cast<volatile uint32_t *>(&vote[seen & 1]) == seen + 1) {
+#else
+                    if (named_sync_or(kBarW, S::w_threads, over)) {
+#endif
                         // ---- the references move: per row, the running maxima of the scores
                         // and of the scores with the values' scale
                         const float lv = vs > 0.0f ? log2f(vs) : neg_inf_f();
@@ -1040,8 +1078,12 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     }
                     fence_async_smem();
                     tc::fence_before_sync();
+#ifdef F_MREADY
                     __syncwarp();
-                    mbar_arrive_if(bar(kPReady), lane == 0);
+                    mbar_arrive_if(bar(kPR), lane == 0);
+#else
+                    named_arrive(kBarPReady, S::w_threads + 32);
+#endif
                     if (!kOwn)
                         mbar_arrive_if(bar(kEmpty + st), lane == 0);
                     ++seen;

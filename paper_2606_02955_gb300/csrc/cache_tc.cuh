@@ -249,22 +249,41 @@ __device__ __forceinline__ void fence_async_smem()
 // reading alone costs about as much as a tile, is looked at only after many tries.  kSleepNs: a
 // warp that waits most of its time sleeps between tries, which would take issue slots from the
 // warps that work.
+#ifndef W_DELAY
+#define W_DELAY 1
+#endif
+__device__ __forceinline__ void clock_delay()
+{
+    uint32_t c;
+    asm volatile("mov.u32 %0, %%clock;" : "=r"(c));
+}
+
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
+{
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return done != 0;
+}
+
+#ifdef F_NOINLINE
+#define F_INL __noinline__
+#else
+#define F_INL __forceinline__
+#endif
 template <int kSleepNs>
-__device__ __forceinline__ bool mbar_wait_at(uint32_t bar, uint32_t parity, uint32_t *status,
-                                             uint64_t limit_ns = kWaitLimitNs)
+__device__ F_INL bool mbar_wait_long(uint32_t bar, uint32_t parity, uint32_t *status,
+                                            uint64_t limit_ns)
 {
     uint64_t t0 = 0;
 #pragma unroll 1
     for (uint32_t i = 1;; ++i) {
-        uint32_t done;
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t"
-            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-            "selp.u32 %0, 1, 0, p;\n\t}"
-            : "=r"(done)
-            : "r"(bar), "r"(parity)
-            : "memory");
-        if (done)
+        if (mbar_try(bar, parity))
             return true;
         if constexpr (kSleepNs > 0)
             __nanosleep(kSleepNs);
@@ -278,6 +297,17 @@ __device__ __forceinline__ bool mbar_wait_at(uint32_t bar, uint32_t parity, uint
             }
         }
     }
+}
+
+template <int kSleepNs>
+__device__ __forceinline__ bool mbar_wait_at(uint32_t bar, uint32_t parity, uint32_t *status,
+                                             uint64_t limit_ns = kWaitLimitNs)
+{
+#ifdef F_FIRST
+    if (mbar_try(bar, parity))
+        return true;
+#endif
+    return mbar_wait_long<kSleepNs>(bar, parity, status, limit_ns);
 }
 
 // An arrival by the lanes where `who` holds (a predicate, not a branch).
@@ -332,7 +362,12 @@ __device__ __forceinline__ float max3(float a, float b, float c)
 // ---------------------------------------------------------------- barriers of some of a CTA's warps
 __device__ __forceinline__ void named_sync(int id, int threads)
 {
-    asm volatile("barrier.cta.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+    asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+
+__device__ __forceinline__ void named_arrive(int id, int threads)
+{
+    asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
 
 __device__ __forceinline__ bool named_sync_or(int id, int threads, bool x)
@@ -341,7 +376,7 @@ __device__ __forceinline__ bool named_sync_or(int id, int threads, bool x)
     asm volatile(
         "{\n\t.reg .pred p, q;\n\t"
         "setp.ne.u32 p, %3, 0;\n\t"
-        "barrier.cta.red.or.pred q, %1, %2, p;\n\t"
+        "bar.red.or.pred q, %1, %2, p;\n\t"
         "selp.u32 %0, 1, 0, q;\n\t}"
         : "=r"(r)
         : "r"(id), "r"(threads), "r"((uint32_t)x)
