@@ -80,6 +80,26 @@ inline bool aligned16(const void *p, const int64_t *strides, int n, int esize)
 
 inline Strides3 strides3(const int64_t *s) { return Strides3{s[0], s[1], s[2]}; }
 
+// SMs of the current device (152, a GB300's, where there is none to ask).
+inline int sm_count()
+{
+    static int cached[64] = {0};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
+        cudaGetLastError();
+        return 152;
+    }
+    if (cached[dev] == 0) {
+        int n = 0;
+        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) {
+            cudaGetLastError();
+            return 152;
+        }
+        cached[dev] = n;
+    }
+    return cached[dev];
+}
+
 // One kernel launch; `pdl` makes it a programmatic dependent of the stream's previous kernel
 // (the kernel then waits with pdl_wait() before it touches memory).
 template <typename... P, typename... A>

@@ -38,15 +38,6 @@
 #include "cache.cuh"
 #include "cache_tc.cuh"
 
-#ifndef U_SLEEP
-#define U_SLEEP 20
-#endif
-#ifndef W_SLEEP
-#define W_SLEEP 0
-#endif
-#ifndef I_SLEEP
-#define I_SLEEP 20
-#endif
 namespace fdllm {
 namespace {
 
@@ -89,7 +80,7 @@ template <int D_, int N_>
 struct Shape {
     static constexpr int D = D_;
     static constexpr int N = N_;                       // rows of a row tile
-    static constexpr int C = N >= 64 ? 4 : N / 16;     // warpgroups sharing a tile's columns
+    static constexpr int C = N / 16;     // warpgroups sharing a tile's columns
     static constexpr int cols = N / C;                 // columns (rows of the problem) a thread
     static constexpr int w_warps = 4 * C;              // warps that make weights
     static constexpr int w_threads = 32 * w_warps;
@@ -98,8 +89,8 @@ struct Shape {
     static constexpr int issuer = loader + 1;
     static constexpr int threads = 32 * (issuer + 1);
     static constexpr int ctas = N >= 64 ? 1 : 2;       // CTAs an SM holds
-    static constexpr int bufs = N >= 64 ? 2 : 1;       // of unpacked keys, and of values
-    static constexpr int stages = N >= 64 ? 8 : 4;
+    static constexpr int bufs = ctas == 1 ? 2 : 1;       // of unpacked keys, and of values
+    static constexpr int stages = ctas == 1 ? 8 : 4;
     // own keys come 32 to a stage; a block's 32 fill one tile, long prompts whole ones
     static constexpr int own_keys = N >= 64 ? 128 : 32;
     static constexpr int code_bytes = kKeys * D / 2;   // of keys, or of values
@@ -239,19 +230,17 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
     // Memory barriers: the ring's stages full and empty; of a segment, by its parity, published
-    // and done with; of a tile, by its parity, scores and sums done.
+    // and done with; of a tile, by its parity, scores and sums done, keys and values
+    // unpacked; weights given.  Every wait follows its barrier phase by phase (one that was two
+    // phases ahead would take the phase before last for its own).
     enum {
         kFull = 0, kEmpty = kFull + S::stages, kSegFull = kEmpty + S::stages, kSegEmpty = kSegFull + 2,
-        kSDone = kSegEmpty + 2, kODone = kSDone + 2, kVoted = kODone + 2, kKR, kVR = kKR + 2, kPR = kVR + 2, kBars
+        kSDone = kSegEmpty + 2, kODone = kSDone + 2, kKReady = kODone + 2, kVReady = kKReady + 2,
+        kPReady = kVReady + 2, kBars
     };
-    // CTA barriers, between warps (these block without a poll): the weights' warps, the
-    // unpacking warps; to the issuing warp, weights given, keys unpacked, values unpacked (by the
-    // tile's parity; none is two tiles ahead).
-    enum { kBarW = 1, kBarU, kBarPReady, kBarKReady, kBarVReady = kBarKReady + 2 };
+    enum { kBarW = 1, kBarU };  // CTA barriers: the weights' warps, the unpacking warps
     __shared__ __align__(8) uint64_t bars[kBars];
     __shared__ uint32_t tmem_base;
-    __shared__ uint32_t vote[2];
-    if (threadIdx.x == 0) vote[0] = vote[1] = 0;
     __shared__ int64_t scan[S::threads / 32];
     __shared__ int64_t find_base;
     __shared__ int find_b;
@@ -276,7 +265,8 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
         for (int i = 0; i < kBars; ++i) {
             const int n = i >= kEmpty && i < kSegFull     ? 4 + S::w_warps
                           : i >= kSegEmpty && i < kSDone ? 4 + S::w_warps + 1
-                          : i == kVoted || i == kPR ? S::w_warps : i >= kKR && i < kPR ? 4
+                          : i >= kKReady && i < kPReady  ? 4
+                          : i == kPReady                 ? S::w_warps
                                                          : 1;
             mbar_init(&bars[i], n);
         }
@@ -340,11 +330,11 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
     auto bar = [&](int i) { return bar0 + 8u * i; };
     bool dead = false;  // a wait gave up: no further wait, the walk goes on to its end
     auto wait = [&](int i, uint32_t parity) {
-        if (!dead && !mbar_wait_at<W_SLEEP>(bar(i), parity, &g_status))
+        if (!dead && !mbar_wait_at<0>(bar(i), parity, &g_status))
             dead = true;
     };
     auto wait_u = [&](int i, uint32_t parity) {
-        if (!dead && !mbar_wait_at<U_SLEEP>(bar(i), parity, &g_status))
+        if (!dead && !mbar_wait_at<20>(bar(i), parity, &g_status))
             dead = true;
     };
     // the same for a whole warp that waits most of its time
@@ -354,7 +344,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
         dead = __any_sync(0xFFFFFFFFu, dead);
     };
     using Long = std::integral_constant<int, 100>;
-    using Short = std::integral_constant<int, I_SLEEP>;
+    using Now = std::integral_constant<int, 0>;
 
     if (warp == S::loader) {
         // ---------------------------------------------------------------- the loading warp
@@ -504,7 +494,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
         uint32_t scores = 0, sums = 0;  // tiles issued so far
         for (uint32_t seg = 0;; ++seg) {
             const uint32_t sb = seg & 1;
-            wait_warp(Short{}, kSegFull + (sb), (seg >> 1) & 1);
+            wait_warp(Now{}, kSegFull + (sb), (seg >> 1) & 1);
             const int done = segs[sb].done, first = segs[sb].first, last = segs[sb].last;
             const int ct = segs[sb].ct, own_total = segs[sb].own;
             __syncwarp();
@@ -515,11 +505,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
             for (int t = first; t <= last; ++t) {
                 if (t < last) {
                     const uint32_t par = scores & 1;
-#ifdef F_MREADY
-                    wait_warp(Short{}, kKR + (par), (scores >> 1) & 1);
-#else
-                    named_sync(kBarKReady + par, 128 + 32);
-#endif
+                    wait_warp(Now{}, kKReady + par, (scores >> 1) & 1);
                     tc::fence_after_sync();
                     const uint64_t q_desc = t < ct ? q16_desc : qt_desc;
                     const uint32_t idesc =
@@ -534,13 +520,8 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 }
                 if (t > first) {
                     const uint32_t par = sums & 1;
-#ifdef F_MREADY
-                    wait_warp(Short{}, kVR + (par), (sums >> 1) & 1);
-                    wait_warp(Short{}, kPR, sums & 1);
-#else
-                    named_sync(kBarVReady + par, 128 + 32);
-                    named_sync(kBarPReady, S::w_threads + 32);
-#endif
+                    wait_warp(Now{}, kVReady + par, (sums >> 1) & 1);
+                    wait_warp(Now{}, kPReady, sums & 1);
                     tc::fence_after_sync();
                     const uint32_t tV = tmem + S::tV + (S::bufs > 1 ? par * 64 : 0);
                     const uint32_t more = t - 1 > first;
@@ -645,11 +626,8 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     any_bad[sb] = 0;
                 named_sync(kBarU, 128);
                 big = fmaxf(fmaxf(q_big[0], q_big[1]), fmaxf(q_big[2], q_big[3]));
-                // 2^-e with e the exponent of the largest, less 13; 0 stays 0
-                const int e = big > 0.0f ? (int)(__float_as_uint(big) >> 23) - 127 - 13 : 0;
-                const int e0 = min(max(e, -100), 100);
+                const int e0 = query_exponent(big);
                 const float unit = __uint_as_float((uint32_t)(127 - e0) << 23);
-                const float odd = unit * 0.0625f;  // the codes of odd channels are 16 times as large
                 if (tid == 0)
                     q_unit[sb] = kCodeUnit * __uint_as_float((uint32_t)(127 + e0) << 23);
                 // the operands' last readers are done: the scores of the tile before
@@ -661,18 +639,8 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     uint4 x = make_uint4(0, 0, 0, 0);
                     if (n < g.rows)
                         x = *reinterpret_cast<const uint4 *>(raw + 16 * i);
-                    float f[8];
-                    const uint32_t xw[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                    for (int v = 0; v < 4; ++v)
-                        unpack2<T>(xw[v], f[2 * v], f[2 * v + 1]);
                     const int at = (c8 >> 3) * (N * 128) + n * 128 + (((c8 & 7) ^ (n & 7)) << 4);
-                    // pairs (c, c + 4)
-                    *reinterpret_cast<uint4 *>(smem + S::q16_off + at) =
-                        make_uint4(pack2<__half>(f[0] * unit, f[4] * unit),
-                                   pack2<__half>(f[1] * odd, f[5] * odd),
-                                   pack2<__half>(f[2] * unit, f[6] * unit),
-                                   pack2<__half>(f[3] * odd, f[7] * odd));
+                    *reinterpret_cast<uint4 *>(smem + S::q16_off + at) = code_queries<T>(x, unit);
                     if (last > ct)
                         *reinterpret_cast<uint4 *>(smem + S::qt_off + at) = interleave8(x);
                 }
@@ -723,11 +691,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 }
                 tmem_wait_st();
                 tc::fence_before_sync();
-#ifdef F_MREADY
-                arrive(kKR + par, 1);
-#else
-                named_arrive(kBarKReady + par, 128 + 32);
-#endif
+                arrive(kKReady + par, 1);
                 // ---- values; their place is free when the sums of `bufs` tiles before are done
                 if (tile >= S::bufs) {
                     wait_u(kODone + ((tile - S::bufs) & 1), ((tile - S::bufs) >> 1) & 1);
@@ -765,11 +729,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 }
                 tmem_wait_st();
                 tc::fence_before_sync();
-#ifdef F_MREADY
-                arrive(kVR + par, 1);
-#else
-                named_arrive(kBarVReady + par, 128 + 32);
-#endif
+                arrive(kVReady + par, 1);
                 if (cached)
                     arrive(kEmpty + (ring % S::stages), 1);
                 else
@@ -820,6 +780,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 const int end = kOwn ? g.own : g.cached;
                 const int base = kOwn ? g.ct : 0;
                 constexpr int step = kOwn ? kOwnKeys : kKeys;
+                float k_factor = 0.0f;  // (the queries' unit is there with the first scores)
 #pragma unroll 1
                 for (int t = from; t < to; ++t) {
                     const int keys = min(step, end - (t - base) * step);
@@ -827,6 +788,8 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     const uint32_t tS = lanes + S::tS + (seen & 1) * N + col0;
                     wait(kSDone + (seen & 1), (seen >> 1) & 1);
                     tc::fence_after_sync();
+                    if (!kOwn && t == from)
+                        k_factor = a.scale * q_unit[sb];
                     // this thread's key: scale and offset, for scores and weights
                     const int j = (t - base) * step + key;
                     const bool valid = key < keys;
@@ -834,7 +797,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     if constexpr (!kOwn) {
                         const uint32_t f = buf0 + st * S::stage_bytes + 2 * S::code_bytes + 4 * key;
                         const uint32_t fk = lds1(f), fv = lds1(f + 4 * kKeys);
-                        ks = bf16_low(fk) * (a.scale * q_unit[sb]);
+                        ks = bf16_low(fk) * k_factor;
                         ko = bf16_high(fk) * a.scale;
                         vs = bf16_low(fv);
                         vo = bf16_high(fv);
@@ -857,40 +820,37 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                                 0xFFFFFFFFu, vs > 0.0f ? __float_as_uint(vs) : 0x7F800000u));
                             // scales within a factor of 2^8: the largest stands for all
                             const bool alike = !(big > 256.0f * small);
-                            float ref = kFar, z = kFar;
+                            const float lv = vs > 0.0f ? log2f(vs) : neg_inf_f();
 #pragma unroll 1
-                            for (int pass = 0; pass < (alike ? 1 : 2); ++pass) {
-                                const float lv = pass == 0 ? 0.0f : vs > 0.0f ? log2f(vs) : neg_inf_f();
-                                float x[kCols];
-#pragma unroll
-                                for (int c8 = 0; c8 < kCols; c8 += 8) {
+                            for (int c8 = 0; c8 < kCols; c8 += 8) {
+                                float x[8];
+                                auto largest = [&](float more) {
                                     uint32_t s[8];
                                     tmem_ld<8>(tS + c8, s);
 #pragma unroll
                                     for (int c = 0; c < 8; ++c) {
                                         const float y = fmaf(__uint_as_float(s[c]), ks,
                                                              ko * rowf[kSumq + sb * N + col0 + c8 + c]);
-                                        x[c8 + c] = c8 + c >= first_col ? y + lv : neg_inf_f();
+                                        x[c] = c8 + c >= first_col ? y + more : neg_inf_f();
                                     }
+                                    warp_columns<8>(x, [](float u, float v) { return fmaxf(u, v); });
+                                    return x[0] == neg_inf_f()    ? kFar
+                                           : fabsf(x[0]) < 1e30f ? x[0]
+                                                                 : 0.0f;
+                                };
+                                const float ref = largest(0.0f);
+                                float z = kFar;
+                                if (!alike)
+                                    z = largest(lv);
+                                else if (big > 0.0f)
+                                    z = ref + log2f(big);
+                                if (lane < 8) {
+                                    const int n = col0 + c8 + lane;
+                                    z = fmaxf(z, ref - kMaxShift);
+                                    nref[n] = -ref;
+                                    refz[n] = z;
+                                    cmul[n] = ref == kFar ? 1.0f : exp2f(ref - z);
                                 }
-                                warp_columns<kCols>(x,
-                                                    [](float u, float v) { return fmaxf(u, v); });
-                                const float m = x[0] == neg_inf_f()    ? kFar
-                                                : fabsf(x[0]) < 1e30f ? x[0]
-                                                                      : 0.0f;
-                                if (pass == 0)
-                                    ref = m;
-                                else
-                                    z = m;
-                            }
-                            if (alike && big > 0.0f)
-                                z = ref + log2f(big);
-                            if (lane < kCols) {
-                                const int n = col0 + lane;
-                                z = fmaxf(z, ref - kMaxShift);
-                                nref[n] = -ref;
-                                refz[n] = z;
-                                cmul[n] = ref == kFar ? 1.0f : exp2f(ref - z);
                             }
                         }
                         sync();
@@ -901,7 +861,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     auto weights = [&](auto again) -> float {
                         constexpr bool kAgain = decltype(again)::value;
                         const uint32_t nr_at = valid ? cols_at + 4 * kNref : cols_at + 4 * kNone;
-                        const uint32_t sq_at = cols_at + 4 * (kSumq + sb * N);
+                        [[maybe_unused]] const uint32_t sq_at = cols_at + 4 * (kSumq + sb * N);
                         const uint64_t ks2 = f2(ks, ks), ko2 = f2(ko, ko);
                         const uint64_t vw2 = f2(vw, vw), vo2 = f2(vo, vo);
                         float top = 0.0f;
@@ -976,15 +936,6 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                                 pl[i] = 0;
                         }
                     }
-#ifdef F_MVOTE
-                    over = __any_sync(0xFFFFFFFFu, over);
-                    if (over) {
-                        if (lane == 0)
-                            *reinterpret_cast<volatile uint32_t *>(&vote[seen & 1]) = seen + 1;
-                        __syncwarp();
-                    }
-                    mbar_arrive_if(bar(kVoted), lane == 0);
-#endif
                     // the sums of the tile before must have read its weights
                     if (seen > summed) {
                         wait(kODone + (summed & 1), (summed >> 1) & 1);
@@ -993,33 +944,25 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     }
                     if (kOwn && t == from && from > begin)
                         scale_sums<kCols>(lanes + S::tO + col0, nullptr, kSumUnit);
-#ifdef F_MVOTE
-                    wait(kVoted, seen & 1);
-                    if (*reinterpret_cast<volatile uint32_t *>(&vote[seen & 1]) == seen + 1) {
-#else
                     if (named_sync_or(kBarW, S::w_threads, over)) {
-#endif
                         // ---- the references move: per row, the running maxima of the scores
                         // and of the scores with the values' scale
                         const float lv = vs > 0.0f ? log2f(vs) : neg_inf_f();
 #pragma unroll 1
-                        for (int z = 0; z < 2; ++z) {
-                            float m[kCols];
+                        for (int i = 0; i < kCols / 4; ++i) {  // eight columns, z = i & 1
+                            const int c8 = i / 2 * 8, z = i & 1;
+                            float m[8];
+                            uint32_t s[8];
+                            tmem_ld<8>(tS + c8, s);
 #pragma unroll
-                            for (int c8 = 0; c8 < kCols; c8 += 8) {
-                                uint32_t s[8];
-                                tmem_ld<8>(tS + c8, s);
-#pragma unroll
-                                for (int c = 0; c < 8; ++c) {
-                                    const float x = fmaf(__uint_as_float(s[c]), ks,
-                                                         ko * rowf[kSumq + sb * N + col0 + c8 + c]);
-                                    m[c8 + c] = c8 + c >= first_col ? x + (z ? lv : 0.0f)
-                                                                    : neg_inf_f();
-                                }
+                            for (int c = 0; c < 8; ++c) {
+                                const float x = fmaf(__uint_as_float(s[c]), ks,
+                                                     ko * rowf[kSumq + sb * N + col0 + c8 + c]);
+                                m[c] = c8 + c >= first_col ? x + (z ? lv : 0.0f) : neg_inf_f();
                             }
-                            warp_columns<kCols>(m, [](float x, float y) { return fmaxf(x, y); });
-                            if (lane < kCols)
-                                wred[ww][z][lane] = m[0];
+                            warp_columns<8>(m, [](float x, float y) { return fmaxf(x, y); });
+                            if (lane < 8)
+                                wred[ww][z][c8 + lane] = m[0];
                         }
                         sync();
                         if (wt < N) {
@@ -1078,12 +1021,8 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     }
                     fence_async_smem();
                     tc::fence_before_sync();
-#ifdef F_MREADY
                     __syncwarp();
-                    mbar_arrive_if(bar(kPR), lane == 0);
-#else
-                    named_arrive(kBarPReady, S::w_threads + 32);
-#endif
+                    mbar_arrive_if(bar(kPReady), lane == 0);
                     if (!kOwn)
                         mbar_arrive_if(bar(kEmpty + st), lane == 0);
                     ++seen;
@@ -1285,25 +1224,6 @@ __global__ void __launch_bounds__(32 * kJoinWarps)
 
 // Rows of a row tile: the smallest width that holds a head's rows, 64 beyond that.
 int tile_rows(int64_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
-
-int sm_count()
-{
-    static int cached[64] = {0};
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
-        cudaGetLastError();
-        return 152;
-    }
-    if (cached[dev] == 0) {
-        int n = 0;
-        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) {
-            cudaGetLastError();
-            return 152;
-        }
-        cached[dev] = n;
-    }
-    return cached[dev];
-}
 
 struct Workspace {
     size_t meta, refs, parts, total;

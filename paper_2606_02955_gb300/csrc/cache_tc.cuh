@@ -125,6 +125,28 @@ __device__ __forceinline__ uint4 interleave8(const uint4 x)
                       __byte_perm(x.y, x.w, 0x5410), __byte_perm(x.y, x.w, 0x7632));
 }
 
+// Queries against codes: fp16, times a power of two 2^-e that brings the largest of them to 2^13
+// (0: 1), and 2^-4 in odd channels.  e from the largest; clamped so that 2^e and 2^-e exist.
+__device__ __forceinline__ int query_exponent(float big)
+{
+    const int e = big > 0.0f ? (int)(__float_as_uint(big) >> 23) - 127 - 13 : 0;
+    return min(max(e, -100), 100);
+}
+
+// Eight channels of a query, in the operand's order; unit = 2^-e.
+template <typename T>
+__device__ __forceinline__ uint4 code_queries(const uint4 x, float unit)
+{
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        unpack2<T>(w[i], f[2 * i], f[2 * i + 1]);
+    const float odd = unit * 0.0625f;
+    return make_uint4(pack2<__half>(f[0] * unit, f[4] * unit), pack2<__half>(f[1] * odd, f[5] * odd),
+                      pack2<__half>(f[2] * unit, f[6] * unit), pack2<__half>(f[3] * odd, f[7] * odd));
+}
+
 // ---------------------------------------------------------------- tensor memory
 // Columns of this warp's 32 lanes, one 32-bit word a column.
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16])
@@ -249,15 +271,6 @@ __device__ __forceinline__ void fence_async_smem()
 // reading alone costs about as much as a tile, is looked at only after many tries.  kSleepNs: a
 // warp that waits most of its time sleeps between tries, which would take issue slots from the
 // warps that work.
-#ifndef W_DELAY
-#define W_DELAY 1
-#endif
-__device__ __forceinline__ void clock_delay()
-{
-    uint32_t c;
-    asm volatile("mov.u32 %0, %%clock;" : "=r"(c));
-}
-
 __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
 {
     uint32_t done;
@@ -271,14 +284,9 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
     return done != 0;
 }
 
-#ifdef F_NOINLINE
-#define F_INL __noinline__
-#else
-#define F_INL __forceinline__
-#endif
 template <int kSleepNs>
-__device__ F_INL bool mbar_wait_long(uint32_t bar, uint32_t parity, uint32_t *status,
-                                            uint64_t limit_ns)
+__device__ __forceinline__ bool mbar_wait_at(uint32_t bar, uint32_t parity, uint32_t *status,
+                                             uint64_t limit_ns = kWaitLimitNs)
 {
     uint64_t t0 = 0;
 #pragma unroll 1
@@ -297,17 +305,6 @@ __device__ F_INL bool mbar_wait_long(uint32_t bar, uint32_t parity, uint32_t *st
             }
         }
     }
-}
-
-template <int kSleepNs>
-__device__ __forceinline__ bool mbar_wait_at(uint32_t bar, uint32_t parity, uint32_t *status,
-                                             uint64_t limit_ns = kWaitLimitNs)
-{
-#ifdef F_FIRST
-    if (mbar_try(bar, parity))
-        return true;
-#endif
-    return mbar_wait_long<kSleepNs>(bar, parity, status, limit_ns);
 }
 
 // An arrival by the lanes where `who` holds (a predicate, not a branch).
