@@ -512,6 +512,12 @@ fdllm_status fdllm_cache_evict(const fdllm_cache *cache, const int32_t *block_ta
                                const int32_t *dst_table, int dst_max_pages, int32_t *out_lens,
                                float *out_weights, int32_t *out_index, void *stream);
 
+/* The sticky device error of fdllm_cache_attention and fdllm_cache_key_weights on the current
+ * device: synchronises `stream`, returns FDLLM_ERR_DEVICE if one of their kernels gave up a
+ * bounded wait since the last call (the results of the calls since then are unusable), FDLLM_OK
+ * otherwise, and clears it. */
+fdllm_status fdllm_cache_status(void *stream);
+
 /* Health check of the library's failure detection: every wait inside the kernels is
  * bounded, and a wait that runs out records a device error and lets the kernel return
  * instead of hanging.  This launches one thread that waits on a barrier nobody completes,

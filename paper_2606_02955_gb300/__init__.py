@@ -29,7 +29,7 @@ __all__ = [
     "fdllm_select_host",
     "KvCache", "fdllm_qk_norm_rope", "fdllm_cache_append", "fdllm_cache_read",
     "fdllm_cache_attention", "fdllm_cache_attention_workspace_bytes",
-    "fdllm_cache_key_weights", "fdllm_cache_evict",
+    "fdllm_cache_key_weights", "fdllm_cache_evict", "fdllm_cache_status",
 ]
 
 BF16, FP32, FP16 = 0, 1, 2
@@ -104,6 +104,8 @@ def _load():
     lib.fdllm_cache_key_weights.restype = i
     lib.fdllm_cache_evict.argtypes = [p, p, i, i, p, p, i, i, i, i, p, i, p, p, p, p]
     lib.fdllm_cache_evict.restype = i
+    lib.fdllm_cache_status.argtypes = [p]
+    lib.fdllm_cache_status.restype = i
     lib.fdllm_check_bounded_wait.argtypes = [d, p]
     lib.fdllm_check_bounded_wait.restype = i
     lib.fdllm_device_status.argtypes = [p]
@@ -551,6 +553,70 @@ class _CacheStruct(ctypes.Structure):
                 ("head_dim", ctypes.c_int)]
 
 
+_Two, _Three, _Four = ctypes.c_int64 * 2, ctypes.c_int64 * 3, ctypes.c_int * 4
+_current_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+_I32, _F32, _U8, _BF16, _F16 = (torch.int32, torch.float32, torch.uint8, torch.bfloat16,
+                                torch.float16)
+_CODES = {_BF16: BF16, _F32: FP32, _F16: FP16}
+
+
+# A decode step makes these calls once a layer and step, on short blocks in a few microseconds of
+# GPU time: the checks below look at each tensor once, and look up why only when one fails.
+
+def _ptr(t, name, dtype, shape, dev):
+    """Pointer of a contiguous tensor of this dtype, shape and device (None: a null pointer)."""
+    if t is None:
+        return None
+    if t.dtype is dtype and t.shape == shape and t.device == dev and t.is_contiguous():
+        return t.data_ptr()
+    _dev(t, name, dtype, shape)
+    raise ValueError("the CUDA tensors of one call must share a device (%s, %s)" % (dev, t.device))
+
+
+def _rows(t, name, dtype, shape, dev, kind):
+    """(pointer, leading strides) of a tensor whose last axis is contiguous."""
+    if t.dtype is not dtype:
+        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    if t.shape != shape:
+        raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    if t.device != dev or not t.is_cuda:
+        raise ValueError("%s must be a CUDA tensor on %s" % (name, dev))
+    st = t.stride()
+    if st[-1] != 1:
+        raise ValueError("the channels of %s must be contiguous" % name)
+    if 1 in shape:  # the stride of an axis of one is never taken
+        st = [x if n > 1 else 0 for x, n in zip(st, shape)]
+    return t.data_ptr(), kind(*st[:-1])
+
+
+def _made(shape, dtype, dev, stream):
+    """A tensor for the call's result.  Where the call runs on another stream than the current
+    one, the allocator is told, and that stream waits for what may still use the memory."""
+    t = torch.empty(shape, dtype=dtype, device=dev)
+    if stream is not None and _stream(stream) != _raw_stream(dev.index):
+        other = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))
+        other.wait_stream(torch.cuda.current_stream())
+        t.record_stream(other)
+    return t
+
+
+def _called_on(which):
+    """Runs a call on the device of its argument number `which`."""
+    def wrap(fn):
+        @functools.wraps(fn)
+        def call(*args, **kwargs):
+            t = args[which] if len(args) > which else kwargs[names[which]]
+            if not isinstance(t, torch.Tensor) or not t.is_cuda:
+                raise ValueError("%s must be a CUDA tensor" % names[which])
+            if t.device.index == _current_device():
+                return fn(*args, **kwargs)
+            with torch.cuda.device(t.device):
+                return fn(*args, **kwargs)
+        names = fn.__code__.co_varnames[:fn.__code__.co_argcount]
+        return call
+    return wrap
+
+
 class KvCache:
     """The 4-bit prefix cache of one layer (fdllm_cache): four CUDA tensors and their sizes.
 
@@ -562,108 +628,42 @@ class KvCache:
                  "head_dim", "device", "_struct", "_ref")
 
     def __init__(self, k_codes, v_codes, k_affine, v_affine):
-        if k_codes.dim() != 4:
-            raise ValueError("k_codes must be [pages, heads, page_size, D/2]")
-        pages, heads, page, half = k_codes.shape
-        _dev(k_codes, "k_codes", torch.uint8)
-        _dev(v_codes, "v_codes", torch.uint8, (pages, heads, 2 * half, page // 2))
-        _dev(k_affine, "k_affine", torch.bfloat16, (pages, heads, page, 2))
-        _dev(v_affine, "v_affine", torch.bfloat16, (pages, heads, page, 2))
-        self.device = k_codes.device
-        for t in (v_codes, k_affine, v_affine):
-            if t.device != self.device:
-                raise ValueError("the cache's tensors must share a device")
+        if k_codes.dim() != 4 or not k_codes.is_cuda:
+            raise ValueError("k_codes must be a CUDA tensor [pages, heads, page_size, D/2]")
+        pages, heads, page, half = shape = k_codes.shape
+        dev = k_codes.device
+        affine = (pages, heads, page, 2)
+        self._struct = _CacheStruct(
+            _ptr(k_codes, "k_codes", _U8, shape, dev),
+            _ptr(v_codes, "v_codes", _U8, (pages, heads, 2 * half, page // 2), dev),
+            _ptr(k_affine, "k_affine", _BF16, affine, dev),
+            _ptr(v_affine, "v_affine", _BF16, affine, dev), pages, heads, page, 2 * half)
+        self._ref = ctypes.addressof(self._struct)
+        self.device = dev
         self.k_codes, self.v_codes = k_codes, v_codes
         self.k_affine, self.v_affine = k_affine, v_affine
         self.pages, self.heads, self.page_size, self.head_dim = pages, heads, page, 2 * half
-        self._struct = _CacheStruct(k_codes.data_ptr(), v_codes.data_ptr(), k_affine.data_ptr(),
-                                    v_affine.data_ptr(), pages, heads, page, 2 * half)
-        self._ref = ctypes.addressof(self._struct)
 
     @classmethod
     def empty(cls, pages: int, heads: int, page_size: int, head_dim: int, device="cuda"):
         affine = (pages, heads, page_size, 2)
-        return cls(torch.empty((pages, heads, page_size, head_dim // 2), dtype=torch.uint8,
-                               device=device),
-                   torch.empty((pages, heads, head_dim, page_size // 2), dtype=torch.uint8,
-                               device=device),
-                   torch.empty(affine, dtype=torch.bfloat16, device=device),
-                   torch.empty(affine, dtype=torch.bfloat16, device=device))
+        return cls(torch.empty((pages, heads, page_size, head_dim // 2), dtype=_U8, device=device),
+                   torch.empty((pages, heads, head_dim, page_size // 2), dtype=_U8, device=device),
+                   torch.empty(affine, dtype=_BF16, device=device),
+                   torch.empty(affine, dtype=_BF16, device=device))
 
 
-_Two, _Three, _Four = ctypes.c_int64 * 2, ctypes.c_int64 * 3, ctypes.c_int * 4
+def _table(table, cache, dev, name="block_table", rows=None):
+    if table.dim() != 2 or (rows is not None and table.shape[0] != rows):
+        raise ValueError("%s must be [%s, max_pages], got %s"
+                         % (name, "B" if rows is None else rows, tuple(table.shape)))
+    if cache.device != dev:
+        raise ValueError("the cache must be on %s" % dev)
+    B, pages = shape = table.shape
+    return _ptr(table, name, _I32, shape, dev), B, pages
 
 
-class _Call:
-    """The device and stream of one call on the cache's operators: makes the device of the
-    arguments current where it is not, checks that they share it, and tells the allocator when
-    a tensor made for the call is used on another stream than the current one."""
-
-    __slots__ = ("device", "stream", "_other", "_back")
-
-    def __init__(self, device, stream):
-        self.device = device
-        self._back = None
-        if device.index != torch.cuda.current_device():
-            self._back = torch.cuda.current_device()
-            torch.cuda.set_device(device)
-        current = torch.cuda.current_stream().cuda_stream
-        self._other = None
-        if stream is None:
-            self.stream = current
-        else:
-            self.stream = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
-            if self.stream != current:
-                self._other = (stream if hasattr(stream, "cuda_stream")
-                               else torch.cuda.ExternalStream(self.stream))
-
-    def __enter__(self):
-        return self
-
-    def __exit__(self, *exc):
-        if self._back is not None:
-            torch.cuda.set_device(self._back)
-
-    def ptr(self, t, name, dtype=None, shape=None):
-        """A contiguous CUDA tensor of the call's device (None: a null pointer)."""
-        if t is None:
-            return None
-        p = _dev(t, name, dtype, shape)
-        if t.device != self.device:
-            raise ValueError("the CUDA tensors of one call must share a device (%s, %s)"
-                             % (self.device, t.device))
-        return p
-
-    def rows(self, t, name, dtype, shape, kind):
-        """A CUDA tensor whose last axis is contiguous: (pointer, leading strides)."""
-        if not t.is_cuda or t.device != self.device:
-            raise ValueError("%s must be a CUDA tensor on %s" % (name, self.device))
-        if t.dtype != dtype:
-            raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
-        if tuple(t.shape) != tuple(shape):
-            raise ValueError("%s must have shape %s, got %s"
-                             % (name, tuple(shape), tuple(t.shape)))
-        st = t.stride()
-        if st[-1] != 1:
-            raise ValueError("the channels of %s must be contiguous" % name)
-        # the stride of an axis of one is never taken
-        return t.data_ptr(), kind(*[x if m > 1 else 0 for x, m in zip(st, t.shape[:-1])])
-
-    def made(self, shape, dtype):
-        t = torch.empty(shape, dtype=dtype, device=self.device)
-        if self._other is not None:
-            # The memory may still be in use by work queued on the current stream.
-            self._other.wait_stream(torch.cuda.current_stream())
-            t.record_stream(self._other)
-        return t
-
-
-def _cuda_device(t, name):
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise ValueError("%s must be a CUDA tensor" % name)
-    return t.device
-
-
+@_called_on(0)
 def fdllm_qk_norm_rope(q: torch.Tensor, k: torch.Tensor | None, positions: torch.Tensor,
                        inv_freq: torch.Tensor, q_weight=None, k_weight=None, eps: float = 1e-6,
                        sections=None, interleaved: bool = False, out_q=None, out_k=None,
@@ -676,79 +676,76 @@ def fdllm_qk_norm_rope(q: torch.Tensor, k: torch.Tensor | None, positions: torch
     ``sections`` the pairs of each axis; a weight of None skips that tensor's norm.
     ``out_q`` / ``out_k`` may be q / k themselves where those are contiguous.  Returns
     (out_q, out_k)."""
-    with _Call(_cuda_device(q, "q"), stream) as c:
-        if q.dim() != 3:
-            raise ValueError("q must be [T, Hq, D]")
-        T, Hq, D = q.shape
-        qp, qs = c.rows(q, "q", q.dtype, (T, Hq, D), _Two)
-        Hk, kp, ks = 0, None, None
-        if k is not None:
-            Hk = k.shape[1] if k.dim() == 3 else -1
-            kp, ks = c.rows(k, "k", q.dtype, (T, Hk, D), _Two)
-        axes = 1 if positions.dim() == 1 else positions.shape[0]
-        pp = c.ptr(positions, "positions", torch.int32, (T,) if positions.dim() == 1 else (axes, T))
-        if inv_freq.is_cuda or inv_freq.dtype != torch.float64 or not inv_freq.is_contiguous():
-            raise ValueError("inv_freq must be a contiguous CPU float64 tensor")
-        if sections is not None and (len(sections) != axes or axes > 4):
-            raise ValueError("sections must name the pairs of each of %d axes (at most 4)" % axes)
-        if out_q is None:
-            out_q = c.made((T, Hq, D), q.dtype)
-        if out_k is None and k is not None:
-            out_k = c.made((T, Hk, D), q.dtype)
-        st = _load().fdllm_qk_norm_rope(
-            qp, qs, kp, ks, _dtype_code(q), T, Hq, Hk, D,
-            c.ptr(q_weight, "q_weight", q.dtype, (D,)), c.ptr(k_weight, "k_weight", q.dtype, (D,)),
-            eps, pp, axes, None if sections is None else _Four(*sections), inv_freq.data_ptr(),
-            inv_freq.numel(), 1 if interleaved else 0, c.ptr(out_q, "out_q", q.dtype, (T, Hq, D)),
-            None if k is None else c.ptr(out_k, "out_k", q.dtype, (T, Hk, D)), c.stream)
+    dev, dt = q.device, q.dtype
+    if q.dim() != 3:
+        raise ValueError("q must be [T, Hq, D]")
+    T, Hq, D = shape = q.shape
+    qp, qs = _rows(q, "q", dt, shape, dev, _Two)
+    Hk, kp, ks = 0, None, None
+    if k is not None:
+        Hk = k.shape[1] if k.dim() == 3 else -1
+        kp, ks = _rows(k, "k", dt, (T, Hk, D), dev, _Two)
+    axes = 1 if positions.dim() == 1 else positions.shape[0]
+    pp = _ptr(positions, "positions", _I32, (T,) if positions.dim() == 1 else (axes, T), dev)
+    if inv_freq.is_cuda or inv_freq.dtype is not torch.float64 or not inv_freq.is_contiguous():
+        raise ValueError("inv_freq must be a contiguous CPU float64 tensor")
+    if sections is not None and (len(sections) != axes or axes > 4):
+        raise ValueError("sections must name the pairs of each of %d axes (at most 4)" % axes)
+    if out_q is None:
+        out_q = _made(shape, dt, dev, stream)
+    if k is not None and out_k is None:
+        out_k = _made((T, Hk, D), dt, dev, stream)
+    st = _load().fdllm_qk_norm_rope(
+        qp, qs, kp, ks, _dtype_code(q), T, Hq, Hk, D, _ptr(q_weight, "q_weight", dt, (D,), dev),
+        _ptr(k_weight, "k_weight", dt, (D,), dev), eps, pp, axes,
+        None if sections is None else _Four(*sections), inv_freq.data_ptr(), inv_freq.numel(),
+        1 if interleaved else 0, _ptr(out_q, "out_q", dt, shape, dev),
+        None if k is None else _ptr(out_k, "out_k", dt, (T, Hk, D), dev),
+        _raw_stream(dev.index) if stream is None else _stream(stream))
+    if st:
         _check(st, "fdllm_qk_norm_rope")
-        return out_q, out_k
+    return out_q, out_k
 
 
-def _table(c, cache, table, name="block_table"):
-    if table.dim() != 2:
-        raise ValueError("%s must be [B, max_pages]" % name)
-    if cache.device != c.device:
-        raise ValueError("the cache must be on %s" % c.device)
-    return c.ptr(table, name, torch.int32), table.shape[0], table.shape[1]
-
-
+@_called_on(3)
 def fdllm_cache_append(cache: KvCache, block_table: torch.Tensor, start, k: torch.Tensor,
                        v: torch.Tensor, count=None, stream=None):
     """Write k, v [B, n, heads, D] (bf16/fp16/fp32, channels contiguous) into slots
     start[b] .. start[b] + count[b] - 1 (int32 [B] each; None: 0 and n)."""
-    with _Call(_cuda_device(k, "k"), stream) as c:
-        tp, B, mp = _table(c, cache, block_table)
-        n = k.shape[1] if k.dim() == 4 else -1
-        shape = (B, n, cache.heads, cache.head_dim)
-        kp, ks = c.rows(k, "k", k.dtype, shape, _Three)
-        vp, vs = c.rows(v, "v", k.dtype, shape, _Three)
-        st = _load().fdllm_cache_append(cache._ref, tp, B, mp,
-                                        c.ptr(start, "start", torch.int32, (B,)),
-                                        c.ptr(count, "count", torch.int32, (B,)), kp, ks, vp, vs,
-                                        _dtype_code(k), n, c.stream)
+    dev, dt = k.device, k.dtype
+    tp, B, mp = _table(block_table, cache, dev)
+    n = k.shape[1] if k.dim() == 4 else -1
+    shape = (B, n, cache.heads, cache.head_dim)
+    kp, ks = _rows(k, "k", dt, shape, dev, _Three)
+    vp, vs = _rows(v, "v", dt, shape, dev, _Three)
+    st = _load().fdllm_cache_append(
+        cache._ref, tp, B, mp, _ptr(start, "start", _I32, (B,), dev),
+        _ptr(count, "count", _I32, (B,), dev), kp, ks, vp, vs, _dtype_code(k), n,
+        _raw_stream(dev.index) if stream is None else _stream(stream))
+    if st:
         _check(st, "fdllm_cache_append")
 
 
+@_called_on(1)
 def fdllm_cache_read(cache: KvCache, block_table: torch.Tensor, start, n: int,
                      dtype=torch.bfloat16, count=None, out_k=None, out_v=None, stream=None):
     """Slots start[b] .. start[b] + n - 1 as dense rows (out_k, out_v) [B, n, heads, D] of
     ``dtype``; rows from count[b] on are zero."""
-    with _Call(_cuda_device(block_table, "block_table"), stream) as c:
-        tp, B, mp = _table(c, cache, block_table)
-        shape = (B, n, cache.heads, cache.head_dim)
-        if out_k is None:
-            out_k = c.made(shape, dtype)
-        if out_v is None:
-            out_v = c.made(shape, dtype)
-        st = _load().fdllm_cache_read(cache._ref, tp, B, mp,
-                                      c.ptr(start, "start", torch.int32, (B,)),
-                                      c.ptr(count, "count", torch.int32, (B,)),
-                                      c.ptr(out_k, "out_k", dtype, shape),
-                                      c.ptr(out_v, "out_v", dtype, shape), _dtype_code(out_k), n,
-                                      c.stream)
+    dev = block_table.device
+    tp, B, mp = _table(block_table, cache, dev)
+    shape = (B, n, cache.heads, cache.head_dim)
+    if out_k is None:
+        out_k = _made(shape, dtype, dev, stream)
+    if out_v is None:
+        out_v = _made(shape, dtype, dev, stream)
+    st = _load().fdllm_cache_read(
+        cache._ref, tp, B, mp, _ptr(start, "start", _I32, (B,), dev),
+        _ptr(count, "count", _I32, (B,), dev), _ptr(out_k, "out_k", dtype, shape, dev),
+        _ptr(out_v, "out_v", dtype, shape, dev), _dtype_code(out_k), n,
+        _raw_stream(dev.index) if stream is None else _stream(stream))
+    if st:
         _check(st, "fdllm_cache_read")
-        return out_k, out_v
+    return out_k, out_v
 
 
 def fdllm_cache_attention_workspace_bytes(B: int, Lq: int, Hq: int, heads: int,
@@ -756,59 +753,78 @@ def fdllm_cache_attention_workspace_bytes(B: int, Lq: int, Hq: int, heads: int,
     return int(_load().fdllm_cache_attention_workspace_bytes(B, Lq, Hq, heads, head_dim))
 
 
-def _queries(c, q, cache):
+# Attention's workspaces, one to a device and stream, grown on demand: calls on one stream are
+# ordered, so they can share it.  A call under stream capture gets memory of its own (the graph
+# may be replayed on any stream).
+_workspaces = {}
+
+
+def _workspace(need, dev, stream):
+    if torch.cuda.is_current_stream_capturing():
+        return _made((need,), _U8, dev, stream)
+    key = (dev.index, _raw_stream(dev.index) if stream is None else _stream(stream))
+    t = _workspaces.get(key)
+    if t is None or t.numel() < need:
+        t = _workspaces[key] = _made((need,), _U8, dev, stream)
+    return t
+
+
+def _queries(q, cache, dev):
     if q.dim() != 4:
         raise ValueError("q must be [B, Lq, Hq, D]")
-    if q.dtype not in (torch.bfloat16, torch.float16):
+    if q.dtype is not _BF16 and q.dtype is not _F16:
         raise TypeError("q must be bfloat16 or float16, got %s" % q.dtype)
-    B, Lq, Hq, D = q.shape
-    qp, qs = c.rows(q, "q", q.dtype, (B, Lq, Hq, cache.head_dim), _Three)
+    B, Lq, Hq, D = shape = q.shape
+    if D != cache.head_dim:
+        raise ValueError("q must be [B, Lq, Hq, %d], got %s" % (cache.head_dim, tuple(shape)))
+    qp, qs = _rows(q, "q", q.dtype, shape, dev, _Three)
     return qp, qs, B, Lq, Hq
 
 
+@_called_on(0)
 def fdllm_cache_attention(q: torch.Tensor, cache: KvCache, block_table: torch.Tensor,
                           cache_lens: torch.Tensor, k_new=None, v_new=None, new_lens=None,
                           causal: bool = False, scale: float | None = None, out=None,
                           return_lse: bool = False, out_lse=None, workspace=None, stream=None):
     """Attention of ``q`` [B, Lq, Hq, D] (bf16/fp16) over the first cache_lens[b] slots of the
     cache and the block's own ``k_new``, ``v_new`` [B, Ln, heads, D].  ``scale`` None: D^-0.5.
-    ``workspace`` a uint8 CUDA tensor of fdllm_cache_attention_workspace_bytes bytes (None:
-    allocated for the call; pass one under stream capture by another library).  Returns out, or
-    (out, lse fp32 [B, Lq, Hq]) with ``return_lse``."""
-    with _Call(_cuda_device(q, "q"), stream) as c:
-        tp, tb, mp = _table(c, cache, block_table)
-        qp, qs, B, Lq, Hq = _queries(c, q, cache)
-        if tb != B:
-            raise ValueError("block_table must have %d rows, got %d" % (B, tb))
-        Ln, kp, ks, vp, vs = 0, None, None, None, None
-        if (k_new is None) != (v_new is None):
-            raise ValueError("k_new and v_new go together")
-        if k_new is not None:
-            Ln = k_new.shape[1] if k_new.dim() == 4 else -1
-            shape = (B, Ln, cache.heads, cache.head_dim)
-            kp, ks = c.rows(k_new, "k_new", q.dtype, shape, _Three)
-            vp, vs = c.rows(v_new, "v_new", q.dtype, shape, _Three)
-        if out is None:
-            out = c.made((B, Lq, Hq, cache.head_dim), q.dtype)
-        if out_lse is None and return_lse:
-            out_lse = c.made((B, Lq, Hq), torch.float32)
-        lib = _load()
-        if workspace is None:
-            need = lib.fdllm_cache_attention_workspace_bytes(B, Lq, Hq, cache.heads,
-                                                             cache.head_dim)
-            workspace = c.made((max(need, 256),), torch.uint8)
-        st = lib.fdllm_cache_attention(
-            qp, qs, _dtype_code(q), B, Lq, Hq, cache._ref, tp, mp,
-            c.ptr(cache_lens, "cache_lens", torch.int32, (B,)), kp, ks, vp, vs, Ln,
-            c.ptr(new_lens, "new_lens", torch.int32, (B,)), 1 if causal else 0,
-            cache.head_dim ** -0.5 if scale is None else scale,
-            c.ptr(out, "out", q.dtype, (B, Lq, Hq, cache.head_dim)),
-            c.ptr(out_lse, "out_lse", torch.float32, (B, Lq, Hq)),
-            c.ptr(workspace, "workspace", torch.uint8), workspace.numel(), c.stream)
+    ``workspace`` a uint8 CUDA tensor of fdllm_cache_attention_workspace_bytes bytes (None: one
+    the binding keeps for the stream; pass one where another library captures the call).
+    Returns out, or (out, lse fp32 [B, Lq, Hq]) with ``return_lse``."""
+    dev, dt = q.device, q.dtype
+    qp, qs, B, Lq, Hq = _queries(q, cache, dev)
+    heads, D = cache.heads, cache.head_dim
+    tp, _, mp = _table(block_table, cache, dev, rows=B)
+    Ln, kp, ks, vp, vs = 0, None, None, None, None
+    if (k_new is None) != (v_new is None):
+        raise ValueError("k_new and v_new go together")
+    if k_new is not None:
+        Ln = k_new.shape[1] if k_new.dim() == 4 else -1
+        own = (B, Ln, heads, D)
+        kp, ks = _rows(k_new, "k_new", dt, own, dev, _Three)
+        vp, vs = _rows(v_new, "v_new", dt, own, dev, _Three)
+    if out is None:
+        out = _made(q.shape, dt, dev, stream)
+    if out_lse is None and return_lse:
+        out_lse = _made((B, Lq, Hq), _F32, dev, stream)
+    lib = _load()
+    if workspace is None:
+        need = lib.fdllm_cache_attention_workspace_bytes(B, Lq, Hq, heads, D)
+        workspace = _workspace(need if need > 256 else 256, dev, stream)
+    st = lib.fdllm_cache_attention(
+        qp, qs, _CODES[dt], B, Lq, Hq, cache._ref, tp, mp,
+        _ptr(cache_lens, "cache_lens", _I32, (B,), dev), kp, ks, vp, vs, Ln,
+        _ptr(new_lens, "new_lens", _I32, (B,), dev), 1 if causal else 0,
+        D ** -0.5 if scale is None else scale, _ptr(out, "out", dt, q.shape, dev),
+        _ptr(out_lse, "out_lse", _F32, (B, Lq, Hq), dev),
+        _ptr(workspace, "workspace", _U8, workspace.shape, dev), workspace.numel(),
+        _raw_stream(dev.index) if stream is None else _stream(stream))
+    if st:
         _check(st, "fdllm_cache_attention")
-        return (out, out_lse) if return_lse else out
+    return (out, out_lse) if return_lse else out
 
 
+@_called_on(0)
 def fdllm_cache_key_weights(q: torch.Tensor, lse: torch.Tensor, cache: KvCache,
                             block_table: torch.Tensor, cache_lens: torch.Tensor, weights=None,
                             scale: float | None = None, max_len: int | None = None, out=None,
@@ -816,29 +832,28 @@ def fdllm_cache_key_weights(q: torch.Tensor, lse: torch.Tensor, cache: KvCache,
     """The attention each cached key receives from ``q`` given attention's ``lse`` [B, Lq, Hq],
     added to ``weights`` fp32 [B, heads, max_len] (None: from zero, ``max_len`` slots or the
     table's).  ``out`` may be ``weights``.  Returns the sums (0 behind cache_lens)."""
-    with _Call(_cuda_device(q, "q"), stream) as c:
-        tp, tb, mp = _table(c, cache, block_table)
-        qp, qs, B, Lq, Hq = _queries(c, q, cache)
-        if tb != B:
-            raise ValueError("block_table must have %d rows, got %d" % (B, tb))
-        if weights is not None:
-            max_len = weights.shape[-1]
-        elif max_len is None:
-            max_len = mp * cache.page_size
-        shape = (B, cache.heads, max_len)
-        if out is None:
-            out = c.made(shape, torch.float32)
-        st = _load().fdllm_cache_key_weights(
-            qp, qs, _dtype_code(q), B, Lq, Hq, cache._ref, tp, mp,
-            c.ptr(cache_lens, "cache_lens", torch.int32, (B,)),
-            c.ptr(lse, "lse", torch.float32, (B, Lq, Hq)),
-            cache.head_dim ** -0.5 if scale is None else scale,
-            c.ptr(weights, "weights", torch.float32, shape),
-            c.ptr(out, "out", torch.float32, shape), max_len, c.stream)
+    dev = q.device
+    qp, qs, B, Lq, Hq = _queries(q, cache, dev)
+    tp, _, mp = _table(block_table, cache, dev, rows=B)
+    if weights is not None:
+        max_len = weights.shape[-1]
+    elif max_len is None:
+        max_len = mp * cache.page_size
+    shape = (B, cache.heads, max_len)
+    if out is None:
+        out = _made(shape, _F32, dev, stream)
+    st = _load().fdllm_cache_key_weights(
+        qp, qs, _CODES[q.dtype], B, Lq, Hq, cache._ref, tp, mp,
+        _ptr(cache_lens, "cache_lens", _I32, (B,), dev), _ptr(lse, "lse", _F32, (B, Lq, Hq), dev),
+        cache.head_dim ** -0.5 if scale is None else scale,
+        _ptr(weights, "weights", _F32, shape, dev), _ptr(out, "out", _F32, shape, dev), max_len,
+        _raw_stream(dev.index) if stream is None else _stream(stream))
+    if st:
         _check(st, "fdllm_cache_key_weights")
-        return out
+    return out
 
 
+@_called_on(3)
 def fdllm_cache_evict(cache: KvCache, block_table: torch.Tensor, cache_lens: torch.Tensor,
                       weights: torch.Tensor, budget: int, dst_table: torch.Tensor,
                       keep_first: int = 0, keep_last: int = 0, out_lens=None, out_weights=None,
@@ -847,27 +862,33 @@ def fdllm_cache_evict(cache: KvCache, block_table: torch.Tensor, cache_lens: tor
     the last ``keep_last`` slots always) into the pages of ``dst_table`` [B, dst_max_pages],
     in slot order.  Returns (lens int32 [B], weights fp32 [B, heads, budget], the slots they
     came from int32 [B, heads, budget])."""
-    with _Call(_cuda_device(weights, "weights"), stream) as c:
-        tp, B, mp = _table(c, cache, block_table)
-        dp, db, dmp = _table(c, cache, dst_table, "dst_table")
-        if db != B:
-            raise ValueError("dst_table must have %d rows, got %d" % (B, db))
-        max_len = weights.shape[-1]
-        shape = (B, cache.heads, budget)
-        if out_lens is None:
-            out_lens = c.made((B,), torch.int32)
-        if out_weights is None:
-            out_weights = c.made(shape, torch.float32)
-        if out_index is None:
-            out_index = c.made(shape, torch.int32)
-        st = _load().fdllm_cache_evict(
-            cache._ref, tp, B, mp, c.ptr(cache_lens, "cache_lens", torch.int32, (B,)),
-            c.ptr(weights, "weights", torch.float32, (B, cache.heads, max_len)), max_len, budget,
-            keep_first, keep_last, dp, dmp, c.ptr(out_lens, "out_lens", torch.int32, (B,)),
-            c.ptr(out_weights, "out_weights", torch.float32, shape),
-            c.ptr(out_index, "out_index", torch.int32, shape), c.stream)
+    dev = weights.device
+    tp, B, mp = _table(block_table, cache, dev)
+    dp, _, dmp = _table(dst_table, cache, dev, "dst_table", B)
+    max_len = weights.shape[-1]
+    shape = (B, cache.heads, budget)
+    if out_lens is None:
+        out_lens = _made((B,), _I32, dev, stream)
+    if out_weights is None:
+        out_weights = _made(shape, _F32, dev, stream)
+    if out_index is None:
+        out_index = _made(shape, _I32, dev, stream)
+    st = _load().fdllm_cache_evict(
+        cache._ref, tp, B, mp, _ptr(cache_lens, "cache_lens", _I32, (B,), dev),
+        _ptr(weights, "weights", _F32, (B, cache.heads, max_len), dev), max_len, budget,
+        keep_first, keep_last, dp, dmp, _ptr(out_lens, "out_lens", _I32, (B,), dev),
+        _ptr(out_weights, "out_weights", _F32, shape, dev),
+        _ptr(out_index, "out_index", _I32, shape, dev),
+        _raw_stream(dev.index) if stream is None else _stream(stream))
+    if st:
         _check(st, "fdllm_cache_evict")
-        return out_lens, out_weights, out_index
+    return out_lens, out_weights, out_index
+
+
+def fdllm_cache_status(stream=None) -> int:
+    """Synchronises and returns (clearing it) the sticky device status of the cache's attention
+    and key-weight kernels on the current device."""
+    return _load().fdllm_cache_status(_stream(stream))
 
 
 def fdllm_check_bounded_wait(seconds: float = 0.01, stream=None) -> int:

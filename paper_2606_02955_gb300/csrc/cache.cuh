@@ -67,6 +67,10 @@ inline bool check_table(const int32_t *table, int B, int max_pages, int page_shi
 bool check_queries(const void *q, const int64_t *strides, int dtype, int B, int Lq, int Hq,
                    int heads);
 
+// The status word of the cache's kernels on the current device (null where it cannot be had);
+// looked up once per device, so the first call on a device must not be under stream capture.
+uint32_t *cache_status_word();
+
 // A base and its strides as 16-byte vectors need them.
 inline bool aligned16(const void *p, const int64_t *strides, int n, int esize)
 {

@@ -70,6 +70,7 @@ struct AttnArgs {
     float *parts;             // [grid][2][N][D] accumulators, at the row's reference
     float *part_refs;         // [grid][2][N][2] (reference, sum)
     int32_t *meta;            // [grid][kMeta]
+    uint32_t *status;         // sticky: a bounded wait gave up
 };
 
 // meta of a CTA: whether it starts a unit that it does not finish (slot 1) and which, whether
@@ -330,16 +331,16 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
     auto bar = [&](int i) { return bar0 + 8u * i; };
     bool dead = false;  // a wait gave up: no further wait, the walk goes on to its end
     auto wait = [&](int i, uint32_t parity) {
-        if (!dead && !mbar_wait_at<0>(bar(i), parity, &g_status))
+        if (!dead && !mbar_wait_at<0>(bar(i), parity, a.status))
             dead = true;
     };
     auto wait_u = [&](int i, uint32_t parity) {
-        if (!dead && !mbar_wait_at<20>(bar(i), parity, &g_status))
+        if (!dead && !mbar_wait_at<20>(bar(i), parity, a.status))
             dead = true;
     };
     // the same for a whole warp that waits most of its time
     auto wait_warp = [&](auto sleep, int i, uint32_t parity) {
-        if (!dead && !mbar_wait_at<decltype(sleep)::value>(bar(i), parity, &g_status))
+        if (!dead && !mbar_wait_at<decltype(sleep)::value>(bar(i), parity, a.status))
             dead = true;
         dead = __any_sync(0xFFFFFFFFu, dead);
     };
@@ -480,7 +481,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
         __syncwarp();
         for (uint32_t i = 0; i < min(ring, (uint32_t)S::stages); ++i) {
             const uint32_t r = ring - 1 - i;
-            mbar_wait_at<100>(bar(kFull + r % S::stages), (r / S::stages) & 1, &g_status,
+            mbar_wait_at<100>(bar(kFull + r % S::stages), (r / S::stages) & 1, a.status,
                               dead ? kDrainLimitNs : kWaitLimitNs);
         }
     } else if (warp == S::issuer) {
@@ -1268,6 +1269,21 @@ cudaError_t run_rows(const AttnArgs &a, int N, int grid, const CUtensorMap &k, c
 
 }  // namespace
 
+uint32_t *cache_status_word()
+{
+    static uint32_t *word[64] = {nullptr};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64)
+        return nullptr;
+    if (!word[dev]) {
+        void *p = nullptr;
+        if (cudaGetSymbolAddress(&p, g_status) != cudaSuccess)
+            return nullptr;
+        word[dev] = static_cast<uint32_t *>(p);
+    }
+    return word[dev];
+}
+
 bool check_queries(const void *q, const int64_t *strides, int dtype, int B, int Lq, int Hq,
                    int heads)
 {
@@ -1357,7 +1373,8 @@ fdllm_status fdllm_cache_attention(const void *q, const int64_t *q_strides, int 
         bound = (int64_t)a.c.heads * a.row_tiles * B * tiles;
     const int grid = (int)(bound < most ? bound : most);
     CUtensorMap k_map, v_map;
-    if (!make_cache_maps(a.c, &k_map, &v_map))
+    a.status = cache_status_word();
+    if (!a.status || !make_cache_maps(a.c, &k_map, &v_map))
         return FDLLM_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool bf = dtype == FDLLM_BF16;
@@ -1367,6 +1384,21 @@ fdllm_status fdllm_cache_attention(const void *q, const int64_t *q_strides, int 
                  : (bf ? run_rows<64, __nv_bfloat16>(a, N, grid, k_map, v_map, s)
                        : run_rows<64, __half>(a, N, grid, k_map, v_map, s));
     return e == cudaSuccess ? FDLLM_OK : FDLLM_ERR_CUDA;
+}
+
+fdllm_status fdllm_cache_status(void *stream)
+{
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    uint32_t *word = cache_status_word(), host = 0;
+    if (!word || cudaMemcpyAsync(&host, word, sizeof host, cudaMemcpyDeviceToHost, s) != cudaSuccess ||
+        cudaStreamSynchronize(s) != cudaSuccess)
+        return FDLLM_ERR_CUDA;
+    if (host == 0)
+        return FDLLM_OK;
+    if (cudaMemsetAsync(word, 0, sizeof host, s) != cudaSuccess ||
+        cudaStreamSynchronize(s) != cudaSuccess)
+        return FDLLM_ERR_CUDA;
+    return FDLLM_ERR_DEVICE;
 }
 
 }  // extern "C"

@@ -41,6 +41,7 @@ struct WeighArgs {
     float *out;
     int max_len;
     int rows;                 // Lq * group
+    uint32_t *status;         // sticky: a bounded wait gave up
 };
 
 template <int D_, int N_>
@@ -61,8 +62,6 @@ struct Shape {
     static constexpr int tmem = tS + 2 * N <= 128 ? 128 : 256;
     static_assert(tS + 2 * N <= tmem && ctas * tmem <= 512, "tensor memory");
 };
-
-__device__ uint32_t g_status;  // sticky: a bounded wait gave up
 
 // A sequence's cached length, or -1 where it is out of range.
 __device__ __forceinline__ int length_of(const WeighArgs &a, int b)
@@ -158,7 +157,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
     auto bar = [&](int i) { return bar0 + 8u * i; };
     bool dead = false;  // a wait gave up: no further wait, the walk goes on to its end
     auto wait = [&](auto sleep, int i, uint32_t parity) {
-        if (!dead && !mbar_wait_at<decltype(sleep)::value>(bar(i), parity, &g_status))
+        if (!dead && !mbar_wait_at<decltype(sleep)::value>(bar(i), parity, a.status))
             dead = true;
     };
     using Long = std::integral_constant<int, 100>;
@@ -237,7 +236,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
         // Nothing may land in this CTA's memory after it has gone.
         for (uint32_t i = 0; i < min(ring, (uint32_t)S::stages); ++i) {
             const uint32_t r = ring - 1 - i;
-            mbar_wait_at<100>(bar(kFull + r % S::stages), (r / S::stages) & 1, &g_status,
+            mbar_wait_at<100>(bar(kFull + r % S::stages), (r / S::stages) & 1, a.status,
                               dead ? kDrainLimitNs : kWaitLimitNs);
         }
     } else if (warp == S::issuer) {
@@ -509,7 +508,8 @@ fdllm_status fdllm_cache_key_weights(const void *q, const int64_t *q_strides, in
     a.out = weights_out;
     a.max_len = max_len;
     CUtensorMap k_map;
-    if (!make_cache_maps(a.c, &k_map, nullptr))
+    a.status = cache_status_word();
+    if (!a.status || !make_cache_maps(a.c, &k_map, nullptr))
         return FDLLM_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool bf = dtype == FDLLM_BF16;
