@@ -3,6 +3,11 @@
 //
 // Bound by memory: a row of D 16-bit values (2 D bytes) becomes D/2 bytes of codes and 4 bytes
 // of scale and offset.
+//
+// Two forms.  A CTA of the tile form takes 32 slots of one head, so that a channel's values fill
+// 16 bytes of v_codes: they change places (slot by channel to channel by slot) in registers and
+// shared memory.  A few tokens (kFewTokens) would leave most of such a CTA idle: there 8 (D = 64:
+// 4) lanes take two neighbouring slots, a byte of v_codes, and touch the bytes themselves.
 #include <cuda_runtime.h>
 
 #include "cache.cuh"
@@ -10,11 +15,8 @@
 namespace fdllm {
 namespace {
 
-// One CTA handles kSlots consecutive slots of one head, a piece that starts at a multiple of
-// kSlots and so lies within one page: a thread holds 16 channels of one slot's keys and values,
-// D / 16 lanes to a row.  The values' codes go through shared memory, because v_codes is
-// channel-major: thread d then owns the 16 bytes of channel d.
-constexpr int kSlots = 32;
+constexpr int kSlots = 32;     // slots of a tile: a piece that lies within one page
+constexpr int kFewTokens = 8;  // calls of at most so many tokens take the few-token form
 
 struct StoreArgs {
     CacheView c;
@@ -34,6 +36,31 @@ __device__ __forceinline__ int count_of(const StoreArgs &a, int b)
 {
     const int c = a.count ? a.count[b] : a.n;
     return min(max(c, 0), a.n);
+}
+
+// x / s for 0 <= x / s <= 15.x, rounded to the nearest integer (ties to even) and clamped to
+// 0..15, as bytes; `near` becomes the largest distance of a quotient from its integer.
+constexpr float kMagic = 12582912.0f;  // 1.5 * 2^23: adding it rounds to an integer
+
+template <bool kExact>
+__device__ __forceinline__ void round_codes(const float (&x)[16], float o, float s, float inv,
+                                            uint32_t (&codes)[4], float &near)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t u[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float d = __fsub_rn(x[4 * i + e], o);
+            float t = kExact ? __fdiv_rn(d, s) : d * inv;
+            t = fminf(fmaxf(t, 0.0f), 15.0f);
+            const float r = __fadd_rn(t, kMagic);
+            near = fmaxf(near, fabsf(t - __fsub_rn(r, kMagic)));
+            u[e] = __float_as_uint(r);
+        }
+        codes[i] = __byte_perm(__byte_perm(u[0], u[1], 0x0040), __byte_perm(u[2], u[3], 0x0040),
+                               0x5410);
+    }
 }
 
 // Scale and offset (packed) and the 16 codes (a byte each, four words) of this lane's part of
@@ -60,29 +87,67 @@ __device__ __forceinline__ uint32_t quantise(const float (&x)[16], uint32_t (&co
     if (!(fabsf(s) + fabsf(o) + poison < __int_as_float(0x7F800000)))
         return 0x7FC07FC0u;  // scale and offset NaN
     if (s != 0.0f) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float t = rintf(__fdiv_rn(__fsub_rn(x[i], o), s));
-            codes[i >> 2] |= (uint32_t)fminf(fmaxf(t, 0.0f), 15.0f) << (8 * (i & 3));
-        }
+        // A product with the reciprocal is within 2^-22 of the quotient, relatively (2^-18 of 15):
+        // only where it comes that close to a half can the two round differently, and there (or
+        // with a reciprocal that is not a normal number) the division decides.
+        const float inv = __frcp_rn(s);
+        float near = 0.0f;
+        const bool normal = s > 0x1p-120f && s < 0x1p120f;
+        round_codes<false>(x, o, s, inv, codes, near);
+        if (!normal || near > 0.49999f)
+            round_codes<true>(x, o, s, inv, codes, near);
     }
     return (__float_as_uint(s) >> 16) | (__float_as_uint(o) & 0xFFFF0000u);
 }
 
-// Bytes of codes two to a word's low half -> nibbles: four byte codes -> 16 bits.
+// Bytes of codes -> nibbles: four byte codes -> 16 bits.
 __device__ __forceinline__ uint32_t nibbles(uint32_t w)
 {
     const uint32_t p = w | (w >> 4);  // byte 0: codes 0, 1; byte 2: codes 2, 3
     return (p & 0xFFu) | ((p >> 8) & 0xFF00u);
 }
 
+// A row's codes of this lane as 8 bytes of k_codes.
+__device__ __forceinline__ uint2 row_nibbles(const uint32_t (&c)[4])
+{
+    return make_uint2(nibbles(c[0]) | (nibbles(c[1]) << 16), nibbles(c[2]) | (nibbles(c[3]) << 16));
+}
+
+template <typename T>
+__device__ __forceinline__ void load16(const T *p, float (&x)[16])
+{
+    load8(p, reinterpret_cast<float (&)[8]>(x[0]));
+    load8(p + 8, reinterpret_cast<float (&)[8]>(x[8]));
+}
+
+template <typename T>
+__device__ __forceinline__ void store16(T *p, const float (&x)[16])
+{
+    store8(p, reinterpret_cast<const float (&)[8]>(x[0]));
+    store8(p + 8, reinterpret_cast<const float (&)[8]>(x[8]));
+}
+
+template <typename T>
+__device__ __forceinline__ const T *row_of(const void *p, const Strides3 &s, int b, int i, int h)
+{
+    return static_cast<const T *>(p) + b * s.batch + i * s.token + h * s.head;
+}
+
+// Code `c` (an integer below 16) of a row with this scale and offset.
+__device__ __forceinline__ float value_of(uint32_t c, uint32_t affine)
+{
+    return fmaf(bf16_low(affine), __uint_as_float(c | 0x4B000000u) - 8388608.0f,
+                bf16_high(affine));
+}
+
+// The tile form.  A thread holds 16 channels of one slot, kLanes = D / 16 lanes a row.
 template <typename T, int D>
 __global__ void __launch_bounds__(2 * D) append_kernel(const __grid_constant__ StoreArgs a)
 {
     constexpr int kLanes = D / 16;
-    __shared__ __align__(16) uint8_t vsm[kSlots][D];
+    __shared__ __align__(16) uint16_t quad[kSlots / 4][D];  // four slots of a channel
     pdl_wait();
-    const int h = blockIdx.y, b = blockIdx.z;
+    const int h = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 31;
     const int start = a.start ? a.start[b] : 0;
     const int count = count_of(a, b);
     if (start < 0 || start > (a.max_pages << a.c.page_shift))
@@ -102,71 +167,65 @@ __global__ void __launch_bounds__(2 * D) append_kernel(const __grid_constant__ S
     for (int j = 0; j < 16; ++j)
         xk[j] = xv[j] = 0.0f;
     if (live) {
-        const T *k = static_cast<const T *>(a.k) + b * a.ks.batch + i * a.ks.token +
-                     h * a.ks.head + 16 * part;
-        const T *v = static_cast<const T *>(a.v) + b * a.vs.batch + i * a.vs.token +
-                     h * a.vs.head + 16 * part;
-        load8(k, reinterpret_cast<float (&)[8]>(xk[0]));
-        load8(k + 8, reinterpret_cast<float (&)[8]>(xk[8]));
-        load8(v, reinterpret_cast<float (&)[8]>(xv[0]));
-        load8(v + 8, reinterpret_cast<float (&)[8]>(xv[8]));
+        load16(row_of<T>(a.k, a.ks, b, i, h) + 16 * part, xk);
+        load16(row_of<T>(a.v, a.vs, b, i, h) + 16 * part, xv);
     }
-    uint32_t ck[4], cv[4];
-    const uint32_t ak = quantise<kLanes>(xk, ck);
-    const uint32_t av = quantise<kLanes>(xv, cv);
+    uint32_t c[4];
     const int64_t at = slot_index(a.c, pg, h, slot);
-    if (live) {
-        *reinterpret_cast<uint2 *>(a.c.kc + at * (D / 2) + 8 * part) =
-            make_uint2(nibbles(ck[0]) | (nibbles(ck[1]) << 16),
-                       nibbles(ck[2]) | (nibbles(ck[3]) << 16));
-        if (part == 0) {
-            a.c.ka[at] = ak;
-            a.c.va[at] = av;
-        }
+    const uint32_t ak = quantise<kLanes>(xk, c);
+    if (live)
+        *reinterpret_cast<uint2 *>(a.c.kc + at * (D / 2) + 8 * part) = row_nibbles(c);
+    const uint32_t av = quantise<kLanes>(xv, c);
+    if (live && part == 0) {
+        a.c.ka[at] = ak;
+        a.c.va[at] = av;
     }
-    *reinterpret_cast<uint4 *>(&vsm[slot - slot0][16 * part]) =
-        make_uint4(cv[0], cv[1], cv[2], cv[3]);
+    // Two slots to a byte: the even slot's lane takes the lower eight channels of both, the odd
+    // slot's the upper; then four slots to 16 bits, four channels a lane.
+    const bool odd = lane & kLanes, high = lane & (2 * kLanes);
+    uint32_t p[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const uint32_t mine = odd ? c[2 + e] : c[e], give = odd ? c[e] : c[2 + e];
+        const uint32_t got = __shfl_xor_sync(0xFFFFFFFFu, give, kLanes);
+        p[e] = odd ? got | (mine << 4) : mine | (got << 4);
+    }
+    const uint32_t mine = high ? p[1] : p[0];
+    const uint32_t got = __shfl_xor_sync(0xFFFFFFFFu, high ? p[0] : p[1], 2 * kLanes);
+    const uint32_t lo = high ? got : mine, hi = high ? mine : got;  // slots 0, 1; slots 2, 3
+    const int channel = 16 * part + (odd ? 8 : 0) + (high ? 4 : 0);
+    *reinterpret_cast<uint2 *>(&quad[(slot - slot0) / 4][channel]) =
+        make_uint2(__byte_perm(lo, hi, 0x5140), __byte_perm(lo, hi, 0x7362));
     __syncthreads();
     const int d = threadIdx.x;
     if (d >= D)
         return;
-    uint8_t *dst = a.c.vc + v_byte(a.c, pg, h, d, slot0);
-    if (slot0 >= start && slot0 + kSlots <= start + count) {
-        uint32_t w[4];
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        w[j] = quad[2 * j][d] | ((uint32_t)quad[2 * j + 1][d] << 16);
+    uint4 *dst = reinterpret_cast<uint4 *>(a.c.vc + v_byte(a.c, pg, h, d, slot0));
+    const int first = max(start - slot0, 0), last = min(start + count - slot0, kSlots);
+    if (first > 0 || last < kSlots) {
+        // A piece at the ends of the range keeps the slots that the call does not write.
+        const uint4 was = *dst;
+        const uint32_t o[4] = {was.x, was.y, was.z, was.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            uint32_t x = 0;
-#pragma unroll
-            for (int t = 0; t < 8; ++t)
-                x |= (uint32_t)vsm[8 * j + t][d] << (4 * t);
-            w[j] = x;
+            const int from = min(max(first - 8 * j, 0), 8), to = min(max(last - 8 * j, 0), 8);
+            const uint64_t all = (1ull << (4 * to)) - 1, none = (1ull << (4 * from)) - 1;
+            const uint32_t m = to > from ? (uint32_t)(all & ~none) : 0u;
+            w[j] = (w[j] & m) | (o[j] & ~m);
         }
-        *reinterpret_cast<uint4 *>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
-        return;
     }
-    // A piece at the ends of the range: bytes that it fills by half keep their other slot.
-    for (int j = 0; j < kSlots / 2; ++j) {
-        const int s = slot0 + 2 * j;
-        const bool lo = s >= start && s < start + count;
-        const bool hi = s + 1 >= start && s + 1 < start + count;
-        if (!lo && !hi)
-            continue;
-        uint8_t x = 0;
-        if (!lo || !hi)
-            x = dst[j] & (lo ? 0xF0u : 0x0Fu);
-        if (lo)
-            x |= vsm[2 * j][d];
-        if (hi)
-            x |= vsm[2 * j + 1][d] << 4;
-        dst[j] = x;
-    }
+    *dst = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 template <typename T, int D>
 __global__ void __launch_bounds__(2 * D) read_kernel(const __grid_constant__ StoreArgs a)
 {
     constexpr int kLanes = D / 16;
-    __shared__ __align__(16) uint8_t vsm[kSlots][D];
+    __shared__ __align__(16) uint16_t quad[kSlots / 4][D];
     pdl_wait();
     const int h = blockIdx.y, b = blockIdx.z;
     const int start = a.start ? a.start[b] : 0;
@@ -181,68 +240,196 @@ __global__ void __launch_bounds__(2 * D) read_kernel(const __grid_constant__ Sto
     // Slots are counted in 64 bits here: start is any int.
     const int64_t slot0 = (int64_t)start + i0;
     const bool inside = slot0 >= 0 && slot0 < ((int64_t)a.max_pages << a.c.page_shift);
-    const int pg = inside ? page_of(a.c, a.table, a.max_pages, b, (int)slot0) : -1;
+    const bool any = i0 < count;
+    const int pg = inside && any ? page_of(a.c, a.table, a.max_pages, b, (int)slot0) : -1;
     const int s = inside ? (int)slot0 : 0;
+    const bool live = i >= 0 && i < count && pg >= 0;
+    uint2 kw = make_uint2(0, 0);
+    uint32_t ak = 0, av = 0;
+    if (live) {
+        const int64_t at = slot_index(a.c, pg, h, s + threadIdx.x / kLanes);
+        kw = *reinterpret_cast<const uint2 *>(a.c.kc + at * (D / 2) + 8 * part);
+        ak = a.c.ka[at];
+        av = a.c.va[at];
+    }
     if (pg >= 0 && threadIdx.x < D) {
         const int d = threadIdx.x;
         const uint4 w = *reinterpret_cast<const uint4 *>(a.c.vc + v_byte(a.c, pg, h, d, s));
         const uint32_t x[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-        for (int j = 0; j < kSlots; ++j)
-            vsm[j][d] = (x[j >> 3] >> (4 * (j & 7))) & 15u;
+        for (int j = 0; j < 4; ++j) {
+            quad[2 * j][d] = (uint16_t)x[j];
+            quad[2 * j + 1][d] = (uint16_t)(x[j] >> 16);
+        }
     }
     __syncthreads();
     if (i < 0 || i >= a.n)
         return;
-    float xk[16], xv[16];
-    if (i >= count) {
-#pragma unroll
-        for (int j = 0; j < 16; ++j)
-            xk[j] = xv[j] = 0.0f;
-    } else if (pg < 0) {
-#pragma unroll
-        for (int j = 0; j < 16; ++j)
-            xk[j] = xv[j] = nan_f();
-    } else {
-        const int64_t at = slot_index(a.c, pg, h, s + threadIdx.x / kLanes);
-        const uint2 w = *reinterpret_cast<const uint2 *>(a.c.kc + at * (D / 2) + 8 * part);
-        const uint32_t ak = a.c.ka[at], av = a.c.va[at];
-        const uint4 c = *reinterpret_cast<const uint4 *>(&vsm[threadIdx.x / kLanes][16 * part]);
-        const uint32_t kw[2] = {w.x, w.y}, vw[4] = {c.x, c.y, c.z, c.w};
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            xk[j] = fmaf(bf16_low(ak), (float)((kw[j >> 3] >> (4 * (j & 7))) & 15u),
-                         bf16_high(ak));
-            xv[j] = fmaf(bf16_low(av), (float)((vw[j >> 2] >> (8 * (j & 3))) & 15u),
-                         bf16_high(av));
-        }
-    }
     const int64_t o = (((int64_t)b * a.n + i) * a.c.heads + h) * D + 16 * part;
     T *ok = static_cast<T *>(a.out_k) + o;
     T *ov = static_cast<T *>(a.out_v) + o;
-    store8(ok, reinterpret_cast<float (&)[8]>(xk[0]));
-    store8(ok + 8, reinterpret_cast<float (&)[8]>(xk[8]));
-    store8(ov, reinterpret_cast<float (&)[8]>(xv[0]));
-    store8(ov + 8, reinterpret_cast<float (&)[8]>(xv[8]));
+    float x[16];
+    if (!live) {
+        // behind the count: 0; no such slot: NaN
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            x[j] = i >= count ? 0.0f : nan_f();
+        store16(ok, x);
+        store16(ov, x);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+        x[j] = value_of(((j < 8 ? kw.x : kw.y) >> (4 * (j & 7))) & 15u, ak);
+    store16(ok, x);
+    const int in = threadIdx.x / kLanes, shift = 4 * (in & 3);
+    const uint4 *q = reinterpret_cast<const uint4 *>(&quad[in / 4][16 * part]);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const uint4 w = q[j];
+        const uint32_t c[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t two = c[e] >> shift;  // this slot's codes of two channels
+            x[8 * j + 2 * e] = value_of(two & 15u, av);
+            x[8 * j + 2 * e + 1] = value_of((two >> 16) & 15u, av);
+        }
+    }
+    store16(ov, x);
+}
+
+// The few-token form: kLanes lanes a pair of slots (2 m, 2 m + 1) of one head.
+template <typename T, int D>
+__global__ void __launch_bounds__(128) append_few_kernel(const __grid_constant__ StoreArgs a,
+                                                         int pairs)
+{
+    constexpr int kLanes = D / 16;
+    pdl_wait();
+    const int b = blockIdx.y, part = threadIdx.x % kLanes;
+    const int row = (blockIdx.x * 128 + threadIdx.x) / kLanes;  // head * pairs + pair
+    const int h = row / pairs, pair = row - h * pairs;
+    const int start = a.start ? a.start[b] : 0;
+    const int end = start + count_of(a, b);
+    const bool there = h < a.c.heads && start >= 0 && start <= (a.max_pages << a.c.page_shift);
+    const int slot0 = there ? (start / 2 + pair) * 2 : 0;
+    const int pg = there && slot0 < end ? page_of(a.c, a.table, a.max_pages, b, slot0) : -1;
+    uint32_t cv[2][4];
+    bool live[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const int slot = slot0 + e, i = slot - start;
+        live[e] = pg >= 0 && slot >= start && slot < end;
+        float xk[16], xv[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            xk[j] = xv[j] = 0.0f;
+        if (live[e]) {
+            load16(row_of<T>(a.k, a.ks, b, i, h) + 16 * part, xk);
+            load16(row_of<T>(a.v, a.vs, b, i, h) + 16 * part, xv);
+        }
+        uint32_t ck[4];
+        const uint32_t ak = quantise<kLanes>(xk, ck);
+        const uint32_t av = quantise<kLanes>(xv, cv[e]);
+        if (live[e]) {
+            const int64_t at = slot_index(a.c, pg, h, slot);
+            *reinterpret_cast<uint2 *>(a.c.kc + at * (D / 2) + 8 * part) = row_nibbles(ck);
+            if (part == 0) {
+                a.c.ka[at] = ak;
+                a.c.va[at] = av;
+            }
+        }
+    }
+    if (!live[0] && !live[1])
+        return;
+    uint8_t *v = a.c.vc + v_byte(a.c, pg, h, 16 * part, slot0);
+    const int64_t step = (int64_t)1 << (a.c.page_shift - 1);  // a channel to the next
+    const uint32_t keep = live[0] && live[1] ? 0u : live[0] ? 0xF0u : 0x0Fu;
+    uint32_t old[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+        old[j] = keep ? v[j * step] : 0u;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+        const uint32_t lo = (cv[0][j >> 2] >> (8 * (j & 3))) & 15u;
+        const uint32_t hi = (cv[1][j >> 2] >> (8 * (j & 3))) & 15u;
+        v[j * step] = (uint8_t)((old[j] & keep) | ((lo | (hi << 4)) & ~keep));
+    }
+}
+
+// kLanes lanes a token of one head.
+template <typename T, int D>
+__global__ void __launch_bounds__(128) read_few_kernel(const __grid_constant__ StoreArgs a)
+{
+    constexpr int kLanes = D / 16;
+    pdl_wait();
+    const int b = blockIdx.y, part = threadIdx.x % kLanes;
+    const int row = (blockIdx.x * 128 + threadIdx.x) / kLanes;  // token * heads + head
+    const int i = row / a.c.heads, h = row - i * a.c.heads;
+    if (i >= a.n)
+        return;
+    const int64_t slot = (int64_t)(a.start ? a.start[b] : 0) + i;
+    const int count = count_of(a, b);
+    const bool inside = slot >= 0 && slot < ((int64_t)a.max_pages << a.c.page_shift);
+    const int pg = inside && i < count ? page_of(a.c, a.table, a.max_pages, b, (int)slot) : -1;
+    const int64_t o = (((int64_t)b * a.n + i) * a.c.heads + h) * D + 16 * part;
+    float xk[16], xv[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+        xk[j] = xv[j] = i >= count ? 0.0f : nan_f();
+    if (pg >= 0) {
+        const int64_t at = slot_index(a.c, pg, h, (int)slot);
+        const uint8_t *v = a.c.vc + v_byte(a.c, pg, h, 16 * part, (int)slot);
+        const int64_t step = (int64_t)1 << (a.c.page_shift - 1);
+        const uint2 kw = *reinterpret_cast<const uint2 *>(a.c.kc + at * (D / 2) + 8 * part);
+        uint32_t c[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            c[j] = v[j * step];
+        const uint32_t ak = a.c.ka[at], av = a.c.va[at];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            xk[j] = value_of(((j < 8 ? kw.x : kw.y) >> (4 * (j & 7))) & 15u, ak);
+            xv[j] = value_of((c[j] >> (4 * ((int)slot & 1))) & 15u, av);
+        }
+    }
+    store16(static_cast<T *>(a.out_k) + o, xk);
+    store16(static_cast<T *>(a.out_v) + o, xv);
 }
 
 // Pieces that n slots from any start can touch.
 int pieces(int n) { return (int)(((int64_t)n + kSlots - 2) / kSlots + 1); }
 
+template <typename T, int D>
+cudaError_t launch_append_rows(const StoreArgs &a, int B, cudaStream_t s)
+{
+    if (a.n <= kFewTokens) {
+        const int pairs = a.n / 2 + 1;
+        const unsigned blocks = (unsigned)(((int64_t)a.c.heads * pairs * (D / 16) + 127) / 128);
+        return launch(append_few_kernel<T, D>, dim3(blocks, B), dim3(128), 0, s, true, a, pairs);
+    }
+    return launch(append_kernel<T, D>, dim3(pieces(a.n), a.c.heads, B), dim3(2 * D), 0, s, true, a);
+}
+
+template <typename T, int D>
+cudaError_t launch_read_rows(const StoreArgs &a, int B, cudaStream_t s)
+{
+    if (a.n <= kFewTokens) {
+        const unsigned blocks = (unsigned)(((int64_t)a.c.heads * a.n * (D / 16) + 127) / 128);
+        return launch(read_few_kernel<T, D>, dim3(blocks, B), dim3(128), 0, s, true, a);
+    }
+    return launch(read_kernel<T, D>, dim3(pieces(a.n), a.c.heads, B), dim3(2 * D), 0, s, true, a);
+}
+
 template <typename T>
 cudaError_t launch_append(const StoreArgs &a, int B, cudaStream_t s)
 {
-    const dim3 grid(pieces(a.n), a.c.heads, B);
-    return a.c.D == 128 ? launch(append_kernel<T, 128>, grid, dim3(256), 0, s, true, a)
-                        : launch(append_kernel<T, 64>, grid, dim3(128), 0, s, true, a);
+    return a.c.D == 128 ? launch_append_rows<T, 128>(a, B, s) : launch_append_rows<T, 64>(a, B, s);
 }
 
 template <typename T>
 cudaError_t launch_read(const StoreArgs &a, int B, cudaStream_t s)
 {
-    const dim3 grid(pieces(a.n), a.c.heads, B);
-    return a.c.D == 128 ? launch(read_kernel<T, 128>, grid, dim3(256), 0, s, true, a)
-                        : launch(read_kernel<T, 64>, grid, dim3(128), 0, s, true, a);
+    return a.c.D == 128 ? launch_read_rows<T, 128>(a, B, s) : launch_read_rows<T, 64>(a, B, s);
 }
 
 bool valid_dtype(int d) { return d == FDLLM_BF16 || d == FDLLM_FP32 || d == FDLLM_FP16; }
