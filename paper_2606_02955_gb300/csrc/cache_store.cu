@@ -10,7 +10,10 @@
 // 4) lanes take two neighbouring slots, a byte of v_codes, and touch the bytes themselves.
 #include <cuda_runtime.h>
 
+#include <type_traits>
+
 #include "cache.cuh"
+#include "cache_tc.cuh"
 
 namespace fdllm {
 namespace {
@@ -38,25 +41,114 @@ __device__ __forceinline__ int count_of(const StoreArgs &a, int b)
     return min(max(c, 0), a.n);
 }
 
-// x / s for 0 <= x / s <= 15.x, rounded to the nearest integer (ties to even) and clamped to
-// 0..15, as bytes; `near` becomes the largest distance of a quotient from its integer.
-constexpr float kMagic = 12582912.0f;  // 1.5 * 2^23: adding it rounds to an integer
+// Sixteen values of this lane: smallest and largest, NaN where one of them is (an infinity makes
+// the range one, or a NaN).  Values of 16 bits are compared two at a time.
+template <typename T>
+struct Row16 {
+    uint32_t w[8];  // of 16-bit types, as they lie in memory
+    __device__ __forceinline__ void load(const T *p)
+    {
+        const uint4 a = reinterpret_cast<const uint4 *>(p)[0], b = reinterpret_cast<const uint4 *>(p)[1];
+        w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
+        w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+    }
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            w[i] = 0;
+    }
+    __device__ __forceinline__ void two(int i, float &x, float &y) const
+    {
+        if constexpr (__is_same(T, __nv_bfloat16)) {
+            x = bf16_low(w[i]);
+            y = bf16_high(w[i]);
+        } else {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
+            x = f.x;
+            y = f.y;
+        }
+    }
+    __device__ __forceinline__ void range(float &low, float &high) const
+    {
+        using P = std::conditional_t<__is_same(T, __nv_bfloat16), __nv_bfloat162, __half2>;
+        P lo = *reinterpret_cast<const P *>(&w[0]), hi = lo;
+#pragma unroll
+        for (int i = 1; i < 8; ++i) {
+            const P x = *reinterpret_cast<const P *>(&w[i]);
+            lo = __hmin2_nan(lo, x);
+            hi = __hmax2_nan(hi, x);
+        }
+        low = fmin_nan(to_float(lo.x), to_float(lo.y));
+        high = fmax_nan(to_float(hi.x), to_float(hi.y));
+    }
+};
 
-template <bool kExact>
-__device__ __forceinline__ void round_codes(const float (&x)[16], float o, float s, float inv,
+template <>
+struct Row16<float> {
+    float v[16];
+    __device__ __forceinline__ void load(const float *p)
+    {
+        load8(p, reinterpret_cast<float (&)[8]>(v[0]));
+        load8(p + 8, reinterpret_cast<float (&)[8]>(v[8]));
+    }
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            v[i] = 0.0f;
+    }
+    __device__ __forceinline__ void two(int i, float &x, float &y) const
+    {
+        x = v[2 * i];
+        y = v[2 * i + 1];
+    }
+    __device__ __forceinline__ void range(float &low, float &high) const
+    {
+        low = high = v[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) {
+            low = fmin_nan(low, v[i]);
+            high = fmax_nan(high, v[i]);
+        }
+    }
+};
+
+// (x - o) / s, rounded to the nearest integer (ties to even) and clamped to 0..15, as bytes;
+// `near` becomes the largest distance of a quotient from its integer.  15 sat(d / (15 s)) clamps
+// in the product; adding 1.5 * 2^23 rounds.
+constexpr float kMagic = 12582912.0f;
+
+template <bool kExact, typename T>
+__device__ __forceinline__ void round_codes(const Row16<T> &x, float o, float s, float inv15,
                                             uint32_t (&codes)[4], float &near)
 {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         uint32_t u[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float d = __fsub_rn(x[4 * i + e], o);
-            float t = kExact ? __fdiv_rn(d, s) : d * inv;
-            t = fminf(fmaxf(t, 0.0f), 15.0f);
-            const float r = __fadd_rn(t, kMagic);
-            near = fmaxf(near, fabsf(t - __fsub_rn(r, kMagic)));
-            u[e] = __float_as_uint(r);
+        for (int e = 0; e < 2; ++e) {
+            float x0, x1, t0, t1;
+            x.two(2 * i + e, x0, x1);
+            if constexpr (kExact) {
+                t0 = __saturatef(__fdiv_rn(__fsub_rn(x0, o), s) * (1.0f / 16.0f));
+                t1 = __saturatef(__fdiv_rn(__fsub_rn(x1, o), s) * (1.0f / 16.0f));
+                u[2 * e] = __float_as_uint(__fadd_rn(fminf(t0 * 16.0f, 15.0f), kMagic));
+                u[2 * e + 1] = __float_as_uint(__fadd_rn(fminf(t1 * 16.0f, 15.0f), kMagic));
+            } else {
+                un2(add2(f2(x0, x1), f2(-o, -o)), t0, t1);
+                t0 = __saturatef(t0 * inv15);
+                t1 = __saturatef(t1 * inv15);
+                const uint64_t t = f2(t0, t1);
+                const uint64_t r = fma2(t, f2(15.0f, 15.0f), f2(kMagic, kMagic));
+                const uint64_t q = add2(r, f2(-kMagic, -kMagic));
+                float e0, e1, r0, r1;
+                un2(fma2(t, f2(-15.0f, -15.0f), q), e0, e1);
+                un2(r, r0, r1);
+                near = max3(near, fabsf(e0), fabsf(e1));
+                u[2 * e] = __float_as_uint(r0);
+                u[2 * e + 1] = __float_as_uint(r1);
+            }
         }
         codes[i] = __byte_perm(__byte_perm(u[0], u[1], 0x0040), __byte_perm(u[2], u[3], 0x0040),
                                0x5410);
@@ -65,37 +157,31 @@ __device__ __forceinline__ void round_codes(const float (&x)[16], float o, float
 
 // Scale and offset (packed) and the 16 codes (a byte each, four words) of this lane's part of
 // a row of 16 * LANES values held by LANES neighbouring lanes.  All lanes of the warp take part.
-template <int LANES>
-__device__ __forceinline__ uint32_t quantise(const float (&x)[16], uint32_t (&codes)[4])
+template <int LANES, typename T>
+__device__ __forceinline__ uint32_t quantise(const Row16<T> &x, uint32_t (&codes)[4])
 {
-    float low = x[0], high = x[0], poison = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        low = fminf(low, x[i]);
-        high = fmaxf(high, x[i]);
-        poison = fmaf(x[i], 0.0f, poison);  // NaN from a NaN or an infinity
-    }
+    float low, high;
+    x.range(low, high);
 #pragma unroll
     for (int m = LANES / 2; m > 0; m >>= 1) {
-        low = fminf(low, __shfl_xor_sync(0xFFFFFFFFu, low, m));
-        high = fmaxf(high, __shfl_xor_sync(0xFFFFFFFFu, high, m));
-        poison += __shfl_xor_sync(0xFFFFFFFFu, poison, m);
+        low = fmin_nan(low, __shfl_xor_sync(0xFFFFFFFFu, low, m));
+        high = fmax_nan(high, __shfl_xor_sync(0xFFFFFFFFu, high, m));
     }
     const float s = __bfloat162float(__float2bfloat16_rn(__fdiv_rn(__fsub_rn(high, low), 15.0f)));
     const float o = __bfloat162float(__float2bfloat16_rn(low));
     codes[0] = codes[1] = codes[2] = codes[3] = 0;
-    if (!(fabsf(s) + fabsf(o) + poison < __int_as_float(0x7F800000)))
+    if (!(fabsf(s) + fabsf(o) < __int_as_float(0x7F800000)))
         return 0x7FC07FC0u;  // scale and offset NaN
     if (s != 0.0f) {
-        // A product with the reciprocal is within 2^-22 of the quotient, relatively (2^-18 of 15):
-        // only where it comes that close to a half can the two round differently, and there (or
-        // with a reciprocal that is not a normal number) the division decides.
-        const float inv = __frcp_rn(s);
+        // The product with the reciprocal is within 2^-21 of the quotient, relatively (2^-17 of
+        // 15): only where it comes that close to a half can the two round differently, and there
+        // (or with a reciprocal that is not a normal number) the division decides.
+        const float inv15 = __fdiv_rn(1.0f / 15.0f, s);
         float near = 0.0f;
-        const bool normal = s > 0x1p-120f && s < 0x1p120f;
-        round_codes<false>(x, o, s, inv, codes, near);
-        if (!normal || near > 0.49999f)
-            round_codes<true>(x, o, s, inv, codes, near);
+        const bool normal = s > 0x1p-110f && s < 0x1p110f;
+        round_codes<false>(x, o, s, inv15, codes, near);
+        if (!normal || near > 0.49998f)
+            round_codes<true>(x, o, s, inv15, codes, near);
     }
     return (__float_as_uint(s) >> 16) | (__float_as_uint(o) & 0xFFFF0000u);
 }
@@ -111,13 +197,6 @@ __device__ __forceinline__ uint32_t nibbles(uint32_t w)
 __device__ __forceinline__ uint2 row_nibbles(const uint32_t (&c)[4])
 {
     return make_uint2(nibbles(c[0]) | (nibbles(c[1]) << 16), nibbles(c[2]) | (nibbles(c[3]) << 16));
-}
-
-template <typename T>
-__device__ __forceinline__ void load16(const T *p, float (&x)[16])
-{
-    load8(p, reinterpret_cast<float (&)[8]>(x[0]));
-    load8(p + 8, reinterpret_cast<float (&)[8]>(x[8]));
 }
 
 template <typename T>
@@ -157,19 +236,19 @@ __global__ void __launch_bounds__(2 * D) append_kernel(const __grid_constant__ S
     const int part = threadIdx.x % kLanes;
     if (slot0 >= start + count)
         return;
+    // (the page is looked up while the rows are on their way)
+    const int i = slot - start;
+    const bool live = i >= 0 && i < count;
+    Row16<T> xk, xv;
+    xk.clear();
+    xv.clear();
+    if (live) {
+        xk.load(row_of<T>(a.k, a.ks, b, i, h) + 16 * part);
+        xv.load(row_of<T>(a.v, a.vs, b, i, h) + 16 * part);
+    }
     const int pg = page_of(a.c, a.table, a.max_pages, b, slot0);
     if (pg < 0)
         return;
-    const int i = slot - start;
-    const bool live = i >= 0 && i < count;
-    float xk[16], xv[16];
-#pragma unroll
-    for (int j = 0; j < 16; ++j)
-        xk[j] = xv[j] = 0.0f;
-    if (live) {
-        load16(row_of<T>(a.k, a.ks, b, i, h) + 16 * part, xk);
-        load16(row_of<T>(a.v, a.vs, b, i, h) + 16 * part, xv);
-    }
     uint32_t c[4];
     const int64_t at = slot_index(a.c, pg, h, slot);
     const uint32_t ak = quantise<kLanes>(xk, c);
@@ -221,81 +300,102 @@ __global__ void __launch_bounds__(2 * D) append_kernel(const __grid_constant__ S
     *dst = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// Reading goes from the page to the codes to the rows; kReadTiles tiles of a CTA make that way
+// together.
+constexpr int kReadTiles = 2;
+
 template <typename T, int D>
 __global__ void __launch_bounds__(2 * D) read_kernel(const __grid_constant__ StoreArgs a)
 {
     constexpr int kLanes = D / 16;
-    __shared__ __align__(16) uint16_t quad[kSlots / 4][D];
+    __shared__ __align__(16) uint16_t quad[kReadTiles][kSlots / 4][D];
     pdl_wait();
     const int h = blockIdx.y, b = blockIdx.z;
     const int start = a.start ? a.start[b] : 0;
     const int count = count_of(a, b);
     // Token i of the call is slot start + i; the first piece starts at or before start.
     const int lead = ((start % kSlots) + kSlots) % kSlots;
-    const int i0 = blockIdx.x * kSlots - lead;
-    if (i0 >= a.n)
+    const int64_t i00 = (int64_t)blockIdx.x * kReadTiles * kSlots - lead;
+    if (i00 >= a.n)
         return;
-    const int i = i0 + threadIdx.x / kLanes;
-    const int part = threadIdx.x % kLanes;
-    // Slots are counted in 64 bits here: start is any int.
-    const int64_t slot0 = (int64_t)start + i0;
-    const bool inside = slot0 >= 0 && slot0 < ((int64_t)a.max_pages << a.c.page_shift);
-    const bool any = i0 < count;
-    const int pg = inside && any ? page_of(a.c, a.table, a.max_pages, b, (int)slot0) : -1;
-    const int s = inside ? (int)slot0 : 0;
-    const bool live = i >= 0 && i < count && pg >= 0;
-    uint2 kw = make_uint2(0, 0);
-    uint32_t ak = 0, av = 0;
-    if (live) {
-        const int64_t at = slot_index(a.c, pg, h, s + threadIdx.x / kLanes);
-        kw = *reinterpret_cast<const uint2 *>(a.c.kc + at * (D / 2) + 8 * part);
-        ak = a.c.ka[at];
-        av = a.c.va[at];
-    }
-    if (pg >= 0 && threadIdx.x < D) {
-        const int d = threadIdx.x;
-        const uint4 w = *reinterpret_cast<const uint4 *>(a.c.vc + v_byte(a.c, pg, h, d, s));
-        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+    const int in = threadIdx.x / kLanes, part = threadIdx.x % kLanes;
+    int pg[kReadTiles], s[kReadTiles];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            quad[2 * j][d] = (uint16_t)x[j];
-            quad[2 * j + 1][d] = (uint16_t)(x[j] >> 16);
+    for (int t = 0; t < kReadTiles; ++t) {
+        const int64_t i0 = i00 + t * kSlots, slot0 = start + i0;
+        const bool inside = slot0 >= 0 && slot0 < ((int64_t)a.max_pages << a.c.page_shift);
+        s[t] = inside ? (int)slot0 : 0;
+        pg[t] = inside && i0 < count ? page_of(a.c, a.table, a.max_pages, b, s[t]) : -1;
+    }
+    uint2 kw[kReadTiles];
+    uint32_t ak[kReadTiles], av[kReadTiles];
+    uint4 w[kReadTiles];
+    bool live[kReadTiles];
+#pragma unroll
+    for (int t = 0; t < kReadTiles; ++t) {
+        const int64_t i = i00 + t * kSlots + in;
+        live[t] = i >= 0 && i < count && pg[t] >= 0;
+        kw[t] = make_uint2(0, 0);
+        ak[t] = av[t] = 0;
+        w[t] = make_uint4(0, 0, 0, 0);
+        if (live[t]) {
+            const int64_t at = slot_index(a.c, pg[t], h, s[t] + in);
+            kw[t] = *reinterpret_cast<const uint2 *>(a.c.kc + at * (D / 2) + 8 * part);
+            ak[t] = a.c.ka[at];
+            av[t] = a.c.va[at];
+        }
+        if (pg[t] >= 0 && threadIdx.x < D)
+            w[t] = *reinterpret_cast<const uint4 *>(a.c.vc +
+                                                    v_byte(a.c, pg[t], h, threadIdx.x, s[t]));
+    }
+    if (threadIdx.x < D) {
+#pragma unroll
+        for (int t = 0; t < kReadTiles; ++t) {
+            const uint32_t x[4] = {w[t].x, w[t].y, w[t].z, w[t].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                quad[t][2 * j][threadIdx.x] = (uint16_t)x[j];
+                quad[t][2 * j + 1][threadIdx.x] = (uint16_t)(x[j] >> 16);
+            }
         }
     }
     __syncthreads();
-    if (i < 0 || i >= a.n)
-        return;
-    const int64_t o = (((int64_t)b * a.n + i) * a.c.heads + h) * D + 16 * part;
-    T *ok = static_cast<T *>(a.out_k) + o;
-    T *ov = static_cast<T *>(a.out_v) + o;
-    float x[16];
-    if (!live) {
-        // behind the count: 0; no such slot: NaN
+#pragma unroll
+    for (int t = 0; t < kReadTiles; ++t) {
+        const int64_t i = i00 + t * kSlots + in;
+        if (i < 0 || i >= a.n)
+            continue;
+        const int64_t o = (((int64_t)b * a.n + i) * a.c.heads + h) * D + 16 * part;
+        T *ok = static_cast<T *>(a.out_k) + o;
+        T *ov = static_cast<T *>(a.out_v) + o;
+        float x[16];
+        if (!live[t]) {
+            // behind the count: 0; no such slot: NaN
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                x[j] = i >= count ? 0.0f : nan_f();
+            store16(ok, x);
+            store16(ov, x);
+            continue;
+        }
 #pragma unroll
         for (int j = 0; j < 16; ++j)
-            x[j] = i >= count ? 0.0f : nan_f();
+            x[j] = value_of(((j < 8 ? kw[t].x : kw[t].y) >> (4 * (j & 7))) & 15u, ak[t]);
         store16(ok, x);
-        store16(ov, x);
-        return;
-    }
+        const uint4 *q = reinterpret_cast<const uint4 *>(&quad[t][in / 4][16 * part]);
 #pragma unroll
-    for (int j = 0; j < 16; ++j)
-        x[j] = value_of(((j < 8 ? kw.x : kw.y) >> (4 * (j & 7))) & 15u, ak);
-    store16(ok, x);
-    const int in = threadIdx.x / kLanes, shift = 4 * (in & 3);
-    const uint4 *q = reinterpret_cast<const uint4 *>(&quad[in / 4][16 * part]);
+        for (int j = 0; j < 2; ++j) {
+            const uint4 v = q[j];
+            const uint32_t c[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const uint4 w = q[j];
-        const uint32_t c[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const uint32_t two = c[e] >> shift;  // this slot's codes of two channels
-            x[8 * j + 2 * e] = value_of(two & 15u, av);
-            x[8 * j + 2 * e + 1] = value_of((two >> 16) & 15u, av);
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t two = c[e] >> (4 * (in & 3));  // this slot's codes of two channels
+                x[8 * j + 2 * e] = value_of(two & 15u, av[t]);
+                x[8 * j + 2 * e + 1] = value_of((two >> 16) & 15u, av[t]);
+            }
         }
+        store16(ov, x);
     }
-    store16(ov, x);
 }
 
 // The few-token form: kLanes lanes a pair of slots (2 m, 2 m + 1) of one head.
@@ -319,13 +419,12 @@ __global__ void __launch_bounds__(128) append_few_kernel(const __grid_constant__
     for (int e = 0; e < 2; ++e) {
         const int slot = slot0 + e, i = slot - start;
         live[e] = pg >= 0 && slot >= start && slot < end;
-        float xk[16], xv[16];
-#pragma unroll
-        for (int j = 0; j < 16; ++j)
-            xk[j] = xv[j] = 0.0f;
+        Row16<T> xk, xv;
+        xk.clear();
+        xv.clear();
         if (live[e]) {
-            load16(row_of<T>(a.k, a.ks, b, i, h) + 16 * part, xk);
-            load16(row_of<T>(a.v, a.vs, b, i, h) + 16 * part, xv);
+            xk.load(row_of<T>(a.k, a.ks, b, i, h) + 16 * part);
+            xv.load(row_of<T>(a.v, a.vs, b, i, h) + 16 * part);
         }
         uint32_t ck[4];
         const uint32_t ak = quantise<kLanes>(xk, ck);
@@ -417,7 +516,8 @@ cudaError_t launch_read_rows(const StoreArgs &a, int B, cudaStream_t s)
         const unsigned blocks = (unsigned)(((int64_t)a.c.heads * a.n * (D / 16) + 127) / 128);
         return launch(read_few_kernel<T, D>, dim3(blocks, B), dim3(128), 0, s, true, a);
     }
-    return launch(read_kernel<T, D>, dim3(pieces(a.n), a.c.heads, B), dim3(2 * D), 0, s, true, a);
+    return launch(read_kernel<T, D>,
+                  dim3((pieces(a.n) + kReadTiles - 1) / kReadTiles, a.c.heads, B), dim3(2 * D), 0, s, true, a);
 }
 
 template <typename T>
