@@ -1,8 +1,9 @@
 // cache_attention.cu -- fdllm_cache_attention: a block's queries over the 4-bit prefix cache
 // and the block's own keys, on the fifth-generation tensor cores.
 //
-// Mathematics.  With k_j = ko_j + ks_j u_j (u_j the codes) and likewise v_j, for the rows r of
-// one key/value head (queries x heads of the group):
+// Mathematics.  With k_j = ko_j + ks_j u_j (u_j the codes) and v_j = vo_j + vs_j w_j (w_j the
+// codes less 8, vo_j the middle of the range), for the rows r of one key/value head (queries x
+// heads of the group):
 //   s_rj = scale (ks_j (q_r . u_j) + ko_j sum(q_r)),
 //   out_r = (sum_j p_rj vs_j w_j + sum_j p_rj vo_j) / sum_j p_rj,   p_rj = e^(s_rj - m_r).
 // The tensor cores see the codes themselves, exact in fp16; scales and offsets act on the
@@ -705,7 +706,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {  // 32 slots
                             uint32_t y[16];
-                            unpack32(lds4(at + v_piece[i]), y);
+                            unpack32_centred(lds4(at + v_piece[i]), y);
                             tmem_st16(tV + 16 * i, y);
                         }
                 } else {
@@ -801,7 +802,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                         ks = bf16_low(fk) * k_factor;
                         ko = bf16_high(fk) * a.scale;
                         vs = bf16_low(fv);
-                        vo = bf16_high(fv);
+                        vo = fmaf(8.0f, vs, bf16_high(fv));
                         if (!valid)
                             ks = ko = vs = vo = 0.0f;
                     }
