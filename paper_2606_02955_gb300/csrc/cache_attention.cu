@@ -82,15 +82,21 @@ template <int D_, int N_>
 struct Shape {
     static constexpr int D = D_;
     static constexpr int N = N_;                       // rows of a row tile
-    static constexpr int C = N / 16;     // warpgroups sharing a tile's columns
+    static constexpr int C = N <= 32 ? N / 16 : N / 32;  // warpgroups sharing a tile's columns
     static constexpr int cols = N / C;                 // columns (rows of the problem) a thread
     static constexpr int w_warps = 4 * C;              // warps that make weights
-    static constexpr int w_threads = 32 * w_warps;
     static constexpr int w_first = 4;                  // (warps 0 to 3 unpack)
     static constexpr int loader = w_first + w_warps;
     static constexpr int issuer = loader + 1;
-    static constexpr int threads = 32 * (issuer + 1);
+    static constexpr int threads = 32 * (loader + 4);  // (two warps of the last group idle)
     static constexpr int ctas = N >= 64 ? 1 : 2;       // CTAs an SM holds
+    // Registers of a thread, by warpgroup: what the launch gives every thread is dealt out
+    // again, the weights' warps taking what the others leave.
+    static constexpr int regs = 65536 / (ctas * threads) / 8 * 8;
+    static constexpr int u_regs = N == 32 ? 40 : 48, l_regs = u_regs;
+    static constexpr int w_regs = (regs * (C + 2) - u_regs - l_regs) / C / 8 * 8;
+    static_assert(C * w_regs + u_regs + l_regs <= regs * (C + 2) && w_regs >= regs &&
+                  u_regs <= regs && l_regs <= regs, "no more than the launch's");
     static constexpr int bufs = ctas == 1 ? 2 : 1;       // of unpacked keys, and of values
     static constexpr int stages = ctas == 1 ? 8 : 4;
     // own keys come 32 to a stage; a block's 32 fill one tile, long prompts whole ones
@@ -115,25 +121,24 @@ struct Shape {
 
 __device__ uint32_t g_status;  // sticky: a bounded wait gave up
 
-// 32 own values of one channel (rows `step` apart in shared memory), as pairs in the operand's
+// Eight own values of one channel (rows `step` apart in shared memory), as pairs in the operand's
 // order; keys from `n` on are 0.  A non-finite value must not meet the zero weights of the rows
 // that do not see it: it is taken out, and the first such key returned for the rows that do.
 template <typename T>
-__device__ __forceinline__ int own_values(const T *v, int step, int n, uint32_t (&y)[16])
+__device__ __forceinline__ int own_values(const T *v, int step, int n, uint32_t (&y)[4])
 {
     constexpr uint32_t kExp = std::is_same<T, __half>::value ? 0x7C00u : 0x7F80u;
     const uint16_t *u = reinterpret_cast<const uint16_t *>(v);
-    int bad = 32;
+    int bad = 8;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-        const int x = (e >> 2) * 8 + (e & 3);  // and four further on
+    for (int x = 0; x < 4; ++x) {  // and four further on
         uint32_t lo = x < n ? u[x * step] : 0u;
         uint32_t hi = x + 4 < n ? u[(x + 4) * step] : 0u;
         if ((lo & kExp) == kExp)
             bad = min(bad, x), lo = 0;
         if ((hi & kExp) == kExp)
             bad = min(bad, x + 4), hi = 0;
-        y[e] = lo | (hi << 16);
+        y[x] = lo | (hi << 16);
     }
     return bad;
 }
@@ -240,7 +245,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
         kSDone = kSegEmpty + 2, kODone = kSDone + 2, kKReady = kODone + 2, kVReady = kKReady + 2,
         kPReady = kVReady + 2, kBars
     };
-    enum { kBarW = 1, kBarU };  // CTA barriers: the weights' warps, the unpacking warps
+    enum { kBarU = 1, kBarW };  // CTA barriers: the unpacking warps, each warpgroup of weights
     __shared__ __align__(8) uint64_t bars[kBars];
     __shared__ uint32_t tmem_base;
     __shared__ int64_t scan[S::threads / 32];
@@ -332,22 +337,24 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
     auto bar = [&](int i) { return bar0 + 8u * i; };
     bool dead = false;  // a wait gave up: no further wait, the walk goes on to its end
     auto wait = [&](int i, uint32_t parity) {
-        if (!dead && !mbar_wait_at<0>(bar(i), parity, a.status))
+        if (!dead && !mbar_wait_at<0>(bar(i), parity))
             dead = true;
     };
     auto wait_u = [&](int i, uint32_t parity) {
-        if (!dead && !mbar_wait_at<20>(bar(i), parity, a.status))
+        if (!dead && !mbar_wait_at<20>(bar(i), parity))
             dead = true;
     };
     // the same for a whole warp that waits most of its time
     auto wait_warp = [&](auto sleep, int i, uint32_t parity) {
-        if (!dead && !mbar_wait_at<decltype(sleep)::value>(bar(i), parity, a.status))
+        if (!dead && !mbar_wait_at<decltype(sleep)::value>(bar(i), parity))
             dead = true;
         dead = __any_sync(0xFFFFFFFFu, dead);
     };
     using Long = std::integral_constant<int, 100>;
     using Now = std::integral_constant<int, 0>;
 
+    if (warp >= S::loader)
+        reg_dec<S::l_regs>();
     if (warp == S::loader) {
         // ---------------------------------------------------------------- the loading warp
         if (w.at < w.end) {
@@ -482,8 +489,9 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
         __syncwarp();
         for (uint32_t i = 0; i < min(ring, (uint32_t)S::stages); ++i) {
             const uint32_t r = ring - 1 - i;
-            mbar_wait_at<100>(bar(kFull + r % S::stages), (r / S::stages) & 1, a.status,
-                              dead ? kDrainLimitNs : kWaitLimitNs);
+            if (!mbar_wait_at<100>(bar(kFull + r % S::stages), (r / S::stages) & 1,
+                                   dead ? kDrainTries : kWaitTries))
+                dead = true;
         }
     } else if (warp == S::issuer) {
         // ---------------------------------------------------------------- the issuing warp
@@ -554,7 +562,10 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 }
             }
         }
+    } else if (warp > S::issuer) {
+        // nothing to do
     } else if (warp < S::w_first) {
+        reg_dec<S::u_regs>();
         // ---------------------------------------------------------------- the unpacking warps
         // Queries, keys and values into the tensor core's operands; a thread is a key of K and
         // a channel of V^T.
@@ -714,19 +725,21 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     for (int i = 0; i < used; ++i) {
                         const uint32_t r = ring + i, s1 = r % S::stages;
                         wait_u(kFull + (s1), (r / S::stages) & 1);
-                        if (D == 128 || d < D) {
-                            uint32_t y[16];
-                            const int bad = own_values<T>(
-                                reinterpret_cast<const T *>(smem + s1 * S::stage_bytes + S::own_v) +
-                                    d,
-                                D, keys - 32 * i, y);
-                            if (bad < 32) {
-                                first_bad[sb][d] =
-                                    min(first_bad[sb][d], (t - ct) * kOwnKeys + 32 * i + bad);
-                                any_bad[sb] = 1;
+                        if (D == 128 || d < D)
+#pragma unroll 1
+                            for (int j = 0; j < 32; j += 8) {
+                                uint32_t y[4];
+                                const int bad = own_values<T>(
+                                    reinterpret_cast<const T *>(smem + s1 * S::stage_bytes +
+                                                                S::own_v) + j * D + d,
+                                    D, keys - 32 * i - j, y);
+                                if (bad < 8) {
+                                    first_bad[sb][d] = min(first_bad[sb][d],
+                                                           (t - ct) * kOwnKeys + 32 * i + j + bad);
+                                    any_bad[sb] = 1;
+                                }
+                                tmem_st<4>(tV + 16 * i + j / 2, y);
                             }
-                            tmem_st16(tV + 16 * i, y);
-                        }
                     }
                 }
                 tmem_wait_st();
@@ -742,8 +755,10 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
             arrive(kSegEmpty + (sb), 1);
         }
     } else {
+        reg_inc<S::w_regs>();
         // ---------------------------------------------------------------- the weights
-        // A thread holds one key's scores of its columns.
+        // A thread holds one key's scores of its columns.  Each warpgroup has columns of its
+        // own, and waits for no other.
         const int wt = tid - 32 * S::w_first, ww = warp - S::w_first;  // thread, warp among these
         const int wg = ww >> 2, quarter = ww & 3, key = wt & 127;
         const int col0 = wg * kCols;  // this thread's columns
@@ -756,7 +771,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
         uint32_t ring = 0;    // stages used so far
         uint32_t seen = 0;    // tiles whose weights were given
         uint32_t summed = 0;  // tiles whose sums were waited for
-        auto sync = [&] { named_sync(kBarW, S::w_threads); };
+        auto sync = [&] { named_sync(kBarW + wg, 128); };
 
         for (uint32_t seg = 0;; ++seg) {
             const uint32_t sb = seg & 1;
@@ -946,7 +961,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     }
                     if (kOwn && t == from && from > begin)
                         scale_sums<kCols>(lanes + S::tO + col0, nullptr, kSumUnit);
-                    if (named_sync_or(kBarW, S::w_threads, over)) {
+                    if (__builtin_expect(named_sync_or(kBarW + wg, 128, over), 0)) {
                         // ---- the references move: per row, the running maxima of the scores
                         // and of the scores with the values' scale
                         const float lv = vs > 0.0f ? log2f(vs) : neg_inf_f();
@@ -967,28 +982,28 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                                 wred[ww][z][c8 + lane] = m[0];
                         }
                         sync();
-                        if (wt < N) {
-                            const int w4 = wt / kCols * 4, c = wt % kCols;
+                        if (key < kCols) {
+                            const int n = col0 + key, w4 = wg * 4, c = key;
                             float s4 = wred[w4][0][c], z4 = wred[w4][1][c];
 #pragma unroll
                             for (int i = 1; i < 4; ++i) {
                                 s4 = fmaxf(s4, wred[w4 + i][0][c]);
                                 z4 = fmaxf(z4, wred[w4 + i][1][c]);
                             }
-                            const float ref = -nref[wt];
+                            const float ref = -nref[n];
                             const float to_ref = fmaxf(ref, s4);
                             // where no value has a scale yet, refz follows at a distance
-                            const float z_old = refz[wt];
+                            const float z_old = refz[n];
                             const float to_z = fmaxf(fmaxf(z_old, z4), to_ref - kMaxShift);
                             // a row whose weights may have overflowed starts anew with this
                             // tile: what it held weighs less than 2^-60 of what it gets
                             const bool anew = to_ref - ref > kTopShift;
-                            redo[wt] = anew ? 1.0f : 0.0f;
-                            fl[wt] = anew ? 0.0f : exp2f(ref - to_ref);
-                            fo[wt] = exp2f(z_old - to_z);
-                            nref[wt] = -to_ref;
-                            refz[wt] = to_z;
-                            cmul[wt] = exp2f(to_ref - to_z);
+                            redo[n] = anew ? 1.0f : 0.0f;
+                            fl[n] = anew ? 0.0f : exp2f(ref - to_ref);
+                            fo[n] = exp2f(z_old - to_z);
+                            nref[n] = -to_ref;
+                            refz[n] = to_z;
+                            cmul[n] = exp2f(to_ref - to_z);
                         }
                         sync();
                         if (t > begin)  // the sums of the tiles before (waited for above)
@@ -1048,8 +1063,9 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
             sync();
             const bool whole = g.starts && g.ends;
             const bool poison = g.wrong || bad_page[sb];
-            if (wt < g.rows) {
-                const int w4 = wt / kCols * 4, c = wt % kCols;
+            const int n = col0 + key;  // a row of the first lanes
+            if (key < kCols && n < g.rows) {
+                const int w4 = wg * 4, c = key;
                 float sum = 0.0f, off = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -1059,27 +1075,27 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 if (poison)
                     sum = nan_f();
                 const bool none = !some || sum == 0.0f;
-                const float ref = none ? kFar : -nref[wt];
+                const float ref = none ? kFar : -nref[n];
                 const float f =
-                    none ? 0.0f : exp2f(refz[wt] - ref) * (g.last > g.ct ? 1.0f : kSumUnit);
+                    none ? 0.0f : exp2f(refz[n] - ref) * (g.last > g.ct ? 1.0f : kSumUnit);
                 if (whole) {
-                    const int r = g.r0 + wt, qi = r / a.group;
+                    const int r = g.r0 + n, qi = r / a.group;
                     const int64_t row =
                         ((int64_t)g.b * a.Lq + qi) * a.Hq + g.h * a.group + r - qi * a.group;
                     const float inv = none ? 0.0f : 1.0f / sum;
-                    row_at[wt] = row * D;
-                    fl[wt] = off * inv;
-                    fo[wt] = f * inv;
+                    row_at[n] = row * D;
+                    fl[n] = off * inv;
+                    fo[n] = f * inv;
                     if (a.lse)
                         a.lse[row] = none ? (poison ? nan_f() : neg_inf_f())
                                           : (ref + log2f(sum)) * 0.6931471805599453f;
                     if (poison)
-                        fl[wt] = nan_f();
+                        fl[n] = nan_f();
                 } else {
-                    const int64_t at = ((int64_t)blockIdx.x * 2 + (g.starts ? 1 : 0)) * N + wt;
-                    row_at[wt] = at * D;
-                    fl[wt] = off;
-                    fo[wt] = f;
+                    const int64_t at = ((int64_t)blockIdx.x * 2 + (g.starts ? 1 : 0)) * N + n;
+                    row_at[n] = at * D;
+                    fl[n] = off;
+                    fo[n] = f;
                     a.part_refs[2 * at] = ref;
                     a.part_refs[2 * at + 1] = sum;
                 }
@@ -1129,6 +1145,8 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 mbar_arrive(&bars[kSegEmpty + (sb)]);
         }
     }
+    if (dead)
+        atomicOr(a.status, kDevStatTimeout);
     tc::fence_before_sync();
     __syncthreads();
     tc::fence_after_sync();

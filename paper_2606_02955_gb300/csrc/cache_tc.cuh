@@ -190,6 +190,10 @@ __device__ __forceinline__ void tmem_st(uint32_t taddr, const uint32_t (&r)[NC])
 {
     if constexpr (NC == 16) {
         tmem_st16(taddr, r);
+    } else if constexpr (NC == 4) {
+        asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr),
+                     "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3])
+                     : "memory");
     } else {
         static_assert(NC == 8, "columns");
         asm volatile(
@@ -292,10 +296,14 @@ __device__ __forceinline__ void fence_async_smem()
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
 }
 
-// mbar_wait on a shared-memory address, for waits that are short as a rule: the timer, whose
-// reading alone costs about as much as a tile, is looked at only after many tries.  kSleepNs: a
-// warp that waits most of its time sleeps between tries, which would take issue slots from the
-// warps that work.
+// Waits on a shared-memory address, a few instructions each: many places of a kernel wait, and
+// code that does not fit the instruction cache costs its warps more than the waits (a wait with a
+// timer at each place: 5% of a block's attention).  The limit is a count of tries, of 20 ns at the
+// least and kSleepNs: a fraction of a second or more, where a wait takes microseconds.  kSleepNs: a warp
+// that waits most of its time sleeps between tries, which would take issue slots from the warps
+// that work.  False: given up; the caller waits no more, and says so in the status word.
+constexpr uint32_t kWaitTries = 1u << 23, kDrainTries = 1u << 20;
+
 __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
 {
     uint32_t done;
@@ -310,26 +318,17 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
 }
 
 template <int kSleepNs>
-__device__ __forceinline__ bool mbar_wait_at(uint32_t bar, uint32_t parity, uint32_t *status,
-                                             uint64_t limit_ns = kWaitLimitNs)
+__device__ __forceinline__ bool mbar_wait_at(uint32_t bar, uint32_t parity,
+                                             uint32_t tries = kWaitTries)
 {
-    uint64_t t0 = 0;
 #pragma unroll 1
-    for (uint32_t i = 1;; ++i) {
+    for (uint32_t i = 0; i < tries; ++i) {
         if (mbar_try(bar, parity))
             return true;
         if constexpr (kSleepNs > 0)
             __nanosleep(kSleepNs);
-        if ((i & 1023u) == 0) {
-            const uint64_t t = global_timer_ns();
-            if (t0 == 0) {
-                t0 = t;
-            } else if (t - t0 > limit_ns) {
-                atomicOr(status, kDevStatTimeout);
-                return false;
-            }
-        }
     }
+    return false;
 }
 
 // An arrival by the lanes where `who` holds (a predicate, not a branch).
@@ -381,15 +380,23 @@ __device__ __forceinline__ float max3(float a, float b, float c)
     return d;
 }
 
+// Registers of the threads of a warpgroup, all of whose warps say so: given back, and taken of
+// what the CTA's launch got for it (the groups' shares never add up to more than that).
+template <int N>
+__device__ __forceinline__ void reg_dec()
+{
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+template <int N>
+__device__ __forceinline__ void reg_inc()
+{
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
+
 // ---------------------------------------------------------------- barriers of some of a CTA's warps
 __device__ __forceinline__ void named_sync(int id, int threads)
 {
     asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
-}
-
-__device__ __forceinline__ void named_arrive(int id, int threads)
-{
-    asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
 
 __device__ __forceinline__ bool named_sync_or(int id, int threads, bool x)

@@ -157,7 +157,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
     auto bar = [&](int i) { return bar0 + 8u * i; };
     bool dead = false;  // a wait gave up: no further wait, the walk goes on to its end
     auto wait = [&](auto sleep, int i, uint32_t parity) {
-        if (!dead && !mbar_wait_at<decltype(sleep)::value>(bar(i), parity, a.status))
+        if (!dead && !mbar_wait_at<decltype(sleep)::value>(bar(i), parity))
             dead = true;
     };
     using Long = std::integral_constant<int, 100>;
@@ -236,8 +236,9 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
         // Nothing may land in this CTA's memory after it has gone.
         for (uint32_t i = 0; i < min(ring, (uint32_t)S::stages); ++i) {
             const uint32_t r = ring - 1 - i;
-            mbar_wait_at<100>(bar(kFull + r % S::stages), (r / S::stages) & 1, a.status,
-                              dead ? kDrainLimitNs : kWaitLimitNs);
+            if (!mbar_wait_at<100>(bar(kFull + r % S::stages), (r / S::stages) & 1,
+                                   dead ? kDrainTries : kWaitTries))
+                dead = true;
         }
     } else if (warp == S::issuer) {
         // ---------------------------------------------------------------- the issuing warp
@@ -438,6 +439,8 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 }
             }
     }
+    if (dead)
+        atomicOr(a.status, kDevStatTimeout);
     tc::fence_before_sync();
     __syncthreads();
     tc::fence_after_sync();
