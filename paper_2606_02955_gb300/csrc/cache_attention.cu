@@ -61,6 +61,7 @@ struct AttnArgs {
     const void *v_new;
     Strides3 ks, vs;
     int Ln;
+    int mapped;               // own keys and values come by tensor map
     const int32_t *new_lens;  // [B] or null
     int causal;
     float scale;              // times log2(e)
@@ -93,7 +94,7 @@ struct Shape {
     // Registers of a thread, by warpgroup: what the launch gives every thread is dealt out
     // again, the weights' warps taking what the others leave.
     static constexpr int regs = 65536 / (ctas * threads) / 8 * 8;
-    static constexpr int u_regs = N == 32 ? 40 : 48, l_regs = u_regs;
+    static constexpr int u_regs = N == 32 ? 40 : 64, l_regs = u_regs;
     static constexpr int w_regs = (regs * (C + 2) - u_regs - l_regs) / C / 8 * 8;
     static_assert(C * w_regs + u_regs + l_regs <= regs * (C + 2) && w_regs >= regs &&
                   u_regs <= regs && l_regs <= regs, "no more than the launch's");
@@ -103,8 +104,8 @@ struct Shape {
     static constexpr int own_keys = N >= 64 ? 128 : 32;
     static constexpr int code_bytes = kKeys * D / 2;   // of keys, or of values
     static constexpr int stage_bytes = 2 * code_bytes + 1024;
-    static constexpr int own_row = 2 * D + 16;         // a stage's own keys: rows apart in banks
-    static constexpr int own_v = 32 * own_row;
+    // a stage's own keys: 64 channels of 32 rows each, their pieces swizzled by row; then values
+    static constexpr int own_v = 64 * D;
     static constexpr int q_bytes = N * D * 2;
     static constexpr int q16_off = stages * stage_bytes;  // queries for codes, in fp16
     static constexpr int qt_off = q16_off + q_bytes;      // queries for own keys, as they are
@@ -231,7 +232,9 @@ template <typename S, typename T>
 __global__ void __launch_bounds__(S::threads, S::ctas)
     attention_kernel(const __grid_constant__ AttnArgs a,
                      const __grid_constant__ CUtensorMap k_map,
-                     const __grid_constant__ CUtensorMap v_map)
+                     const __grid_constant__ CUtensorMap v_map,
+                     const __grid_constant__ CUtensorMap kn_map,
+                     const __grid_constant__ CUtensorMap vn_map)
 {
     constexpr int D = S::D, N = S::N, kCols = S::cols, kOwnKeys = S::own_keys;
     extern __shared__ uint8_t smem_raw[];
@@ -286,6 +289,10 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
     if (warp == S::loader && lane == 0) {
         tc::prefetch_tensormap(&k_map);
         tc::prefetch_tensormap(&v_map);
+        if (a.mapped) {
+            tc::prefetch_tensormap(&kn_map);
+            tc::prefetch_tensormap(&vn_map);
+        }
     }
     pdl_wait();
 
@@ -467,18 +474,33 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     const int n = min(32, j1 - j0);
                     if (dead)
                         continue;
-                    if (lane == 0)
-                        mbar_arrive_expect_tx(&bars[kFull + st], (uint32_t)n * D * 4);
-                    __syncwarp();
-                    if (lane < n) {
-                        bulk_copy_g2s(buf + lane * S::own_row,
-                                      static_cast<const T *>(a.k_new) + w.b * a.ks.batch +
-                                          (int64_t)(j0 + lane) * a.ks.token + (int64_t)h * a.ks.head,
-                                      D * 2, &bars[kFull + st]);
-                        bulk_copy_g2s(buf + S::own_v + lane * (D * 2),
-                                      static_cast<const T *>(a.v_new) + w.b * a.vs.batch +
-                                          (int64_t)(j0 + lane) * a.vs.token + (int64_t)h * a.vs.head,
-                                      D * 2, &bars[kFull + st]);
+                    if (a.mapped) {
+                        if (lane == 0) {
+                            mbar_arrive_expect_tx(&bars[kFull + st], 32 * D * 4);
+#pragma unroll
+                            for (int i = 0; i < D / 64; ++i)
+                                tma_load_4d(buf + i * 4096, &kn_map, 64 * i, h, j0, w.b,
+                                            &bars[kFull + st]);
+                            tma_load_4d(buf + S::own_v, &vn_map, 0, h, j0, w.b, &bars[kFull + st]);
+                        }
+                    } else {  // rows that repeat: as a map would lay them out
+                        if (lane == 0)
+                            mbar_arrive_expect_tx(&bars[kFull + st], (uint32_t)n * D * 4);
+                        __syncwarp();
+                        if (lane < n) {
+                            const T *k = static_cast<const T *>(a.k_new) + w.b * a.ks.batch +
+                                         (int64_t)(j0 + lane) * a.ks.token + (int64_t)h * a.ks.head;
+#pragma unroll 1
+                            for (int i = 0; i < D / 8; ++i)
+                                bulk_copy_g2s(buf + (i >> 3) * 4096 + lane * 128 +
+                                                  (((i & 7) ^ (lane & 7)) << 4),
+                                              k + 8 * i, 16, &bars[kFull + st]);
+                            bulk_copy_g2s(buf + S::own_v + lane * (D * 2),
+                                          static_cast<const T *>(a.v_new) + w.b * a.vs.batch +
+                                              (int64_t)(j0 + lane) * a.vs.token +
+                                              (int64_t)h * a.vs.head,
+                                          D * 2, &bars[kFull + st]);
+                        }
                     }
                     __syncwarp();
                 }
@@ -691,12 +713,13 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                         const uint32_t r = ring + warp, s1 = r % S::stages;
                         wait_u(kFull + (s1), (r / S::stages) & 1);
                         tc::fence_after_sync();
-                        const uint8_t *row = smem + s1 * S::stage_bytes + lane * S::own_row;
+                        const uint8_t *row = smem + s1 * S::stage_bytes + lane * 128;
 #pragma unroll 1
                         for (int v = 0; v < D / 8; ++v) {
                             uint4 x = make_uint4(0, 0, 0, 0);
                             if (key < keys)
-                                x = interleave8(*reinterpret_cast<const uint4 *>(row + 16 * v));
+                                x = interleave8(*reinterpret_cast<const uint4 *>(
+                                    row + (v >> 3) * 4096 + (((v & 7) ^ (lane & 7)) << 4)));
                             const uint32_t y[4] = {x.x, x.y, x.z, x.w};
                             tmem_st<4>(tK + 4 * v, y);
                         }
@@ -1272,15 +1295,14 @@ Workspace workspace_of(int grid, int N, int D)
 int full_grid(int N) { return sm_count() * (N >= 64 ? 1 : 2); }
 
 template <typename S, typename T>
-cudaError_t run(const AttnArgs &a, int grid, const CUtensorMap &k_map, const CUtensorMap &v_map,
-                cudaStream_t s)
+cudaError_t run(const AttnArgs &a, int grid, const CUtensorMap (&maps)[4], cudaStream_t s)
 {
     static const cudaError_t ready = cudaFuncSetAttribute(
         attention_kernel<S, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::smem);
     if (ready != cudaSuccess)
         return ready;
     cudaError_t e = launch(attention_kernel<S, T>, dim3(grid), dim3(S::threads), S::smem, s, true,
-                           a, k_map, v_map);
+                           a, maps[0], maps[1], maps[2], maps[3]);
     if (e != cudaSuccess)
         return e;
     return launch(combine_kernel<T, S::D>, dim3(grid, (S::N + kJoinWarps - 1) / kJoinWarps),
@@ -1288,12 +1310,12 @@ cudaError_t run(const AttnArgs &a, int grid, const CUtensorMap &k_map, const CUt
 }
 
 template <int D, typename T>
-cudaError_t run_rows(const AttnArgs &a, int N, int grid, const CUtensorMap &k, const CUtensorMap &v,
+cudaError_t run_rows(const AttnArgs &a, int N, int grid, const CUtensorMap (&maps)[4],
                      cudaStream_t s)
 {
-    return N == 16   ? run<Shape<D, 16>, T>(a, grid, k, v, s)
-           : N == 32 ? run<Shape<D, 32>, T>(a, grid, k, v, s)
-                     : run<Shape<D, 64>, T>(a, grid, k, v, s);
+    return N == 16   ? run<Shape<D, 16>, T>(a, grid, maps, s)
+           : N == 32 ? run<Shape<D, 32>, T>(a, grid, maps, s)
+                     : run<Shape<D, 64>, T>(a, grid, maps, s);
 }
 
 }  // namespace
@@ -1401,17 +1423,20 @@ fdllm_status fdllm_cache_attention(const void *q, const int64_t *q_strides, int 
     if ((int64_t)a.c.heads * a.row_tiles < most && (int64_t)a.c.heads * a.row_tiles * B < most)
         bound = (int64_t)a.c.heads * a.row_tiles * B * tiles;
     const int grid = (int)(bound < most ? bound : most);
-    CUtensorMap k_map, v_map;
+    CUtensorMap maps[4] = {};  // the cache's keys and values, the block's own
     a.status = cache_status_word();
-    if (!a.status || !make_cache_maps(a.c, &k_map, &v_map))
+    if (!a.status || !make_cache_maps(a.c, &maps[0], &maps[1]))
         return FDLLM_ERR_CUDA;
+    a.mapped = Ln > 0 &&
+               make_rows_map(&maps[2], k_new, a.ks, B, Ln, a.c.heads, D, 64, true) &&
+               make_rows_map(&maps[3], v_new, a.vs, B, Ln, a.c.heads, D, D, false);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool bf = dtype == FDLLM_BF16;
     const cudaError_t e =
-        D == 128 ? (bf ? run_rows<128, __nv_bfloat16>(a, N, grid, k_map, v_map, s)
-                       : run_rows<128, __half>(a, N, grid, k_map, v_map, s))
-                 : (bf ? run_rows<64, __nv_bfloat16>(a, N, grid, k_map, v_map, s)
-                       : run_rows<64, __half>(a, N, grid, k_map, v_map, s));
+        D == 128 ? (bf ? run_rows<128, __nv_bfloat16>(a, N, grid, maps, s)
+                       : run_rows<128, __half>(a, N, grid, maps, s))
+                 : (bf ? run_rows<64, __nv_bfloat16>(a, N, grid, maps, s)
+                       : run_rows<64, __half>(a, N, grid, maps, s));
     return e == cudaSuccess ? FDLLM_OK : FDLLM_ERR_CUDA;
 }
 

@@ -11,24 +11,56 @@
 
 namespace fdllm {
 
-// Tensor maps of a cache's codes: keys as rows of D/2 bytes, one box a page's (or a tile's)
-// slots; values as rows of page/2 bytes, one box D channels of up to 128 slots.  The swizzle
-// follows the box's row, so that 16-byte reads of one row a thread meet no bank twice.
-inline bool make_cache_maps(const CacheView &c, CUtensorMap *k, CUtensorMap *v)
+using EncodeFn = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *,
+                              const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                              const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+inline EncodeFn encode_tiled()
 {
-    using Fn = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *,
-                            const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
-                            const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
-                            CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-    static const Fn encode = [] {
+    static const EncodeFn encode = [] {
         void *p = nullptr;
         cudaDriverEntryPointQueryResult q;
         if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000,
                                              cudaEnableDefault, &q) != cudaSuccess ||
             q != cudaDriverEntryPointSuccess)
-            return (Fn) nullptr;
-        return reinterpret_cast<Fn>(p);
+            return (EncodeFn) nullptr;
+        return reinterpret_cast<EncodeFn>(p);
     }();
+    return encode;
+}
+
+// Tensor map of rows [B, tokens, heads, D] of 16-bit values: one box `box_inner` channels of 32
+// tokens of a head, swizzled where they are 64.  False where a map cannot hold the strides (an
+// axis of several that repeats one row).
+inline bool make_rows_map(CUtensorMap *m, const void *base, const Strides3 &s, int B, int tokens,
+                          int heads, int D, int box_inner, bool swizzle)
+{
+    const EncodeFn encode = encode_tiled();
+    const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)heads, (cuuint64_t)tokens, (cuuint64_t)B};
+    cuuint64_t strides[3];
+    const int64_t elements[3] = {s.head, s.token, s.batch};
+    for (int i = 0; i < 3; ++i) {
+        const int64_t e = dims[i + 1] == 1 ? D : elements[i];
+        if (e <= 0 || e >= ((int64_t)1 << 38))
+            return false;
+        strides[i] = 2 * (cuuint64_t)e;
+    }
+    const cuuint32_t box[4] = {(cuuint32_t)box_inner, 1, 32, 1};
+    const cuuint32_t unit[4] = {1, 1, 1, 1};
+    return encode && encode(m, CU_TENSOR_MAP_DATA_TYPE_UINT16, 4, const_cast<void *>(base), dims,
+                            strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                            swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+                            CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Tensor maps of a cache's codes: keys as rows of D/2 bytes, one box a page's (or a tile's)
+// slots; values as rows of page/2 bytes, one box D channels of up to 128 slots.  The swizzle
+// follows the box's row, so that 16-byte reads of one row a thread meet no bank twice.
+inline bool make_cache_maps(const CacheView &c, CUtensorMap *k, CUtensorMap *v)
+{
+    const EncodeFn encode = encode_tiled();
     if (!encode)
         return false;
     const int page = 1 << c.page_shift, span = page < 128 ? page : 128;
@@ -53,6 +85,16 @@ inline bool make_cache_maps(const CacheView &c, CUtensorMap *k, CUtensorMap *v)
 }
 
 #ifdef __CUDACC__
+
+__device__ __forceinline__ void tma_load_4d(void *dst, const CUtensorMap *map, int32_t x, int32_t y,
+                                            int32_t z, int32_t w, uint64_t *bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(smem_addr(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_addr(bar))
+        : "memory");
+}
 
 // ---------------------------------------------------------------- packed fp32 pairs
 __device__ __forceinline__ uint64_t f2(float lo, float hi)
