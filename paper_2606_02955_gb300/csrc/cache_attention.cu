@@ -47,6 +47,7 @@ constexpr float kFar = -1e30f;            // reference of a row that has seen no
 constexpr float kTopWeight = 16384.0f;    // largest weight (fp16 holds 65504)
 constexpr float kTopShift = 90.0f;        // a score this far above its reference may overflow
 constexpr float kMaxShift = 120.0f;       // c = 2^(ref - refz) stays below 2^120
+constexpr int kNever = 0x7FFFFFFF;
 constexpr float kSumUnit = 1048576.0f;    // sums over codes come in units of 2^-20
 
 struct AttnArgs {
@@ -161,7 +162,7 @@ __device__ __forceinline__ void scale_sums(uint32_t taddr, const float *f, float
 }
 
 // A unit's beginning and end cost about as much as this many tiles.
-constexpr int kUnitCost = 3;
+constexpr int kUnitCost = 7;
 
 // One sequence's share of the work.
 struct Sequence {
@@ -267,8 +268,11 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
     __shared__ __align__(16) float rowf[kRowFloats];
     float *const nref = rowf + kNref, *const cmul = rowf + kCmul, *const refz = rowf + kRefz;
     float *const fl = rowf + kFl, *const fo = rowf + kFo, *const redo = rowf + kRedo;
-    __shared__ int64_t row_at[N];
-    __shared__ float wred[S::w_warps][2][kCols];
+    // by the segment's parity: where a row's results go (in rows of D), their factors (of the
+    // sums, and added), and sums of each warp's keys
+    __shared__ int64_t row_at[2][N];
+    __shared__ float2 fin[2][N];
+    __shared__ float wred[2][S::w_warps][2][kCols];
 
     const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31;
     if (tid == 0) {
@@ -395,8 +399,18 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     g.wrong = w.s.wrong;
                     bad_page[sb] = 0;
                 }
-                mbar_arrive(&bars[kSegFull + (sb)]);
             }
+            if (more) {
+                const bool starts = w.first == 0, whole = starts && w.last == w.s.tiles;
+                for (int n = lane; n < rows; n += 32) {
+                    const int qi = (r0 + n) / a.group, j = (r0 + n) - qi * a.group;
+                    row_at[sb][n] = whole ? ((int64_t)w.b * a.Lq + qi) * a.Hq + h * a.group + j
+                                          : ((int64_t)blockIdx.x * 2 + starts) * N + n;
+                }
+            }
+            __syncwarp();
+            if (lane == 0)
+                mbar_arrive(&bars[kSegFull + (sb)]);
             __syncwarp();
             if (!more)
                 break;
@@ -629,7 +643,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 const uint8_t *raw = smem + st * S::stage_bytes;
                 constexpr int kMine = N * (D / 8) / 128;
                 float big = 0.0f;
-#pragma unroll 2
+#pragma unroll 1
                 for (int m = 0; m < kMine; ++m) {
                     const int i = tid + m * 128, n = i / (D / 8), c8 = i % (D / 8);
                     uint4 x = make_uint4(0, 0, 0, 0);
@@ -656,7 +670,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 if (lane == 0)
                     q_big[warp] = __uint_as_float(wbig);
                 if (tid < D)
-                    first_bad[sb][tid] = 0x7FFFFFFF;
+                    first_bad[sb][tid] = kNever;
                 if (tid == 0)
                     any_bad[sb] = 0;
                 named_sync(kBarU, 128);
@@ -668,7 +682,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 // the operands' last readers are done: the scores of the tile before
                 if (tile > 0)
                     wait_u(kSDone + ((tile - 1) & 1), ((tile - 1) >> 1) & 1);
-#pragma unroll 2
+#pragma unroll 1
                 for (int m = 0; m < kMine; ++m) {
                     const int i = tid + m * 128, n = i / (D / 8), c8 = i % (D / 8);
                     uint4 x = make_uint4(0, 0, 0, 0);
@@ -860,7 +874,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     const int first_col = !valid || (kOwn && a.causal && j >= a.Lq) ? kCols
                                           : kOwn && a.causal ? j * a.group - (g.r0 + col0)
                                                              : 0;
-                    if (t == begin) {
+                    if (__builtin_expect(t == begin, 0)) {
                         // ---- the references: the largest score of the tile's first 32 keys
                         // that the row sees, with the largest scale of their values
                         if (quarter == 0) {
@@ -1012,16 +1026,16 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                             }
                             warp_columns<8>(m, [](float x, float y) { return fmaxf(x, y); });
                             if (lane < 8)
-                                wred[ww][z][c8 + lane] = m[0];
+                                wred[sb][ww][z][c8 + lane] = m[0];
                         }
                         sync();
                         if (key < kCols) {
                             const int n = col0 + key, w4 = wg * 4, c = key;
-                            float s4 = wred[w4][0][c], z4 = wred[w4][1][c];
+                            float s4 = wred[sb][w4][0][c], z4 = wred[sb][w4][1][c];
 #pragma unroll
                             for (int i = 1; i < 4; ++i) {
-                                s4 = fmaxf(s4, wred[w4 + i][0][c]);
-                                z4 = fmaxf(z4, wred[w4 + i][1][c]);
+                                s4 = fmaxf(s4, wred[sb][w4 + i][0][c]);
+                                z4 = fmaxf(z4, wred[sb][w4 + i][1][c]);
                             }
                             const float ref = -nref[n];
                             const float to_ref = fmaxf(ref, s4);
@@ -1091,7 +1105,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     un2(z ? pm2[c] : l2[c], x[2 * c], x[2 * c + 1]);
                 warp_columns<kCols>(x, [](float u, float v) { return u + v; });
                 if (lane < kCols)
-                    wred[ww][z][lane] = x[0];
+                    wred[sb][ww][z][lane] = x[0];
             }
             sync();
             const bool whole = g.starts && g.ends;
@@ -1102,8 +1116,8 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 float sum = 0.0f, off = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    sum += wred[w4 + i][0][c];
-                    off += wred[w4 + i][1][c];
+                    sum += wred[sb][w4 + i][0][c];
+                    off += wred[sb][w4 + i][1][c];
                 }
                 if (poison)
                     sum = nan_f();
@@ -1112,23 +1126,14 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 const float f =
                     none ? 0.0f : exp2f(refz[n] - ref) * (g.last > g.ct ? 1.0f : kSumUnit);
                 if (whole) {
-                    const int r = g.r0 + n, qi = r / a.group;
-                    const int64_t row =
-                        ((int64_t)g.b * a.Lq + qi) * a.Hq + g.h * a.group + r - qi * a.group;
                     const float inv = none ? 0.0f : 1.0f / sum;
-                    row_at[n] = row * D;
-                    fl[n] = off * inv;
-                    fo[n] = f * inv;
+                    fin[sb][n] = make_float2(f * inv, poison ? nan_f() : off * inv);
                     if (a.lse)
-                        a.lse[row] = none ? (poison ? nan_f() : neg_inf_f())
+                        a.lse[row_at[sb][n]] = none ? (poison ? nan_f() : neg_inf_f())
                                           : (ref + log2f(sum)) * 0.6931471805599453f;
-                    if (poison)
-                        fl[n] = nan_f();
                 } else {
-                    const int64_t at = ((int64_t)blockIdx.x * 2 + (g.starts ? 1 : 0)) * N + n;
-                    row_at[n] = at * D;
-                    fl[n] = off;
-                    fo[n] = f;
+                    const int64_t at = row_at[sb][n];
+                    fin[sb][n] = make_float2(f, off);
                     a.part_refs[2 * at] = ref;
                     a.part_refs[2 * at + 1] = sum;
                 }
@@ -1150,30 +1155,35 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
             tc::fence_after_sync();
             sync();
             const int d = key;
-            const int bad = some && any_bad[sb] ? first_bad[sb][min(d, D - 1)] : 0x7FFFFFFF;
+            const int bad = some && any_bad[sb] ? first_bad[sb][min(d, D - 1)] : kNever;
+            const int rows = g.rows;
 #pragma unroll 1
             for (int c8 = 0; c8 < kCols; c8 += 8) {
                 uint32_t o[8] = {0, 0, 0, 0, 0, 0, 0, 0};
                 if (some)
                     tmem_ld<8>(lanes + S::tO + col0 + c8, o);
+                if (D == 64 && quarter >= 2)
+                    continue;
                 if (D == 128 || d < D)
 #pragma unroll
                     for (int c = 0; c < 8; ++c) {
                         const int n = col0 + c8 + c;
-                        if (n < g.rows) {
-                            float x = fmaf(__uint_as_float(o[c]), fo[n], fl[n]);
-                            if (bad != 0x7FFFFFFF && (!a.causal || bad <= (g.r0 + n) / a.group))
+                        if (n < rows) {
+                            const float2 f = fin[sb][n];
+                            float x = fmaf(__uint_as_float(o[c]), f.x, f.y);
+                            if (bad != kNever && (!a.causal || bad <= (g.r0 + n) / a.group))
                                 x = nan_f();
+                            const int64_t at = row_at[sb][n] * D + d;
                             if (whole)
-                                static_cast<T *>(a.out)[row_at[n] + d] = from_float<T>(x);
+                                static_cast<T *>(a.out)[at] = from_float<T>(x);
                             else
-                                a.parts[row_at[n] + d] = x;
+                                a.parts[at] = x;
                         }
                     }
             }
+            // (what the next segment overwrites is by parity, or read no more)
             tc::fence_before_sync();
-            sync();  // the next segment overwrites the references and its sums
-            tc::fence_after_sync();
+            __syncwarp();
             if (lane == 0)
                 mbar_arrive(&bars[kSegEmpty + (sb)]);
         }
