@@ -1,9 +1,9 @@
 // cache_attention.cu -- fdllm_cache_attention: a block's queries over the 4-bit prefix cache
 // and the block's own keys, on the fifth-generation tensor cores.
 //
-// Mathematics.  With k_j = ko_j + ks_j u_j (u_j the codes) and v_j = vo_j + vs_j w_j (w_j the
-// codes less 8, vo_j the middle of the range), for the rows r of one key/value head (queries x
-// heads of the group):
+// Mathematics.  With k_j = ko_j + ks_j u_j and v_j = vo_j + vs_j w_j (u_j and w_j the codes less
+// a constant, which the offsets ko_j and vo_j make up for), for the rows r of one key/value head
+// (queries x heads of the group):
 //   s_rj = scale (ks_j (q_r . u_j) + ko_j sum(q_r)),
 //   out_r = (sum_j p_rj vs_j w_j + sum_j p_rj vo_j) / sum_j p_rj,   p_rj = e^(s_rj - m_r).
 // The tensor cores see the codes themselves, exact in fp16; scales and offsets act on the
@@ -48,7 +48,7 @@ constexpr float kTopWeight = 16384.0f;    // largest weight (fp16 holds 65504)
 constexpr float kTopShift = 90.0f;        // a score this far above its reference may overflow
 constexpr float kMaxShift = 120.0f;       // c = 2^(ref - refz) stays below 2^120
 constexpr int kNever = 0x7FFFFFFF;
-constexpr float kSumUnit = 1048576.0f;    // sums over codes come in units of 2^-20
+constexpr float kSumUnit = 1048576.0f;    // sums over values' codes come in units of 2^-20
 
 struct AttnArgs {
     CacheView c;
@@ -678,7 +678,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 const int e0 = query_exponent(big);
                 const float unit = __uint_as_float((uint32_t)(127 - e0) << 23);
                 if (tid == 0)
-                    q_unit[sb] = kCodeUnit * __uint_as_float((uint32_t)(127 + e0) << 23);
+                    q_unit[sb] = __uint_as_float((uint32_t)(127 + e0) << 23);
                 // the operands' last readers are done: the scores of the tile before
                 if (tile > 0)
                     wait_u(kSDone + ((tile - 1) & 1), ((tile - 1) >> 1) & 1);
@@ -762,7 +762,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
 #pragma unroll
                             for (int v = 0; v < 4; ++v) {  // 32 slots
                                 uint32_t y[16];
-                                unpack32_centred(lds4(at + v_piece[v]), y);
+                                unpack32_values(lds4(at + v_piece[v]), y);
                                 tmem_st16(tV + 16 * v, y);
                             }
                         tmem_wait_st();
@@ -862,9 +862,9 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                         const uint32_t f = buf0 + st * S::stage_bytes + 2 * S::code_bytes + 4 * key;
                         const uint32_t fk = lds1(f), fv = lds1(f + 4 * kKeys);
                         ks = bf16_low(fk) * k_factor;
-                        ko = bf16_high(fk) * a.scale;
+                        ko = fmaf(8.0f, bf16_low(fk), bf16_high(fk)) * a.scale;
                         vs = bf16_low(fv);
-                        vo = fmaf(8.0f, vs, bf16_high(fv));
+                        vo = fmaf(key & 1 ? 15.0f : 0.0f, vs, bf16_high(fv));
                         if (!valid)
                             ks = ko = vs = vo = 0.0f;
                     }

@@ -157,32 +157,43 @@ __device__ __forceinline__ void unpack2(uint32_t w, float &lo, float &hi)
 // Inside every group of eight, the contraction runs over elements 0 4 1 5 2 6 3 7: the order in
 // which masking a word of eight 4-bit codes yields pairs.
 //
-// A word's codes as four fp16 pairs, unconverted: four bits in a number's lowest places are the
-// subnormal code * 2^-24, exactly.  The codes of odd place are left in the next four bits, 16
-// times as much; the other operand makes up for both (a mask a pair, one shift a word; taking
-// the constant off a number with the code in its last places took twice as many instructions).
-constexpr float kCodeUnit = 16777216.0f;  // 2^24
+// A word's codes as four fp16 pairs, the codes of odd place 16 times as large; the other operand
+// makes up for that.
+//
+// Keys: each code less 8.  A code in the lowest places of 1024 (fp16's unit there is 1) makes
+// 1024 + code, or 1024 + 16 code, and 1032 or 1152 come off exactly.  Left where they lie, four
+// bits are the subnormals code * 2^-24, for half the instructions; but the tensor core lines its
+// products up by their exponents before it adds them, and subnormals lose as many places as they
+// lack: scores were off by 5e-6, ten times what fp32 sums of the same terms are.
 __device__ __forceinline__ void unpack32(const uint4 x, uint32_t (&y)[16])
 {
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        y[4 * i] = w[i] & 0x000F000Fu;
-        y[4 * i + 1] = w[i] & 0x00F000F0u;
-        y[4 * i + 2] = (w[i] >> 8) & 0x000F000Fu;
-        y[4 * i + 3] = (w[i] >> 8) & 0x00F000F0u;
+        y[4 * i] = (w[i] & 0x000F000Fu) | 0x64006400u;
+        y[4 * i + 1] = (w[i] & 0x00F000F0u) | 0x64006400u;
+        y[4 * i + 2] = ((w[i] >> 8) & 0x000F000Fu) | 0x64006400u;
+        y[4 * i + 3] = ((w[i] >> 8) & 0x00F000F0u) | 0x64006400u;
     }
-}
-
-// The same, less 8 (an exact sum of subnormals): for values, whose sums over tens of thousands of
-// keys would grow to a multiple of what is left of them after the offsets, and lose that much of
-// their 24 bits (of 32000 keys 2.4e-3 of the result; centred, what its rounding leaves).
-__device__ __forceinline__ void unpack32_centred(const uint4 x, uint32_t (&y)[16])
-{
-    unpack32(x, y);
 #pragma unroll
     for (int i = 0; i < 16; ++i)
-        asm("add.rn.f16x2 %0, %0, %1;" : "+r"(y[i]) : "r"(i & 1 ? 0x80808080u : 0x80088008u));
+        asm("sub.rn.f16x2 %0, %0, %1;" : "+r"(y[i]) : "r"(i & 1 ? 0x64806480u : 0x64086408u));
+}
+
+// Values: those subnormals (kSumUnit), whose sums are of weights in 11 bits anyway; codes of odd
+// place less 15, by their complement and the sign, so that sums over tens of thousands of keys do
+// not grow to a multiple of what the offsets leave of them (of 32000 keys 2.4e-3 of the result;
+// so 1.7e-3, which is what bf16 rounds).
+__device__ __forceinline__ void unpack32_values(const uint4 x, uint32_t (&y)[16])
+{
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        y[4 * i] = w[i] & 0x000F000Fu;
+        y[4 * i + 1] = (~w[i] & 0x00F000F0u) | 0x80008000u;
+        y[4 * i + 2] = (w[i] >> 8) & 0x000F000Fu;
+        y[4 * i + 3] = (~(w[i] >> 8) & 0x00F000F0u) | 0x80008000u;
+    }
 }
 
 // Eight 16-bit values in the same order.

@@ -25,6 +25,7 @@ namespace fdllm {
 namespace {
 
 constexpr int kKeys = 128;   // keys of a tile
+constexpr float kLog2eLow = 1.925963e-08f;  // log2(e) - kLog2e
 constexpr int kUnitCost = 1; // a segment's queries cost about as much as this many tiles
 
 struct WeighArgs {
@@ -95,7 +96,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
     __shared__ int64_t scan[S::threads / 32];
     __shared__ int64_t find_base;
     __shared__ int find_b;
-    __shared__ float q_big[4];
+    __shared__ float q_big[8];
     // of the queries held: sum of the channels; -lse in base 2 (-inf: the row counts nothing)
     __shared__ __align__(16) float sumq[S::group * N], nlse[S::group * N];
 
@@ -189,6 +190,81 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
         return false;
     };
     constexpr int kHeld = S::group * N;
+
+    // Rows [g0, g0 + held) of the queries into the operand, by the unpacking and the weighing
+    // warps together: as they are, with their sums and the largest, then in place times a power
+    // of two (the exponent of which is returned).  Their -lse lose the whole number `shift`, near
+    // all of them as a rule, so that the small differences of large scores keep their bits.
+    auto hold_queries = [&](int g0, int held, float &shift) -> int {
+        const int chunks = (held + N - 1) / N * N * (D / 8);  // of 8 channels
+        const auto place = [&](int i) {
+            const int r = i / (D / 8), c8 = i % (D / 8), m = r % N;
+            return smem + S::q_off + r / N * S::q_bytes + (c8 >> 3) * (N * 128) + m * 128 +
+                   (((c8 & 7) ^ (m & 7)) << 4);
+        };
+        named_sync(kBarW, 256);
+        float big = 0.0f;
+#pragma unroll 4
+        for (int i = tid; i < chunks; i += 256) {
+            const int r = i / (D / 8), c8 = i % (D / 8);
+            uint4 x = make_uint4(0, 0, 0, 0);
+            if (r < held) {
+                const int qi = (g0 + r) / a.group, g = (g0 + r) - qi * a.group;
+                x = *reinterpret_cast<const uint4 *>(
+                    static_cast<const T *>(a.q) + b * a.qs.batch + qi * a.qs.token +
+                    (int64_t)(h * a.group + g) * a.qs.head + 8 * c8);
+            }
+            *reinterpret_cast<uint4 *>(place(i)) = x;
+            const uint32_t xw[4] = {x.x, x.y, x.z, x.w};
+            float sum = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float lo, hi;
+                unpack2<T>(xw[e], lo, hi);
+                sum += lo + hi;
+                big = fmaxf(big, fabsf(lo) <= 3.4e38f ? fabsf(lo) : 0.0f);
+                big = fmaxf(big, fabsf(hi) <= 3.4e38f ? fabsf(hi) : 0.0f);
+            }
+#pragma unroll
+            for (int m = D / 16; m > 0; m >>= 1)
+                sum += __shfl_xor_sync(0xFFFFFFFFu, sum, m);
+            if (c8 == 0)
+                sumq[r] = sum;
+        }
+        const auto lse_of = [&](int r) {
+            const int qi = (g0 + r) / a.group, g = (g0 + r) - qi * a.group;
+            return a.lse[((int64_t)b * a.Lq + qi) * a.Hq + h * a.group + g];
+        };
+        const float l0 = lse_of(0);
+        shift = fabsf(l0) < 1e6f ? rintf(-l0 * kLog2e) : 0.0f;
+        for (int r = tid; r < kHeld; r += 256) {
+            float x = neg_inf_f();
+            if (r < held) {
+                const float l = lse_of(r);
+                if (l != neg_inf_f())  // log2(e) in two parts
+                    x = fmaf(-l, kLog2eLow, fmaf(-l, kLog2e, -shift));
+            }
+            nlse[r] = x;
+        }
+        const uint32_t wbig = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(big));
+        if (lane == 0)
+            q_big[warp] = __uint_as_float(wbig);
+        named_sync(kBarW, 256);
+        big = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            big = fmaxf(big, q_big[i]);
+        const int e0 = query_exponent(big);
+        const float unit = __uint_as_float((uint32_t)(127 - e0) << 23);
+#pragma unroll 4
+        for (int i = tid; i < chunks; i += 256) {
+            uint4 *x = reinterpret_cast<uint4 *>(place(i));
+            *x = code_queries<T>(*x, unit);
+        }
+        fence_async_smem();
+        named_sync(kBarW, 256);
+        return e0;
+    };
     const int page = 1 << a.c.page_shift;
     const int span = min(page, kKeys);  // slots of a page in a tile
 
@@ -278,69 +354,11 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
         uint32_t ring = 0;  // key tiles so far
         while (next())
             for (int g0 = 0; g0 < a.rows; g0 += kHeld) {
-                const int held = min(kHeld, a.rows - g0);
-                // ---- the group's queries; the products that read the ones before are done, and
-                // their sums are (kBarW, with the weighing warps)
+                // the products that read the queries before are done
                 if (ring > 0)
                     wait(Short{}, kKFree, (ring - 1) & 1);
-                named_sync(kBarW, 256);
-                float big = 0.0f;
-                const int chunks = (held + N - 1) / N * N * (D / 8);
-                const auto chunk = [&](int i) {
-                    const int r = i / (D / 8), c8 = i % (D / 8);
-                    uint4 x = make_uint4(0, 0, 0, 0);
-                    if (r < held) {
-                        const int qi = (g0 + r) / a.group, g = (g0 + r) - qi * a.group;
-                        x = *reinterpret_cast<const uint4 *>(
-                            static_cast<const T *>(a.q) + b * a.qs.batch + qi * a.qs.token +
-                            (int64_t)(h * a.group + g) * a.qs.head + 8 * c8);
-                    }
-                    return x;
-                };
-#pragma unroll 4
-                for (int i = tid; i < chunks; i += 128) {
-                    const uint4 x = chunk(i);
-                    const uint32_t xw[4] = {x.x, x.y, x.z, x.w};
-                    float sum = 0.0f;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float lo, hi;
-                        unpack2<T>(xw[e], lo, hi);
-                        sum += lo + hi;
-                        big = fmaxf(big, fabsf(lo) <= 3.4e38f ? fabsf(lo) : 0.0f);
-                        big = fmaxf(big, fabsf(hi) <= 3.4e38f ? fabsf(hi) : 0.0f);
-                    }
-#pragma unroll
-                    for (int m = D / 16; m > 0; m >>= 1)
-                        sum += __shfl_xor_sync(0xFFFFFFFFu, sum, m);
-                    if (i % (D / 8) == 0)
-                        sumq[i / (D / 8)] = sum;
-                }
-                for (int r = tid; r < kHeld; r += 128) {
-                    float x = neg_inf_f();
-                    if (r < held) {
-                        const int qi = (g0 + r) / a.group, g = (g0 + r) - qi * a.group;
-                        const float l =
-                            a.lse[((int64_t)b * a.Lq + qi) * a.Hq + h * a.group + g];
-                        x = l == neg_inf_f() ? neg_inf_f() : -l * kLog2e;
-                    }
-                    nlse[r] = x;
-                }
-                const uint32_t wbig = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(big));
-                if (lane == 0)
-                    q_big[warp] = __uint_as_float(wbig);
-                named_sync(kBarW, 256);
-                big = fmaxf(fmaxf(q_big[0], q_big[1]), fmaxf(q_big[2], q_big[3]));
-                const float unit = __uint_as_float((uint32_t)(127 - query_exponent(big)) << 23);
-#pragma unroll 4
-                for (int i = tid; i < chunks; i += 128) {
-                    const uint4 x = chunk(i);
-                    const int r = i / (D / 8), c8 = i % (D / 8), m = r % N;
-                    *reinterpret_cast<uint4 *>(smem + S::q_off + r / N * S::q_bytes +
-                                               (c8 >> 3) * (N * 128) + m * 128 +
-                                               (((c8 & 7) ^ (m & 7)) << 4)) = code_queries<T>(x, unit);
-                }
-                fence_async_smem();
+                float shift;
+                hold_queries(g0, min(kHeld, a.rows - g0), shift);
                 for (int t = first; t < last; ++t, ++ring) {
                     const uint32_t st = ring % S::stages;
                     wait(Short{}, kFull + st, (ring / S::stages) & 1);
@@ -374,11 +392,10 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
         while (next())
             for (int g0 = 0; g0 < a.rows; g0 += kHeld) {
                 const int held = min(kHeld, a.rows - g0);
-                named_sync(kBarW, 256);
-                named_sync(kBarW, 256);
-                const float big = fmaxf(fmaxf(q_big[0], q_big[1]), fmaxf(q_big[2], q_big[3]));
-                const float k_factor =
-                    a.scale * kCodeUnit * __uint_as_float((uint32_t)(127 + query_exponent(big)) << 23);
+                float shift;
+                const int e0 = hold_queries(g0, held, shift);
+                const uint64_t shift2 = f2(shift, shift);
+                const float k_factor = a.scale * __uint_as_float((uint32_t)(127 + e0) << 23);
                 for (int t = first; t < last; ++t, ++ring) {
                     const uint32_t st = ring % S::stages;
                     const int j = t * kKeys + key;
@@ -398,7 +415,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                             const uint32_t f = lds1(buf0 + st * S::stage_bytes + S::code_bytes +
                                                     4 * key);
                             ks = bf16_low(f) * k_factor;
-                            ko = bf16_high(f) * a.scale;
+                            ko = fmaf(8.0f, bf16_low(f), bf16_high(f)) * a.scale;
                             bad = (bad_pieces[st] >> (key / span)) & 1;
                             __syncwarp();
                             mbar_arrive_if(bar(kEmpty + st), lane == 0);
@@ -426,7 +443,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                                         fma2(ko2, e ? f2(sq.z, sq.w) : f2(sq.x, sq.y),
                                              e ? f2(nl.z, nl.w) : f2(nl.x, nl.y)));
                                     float y0, y1;
-                                    un2(y, y0, y1);
+                                    un2(add2(y, shift2), y0, y1);
                                     sum2 = add2(sum2, f2(ex2_mufu(y0), ex2_mufu(y1)));
                                 }
                             }
