@@ -20,9 +20,12 @@
 // written to shared memory by threads (16-byte stores, rows contiguous).
 //
 // A row's reference (the running maximum of a softmax) is the largest score of the first 32 keys
-// it meets, and moves only when a weight leaves the range that fp16 and fp32 hold (kTopWeight), which one
-// vote a tile decides.  Weights are scaled by the cached row's scale before they are rounded to
-// fp16; a second reference of the row keeps their largest near 1 whatever the scales are.
+// it meets, and moves only when a weight leaves the range that fp16 and fp32 hold (kTopWeight),
+// which one vote a tile decides.  Weights are scaled by the cached row's scale before they are
+// rounded to fp16; a second reference of the row keeps their largest near 1 whatever the scales
+// are.  The roundings: fp16's 11 bits of a weight, below what bf16 keeps of the result (for fp16
+// results a second number holds what the first left); own values stay in their type, and their
+// weights are a sum of two numbers of it.
 //
 // Warps.  One loads (queries, codes, own keys and values, through one ring of shared-memory
 // stages), one issues the products, four unpack, four to sixteen make weights: an unpacking
@@ -32,6 +35,14 @@
 // kUnitCost tiles for each unit's beginning and end, are cut into equal ranges, one to a CTA
 // (the lengths are read on the device); a unit that crosses a CTA's end leaves fp32 partials,
 // joined by combine_kernel in tile order.
+//
+// Bound by the latency of the chain from unpacked keys to given weights and by the instructions
+// of the weights (about 300 a warp and tile), then by a unit's beginning and end; the tensor pipe is
+// busy 6 to 25 % of the time, memory 10 to 30 %.  Code that fits the instruction cache counts
+// as much as its instructions.  Measured: 64 sequences of 32 queries and own keys over prefixes of
+// 200 to 1024 keys, 32 heads of 128 channels: 131 us of GPU time (237 MB); 2 sequences of 64 queries of
+// 32 heads over 32000 keys of 8: 138 (66 GFLOP); one token of 32 heads over 1021 keys of 8: 13; and 7
+// for combine_kernel.
 #include <cuda_runtime.h>
 
 #include <type_traits>
@@ -1285,7 +1296,9 @@ __global__ void __launch_bounds__(32 * kJoinWarps)
         a.lse[row] = sum == 0.0f ? neg_inf_f() : (top + log2f(sum)) * 0.6931471805599453f;
 }
 
-// Rows of a row tile: the smallest width that holds a head's rows, 64 beyond that.
+// Rows of a row tile: the smallest width that holds a head's rows, 64 beyond that.  (64 sequences
+// of 32 heads, 512 cached keys: 16 rows a head 93 us, in a tile of 32 116, of 64 164; 32 rows 116,
+// in a tile of 64 173.)
 int tile_rows(int64_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
 
 struct Workspace {

@@ -54,7 +54,7 @@ __device__ __forceinline__ uint32_t order_key(float w)
 // result does not depend on any order of arrival.
 //
 // A long row takes a cluster of kCluster CTAs, neighbouring parts of the row by rank: they leave
-// their counts in one another's shared memory (16 CTAs for 16 heads of 32000 keys took 45 us).
+// their counts in one another's shared memory.
 template <int kThreads, int kPerThread, int kCluster>
 struct SelectShared {
     uint32_t digits[2][kThreads / 32][8];  // counts of the warps, two digits a word, by the round's parity
@@ -316,9 +316,13 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const __grid_con
         meet<kCluster>();  // no CTA leaves while another may still write into it
 }
 
-// Rows of up to 2048 slots take one CTA of 256 threads of 8 slots; longer ones a cluster of eight
-// of 512, whose 32768 slots stay in registers (rows beyond that are read again each round).
-constexpr int kShortRow = 2048;
+// Who takes a row.  One CTA where its threads hold the row in registers, 8 slots each: 256 threads
+// to 2048 slots, 512 to 4096 (256 rows of 3000: 26 us; 33 with 256 threads, which read the row
+// again each round; 208 with a cluster of eight, whose barriers every row pays).  Longer rows a
+// cluster, of eight for a few of them (16 rows of 32000: 33 us; of two 68, of one 101), of two for
+// rows of up to 8192 (16 of 8000: 23 us; eight 32, one 35) and for many (256 of 8000: 43 us; eight
+// 215; 64 of 32000: 69, eight 72).
+constexpr int kShortRow = 2048, kOneRow = 4096, kTwoRow = 8192, kManyRows = 64;
 
 template <int kThreads, int kPerThread, int kCluster>
 cudaError_t launch_select(const EvictArgs &a, int B, cudaStream_t s)
@@ -481,8 +485,13 @@ extern "C" fdllm_status fdllm_cache_evict(const fdllm_cache *cache, const int32_
     a.out_weights = out_weights;
     a.out_index = out_index;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if ((max_len <= kShortRow ? launch_select<256, 8, 1>(a, B, s) : launch_select<512, 8, 8>(a, B, s)) !=
-        cudaSuccess)
+    const cudaError_t selected =
+        max_len <= kShortRow ? launch_select<256, 8, 1>(a, B, s)
+        : max_len <= kOneRow ? launch_select<512, 8, 1>(a, B, s)
+        : max_len <= kTwoRow || (int64_t)B * a.c.heads >= kManyRows
+            ? launch_select<512, 8, 2>(a, B, s)
+            : launch_select<512, 8, 8>(a, B, s);
+    if (selected != cudaSuccess)
         return FDLLM_ERR_CUDA;
     const dim3 grid((budget + kMoveSlots - 1) / kMoveSlots, a.c.heads, B);
     const cudaError_t e =

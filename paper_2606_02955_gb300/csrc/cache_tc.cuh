@@ -350,11 +350,12 @@ __device__ __forceinline__ void fence_async_smem()
 }
 
 // Waits on a shared-memory address, a few instructions each: many places of a kernel wait, and
-// code that does not fit the instruction cache costs its warps more than the waits (a wait with a
-// timer at each place: 5% of a block's attention).  The limit is a count of tries, of 20 ns at the
-// least and kSleepNs: a fraction of a second or more, where a wait takes microseconds.  kSleepNs: a warp
-// that waits most of its time sleeps between tries, which would take issue slots from the warps
-// that work.  False: given up; the caller waits no more, and says so in the status word.
+// code that does not fit the instruction cache costs its warps more than the waits (with a timer at
+// each place 64 blocks' attention took 195 us instead of 143).  The limit is a count of tries, of
+// 20 ns at the least and kSleepNs: a fraction of a second or more, where a wait takes microseconds.
+// kSleepNs: a warp that waits most of its time sleeps between tries, which would take issue slots
+// from the warps that work.  False: given up; the caller waits no more, and says so in the status
+// word.
 constexpr uint32_t kWaitTries = 1u << 23, kDrainTries = 1u << 20;
 
 __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)

@@ -6,7 +6,7 @@
 //
 // Layout.  A tile is 128 keys.  S^T [128 keys x N rows] = K . Q^T puts a key's scores in one
 // thread, so that the sum over the rows never leaves it: no shuffle, no atomic, one order.  The
-// unpacked keys stay in tensor memory while the row tiles of a group (up to kGroup * N rows, their
+// unpacked keys stay in tensor memory while the row tiles of a group (four of 64 rows, their
 // queries in shared memory) pass by; more rows take the CTA's keys once again.
 //
 // Bound by the exponentials and their arithmetic (3 instructions a row and key) above about 32
@@ -14,6 +14,9 @@
 //
 // Split.  The key tiles of all (sequence, head) units in order are cut into equal ranges, one to
 // a CTA; tiles share nothing, so nothing is joined.
+//
+// Measured: 8 sequences of 32 queries over 500 to 1024 keys, 32 heads of 128 channels: 16.5 us of
+// GPU time; 2 sequences of 64 queries of 32 heads over 32000 keys of 8 (256 rows a head): 66.
 #include <cuda_runtime.h>
 
 #include <type_traits>
@@ -85,8 +88,8 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
     // Memory barriers: the ring's stages full and empty; scores done, by their parity; all of a
-    // key tile's products done, its keys unpacked; scores read, by their parity.  (Each is waited for phase by phase: a wait two phases ahead
-    // would take the phase before last for its own.)
+    // key tile's products done, its keys unpacked; scores read, by their parity.  (Each is waited
+    // for phase by phase: a wait two phases ahead would take the phase before last for its own.)
     enum { kFull = 0, kEmpty = kFull + S::stages, kSDone = kEmpty + S::stages,
            kKFree = kSDone + 2, kKReady, kSFree, kBars = kSFree + 2 };
     enum { kBarW = 1 };  // CTA barrier of the unpacking and weighing warps
@@ -465,7 +468,8 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
         tc::tmem_dealloc(tmem, S::tmem);
 }
 
-// Rows of a row tile: the smallest width that holds a head's rows, 64 beyond that.
+// Rows of a row tile: the smallest width that holds a head's rows, 64 beyond that.  (64 sequences
+// of 32 heads, 512 keys: 16 rows a head 40 us, in a tile of 32 46, of 64 62; 32 rows 50, of 64 65.)
 int tile_rows(int64_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
 
 template <typename S, typename T>

@@ -2,7 +2,8 @@
 // rotary positions over up to four position axes, one pass over the rows.
 //
 // Bound by memory: each row is read once and written once (4 bytes moved per 16-bit value
-// against about 10 operations).
+// against about 10 operations).  Measured: 16381 tokens of 32 + 8 heads of 128 channels, bf16, three
+// axes: 69 us (336 MB, 4.9 TB/s); 32 tokens of 64 heads: 3 us.
 #include <cuda_runtime.h>
 
 #include "cache.cuh"
@@ -188,7 +189,8 @@ __global__ void __launch_bounds__(kThreads) qk_any_kernel(const __grid_constant_
 }
 
 // Four tokens to a CTA share one pass of angles where that leaves a few CTAs for every SM;
-// fewer tokens take one CTA each, so that a short block still spreads over the SMs.
+// fewer tokens take one CTA each, so that a short block still spreads over the SMs (40 heads: 32
+// tokens 3.1 us, in fours 5.7; 2048 tokens 11.7 both ways; 8192 tokens in fours 37.4, one by one 45.9).
 constexpr int kManyTokens = 4 * 1024;
 
 template <typename T, int D>

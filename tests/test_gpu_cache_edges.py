@@ -72,7 +72,15 @@ def test_evict_around_the_forms_of_the_selection(fd, n, budget):
     check_evict(fd, [n], 1, 64, 256, budget, 4, 64, w.cuda(), seed=n)
 
 
-@pytest.mark.parametrize("n", [7, 8, 9, 31, 32, 33])
+@pytest.mark.parametrize("n,heads", [(3000, 5), (4097, 3), (8193, 65), (9000, 66)])
+def test_evict_of_many_long_rows(fd, n, heads):
+    g = torch.Generator().manual_seed(n)
+    w = torch.rand(1, heads, n, generator=g)
+    w[0, 1] = torch.floor(8 * w[0, 1])
+    check_evict(fd, [n], heads, 64, 256, 129, 4, 5, w.cuda(), seed=n)
+
+
+@pytest.mark.parametrize("n", [1, 2, 3, 7, 8, 9, 31, 32, 33])
 @pytest.mark.parametrize("start", [0, 1, 31])
 def test_append_around_the_few_token_form(fd, n, start):
     cache = fd.KvCache.empty(6, 3, 32, 128)
