@@ -1320,8 +1320,15 @@ int full_grid(int N) { return sm_count() * (N >= 64 ? 1 : 2); }
 template <typename S, typename T>
 cudaError_t run(const AttnArgs &a, int grid, const CUtensorMap (&maps)[4], cudaStream_t s)
 {
-    static const cudaError_t ready = cudaFuncSetAttribute(
-        attention_kernel<S, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::smem);
+    static const cudaError_t ready = [] {
+        // the roles' shares of registers must not add up to more than the launch gives
+        cudaFuncAttributes f;
+        const cudaError_t e = cudaFuncGetAttributes(&f, attention_kernel<S, T>);
+        if (e != cudaSuccess || f.numRegs < S::regs)
+            return e != cudaSuccess ? e : cudaErrorInvalidKernelImage;
+        return cudaFuncSetAttribute(attention_kernel<S, T>,
+                                    cudaFuncAttributeMaxDynamicSharedMemorySize, S::smem);
+    }();
     if (ready != cudaSuccess)
         return ready;
     cudaError_t e = launch(attention_kernel<S, T>, dim3(grid), dim3(S::threads), S::smem, s, true,
