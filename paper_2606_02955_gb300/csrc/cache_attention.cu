@@ -28,8 +28,8 @@
 // weights are a sum of two numbers of it.
 //
 // Warps.  One loads (queries, codes, own keys and values, through one ring of shared-memory
-// stages), one issues the products, four unpack, four to sixteen make weights: an unpacking
-// warp is tiles ahead, in the next unit's queries while the weights' warps write a unit's end.
+// stages), one issues the products, four unpack, four or eight make weights: an unpacking warp is
+// ahead, in the next unit's queries while the weights' warps write a unit's end.
 //
 // Split.  The tiles of all (sequence, head, row tile) units in order, with a charge of
 // kUnitCost tiles for each unit's beginning and end, are cut into equal ranges, one to a CTA
@@ -37,12 +37,11 @@
 // joined by combine_kernel in tile order.
 //
 // Bound by the latency of the chain from unpacked keys to given weights and by the instructions
-// of the weights (about 300 a warp and tile), then by a unit's beginning and end; the tensor pipe is
-// busy 6 to 25 % of the time, memory 10 to 30 %.  Code that fits the instruction cache counts
-// as much as its instructions.  Measured: 64 sequences of 32 queries and own keys over prefixes of
-// 200 to 1024 keys, 32 heads of 128 channels: 131 us of GPU time (237 MB); 2 sequences of 64 queries of
-// 32 heads over 32000 keys of 8: 138 (66 GFLOP); one token of 32 heads over 1021 keys of 8: 13; and 7
-// for combine_kernel.
+// of the weights (about 300 a warp and tile), then by a unit's beginning and end.  Code that fits the
+// instruction cache counts as much as its instructions.  Measured: 64 sequences of 32 queries and
+// own keys over prefixes of 200 to 1024 keys, 32 heads of 128 channels: 131 us of GPU time (237 MB; the
+// tensor pipe 9 % busy, memory 25 %); 2 sequences of 64 queries of 32 heads over 32000 keys of 8: 138
+// (66 GFLOP); one token of 32 heads over 1021 keys of 8: 13; and 7 for combine_kernel.
 #include <cuda_runtime.h>
 
 #include <type_traits>
@@ -58,7 +57,7 @@ constexpr float kFar = -1e30f;            // reference of a row that has seen no
 constexpr float kTopWeight = 16384.0f;    // largest weight (fp16 holds 65504)
 constexpr float kTopShift = 90.0f;        // a score this far above its reference may overflow
 constexpr float kMaxShift = 120.0f;       // c = 2^(ref - refz) stays below 2^120
-constexpr int kNever = 0x7FFFFFFF;
+constexpr int kNever = 0x7FFFFFFF;         // no such key
 constexpr float kSumUnit = 1048576.0f;    // sums over values' codes come in units of 2^-20
 
 struct AttnArgs {
@@ -95,7 +94,9 @@ template <int D_, int N_>
 struct Shape {
     static constexpr int D = D_;
     static constexpr int N = N_;                       // rows of a row tile
-    static constexpr int C = N <= 32 ? N / 16 : N / 32;  // warpgroups sharing a tile's columns
+    // Warpgroups sharing a tile's columns: 16 columns a thread, 32 where the registers are there
+    // (32 rows: 143 us, with 32 a thread 219; 64 rows over 32000 keys: 133, with 16 a thread 139).
+    static constexpr int C = N <= 32 ? N / 16 : N / 32;
     static constexpr int cols = N / C;                 // columns (rows of the problem) a thread
     static constexpr int w_warps = 4 * C;              // warps that make weights
     static constexpr int w_first = 4;                  // (warps 0 to 3 unpack)
@@ -104,7 +105,8 @@ struct Shape {
     static constexpr int threads = 32 * (loader + 4);  // (two warps of the last group idle)
     static constexpr int ctas = N >= 64 ? 1 : 2;       // CTAs an SM holds
     // Registers of a thread, by warpgroup: what the launch gives every thread is dealt out
-    // again, the weights' warps taking what the others leave.
+    // again, the weights' warps taking what the others leave: spilled registers cost them more than
+    // the others (an even share: 201 us for blocks of 32 rows; 40 of 64 for the others: 196, 48: 203).
     static constexpr int regs = 65536 / (ctas * threads) / 8 * 8;
     static constexpr int u_regs = N == 32 ? 40 : 64, l_regs = u_regs;
     static constexpr int w_regs = (regs * (C + 2) - u_regs - l_regs) / C / 8 * 8;
@@ -172,7 +174,8 @@ __device__ __forceinline__ void scale_sums(uint32_t taddr, const float *f, float
     tmem_wait_st();
 }
 
-// A unit's beginning and end cost about as much as this many tiles.
+// A unit's beginning and end cost about as much as this many tiles (4 to 8 by the rows; 3 here
+// took 136 us instead of 131).
 constexpr int kUnitCost = 7;
 
 // One sequence's share of the work.

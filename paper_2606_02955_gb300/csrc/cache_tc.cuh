@@ -241,9 +241,7 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
 template <int NC>
 __device__ __forceinline__ void tmem_st(uint32_t taddr, const uint32_t (&r)[NC])
 {
-    if constexpr (NC == 16) {
-        tmem_st16(taddr, r);
-    } else if constexpr (NC == 4) {
+    if constexpr (NC == 4) {
         asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr),
                      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3])
                      : "memory");
