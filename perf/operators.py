@@ -154,7 +154,7 @@ def work(case):
 def _affine_codes(x):
     """Rows of D values in 32 bits -> (codes as numbers 0..15, scale, offset in bfloat16)."""
     low, high = x.amin(-1, keepdim=True), x.amax(-1, keepdim=True)
-    scale = ((high - low) / torch.full_like(high, 15.0)).to(torch.bfloat16)
+    scale = ((high - low) / 15.0).to(torch.bfloat16)
     offset = low.to(torch.bfloat16)
     s = scale.float()
     codes = ((x - offset.float()) / torch.where(s == 0, torch.ones_like(s), s)).round().clamp(0, 15)
