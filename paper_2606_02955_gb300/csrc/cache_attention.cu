@@ -23,9 +23,12 @@
 // it meets, and moves only when a weight leaves the range that fp16 and fp32 hold (kTopWeight),
 // which one vote a tile decides.  Weights are scaled by the cached row's scale before they are
 // rounded to fp16; a second reference of the row keeps their largest near 1 whatever the scales
-// are.  The roundings: fp16's 11 bits of a weight, below what bf16 keeps of the result (for fp16
-// results a second number holds what the first left); own values stay in their type, and their
-// weights are a sum of two numbers of it.
+// are.  A weight is held as two numbers of the values' operand type (fp16 for codes, their own
+// type for own values): rounded, and what that left times 2^11, as columns of one product with
+// sums of their own.  So it keeps 22 bits (16 of bf16), and one far below the largest, a subnormal of the first
+// number, keeps its place to 2^-36 of it: a key that outweighs all others at the front of a long
+// cache takes nothing from the many small ones behind it.  (With the first number alone the
+// results' error was 1.77e-3 for blocks of bf16, of which its rounding is 1.66e-3.)
 //
 // Warps.  One loads (queries, codes, own keys and values, through one ring of shared-memory
 // stages), one issues the products, four unpack, four or eight make weights: an unpacking warp is
@@ -59,6 +62,7 @@ constexpr float kTopShift = 90.0f;        // a score this far above its referenc
 constexpr float kMaxShift = 120.0f;       // c = 2^(ref - refz) stays below 2^120
 constexpr int kNever = 0x7FFFFFFF;         // no such key
 constexpr float kSumUnit = 1048576.0f;    // sums over values' codes come in units of 2^-20
+constexpr float kRest = 2048.0f;          // what a weight's rounding left is held times this
 
 struct AttnArgs {
     CacheView c;
@@ -124,12 +128,13 @@ struct Shape {
     static constexpr int q16_off = stages * stage_bytes;  // queries for codes, in fp16
     static constexpr int qt_off = q16_off + q_bytes;      // queries for own keys, as they are
     static constexpr int p_off = qt_off + q_bytes;
-    static constexpr int lo_off = p_off + kKeys * N * 2;
-    static constexpr int smem = lo_off + kKeys * N * 2 + 1024;  // and room to align the base
+    static constexpr int p_step = 2 * N * 16;  // 8 keys' weights: first numbers, then second ones
+    static constexpr int smem = p_off + kKeys / 8 * p_step + 1024;  // and room to align the base
     // tensor memory columns
-    static constexpr int tK = 0, tV = 64 * bufs, tS = 128 * bufs, tO = tS + 2 * N;
-    static constexpr int tmem = tO + N <= 256 ? 256 : 512;
-    static_assert(tO + N <= tmem && ctas * tmem <= 512, "tensor memory");
+    // (tO: the sums of the weights' first numbers; tL: of their second)
+    static constexpr int tK = 0, tV = 64 * bufs, tS = 128 * bufs, tO = tS + 2 * N, tL = tO + N;
+    static constexpr int tmem = tL + N <= 256 ? 256 : 512;
+    static_assert(tL + N <= tmem && ctas * tmem <= 512, "tensor memory");
     static_assert(q_bytes <= stage_bytes && own_v + 64 * D <= stage_bytes, "a stage holds them");
     static_assert(stages >= 2 * own_keys / 32, "two own tiles are in flight");
 };
@@ -549,8 +554,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
         // scores while the others make weights.
         const uint64_t q16_desc = tc::sw128_kmajor_desc(smem + S::q16_off);
         const uint64_t qt_desc = tc::sw128_kmajor_desc(smem + S::qt_off);
-        const uint64_t p_desc = mn_desc(smem + S::p_off, 128, N * 16);
-        const uint64_t lo_desc = mn_desc(smem + S::lo_off, 128, N * 16);
+        const uint64_t p_desc = mn_desc(smem + S::p_off, 128, S::p_step);
         uint32_t scores = 0, sums = 0;  // tiles issued so far
         for (uint32_t seg = 0;; ++seg) {
             const uint32_t sb = seg & 1;
@@ -586,26 +590,18 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     const uint32_t tV = tmem + S::tV + (S::bufs > 1 ? par * 64 : 0);
                     const uint32_t more = t - 1 > first;
                     if (t - 1 < ct) {
-                        constexpr uint32_t idesc = idesc_f16<__half>(128, N, true);
+                        constexpr uint32_t idesc = idesc_f16<__half>(128, 2 * N, true);
 #pragma unroll
                         for (int k = 0; k < kKeys / 16; ++k)
-                            mma_ts(tmem + S::tO, tV + 8 * k, p_desc + k * ((2 * N * 16) >> 4),
+                            mma_ts(tmem + S::tO, tV + 8 * k, p_desc + k * ((2 * S::p_step) >> 4),
                                    idesc, k > 0 ? 1u : more);
-                        if (!std::is_same<T, __nv_bfloat16>::value)
-#pragma unroll
-                            for (int k = 0; k < kKeys / 16; ++k)
-                                mma_ts(tmem + S::tO, tV + 8 * k, lo_desc + k * ((2 * N * 16) >> 4),
-                                       idesc, 1);
                     } else {
-                        constexpr uint32_t idesc = idesc_f16<T>(128, N, true);
+                        constexpr uint32_t idesc = idesc_f16<T>(128, 2 * N, true);
                         const int keys = min(kOwnKeys, own_total - (t - 1 - ct) * kOwnKeys);
                         const int steps = (keys + 31) / 32 * 2;
-                        for (int k = 0; k < steps; ++k) {
-                            mma_ts(tmem + S::tO, tV + 8 * k, p_desc + k * ((2 * N * 16) >> 4),
+                        for (int k = 0; k < steps; ++k)
+                            mma_ts(tmem + S::tO, tV + 8 * k, p_desc + k * ((2 * S::p_step) >> 4),
                                    idesc, k > 0 ? 1u : more);
-                            mma_ts(tmem + S::tO, tV + 8 * k, lo_desc + k * ((2 * N * 16) >> 4),
-                                   idesc, 1);
-                        }
                     }
                     mma_commit(&bars[kODone + par]);
                     ++sums;
@@ -826,7 +822,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
         const uint32_t lanes = tmem + ((uint32_t)quarter << 21);
         // where this thread's weights go: 16 bytes (8 rows of its key) a column group
         const int kappa = (key & ~7) | ((key & 3) << 1) | ((key >> 2) & 1);
-        const uint32_t p_at = buf0 + S::p_off + (kappa >> 3) * (N * 16) + (col0 >> 3) * 128 +
+        const uint32_t p_at = buf0 + S::p_off + (kappa >> 3) * S::p_step + (col0 >> 3) * 128 +
                               (kappa & 7) * 16;
         const uint32_t cols_at = row0 + 4 * col0;
         uint32_t ring = 0;    // stages used so far
@@ -851,9 +847,6 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
             // Tiles [from, to) of the unit, all of them cached or all of them own.
             auto tiles = [&](auto own_tag, int from, int to) {
                 constexpr bool kOwn = decltype(own_tag)::value;
-                // own values: weights as a sum of two numbers of T; cached ones need a second
-                // number only for results of 11 bits
-                constexpr bool kSplit = kOwn || !std::is_same<T, __nv_bfloat16>::value;
                 using W = std::conditional_t<kOwn, T, __half>;  // weights and values
                 const int end = kOwn ? g.own : g.cached;
                 const int base = kOwn ? g.ct : 0;
@@ -933,7 +926,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                         }
                         sync();
                     }
-                    uint32_t ph[kCols / 2], pl[kSplit ? kCols / 2 : 1];
+                    uint32_t ph[kCols / 2], pl[kCols / 2];
                     // Weights of this thread's columns, and their sums.  The second time (after
                     // the references moved) only the rows of `redo` are summed again.
                     auto weights = [&](auto again) -> float {
@@ -988,15 +981,16 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                                         if constexpr (!kOwn)
                                             pm2[i] = fma2(p, vo2, pm2[i]);
                                     }
-                                    un2(mul2(p, kOwn ? cm2[e] : mul2(vw2, cm2[e])), z0, z1);
+                                    const uint64_t z = mul2(p, kOwn ? cm2[e] : mul2(vw2, cm2[e]));
+                                    un2(z, z0, z1);
                                     top = max3(top, y0, y1);
                                     top = max3(top, z0, z1);
                                     ph[i] = pack2<W>(z0, z1);
-                                    if constexpr (kSplit) {
-                                        float h0, h1;
-                                        unpack2<W>(ph[i], h0, h1);
-                                        pl[i] = pack2<W>(z0 - h0, z1 - h1);
-                                    }
+                                    unpack2<W>(ph[i], z0, z1);
+                                    un2(fma2(f2(z0, z1), f2(-kRest, -kRest),
+                                             mul2(z, f2(kRest, kRest))),
+                                        z0, z1);
+                                    pl[i] = pack2<W>(z0, z1);
                                 }
                             }
                         }
@@ -1008,11 +1002,8 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                         over = weights(std::false_type{}) > kTopWeight;
                     } else {
 #pragma unroll
-                        for (int i = 0; i < kCols / 2; ++i) {
-                            ph[i] = 0;
-                            if constexpr (kSplit)
-                                pl[i] = 0;
-                        }
+                        for (int i = 0; i < kCols / 2; ++i)
+                            ph[i] = pl[i] = 0;
                     }
                     // the sums of the tile before must have read its weights
                     if (seen > summed) {
@@ -1021,7 +1012,8 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                         tc::fence_after_sync();
                     }
                     if (kOwn && t == from && from > begin)
-                        scale_sums<kCols>(lanes + S::tO + col0, nullptr, kSumUnit);
+                        for (int at : {S::tO, S::tL})
+                            scale_sums<kCols>(lanes + at + col0, nullptr, kSumUnit);
                     if (__builtin_expect(named_sync_or(kBarW + wg, 128, over), 0)) {
                         // ---- the references move: per row, the running maxima of the scores
                         // and of the scores with the values' scale
@@ -1068,7 +1060,8 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                         }
                         sync();
                         if (t > begin)  // the sums of the tiles before (waited for above)
-                            scale_sums<kCols>(lanes + S::tO + col0, fo + col0, 1.0f);
+                            for (int at : {S::tO, S::tL})
+                                scale_sums<kCols>(lanes + at + col0, fo + col0, 1.0f);
 #pragma unroll
                         for (int c = 0; c < kCols / 2; ++c) {
                             float x0, x1, m0, m1;
@@ -1092,9 +1085,8 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                         for (int q = 0; q < kCols / 8; ++q) {
                             sts4(p_at + 128 * q, ph[4 * q], ph[4 * q + 1], ph[4 * q + 2],
                                  ph[4 * q + 3]);
-                            if constexpr (kSplit)
-                                sts4(p_at + (S::lo_off - S::p_off) + 128 * q, pl[4 * q],
-                                     pl[4 * q + 1], pl[4 * q + 2], pl[4 * q + 3]);
+                            sts4(p_at + N * 16 + 128 * q, pl[4 * q], pl[4 * q + 1], pl[4 * q + 2],
+                                 pl[4 * q + 3]);
                         }
                     }
                     fence_async_smem();
@@ -1173,9 +1165,11 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
             const int rows = g.rows;
 #pragma unroll 1
             for (int c8 = 0; c8 < kCols; c8 += 8) {
-                uint32_t o[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-                if (some)
+                uint32_t o[8] = {0, 0, 0, 0, 0, 0, 0, 0}, rest[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+                if (some) {
                     tmem_ld<8>(lanes + S::tO + col0 + c8, o);
+                    tmem_ld<8>(lanes + S::tL + col0 + c8, rest);
+                }
                 if (D == 64 && quarter >= 2)
                     continue;
                 if (D == 128 || d < D)
@@ -1184,7 +1178,9 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                         const int n = col0 + c8 + c;
                         if (n < rows) {
                             const float2 f = fin[sb][n];
-                            float x = fmaf(__uint_as_float(o[c]), f.x, f.y);
+                            float x = fmaf(fmaf(__uint_as_float(rest[c]), 1.0f / kRest,
+                                                __uint_as_float(o[c])),
+                                           f.x, f.y);
                             if (bad != kNever && (!a.causal || bad <= (g.r0 + n) / a.group))
                                 x = nan_f();
                             const int64_t at = row_at[sb][n] * D + d;
