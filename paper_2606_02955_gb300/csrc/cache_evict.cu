@@ -47,7 +47,7 @@ __device__ __forceinline__ uint32_t order_key(float w)
 // a radix select over the 32-bit order keys, four bits a round from the highest in which the keys
 // differ.  The row passes through shared memory once (coalesced in, neighbouring slots to a thread
 // out) and its keys stay in registers; a thread counts its digits in one 64-bit number, four bits
-// a digit, and a warp adds them up with eight reductions.  (A histogram in shared memory took 32 K
+// a digit, and a warp adds them up with eight reductions, pass by pass into 32 bits.  (A histogram in shared memory took 32 K
 // atomics on the few bins that weights of one magnitude share: 72 us for 16 heads of 32000 keys;
 // a bisection by single bits 38 us, mostly its 32 rounds' barriers.)  A scan of the counts of keys
 // above the threshold and at it then places the kept slots in order.  Only counts are shared: the
@@ -57,7 +57,7 @@ __device__ __forceinline__ uint32_t order_key(float w)
 // their counts in one another's shared memory.
 template <int kThreads, int kPerThread, int kCluster>
 struct SelectShared {
-    uint32_t digits[2][kThreads / 32][8];  // counts of the warps, two digits a word, by the round's parity
+    int digits[2][kThreads / 32][16];      // counts of the warps, by the round's parity
     int cta_digits[2][kCluster][16];       // of the CTAs
     int sure[32], ties[32];
     int cta_sure[kCluster], cta_ties[kCluster];
@@ -177,7 +177,7 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const __grid_con
         uint32_t prefix = top < 0 ? low : shift == 28 ? 0u : low >> (shift + 4) << (shift + 4);
         bool whole = false;  // all keys from the prefix on are taken
         for (; shift >= 0 && !whole; shift -= 4, par ^= 1) {
-            uint32_t sums[8] = {};
+            int held = 0;  // lane d < 16: the warp's keys with digit d
             for (int p = 0; p < passes; ++p) {
                 if (passes > 1)
                     load_keys(p);
@@ -189,18 +189,20 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const __grid_con
                     c += d < 16u ? 1ull << (4 * d) : 0ull;
                 }
                 static_assert(kPerThread < 16, "a digit's count has four bits");
+                // (two digits a word hold one pass's counts; a row of millions of slots has more
+                // keys of a digit than half a word counts, so passes add up in whole ones)
+                uint32_t word = 0;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const uint32_t two = (uint32_t)(c >> (8 * i));
-                    sums[i] += __reduce_add_sync(0xFFFFFFFFu, (two & 15u) | ((two & 0xF0u) << 12));
+                    const uint32_t sum =
+                        __reduce_add_sync(0xFFFFFFFFu, (two & 15u) | ((two & 0xF0u) << 12));
+                    word = lane >> 1 == i ? sum : word;
                 }
+                held += (int)((word >> (16 * (lane & 1))) & 0xFFFFu);
             }
-            uint32_t word = sums[0];
-#pragma unroll
-            for (int i = 1; i < 8; ++i)
-                word = lane == i ? sums[i] : word;
-            if (lane < 8)
-                sh.digits[par][warp][lane] = word;
+            if (lane < 16)
+                sh.digits[par][warp][lane] = held;
             __syncthreads();
             // lane d < 16 of every warp: the CTA's keys with digit d, then the cluster's
             int count = 0;
@@ -208,7 +210,7 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const __grid_con
                 if (lane < 16)
 #pragma unroll 8
                     for (int i = 0; i < kWarps; ++i)
-                        count += (sh.digits[par][i][lane >> 1] >> (16 * (lane & 1))) & 0xFFFFu;
+                        count += sh.digits[par][i][lane];
             }
             if constexpr (kCluster > 1) {
                 if (warp == 0 && lane < 16)
@@ -298,7 +300,7 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const __grid_con
             bool keep = (sure >> e) & 1u;
             if ((tie >> e) & 1u)
                 keep = t++ < ties;
-            if (keep) {
+            if (keep && at < a.budget) {  // (weights that change under the call stay in bounds)
                 index[at] = from + e;
                 kept_w[at] = mine[e];
                 ++at;
