@@ -30,13 +30,34 @@ inline EncodeFn encode_tiled()
     return encode;
 }
 
+// One tensor map.  The driver's function wants the device's context current, which a host thread
+// has only from its first runtime call that needs one on (memory a binding keeps needs none): a
+// first failure makes it current and tries again.
+inline bool encode_map(CUtensorMap *m, CUtensorMapDataType type, int rank, const void *base,
+                       const cuuint64_t *dims, const cuuint64_t *strides, const cuuint32_t *box,
+                       CUtensorMapSwizzle swizzle, CUtensorMapL2promotion promotion)
+{
+    const EncodeFn encode = encode_tiled();
+    const cuuint32_t unit[5] = {1, 1, 1, 1, 1};
+    const auto done = [&] {
+        return encode(m, type, (cuuint32_t)rank, const_cast<void *>(base), dims, strides, box, unit,
+                      CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, promotion,
+                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    };
+    if (!encode)
+        return false;
+    if (done())
+        return true;
+    int dev = 0;
+    return cudaGetDevice(&dev) == cudaSuccess && cudaSetDevice(dev) == cudaSuccess && done();
+}
+
 // Tensor map of rows [B, tokens, heads, D] of 16-bit values: one box `box_inner` channels of 32
 // tokens of a head, swizzled where they are 64.  False where a map cannot hold the strides (an
 // axis of several that repeats one row).
 inline bool make_rows_map(CUtensorMap *m, const void *base, const Strides3 &s, int B, int tokens,
                           int heads, int D, int box_inner, bool swizzle)
 {
-    const EncodeFn encode = encode_tiled();
     const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)heads, (cuuint64_t)tokens, (cuuint64_t)B};
     cuuint64_t strides[3];
     const int64_t elements[3] = {s.head, s.token, s.batch};
@@ -47,12 +68,9 @@ inline bool make_rows_map(CUtensorMap *m, const void *base, const Strides3 &s, i
         strides[i] = 2 * (cuuint64_t)e;
     }
     const cuuint32_t box[4] = {(cuuint32_t)box_inner, 1, 32, 1};
-    const cuuint32_t unit[4] = {1, 1, 1, 1};
-    return encode && encode(m, CU_TENSOR_MAP_DATA_TYPE_UINT16, 4, const_cast<void *>(base), dims,
-                            strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                            swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
-                            CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
-                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    return encode_map(m, CU_TENSOR_MAP_DATA_TYPE_UINT16, 4, base, dims, strides, box,
+                      swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+                      CU_TENSOR_MAP_L2_PROMOTION_L2_128B);
 }
 
 // Tensor maps of a cache's codes: keys as rows of D/2 bytes, one box a page's (or a tile's)
@@ -60,22 +78,17 @@ inline bool make_rows_map(CUtensorMap *m, const void *base, const Strides3 &s, i
 // follows the box's row, so that 16-byte reads of one row a thread meet no bank twice.
 inline bool make_cache_maps(const CacheView &c, CUtensorMap *k, CUtensorMap *v)
 {
-    const EncodeFn encode = encode_tiled();
-    if (!encode)
-        return false;
     const int page = 1 << c.page_shift, span = page < 128 ? page : 128;
     const auto map = [&](CUtensorMap *m, void *base, int64_t inner, int64_t outer, int box_inner,
                          int box_outer) {
         const cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)outer};
         const cuuint64_t strides[1] = {(cuuint64_t)inner};
         const cuuint32_t box[2] = {(cuuint32_t)box_inner, (cuuint32_t)box_outer};
-        const cuuint32_t unit[2] = {1, 1};
         const CUtensorMapSwizzle sw = box_inner == 64   ? CU_TENSOR_MAP_SWIZZLE_64B
                                       : box_inner == 32 ? CU_TENSOR_MAP_SWIZZLE_32B
                                                         : CU_TENSOR_MAP_SWIZZLE_NONE;
-        return encode(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, base, dims, strides, box, unit,
-                      CU_TENSOR_MAP_INTERLEAVE_NONE, sw, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+        return encode_map(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, base, dims, strides, box, sw,
+                          CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
     };
     const int64_t ph = (int64_t)c.pages * c.heads;
     if (ph * page >= ((int64_t)1 << 31) || ph * c.D >= ((int64_t)1 << 31))
