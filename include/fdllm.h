@@ -453,7 +453,8 @@ fdllm_status fdllm_cache_read(const fdllm_cache *cache, const int32_t *block_tab
  *   causal       1: query i sees own keys j <= i only (all cached keys always).
  *   out          [B, Lq, Hq, D] in q's dtype, contiguous.   out_lse [B, Lq, Hq] fp32 or NULL.
  *   workspace    device, 256-byte aligned, fdllm_cache_attention_workspace_bytes() bytes, of
- *                any content; calls that may overlap on the GPU need their own.
+ *                any content; calls that may overlap on the GPU need their own, and so do
+ *                calls of several host threads on one stream (a call is two launches).
  * A query that sees no key gets out = 0 and out_lse = -inf.  A sequence whose cache_lens or
  * new_lens is out of range (negative, past the table, past Ln) or that meets a page out of
  * range among its first cache_lens slots gets NaN, for all its rows where the lengths are

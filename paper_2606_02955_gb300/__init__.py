@@ -753,22 +753,6 @@ def fdllm_cache_attention_workspace_bytes(B: int, Lq: int, Hq: int, heads: int,
     return int(_load().fdllm_cache_attention_workspace_bytes(B, Lq, Hq, heads, head_dim))
 
 
-# Attention's workspaces, one to a device and stream, grown on demand: calls on one stream are
-# ordered, so they can share it.  A call under stream capture gets memory of its own (the graph
-# may be replayed on any stream).
-_workspaces = {}
-
-
-def _workspace(need, dev, stream):
-    if torch.cuda.is_current_stream_capturing():
-        return _made((need,), _U8, dev, stream)
-    key = (dev.index, _raw_stream(dev.index) if stream is None else _stream(stream))
-    t = _workspaces.get(key)
-    if t is None or t.numel() < need:
-        t = _workspaces[key] = _made((need,), _U8, dev, stream)
-    return t
-
-
 def _queries(q, cache, dev):
     if q.dim() != 4:
         raise ValueError("q must be [B, Lq, Hq, D]")
@@ -789,7 +773,7 @@ def fdllm_cache_attention(q: torch.Tensor, cache: KvCache, block_table: torch.Te
     """Attention of ``q`` [B, Lq, Hq, D] (bf16/fp16) over the first cache_lens[b] slots of the
     cache and the block's own ``k_new``, ``v_new`` [B, Ln, heads, D].  ``scale`` None: D^-0.5.
     ``workspace`` a uint8 CUDA tensor of fdllm_cache_attention_workspace_bytes bytes (None: one
-    the binding keeps for the stream; pass one where another library captures the call).
+    of the call's own from torch's allocator; pass one where another library captures the call).
     Returns out, or (out, lse fp32 [B, Lq, Hq]) with ``return_lse``."""
     dev, dt = q.device, q.dtype
     qp, qs, B, Lq, Hq = _queries(q, cache, dev)
@@ -809,8 +793,10 @@ def fdllm_cache_attention(q: torch.Tensor, cache: KvCache, block_table: torch.Te
         out_lse = _made((B, Lq, Hq), _F32, dev, stream)
     lib = _load()
     if workspace is None:
+        # Of this call alone: it is two launches, between which another thread may enqueue a call
+        # of its own on the stream.  (The allocator hands the memory out again in stream order.)
         need = lib.fdllm_cache_attention_workspace_bytes(B, Lq, Hq, heads, D)
-        workspace = _workspace(need if need > 256 else 256, dev, stream)
+        workspace = _made((need if need > 256 else 256,), _U8, dev, stream)
     st = lib.fdllm_cache_attention(
         qp, qs, _CODES[dt], B, Lq, Hq, cache._ref, tp, mp,
         _ptr(cache_lens, "cache_lens", _I32, (B,), dev), kp, ks, vp, vs, Ln,

@@ -59,3 +59,53 @@ def test_a_thread_whose_first_call_it_is(fd, name):
         assert torch.equal(got_w, w)
     if name == "norm":
         assert torch.equal(got_q, q[0])
+
+
+def test_a_call_inside_another_has_a_workspace_of_its_own(fd, monkeypatch):
+    """What two threads do at the worst, in one: while a call is in the library, another is made
+    on the same stream.  Neither may be given the other's workspace."""
+    cache, table = ref.make_cache(fd, [40], 2, 64, 32, seed=3)
+    q = gaussian((1, 2, 4, 64), 5, torch.bfloat16)
+    lib, seen = fd._load(), []
+
+    class Library:
+        fdllm_cache_attention_workspace_bytes = lib.fdllm_cache_attention_workspace_bytes
+
+        def fdllm_cache_attention(self, *args):
+            seen.append(args[-3])
+            if len(seen) == 1:
+                fd.fdllm_cache_attention(q, cache, table, ints([40]))
+            return lib.fdllm_cache_attention(*args)
+
+    monkeypatch.setattr(fd, "_load", lambda: Library())
+    fd.fdllm_cache_attention(q, cache, table, ints([40]))
+    assert len(seen) == 2 and seen[0] and seen[1] and seen[0] != seen[1]
+
+
+def test_threads_on_one_stream(fd):
+    """Four threads, each with a batch of its own whose units are cut between thread blocks."""
+    work = []
+    for i, (B, n) in enumerate([(1, 3000), (3, 900), (2, 1500), (5, 333)]):
+        cache, table = ref.make_cache(fd, [n] * B, 2, 128, 64, seed=i)
+        q = gaussian((B, 32, 4, 128), i, torch.bfloat16)
+        work.append((q, cache, table, ints([n] * B)))
+    want = [fd.fdllm_cache_attention(*w, return_lse=True) for w in work]
+    got, errors = [[] for _ in work], []
+
+    def many(i):
+        try:
+            for _ in range(200):
+                got[i].append(fd.fdllm_cache_attention(*work[i], return_lse=True))
+        except Exception as e:  # a thread's exception is the test's
+            errors.append(e)
+
+    threads = [threading.Thread(target=many, args=(i,)) for i in range(len(work))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not errors
+    for i, results in enumerate(got):
+        assert len(results) == 200
+        assert all(torch.equal(a, b) for r in results for a, b in zip(r, want[i]))
