@@ -6,6 +6,7 @@
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cmath>
 #include <cstdint>
 
@@ -84,24 +85,52 @@ inline bool aligned16(const void *p, const int64_t *strides, int n, int esize)
 
 inline Strides3 strides3(const int64_t *s) { return Strides3{s[0], s[1], s[2]}; }
 
+constexpr int kMaxCacheDevices = 64;
+
+// What a kernel needs set up once on each device (its limit of shared memory holds for the
+// current one only).  A failure is not kept: the next call tries again.  Two threads may come
+// first at once; the set-up then runs twice, to the same end.
+struct PerDevice {
+    std::atomic<bool> ready[kMaxCacheDevices] = {};
+
+    template <typename F>
+    cudaError_t once(F setup)
+    {
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e != cudaSuccess)
+            return e;
+        if (dev < 0 || dev >= kMaxCacheDevices)
+            return cudaErrorInvalidDevice;
+        if (ready[dev].load(std::memory_order_acquire))
+            return cudaSuccess;
+        e = setup();
+        if (e == cudaSuccess)
+            ready[dev].store(true, std::memory_order_release);
+        else
+            cudaGetLastError();
+        return e;
+    }
+};
+
 // SMs of the current device (152, a GB300's, where there is none to ask).
 inline int sm_count()
 {
-    static int cached[64] = {0};
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
+    static std::atomic<int> cached[kMaxCacheDevices] = {};
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxCacheDevices) {
         cudaGetLastError();
         return 152;
     }
-    if (cached[dev] == 0) {
-        int n = 0;
-        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) {
-            cudaGetLastError();
-            return 152;
-        }
-        cached[dev] = n;
+    n = cached[dev].load(std::memory_order_relaxed);
+    if (n > 0)
+        return n;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) {
+        cudaGetLastError();
+        return 152;
     }
-    return cached[dev];
+    cached[dev].store(n, std::memory_order_relaxed);
+    return n;
 }
 
 // One kernel launch; `pdl` makes it a programmatic dependent of the stream's previous kernel

@@ -1319,18 +1319,19 @@ int full_grid(int N) { return sm_count() * (N >= 64 ? 1 : 2); }
 template <typename S, typename T>
 cudaError_t run(const AttnArgs &a, int grid, const CUtensorMap (&maps)[4], cudaStream_t s)
 {
-    static const cudaError_t ready = [] {
+    static PerDevice ready;
+    cudaError_t e = ready.once([] {
         // the roles' shares of registers must not add up to more than the launch gives
         cudaFuncAttributes f;
-        const cudaError_t e = cudaFuncGetAttributes(&f, attention_kernel<S, T>);
-        if (e != cudaSuccess || f.numRegs < S::regs)
-            return e != cudaSuccess ? e : cudaErrorInvalidKernelImage;
+        const cudaError_t got = cudaFuncGetAttributes(&f, attention_kernel<S, T>);
+        if (got != cudaSuccess || f.numRegs < S::regs)
+            return got != cudaSuccess ? got : cudaErrorInvalidKernelImage;
         return cudaFuncSetAttribute(attention_kernel<S, T>,
                                     cudaFuncAttributeMaxDynamicSharedMemorySize, S::smem);
-    }();
-    if (ready != cudaSuccess)
-        return ready;
-    cudaError_t e = launch(attention_kernel<S, T>, dim3(grid), dim3(S::threads), S::smem, s, true,
+    });
+    if (e != cudaSuccess)
+        return e;
+    e = launch(attention_kernel<S, T>, dim3(grid), dim3(S::threads), S::smem, s, true,
                            a, maps[0], maps[1], maps[2], maps[3]);
     if (e != cudaSuccess)
         return e;
@@ -1351,17 +1352,19 @@ cudaError_t run_rows(const AttnArgs &a, int N, int grid, const CUtensorMap (&map
 
 uint32_t *cache_status_word()
 {
-    static uint32_t *word[64] = {nullptr};
+    static std::atomic<uint32_t *> word[kMaxCacheDevices] = {};
     int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64)
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxCacheDevices)
         return nullptr;
-    if (!word[dev]) {
-        void *p = nullptr;
-        if (cudaGetSymbolAddress(&p, g_status) != cudaSuccess)
+    void *p = word[dev].load(std::memory_order_relaxed);
+    if (!p) {
+        if (cudaGetSymbolAddress(&p, g_status) != cudaSuccess) {
+            cudaGetLastError();
             return nullptr;
-        word[dev] = static_cast<uint32_t *>(p);
+        }
+        word[dev].store(static_cast<uint32_t *>(p), std::memory_order_relaxed);
     }
-    return word[dev];
+    return static_cast<uint32_t *>(p);
 }
 
 bool check_queries(const void *q, const int64_t *strides, int dtype, int B, int Lq, int Hq,

@@ -330,11 +330,13 @@ template <int kThreads, int kPerThread, int kCluster>
 cudaError_t launch_select(const EvictArgs &a, int B, cudaStream_t s)
 {
     constexpr int kBytes = sizeof(SelectShared<kThreads, kPerThread, kCluster>);
-    static const cudaError_t ready =
-        cudaFuncSetAttribute(evict_select_kernel<kThreads, kPerThread, kCluster>,
-                             cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
-    if (ready != cudaSuccess)
-        return ready;
+    static PerDevice ready;
+    const cudaError_t e = ready.once([] {
+        return cudaFuncSetAttribute(evict_select_kernel<kThreads, kPerThread, kCluster>,
+                                    cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+    });
+    if (e != cudaSuccess)
+        return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(a.c.heads * kCluster, B);
     cfg.blockDim = dim3(kThreads);

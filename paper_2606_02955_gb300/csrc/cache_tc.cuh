@@ -18,16 +18,19 @@ using EncodeFn = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, vo
 
 inline EncodeFn encode_tiled()
 {
-    static const EncodeFn encode = [] {
-        void *p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000,
-                                             cudaEnableDefault, &q) != cudaSuccess ||
-            q != cudaDriverEntryPointSuccess)
-            return (EncodeFn) nullptr;
-        return reinterpret_cast<EncodeFn>(p);
-    }();
-    return encode;
+    static std::atomic<EncodeFn> encode{nullptr};
+    if (const EncodeFn f = encode.load(std::memory_order_relaxed))
+        return f;
+    void *p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault,
+                                         &q) != cudaSuccess ||
+        q != cudaDriverEntryPointSuccess) {
+        cudaGetLastError();
+        return nullptr;
+    }
+    encode.store(reinterpret_cast<EncodeFn>(p), std::memory_order_relaxed);
+    return reinterpret_cast<EncodeFn>(p);
 }
 
 // One tensor map.  The driver's function wants the device's context current, which a host thread

@@ -475,10 +475,13 @@ int tile_rows(int64_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
 template <typename S, typename T>
 cudaError_t run(const WeighArgs &a, const CUtensorMap &k_map, cudaStream_t s)
 {
-    static const cudaError_t ready = cudaFuncSetAttribute(
-        weigh_kernel<S, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::smem);
-    if (ready != cudaSuccess)
-        return ready;
+    static PerDevice ready;
+    const cudaError_t e = ready.once([] {
+        return cudaFuncSetAttribute(weigh_kernel<S, T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                    S::smem);
+    });
+    if (e != cudaSuccess)
+        return e;
     return launch(weigh_kernel<S, T>, dim3(sm_count() * S::ctas), dim3(S::threads), S::smem, s,
                   true, a, k_map);
 }

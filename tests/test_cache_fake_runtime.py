@@ -1,0 +1,93 @@
+"""The cache's entry points over a stand-in for the CUDA runtime (fake_cudart.cpp): what they set
+up on which device, and what they do when that fails.  No GPU; each case is a process of its own,
+since the library keeps its set-up for the life of one."""
+import os
+import shutil
+import subprocess
+import sys
+
+import pytest
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+
+PRELUDE = """
+import ctypes
+lib, fake = ctypes.CDLL(%r), ctypes.CDLL(%r)
+A16 = 0x10000  # a device pointer that nothing reads
+class Cache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k_codes", "v_codes", "k_affine", "v_affine")] + \
+               [(n, ctypes.c_int) for n in ("pages", "heads", "page_size", "head_dim")]
+def strides(*s):
+    return (ctypes.c_int64 * len(s))(*s)
+p, i, d, sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_double, ctypes.c_size_t
+lib.fdllm_cache_attention.argtypes = [p, p, i, i, i, i, p, p, i, p, p, p, p, p, i, p, i, d, p, p, p, sz, p]
+lib.fdllm_cache_key_weights.argtypes = [p, p, i, i, i, i, p, p, i, p, p, d, p, p, i, p]
+lib.fdllm_cache_evict.argtypes = [p, p, i, i, p, p, i, i, i, i, p, i, p, p, p, p]
+fake.fake_map.restype = ctypes.c_ulonglong
+def cache(**kw):
+    f = dict(k_codes=A16, v_codes=A16, k_affine=A16, v_affine=A16, pages=4, heads=2, page_size=64, head_dim=128)
+    f.update(kw)
+    return Cache(**f)
+def attend(c, Lq, Ln=0):
+    D, h = c.head_dim, c.heads
+    q, k = strides(Lq * h * D, h * D, D), strides(max(Ln, 1) * h * D, h * D, D)
+    new = A16 if Ln else None
+    return lib.fdllm_cache_attention(A16, q, 0, 1, Lq, h, ctypes.byref(c), A16, 4, A16, new, k, new, k, Ln,
+                                     None, 0, 1.0, A16, None, A16, 1 << 40, None)
+def weigh(c, Lq):
+    D, h = c.head_dim, c.heads
+    return lib.fdllm_cache_key_weights(A16, strides(Lq * h * D, h * D, D), 0, 1, Lq, h, ctypes.byref(c), A16, 4,
+                                       A16, A16, 1.0, None, A16, 64, None)
+def evict(c, max_len):
+    return lib.fdllm_cache_evict(ctypes.byref(c), A16, 1, 4, A16, A16, max_len, 8, 0, 0, A16, 1, A16, A16, A16, None)
+def maps():
+    return [tuple([int(fake.fake_map(m, 0, 0))] + [[int(fake.fake_map(m, w, a)) for a in range(int(fake.fake_map(m, 0, 0)))]
+                                                  for w in (1, 2, 3)]) for m in range(fake.fake_maps())]
+"""
+
+
+@pytest.fixture(scope="module")
+def run(cuda_lib_path, tmp_path_factory):
+    nvcc = shutil.which("nvcc") or "/usr/local/cuda/bin/nvcc"
+    include = os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(nvcc))), "include")
+    fake = str(tmp_path_factory.mktemp("fake") / "libfake_cudart.so")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-I", include,
+                    os.path.join(HERE, "fake_cudart.cpp"), "-o", fake], check=True)
+
+    def go(body):
+        code = PRELUDE % (cuda_lib_path, fake) + body
+        r = subprocess.run([sys.executable, "-S", "-c", code], env={**os.environ, "LD_PRELOAD": fake},
+                           capture_output=True, text=True, timeout=120)
+        assert r.returncode == 0, r.stdout + r.stderr
+
+    return go
+
+
+CALLS = ["attend(cache(), 1)", "attend(cache(), 20)", "attend(cache(), 40)", "attend(cache(head_dim=64), 40, 40)",
+         "weigh(cache(), 1)", "weigh(cache(), 40)", "evict(cache(), 1000)", "evict(cache(), 20000)"]
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_every_device_is_set_up(run, call):
+    run("""
+for device in (0, 1, 0, 3):
+    fake.fake_set_device(device)
+    before = fake.fake_launches()
+    assert %s == 0, device
+    assert fake.fake_launches() > before
+""" % call)
+
+
+@pytest.mark.parametrize("call", CALLS)
+@pytest.mark.parametrize("which", [1, 2, 3, 4])
+def test_a_failed_set_up_is_tried_again(run, call, which):
+    """The first, second ... of a first call's set-up steps fails, once (a call that has fewer
+    steps is told nothing)."""
+    run("""
+fake.fake_fail(%d)
+first = %s
+failed = fake.fake_failed()
+assert first == (4 if failed else 0), first
+fake.fake_fail(0)
+assert [%s for _ in range(2)] == [0, 0]
+""" % (which, call, call))
