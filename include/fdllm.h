@@ -383,7 +383,7 @@ typedef struct {
     void *k_affine;  /* bfloat16 [pages, heads, page_size, 2]: (scale, offset)            */
     void *v_affine;  /* bfloat16 [pages, heads, page_size, 2]: (scale, offset)            */
     int pages;
-    int heads;       /* key/value heads                                                   */
+    int heads;       /* key/value heads; pages * heads below 2^31                         */
     int page_size;   /* 32, 64, 128 or 256                                                */
     int head_dim;    /* D: 64 or 128                                                      */
 } fdllm_cache;

@@ -35,7 +35,8 @@ struct Strides3 {
 inline fdllm_status check_cache(const fdllm_cache *c, CacheView &v)
 {
     if (!c || !c->k_codes || !c->v_codes || !c->k_affine || !c->v_affine || c->pages < 1 ||
-        c->heads < 1 || (c->head_dim != 64 && c->head_dim != 128))
+        c->heads < 1 || (c->head_dim != 64 && c->head_dim != 128) ||
+        (int64_t)c->pages * c->heads >= ((int64_t)1 << 31))  // (tensor maps count them in 32 bits)
         return FDLLM_ERR_ARG;
     int shift = 5;
     while (shift < 8 && (1 << shift) != c->page_size)

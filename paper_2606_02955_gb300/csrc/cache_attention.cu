@@ -487,10 +487,10 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     const int i = lane;
                     const int in_page = (t * kKeys + i * span) & (page - 1);
                     const int64_t ph = (int64_t)pg * a.c.heads + h;
-                    tc::tma_load_2d(buf + i * span * (D / 2), &k_map, 0, (int)(ph * page + in_page),
-                                    &bars[kFull + st]);
-                    tc::tma_load_2d(buf + S::code_bytes + i * (span / 2) * D, &v_map, in_page / 2,
-                                    (int)(ph * D), &bars[kFull + st]);
+                    tma_load_3d(buf + i * span * (D / 2), &k_map, 0, in_page, (int)ph,
+                                &bars[kFull + st]);
+                    tma_load_3d(buf + S::code_bytes + i * (span / 2) * D, &v_map, in_page / 2, 0,
+                                (int)ph, &bars[kFull + st]);
                     uint8_t *aff = buf + 2 * S::code_bytes + i * span * 4;
                     bulk_copy_g2s(aff, a.c.ka + ph * page + in_page, span * 4, &bars[kFull + st]);
                     bulk_copy_g2s(aff + 512, a.c.va + ph * page + in_page, span * 4, &bars[kFull + st]);

@@ -76,31 +76,40 @@ inline bool make_rows_map(CUtensorMap *m, const void *base, const Strides3 &s, i
                       CU_TENSOR_MAP_L2_PROMOTION_L2_128B);
 }
 
-// Tensor maps of a cache's codes: keys as rows of D/2 bytes, one box a page's (or a tile's)
-// slots; values as rows of page/2 bytes, one box D channels of up to 128 slots.  The swizzle
-// follows the box's row, so that 16-byte reads of one row a thread meet no bank twice.
+// Tensor maps of a cache's codes, with the page and head as an axis of its own (rows counted
+// over all pages pass 31 bits in a pool of 73 GB): keys as rows of D/2 bytes, one box a page's (or
+// a tile's) slots; values as rows of page/2 bytes, one box D channels of up to 128 slots.  The
+// swizzle follows the box's row, so that 16-byte reads of one row a thread meet no bank twice.
 inline bool make_cache_maps(const CacheView &c, CUtensorMap *k, CUtensorMap *v)
 {
     const int page = 1 << c.page_shift, span = page < 128 ? page : 128;
-    const auto map = [&](CUtensorMap *m, void *base, int64_t inner, int64_t outer, int box_inner,
-                         int box_outer) {
-        const cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)outer};
-        const cuuint64_t strides[1] = {(cuuint64_t)inner};
-        const cuuint32_t box[2] = {(cuuint32_t)box_inner, (cuuint32_t)box_outer};
+    const auto map = [&](CUtensorMap *m, void *base, int inner, int rows, int box_inner,
+                         int box_rows) {
+        const cuuint64_t dims[3] = {(cuuint64_t)inner, (cuuint64_t)rows,
+                                    (cuuint64_t)c.pages * c.heads};
+        const cuuint64_t strides[2] = {(cuuint64_t)inner, (cuuint64_t)inner * rows};
+        const cuuint32_t box[3] = {(cuuint32_t)box_inner, (cuuint32_t)box_rows, 1};
         const CUtensorMapSwizzle sw = box_inner == 64   ? CU_TENSOR_MAP_SWIZZLE_64B
                                       : box_inner == 32 ? CU_TENSOR_MAP_SWIZZLE_32B
                                                         : CU_TENSOR_MAP_SWIZZLE_NONE;
-        return encode_map(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, base, dims, strides, box, sw,
+        return encode_map(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, base, dims, strides, box, sw,
                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
     };
-    const int64_t ph = (int64_t)c.pages * c.heads;
-    if (ph * page >= ((int64_t)1 << 31) || ph * c.D >= ((int64_t)1 << 31))
-        return false;  // box coordinates are 32-bit; such a pool exceeds the GPU's memory
-    return map(k, c.kc, c.D / 2, ph * page, c.D / 2, span) &&
-           (!v || map(v, c.vc, page / 2, ph * c.D, span / 2, c.D));
+    return map(k, c.kc, c.D / 2, page, c.D / 2, span) &&
+           (!v || map(v, c.vc, page / 2, c.D, span / 2, c.D));
 }
 
 #ifdef __CUDACC__
+
+__device__ __forceinline__ void tma_load_3d(void *dst, const CUtensorMap *map, int32_t x, int32_t y,
+                                            int32_t z, uint64_t *bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(smem_addr(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(smem_addr(bar))
+        : "memory");
+}
 
 __device__ __forceinline__ void tma_load_4d(void *dst, const CUtensorMap *map, int32_t x, int32_t y,
                                             int32_t z, int32_t w, uint64_t *bar)

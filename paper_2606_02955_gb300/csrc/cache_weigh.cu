@@ -303,11 +303,11 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     if (mine && !dead) {
                         uint8_t *buf = smem + st * S::stage_bytes;
                         const int in_page = (t * kKeys + lane * span) & (page - 1);
-                        const int64_t row = ((int64_t)pg * a.c.heads + h) * page + in_page;
-                        tc::tma_load_2d(buf + lane * span * (D / 2), &k_map, 0, (int)row,
-                                        &bars[kFull + st]);
-                        bulk_copy_g2s(buf + S::code_bytes + lane * span * 4, a.c.ka + row, span * 4,
-                                      &bars[kFull + st]);
+                        const int64_t ph = (int64_t)pg * a.c.heads + h;
+                        tma_load_3d(buf + lane * span * (D / 2), &k_map, 0, in_page, (int)ph,
+                                    &bars[kFull + st]);
+                        bulk_copy_g2s(buf + S::code_bytes + lane * span * 4,
+                                      a.c.ka + ph * page + in_page, span * 4, &bars[kFull + st]);
                     }
                     __syncwarp();
                 }

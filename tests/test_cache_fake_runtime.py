@@ -91,3 +91,27 @@ assert first == (4 if failed else 0), first
 fake.fake_fail(0)
 assert [%s for _ in range(2)] == [0, 0]
 """ % (which, call, call))
+
+
+@pytest.mark.parametrize("page,D,pages,heads", [
+    (32, 128, (1 << 20) + 1, 16),   # 73 GB: as many rows of channels as 31 bits count
+    (64, 128, (1 << 20) + 1, 16), (32, 64, 1 << 25, 1), (256, 64, 1 << 20, 8), (32, 64, (1 << 31) - 1, 1),
+])
+def test_maps_of_large_pools(run, page, D, pages, heads):
+    """Every axis of a tensor map is within 32-bit coordinates, whatever the pool's size."""
+    run("""
+c = cache(pages=%d, heads=%d, page_size=%d, head_dim=%d)
+assert attend(c, 3) == 0 and weigh(c, 3) == 0
+pages, heads, page, D = %d, %d, %d, %d
+k, v, k2 = maps()
+span = min(page, 128)
+assert k == k2 == (3, [D // 2, page, pages * heads], [D // 2, page * D // 2, 0], [D // 2, span, 1]), k
+assert v == (3, [page // 2, D, pages * heads], [page // 2, page * D // 2, 0], [span // 2, D, 1]), v
+""" % ((pages, heads, page, D) * 2))
+
+
+def test_more_page_heads_than_a_map_counts_are_refused(run):
+    run("""
+c = cache(pages=1 << 28, heads=8)
+assert attend(c, 3) == 1 and weigh(c, 3) == 1 and evict(c, 100) == 1 and fake.fake_launches() == 0
+""")
