@@ -59,7 +59,7 @@ constexpr int kKeys = 128;                // keys of a tile
 constexpr float kFar = -1e30f;            // reference of a row that has seen no key
 constexpr float kTopWeight = 16384.0f;    // largest weight (fp16 holds 65504)
 constexpr float kTopShift = 90.0f;        // a score this far above its reference may overflow
-constexpr float kMaxShift = 120.0f;       // c = 2^(ref - refz) stays below 2^120
+constexpr float kMaxShift = 120.0f;       // c = 2^-refd stays below 2^120
 constexpr int kNever = 0x7FFFFFFF;         // no such key
 constexpr float kSumUnit = 1048576.0f;    // sums over values' codes come in units of 2^-20
 constexpr float kRest = 2048.0f;          // what a weight's rounding left is held times this
@@ -280,12 +280,13 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
     __shared__ int bad_page[2], any_bad[2];
     __shared__ float q_unit[2], q_big[4];
     __shared__ int first_bad[2][D];
-    // per row: the reference (negated), 2^(ref - refz), the queries' sums (by the segment's
-    // parity); -inf, the references of absent keys; the reference of the scaled weights; factors
-    enum { kNref = 0, kCmul = N, kSumq = 2 * N, kNone = 4 * N, kRefz = 5 * N, kFl = 6 * N,
+    // per row: the reference (negated), 2^-refd, the queries' sums (by the segment's
+    // parity); -inf, the references of absent keys; the scaled weights' reference less the row's
+    // (apart, so that references of 2^24 and more leave it its bits); factors
+    enum { kNref = 0, kCmul = N, kSumq = 2 * N, kNone = 4 * N, kRefd = 5 * N, kFl = 6 * N,
            kFo = 7 * N, kRedo = 8 * N, kRowFloats = 9 * N };
     __shared__ __align__(16) float rowf[kRowFloats];
-    float *const nref = rowf + kNref, *const cmul = rowf + kCmul, *const refz = rowf + kRefz;
+    float *const nref = rowf + kNref, *const cmul = rowf + kCmul, *const refd = rowf + kRefd;
     float *const fl = rowf + kFl, *const fo = rowf + kFo, *const redo = rowf + kRedo;
     // by the segment's parity: where a row's results go (in rows of D), their factors (of the
     // sums, and added), and sums of each warp's keys
@@ -895,32 +896,34 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
 #pragma unroll 1
                             for (int c8 = 0; c8 < kCols; c8 += 8) {
                                 float x[8];
-                                auto largest = [&](float more) {
+                                // lane c: column c's largest score, or score over `ref` and more
+                                auto largest = [&](bool over_ref, float ref, float more) {
                                     uint32_t s[8];
                                     tmem_ld<8>(tS + c8, s);
 #pragma unroll
                                     for (int c = 0; c < 8; ++c) {
-                                        const float y = fmaf(__uint_as_float(s[c]), ks,
-                                                             ko * rowf[kSumq + sb * N + col0 + c8 + c]);
-                                        x[c] = c8 + c >= first_col ? y + more : neg_inf_f();
+                                        float y = fmaf(__uint_as_float(s[c]), ks,
+                                                       ko * rowf[kSumq + sb * N + col0 + c8 + c]);
+                                        if (over_ref)
+                                            y = (y - __shfl_sync(0xFFFFFFFFu, ref, c)) + more;
+                                        x[c] = c8 + c >= first_col ? y : neg_inf_f();
                                     }
                                     warp_columns<8>(x, [](float u, float v) { return fmaxf(u, v); });
                                     return x[0] == neg_inf_f()    ? kFar
                                            : fabsf(x[0]) < 1e30f ? x[0]
                                                                  : 0.0f;
                                 };
-                                const float ref = largest(0.0f);
-                                float z = kFar;
+                                const float ref = largest(false, 0.0f, 0.0f);
+                                float z = -kMaxShift;
                                 if (!alike)
-                                    z = largest(lv);
+                                    z = fmaxf(z, largest(true, ref, lv));
                                 else if (big > 0.0f)
-                                    z = ref + log2f(big);
+                                    z = fmaxf(z, log2f(big));
                                 if (lane < 8) {
                                     const int n = col0 + c8 + lane;
-                                    z = fmaxf(z, ref - kMaxShift);
                                     nref[n] = -ref;
-                                    refz[n] = z;
-                                    cmul[n] = ref == kFar ? 1.0f : exp2f(ref - z);
+                                    refd[n] = z;
+                                    cmul[n] = ref == kFar ? 1.0f : exp2f(-z);
                                 }
                             }
                         }
@@ -944,11 +947,14 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                             for (int c = c8; c < c8 + 8; c += 4) {
                                 const float4 nr = lds4f(nr_at + 4 * c);
                                 const float4 cm = lds4f(cols_at + 4 * (kCmul + c));
-                                uint64_t y[2] = {f2(nr.x, nr.y), f2(nr.z, nr.w)};
+                                // (the score first, rounded as the references' are, then less
+                                // its reference: the largest weight is 1 however large scores are)
+                                const uint64_t nr2[2] = {f2(nr.x, nr.y), f2(nr.z, nr.w)};
+                                [[maybe_unused]] uint64_t y[2];
                                 if constexpr (!kOwn) {
                                     const float4 sq = lds4f(sq_at + 4 * c);
-                                    y[0] = fma2(ko2, f2(sq.x, sq.y), y[0]);
-                                    y[1] = fma2(ko2, f2(sq.z, sq.w), y[1]);
+                                    y[0] = mul2(ko2, f2(sq.x, sq.y));
+                                    y[1] = mul2(ko2, f2(sq.z, sq.w));
                                 }
                                 const uint64_t cm2[2] = {f2(cm.x, cm.y), f2(cm.z, cm.w)};
                                 uint64_t rd2[2];
@@ -960,10 +966,16 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                                 for (int e = 0; e < 2; ++e) {
                                     const int i = c / 2 + e;
                                     float y0, y1, z0, z1;
-                                    un2(fma2(f2(__uint_as_float(s[2 * i - c8]),
-                                                __uint_as_float(s[2 * i + 1 - c8])),
-                                             ks2, y[e]),
-                                        y0, y1);
+                                    const uint64_t s2 = f2(__uint_as_float(s[2 * i - c8]),
+                                                           __uint_as_float(s[2 * i + 1 - c8]));
+                                    if constexpr (kOwn) {  // (packed, the two would be fused)
+                                        un2(s2, y0, y1);
+                                        un2(nr2[e], z0, z1);
+                                        y0 = __fadd_rn(__fmul_rn(y0, ks), z0);
+                                        y1 = __fadd_rn(__fmul_rn(y1, ks), z1);
+                                    } else {
+                                        un2(add2(fma2(s2, ks2, y[e]), nr2[e]), y0, y1);
+                                    }
                                     if constexpr (kOwn) {
                                         y0 = 2 * i >= first_col ? y0 : neg_inf_f();
                                         y1 = 2 * i + 1 >= first_col ? y1 : neg_inf_f();
@@ -1016,19 +1028,30 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                             scale_sums<kCols>(lanes + at + col0, nullptr, kSumUnit);
                     if (__builtin_expect(named_sync_or(kBarW + wg, 128, over), 0)) {
                         // ---- the references move: per row, the running maxima of the scores
-                        // and of the scores with the values' scale
+                        // and, over the new one, of the scores with the values' scale
                         const float lv = vs > 0.0f ? log2f(vs) : neg_inf_f();
+                        auto of_warps = [&](int z, int c) {  // the four warps' largest
+                            const int w4 = wg * 4;
+                            return fmaxf(fmaxf(wred[sb][w4][z][c], wred[sb][w4 + 1][z][c]),
+                                         fmaxf(wred[sb][w4 + 2][z][c], wred[sb][w4 + 3][z][c]));
+                        };
 #pragma unroll 1
-                        for (int i = 0; i < kCols / 4; ++i) {  // eight columns, z = i & 1
-                            const int c8 = i / 2 * 8, z = i & 1;
-                            float m[8];
+                        for (int i = 0; i < kCols / 4; ++i) {  // eight columns a turn, z = 0, then 1
+                            const int z = i >= kCols / 8, c8 = (i - z * (kCols / 8)) * 8;
+                            if (i == kCols / 8)
+                                sync();
+                            float to = 0.0f, m[8];
+                            if (z)
+                                to = fmaxf(-nref[col0 + c8 + (lane & 7)], of_warps(0, c8 + (lane & 7)));
                             uint32_t s[8];
                             tmem_ld<8>(tS + c8, s);
 #pragma unroll
                             for (int c = 0; c < 8; ++c) {
-                                const float x = fmaf(__uint_as_float(s[c]), ks,
-                                                     ko * rowf[kSumq + sb * N + col0 + c8 + c]);
-                                m[c] = c8 + c >= first_col ? x + (z ? lv : 0.0f) : neg_inf_f();
+                                float x = fmaf(__uint_as_float(s[c]), ks,
+                                               ko * rowf[kSumq + sb * N + col0 + c8 + c]);
+                                if (z)
+                                    x = (x - __shfl_sync(0xFFFFFFFFu, to, c)) + lv;
+                                m[c] = c8 + c >= first_col ? x : neg_inf_f();
                             }
                             warp_columns<8>(m, [](float x, float y) { return fmaxf(x, y); });
                             if (lane < 8)
@@ -1036,18 +1059,13 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                         }
                         sync();
                         if (key < kCols) {
-                            const int n = col0 + key, w4 = wg * 4, c = key;
-                            float s4 = wred[sb][w4][0][c], z4 = wred[sb][w4][1][c];
-#pragma unroll
-                            for (int i = 1; i < 4; ++i) {
-                                s4 = fmaxf(s4, wred[sb][w4 + i][0][c]);
-                                z4 = fmaxf(z4, wred[sb][w4 + i][1][c]);
-                            }
+                            const int n = col0 + key;
                             const float ref = -nref[n];
-                            const float to_ref = fmaxf(ref, s4);
-                            // where no value has a scale yet, refz follows at a distance
-                            const float z_old = refz[n];
-                            const float to_z = fmaxf(fmaxf(z_old, z4), to_ref - kMaxShift);
+                            const float to_ref = fmaxf(ref, of_warps(0, key));
+                            // where no value has a scale yet, the second reference follows at a
+                            // distance
+                            const float z_old = refd[n] + (ref - to_ref);
+                            const float to_z = fmaxf(fmaxf(z_old, of_warps(1, key)), -kMaxShift);
                             // a row whose weights may have overflowed starts anew with this
                             // tile: what it held weighs less than 2^-60 of what it gets
                             const bool anew = to_ref - ref > kTopShift;
@@ -1055,8 +1073,8 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                             fl[n] = anew ? 0.0f : exp2f(ref - to_ref);
                             fo[n] = exp2f(z_old - to_z);
                             nref[n] = -to_ref;
-                            refz[n] = to_z;
-                            cmul[n] = exp2f(to_ref - to_z);
+                            refd[n] = to_z;
+                            cmul[n] = exp2f(-to_z);
                         }
                         sync();
                         if (t > begin)  // the sums of the tiles before (waited for above)
@@ -1130,7 +1148,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 const bool none = !some || sum == 0.0f;
                 const float ref = none ? kFar : -nref[n];
                 const float f =
-                    none ? 0.0f : exp2f(refz[n] - ref) * (g.last > g.ct ? 1.0f : kSumUnit);
+                    none ? 0.0f : exp2f(refd[n]) * (g.last > g.ct ? 1.0f : kSumUnit);
                 if (whole) {
                     const float inv = none ? 0.0f : 1.0f / sum;
                     fin[sb][n] = make_float2(f * inv, poison ? nan_f() : off * inv);

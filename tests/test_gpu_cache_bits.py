@@ -61,3 +61,34 @@ def test_the_error_is_the_rounding_of_the_result(fd, dtype, Lq, Hq, heads, D, le
     rounding = float((want.to(dtype).double() - want).square().mean().sqrt())
     error = float((out - want).square().mean().sqrt())
     assert error <= 1.01 * rounding, error / rounding
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("Lq", [1, 20, 40])
+@pytest.mark.parametrize("power", [16, 28, 40])
+def test_scores_beyond_the_bits_of_fp32(fd, dtype, Lq, power):
+    """Scores 2^power times 0 to 15: all weight is on the keys of the largest, equally, although a
+    score of this size is rounded to a multiple of many units."""
+    D, n = 64, 300
+    cache, table = ref.make_cache(fd, [n], 1, D, 64, seed=power)
+    code = torch.arange(n) * 7 % 16
+    code[:40] = 3
+    k = torch.zeros(1, n, 1, D)
+    k[0, :, 0, 0], k[..., 1] = code.float(), 15.0  # scale 1, offset 0: held exactly
+    v = gaussian((1, n, 1, D), 1, torch.float32)
+    fd.fdllm_cache_append(cache, table, None, k.cuda(), v)
+    q = torch.zeros(1, Lq, 1, D, dtype=dtype, device="cuda")
+    q[..., 0] = 16.0
+    out, lse = fd.fdllm_cache_attention(q, cache, table, ints([n]), scale=2.0 ** (power - 4), return_lse=True)
+    most = code == 15
+    want, want_lse = ref.values(v)[0, most, 0].mean(0), 15 * 2.0 ** power + math.log(int(most.sum()))
+    reach = float(v.abs().max())
+    assert bool(((out.cpu().double() - want).abs() <= ref.EPS[dtype] * want.abs() + 2.0 ** -18 * reach).all())
+    assert bool(((lse.cpu().double() / want_lse - 1).abs() <= 2.0 ** -20).all())
+    # and as own keys, of which the last outweighs all
+    own = torch.zeros(1, Lq, 1, D, dtype=dtype, device="cuda")
+    own[0, :, 0, 0] = 1.0
+    own[0, -1, 0, 0] = 17.0
+    v_own = gaussian((1, Lq, 1, D), 2, dtype)
+    out = fd.fdllm_cache_attention(q, cache, table, ints([n]), own, v_own, scale=2.0 ** (power - 4))
+    assert torch.equal(out[0, :, 0], v_own[0, -1:, 0].expand(Lq, -1))
