@@ -8,7 +8,9 @@
 //   out_r = (sum_j p_rj vs_j w_j + sum_j p_rj vo_j) / sum_j p_rj,   p_rj = e^(s_rj - m_r).
 // The tensor cores see the codes themselves, exact in fp16; scales and offsets act on the
 // scores and the weights.  Queries enter the first product as fp16 too, times a power of two
-// that brings the tile's largest to 2^13: exact but for elements below 2^-23 of it.
+// that brings the row's largest to 2^13: exact but for elements below 2^-23 of it.  (One power for
+// all rows of a tile took the others' bits where one row's values were 2^20 times theirs, those
+// of a padded position for instance.)
 //
 // Layout.  A tile is 128 keys.  Both products are taken transposed, with the unpacked codes as
 // the A operand in tensor memory, so that the codes go from registers straight to the tensor
@@ -278,13 +280,13 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
     // unit, the first own key with a non-finite value (by channel)
     __shared__ Segment segs[2];
     __shared__ int bad_page[2], any_bad[2];
-    __shared__ float q_unit[2], q_big[4];
     __shared__ int first_bad[2][D];
     // per row: the reference (negated), 2^-refd, the queries' sums (by the segment's
     // parity); -inf, the references of absent keys; the scaled weights' reference less the row's
-    // (apart, so that references of 2^24 and more leave it its bits); factors
+    // (apart, so that references of 2^24 and more leave it its bits); factors;
+    // the queries' units (by the segment's parity)
     enum { kNref = 0, kCmul = N, kSumq = 2 * N, kNone = 4 * N, kRefd = 5 * N, kFl = 6 * N,
-           kFo = 7 * N, kRedo = 8 * N, kRowFloats = 9 * N };
+           kFo = 7 * N, kRedo = 8 * N, kMulq = 9 * N, kRowFloats = 11 * N };
     __shared__ __align__(16) float rowf[kRowFloats];
     float *const nref = rowf + kNref, *const cmul = rowf + kCmul, *const refd = rowf + kRefd;
     float *const fl = rowf + kFl, *const fo = rowf + kFo, *const redo = rowf + kRedo;
@@ -653,43 +655,11 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 wait_u(kFull + (st), (ring / S::stages) & 1);
                 const uint8_t *raw = smem + st * S::stage_bytes;
                 constexpr int kMine = N * (D / 8) / 128;
-                float big = 0.0f;
-#pragma unroll 1
-                for (int m = 0; m < kMine; ++m) {
-                    const int i = tid + m * 128, n = i / (D / 8), c8 = i % (D / 8);
-                    uint4 x = make_uint4(0, 0, 0, 0);
-                    if (n < g.rows)
-                        x = *reinterpret_cast<const uint4 *>(raw + 16 * i);
-                    float f[8], sum = 0.0f;
-                    const uint32_t xw[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        unpack2<T>(xw[e], f[2 * e], f[2 * e + 1]);
-                        sum += f[2 * e] + f[2 * e + 1];
-                    }
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        big = fmaxf(big, fabsf(f[e]) <= 3.4e38f ? fabsf(f[e]) : 0.0f);
-#pragma unroll
-                    for (int s = D / 16; s > 0; s >>= 1)
-                        sum += __shfl_xor_sync(0xFFFFFFFFu, sum, s);
-                    if (c8 == 0)
-                        rowf[kSumq + sb * N + n] = sum;
-                }
-                const uint32_t wbig = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(big));
-                named_sync(kBarU, 128);  // (the segment before has read its own)
-                if (lane == 0)
-                    q_big[warp] = __uint_as_float(wbig);
                 if (tid < D)
                     first_bad[sb][tid] = kNever;
                 if (tid == 0)
                     any_bad[sb] = 0;
                 named_sync(kBarU, 128);
-                big = fmaxf(fmaxf(q_big[0], q_big[1]), fmaxf(q_big[2], q_big[3]));
-                const int e0 = query_exponent(big);
-                const float unit = __uint_as_float((uint32_t)(127 - e0) << 23);
-                if (tid == 0)
-                    q_unit[sb] = __uint_as_float((uint32_t)(127 + e0) << 23);
                 // the operands' last readers are done: the scores of the tile before
                 if (tile > 0)
                     wait_u(kSDone + ((tile - 1) & 1), ((tile - 1) >> 1) & 1);
@@ -699,6 +669,19 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     uint4 x = make_uint4(0, 0, 0, 0);
                     if (n < g.rows)
                         x = *reinterpret_cast<const uint4 *>(raw + 16 * i);
+                    float sum, top;
+                    sum_and_top<T>(x, sum, top);
+#pragma unroll
+                    for (int s = D / 16; s > 0; s >>= 1) {
+                        sum += __shfl_xor_sync(0xFFFFFFFFu, sum, s);
+                        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, s));
+                    }
+                    const int e = query_exponent(top);
+                    const float unit = power_of_two(-e);
+                    if (c8 == 0) {
+                        rowf[kSumq + sb * N + n] = sum * unit;
+                        rowf[kMulq + sb * N + n] = power_of_two(e);
+                    }
                     const int at = (c8 >> 3) * (N * 128) + n * 128 + (((c8 & 7) ^ (n & 7)) << 4);
                     *reinterpret_cast<uint4 *>(smem + S::q16_off + at) = code_queries<T>(x, unit);
                     if (last > ct)
@@ -852,7 +835,6 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 const int end = kOwn ? g.own : g.cached;
                 const int base = kOwn ? g.ct : 0;
                 constexpr int step = kOwn ? kOwnKeys : kKeys;
-                float k_factor = 0.0f;  // (the queries' unit is there with the first scores)
 #pragma unroll 1
                 for (int t = from; t < to; ++t) {
                     const int keys = min(step, end - (t - base) * step);
@@ -860,8 +842,6 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     const uint32_t tS = lanes + S::tS + (seen & 1) * N + col0;
                     wait(kSDone + (seen & 1), (seen >> 1) & 1);
                     tc::fence_after_sync();
-                    if (!kOwn && t == from)
-                        k_factor = a.scale * q_unit[sb];
                     // this thread's key: scale and offset, for scores and weights
                     const int j = (t - base) * step + key;
                     const bool valid = key < keys;
@@ -869,7 +849,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     if constexpr (!kOwn) {
                         const uint32_t f = buf0 + st * S::stage_bytes + 2 * S::code_bytes + 4 * key;
                         const uint32_t fk = lds1(f), fv = lds1(f + 4 * kKeys);
-                        ks = bf16_low(fk) * k_factor;
+                        ks = bf16_low(fk) * a.scale;
                         ko = fmaf(8.0f, bf16_low(fk), bf16_high(fk)) * a.scale;
                         vs = bf16_low(fv);
                         vo = fmaf(key & 1 ? 15.0f : 0.0f, vs, bf16_high(fv));
@@ -878,6 +858,14 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     }
                     // values' codes of odd slots are 16 times as large: their weights are not
                     const float vw = kOwn || (key & 1) ? vs : 16.0f * vs;
+                    // a score of this key, as the weights' are computed (times a power of two)
+                    auto score = [&](uint32_t s, int c) {
+                        if constexpr (kOwn)
+                            return __fmul_rn(__uint_as_float(s), ks);
+                        else
+                            return fmaf(__uint_as_float(s), ks, ko * rowf[kSumq + sb * N + col0 + c]) *
+                                   rowf[kMulq + sb * N + col0 + c];
+                    };
                     // the rows of this thread that see its key: those from first_col on
                     const int first_col = !valid || (kOwn && a.causal && j >= a.Lq) ? kCols
                                           : kOwn && a.causal ? j * a.group - (g.r0 + col0)
@@ -902,8 +890,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                                     tmem_ld<8>(tS + c8, s);
 #pragma unroll
                                     for (int c = 0; c < 8; ++c) {
-                                        float y = fmaf(__uint_as_float(s[c]), ks,
-                                                       ko * rowf[kSumq + sb * N + col0 + c8 + c]);
+                                        float y = score(s[c], c8 + c);
                                         if (over_ref)
                                             y = (y - __shfl_sync(0xFFFFFFFFu, ref, c)) + more;
                                         x[c] = c8 + c >= first_col ? y : neg_inf_f();
@@ -936,6 +923,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                         constexpr bool kAgain = decltype(again)::value;
                         const uint32_t nr_at = valid ? cols_at + 4 * kNref : cols_at + 4 * kNone;
                         [[maybe_unused]] const uint32_t sq_at = cols_at + 4 * (kSumq + sb * N);
+                        [[maybe_unused]] const uint32_t mq_at = cols_at + 4 * (kMulq + sb * N);
                         const uint64_t ks2 = f2(ks, ks), ko2 = f2(ko, ko);
                         const uint64_t vw2 = f2(vw, vw), vo2 = f2(vo, vo);
                         float top = 0.0f;
@@ -950,8 +938,10 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                                 // (the score first, rounded as the references' are, then less
                                 // its reference: the largest weight is 1 however large scores are)
                                 const uint64_t nr2[2] = {f2(nr.x, nr.y), f2(nr.z, nr.w)};
-                                [[maybe_unused]] uint64_t y[2];
+                                [[maybe_unused]] uint64_t y[2], mq2[2];
                                 if constexpr (!kOwn) {
+                                    const float4 mq = lds4f(mq_at + 4 * c);
+                                    mq2[0] = f2(mq.x, mq.y), mq2[1] = f2(mq.z, mq.w);
                                     const float4 sq = lds4f(sq_at + 4 * c);
                                     y[0] = mul2(ko2, f2(sq.x, sq.y));
                                     y[1] = mul2(ko2, f2(sq.z, sq.w));
@@ -974,7 +964,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                                         y0 = __fadd_rn(__fmul_rn(y0, ks), z0);
                                         y1 = __fadd_rn(__fmul_rn(y1, ks), z1);
                                     } else {
-                                        un2(add2(fma2(s2, ks2, y[e]), nr2[e]), y0, y1);
+                                        un2(fma2(fma2(s2, ks2, y[e]), mq2[e], nr2[e]), y0, y1);
                                     }
                                     if constexpr (kOwn) {
                                         y0 = 2 * i >= first_col ? y0 : neg_inf_f();
@@ -1047,8 +1037,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                             tmem_ld<8>(tS + c8, s);
 #pragma unroll
                             for (int c = 0; c < 8; ++c) {
-                                float x = fmaf(__uint_as_float(s[c]), ks,
-                                               ko * rowf[kSumq + sb * N + col0 + c8 + c]);
+                                float x = score(s[c], c8 + c);
                                 if (z)
                                     x = (x - __shfl_sync(0xFFFFFFFFu, to, c)) + lv;
                                 m[c] = c8 + c >= first_col ? x : neg_inf_f();

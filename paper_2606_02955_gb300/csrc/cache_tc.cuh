@@ -228,12 +228,33 @@ __device__ __forceinline__ uint4 interleave8(const uint4 x)
                       __byte_perm(x.y, x.w, 0x5410), __byte_perm(x.y, x.w, 0x7632));
 }
 
-// Queries against codes: fp16, times a power of two 2^-e that brings the largest of them to 2^13
+// Queries against codes: fp16, times a power of two 2^-e that brings the row's largest to 2^13
 // (0: 1), and 2^-4 in odd channels.  e from the largest; clamped so that 2^e and 2^-e exist.
 __device__ __forceinline__ int query_exponent(float big)
 {
     const int e = big > 0.0f ? (int)(__float_as_uint(big) >> 23) - 127 - 13 : 0;
     return min(max(e, -100), 100);
+}
+
+__device__ __forceinline__ float power_of_two(int e)  // of a normal number
+{
+    return __uint_as_float((uint32_t)(127 + e) << 23);
+}
+
+// Of eight channels of a query: their sum, and the largest finite one's size.
+template <typename T>
+__device__ __forceinline__ void sum_and_top(const uint4 x, float &sum, float &top)
+{
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    sum = top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float lo, hi;
+        unpack2<T>(w[i], lo, hi);
+        sum += lo + hi;
+        top = fmaxf(top, fabsf(lo) <= 3.4e38f ? fabsf(lo) : 0.0f);
+        top = fmaxf(top, fabsf(hi) <= 3.4e38f ? fabsf(hi) : 0.0f);
+    }
 }
 
 // Eight channels of a query, in the operand's order; unit = 2^-e.

@@ -99,9 +99,9 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
     __shared__ int64_t scan[S::threads / 32];
     __shared__ int64_t find_base;
     __shared__ int find_b;
-    __shared__ float q_big[8];
-    // of the queries held: sum of the channels; -lse in base 2 (-inf: the row counts nothing)
-    __shared__ __align__(16) float sumq[S::group * N], nlse[S::group * N];
+    // of the queries held: sum of the channels; their unit; -lse in base 2 (-inf: the row counts
+    // nothing)
+    __shared__ __align__(16) float sumq[S::group * N], mulq[S::group * N], nlse[S::group * N];
 
     const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31;
     if (tid == 0) {
@@ -156,8 +156,8 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
     pdl_launch_dependents();
 
     uint32_t bar0 = smem_addr(bars), buf0 = smem_addr(smem), sum0 = smem_addr(sumq),
-             lse0 = smem_addr(nlse);
-    asm volatile("" : "+r"(bar0), "+r"(buf0), "+r"(sum0), "+r"(lse0));
+             mul0 = smem_addr(mulq), lse0 = smem_addr(nlse);
+    asm volatile("" : "+r"(bar0), "+r"(buf0), "+r"(sum0), "+r"(mul0), "+r"(lse0));
     auto bar = [&](int i) { return bar0 + 8u * i; };
     bool dead = false;  // a wait gave up: no further wait, the walk goes on to its end
     auto wait = [&](auto sleep, int i, uint32_t parity) {
@@ -195,21 +195,15 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
     constexpr int kHeld = S::group * N;
 
     // Rows [g0, g0 + held) of the queries into the operand, by the unpacking and the weighing
-    // warps together: as they are, with their sums and the largest, then in place times a power
-    // of two (the exponent of which is returned).  Their -lse lose the whole number `shift`, near
-    // all of them as a rule, so that the small differences of large scores keep their bits.
-    auto hold_queries = [&](int g0, int held, float &shift) -> int {
+    // warps together: times a power of two of each row, with their sums in that unit.  Their -lse
+    // lose the whole number `shift`, near all of them as a rule, so that the small differences of
+    // large scores keep their bits.
+    auto hold_queries = [&](int g0, int held, float &shift) {
         const int chunks = (held + N - 1) / N * N * (D / 8);  // of 8 channels
-        const auto place = [&](int i) {
-            const int r = i / (D / 8), c8 = i % (D / 8), m = r % N;
-            return smem + S::q_off + r / N * S::q_bytes + (c8 >> 3) * (N * 128) + m * 128 +
-                   (((c8 & 7) ^ (m & 7)) << 4);
-        };
         named_sync(kBarW, 256);
-        float big = 0.0f;
 #pragma unroll 4
         for (int i = tid; i < chunks; i += 256) {
-            const int r = i / (D / 8), c8 = i % (D / 8);
+            const int r = i / (D / 8), c8 = i % (D / 8), m = r % N;
             uint4 x = make_uint4(0, 0, 0, 0);
             if (r < held) {
                 const int qi = (g0 + r) / a.group, g = (g0 + r) - qi * a.group;
@@ -217,22 +211,22 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     static_cast<const T *>(a.q) + b * a.qs.batch + qi * a.qs.token +
                     (int64_t)(h * a.group + g) * a.qs.head + 8 * c8);
             }
-            *reinterpret_cast<uint4 *>(place(i)) = x;
-            const uint32_t xw[4] = {x.x, x.y, x.z, x.w};
-            float sum = 0.0f;
+            float sum, top;
+            sum_and_top<T>(x, sum, top);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float lo, hi;
-                unpack2<T>(xw[e], lo, hi);
-                sum += lo + hi;
-                big = fmaxf(big, fabsf(lo) <= 3.4e38f ? fabsf(lo) : 0.0f);
-                big = fmaxf(big, fabsf(hi) <= 3.4e38f ? fabsf(hi) : 0.0f);
+            for (int s = D / 16; s > 0; s >>= 1) {
+                sum += __shfl_xor_sync(0xFFFFFFFFu, sum, s);
+                top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, s));
             }
-#pragma unroll
-            for (int m = D / 16; m > 0; m >>= 1)
-                sum += __shfl_xor_sync(0xFFFFFFFFu, sum, m);
-            if (c8 == 0)
-                sumq[r] = sum;
+            const int e = query_exponent(top);
+            const float unit = power_of_two(-e);
+            if (c8 == 0) {
+                sumq[r] = sum * unit;
+                mulq[r] = power_of_two(e);
+            }
+            *reinterpret_cast<uint4 *>(smem + S::q_off + r / N * S::q_bytes + (c8 >> 3) * (N * 128) +
+                                       m * 128 + (((c8 & 7) ^ (m & 7)) << 4)) =
+                code_queries<T>(x, unit);
         }
         const auto lse_of = [&](int r) {
             const int qi = (g0 + r) / a.group, g = (g0 + r) - qi * a.group;
@@ -249,24 +243,8 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
             }
             nlse[r] = x;
         }
-        const uint32_t wbig = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(big));
-        if (lane == 0)
-            q_big[warp] = __uint_as_float(wbig);
-        named_sync(kBarW, 256);
-        big = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            big = fmaxf(big, q_big[i]);
-        const int e0 = query_exponent(big);
-        const float unit = __uint_as_float((uint32_t)(127 - e0) << 23);
-#pragma unroll 4
-        for (int i = tid; i < chunks; i += 256) {
-            uint4 *x = reinterpret_cast<uint4 *>(place(i));
-            *x = code_queries<T>(*x, unit);
-        }
         fence_async_smem();
         named_sync(kBarW, 256);
-        return e0;
     };
     const int page = 1 << a.c.page_shift;
     const int span = min(page, kKeys);  // slots of a page in a tile
@@ -396,9 +374,8 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
             for (int g0 = 0; g0 < a.rows; g0 += kHeld) {
                 const int held = min(kHeld, a.rows - g0);
                 float shift;
-                const int e0 = hold_queries(g0, held, shift);
+                hold_queries(g0, held, shift);
                 const uint64_t shift2 = f2(shift, shift);
-                const float k_factor = a.scale * __uint_as_float((uint32_t)(127 + e0) << 23);
                 for (int t = first; t < last; ++t, ++ring) {
                     const uint32_t st = ring % S::stages;
                     const int j = t * kKeys + key;
@@ -417,7 +394,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                         if (r == 0) {
                             const uint32_t f = lds1(buf0 + st * S::stage_bytes + S::code_bytes +
                                                     4 * key);
-                            ks = bf16_low(f) * k_factor;
+                            ks = bf16_low(f) * a.scale;
                             ko = fmaf(8.0f, bf16_low(f), bf16_high(f)) * a.scale;
                             bad = (bad_pieces[st] >> (key / span)) & 1;
                             __syncwarp();
@@ -436,17 +413,18 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
 #pragma unroll
                             for (int c = 0; c < 16; c += 4) {
                                 const float4 sq = lds4f(sum0 + 4 * (r * N + c16 + c));
+                                const float4 mq = lds4f(mul0 + 4 * (r * N + c16 + c));
                                 const float4 nl = lds4f(lse0 + 4 * (r * N + c16 + c));
 #pragma unroll
                                 for (int e = 0; e < 2; ++e) {
                                     const uint64_t y = fma2(
                                         f2(__uint_as_float(s[c + 2 * e]),
                                            __uint_as_float(s[c + 2 * e + 1])),
-                                        ks2,
-                                        fma2(ko2, e ? f2(sq.z, sq.w) : f2(sq.x, sq.y),
-                                             e ? f2(nl.z, nl.w) : f2(nl.x, nl.y)));
+                                        ks2, mul2(ko2, e ? f2(sq.z, sq.w) : f2(sq.x, sq.y)));
                                     float y0, y1;
-                                    un2(add2(y, shift2), y0, y1);
+                                    un2(add2(fma2(y, e ? f2(mq.z, mq.w) : f2(mq.x, mq.y), shift2),
+                                             e ? f2(nl.z, nl.w) : f2(nl.x, nl.y)),
+                                        y0, y1);
                                     sum2 = add2(sum2, f2(ex2_mufu(y0), ex2_mufu(y1)));
                                 }
                             }

@@ -10,7 +10,7 @@ import pytest
 import torch
 
 import cache_ref as ref
-from test_gpu_cache_attention import gaussian, ints
+from test_gpu_cache_attention import check, gaussian, ints
 
 pytestmark = pytest.mark.gpu
 
@@ -92,3 +92,32 @@ def test_scores_beyond_the_bits_of_fp32(fd, dtype, Lq, power):
     v_own = gaussian((1, Lq, 1, D), 2, dtype)
     out = fd.fdllm_cache_attention(q, cache, table, ints([n]), own, v_own, scale=2.0 ** (power - 4))
     assert torch.equal(out[0, :, 0], v_own[0, -1:, 0].expand(Lq, -1))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("Lq,Hq,heads,D,lens", [
+    (1, 8, 1, 128, [300, 65]), (16, 4, 2, 64, [130, 257]), (40, 4, 1, 128, [700]), (150, 4, 2, 128, [513, 130]),
+])
+def test_rows_of_very_different_sizes_do_not_mix(fd, dtype, Lq, Hq, heads, D, lens):
+    """A few queries are 2^24 to 2^26 times as large as the others of their head: the others'
+    scores keep the bits that they have alone."""
+    B = len(lens)
+    cache, table = ref.make_cache(fd, lens, heads, D, 64, seed=D + Lq)
+    small = 1.0 if dtype is torch.bfloat16 else 2.0 ** -14
+    q = gaussian((B, Lq, Hq, D), 1, torch.float32, 1.5) * small
+    q[:, ::13, 1] *= 2.0 ** (24 if dtype is torch.bfloat16 else 26)
+    q[:, 0, 2] = 0.0
+    q = q.to(dtype)
+    scale = D ** -0.5 / small
+    k, v = gaussian((B, Lq, heads, D), 2, dtype, 0.2), gaussian((B, Lq, heads, D), 3, dtype)
+    for own in (dict(), dict(k_new=k, v_new=v)):
+        _, lse = check(fd, q, cache, table, lens, scale=scale, **own)
+    # (against the cached keys alone, so that the weights of every query sum to 1)
+    _, lse = check(fd, q, cache, table, lens, scale=scale)
+    w = torch.zeros(B, heads, table.shape[1] * 64, device="cuda")
+    # (a log-sum-exp of 2^24 holds weights to a factor of e: those rows are left out)
+    big = q.abs().amax(-1).float() > 1e3 * small
+    alone = fd.fdllm_cache_key_weights(q, torch.where(big, -math.inf, lse), cache, table, ints(lens),
+                                       weights=w, scale=scale)
+    want, tol = ref.key_weights(q, torch.where(big, -math.inf, lse), cache, table, lens, w, scale=scale)
+    assert bool(((alone.cpu().double() - want).abs() <= tol).all())
