@@ -481,7 +481,7 @@ size_t fdllm_cache_attention_workspace_bytes(int B, int Lq, int Hq, int heads, i
  * for j < cache_lens[b], and 0 from there to max_len - 1.
  *   q, cache, block_table, cache_lens, scale   as in fdllm_cache_attention.
  *   lse          [B, Lq, Hq] fp32, contiguous: fdllm_cache_attention's out_lse (a row of -inf
- *                counts as 0: it saw no key).
+ *                counts as 0, whatever its queries hold: it saw no key, or is padding).
  *   weights_in   [B, heads, max_len] fp32 or NULL (0); weights_out the same shape, may be
  *                weights_in.
  * Deterministic (no atomics).  A sequence whose length is negative, past the table or past

@@ -198,7 +198,12 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
     // warps together: times a power of two of each row, with their sums in that unit.  Their -lse
     // lose the whole number `shift`, near all of them as a rule, so that the small differences of
     // large scores keep their bits.
+    // A row whose -lse is infinite counts nothing, whatever it holds: its queries are taken as 0.
     auto hold_queries = [&](int g0, int held, float &shift) {
+        const auto lse_of = [&](int r) {
+            const int qi = (g0 + r) / a.group, g = (g0 + r) - qi * a.group;
+            return a.lse[((int64_t)b * a.Lq + qi) * a.Hq + h * a.group + g];
+        };
         const int chunks = (held + N - 1) / N * N * (D / 8);  // of 8 channels
         named_sync(kBarW, 256);
 #pragma unroll 4
@@ -210,6 +215,8 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 x = *reinterpret_cast<const uint4 *>(
                     static_cast<const T *>(a.q) + b * a.qs.batch + qi * a.qs.token +
                     (int64_t)(h * a.group + g) * a.qs.head + 8 * c8);
+                if (lse_of(r) == neg_inf_f())
+                    x = make_uint4(0, 0, 0, 0);
             }
             float sum, top;
             sum_and_top<T>(x, sum, top);
@@ -228,10 +235,6 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                                        m * 128 + (((c8 & 7) ^ (m & 7)) << 4)) =
                 code_queries<T>(x, unit);
         }
-        const auto lse_of = [&](int r) {
-            const int qi = (g0 + r) / a.group, g = (g0 + r) - qi * a.group;
-            return a.lse[((int64_t)b * a.Lq + qi) * a.Hq + h * a.group + g];
-        };
         const float l0 = lse_of(0);
         shift = fabsf(l0) < 1e6f ? rintf(-l0 * kLog2e) : 0.0f;
         for (int r = tid; r < kHeld; r += 256) {
