@@ -519,6 +519,11 @@ fdllm_status fdllm_cache_evict(const fdllm_cache *cache, const int32_t *block_ta
  * otherwise, and clears it. */
 fdllm_status fdllm_cache_status(void *stream);
 
+/* Health check of those kernels' bounded waits: enqueues a warp that waits on a barrier nobody
+ * completes and gives up after `tries` tries (1 to 2^18; 0: the kernels' own limit, about a
+ * second), so that fdllm_cache_status reports FDLLM_ERR_DEVICE once. */
+fdllm_status fdllm_cache_check_wait(int tries, void *stream);
+
 /* Health check of the library's failure detection: every wait inside the kernels is
  * bounded, and a wait that runs out records a device error and lets the kernel return
  * instead of hanging.  This launches one thread that waits on a barrier nobody completes,

@@ -30,6 +30,7 @@ __all__ = [
     "KvCache", "fdllm_qk_norm_rope", "fdllm_cache_append", "fdllm_cache_read",
     "fdllm_cache_attention", "fdllm_cache_attention_workspace_bytes",
     "fdllm_cache_key_weights", "fdllm_cache_evict", "fdllm_cache_status",
+    "fdllm_cache_check_wait",
 ]
 
 BF16, FP32, FP16 = 0, 1, 2
@@ -106,6 +107,8 @@ def _load():
     lib.fdllm_cache_evict.restype = i
     lib.fdllm_cache_status.argtypes = [p]
     lib.fdllm_cache_status.restype = i
+    lib.fdllm_cache_check_wait.argtypes = [i, p]
+    lib.fdllm_cache_check_wait.restype = i
     lib.fdllm_check_bounded_wait.argtypes = [d, p]
     lib.fdllm_check_bounded_wait.restype = i
     lib.fdllm_device_status.argtypes = [p]
@@ -875,6 +878,13 @@ def fdllm_cache_status(stream=None) -> int:
     """Synchronises and returns (clearing it) the sticky device status of the cache's attention
     and key-weight kernels on the current device."""
     return _load().fdllm_cache_status(_stream(stream))
+
+
+def fdllm_cache_check_wait(tries: int = 0, stream=None) -> int:
+    """Enqueues a warp of the cache kernels' kind that waits on a barrier nobody completes and
+    gives up after ``tries`` tries (0: the kernels' own limit); fdllm_cache_status then reports
+    FDLLM_ERR_DEVICE (6) once.  Returns the status code of the launch."""
+    return _load().fdllm_cache_check_wait(tries, _stream(stream))
 
 
 def fdllm_check_bounded_wait(seconds: float = 0.01, stream=None) -> int:

@@ -1214,6 +1214,19 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
         tc::tmem_dealloc(tmem, S::tmem);
 }
 
+// One warp waits on a barrier that nobody completes, as the kernels' warps wait.
+__global__ void wait_probe_kernel(uint32_t *status, uint32_t tries)
+{
+    __shared__ __align__(8) uint64_t bar;
+    if (threadIdx.x == 0) {
+        mbar_init(&bar, 1);
+        fence_mbar_init();
+    }
+    __syncthreads();
+    if (!mbar_wait_at<20>(smem_addr(&bar), 0, tries))
+        atomicOr(status, kDevStatTimeout);
+}
+
 // Joins the partials of the unit that CTA blockIdx.x of the attention began and did not finish:
 // its slot 1, then slot 0 of the CTAs after it up to the one where the unit ends.  A warp takes a
 // row, a lane D / 32 channels; the parts' factors are computed a lane each.
@@ -1476,6 +1489,18 @@ fdllm_status fdllm_cache_attention(const void *q, const int64_t *q_strides, int 
                        : run_rows<128, __half>(a, N, grid, maps, s))
                  : (bf ? run_rows<64, __nv_bfloat16>(a, N, grid, maps, s)
                        : run_rows<64, __half>(a, N, grid, maps, s));
+    return e == cudaSuccess ? FDLLM_OK : FDLLM_ERR_CUDA;
+}
+
+fdllm_status fdllm_cache_check_wait(int tries, void *stream)
+{
+    if (tries < 0 || tries > (int)kWaitTries)
+        return FDLLM_ERR_ARG;
+    uint32_t *word = cache_status_word();
+    if (!word)
+        return FDLLM_ERR_CUDA;
+    const cudaError_t e = launch(wait_probe_kernel, dim3(1), dim3(32), 0, static_cast<cudaStream_t>(stream),
+                                 false, word, tries > 0 ? (uint32_t)tries : kWaitTries);
     return e == cudaSuccess ? FDLLM_OK : FDLLM_ERR_CUDA;
 }
 

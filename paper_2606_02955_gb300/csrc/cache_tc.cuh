@@ -395,12 +395,13 @@ __device__ __forceinline__ void fence_async_smem()
 
 // Waits on a shared-memory address, a few instructions each: many places of a kernel wait, and
 // code that does not fit the instruction cache costs its warps more than the waits (with a timer at
-// each place 64 blocks' attention took 195 us instead of 143).  The limit is a count of tries, of
-// 20 ns at the least and kSleepNs: a fraction of a second or more, where a wait takes microseconds.
+// each place 64 blocks' attention took 195 us instead of 143).  The limit is a count of tries; a
+// try on a barrier that does not complete takes the hardware's 4 us (measured), so that 2^18 of
+// them are a second, where a wait takes microseconds.
 // kSleepNs: a warp that waits most of its time sleeps between tries, which would take issue slots
 // from the warps that work.  False: given up; the caller waits no more, and says so in the status
 // word.
-constexpr uint32_t kWaitTries = 1u << 23, kDrainTries = 1u << 20;
+constexpr uint32_t kWaitTries = 1u << 18, kDrainTries = 1u << 15;
 
 __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
 {
