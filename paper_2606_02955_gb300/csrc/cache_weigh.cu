@@ -159,7 +159,9 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
              mul0 = smem_addr(mulq), lse0 = smem_addr(nlse);
     asm volatile("" : "+r"(bar0), "+r"(buf0), "+r"(sum0), "+r"(mul0), "+r"(lse0));
     auto bar = [&](int i) { return bar0 + 8u * i; };
-    bool dead = false;  // a wait gave up: no further wait, the walk goes on to its end
+    // A wait gave up: no further wait.  The loading and the issuing warp stop at once and wait, with
+    // a limit, for what they have in flight; the others walk on to the end of their range.
+    bool dead = false;
     auto wait = [&](auto sleep, int i, uint32_t parity) {
         if (!dead && !mbar_wait_at<decltype(sleep)::value>(bar(i), parity))
             dead = true;
@@ -256,8 +258,8 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
         // ---------------------------------------------------------------- the loading warp
         uint32_t ring = 0;
         const int pieces = kKeys / span;
-        while (next())
-            for (int g0 = 0; g0 < a.rows; g0 += kHeld) {
+        while (!dead && next())
+            for (int g0 = 0; g0 < a.rows && !dead; g0 += kHeld) {
                 int pg_lane = -1;
                 for (int t = first; t < last; ++t, ++ring) {
                     const int batch = (t - first) * pieces;
@@ -268,20 +270,22 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                     const uint32_t st = ring % S::stages;
                     wait(Long{}, kEmpty + st, ((ring / S::stages) & 1) ^ 1);
                     dead = __any_sync(0xFFFFFFFFu, dead);
+                    if (dead)
+                        break;
                     const int pg = __shfl_sync(0xFFFFFFFFu, pg_lane, (batch & 31) + (lane & 3));
                     const bool mine = lane < pieces && pg >= 0;
                     const uint32_t there = __ballot_sync(0xFFFFFFFFu, mine);
                     const uint32_t bad = __ballot_sync(0xFFFFFFFFu, lane < pieces && pg == -1);
                     if (lane == 0) {
                         bad_pieces[st] = (uint8_t)bad;
-                        if (!dead && there)
+                        if (there)
                             mbar_arrive_expect_tx(&bars[kFull + st],
                                                   (uint32_t)__popc(there) * span * (D / 2 + 4));
-                        else if (!dead)
+                        else
                             mbar_arrive(&bars[kFull + st]);
                     }
                     __syncwarp();
-                    if (mine && !dead) {
+                    if (mine) {
                         uint8_t *buf = smem + st * S::stage_bytes;
                         const int in_page = (t * kKeys + lane * span) & (page - 1);
                         const int64_t ph = (int64_t)pg * a.c.heads + h;
@@ -303,21 +307,25 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
     } else if (warp == S::issuer) {
         // ---------------------------------------------------------------- the issuing warp
         const uint64_t q_desc = tc::sw128_kmajor_desc(smem + S::q_off);
-        uint32_t scores = 0, ring = 0;
+        uint32_t scores = 0, ring = 0, freed = 0;
         auto wait_warp = [&](int i, uint32_t parity) {
             wait(Now{}, i, parity);
             dead = __any_sync(0xFFFFFFFFu, dead);
         };
-        while (next())
-            for (int g0 = 0; g0 < a.rows; g0 += kHeld) {
+        while (!dead && next())
+            for (int g0 = 0; g0 < a.rows && !dead; g0 += kHeld) {
                 const int held = min(kHeld, a.rows - g0);
-                for (int t = first; t < last; ++t, ++ring) {
+                for (int t = first; t < last && !dead; ++t, ++ring) {
                     wait_warp(kKReady, ring & 1);
+                    if (dead)
+                        break;
                     tc::fence_after_sync();
                     for (int r = 0; r * N < held; ++r, ++scores) {
                         const uint32_t par = scores & 1;
                         if (scores >= 2)
                             wait_warp(kSFree + par, ((scores - 2) >> 1) & 1);
+                        if (dead)
+                            break;
                         tc::fence_after_sync();
 #pragma unroll
                         for (int k = 0; k < D / 16; ++k)
@@ -328,8 +336,15 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                         mma_commit(&bars[kSDone + par]);
                     }
                     mma_commit(&bars[kKFree]);
+                    ++freed;
                 }
             }
+        // Nor may a product read or write what this CTA gives back: the last of them.
+        const uint32_t tries = dead ? kDrainTries : kWaitTries;
+        if (scores > 0 && !mbar_wait_at<0>(bar(kSDone + ((scores - 1) & 1)), ((scores - 1) >> 1) & 1, tries))
+            dead = true;
+        if (freed > 0 && !mbar_wait_at<0>(bar(kKFree), (freed - 1) & 1, tries))
+            dead = true;
     } else if (warp < 4) {
         // ---------------------------------------------------------------- the unpacking warps
         const int key = tid;
