@@ -361,8 +361,9 @@ fdllm_status fdllm_profile_terms(const float *conf, const uint8_t *mask, int B, 
  * receives (fdllm_cache_key_weights) and drop the keys that receive little
  * (fdllm_cache_evict).  fdllm_qk_norm_rope makes the queries and keys that enter it.  All of
  * them are asynchronous on `stream`, allocate nothing, use no library workspace and may be
- * captured into a CUDA graph (the forward pass of fdllm_decode_loop, for instance).  They are
- * forms for inference and have no gradients.
+ * captured into a CUDA graph (in the forward pass of fdllm_decode_loop, for instance); the first
+ * call of each with a head size, dtype and range of lengths sets its kernel up on the device and
+ * must come before a capture.  They are forms for inference and have no gradients.
  *
  * A row of D values (one token's keys, or values, of one head) is held as 4-bit codes with
  * two bfloat16 numbers, value = offset + scale * code:

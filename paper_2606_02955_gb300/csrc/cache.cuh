@@ -135,7 +135,7 @@ inline int sm_count()
 }
 
 // One kernel launch; `pdl` makes it a programmatic dependent of the stream's previous kernel
-// (the kernel then waits with pdl_wait() before it touches memory).
+// (the kernel then waits with pdl_wait() before it touches memory), but for plain_launches.
 template <typename... P, typename... A>
 cudaError_t launch(void (*kern)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream,
                    bool pdl, A... args)
@@ -149,7 +149,7 @@ cudaError_t launch(void (*kern)(P...), dim3 grid, dim3 block, size_t smem, cudaS
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = pdl ? 1 : 0;
+    cfg.numAttrs = pdl && !plain_launches ? 1 : 0;
     return cudaLaunchKernelEx(&cfg, kern, P(args)...);
 }
 

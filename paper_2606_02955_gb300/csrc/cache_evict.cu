@@ -343,12 +343,12 @@ cudaError_t launch_select(const EvictArgs &a, int B, cudaStream_t s)
     cfg.dynamicSmemBytes = kBytes;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim = {kCluster, 1, 1};
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim = {kCluster, 1, 1};
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = kCluster > 1 ? 2 : 1;
+    cfg.numAttrs = plain_launches ? 1 : 2;
     return cudaLaunchKernelEx(&cfg, evict_select_kernel<kThreads, kPerThread, kCluster>, a);
 }
 

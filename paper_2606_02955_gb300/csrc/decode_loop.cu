@@ -12,6 +12,9 @@
 #include "fdllm_internal.cuh"
 
 namespace fdllm {
+
+thread_local bool plain_launches = false;
+
 namespace {
 
 // Why the loop stopped before the generation finished (LoopState::stop_reason).
@@ -167,8 +170,10 @@ fdllm_status build_loop_graph(const LoopArgs &a, cudaStream_t cs, bool pdl, Loop
                                       cudaStreamCaptureModeRelaxed) != cudaSuccess)
         return FDLLM_ERR_CUDA;
     fdllm_status st = FDLLM_OK;
+    plain_launches = !pdl;
     if (a.forward(a.user, &a.st->step, a.block_mask, a.logits, cs) != 0)
         st = FDLLM_ERR_ARG;
+    plain_launches = false;
     if (st == FDLLM_OK)
         st = run_step_select(a, cs, pdl);
     if (st == FDLLM_OK) {

@@ -14,6 +14,9 @@ namespace {
 int device = 0;       // the current device
 int fail_in = 0;      // the so manieth of the next set-up calls fails (0: none)
 int launches = 0;
+int programmatic = 0;          // of them, programmatic dependents, since the last capture began
+bool reject_programmatic = false;
+int instantiated = 0;
 bool maps_fail = false;
 std::map<std::pair<int, const void *>, int> shared_limit;  // of (device, kernel)
 struct Map {
@@ -57,6 +60,9 @@ void fake_fail(int n) { fail_in = n; }
 int fake_failed() { return fail_in == 0; }
 void fake_maps_fail(int x) { maps_fail = x != 0; }
 int fake_launches() { return launches; }
+int fake_programmatic() { return programmatic; }
+void fake_reject_programmatic(int x) { reject_programmatic = x != 0; }
+int fake_instantiated() { return instantiated; }
 int fake_maps() { return (int)maps.size(); }
 unsigned long long fake_map(int i, int what, int axis)
 {
@@ -101,6 +107,9 @@ cudaError_t cudaLaunchKernelExC(const cudaLaunchConfig_t *c, const void *f, void
     if ((long long)c->dynamicSmemBytes > limit)
         return cudaErrorInvalidValue;
     ++launches;
+    for (unsigned i = 0; i < c->numAttrs; ++i)
+        programmatic += c->attrs[i].id == cudaLaunchAttributeProgrammaticStreamSerialization &&
+                        c->attrs[i].val.programmaticStreamSerializationAllowed;
     return cudaSuccess;
 }
 cudaError_t cudaGetSymbolAddress(void **p, const void *)
@@ -118,5 +127,77 @@ cudaError_t cudaGetDriverEntryPointByVersion(const char *, void **f, unsigned, u
     *q = cudaDriverEntryPointSuccess;
     return cudaSuccess;
 }
+
+// What a device-resident loop needs besides: a graph that is refused, where it has programmatic
+// edges, and memory that reads as 0.
+cudaError_t __cudaGetKernel(cudaKernel_t *k, const void *f)
+{
+    *k = static_cast<cudaKernel_t>(const_cast<void *>(f));
+    return cudaSuccess;
+}
+cudaError_t __cudaLaunchKernel(cudaKernel_t, dim3, dim3, void **, size_t, cudaStream_t)
+{
+    return cudaSuccess;
+}
+cudaError_t cudaOccupancyMaxActiveBlocksPerMultiprocessorWithFlags(int *n, const void *, int, size_t, unsigned)
+{
+    *n = 1;
+    return cudaSuccess;
+}
+cudaError_t cudaMalloc(void **p, size_t)
+{
+    static char memory[1 << 20];
+    *p = memory;
+    return cudaSuccess;
+}
+cudaError_t cudaFree(void *) { return cudaSuccess; }
+cudaError_t cudaMemsetAsync(void *, int, size_t, cudaStream_t) { return cudaSuccess; }
+cudaError_t cudaMemcpyAsync(void *to, const void *, size_t n, cudaMemcpyKind, cudaStream_t)
+{
+    std::memset(to, 0, n);
+    return cudaSuccess;
+}
+cudaError_t cudaStreamSynchronize(cudaStream_t) { return cudaSuccess; }
+cudaError_t cudaStreamCreateWithFlags(cudaStream_t *s, unsigned)
+{
+    *s = reinterpret_cast<cudaStream_t>(0x1000);
+    return cudaSuccess;
+}
+cudaError_t cudaStreamDestroy(cudaStream_t) { return cudaSuccess; }
+cudaError_t cudaGraphCreate(cudaGraph_t *g, unsigned)
+{
+    *g = reinterpret_cast<cudaGraph_t>(0x2000);
+    return cudaSuccess;
+}
+cudaError_t cudaGraphConditionalHandleCreate(cudaGraphConditionalHandle *h, cudaGraph_t, unsigned, unsigned)
+{
+    *h = 1;
+    return cudaSuccess;
+}
+cudaError_t cudaGraphAddNode(cudaGraphNode_t *, cudaGraph_t, const cudaGraphNode_t *,
+                             const cudaGraphEdgeData *, size_t, cudaGraphNodeParams *p)
+{
+    static cudaGraph_t body[1] = {reinterpret_cast<cudaGraph_t>(0x3000)};
+    p->conditional.phGraph_out = body;
+    return cudaSuccess;
+}
+cudaError_t cudaStreamBeginCaptureToGraph(cudaStream_t, cudaGraph_t, const cudaGraphNode_t *,
+                                          const cudaGraphEdgeData *, size_t, cudaStreamCaptureMode)
+{
+    programmatic = 0;
+    return cudaSuccess;
+}
+cudaError_t cudaStreamEndCapture(cudaStream_t, cudaGraph_t *) { return cudaSuccess; }
+cudaError_t cudaGraphInstantiate(cudaGraphExec_t *e, cudaGraph_t, unsigned long long)
+{
+    if (reject_programmatic && programmatic > 0)
+        return cudaErrorNotSupported;
+    ++instantiated;
+    *e = reinterpret_cast<cudaGraphExec_t>(0x4000);
+    return cudaSuccess;
+}
+cudaError_t cudaGraphExecDestroy(cudaGraphExec_t) { return cudaSuccess; }
+cudaError_t cudaGraphDestroy(cudaGraph_t) { return cudaSuccess; }
+cudaError_t cudaGraphLaunch(cudaGraphExec_t, cudaStream_t) { return cudaSuccess; }
 
 }  // extern "C"

@@ -115,3 +115,35 @@ def test_more_page_heads_than_a_map_counts_are_refused(run):
 c = cache(pages=1 << 28, heads=8)
 assert attend(c, 3) == 1 and weigh(c, 3) == 1 and evict(c, 100) == 1 and fake.fake_launches() == 0
 """)
+
+
+@pytest.mark.parametrize("rejects", [0, 1])
+def test_the_decode_loops_second_capture_has_no_programmatic_edges(run, rejects):
+    """Where a driver rejects programmatic edges in the loop's body, the body is captured again
+    without: the forward pass's operators have to do without them too."""
+    run("""
+FORWARD = ctypes.CFUNCTYPE(ctypes.c_int, p, p, p, p, p)
+lib.fdllm_cache_append.argtypes = [p, p, i, i, p, p, p, p, p, p, i, i, p]
+lib.fdllm_cache_read.argtypes = [p, p, i, i, p, p, p, p, i, i, p]
+lib.fdllm_qk_norm_rope.argtypes = [p, p, p, p, i, i, i, i, i, p, p, d, p, i, p, p, i, i, p, p, p]
+lib.fdllm_decode_loop.argtypes = [i, i, i, i, i, d, i, FORWARD, p, p, p, p, i, p, p]
+used = []
+def forward(user, state, mask, logits, stream):
+    before = fake.fake_programmatic()
+    c, s = cache(), strides(256, 256, 128)
+    st = [attend(c, 3), weigh(c, 3), evict(c, 1000), evict(c, 20000),
+          lib.fdllm_cache_append(ctypes.byref(c), A16, 1, 4, None, None, A16, s, A16, s, 0, 3, stream),
+          lib.fdllm_cache_read(ctypes.byref(c), A16, 1, 4, None, None, A16, A16, 0, 3, stream),
+          lib.fdllm_qk_norm_rope(A16, strides(128, 128), None, None, 0, 4, 1, 0, 128, None, None, 0.0, A16, 1, None,
+                                 (ctypes.c_double * 64)(), 64, 0, A16, None, stream)]
+    used.append(fake.fake_programmatic() - before)
+    return max(st)
+steps = ctypes.c_int(0)
+fake.fake_reject_programmatic(%d)
+st = lib.fdllm_decode_loop(1, 8, 8, 512, 0, 0.75, 0, FORWARD(forward), None, A16, A16, A16, 9, ctypes.byref(steps), None)
+assert st == 0 and fake.fake_instantiated() == 1, (st, used)
+assert used[0] > 0 and used[1:] == [0] * %d, used
+# and outside the loop they have them again
+before = fake.fake_programmatic()
+assert attend(cache(), 3) == 0 and fake.fake_programmatic() > before
+""" % (rejects, rejects))
