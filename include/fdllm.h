@@ -425,8 +425,9 @@ fdllm_status fdllm_qk_norm_rope(const void *q, const int64_t *q_strides, const v
  *          (FDLLM_ERR_ALIGN).
  *   start  [B] int32 device, or NULL: 0.      count  [B] int32 device, or NULL: n; tokens from
  *          count[b] on are padding and not written.
- * A token whose slot is negative, past the table or in a page out of range is not written
- * (device data, not checked on the host; attention over such a slot reports NaN).  Two slots
+ * A token whose slot is past the table or in a page out of range is not written, and of a
+ * sequence whose start is negative none is (device data, not checked on the host; attention over
+ * such a slot reports NaN, and fdllm_cache_read takes each slot for itself).  Two slots
  * share a byte of v_codes: calls writing one sequence must be ordered on the GPU. */
 fdllm_status fdllm_cache_append(const fdllm_cache *cache, const int32_t *block_table, int B,
                                 int max_pages, const int32_t *start, const int32_t *count,

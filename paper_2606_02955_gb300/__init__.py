@@ -714,7 +714,8 @@ def fdllm_qk_norm_rope(q: torch.Tensor, k: torch.Tensor | None, positions: torch
 def fdllm_cache_append(cache: KvCache, block_table: torch.Tensor, start, k: torch.Tensor,
                        v: torch.Tensor, count=None, stream=None):
     """Write k, v [B, n, heads, D] (bf16/fp16/fp32, channels contiguous) into slots
-    start[b] .. start[b] + count[b] - 1 (int32 [B] each; None: 0 and n)."""
+    start[b] .. start[b] + count[b] - 1 (int32 [B] each; None: 0 and n).  A sequence whose start
+    is negative is not written."""
     dev, dt = k.device, k.dtype
     tp, B, mp = _table(block_table, cache, dev)
     n = k.shape[1] if k.dim() == 4 else -1
