@@ -134,6 +134,10 @@ inline int sm_count()
     return n;
 }
 
+// Set on this thread while the decode loop (decode_loop.cu) captures its body without programmatic
+// edges: the operators that a forward pass calls launch in plain stream order too.
+extern thread_local bool plain_launches;
+
 // One kernel launch; `pdl` makes it a programmatic dependent of the stream's previous kernel
 // (the kernel then waits with pdl_wait() before it touches memory), but for plain_launches.
 template <typename... P, typename... A>

@@ -13,7 +13,7 @@
 
 namespace fdllm {
 
-thread_local bool plain_launches = false;
+thread_local bool plain_launches = false;  // (declared with the cache's launches, in cache.cuh)
 
 namespace {
 

@@ -165,10 +165,6 @@ fdllm_status select_owned(const void *logits, int dtype, int B, int L, int V, ui
                           double param, int mode, int32_t *out_tokens, uint8_t *out_commit,
                           int32_t *out_n, cudaStream_t stream, bool pdl);
 
-// Set on this thread while the decode loop captures its body without programmatic edges: the
-// operators that a forward pass calls launch in plain stream order too (cache.cuh).
-extern thread_local bool plain_launches;
-
 struct ProfileTermsArgs {
     const float *conf;       // [B, L]
     const uint8_t *mask;     // [B, L]
