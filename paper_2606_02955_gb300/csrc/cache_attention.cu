@@ -711,107 +711,94 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
                 arrive(kEmpty + st, kForAll);
                 ++ring;
             }
-            // With one buffer a tile's values wait for the sums of the tile before: the next tile's
-            // keys, which do not, come first (138 us from 143 for 64 blocks of 32 rows; with two
-            // buffers 140 from 133 for 64 rows, so there a tile's values come with its keys).
-            constexpr int kLag = S::bufs > 1 ? 0 : 1;
-            uint32_t ring_v = ring;
-            for (int i = first; i < last + kLag; ++i) {
-                if (i < last) {
-                    // ---- keys; their place is free when the scores of `bufs` tiles before are done
-                    const int t = i;
-                    const uint32_t par = tile & 1;
-                    const bool cached = t < ct;
-                    const int keys = cached ? kKeys : min(kOwnKeys, own - (t - ct) * kOwnKeys);
-                    const uint32_t tK = lanes + S::tK + (S::bufs > 1 ? par * 64 : 0);
-                    if (tile >= S::bufs)
-                        wait_u(kSDone + ((tile - S::bufs) & 1), ((tile - S::bufs) >> 1) & 1);
-                    if (cached) {
-                        const uint32_t s1 = ring % S::stages;
-                        wait_u(kFull + (s1), (ring / S::stages) & 1);
-                        tc::fence_after_sync();
-                        const uint32_t row = buf0 + s1 * S::stage_bytes;
+            // A tile's values come with its keys.  (The next tile's keys first: 164 us for 64 blocks
+            // of 32 rows, not 156; 970 for prompts of 8 x 1021, not 829; 161, not 163, for 64 rows over
+            // 32000 keys.)
+            for (int t = first; t < last; ++t, ++tile) {
+                const uint32_t par = tile & 1;
+                const bool cached = t < ct;
+                const int keys = cached ? kKeys : min(kOwnKeys, own - (t - ct) * kOwnKeys);
+                const int used = cached ? 1 : (keys + 31) / 32;
+                // ---- keys; their place is free when the scores of `bufs` tiles before are done
+                const uint32_t tK = lanes + S::tK + (S::bufs > 1 ? par * 64 : 0);
+                if (tile >= S::bufs)
+                    wait_u(kSDone + ((tile - S::bufs) & 1), ((tile - S::bufs) >> 1) & 1);
+                if (cached) {
+                    const uint32_t s1 = ring % S::stages;
+                    wait_u(kFull + (s1), (ring / S::stages) & 1);
+                    tc::fence_after_sync();
+                    const uint32_t row = buf0 + s1 * S::stage_bytes;
 #pragma unroll
-                        for (int v = 0; v < D / 32; ++v) {
-                            uint32_t y[16];
-                            unpack32(lds4(row + (k_row ^ (v << 4))), y);
-                            tmem_st16(tK + 16 * v, y);
-                        }
-                    } else if (32 * warp < keys) {
-                        const uint32_t r = ring + warp, s1 = r % S::stages;
-                        wait_u(kFull + (s1), (r / S::stages) & 1);
-                        tc::fence_after_sync();
-                        const uint8_t *row = smem + s1 * S::stage_bytes + lane * 128;
+                    for (int v = 0; v < D / 32; ++v) {
+                        uint32_t y[16];
+                        unpack32(lds4(row + (k_row ^ (v << 4))), y);
+                        tmem_st16(tK + 16 * v, y);
+                    }
+                } else if (32 * warp < keys) {
+                    const uint32_t r = ring + warp, s1 = r % S::stages;
+                    wait_u(kFull + (s1), (r / S::stages) & 1);
+                    tc::fence_after_sync();
+                    const uint8_t *row = smem + s1 * S::stage_bytes + lane * 128;
 #pragma unroll 1
-                        for (int v = 0; v < D / 8; ++v) {
-                            uint4 x = make_uint4(0, 0, 0, 0);
-                            if (key < keys)
-                                x = interleave8(*reinterpret_cast<const uint4 *>(
-                                    row + (v >> 3) * 4096 + (((v & 7) ^ (lane & 7)) << 4)));
-                            const uint32_t y[4] = {x.x, x.y, x.z, x.w};
-                            tmem_st<4>(tK + 4 * v, y);
+                    for (int v = 0; v < D / 8; ++v) {
+                        uint4 x = make_uint4(0, 0, 0, 0);
+                        if (key < keys)
+                            x = interleave8(*reinterpret_cast<const uint4 *>(
+                                row + (v >> 3) * 4096 + (((v & 7) ^ (lane & 7)) << 4)));
+                        const uint32_t y[4] = {x.x, x.y, x.z, x.w};
+                        tmem_st<4>(tK + 4 * v, y);
+                    }
+                }
+                tmem_wait_st();
+                tc::fence_before_sync();
+                arrive(kKReady + par, 1);
+                // ---- values; their place is free when the sums of `bufs` tiles before are done
+                const uint32_t tV = lanes + S::tV + (S::bufs > 1 ? par * 64 : 0);
+                if (tile >= S::bufs)
+                    wait_u(kODone + ((tile - S::bufs) & 1), ((tile - S::bufs) >> 1) & 1);
+                tc::fence_after_sync();
+                const int d = key;
+                if (cached) {
+                    const uint32_t at = buf0 + (ring % S::stages) * S::stage_bytes;
+                    if (D == 128 || d < D)
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) {  // 32 slots
+                            uint32_t y[16];
+                            unpack32_values(lds4(at + v_piece[v]), y);
+                            tmem_st16(tV + 16 * v, y);
                         }
+                    tmem_wait_st();
+                    tc::fence_before_sync();
+                    arrive(kVReady + par, 1);
+                    arrive(kEmpty + (ring % S::stages), 1);
+                } else {
+#pragma unroll 1
+                    for (int v = 0; v < used; ++v) {
+                        const uint32_t r = ring + v, s1 = r % S::stages;
+                        wait_u(kFull + (s1), (r / S::stages) & 1);
+                        if (D == 128 || d < D)
+#pragma unroll 1
+                            for (int j = 0; j < 32; j += 8) {
+                                uint32_t y[4];
+                                const int bad = own_values<T>(
+                                    reinterpret_cast<const T *>(smem + s1 * S::stage_bytes +
+                                                                S::own_v) + j * D + d,
+                                    D, keys - 32 * v - j, y);
+                                if (bad < 8) {
+                                    first_bad[sb][d] = min(
+                                        first_bad[sb][d], (t - ct) * kOwnKeys + 32 * v + j + bad);
+                                    any_bad[sb] = 1;
+                                }
+                                tmem_st<4>(tV + 16 * v + j / 2, y);
+                            }
                     }
                     tmem_wait_st();
                     tc::fence_before_sync();
-                    arrive(kKReady + par, 1);
-                    ring += cached ? 1 : (keys + 31) / 32;
-                    ++tile;
+                    arrive(kVReady + par, 1);
+                    for (int v = 0; v < used; ++v)
+                        arrive(kEmpty + ((ring + v) % S::stages), kForAll);
                 }
-                if (i >= first + kLag) {
-                    // ---- values; their place is free when the sums of `bufs` tiles before are done
-                    const int t = i - kLag;
-                    const uint32_t tv = tile - (kLag && i < last ? 2 : 1);  // the tile's number
-                    const bool cached = t < ct;
-                    const int keys = cached ? kKeys : min(kOwnKeys, own - (t - ct) * kOwnKeys);
-                    const int used = cached ? 1 : (keys + 31) / 32;
-                    const uint32_t tV = lanes + S::tV + (S::bufs > 1 ? (tv & 1) * 64 : 0);
-                    if (tv >= S::bufs)
-                        wait_u(kODone + ((tv - S::bufs) & 1), ((tv - S::bufs) >> 1) & 1);
-                    tc::fence_after_sync();
-                    const int d = key;
-                    if (cached) {
-                        const uint32_t at = buf0 + (ring_v % S::stages) * S::stage_bytes;
-                        if (D == 128 || d < D)
-#pragma unroll
-                            for (int v = 0; v < 4; ++v) {  // 32 slots
-                                uint32_t y[16];
-                                unpack32_values(lds4(at + v_piece[v]), y);
-                                tmem_st16(tV + 16 * v, y);
-                            }
-                        tmem_wait_st();
-                        tc::fence_before_sync();
-                        arrive(kVReady + (tv & 1), 1);
-                        arrive(kEmpty + (ring_v % S::stages), 1);
-                    } else {
-#pragma unroll 1
-                        for (int v = 0; v < used; ++v) {
-                            const uint32_t r = ring_v + v, s1 = r % S::stages;
-                            wait_u(kFull + (s1), (r / S::stages) & 1);
-                            if (D == 128 || d < D)
-#pragma unroll 1
-                                for (int j = 0; j < 32; j += 8) {
-                                    uint32_t y[4];
-                                    const int bad = own_values<T>(
-                                        reinterpret_cast<const T *>(smem + s1 * S::stage_bytes +
-                                                                    S::own_v) + j * D + d,
-                                        D, keys - 32 * v - j, y);
-                                    if (bad < 8) {
-                                        first_bad[sb][d] = min(
-                                            first_bad[sb][d], (t - ct) * kOwnKeys + 32 * v + j + bad);
-                                        any_bad[sb] = 1;
-                                    }
-                                    tmem_st<4>(tV + 16 * v + j / 2, y);
-                                }
-                        }
-                        tmem_wait_st();
-                        tc::fence_before_sync();
-                        arrive(kVReady + (tv & 1), 1);
-                        for (int v = 0; v < used; ++v)
-                            arrive(kEmpty + ((ring_v + v) % S::stages), kForAll);
-                    }
-                    ring_v += used;
-                }
+                ring += used;
             }
             arrive(kSegEmpty + (sb), 1);
         }
