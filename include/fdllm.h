@@ -461,9 +461,10 @@ fdllm_status fdllm_cache_read(const fdllm_cache *cache, const int32_t *block_tab
  * new_lens is out of range (negative, past the table, past Ln) or that meets a page out of
  * range among its first cache_lens slots gets NaN, for all its rows where the lengths are
  * wrong and for the heads and rows that meet the page otherwise.  Non-finite values behind
- * the lengths or the causal bound change nothing.  Scores and sums are fp32; the weights enter
- * the second product as fp16 with the scale of the cached row folded in (own values: as a sum
- * of two numbers of q's dtype).
+ * the lengths or the causal bound change nothing, and no query's values, whatever their size, take
+ * accuracy from another's results.  Scores and sums are fp32; a weight, with the scale of the
+ * cached row folded in, enters the second product as two fp16 numbers, 22 bits of it (own values:
+ * two numbers of q's dtype).
  * q, k_new and v_new: 16-byte aligned bases and strides (FDLLM_ERR_ALIGN). */
 fdllm_status fdllm_cache_attention(const void *q, const int64_t *q_strides, int dtype, int B,
                                    int Lq, int Hq, const fdllm_cache *cache,

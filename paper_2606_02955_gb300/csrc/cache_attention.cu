@@ -27,10 +27,10 @@
 // rounded to fp16; a second reference of the row keeps their largest near 1 whatever the scales
 // are.  A weight is held as two numbers of the values' operand type (fp16 for codes, their own
 // type for own values): rounded, and what that left times 2^11, as columns of one product with
-// sums of their own.  So it keeps 22 bits (16 of bf16), and one far below the largest, a subnormal of the first
-// number, keeps its place to 2^-36 of it: a key that outweighs all others at the front of a long
-// cache takes nothing from the many small ones behind it.  (With the first number alone the
-// results' error was 1.77e-3 for blocks of bf16, of which its rounding is 1.66e-3.)
+// sums of their own.  So it keeps 22 bits (16 of bf16), and one far below the largest, a subnormal
+// of the first number, keeps its place to 2^-36 of it: a key that outweighs all others at the front
+// of a long cache takes nothing from the many small ones behind it.  (With the first number alone
+// the results' error was 1.77e-3 for blocks of bf16, of which its rounding is 1.66e-3.)
 //
 // Warps.  One loads (queries, codes, own keys and values, through one ring of shared-memory
 // stages), one issues the products, four unpack, four or eight make weights: an unpacking warp is
@@ -42,11 +42,11 @@
 // joined by combine_kernel in tile order.
 //
 // Bound by the latency of the chain from unpacked keys to given weights and by the instructions
-// of the weights (about 300 a warp and tile), then by a unit's beginning and end.  Code that fits the
-// instruction cache counts as much as its instructions.  Measured: 64 sequences of 32 queries and
-// own keys over prefixes of 200 to 1024 keys, 32 heads of 128 channels: 131 us of GPU time (237 MB; the
-// tensor pipe 9 % busy, memory 25 %); 2 sequences of 64 queries of 32 heads over 32000 keys of 8: 138
-// (66 GFLOP); one token of 32 heads over 1021 keys of 8: 13; and 7 for combine_kernel.
+// of the weights (about 350 a warp and tile), then by a unit's beginning and end.  Code that fits the
+// instruction cache counts as much as its instructions.  Measured (GPU time, each launch by itself): 64
+// sequences of 32 queries and own keys over prefixes of 200 to 1024 keys, 32 heads of 128 channels: 151 us
+// (237 MB; the tensor pipe 11 % busy, memory 22 %); 2 sequences of 64 queries of 32 heads over 32000 keys of
+// 8: 161 (66 GFLOP); one token of 32 heads over 1021 keys of 8: 13; and 7 for combine_kernel.
 #include <cuda_runtime.h>
 
 #include <type_traits>
@@ -101,7 +101,7 @@ struct Shape {
     static constexpr int D = D_;
     static constexpr int N = N_;                       // rows of a row tile
     // Warpgroups sharing a tile's columns: 16 columns a thread, 32 where the registers are there
-    // (32 rows: 143 us, with 32 a thread 219; 64 rows over 32000 keys: 133, with 16 a thread 139).
+    // (32 rows: 164 us, with 32 a thread 180; 64 rows over 32000 keys: 164, with 16 a thread 174).
     static constexpr int C = N <= 32 ? N / 16 : N / 32;
     static constexpr int cols = N / C;                 // columns (rows of the problem) a thread
     static constexpr int w_warps = 4 * C;              // warps that make weights
@@ -112,7 +112,7 @@ struct Shape {
     static constexpr int ctas = N >= 64 ? 1 : 2;       // CTAs an SM holds
     // Registers of a thread, by warpgroup: what the launch gives every thread is dealt out
     // again, the weights' warps taking what the others leave: spilled registers cost them more than
-    // the others (an even share: 201 us for blocks of 32 rows; 40 of 64 for the others: 196, 48: 203).
+    // the others (an even share: 224 us for blocks of 32 rows; 40 of 64 for the others: 164, 48: 171).
     static constexpr int regs = 65536 / (ctas * threads) / 8 * 8;
     static constexpr int u_regs = N == 32 ? 40 : 64, l_regs = u_regs;
     static constexpr int w_regs = (regs * (C + 2) - u_regs - l_regs) / C / 8 * 8;
@@ -181,8 +181,8 @@ __device__ __forceinline__ void scale_sums(uint32_t taddr, const float *f, float
     tmem_wait_st();
 }
 
-// A unit's beginning and end cost about as much as this many tiles (4 to 8 by the rows; 3 here
-// took 136 us instead of 131).
+// A unit's beginning and end cost about as much as this many tiles (4 to 8 by the rows; 64 blocks
+// of 32 rows: 164 us, with 3 here 165).
 constexpr int kUnitCost = 7;
 
 // One sequence's share of the work.
@@ -1323,8 +1323,8 @@ __global__ void __launch_bounds__(32 * kJoinWarps)
 }
 
 // Rows of a row tile: the smallest width that holds a head's rows, 64 beyond that.  (64 sequences
-// of 32 heads, 512 cached keys: 16 rows a head 93 us, in a tile of 32 116, of 64 164; 32 rows 116,
-// in a tile of 64 173.)
+// of 32 heads, 512 cached keys: 16 rows a head 99 us, in a tile of 32 139, of 64 175; 32 rows 139,
+// in a tile of 64 184.)
 int tile_rows(int64_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
 
 struct Workspace {

@@ -205,8 +205,8 @@ __device__ __forceinline__ void unpack32(const uint4 x, uint32_t (&y)[16])
         asm("sub.rn.f16x2 %0, %0, %1;" : "+r"(y[i]) : "r"(i & 1 ? 0x64806480u : 0x64086408u));
 }
 
-// Values: those subnormals (kSumUnit), whose sums are of weights in 11 bits anyway; codes of odd
-// place less 15, by their complement and the sign, so that sums over tens of thousands of keys do
+// Values: those subnormals (kSumUnit), since 5e-6 is a hundredth of what the results' types round;
+// codes of odd place less 15, by their complement and the sign, so that sums over tens of thousands of keys do
 // not grow to a multiple of what the offsets leave of them (of 32000 keys 2.4e-3 of the result;
 // so 1.7e-3, which is what bf16 rounds).
 __device__ __forceinline__ void unpack32_values(const uint4 x, uint32_t (&y)[16])
@@ -395,7 +395,7 @@ __device__ __forceinline__ void fence_async_smem()
 
 // Waits on a shared-memory address, a few instructions each: many places of a kernel wait, and
 // code that does not fit the instruction cache costs its warps more than the waits (with a timer at
-// each place 64 blocks' attention took 195 us instead of 143).  The limit is a count of tries; a
+// each place 64 blocks' attention took 195 us, then 143 without).  The limit is a count of tries; a
 // try on a barrier that does not complete takes the hardware's 4 us (measured), so that 2^18 of
 // them are a second, where a wait takes microseconds.
 // kSleepNs: a warp that waits most of its time sleeps between tries, which would take issue slots

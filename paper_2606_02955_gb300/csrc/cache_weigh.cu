@@ -9,14 +9,15 @@
 // unpacked keys stay in tensor memory while the row tiles of a group (four of 64 rows, their
 // queries in shared memory) pass by; more rows take the CTA's keys once again.
 //
-// Bound by the exponentials and their arithmetic (3 instructions a row and key) above about 32
-// rows a head, below that by the codes: D/2 + 4 bytes of the cache a key, and 8 of weights.
+// Bound by the scores' arithmetic and the exponentials (a warpgroup of two weighs, the other only
+// unpacks) above about 32 rows a head, below that by the codes: D/2 + 4 bytes of the cache a key, and 8 of weights.
 //
 // Split.  The key tiles of all (sequence, head) units in order are cut into equal ranges, one to
 // a CTA; tiles share nothing, so nothing is joined.
 //
-// Measured: 8 sequences of 32 queries over 500 to 1024 keys, 32 heads of 128 channels: 16.5 us of
-// GPU time; 2 sequences of 64 queries of 32 heads over 32000 keys of 8 (256 rows a head): 66.
+// Measured (GPU time, each launch by itself): 8 sequences of 32 queries over 500 to 1024 keys, 32
+// heads of 128 channels: 16 us; 2 sequences of 64 queries of 32 heads over 32000 keys of 8 (256 rows a
+// head): 68 (calls in a row: 65).
 #include <cuda_runtime.h>
 
 #include <type_traits>
@@ -465,7 +466,7 @@ __global__ void __launch_bounds__(S::threads, S::ctas)
 }
 
 // Rows of a row tile: the smallest width that holds a head's rows, 64 beyond that.  (64 sequences
-// of 32 heads, 512 keys: 16 rows a head 40 us, in a tile of 32 46, of 64 62; 32 rows 50, of 64 65.)
+// of 32 heads, 512 keys: 16 rows a head 42 us, in a tile of 32 48, of 64 65; 32 rows 53, of 64 70.)
 int tile_rows(int64_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
 
 template <typename S, typename T>
