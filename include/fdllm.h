@@ -516,6 +516,144 @@ fdllm_status fdllm_cache_evict(const fdllm_cache *cache, const int32_t *block_ta
                                const int32_t *dst_table, int dst_max_pages, int32_t *out_lens,
                                float *out_weights, int32_t *out_index, void *stream);
 
+/* ------------------------------------------------------ drafting and its verification --- */
+/* A drafter proposes tokens and a target model takes or rejects them: a chain of them, or a tree
+ * whose branches are alternatives.  Nodes of a draft: node 0 is the root, the last committed token
+ * (the token whose keys are not in the cache yet); nodes 1 .. M - 1 are drafted tokens, each
+ * behind its parent, parents[b][j] < j.  fdllm_tree_mask and fdllm_cache_tree_attention run the
+ * nodes through the target in one pass, fdllm_verify_draft takes the tokens, and
+ * fdllm_distill_loss, fdllm_distill_grad and fdllm_distill_step train the drafter on its target's top
+ * logits.  All of them are asynchronous on `stream`, allocate nothing and may be captured into a
+ * CUDA graph; the first call of each with a dtype (attention: with a head size, dtype and range of
+ * lengths) on a device sets its kernels up and must come before a capture.  They are
+ * deterministic: the same inputs give the same bits. */
+
+/* The bits of which node sees which, and the nodes' depths.
+ *   parents    [B, M] int32 device; node 0's is not read.  A node whose parent is not in 0 .. j - 1
+ *              is detached: a root of its own.
+ *   lens       [B] int32 device, or NULL: M.  Nodes from lens[b] on are padding (a value out of
+ *              0 .. M counts as the nearer end).
+ *   M          1 to FDLLM_MAX_L.
+ *   out_mask   [B, M, ceil(M / 32)] uint32: bit j % 32 of word j / 32 of row i is set where node j is
+ *              node i or an ancestor of it.  Padding rows are 0.
+ *   out_depth  [B, M] int32, or NULL: steps from the root (a node's position is the root's plus its
+ *              depth); -1 for padding. */
+fdllm_status fdllm_tree_mask(const int32_t *parents, const int32_t *lens, int B, int M,
+                             uint32_t *out_mask, int32_t *out_depth, void *stream);
+
+/* fdllm_cache_attention with a bit for each query and own key in causal's place: query i sees all
+ * cached keys and the own keys j whose bits are set.
+ *   mask   [B, Lq, ceil(Ln / 32)] uint32 device, bit j % 32 of word j / 32 of row i (fdllm_tree_mask's
+ *          out_mask for Lq = Ln = M; any other pattern does as well, an empty row among them).  Bits
+ *          from new_lens[b] on are not read as set.  May be NULL where Ln = 0.
+ * Everything else, the workspace and its size among it, as fdllm_cache_attention; a non-finite
+ * value of an own key reaches the queries that see it and no others. */
+fdllm_status fdllm_cache_tree_attention(const void *q, const int64_t *q_strides, int dtype, int B,
+                                        int Lq, int Hq, const fdllm_cache *cache,
+                                        const int32_t *block_table, int max_pages,
+                                        const int32_t *cache_lens, const void *k_new,
+                                        const int64_t *k_strides, const void *v_new,
+                                        const int64_t *v_strides, int Ln, const int32_t *new_lens,
+                                        const uint32_t *mask, double scale, void *out,
+                                        float *out_lse, void *workspace, size_t workspace_bytes,
+                                        void *stream);
+
+/* Bytes of workspace fdllm_verify_draft needs (a pure host function).  0 for sizes out of range. */
+size_t fdllm_verify_draft_workspace_bytes(int B, int M, int V, int dtype);
+
+/* Takes drafted tokens by the target's probabilities and given random numbers, so that what
+ * comes out is distributed as the target's own samples.  With p_c = softmax(target row c /
+ * temperature), q_c = softmax(draft row c / draft_temperature), from the root on:
+ *   draft given (a chain drawn from q): node c + 1, token d, is taken iff
+ *       uniform[b][c + 1] * q_c(d) < p_c(d).
+ *       Behind the first that is not, the next token is drawn from max(p_c - q_c, 0).
+ *   draft NULL (tokens that were chosen, not drawn; a chain or a tree): the children of c are
+ *       tried in order of their numbers, child k iff uniform[b][k] * (1 - S) < p_c(d_k) with S the
+ *       p_c of the children tried before it (a token tried before counts 0).  Where none is
+ *       taken, the next token is drawn from p_c without the tokens tried.
+ *   temperature 0 (greedy): a child is taken iff its token is the argmax after c (lowest index on
+ *       ties); the next token is the argmax.
+ *   A token is drawn as argmax_v r(v) / noise[b][v] (lowest index on ties) from the weights r: noise
+ *   holds exponential variables.  Weights that are all 0 give way to p_c.
+ * Probabilities and weights are fp32 (relative error within 1e-5), the tests of tokens 64-bit
+ * products of them.
+ *   target     [B, M, V] device, dtype as given, row j the logits after node j; base 16-byte
+ *              aligned (FDLLM_ERR_ALIGN), V any from 1 to 2^20.
+ *   draft      [B, M - 1, V] in the same dtype and alignment, row j the logits that node j + 1 was
+ *              drawn from; or NULL.  Only with parents NULL and temperature > 0 (FDLLM_ERR_ARG).
+ *   tokens     [B, M] int32 device: the nodes' tokens (node 0's is not read).  A token out of the
+ *              vocabulary is never taken.
+ *   parents    [B, M] int32 device, or NULL: a chain.  A node whose parent is not in 0 .. j - 1 is
+ *              never reached.
+ *   lens       [B] int32 device, or NULL: M.  Nodes from lens[b] on are padding, their rows not
+ *              read (a value out of 1 .. M counts as the nearer end).
+ *   M          1 (no drafts: the next token is drawn from row 0) to FDLLM_MAX_L.
+ *   temperature, draft_temperature   1e-6 to 1e6, or temperature 0.
+ *   uniform    [B, M] fp32 device in [0, 1); entry 0 is not read.   noise  [B, V] fp32 device, > 0,
+ *              base 16-byte aligned; a token whose noise is NaN, negative or infinite is not drawn.
+ *              Both may be NULL where temperature is 0.
+ *   out_tokens [B, M] int32: the taken tokens, then the next token; -1 behind.
+ *   out_nodes  [B, M] int32: the root (0), then the taken nodes: the rows whose keys and values
+ *              enter the cache; -1 behind.
+ *   out_n      [B] int32: taken tokens, 0 .. M - 1; FDLLM_ROW_NONFINITE (and -1 in the row of the
+ *              others) where a row on the way holds a NaN or its maximum is infinite.
+ *   workspace  device, 256-byte aligned, fdllm_verify_draft_workspace_bytes() bytes of any content;
+ *              calls that may overlap on the GPU need their own. */
+fdllm_status fdllm_verify_draft(const void *target, const void *draft, int dtype, int B, int M,
+                                int V, const int32_t *tokens, const int32_t *parents,
+                                const int32_t *lens, double temperature, double draft_temperature,
+                                const float *uniform, const float *noise, int32_t *out_tokens,
+                                int32_t *out_nodes, int32_t *out_n, void *workspace,
+                                size_t workspace_bytes, void *stream);
+
+/* The loss of a student on its teacher's top logits at the masked positions.  With
+ * q = softmax(x / temperature) of a position's logits x, and of its listed tokens the teacher's
+ * probabilities p_k:
+ *   teacher_lse NULL: p = softmax(top_logits / temperature) over the listed tokens, R = 0;
+ *   teacher_lse given: p_k = exp(top_logits_k / temperature - teacher_lse), and R = max(0, 1 - sum p)
+ *       is the teacher's rest, held against the student's rest r = sum of q over all other tokens:
+ *   out_loss = sum_k p_k (log p_k - log q_k) + R (log R - log r).
+ * A term with p_k = 0, or R = 0, is 0, and so is the rest's where the student has no other token
+ * (r = 0).  All in fp32, sums of exponentials relative to their own maxima, r summed by itself.
+ *   logits       [B, L, V] device, dtype as given, base 16-byte aligned (FDLLM_ERR_ALIGN), V any
+ *                from 1 to 2^20; B * L below 2^31.  Read at masked positions only.
+ *   mask         [B, L] uint8 device, nonzero = masked (counted).
+ *   top_index    [B, L, K] int32 device: the listed tokens; an index out of 0 .. V - 1 is an absent
+ *                entry; masses of a token listed more than once add up.   K  1 to 1024.
+ *   top_logits   [B, L, K] device in top_dtype (bf16, fp16 or fp32).
+ *   teacher_lse  [B, L] fp32 device: logsumexp(all the teacher's logits / temperature); or NULL.
+ *   temperature  1e-6 to 1e6.
+ *   out_loss     [B, L] fp32: 0 at positions that are not masked; NaN where a masked row of the
+ *                student holds a NaN or its maximum is infinite, or the teacher's numbers are NaN.
+ *   out_stats    [B, L, 4] fp32, 16-byte aligned, or NULL: what fdllm_distill_grad needs. */
+fdllm_status fdllm_distill_loss(const void *logits, int dtype, int B, int L, int V,
+                                const uint8_t *mask, const int32_t *top_index,
+                                const void *top_logits, int top_dtype, int K,
+                                const float *teacher_lse, double temperature, float *out_loss,
+                                float *out_stats, void *stream);
+
+/* Its gradient, given that of each position's loss:
+ *   out_grad = grad_loss / temperature * (q_v (P + R) - p_v)     at a listed token, P = sum p,
+ *              grad_loss / temperature * (q_v (P + R) - R q_v / r)  at another,
+ * 0 at positions that are not masked, in the logits' dtype (rounded once), NaN where the loss is.
+ *   stats      fdllm_distill_loss's out_stats for the same arguments.
+ *   grad_loss  [B, L] fp32 device, read at masked positions.
+ *   out_grad   [B, L, V], 16-byte aligned; may be `logits` itself. */
+fdllm_status fdllm_distill_grad(const void *logits, int dtype, int B, int L, int V,
+                                const uint8_t *mask, const int32_t *top_index,
+                                const void *top_logits, int top_dtype, int K,
+                                const float *teacher_lse, double temperature, const float *stats,
+                                const float *grad_loss, void *out_grad, void *stream);
+
+/* Both in one call that reads the logits once, where grad_loss is known beforehand (1 / count, for a
+ * mean).  Arguments as above. */
+fdllm_status fdllm_distill_step(const void *logits, int dtype, int B, int L, int V,
+                                const uint8_t *mask, const int32_t *top_index,
+                                const void *top_logits, int top_dtype, int K,
+                                const float *teacher_lse, double temperature,
+                                const float *grad_loss, float *out_loss, void *out_grad,
+                                void *stream);
+
 /* The sticky device error of fdllm_cache_attention and fdllm_cache_key_weights on the current
  * device: synchronises `stream`, returns FDLLM_ERR_DEVICE if one of their kernels gave up a
  * bounded wait since the last call (the results of the calls since then are unusable), FDLLM_OK

@@ -31,6 +31,9 @@ __all__ = [
     "fdllm_cache_attention", "fdllm_cache_attention_workspace_bytes",
     "fdllm_cache_key_weights", "fdllm_cache_evict", "fdllm_cache_status",
     "fdllm_cache_check_wait",
+    "fdllm_tree_mask", "fdllm_cache_tree_attention", "fdllm_verify_draft",
+    "fdllm_verify_draft_workspace_bytes", "fdllm_distill_loss", "fdllm_distill_grad",
+    "fdllm_distill_step",
 ]
 
 BF16, FP32, FP16 = 0, 1, 2
@@ -109,6 +112,21 @@ def _load():
     lib.fdllm_cache_status.restype = i
     lib.fdllm_cache_check_wait.argtypes = [i, p]
     lib.fdllm_cache_check_wait.restype = i
+    lib.fdllm_tree_mask.argtypes = [p, p, i, i, p, p, p]
+    lib.fdllm_tree_mask.restype = i
+    lib.fdllm_cache_tree_attention.argtypes = [p, p, i, i, i, i, p, p, i, p, p, p, p, p, i, p, p, d,
+                                               p, p, p, sz, p]
+    lib.fdllm_cache_tree_attention.restype = i
+    lib.fdllm_verify_draft.argtypes = [p, p, i, i, i, i, p, p, p, d, d, p, p, p, p, p, p, sz, p]
+    lib.fdllm_verify_draft.restype = i
+    lib.fdllm_verify_draft_workspace_bytes.argtypes = [i, i, i, i]
+    lib.fdllm_verify_draft_workspace_bytes.restype = sz
+    lib.fdllm_distill_loss.argtypes = [p, i, i, i, i, p, p, p, i, i, p, d, p, p, p]
+    lib.fdllm_distill_loss.restype = i
+    lib.fdllm_distill_grad.argtypes = [p, i, i, i, i, p, p, p, i, i, p, d, p, p, p, p]
+    lib.fdllm_distill_grad.restype = i
+    lib.fdllm_distill_step.argtypes = [p, i, i, i, i, p, p, p, i, i, p, d, p, p, p, p]
+    lib.fdllm_distill_step.restype = i
     lib.fdllm_check_bounded_wait.argtypes = [d, p]
     lib.fdllm_check_bounded_wait.restype = i
     lib.fdllm_device_status.argtypes = [p]
@@ -873,6 +891,246 @@ def fdllm_cache_evict(cache: KvCache, block_table: torch.Tensor, cache_lens: tor
     if st:
         _check(st, "fdllm_cache_evict")
     return out_lens, out_weights, out_index
+
+
+@_called_on(0)
+def fdllm_tree_mask(parents: torch.Tensor, lens=None, out_mask=None, out_depth=None, stream=None):
+    """Which node of a draft's tree sees which: ``parents`` int32 [B, M] (node 0 the root, a node's
+    parent before it), ``lens`` int32 [B] (None: M nodes each).  Returns (mask int32 [B, M,
+    ceil(M / 32)], bit j % 32 of word j / 32 of row i set where node j is i or an ancestor of it;
+    depth int32 [B, M], -1 behind lens)."""
+    dev = parents.device
+    if parents.dim() != 2:
+        raise ValueError("parents must be [B, M], got %s" % (tuple(parents.shape),))
+    B, M = shape = parents.shape
+    bits = (B, M, (M + 31) // 32)
+    if out_mask is None:
+        out_mask = _made(bits, _I32, dev, stream)
+    if out_depth is None:
+        out_depth = _made(shape, _I32, dev, stream)
+    st = _load().fdllm_tree_mask(
+        _ptr(parents, "parents", _I32, shape, dev), _ptr(lens, "lens", _I32, (B,), dev), B, M,
+        _ptr(out_mask, "out_mask", _I32, bits, dev), _ptr(out_depth, "out_depth", _I32, shape, dev),
+        _raw_stream(dev.index) if stream is None else _stream(stream))
+    if st:
+        _check(st, "fdllm_tree_mask")
+    return out_mask, out_depth
+
+
+@_called_on(0)
+def fdllm_cache_tree_attention(q: torch.Tensor, cache: KvCache, block_table: torch.Tensor,
+                               cache_lens: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor,
+                               mask: torch.Tensor, new_lens=None, scale: float | None = None,
+                               out=None, return_lse: bool = False, out_lse=None, workspace=None,
+                               stream=None):
+    """fdllm_cache_attention of a draft's nodes: query i of ``q`` [B, Lq, Hq, D] sees the first
+    cache_lens[b] slots of the cache and the own keys whose bits are set in ``mask`` int32 [B, Lq,
+    ceil(Ln / 32)] (fdllm_tree_mask's).  Everything else as fdllm_cache_attention."""
+    dev, dt = q.device, q.dtype
+    qp, qs, B, Lq, Hq = _queries(q, cache, dev)
+    heads, D = cache.heads, cache.head_dim
+    tp, _, mp = _table(block_table, cache, dev, rows=B)
+    Ln = k_new.shape[1] if k_new.dim() == 4 else -1
+    own = (B, Ln, heads, D)
+    kp, ks = _rows(k_new, "k_new", dt, own, dev, _Three)
+    vp, vs = _rows(v_new, "v_new", dt, own, dev, _Three)
+    if out is None:
+        out = _made(q.shape, dt, dev, stream)
+    if out_lse is None and return_lse:
+        out_lse = _made((B, Lq, Hq), _F32, dev, stream)
+    lib = _load()
+    if workspace is None:  # of this call alone, as fdllm_cache_attention's
+        need = lib.fdllm_cache_attention_workspace_bytes(B, Lq, Hq, heads, D)
+        workspace = _made((need if need > 256 else 256,), _U8, dev, stream)
+    st = lib.fdllm_cache_tree_attention(
+        qp, qs, _CODES[dt], B, Lq, Hq, cache._ref, tp, mp,
+        _ptr(cache_lens, "cache_lens", _I32, (B,), dev), kp, ks, vp, vs, Ln,
+        _ptr(new_lens, "new_lens", _I32, (B,), dev),
+        _ptr(mask, "mask", _I32, (B, Lq, (Ln + 31) // 32), dev),
+        D ** -0.5 if scale is None else scale, _ptr(out, "out", dt, q.shape, dev),
+        _ptr(out_lse, "out_lse", _F32, (B, Lq, Hq), dev),
+        _ptr(workspace, "workspace", _U8, workspace.shape, dev), workspace.numel(),
+        _raw_stream(dev.index) if stream is None else _stream(stream))
+    if st:
+        _check(st, "fdllm_cache_tree_attention")
+    return (out, out_lse) if return_lse else out
+
+
+def _logits(x, name, dims):
+    """(dtype code, shape) of contiguous logits."""
+    if x.dim() != dims or x.dtype not in _CODES:
+        raise TypeError("%s must be %d-dimensional bfloat16, float16 or float32, got %s %s"
+                        % (name, dims, x.dtype, tuple(x.shape)))
+    return _CODES[x.dtype], x.shape
+
+
+def fdllm_verify_draft_workspace_bytes(B: int, M: int, V: int, dtype=BF16) -> int:
+    return int(_load().fdllm_verify_draft_workspace_bytes(B, M, V, dtype))
+
+
+@_called_on(0)
+def fdllm_verify_draft(target: torch.Tensor, tokens: torch.Tensor, parents=None, lens=None,
+                       draft=None, temperature: float = 1.0, draft_temperature: float | None = None,
+                       uniform=None, noise=None, out_tokens=None, out_nodes=None, out_n=None,
+                       workspace=None, stream=None):
+    """Take drafted tokens by the target's probabilities and given random numbers.
+
+    ``target`` [B, M, V] bf16/fp16/fp32, row j the target's logits after node j (node 0 the last
+    committed token); ``tokens`` int32 [B, M] the nodes' tokens; ``parents`` int32 [B, M] a tree
+    (None: a chain); ``lens`` int32 [B] the counts of nodes; ``draft`` [B, M - 1, V] the logits a
+    chain was drawn from at ``draft_temperature`` (None: ``temperature``), or None where the tokens
+    were chosen; ``uniform`` fp32 [B, M] in [0, 1) and ``noise`` fp32 [B, V] exponential variables
+    (None at temperature 0, which is greedy).  Returns (tokens int32 [B, M]: the taken ones, then
+    the next; nodes int32 [B, M]: the root, then the taken ones; -1 behind; n int32 [B])."""
+    dev, dt = target.device, target.dtype
+    code, shape = _logits(target, "target", 3)
+    B, M, V = shape
+    nodes = (B, M)
+    if out_tokens is None:
+        out_tokens = _made(nodes, _I32, dev, stream)
+    if out_nodes is None:
+        out_nodes = _made(nodes, _I32, dev, stream)
+    if out_n is None:
+        out_n = _made((B,), _I32, dev, stream)
+    lib = _load()
+    if workspace is None:  # of this call alone: it is several launches
+        need = lib.fdllm_verify_draft_workspace_bytes(B, M, V, code)
+        workspace = _made((need if need > 256 else 256,), _U8, dev, stream)
+    st = lib.fdllm_verify_draft(
+        _ptr(target, "target", dt, shape, dev), _ptr(draft, "draft", dt, (B, M - 1, V), dev), code,
+        B, M, V, _ptr(tokens, "tokens", _I32, nodes, dev), _ptr(parents, "parents", _I32, nodes, dev),
+        _ptr(lens, "lens", _I32, (B,), dev), temperature,
+        temperature if draft_temperature is None else draft_temperature,
+        _ptr(uniform, "uniform", _F32, nodes, dev), _ptr(noise, "noise", _F32, (B, V), dev),
+        _ptr(out_tokens, "out_tokens", _I32, nodes, dev),
+        _ptr(out_nodes, "out_nodes", _I32, nodes, dev), _ptr(out_n, "out_n", _I32, (B,), dev),
+        _ptr(workspace, "workspace", _U8, workspace.shape, dev), workspace.numel(),
+        _raw_stream(dev.index) if stream is None else _stream(stream))
+    if st:
+        _check(st, "fdllm_verify_draft")
+    return out_tokens, out_nodes, out_n
+
+
+def _distill_args(logits, mask, top_index, top_logits, teacher_lse, dev):
+    """The arguments that the distillation calls share, up to teacher_lse."""
+    code, shape = _logits(logits, "logits", 3)
+    top, top_shape = _logits(top_logits, "top_logits", 3)
+    B, L, V = shape
+    K = top_shape[2]
+    rows = (B, L)
+    return (_ptr(logits, "logits", logits.dtype, shape, dev), code, B, L, V,
+            _ptr(mask, "mask", _U8, rows, dev), _ptr(top_index, "top_index", _I32, (B, L, K), dev),
+            _ptr(top_logits, "top_logits", top_logits.dtype, (B, L, K), dev), top, K,
+            _ptr(teacher_lse, "teacher_lse", _F32, rows, dev))
+
+
+class _DistillLoss(torch.autograd.Function):
+    """The loss with its gradient for autograd: forward keeps four numbers of each position."""
+
+    @staticmethod
+    def forward(ctx, logits, mask, top_index, top_logits, teacher_lse, temperature):
+        stats = torch.empty((*mask.shape, 4), dtype=_F32, device=logits.device)
+        loss = _distill_loss(logits, mask, top_index, top_logits, teacher_lse, temperature, None,
+                             stats, None)
+        ctx.save_for_backward(logits, mask, top_index, top_logits, teacher_lse, stats)
+        ctx.temperature = temperature
+        return loss
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad_loss):
+        logits, mask, top_index, top_logits, teacher_lse, stats = ctx.saved_tensors
+        grad = fdllm_distill_grad(logits, mask, top_index, top_logits, stats, grad_loss.contiguous(),
+                                  teacher_lse=teacher_lse, temperature=ctx.temperature)
+        return grad, None, None, None, None, None
+
+
+def _distill_loss(logits, mask, top_index, top_logits, teacher_lse, temperature, out_loss, out_stats,
+                  stream):
+    dev = logits.device
+    args = _distill_args(logits, mask, top_index, top_logits, teacher_lse, dev)
+    B, L = args[2:4]
+    if out_loss is None:
+        out_loss = _made((B, L), _F32, dev, stream)
+    st = _load().fdllm_distill_loss(
+        *args, temperature, _ptr(out_loss, "out_loss", _F32, (B, L), dev),
+        _ptr(out_stats, "out_stats", _F32, (B, L, 4), dev),
+        _raw_stream(dev.index) if stream is None else _stream(stream))
+    if st:
+        _check(st, "fdllm_distill_loss")
+    return out_loss
+
+
+@_called_on(0)
+def fdllm_distill_loss(logits: torch.Tensor, mask: torch.Tensor, top_index: torch.Tensor,
+                       top_logits: torch.Tensor, teacher_lse=None, temperature: float = 1.0,
+                       out_loss=None, out_stats=None, stream=None):
+    """The loss of ``logits`` [B, L, V] (bf16/fp16/fp32) on a teacher's top logits at the masked
+    positions: fp32 [B, L], 0 elsewhere.
+
+    ``mask`` uint8 [B, L]; ``top_index`` int32 [B, L, K] (out of the vocabulary: absent) and
+    ``top_logits`` [B, L, K] (bf16/fp16/fp32); ``teacher_lse`` fp32 [B, L], the log-sum-exp of all
+    of the teacher's logits / temperature, counts the rest of the vocabulary as one class (None: the
+    teacher's probabilities are taken over its listed tokens).
+
+    Differentiable with respect to ``logits`` where they require a gradient (the call then runs on
+    the current stream and makes its own outputs; the teacher's tensors get none).  In a CUDA graph
+    that holds the backward pass too, use fdllm_distill_step, or fdllm_distill_grad with
+    ``out_stats`` fp32 [B, L, 4]."""
+    if logits.requires_grad and torch.is_grad_enabled():
+        if out_loss is not None or out_stats is not None or stream is not None:
+            raise ValueError("a loss for autograd makes its own outputs on the current stream: "
+                             "out_loss, out_stats and stream must be None")
+        if top_logits.requires_grad or (teacher_lse is not None and teacher_lse.requires_grad):
+            raise ValueError("the teacher's tensors get no gradient: detach them")
+        return _DistillLoss.apply(logits, mask, top_index, top_logits, teacher_lse, temperature)
+    return _distill_loss(logits, mask, top_index, top_logits, teacher_lse, temperature, out_loss,
+                         out_stats, stream)
+
+
+@_called_on(0)
+def fdllm_distill_grad(logits: torch.Tensor, mask: torch.Tensor, top_index: torch.Tensor,
+                       top_logits: torch.Tensor, stats: torch.Tensor, grad_loss: torch.Tensor,
+                       teacher_lse=None, temperature: float = 1.0, out_grad=None, stream=None):
+    """The gradient of fdllm_distill_loss with respect to ``logits`` from its ``out_stats`` and the
+    gradient fp32 [B, L] of each position's loss.  ``out_grad`` may be ``logits``."""
+    dev = logits.device
+    args = _distill_args(logits, mask, top_index, top_logits, teacher_lse, dev)
+    B, L = args[2:4]
+    if out_grad is None:
+        out_grad = _made(logits.shape, logits.dtype, dev, stream)
+    st = _load().fdllm_distill_grad(
+        *args, temperature, _ptr(stats, "stats", _F32, (B, L, 4), dev),
+        _ptr(grad_loss, "grad_loss", _F32, (B, L), dev),
+        _ptr(out_grad, "out_grad", logits.dtype, logits.shape, dev),
+        _raw_stream(dev.index) if stream is None else _stream(stream))
+    if st:
+        _check(st, "fdllm_distill_grad")
+    return out_grad
+
+
+@_called_on(0)
+def fdllm_distill_step(logits: torch.Tensor, mask: torch.Tensor, top_index: torch.Tensor,
+                       top_logits: torch.Tensor, grad_loss: torch.Tensor, teacher_lse=None,
+                       temperature: float = 1.0, out_loss=None, out_grad=None, stream=None):
+    """Loss and gradient in one call that reads the logits once, given the gradient fp32 [B, L] of
+    each position's loss beforehand (1 / count, for a mean).  Returns (loss fp32 [B, L], gradient
+    [B, L, V] in the logits' dtype); ``out_grad`` may be ``logits``."""
+    dev = logits.device
+    args = _distill_args(logits, mask, top_index, top_logits, teacher_lse, dev)
+    B, L = args[2:4]
+    if out_loss is None:
+        out_loss = _made((B, L), _F32, dev, stream)
+    if out_grad is None:
+        out_grad = _made(logits.shape, logits.dtype, dev, stream)
+    st = _load().fdllm_distill_step(
+        *args, temperature, _ptr(grad_loss, "grad_loss", _F32, (B, L), dev),
+        _ptr(out_loss, "out_loss", _F32, (B, L), dev),
+        _ptr(out_grad, "out_grad", logits.dtype, logits.shape, dev),
+        _raw_stream(dev.index) if stream is None else _stream(stream))
+    if st:
+        _check(st, "fdllm_distill_step")
+    return out_loss, out_grad
 
 
 def fdllm_cache_status(stream=None) -> int:

@@ -18,7 +18,8 @@ OBJ_DIR = os.path.join(HERE, "_build")
 LIB_PATH = os.path.join(HERE, "libfdllm.so")
 SOURCES = ["fdllm_abi.cu", "vocab_reduce.cu", "profile_select.cu", "decode_loop.cu",
            "lmhead.cu", "host_io.cu", "qk_norm_rope.cu", "cache_store.cu",
-           "cache_attention.cu", "cache_weigh.cu", "cache_evict.cu"]
+           "cache_attention.cu", "cache_tree.cu", "cache_weigh.cu", "cache_evict.cu", "verify.cu",
+           "distill.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC]
 
