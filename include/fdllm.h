@@ -574,7 +574,8 @@ size_t fdllm_verify_draft_workspace_bytes(int B, int M, int V, int dtype);
  *   temperature 0 (greedy): a child is taken iff its token is the argmax after c (lowest index on
  *       ties); the next token is the argmax.
  *   A token is drawn as argmax_v r(v) / noise[b][v] (lowest index on ties) from the weights r: noise
- *   holds exponential variables.  Weights that are all 0 give way to p_c.
+ *   holds exponential variables.  Weights that are all 0 give way to p_c, and where no token
+ *   can be drawn from that either, the next token is the argmax.
  * Probabilities and weights are fp32 (relative error within 1e-5), the tests of tokens 64-bit
  * products of them.
  *   target     [B, M, V] device, dtype as given, row j the logits after node j; base 16-byte

@@ -9,15 +9,27 @@
 //   is, the next token is drawn from p_c without the children's tokens.
 // A token is drawn from weights r(v) as argmax r(v) / E(v), E given (exponential variables): r needs
 // no norm, and no sum over the vocabulary has to be exact to the last token's share.
+#include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
+#include "cache_tc.cuh"
+#include "ptx.cuh"
 #include "vocab_rows.cuh"
 
 namespace fdllm {
 namespace {
 
+namespace cg = cooperative_groups;
+
 constexpr int kMaxNodes = FDLLM_MAX_L;
-constexpr int kThreads = 512;
+constexpr int kMathWarps = 16;
+constexpr int kMath = 32 * kMathWarps;
+constexpr int kChunk = 65536;  // bytes of a stage
+constexpr int kStages = 3;
+constexpr int kChunkVecs = kChunk / 16;
+constexpr int kSmallRow = 8192;  // rows up to this many bytes: a warp each
+constexpr int kDraw = 512;       // threads of a CTA of the walk and the draw
+constexpr int kMaxRanks = 8;     // CTAs of a cluster of them
 
 struct VerifyArgs {
     const void *target;       // [B, M, V]
@@ -33,24 +45,222 @@ struct VerifyArgs {
     int32_t *out_tokens;      // [B, M]
     int32_t *out_nodes;       // [B, M]
     int32_t *out_n;           // [B]
-    UnitPartial *partials;    // [B, M] of the target's rows, [B, M - 1] of the draft's
+    UnitPartial *parts;       // [B, M] of the target's rows, [B, M - 1] of the draft's; each `per` long
+    int per;                  // parts of a row
+    int pieces, piece_vecs;   // pieces of a row, vectors of one
+    uint32_t *status;         // sticky: a bounded wait gave up
 };
 
 __device__ __forceinline__ int nodes_of(const VerifyArgs &a, int b)
 {
-    return a.lens ? min(max(a.lens[b], 1), a.M) : a.M;
+    return a.lens ? min(max(__ldg(a.lens + b), 1), a.M) : a.M;
 }
 
-// One CTA a row: maximum, its first index, and the sum relative to it.
+// Where row j of sequence b is: of the target, or of the draft.
+struct RowAt {
+    int64_t part;  // its parts
+    const uint8_t *p;
+};
+
 template <typename T>
-__global__ void __launch_bounds__(kThreads) verify_rows_kernel(const __grid_constant__ VerifyArgs a)
+__device__ __forceinline__ RowAt row_at(const VerifyArgs &a, int b, int j, bool of_draft)
+{
+    RowAt r;
+    const int64_t at = of_draft ? (int64_t)b * (a.M - 1) + j : (int64_t)b * a.M + j;
+    r.part = (of_draft ? (int64_t)a.B * a.M + at : at) * a.per;
+    r.p = static_cast<const uint8_t *>(of_draft ? a.draft : a.target) + at * a.V * (int64_t)sizeof(T);
+    return r;
+}
+
+// The largest of a vector's values; NaN where one is.
+template <typename T>
+__device__ __forceinline__ float vector_most(const uint4 &r)
+{
+    if constexpr (sizeof(T) == 4) {
+        return fmax_nan(fmax_nan(__uint_as_float(r.x), __uint_as_float(r.y)),
+                        fmax_nan(__uint_as_float(r.z), __uint_as_float(r.w)));
+    } else {
+        using P = std::conditional_t<__is_same(T, __nv_bfloat16), __nv_bfloat162, __half2>;
+        auto as = [](const uint32_t &w) { return *reinterpret_cast<const P *>(&w); };
+        const P m = __hmax2_nan(__hmax2_nan(as(r.x), as(r.y)), __hmax2_nan(as(r.z), as(r.w)));
+        return fmax_nan(to_float(m.x), to_float(m.y));
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ constexpr uint32_t no_values()  // a word of -inf
+{
+    return sizeof(T) == 4 ? 0xFF800000u : __is_same(T, __nv_bfloat16) ? 0xFF80FF80u : 0xFC00FC00u;
+}
+
+// A thread's sum of 2^((x - m) c) over its vectors.  m is a reference, not the maximum: it moves only
+// where a value exceeds it by kSlack, so that few vectors pay for that, and terms stay below 2^kSlack.
+// Below kFar the terms are 2^(x c - r), r = m c rounded, in one operation: the product is exact
+// there, and what r's rounding leaves, at most 2^-3 and the same for all terms, is taken out at the
+// end.  Beyond kFar, x less m comes first.
+constexpr float kSlack = 12.0f, kFar = 2097152.0f;
+
+struct Summed {
+    ExpSum z;
+    float r = 0.0f;
+    bool far = true;  // (so that a first value of -FLT_MAX, which moves nothing, counts 1)
+
+    template <typename T, int N>
+    __device__ __forceinline__ void add(const uint4 (&x)[N], float c)
+    {
+        constexpr int E = 16 / sizeof(T);
+        float top = vector_most<T>(x[0]);
+#pragma unroll
+        for (int n = 1; n < N; ++n)
+            top = fmax_nan(top, vector_most<T>(x[n]));
+        // (a NaN fails the test as well, and moves nothing: its term makes the sum NaN)
+        if (!((top - z.m) * c <= kSlack)) {
+            if (top > z.m) {
+                settle(c);
+                z.raise(top, c);
+                r = z.m * c;
+                far = !(fabsf(r) < kFar);
+                if (!far)
+                    z.z *= ex2_mufu(fmaf(z.m, c, -r));
+            }
+        }
+        uint64_t s2 = 0;
+        auto terms = [&](auto far_tag) {
+            constexpr bool kIsFar = decltype(far_tag)::value;
+            const uint64_t c2 = f2(c, c), n2 = kIsFar ? f2(-z.m, -z.m) : f2(-r, -r);
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                float y[E];
+                widen<T>(x[n], y);
+#pragma unroll
+                for (int e = 0; e < E; e += 2) {
+                    float t0, t1;
+                    const uint64_t y2 = f2(y[e], y[e + 1]);
+                    un2(kIsFar ? mul2(add2(y2, n2), c2) : fma2(y2, c2, n2), t0, t1);
+                    s2 = add2(s2, f2(ex2_mufu(t0), ex2_mufu(t1)));
+                }
+            }
+        };
+        if (__builtin_expect(far, 0))
+            terms(std::true_type{});
+        else
+            terms(std::false_type{});
+        float s0, s1;
+        un2(s2, s0, s1);
+        z.z += s0 + s1;
+    }
+    // The sum relative to m itself.
+    __device__ __forceinline__ void settle(float c)
+    {
+        if (!far && z.z != 0.0f)
+            z.z *= ex2_mufu(-fmaf(z.m, c, -r));
+        far = true;
+    }
+};
+
+// A thread's largest value and its first index; `nan` where a value is one.
+struct Largest {
+    float m = -INFINITY;
+    uint32_t first = kNoIdx;
+    float nan = -INFINITY;
+
+    template <typename T, int N>
+    __device__ __forceinline__ void add(const uint4 (&x)[N], const int (&i)[N])
+    {
+        constexpr int E = 16 / sizeof(T);
+        float top = -INFINITY;
+        uint4 r = x[0];
+        int at = i[0];
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const float y = vector_most<T>(x[n]);
+            nan = fmax_nan(nan, y);
+            if (y > top) {
+                top = y;
+                r = x[n];
+                at = i[n];
+            }
+        }
+        if (top > m) {
+            float y[E];
+            widen<T>(r, y);
+#pragma unroll
+            for (int e = E - 1; e >= 0; --e)
+                if (y[e] == top)
+                    first = at + e;
+            m = top;
+        }
+    }
+    __device__ __forceinline__ void add(float x, int i)
+    {
+        nan = fmax_nan(nan, x);
+        if (x > m || (x == m && (uint32_t)i < first)) {
+            m = x;
+            first = i;
+        }
+    }
+};
+
+// What a warp makes of its share of a row: its part of the sum, or its largest value (S then 1, or
+// NaN, and 0 where there is no finite value).
+template <typename T, bool kGreedy>
+struct Share {
+    Summed s;
+    Largest l;
+    template <int N>
+    __device__ __forceinline__ void add(const uint4 (&x)[N], const int (&i)[N], float c)
+    {
+        if constexpr (kGreedy)
+            l.template add<T, N>(x, i);
+        else
+            s.template add<T, N>(x, c);
+    }
+    // The values before the row's first whole vector and behind its last.
+    __device__ __forceinline__ void add_ends(const RowSpan<T> &r, float c)
+    {
+        const int lane = threadIdx.x & 31;
+        const int i = lane < 8 ? lane : r.tail() + lane - 8;
+        if (!(lane < 8 ? i < r.head : i < r.V && lane < 16))
+            return;
+        const float x = to_float(r.row[i]);
+        if constexpr (kGreedy) {
+            l.add(x, i);
+        } else {
+            s.settle(c);
+            s.z.add(x, c);
+        }
+    }
+    __device__ __forceinline__ UnitPartial join(float c)
+    {
+        UnitPartial p;
+        p.pad = 0;
+        if constexpr (kGreedy) {
+            p.M = warp_most(l.m);
+            p.idx = __reduce_min_sync(0xFFFFFFFFu, l.m == p.M ? l.first : kNoIdx);
+            const bool bad = __any_sync(0xFFFFFFFFu, l.nan != l.nan);
+            p.S = bad ? nan_f() : p.M == -INFINITY ? 0.0f : 1.0f;
+        } else {
+            s.settle(c);
+            const ExpSum z = warp_sum(s.z, c);
+            p.M = z.m;
+            p.S = z.z;
+            p.idx = kNoIdx;
+        }
+        return p;
+    }
+};
+
+// ---- Rows of up to kSmallRow bytes: a warp each.
+template <typename T, bool kGreedy>
+__global__ void __launch_bounds__(256) verify_small_kernel(const __grid_constant__ VerifyArgs a)
 {
     constexpr int E = 16 / sizeof(T);
-    __shared__ ExpSum sums[kThreads / 32];
-    __shared__ uint32_t firsts[kThreads / 32];
     pdl_wait();
+    if (threadIdx.x == 0)
+        pdl_launch_dependents();
+    const int lane = threadIdx.x & 31;
     const int64_t targets = (int64_t)a.B * a.M, rows = targets + (a.draft ? (int64_t)a.B * (a.M - 1) : 0);
-    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
+    for (int64_t row = blockIdx.x * 8ll + (threadIdx.x >> 5); row < rows; row += gridDim.x * 8ll) {
         const bool of_draft = row >= targets;
         const int64_t at = of_draft ? row - targets : row;
         const int per = of_draft ? a.M - 1 : a.M;
@@ -58,200 +268,535 @@ __global__ void __launch_bounds__(kThreads) verify_rows_kernel(const __grid_cons
         if (j >= nodes_of(a, b) - (of_draft ? 1 : 0))
             continue;
         const float c = of_draft ? a.cd : a.ct;
-        const RowSpan<T> s(static_cast<const T *>(of_draft ? a.draft : a.target) + at * a.V, a.V);
-        ExpSum z;
-        uint32_t first = kNoIdx;
-        auto one = [&](int i) {
-            const float x = to_float(s.row[i]);
-            if (x > z.m || (x == z.m && (uint32_t)i < first))
-                first = i;
-            z.add(x, c);
-        };
-        for (int i = threadIdx.x; i < s.vecs; i += kThreads) {
-            float y[E];
-            widen<T>(s.vectors()[i], y);
-            float top = y[0];
+        const RowAt where = row_at<T>(a, b, j, of_draft);
+        const RowSpan<T> r(reinterpret_cast<const T *>(where.p), a.V);
+        Share<T, kGreedy> s;
+        constexpr uint32_t kPad = no_values<T>();
+        for (int v = lane; v < r.vecs; v += 128) {
+            uint4 x[4];
+            int i[4];
 #pragma unroll
-            for (int e = 1; e < E; ++e)
-                top = fmaxf(top, y[e]);
-            if (top > z.m || first == kNoIdx) {
-#pragma unroll
-                for (int e = E - 1; e >= 0; --e)
-                    if (y[e] == top && top >= z.m)
-                        first = s.head + i * E + e;
-                z.raise(top, c);
+            for (int n = 0; n < 4; ++n) {
+                const int w = v + 32 * n;
+                x[n] = w < r.vecs ? r.vectors()[w] : make_uint4(kPad, kPad, kPad, kPad);
+                i[n] = r.head + w * E;
             }
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-                z.z += ex2_mufu((y[e] - z.m) * c);
+            s.template add<4>(x, i, c);
         }
-        for (int i = threadIdx.x; i < s.head; i += kThreads)
-            one(i);
-        for (int i = s.tail() + threadIdx.x; i < a.V; i += kThreads)
-            one(i);
-        const float top = warp_most(z.m);
-        first = __reduce_min_sync(0xFFFFFFFFu, z.m == top ? first : kNoIdx);
-        z = warp_sum(z, c);
-        __syncthreads();
-        if ((threadIdx.x & 31) == 0) {
-            sums[threadIdx.x >> 5] = z;
-            firsts[threadIdx.x >> 5] = first;
-        }
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            for (int w = 1; w < kThreads / 32; ++w) {
-                if (sums[w].m > z.m || (sums[w].m == z.m && firsts[w] < first))
-                    first = firsts[w];
-                z.merge(sums[w], c);
-            }
-            UnitPartial p;
-            p.M = z.m;
-            p.S = z.z;
-            p.idx = first;
-            p.pad = 0;
-            a.partials[row] = p;
-        }
+        s.add_ends(r, c);
+        const UnitPartial p = s.join(c);
+        if (lane == 0)
+            a.parts[where.part] = p;
     }
 }
 
-// One CTA a sequence: the walk, then the draw.
-template <typename T>
-__global__ void __launch_bounds__(kThreads) verify_walk_kernel(const __grid_constant__ VerifyArgs a)
+// ---- Longer rows: pieces of them stream through a ring of shared memory, filled by bulk copies.
+// Every warp leaves its own part of a piece: no warp waits for another but through the ring.
+struct Stage {
+    uint32_t n;     // vectors, 0: no more
+    int32_t at;     // index in the row of their first value
+    uint32_t last;  // 1: the piece ends here, 2: and the row
+    float c;
+    int64_t part;   // the piece's parts
+    const void *row;
+};
+
+struct StreamShared {
+    uint64_t full[kStages], empty[kStages];
+    Stage stage[kStages];
+};
+constexpr int kStreamSmem = kStages * kChunk + (int)sizeof(StreamShared);
+
+template <typename T, bool kGreedy>
+__global__ void __launch_bounds__(kMath + 32, 1)
+    verify_stream_kernel(const __grid_constant__ VerifyArgs a)
 {
-    __shared__ float take[kMaxNodes];   // p of a node's token after its parent
-    __shared__ float drawn[kMaxNodes];  // q of it
-    __shared__ short parent[kMaxNodes];
-    __shared__ uint8_t bad[kMaxNodes];
-    __shared__ int path[kMaxNodes + 1];
-    __shared__ int cur, taken, failed, rejected;
-    __shared__ unsigned long long best[kThreads / 32];
-    extern __shared__ __align__(16) uint32_t gone[];  // tokens of the last node's children
+    constexpr int E = 16 / sizeof(T);
+    constexpr int kPer = kChunkVecs / kMath;
+    extern __shared__ __align__(128) uint8_t ring[];
+    StreamShared &sm = *reinterpret_cast<StreamShared *>(ring + kStages * kChunk);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(&sm.full[i], 1);
+            mbar_init(&sm.empty[i], kMathWarps);
+        }
+        fence_mbar_init();
+    }
+    __syncthreads();
     pdl_wait();
-    const int b = blockIdx.x, tid = threadIdx.x, n = nodes_of(a, b);
-    const int64_t base = (int64_t)b * a.M, dbase = (int64_t)a.B * a.M + (int64_t)b * (a.M - 1);
-    const T *target = static_cast<const T *>(a.target) + base * a.V;
-    const T *draft = static_cast<const T *>(a.draft) + (int64_t)b * (a.M - 1) * a.V;
-    const UnitPartial *tp = a.partials + base, *dp = a.partials + dbase;
-    auto fine = [](const UnitPartial &p) {
-        return p.S > 0.0f && p.S <= FLT_MAX && finite_f(p.M);
-    };
-    if (!a.greedy)
-        for (int i = tid; i < (a.V + 31) / 32; i += kThreads)
-            gone[i] = 0;
-    for (int j = tid; j < n; j += kThreads) {
-        bad[j] = !fine(tp[j]) || (a.draft && j < n - 1 && !fine(dp[j]));
-        const int pa = j == 0 ? -1 : a.parents ? a.parents[base + j] : j - 1;
-        const bool hung = pa >= 0 && pa < j;
-        parent[j] = hung ? pa : -1;
-        take[j] = drawn[j] = 0.0f;
-        const int d = a.tokens[base + j];
-        if (!hung || d < 0 || d >= a.V)
+    if (threadIdx.x == 0)
+        pdl_launch_dependents();
+    if (warp == kMathWarps) {
+        // ------------------------------------------------------------ the copying lane
+        if (lane != 0)
+            return;
+        const uint64_t policy = make_evict_first_policy();
+        const uint32_t kinds = a.draft ? 2 : 1;
+        const uint32_t units = (uint32_t)a.B * a.M * kinds * a.pieces;
+        uint32_t k = 0;
+        bool alive = true;
+        for (uint32_t u = blockIdx.x; u < units && alive; u += gridDim.x) {
+            // nodes first, so that all sequences' early rows come first
+            const uint32_t row = u / a.pieces, piece = u - row * a.pieces;
+            const uint32_t bj = row / kinds, of_draft = row - bj * kinds;
+            const int j = (int)(bj / a.B), b = (int)(bj - (uint32_t)j * a.B);
+            if (j >= nodes_of(a, b) - (int)of_draft)
+                continue;
+            const RowAt where = row_at<T>(a, b, j, of_draft);
+            const RowSpan<T> r(reinterpret_cast<const T *>(where.p), a.V);
+            const int end = (int)piece + 1 < a.pieces ? (int)(piece + 1) * a.piece_vecs : r.vecs;
+            for (int v = piece * a.piece_vecs; v < end; v += kChunkVecs, ++k) {
+                const uint32_t s = k % kStages;
+                if (k >= kStages && !mbar_wait(&sm.empty[s], (k / kStages - 1) & 1, a.status)) {
+                    alive = false;
+                    break;
+                }
+                const uint32_t n = min(kChunkVecs, end - v);
+                Stage st;
+                st.n = n;
+                st.at = r.head + v * E;
+                st.last = v + (int)n < end ? 0 : (int)piece + 1 < a.pieces ? 1 : 2;
+                st.c = of_draft ? a.cd : a.ct;
+                st.part = where.part + piece * kMathWarps;
+                st.row = r.row;
+                sm.stage[s] = st;
+                mbar_arrive_expect_tx(&sm.full[s], n * 16);
+                bulk_copy_g2s_hint(ring + s * kChunk, r.vectors() + v, n * 16, &sm.full[s], policy);
+            }
+        }
+        if (alive) {
+            const uint32_t s = k % kStages;
+            if (k < kStages || mbar_wait(&sm.empty[s], (k / kStages - 1) & 1, a.status)) {
+                sm.stage[s].n = 0;
+                mbar_arrive(&sm.full[s]);
+            } else {
+                alive = false;
+            }
+        }
+        // nothing may land in this CTA's memory after it has gone
+        // (the stage that holds the end had its last copy taken)
+        const uint32_t most = alive ? kStages - 1 : kStages;
+        for (uint32_t i = k > most ? k - most : 0; i < k; ++i)
+            mbar_wait(&sm.full[i % kStages], (i / kStages) & 1, a.status, kDrainLimitNs);
+        return;
+    }
+    // ---------------------------------------------------------------- the counting warps
+    constexpr uint32_t kPad = no_values<T>();
+    Share<T, kGreedy> sum;
+    for (uint32_t k = 0;; ++k) {
+        const uint32_t s = k % kStages;
+        if (!mbar_wait(&sm.full[s], (k / kStages) & 1, a.status))
+            return;
+        const Stage &st = sm.stage[s];
+        const uint32_t vecs = st.n, last = st.last;
+        if (vecs == 0)
+            return;
+        const float c = st.c;
+        const int64_t part = st.part;
+        const T *row = static_cast<const T *>(st.row);
+        const uint4 *buf = reinterpret_cast<const uint4 *>(ring + s * kChunk);
+        uint4 x[kPer];
+        int i[kPer];
+        if (vecs == kChunkVecs) {
+#pragma unroll
+            for (int n = 0; n < kPer; ++n)
+                x[n] = buf[threadIdx.x + n * kMath];
+        } else {
+#pragma unroll
+            for (int n = 0; n < kPer; ++n) {
+                const uint32_t v = threadIdx.x + n * kMath;
+                x[n] = v < vecs ? buf[v] : make_uint4(kPad, kPad, kPad, kPad);
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < kPer; ++n)
+            i[n] = st.at + (threadIdx.x + n * kMath) * E;
+        __syncwarp();
+        if (lane == 0)
+            mbar_arrive(&sm.empty[s]);
+        sum.template add<kPer>(x, i, c);
+        if (!last)
             continue;
+        if (last == 2 && warp == 0)
+            sum.add_ends(RowSpan<T>(row, a.V), c);
+        const UnitPartial p = sum.join(c);
+        if (lane == 0)
+            a.parts[part + warp] = p;
+        sum = Share<T, kGreedy>();
+    }
+}
+
+// ---- The walk.
+// A row's parts joined, by a warp.
+struct RowSum {
+    ExpSum z;
+    uint32_t first = kNoIdx;
+};
+
+__device__ __forceinline__ RowSum row_sum(const VerifyArgs &a, int64_t part, float c)
+{
+    RowSum s;
+    for (int i = threadIdx.x & 31; i < a.per; i += 32) {
+        const int4 r = __ldcg(reinterpret_cast<const int4 *>(a.parts + part + i));
+        ExpSum o;
+        o.m = __int_as_float(r.x);
+        o.z = __int_as_float(r.y);
         if (a.greedy) {
-            take[j] = tp[pa].idx == (uint32_t)d ? 1.0f : 0.0f;
+            if (o.m > s.z.m || (o.m == s.z.m && (uint32_t)r.z < s.first))
+                s.first = (uint32_t)r.z;
+            s.z.m = fmaxf(s.z.m, o.m);
+            s.z.z += o.z;
+        } else {
+            s.z.merge(o, c);
+        }
+    }
+    if (a.greedy) {
+        const float top = warp_most(s.z.m);
+        s.first = __reduce_min_sync(0xFFFFFFFFu, s.z.m == top ? s.first : kNoIdx);
+        s.z.m = top;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1)
+            s.z.z += __shfl_xor_sync(0xFFFFFFFFu, s.z.z, o);
+    } else {
+        s.z = warp_sum(s.z, c);
+    }
+    return s;
+}
+
+__device__ __forceinline__ bool usable(const ExpSum &z)
+{
+    return z.z > 0.0f && z.z <= FLT_MAX && finite_f(z.m);
+}
+
+constexpr int kNone = 0, kBad = -1;  // choices that are no child
+
+// A sequence's nodes, and what the walk finds out about them: arrays of M in shared memory.
+struct Nodes {
+    ExpSum *of, *less;   // row sums: the target's, the draft's
+    float *uniform;
+    float *x, *y;        // the logits of its token after its parent: target's, draft's
+    int *token;
+    uint32_t *first;     // greedy: the largest logit's index
+    short *parent;       // -1: none
+    short *choice;
+    short *path;
+    uint32_t *gone;      // a bit for each token of the slice: those tried after the last node
+    static constexpr int kBytes = 2 * 8 + 5 * 4 + 3 * 2;  // of a node
+
+    __device__ __forceinline__ Nodes(uint8_t *p, int M)
+    {
+        M = (M + 7) / 8 * 8;
+        of = reinterpret_cast<ExpSum *>(p);
+        less = of + M;
+        uniform = reinterpret_cast<float *>(less + M);
+        x = uniform + M;
+        y = x + M;
+        token = reinterpret_cast<int *>(y + M);
+        first = reinterpret_cast<uint32_t *>(token + M);
+        parent = reinterpret_cast<short *>(first + M);
+        choice = parent + M;
+        path = choice + M;
+        gone = reinterpret_cast<uint32_t *>(path + M);
+    }
+};
+inline size_t draw_smem(int M, int V, int ranks, bool greedy)
+{
+    return (size_t)(M + 7) / 8 * 8 * Nodes::kBytes +
+           (greedy ? 0 : (size_t)((V + ranks - 1) / ranks + 31) / 32 * 4);
+}
+
+// Which child of node c is taken, by a warp; kNone, or kBad where a row of c is unusable.
+__device__ __forceinline__ int decide(const VerifyArgs &a, const Nodes &s, int c, int n, const RowSum &t,
+                                      const RowSum &q)
+{
+    const int lane = threadIdx.x & 31;
+    const bool drawn = a.draft && c + 1 < n;
+    if (!usable(t.z) || (drawn && !usable(q.z)))
+        return kBad;
+    const int end = a.parents ? n : min(n, c + 2);
+    double left = 1.0;
+    for (int j0 = c + 1; j0 < end; j0 += 32) {
+        const int j = j0 + lane;
+        const bool child = j < end && s.parent[j] == c;
+        uint32_t kids = __ballot_sync(0xFFFFFFFFu, child);
+        if (!kids)
+            continue;
+        const int d = child ? s.token[j] : -1;
+        const bool inside = d >= 0 && d < a.V;
+        if (a.greedy) {
+            const uint32_t hit = __ballot_sync(0xFFFFFFFFu, inside && (uint32_t)d == t.first);
+            if (hit)
+                return j0 + __ffs(hit) - 1;
             continue;
         }
-        const float x = to_float(target[(int64_t)pa * a.V + d]);
-        take[j] = ex2_mufu((x - tp[pa].M) * a.ct) / tp[pa].S;
-        if (a.draft) {
-            const float y = to_float(draft[(int64_t)pa * a.V + d]);
-            drawn[j] = ex2_mufu((y - dp[pa].M) * a.cd) / dp[pa].S;
-        } else {
-            for (int i = 1; i < j; ++i)
-                if (a.tokens[base + i] == d && (a.parents ? a.parents[base + i] : i - 1) == pa)
-                    take[j] = 0.0f;  // its token is gone with the sibling before it
+        float p = 0.0f, other = 0.0f;
+        if (inside) {
+            p = ex2_mufu((s.x[j] - t.z.m) * a.ct) / t.z.z;
+            if (drawn)
+                other = ex2_mufu((s.y[j] - q.z.m) * a.cd) / q.z.z;
+        }
+        // a token that was tried before counts 0: among these 32, and among those before them
+        if (__match_any_sync(0xFFFFFFFFu, d) & kids & ((1u << lane) - 1))
+            p = 0.0f;
+        for (int i0 = c + 1; i0 < j0; i0 += 32) {
+            const bool kin = s.parent[i0 + lane] == c;
+            const int e = s.token[i0 + lane];
+            for (uint32_t bits = __ballot_sync(0xFFFFFFFFu, kin); bits; bits &= bits - 1)
+                if (__shfl_sync(0xFFFFFFFFu, e, __ffs(bits) - 1) == d)
+                    p = 0.0f;
+        }
+        const float u = child ? s.uniform[j] : 0.0f;
+        for (; kids; kids &= kids - 1) {
+            const int k = __ffs(kids) - 1;
+            const float pk = __shfl_sync(0xFFFFFFFFu, p, k), uk = __shfl_sync(0xFFFFFFFFu, u, k);
+            const float qk = __shfl_sync(0xFFFFFFFFu, other, k);
+            if ((double)uk * (drawn ? (double)qk : left) < (double)pk)
+                return j0 + k;
+            left -= pk;
+        }
+    }
+    return kNone;
+}
+
+// The cluster's barrier, in its two halves.  A CTA may leave behind its last arrival.
+__device__ __forceinline__ void cluster_arrive()
+{
+    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait()
+{
+    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+}
+
+// Clusters of CTAs, one to a sequence: the walk, in each CTA; then the draw, each CTA a slice of the
+// vocabulary.  What the call was given is read, and the noise brought to the L2, while the rows'
+// sums are still under way: it was there before their kernel began.
+template <typename T>
+__global__ void __launch_bounds__(kDraw, 2) verify_draw_kernel(const __grid_constant__ VerifyArgs a)
+{
+    constexpr int E = 16 / sizeof(T);
+    __shared__ int taken, failed;
+    __shared__ unsigned long long best[kDraw / 32], of_cta[kMaxRanks];
+    extern __shared__ __align__(16) uint8_t dynamic[];
+    const Nodes s(dynamic, a.M);
+    uint32_t *const gone = s.gone;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int ranks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int b = blockIdx.x / ranks, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int slice = ((a.V + ranks - 1) / ranks + 31) / 32 * 32;
+    const int v0 = min(a.V, rank * slice), v1 = min(a.V, v0 + slice);
+    const int64_t base = (int64_t)b * a.M;
+    const float *noise = a.noise + (int64_t)b * a.V;
+    cluster_arrive();
+    if (!a.greedy) {
+        for (int i = tid; i < slice / 32; i += kDraw)
+            gone[i] = 0;
+        for (int v = v0 + tid * 32; v < v1; v += kDraw * 32)
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(noise + v));
+    }
+    const int n = nodes_of(a, b);
+    for (int j = tid; j < n; j += kDraw) {
+        const int p = j == 0 ? -1 : a.parents ? a.parents[base + j] : j - 1;
+        const int d = a.tokens[base + j];
+        s.parent[j] = p >= 0 && p < j ? p : -1;
+        s.token[j] = d;
+        if (a.greedy)
+            continue;
+        s.uniform[j] = a.uniform[base + j];
+        if (p >= 0 && p < j && d >= 0 && d < a.V) {
+            s.x[j] = to_float(reinterpret_cast<const T *>(row_at<T>(a, b, p, false).p)[d]);
+            if (a.draft)
+                s.y[j] = to_float(reinterpret_cast<const T *>(row_at<T>(a, b, p, true).p)[d]);
+        }
+    }
+    pdl_wait();
+    cluster_wait();  // every CTA of the cluster is there
+    __syncthreads();
+    for (int c = warp; c < n; c += kDraw / 32) {
+        const RowSum t = row_sum(a, row_at<T>(a, b, c, false).part, a.ct);
+        RowSum q;
+        if (a.draft && c + 1 < n)
+            q = row_sum(a, row_at<T>(a, b, c, true).part, a.cd);
+        const int to = decide(a, s, c, n, t, q);
+        if (lane == 0) {
+            s.choice[c] = (short)to;
+            s.of[c] = t.z;
+            s.less[c] = q.z;
+            s.first[c] = t.first;
         }
     }
     __syncthreads();
     if (tid == 0) {
-        int at = 0, len = 0, wrong = bad[0], stop = 0;
-        double left = 1.0;
-        path[0] = 0;
-        for (int j = 1; j < n && !wrong && !stop; ++j) {
-            if (parent[j] != at)
-                continue;
-            bool ok;
-            if (a.greedy)
-                ok = take[j] != 0.0f;
-            else if (a.draft)
-                ok = (double)a.uniform[base + j] * drawn[j] < take[j];
-            else
-                ok = (double)a.uniform[base + j] * left < take[j];
-            if (ok) {
-                at = j;
-                path[++len] = j;
-                left = 1.0;
-                wrong = bad[j];
-            } else {
-                left -= take[j];
-                stop = a.draft != nullptr;
+        int at = 0, len = 0;
+        for (;; ++len) {
+            s.path[len] = (short)at;
+            const int to = s.choice[at];
+            if (to <= 0) {
+                failed = to == kBad;
+                break;
             }
+            at = to;
         }
-        cur = at;
         taken = len;
-        failed = wrong;
-        rejected = stop;
     }
     __syncthreads();
     int extra = -1;
     if (!failed) {
-        const UnitPartial p = tp[cur];
-        extra = (int)p.idx;
-        if (!a.greedy) {
-            if (!a.draft)
-                for (int j = 1 + tid; j < n; j += kThreads) {
-                    const int d = a.tokens[base + j];
-                    if (parent[j] == cur && d >= 0 && d < a.V)
-                        atomicOr(&gone[d >> 5], 1u << (d & 31));
+        const int cur = s.path[taken];
+        if (a.greedy) {
+            extra = (int)s.first[cur];
+        } else {
+            if (!a.draft) {
+                for (int j = cur + 1 + tid; j < n; j += kDraw) {
+                    const int d = s.token[j];
+                    if (s.parent[j] == cur && d >= v0 && d < v1)
+                        atomicOr(&gone[(d - v0) >> 5], 1u << ((d - v0) & 31));
                 }
-            __syncthreads();
-            const T *row = target + (int64_t)cur * a.V, *drow = draft + (int64_t)cur * a.V;
-            const float *noise = a.noise + (int64_t)b * a.V;
-            UnitPartial q = {};
-            if (rejected)
-                q = dp[cur];
-            unsigned long long top = 0;
-            for (int turn = 0; turn < 2 && top == 0; ++turn) {  // the second: from p itself
-                for (int v = tid; v < a.V; v += kThreads) {
-                    float r = ex2_mufu((to_float(row[v]) - p.M) * a.ct) / p.S;
-                    if (turn == 0 && rejected)
-                        r = fmaxf(r - ex2_mufu((to_float(drow[v]) - q.M) * a.cd) / q.S, 0.0f);
-                    if (turn == 0 && (gone[v >> 5] >> (v & 31)) & 1u)
-                        r = 0.0f;
-                    const float key = __fdiv_rn(r, noise[v]);
-                    if (r > 0.0f && key > 0.0f) {
-                        const unsigned long long k =
-                            ((unsigned long long)__float_as_uint(key) << 32) | (0xFFFFFFFFu - v);
-                        top = k > top ? k : top;
+                __syncthreads();
+            }
+            const bool rejected = a.draft && cur + 1 < n;
+            const T *row = reinterpret_cast<const T *>(row_at<T>(a, b, cur, false).p);
+            const T *less = rejected ? reinterpret_cast<const T *>(row_at<T>(a, b, cur, true).p) : row;
+            const float pm = s.of[cur].m, pz = 1.0f / s.of[cur].z;
+            const float qm = rejected ? s.less[cur].m : 0.0f, qz = rejected ? 1.0f / s.less[cur].z : 0.0f;
+            float key = 0.0f;  // the best so far, and its token
+            uint32_t at = 0;
+            // r / E, where it is more than the best: compared as r > best E, and divided then.  (A NaN or
+            // an infinity in E fails the test, what is negative gives no key.)
+            auto weigh = [&](float r, float e, int v) {
+                if (r > key * e) {
+                    const float k = __fdiv_rn(r, e);
+                    if (k > key) {
+                        key = k;
+                        at = v;
                     }
                 }
+            };
+            auto p_of = [&](float x) { return ex2_mufu((x - pm) * a.ct) * pz; };
+            auto q_of = [&](float y) { return ex2_mufu((y - qm) * a.cd) * qz; };
+            auto best_of_cta = [&]() -> unsigned long long {  // in thread 0
+                unsigned long long top =
+                    key > 0.0f ? ((unsigned long long)__float_as_uint(key) << 32) | (0xFFFFFFFFu - at) : 0;
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) {
                     const unsigned long long k = __shfl_xor_sync(0xFFFFFFFFu, top, o);
                     top = k > top ? k : top;
                 }
                 __syncthreads();
-                if ((tid & 31) == 0)
-                    best[tid >> 5] = top;
+                if (lane == 0)
+                    best[warp] = top;
                 __syncthreads();
-                for (int w = 0; w < kThreads / 32; ++w)
-                    top = best[w] > top ? best[w] : top;
+                if (tid == 0)
+                    for (int w = 1; w < kDraw / 32; ++w)
+                        top = best[w] > top ? best[w] : top;
+                return top;
+            };
+            if (((int64_t)a.V * sizeof(T)) % 16 == 0) {
+                constexpr int kTwo = 2;  // vectors of a thread in flight
+                for (int w = v0 + tid * E; w < v1; w += kTwo * kDraw * E) {
+                    uint4 xr[kTwo], yr[kTwo];
+                    float4 er[kTwo][E / 4];
+#pragma unroll
+                    for (int k = 0; k < kTwo; ++k) {
+                        const int v = w + k * kDraw * E;
+                        if (v >= v1)
+                            continue;
+                        xr[k] = *reinterpret_cast<const uint4 *>(row + v);
+                        if (rejected)
+                            yr[k] = *reinterpret_cast<const uint4 *>(less + v);
+#pragma unroll
+                        for (int i = 0; i < E / 4; ++i)
+                            er[k][i] = reinterpret_cast<const float4 *>(noise + v)[i];
+                    }
+#pragma unroll
+                    for (int k = 0; k < kTwo; ++k) {
+                        const int v = w + k * kDraw * E;
+                        if (v >= v1)
+                            continue;
+                        float x[E];
+                        widen<T>(xr[k], x);
+#pragma unroll
+                        for (int i = 0; i < E; ++i)
+                            x[i] = p_of(x[i]);
+                        if (rejected) {
+                            float y[E];
+                            widen<T>(yr[k], y);
+#pragma unroll
+                            for (int i = 0; i < E; ++i)
+                                x[i] -= q_of(y[i]);
+                        }
+                        const uint32_t out = gone[(v - v0) >> 5] >> ((v - v0) & 31);
+                        if (out & ((1u << E) - 1))
+#pragma unroll
+                            for (int i = 0; i < E; ++i)
+                                x[i] = (out >> i) & 1u ? 0.0f : x[i];
+#pragma unroll
+                        for (int i = 0; i < E; ++i) {
+                            const float4 f = er[k][i / 4];
+                            weigh(x[i], i % 4 == 0 ? f.x : i % 4 == 1 ? f.y : i % 4 == 2 ? f.z : f.w, v + i);
+                        }
+                    }
+                }
+            } else {
+#pragma unroll 4
+                for (int v = v0 + tid; v < v1; v += kDraw) {
+                    float r = p_of(to_float(row[v]));
+                    if (rejected)
+                        r -= q_of(to_float(less[v]));
+                    weigh((gone[(v - v0) >> 5] >> ((v - v0) & 31)) & 1u ? 0.0f : r, noise[v], v);
+                }
             }
-            if (top)
-                extra = (int)(0xFFFFFFFFu - (uint32_t)top);
+            unsigned long long top = best_of_cta();
+            if (tid == 0)
+                cluster.map_shared_rank(of_cta, 0)[rank] = top;
+            cluster_arrive();
+            if (rank != 0)
+                return;
+            cluster_wait();
+            top = of_cta[0];
+            for (int i = 1; i < ranks; ++i)
+                top = of_cta[i] > top ? of_cta[i] : top;
+            // no weight left: from p itself, and then its largest, by this CTA alone
+            for (int turn = 1; turn < 3 && top == 0; ++turn) {
+                for (int v = tid; v < a.V; v += kDraw)
+                    weigh(p_of(to_float(row[v])), turn == 1 ? noise[v] : 1.0f, v);
+                top = best_of_cta();
+                __syncthreads();
+                if (tid == 0)
+                    of_cta[0] = top;
+                __syncthreads();
+                top = of_cta[0];
+            }
+            extra = (int)(0xFFFFFFFFu - (uint32_t)top);
         }
     }
-    for (int j = tid; j < a.M; j += kThreads) {
+    if (rank != 0)
+        return;
+    const bool dead = (__ldcg(a.status) & kDevStatTimeout) != 0;
+    for (int j = tid; j < a.M; j += kDraw) {
         int token = -1, node = -1;
-        if (!failed && j <= taken) {
-            node = path[j];
-            token = j < taken ? a.tokens[base + path[j + 1]] : extra;
+        if (!failed && !dead && j <= taken) {
+            node = s.path[j];
+            token = j < taken ? s.token[s.path[j + 1]] : extra;
         }
         a.out_tokens[base + j] = token;
         a.out_nodes[base + j] = node;
     }
     if (tid == 0)
-        a.out_n[b] = failed ? FDLLM_ROW_NONFINITE : taken;
+        a.out_n[b] = dead ? FDLLM_ROW_DEVICE_ERROR : failed ? FDLLM_ROW_NONFINITE : taken;
+}
+
+// CTAs that share a sequence's draw: as many as fill the GPU once, where slices stay long enough.
+int draw_ranks(const VerifyArgs &a)
+{
+    if (a.greedy)
+        return 1;
+    int ranks = 1;
+    while (ranks < kMaxRanks && ((int64_t)a.B * ranks * 2 <= 2 * sm_count() || a.V / ranks > (1 << 17)) &&
+           a.V / ranks >= 4096)
+        ranks *= 2;
+    return ranks;
 }
 
 template <typename T>
@@ -259,28 +804,86 @@ cudaError_t launch_verify(const VerifyArgs &a, cudaStream_t s)
 {
     static PerDevice ready;
     cudaError_t e = ready.once([] {
-        return cudaFuncSetAttribute(verify_walk_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                    kMaxRowV / 8);
+        cudaError_t r = cudaFuncSetAttribute(verify_stream_kernel<T, true>,
+                                             cudaFuncAttributeMaxDynamicSharedMemorySize, kStreamSmem);
+        if (r == cudaSuccess)
+            r = cudaFuncSetAttribute(verify_stream_kernel<T, false>,
+                                     cudaFuncAttributeMaxDynamicSharedMemorySize, kStreamSmem);
+        if (r == cudaSuccess)
+            r = cudaFuncSetAttribute(verify_draw_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                     kMaxNodes * Nodes::kBytes + kMaxRowV / 8);
+        return r;
     });
     if (e != cudaSuccess)
         return e;
-    const int64_t rows = (int64_t)a.B * (a.draft ? 2 * a.M - 1 : a.M), most = (int64_t)sm_count() * 4;
-    e = launch(verify_rows_kernel<T>, dim3((unsigned)(rows < most ? rows : most)), dim3(kThreads), 0, s,
-               true, a);
+    const int64_t rows = (int64_t)a.B * (a.draft ? 2 * a.M - 1 : a.M);
+    auto small = a.greedy ? verify_small_kernel<T, true> : verify_small_kernel<T, false>;
+    auto stream = a.greedy ? verify_stream_kernel<T, true> : verify_stream_kernel<T, false>;
+    if ((int64_t)a.V * sizeof(T) <= kSmallRow) {
+        const int64_t want = (rows + 7) / 8, most = (int64_t)sm_count() * 8;
+        e = launch(small, dim3((unsigned)(want < most ? want : most)), dim3(256), 0, s, true, a);
+    } else {
+        const int64_t units = rows * a.pieces, most = sm_count();
+        e = launch(stream, dim3((unsigned)(units < most ? units : most)), dim3(kMath + 32),
+                   kStreamSmem, s, true, a);
+    }
     if (e != cudaSuccess)
         return e;
-    return launch(verify_walk_kernel<T>, dim3(a.B), dim3(kThreads),
-                  a.greedy ? 0 : (size_t)((a.V + 31) / 32) * 4, s, true, a);
+    const int ranks = draw_ranks(a);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(a.B * ranks));
+    cfg.blockDim = dim3(kDraw);
+    cfg.dynamicSmemBytes = draw_smem(a.M, a.V, ranks, a.greedy);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim = {(unsigned)ranks, 1, 1};
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = plain_launches ? 1 : 2;
+    return cudaLaunchKernelEx(&cfg, verify_draw_kernel<T>, VerifyArgs(a));
 }
 
-size_t verify_bytes(int B, int M)
+// How rows are cut: whole, or in pieces of whole chunks so that every SM has some, and no piece is
+// longer than four chunks.
+void cut_rows(int64_t rows, int V, int es, int &pieces, int &piece_vecs, int &per)
 {
-    return ((size_t)B * (2 * (size_t)M - 1) * sizeof(UnitPartial) + 255) / 256 * 256;
+    if ((int64_t)V * es <= kSmallRow) {
+        pieces = per = 1;
+        piece_vecs = 0;
+        return;
+    }
+    // vectors that a row has wherever it begins, so that no piece is empty
+    const int E = 16 / es, vecs = (V - (E - 1)) / E;
+    const int chunks = (vecs + kChunkVecs - 1) / kChunkVecs;
+    int of = 4;
+    while (of > 1 && rows * ((chunks + of - 1) / of) < 2 * 152)
+        --of;
+    pieces = (chunks + of - 1) / of;
+    piece_vecs = of * kChunkVecs;
+    per = pieces * kMathWarps;
+}
+
+int64_t verify_rows(int B, int M) { return (int64_t)B * (2 * (int64_t)M - 1); }
+
+size_t verify_bytes(int B, int M, int V, int dtype)
+{
+    int pieces, vecs, most = 0;
+    // (with the draft's rows or without)
+    for (int64_t rows : {verify_rows(B, M), (int64_t)B * M}) {
+        int per;
+        cut_rows(rows, V, rows_esize(dtype), pieces, vecs, per);
+        most = per > most ? per : most;
+    }
+    return ((size_t)verify_rows(B, M) * most * sizeof(UnitPartial) + 255) / 256 * 256;
 }
 
 bool verify_sizes(int B, int M, int V)
 {
-    return B >= 1 && B <= kMaxGridYZ && M >= 1 && M <= kMaxNodes && V >= 1 && V <= kMaxRowV;
+    // (pieces are counted in 32 bits)
+    return B >= 1 && B <= kMaxGridYZ && M >= 1 && M <= kMaxNodes && V >= 1 && V <= kMaxRowV &&
+           verify_rows(B, M) * (V / 4096 + 1) < ((int64_t)1 << 31);
 }
 
 }  // namespace
@@ -292,7 +895,7 @@ extern "C" {
 
 size_t fdllm_verify_draft_workspace_bytes(int B, int M, int V, int dtype)
 {
-    return verify_sizes(B, M, V) && rows_dtype(dtype) ? verify_bytes(B, M) : 0;
+    return verify_sizes(B, M, V) && rows_dtype(dtype) ? verify_bytes(B, M, V, dtype) : 0;
 }
 
 fdllm_status fdllm_verify_draft(const void *target, const void *draft, int dtype, int B, int M,
@@ -312,7 +915,7 @@ fdllm_status fdllm_verify_draft(const void *target, const void *draft, int dtype
           reinterpret_cast<uintptr_t>(noise)) & 15u) != 0)
         return FDLLM_ERR_ALIGN;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 ||
-        workspace_bytes < verify_bytes(B, M))
+        workspace_bytes < verify_bytes(B, M, V, dtype))
         return FDLLM_ERR_WORKSPACE;
     VerifyArgs a = {};
     a.target = target;
@@ -331,7 +934,11 @@ fdllm_status fdllm_verify_draft(const void *target, const void *draft, int dtype
     a.out_tokens = out_tokens;
     a.out_nodes = out_nodes;
     a.out_n = out_n;
-    a.partials = static_cast<UnitPartial *>(workspace);
+    a.parts = static_cast<UnitPartial *>(workspace);
+    cut_rows((int64_t)B * (a.draft ? 2 * M - 1 : M), V, rows_esize(dtype), a.pieces, a.piece_vecs, a.per);
+    a.status = cache_status_word();
+    if (!a.status)
+        return FDLLM_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const cudaError_t e = dtype == FDLLM_BF16   ? launch_verify<__nv_bfloat16>(a, s)
                           : dtype == FDLLM_FP16 ? launch_verify<__half>(a, s)

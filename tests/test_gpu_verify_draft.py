@@ -57,8 +57,10 @@ def cuda(x):
 
 
 def run(fd, target, tokens, **kw):
-    return [x.cpu() for x in fd.fdllm_verify_draft(
+    got = [x.cpu() for x in fd.fdllm_verify_draft(
         target.cuda(), tokens.cuda(), **{k: cuda(v) for k, v in kw.items()})]
+    assert fd.fdllm_cache_status() == 0
+    return got
 
 
 def check(fd, target, tokens, most_near=0, **kw):
