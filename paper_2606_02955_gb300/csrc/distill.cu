@@ -19,7 +19,8 @@ namespace fdllm {
 namespace {
 
 constexpr int kMaxTop = 1024;
-constexpr int kThreads = 512;
+constexpr int kThreads = 128;      // of a CTA of the small form
+constexpr int kSmallRow = 16384;   // rows up to this many bytes take it
 
 struct DistillArgs {
     const void *logits;      // [rows, V]
@@ -38,6 +39,7 @@ struct DistillArgs {
     float4 *stats_out;       // [rows]: what the gradient needs of a row
     const float4 *stats_in;
     void *grad;              // [rows, V]
+    uint32_t *status;        // sticky: a bounded wait gave up
 };
 
 __device__ __forceinline__ float top_value(const DistillArgs &a, int64_t i)
@@ -78,9 +80,10 @@ struct Most {  // a NaN stays
     }
 };
 
+// ---- Short rows: a CTA of kThreads to a row.
 // kSum: the row's sums are taken (else they are given); kGrad: the gradient is written.
 template <typename T, bool kSum, bool kGrad>
-__global__ void __launch_bounds__(kThreads) distill_kernel(const __grid_constant__ DistillArgs a)
+__global__ void __launch_bounds__(kThreads, 8) distill_small_kernel(const __grid_constant__ DistillArgs a)
 {
     constexpr int E = 16 / sizeof(T);
     constexpr int kMine = kMaxTop / kThreads;  // listed tokens of a thread
@@ -289,32 +292,755 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(const __grid_constant
     }
 }
 
+// ---- Longer rows: a CTA, or a cluster of them, holds a row in shared memory from its sum to its
+// gradient.
+//
+// Roles.  Sixteen warps walk the row (the sum, then the gradient); four look after the teacher: for the
+// row to come they read its list and the student's logits of it, make the probabilities and what
+// else is of the list alone, and mark the listed tokens, and for the row before they write the
+// listed tokens' gradients over what the sixteen wrote there; one lane copies rows into a ring of
+// shared memory, and one warp writes the rows of zeros.
+//
+// The ring.  Chunks of a row come in order; the first pass gives back those that the ring cannot
+// hold beside the others, which come again (from the L2, where they have just been) behind the
+// row's last; the second pass starts with the oldest that is still there, and each chunk it gives back
+// makes room for one of the next row.
+constexpr int kMathWarps = 16, kMath = 32 * kMathWarps;
+constexpr int kTeachers = 128;
+constexpr int kRingThreads = kMath + kTeachers + 64;
+constexpr int kChunk = 32768, kChunkVecs = kChunk / 16, kPer = kChunkVecs / kMath;
+constexpr int kStages = 6;
+constexpr int kMostListed = 1 << 17;  // tokens of a CTA's share of a row: their bits take 16 KB
+constexpr int kZeros = 2048;
+constexpr int kMaxRanks = 8;
+enum { kBarMath = 1, kBarTeach };
+
+// The masked rows, or the others, of this cluster: every n-th of them.  A warp looks at 512 rows at a
+// time, 16 to a lane.
+struct RowWalk {
+    const uint8_t *mask;
+    int64_t rows, base, before;  // rows below base are passed, `before` of the kind among them
+    uint32_t bits, upto;         // this lane's 16 rows; how many of the kind up to and with them
+    int in_block;
+    bool masked;
+
+    __device__ __forceinline__ void load()
+    {
+        const int64_t r = base + 16 * (threadIdx.x & 31);
+        bits = 0;
+        if (r + 16 <= rows && (reinterpret_cast<uintptr_t>(mask + r) & 15u) == 0) {
+            const uint4 v = *reinterpret_cast<const uint4 *>(mask + r);
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                bits |= ((w[i >> 2] >> (8 * (i & 3))) & 0xFFu) != 0 ? 1u << i : 0u;
+        } else {
+            for (int i = 0; i < 16 && r + i < rows; ++i)
+                bits |= mask[r + i] != 0 ? 1u << i : 0u;
+        }
+        if (!masked)
+            bits = ~bits & (r >= rows ? 0u : r + 16 <= rows ? 0xFFFFu : (1u << (rows - r)) - 1);
+        upto = __popc(bits);
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t x = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+            upto += (threadIdx.x & 31) >= o ? x : 0;
+        }
+        in_block = (int)__shfl_sync(0xFFFFFFFFu, upto, 31);
+    }
+    __device__ __forceinline__ RowWalk(const uint8_t *m, int64_t n, bool of_masked)
+        : mask(m), rows(n), base(0), before(0), masked(of_masked)
+    {
+        load();
+    }
+    // The rank-th row of the kind (ranks grow from call to call), -1: there are not so many.
+    __device__ __forceinline__ int64_t find(int64_t rank)
+    {
+        while (rank >= before + in_block) {
+            if (base + 512 >= rows)
+                return -1;
+            before += in_block;
+            base += 512;
+            load();
+        }
+        const uint32_t in = (uint32_t)(rank - before);
+        const uint32_t lane = __ffs(__ballot_sync(0xFFFFFFFFu, upto > in)) - 1;
+        uint32_t skip = in - (upto - __popc(bits)), b = bits;
+        if ((threadIdx.x & 31) == lane)
+            for (; skip > 0; --skip)
+                b &= b - 1;
+        const int at = __shfl_sync(0xFFFFFFFFu, __ffs(b) - 1, lane);
+        return base + 16 * lane + at;
+    }
+};
+
+// A CTA's share of a row: whole vectors [v0, v1), the first CTA's with the values before them, the
+// last's with those behind.
 template <typename T>
-cudaError_t launch_distill(const DistillArgs &a, bool sum, bool grad, cudaStream_t s)
+struct RowShare {
+    RowSpan<T> r;
+    int v0, v1;
+    __device__ __forceinline__ RowShare(const void *base, int64_t row, int V, int rank, int ranks)
+        : r(static_cast<const T *>(base) + row * V, V)
+    {
+        const int per = (r.vecs + ranks - 1) / ranks;
+        v0 = min(r.vecs, rank * per);
+        v1 = min(r.vecs, v0 + per);
+    }
+    __device__ __forceinline__ int chunks() const { return (v1 - v0 + kChunkVecs - 1) / kChunkVecs; }
+    __device__ __forceinline__ int in_chunk(int j) const { return min(kChunkVecs, v1 - v0 - j * kChunkVecs); }
+};
+
+// What the teachers' warps leave for a row.
+struct Taught {
+    int64_t row;         // -1: no more
+    float P, R;
+    float A;             // sum p_k (log p_k - (x_k - m) / T)
+    ExpSum x;            // of the listed tokens' logits
+    float scale;         // gradient of the loss / T
+    uint32_t ends;       // a bit for each listed value out of the whole vectors: 8 before, 8 behind
+    float M, Z;          // of all tokens, and
+    ExpSum rest;         // of the others, where they are given
+};
+
+struct RingShared {
+    uint64_t full[kStages], empty[kStages];
+    uint64_t ready[2];    // of a row, by parity: its list is taught
+    uint64_t swept[2];    // the first pass is done, its marks are not needed
+    uint64_t written[2];  // the second is done, the listed tokens may be written
+    uint64_t crossed[2];  // the cluster's sums are here
+    Taught taught[2];
+    float4 fix[2];        // for the listed tokens: M, Z, P + R, scale
+    ExpSum part[2][kMathWarps];
+    ExpSum of_rank[2][kMaxRanks];
+    float reduce[3][4];
+    int twice;
+    uint32_t ends;
+};
+
+constexpr int kListedOff = kStages * kChunk, kZerosOff = kListedOff + kMostListed / 8 + 16;
+constexpr int kDupOff = kZerosOff + kZeros, kSharedOff = kDupOff + kMaxTop * 8;
+constexpr int kRingSmem = kSharedOff + (int)sizeof(RingShared);
+static_assert(kRingSmem <= 227 * 1024 && kSharedOff % 16 == 0 && kZerosOff % 16 == 0, "shared memory");
+
+// Eight bytes to another CTA of the cluster, counted by a barrier there.
+__device__ __forceinline__ void send_sum(const ExpSum *slot, const uint64_t *bar, int to, const ExpSum &v)
 {
-    const size_t smem = (size_t)((a.V + 31) / 32) * 4;
+    uint32_t at, b;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_addr(slot)), "r"(to));
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(b) : "r"(smem_addr(bar)), "r"(to));
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.b32 [%0], {%1, %2}, [%3];" ::"r"(at),
+                 "r"(__float_as_uint(v.m)), "r"(__float_as_uint(v.z)), "r"(b)
+                 : "memory");
+}
+
+// -inf in the place of the values whose bits are set.
+template <typename T>
+__device__ __forceinline__ void leave_out(uint4 &r, uint32_t bits)
+{
+    constexpr uint32_t kPad = no_values<T>();
+    uint32_t *w = reinterpret_cast<uint32_t *>(&r);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) {
+            w[i] = (bits >> i) & 1u ? kPad : w[i];
+        } else {
+            const uint32_t keep = ((bits >> (2 * i)) & 1u ? 0u : 0xFFFFu) |
+                                  ((bits >> (2 * i + 1)) & 1u ? 0u : 0xFFFF0000u);
+            w[i] = (w[i] & keep) | (kPad & ~keep);
+        }
+    }
+}
+
+// Sum (or maximum) over the teachers' warps, the same bits in every thread.
+template <typename F>
+__device__ __forceinline__ float teach_reduce(float x, float *of_warp, F f)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+        x = f(x, __shfl_xor_sync(0xFFFFFFFFu, x, o));
+    if ((threadIdx.x & 31) == 0)
+        of_warp[(threadIdx.x - kMath) >> 5] = x;
+    named_sync(kBarTeach, kTeachers);
+    return f(f(of_warp[0], of_warp[1]), f(of_warp[2], of_warp[3]));
+}
+
+template <typename T, bool kSum, bool kGrad>
+__global__ void __launch_bounds__(kRingThreads, 1)
+    distill_ring_kernel(const __grid_constant__ DistillArgs a, int ranks)
+{
+    constexpr int E = 16 / sizeof(T);
+    extern __shared__ __align__(128) uint8_t smem[];
+    uint8_t *const listed = smem + kListedOff;  // a bit for each value of the share's vectors
+    RingShared &sm = *reinterpret_cast<RingShared *>(smem + kSharedOff);
+    const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31;
+    const int rank = blockIdx.x % ranks, cluster = blockIdx.x / ranks, clusters = gridDim.x / ranks;
+    const float c = a.inv_t * kLog2e;
+    if (tid == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(&sm.full[i], 1);
+            mbar_init(&sm.empty[i], kMathWarps);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&sm.ready[i], 1);
+            mbar_init(&sm.swept[i], 1);
+            mbar_init(&sm.written[i], kMathWarps);
+            mbar_init(&sm.crossed[i], 1);
+        }
+        fence_mbar_init();
+    }
+    for (int i = tid; i < (kMostListed / 8 + 16) / 4; i += kRingThreads)
+        reinterpret_cast<uint32_t *>(listed)[i] = 0;
+    for (int i = tid; i < kZeros / 4; i += kRingThreads)
+        reinterpret_cast<uint32_t *>(smem + kZerosOff)[i] = 0;
+    fence_async_smem();
+    __syncthreads();
+    if (ranks > 1) {
+        cluster_arrive();
+        cluster_wait();
+    }
+    pdl_wait();
+    // A wait that gave up: no further wait.  Math's and the teachers' warps leave by a vote, before
+    // they look at what was never left for them.
+    bool dead = false;
+    auto wait = [&](uint64_t *bar, uint32_t parity) {
+        if (!dead && !mbar_wait(bar, parity, a.status))
+            dead = true;
+    };
+
+    if (warp < kMathWarps) {
+        // ------------------------------------------------------------ the row
+        uint32_t kb = 0;  // chunks of the rows before
+        for (uint32_t i = 0;; ++i) {
+            const uint32_t par = i & 1;
+            wait(&sm.ready[par], (i >> 1) & 1);
+            const Taught &of = sm.taught[par];
+            if (named_sync_or(kBarMath, kMath, dead || of.row < 0))
+                break;
+            const RowShare<T> sh(a.logits, of.row, a.V, rank, ranks);
+            const int chunks = sh.chunks();
+            const int again = kSum && kGrad ? max(0, chunks - kStages) : 0;
+            const int end = lane < 8 ? lane : sh.r.tail() + lane - 8;  // warp 0: a value of the ends
+            const bool has_end = warp == 0 && lane < 16 &&
+                                 (lane < 8 ? rank == 0 && end < sh.r.head : rank == ranks - 1 && end < a.V);
+            float M = of.M, Z = of.Z, R = of.R;
+            ExpSum rest = of.rest;
+            if constexpr (kSum) {
+                // ---- the tokens that are not listed
+                Summed sum;
+                for (int j = 0; j < chunks; ++j) {
+                    const uint32_t k = kb + j, st = k % kStages;
+                    wait(&sm.full[st], (k / kStages) & 1);
+                    const uint4 *buf = reinterpret_cast<const uint4 *>(smem + st * kChunk);
+                    const int n = sh.in_chunk(j);
+                    uint4 x[kPer];
+                    uint32_t bits[kPer], any = 0;
+#pragma unroll
+                    for (int q = 0; q < kPer; ++q) {
+                        const int v = tid + q * kMath, at = j * kChunkVecs + v;
+                        constexpr uint32_t kPad = no_values<T>();
+                        x[q] = make_uint4(kPad, kPad, kPad, kPad);
+                        bits[q] = 0;
+                        if (v < n) {
+                            x[q] = buf[v];
+                            bits[q] = E == 8 ? listed[at] : (listed[at >> 1] >> (4 * (at & 1))) & 15u;
+                        }
+                        any |= bits[q];
+                    }
+                    if (!kGrad || j < again) {
+                        __syncwarp();
+                        if (lane == 0)
+                            mbar_arrive(&sm.empty[st]);
+                    }
+                    if (any)
+#pragma unroll
+                        for (int q = 0; q < kPer; ++q)
+                            if (bits[q])
+                                leave_out<T>(x[q], bits[q]);
+                    sum.add<T, kPer>(x, c);
+                }
+                sum.settle(c);
+                if (has_end && !((of.ends >> lane) & 1u))
+                    sum.z.add(to_float(sh.r.row[end]), c);
+                __syncwarp();
+                rest = warp_sum(sum.z, c);
+                if (lane == 0)
+                    sm.part[par][warp] = rest;
+                named_sync(kBarMath, kMath);
+                if (tid == 0)
+                    mbar_arrive(&sm.swept[par]);
+                rest = sm.part[par][lane & 15];
+#pragma unroll
+                for (int o = 8; o > 0; o >>= 1) {
+                    ExpSum p;
+                    p.m = __shfl_xor_sync(0xFFFFFFFFu, rest.m, o);
+                    p.z = __shfl_xor_sync(0xFFFFFFFFu, rest.z, o);
+                    rest.merge(p, c);
+                }
+                if (ranks > 1) {
+                    if (tid == 0)
+                        mbar_arrive_expect_tx(&sm.crossed[par], 8 * ranks);
+                    if (warp == 0 && lane < ranks)
+                        send_sum(&sm.of_rank[par][rank], &sm.crossed[par], lane, rest);
+                    wait(&sm.crossed[par], (i >> 1) & 1);
+                    rest = sm.of_rank[par][0];
+                    for (int q = 1; q < ranks; ++q)
+                        rest.merge(sm.of_rank[par][q], c);
+                }
+                // ---- all tokens, the listed ones among them
+                M = fmaxf(rest.m, of.x.m);
+                Z = rest.z * ex2_mufu((rest.m - M) * c) + of.x.z * ex2_mufu((of.x.m - M) * c);
+                if (!(Z > 0.0f && Z <= FLT_MAX) || !finite_f(M))
+                    Z = nan_f();
+                if (rest.z == 0.0f)
+                    R = 0.0f;
+                if (rank == 0 && tid == 0) {
+                    const float log_z = logf(Z);
+                    float loss = of.A;
+                    if (of.P != 0.0f)
+                        loss += of.P * ((M - of.x.m) * a.inv_t + log_z);
+                    if (R > 0.0f)
+                        loss += R * (logf(R) - ((rest.m - M) * a.inv_t + logf(rest.z) - log_z));
+                    a.loss[of.row] = Z == Z ? loss : Z;
+                    if (a.stats_out)
+                        a.stats_out[of.row] = make_float4(M, Z, rest.m, rest.z);
+                }
+            } else if (rest.z == 0.0f) {
+                R = 0.0f;
+            }
+            if constexpr (kGrad) {
+                const float scale = of.scale;
+                const float r = rest.z * ex2_mufu((rest.m - M) * c) / Z;
+                if (tid == 0)
+                    sm.fix[par] = make_float4(M, Z, of.P + R, scale);
+                // of s_v relative to the reference of the others
+                float f = rest.z == 0.0f ? (Z == Z ? 0.0f : Z) : scale * (r * (of.P + R) - R) / rest.z;
+                T *grad = static_cast<T *>(a.grad) + of.row * a.V;
+                if (has_end)
+                    grad[end] = from_float<T>(ex2_mufu((to_float(sh.r.row[end]) - rest.m) * c) * f);
+                uint4 *out = reinterpret_cast<uint4 *>(grad + sh.r.head) + sh.v0;
+                const float ref = rest.m * c;
+                const bool far = !(fabsf(ref) < kFar);
+                if (!far)
+                    f *= ex2_mufu(-fmaf(rest.m, c, -ref));
+                const uint64_t f2f = f2(f, f), c2 = f2(c, c);
+                const uint64_t n2 = far ? f2(-rest.m, -rest.m) : f2(-ref, -ref);
+                for (int q = 0; q < chunks; ++q) {
+                    // the retained chunks, then those that came again
+                    const int j = q < chunks - again ? q + again : q - (chunks - again);
+                    const uint32_t k = kb + (q < chunks - again ? j : chunks + j), st = k % kStages;
+                    if (!kSum || q >= chunks - again)
+                        wait(&sm.full[st], (k / kStages) & 1);
+                    const uint4 *buf = reinterpret_cast<const uint4 *>(smem + st * kChunk);
+                    const int n = sh.in_chunk(j);
+                    uint4 x[kPer];
+#pragma unroll
+                    for (int p = 0; p < kPer; ++p) {
+                        const int v = tid + p * kMath;
+                        if (v < n)
+                            x[p] = buf[v];
+                    }
+                    __syncwarp();
+                    if (lane == 0)
+                        mbar_arrive(&sm.empty[st]);
+#pragma unroll
+                    for (int p = 0; p < kPer; ++p) {
+                        const int v = tid + p * kMath;
+                        if (v >= n)
+                            continue;
+                        float y[E];
+                        widen<T>(x[p], y);
+#pragma unroll
+                        for (int e = 0; e < E; e += 2) {
+                            const uint64_t y2 = f2(y[e], y[e + 1]);
+                            float t0, t1;
+                            un2(far ? mul2(add2(y2, n2), c2) : fma2(y2, c2, n2), t0, t1);
+                            un2(mul2(f2(ex2_mufu(t0), ex2_mufu(t1)), f2f), y[e], y[e + 1]);
+                        }
+                        __stcs(out + j * kChunkVecs + v, narrow<T>(y));
+                    }
+                }
+                __syncwarp();
+                if (lane == 0)
+                    mbar_arrive(&sm.written[par]);
+            }
+            kb += chunks + again;
+        }
+    } else if (warp < kMathWarps + kTeachers / 32) {
+        // ------------------------------------------------------------ the teacher
+        constexpr int kMine = kMaxTop / kTeachers;
+        const int t = tid - kMath;
+        int *const idx = reinterpret_cast<int *>(smem + kDupOff);
+        float *const mass = reinterpret_cast<float *>(idx + kMaxTop);
+        RowWalk walk(a.mask, a.rows, true);
+        int old[kMine];  // of the row before: its listed tokens, and what their gradients need
+        float old_p[kMine], old_x[kMine];
+        int64_t old_row = -1;
+#pragma unroll
+        for (int j = 0; j < kMine; ++j)
+            old[j] = -1, old_p[j] = old_x[j] = 0.0f;
+        for (uint32_t i = 0;; ++i) {
+            const uint32_t par = i & 1;
+            const int64_t row = walk.find(cluster + (int64_t)i * clusters);
+            int v[kMine];
+            float m[kMine], x[kMine];
+            float P = 0.0f, R = 0.0f, A = 0.0f, scale = 0.0f;
+            ExpSum of_x;
+            float4 given = make_float4(0, 0, 0, 0);
+            if (row >= 0) {
+                const T *logits = static_cast<const T *>(a.logits) + row * a.V;
+                float most = -FLT_MAX;
+#pragma unroll
+                for (int j = 0; j < kMine; ++j) {
+                    const int k = t + j * kTeachers;
+                    v[j] = -1;
+                    m[j] = neg_inf_f();
+                    if (k < a.K) {
+                        const int at = a.index[row * a.K + k];
+                        if (at >= 0 && at < a.V) {
+                            v[j] = at;
+                            m[j] = __fdiv_rn(top_value(a, row * a.K + k), a.temperature);
+                        }
+                        most = Most()(most, m[j]);
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < kMine; ++j)
+                    x[j] = v[j] >= 0 ? to_float(logits[v[j]]) : neg_inf_f();
+                if (kGrad)
+                    scale = a.grad_loss[row] * a.inv_t;
+                if (!kSum)
+                    given = a.stats_in[row];
+                most = a.lse ? a.lse[row] : teach_reduce(most, sm.reduce[0], Most());
+#pragma unroll
+                for (int j = 0; j < kMine; ++j) {
+                    m[j] = v[j] >= 0 ? expf(m[j] - most) : 0.0f;
+                    P += m[j];
+                }
+                P = teach_reduce(P, sm.reduce[1], Add());
+                if (a.lse) {
+                    R = fmaxf(1.0f - P, 0.0f);
+                } else if (P != 0.0f) {
+#pragma unroll
+                    for (int j = 0; j < kMine; ++j)
+                        m[j] = __fdiv_rn(m[j], P);
+                    P = P == P ? 1.0f : P;
+                }
+            }
+            // ---- the marks: the row before's go, this one's come
+            if (kSum && i > 0)
+                wait(&sm.swept[par ^ 1], ((i - 1) >> 1) & 1);
+            if (named_sync_or(kBarTeach, kTeachers, dead))
+                break;
+            auto mark = [&](int64_t of_row, int at, bool set) -> bool {  // whether it was set before
+                const RowShare<T> sh(a.logits, of_row, a.V, rank, ranks);
+                uint32_t *word, bit;
+                if (at < sh.r.head) {
+                    word = &sm.ends;
+                    bit = at;
+                } else if (at >= sh.r.tail()) {
+                    word = &sm.ends;
+                    bit = 8 + at - sh.r.tail();
+                } else {
+                    const int b = at - sh.r.head - sh.v0 * E;
+                    if (b < 0 || b >= (sh.v1 - sh.v0) * E)
+                        return false;
+                    word = reinterpret_cast<uint32_t *>(listed) + (b >> 5);
+                    bit = b & 31;
+                }
+                if (set)
+                    return (atomicOr(word, 1u << bit) >> bit) & 1u;
+                atomicAnd(word, ~(1u << bit));
+                return false;
+            };
+            if (old_row >= 0)
+#pragma unroll
+                for (int j = 0; j < kMine; ++j)
+                    if (old[j] >= 0)
+                        mark(old_row, old[j], false);
+            if (t == 0) {
+                sm.ends = 0;
+                sm.twice = 0;
+            }
+            named_sync(kBarTeach, kTeachers);
+            if (row >= 0) {
+                bool again = false;
+#pragma unroll
+                for (int j = 0; j < kMine; ++j)
+                    if (v[j] >= 0)
+                        again |= mark(row, v[j], true);
+                if (ranks > 1) {
+                    // the marks are of this CTA's share: other tokens are looked up in a table
+                    const int size = a.K <= 64 ? 128 : 2 << (32 - __clz(a.K - 1));
+                    for (int q = t; q < size; q += kTeachers)
+                        idx[q] = -1;
+                    named_sync(kBarTeach, kTeachers);
+#pragma unroll
+                    for (int j = 0; j < kMine; ++j) {
+                        if (v[j] < 0)
+                            continue;
+                        int h = (int)((uint32_t)v[j] * 2654435761u >> (__clz(size) + 1));
+                        for (int q = 0; q < size; ++q, h = (h + 1) & (size - 1)) {
+                            const int there = atomicCAS(&idx[h], -1, v[j]);
+                            if (there == -1)
+                                break;
+                            if (there == v[j]) {
+                                again = true;
+                                break;
+                            }
+                        }
+                    }
+                }
+                if (again)
+                    sm.twice = 1;
+                named_sync(kBarTeach, kTeachers);
+                if (sm.twice) {
+                    // a token listed more than once: its masses count together, in its first place
+#pragma unroll
+                    for (int j = 0; j < kMine; ++j)
+                        if (t + j * kTeachers < a.K) {
+                            idx[t + j * kTeachers] = v[j];
+                            mass[t + j * kTeachers] = m[j];
+                        }
+                    named_sync(kBarTeach, kTeachers);
+#pragma unroll
+                    for (int j = 0; j < kMine; ++j) {
+                        const int k = t + j * kTeachers;
+                        if (v[j] < 0)
+                            continue;
+                        m[j] = 0.0f;
+                        for (int q = 0; q < a.K; ++q)
+                            if (idx[q] == v[j]) {
+                                if (q < k) {
+                                    v[j] = -1;
+                                    break;
+                                }
+                                m[j] += mass[q];
+                            }
+                    }
+                }
+                // ---- what is of the listed tokens alone
+                float top = -FLT_MAX;
+#pragma unroll
+                for (int j = 0; j < kMine; ++j)
+                    if (v[j] >= 0)
+                        top = Most()(top, x[j]);
+                top = teach_reduce(top, sm.reduce[0], Most());
+                of_x.m = top;
+                float z = 0.0f;
+#pragma unroll
+                for (int j = 0; j < kMine; ++j)
+                    if (v[j] >= 0) {
+                        z += ex2_mufu((x[j] - top) * c);
+                        if (m[j] != 0.0f)
+                            A += m[j] * (logf(m[j]) - (x[j] - top) * a.inv_t);
+                    }
+                of_x.z = teach_reduce(z, sm.reduce[1], Add());
+                A = teach_reduce(A, sm.reduce[2], Add());
+            }
+            if (t == 0) {
+                Taught &of = sm.taught[par];
+                of.row = row;
+                of.P = P;
+                of.R = R;
+                of.A = A;
+                of.x = of_x;
+                of.scale = scale;
+                of.ends = sm.ends;
+                of.M = given.x;
+                of.Z = given.y;
+                of.rest.m = given.z;
+                of.rest.z = given.w;
+                mbar_arrive(&sm.ready[par]);
+            }
+            // ---- the gradients of the row before's listed tokens
+            if (kGrad && old_row >= 0) {
+                wait(&sm.written[par ^ 1], ((i - 1) >> 1) & 1);
+                if (!dead) {
+                    const float4 fix = sm.fix[par ^ 1];
+                    const RowShare<T> sh(a.logits, old_row, a.V, rank, ranks);
+                    T *grad = static_cast<T *>(a.grad) + old_row * a.V;
+#pragma unroll
+                    for (int j = 0; j < kMine; ++j) {
+                        const int at = old[j];
+                        if (at < 0)
+                            continue;
+                        const int b = at - sh.r.head;
+                        const bool mine = at < sh.r.head       ? rank == 0
+                                          : at >= sh.r.tail() ? rank == ranks - 1
+                                                              : b >= sh.v0 * E && b < sh.v1 * E;
+                        if (mine)
+                            grad[at] = from_float<T>(
+                                fix.w * (ex2_mufu((old_x[j] - fix.x) * c) / fix.y * fix.z - old_p[j]));
+                    }
+                }
+            }
+            if (row < 0)
+                break;
+            old_row = row;
+#pragma unroll
+            for (int j = 0; j < kMine; ++j) {
+                old[j] = v[j];
+                old_p[j] = m[j];
+                old_x[j] = x[j];
+            }
+        }
+    } else if (warp == kMathWarps + kTeachers / 32) {
+        // ------------------------------------------------------------ the copies
+        const uint64_t policy = make_evict_first_policy();
+        RowWalk walk(a.mask, a.rows, true);
+        uint32_t k = 0;
+        for (uint32_t i = 0; !dead; ++i) {
+            const int64_t row = walk.find(cluster + (int64_t)i * clusters);
+            if (row < 0)
+                break;
+            const RowShare<T> sh(a.logits, row, a.V, rank, ranks);
+            const int chunks = sh.chunks();
+            const int again = kSum && kGrad ? max(0, chunks - kStages) : 0;
+            if (lane == 0)
+                for (int q = 0; q < chunks + again; ++q, ++k) {
+                    const int j = q < chunks ? q : q - chunks;
+                    const uint32_t st = k % kStages, n = sh.in_chunk(j) * 16;
+                    if (k >= kStages)
+                        wait(&sm.empty[st], (k / kStages - 1) & 1);
+                    if (dead)
+                        break;
+                    const void *src = sh.r.vectors() + sh.v0 + j * kChunkVecs;
+                    mbar_arrive_expect_tx(&sm.full[st], n);
+                    if (q < again)  // (comes again)
+                        bulk_copy_g2s(smem + st * kChunk, src, n, &sm.full[st]);
+                    else
+                        bulk_copy_g2s_hint(smem + st * kChunk, src, n, &sm.full[st], policy);
+                }
+            dead = __any_sync(0xFFFFFFFFu, dead);
+        }
+        // nothing may land in this CTA's memory after it has gone
+        if (lane == 0)
+            for (uint32_t i = k > kStages ? k - kStages : 0; i < k; ++i)
+                mbar_wait(&sm.full[i % kStages], (i / kStages) & 1, a.status, kDrainLimitNs);
+    } else {
+        // ------------------------------------------------------------ positions that do not count
+        RowWalk walk(a.mask, a.rows, false);
+        for (uint32_t i = 0;; ++i) {
+            const int64_t row = walk.find(cluster + (int64_t)i * clusters);
+            if (row < 0)
+                break;
+            if (kSum && rank == 0 && lane == 0) {
+                a.loss[row] = 0.0f;
+                if (a.stats_out)
+                    a.stats_out[row] = make_float4(0, 0, 0, 0);
+            }
+            if constexpr (kGrad) {
+                const RowShare<T> sh(a.grad, row, a.V, rank, ranks);
+                T *grad = static_cast<T *>(a.grad) + row * a.V;
+                if (rank == 0 && lane < sh.r.head)
+                    grad[lane] = from_float<T>(0.0f);
+                if (rank == ranks - 1 && sh.r.tail() + lane < a.V)
+                    grad[sh.r.tail() + lane] = from_float<T>(0.0f);
+                const int64_t bytes = (int64_t)(sh.v1 - sh.v0) * 16;
+                uint8_t *p = reinterpret_cast<uint8_t *>(grad + sh.r.head) + (int64_t)sh.v0 * 16;
+                for (int64_t o = (int64_t)lane * kZeros; o < bytes; o += 32 * kZeros)
+                    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(p + o),
+                                 "r"(smem_addr(smem + kZerosOff)), "r"((uint32_t)min((int64_t)kZeros, bytes - o))
+                                 : "memory");
+                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+            }
+        }
+        if constexpr (kGrad)
+            asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    }
+    if (ranks > 1) {  // no CTA leaves while another may send to it
+        __syncwarp();
+        cluster_arrive();
+        cluster_wait();
+    }
+}
+
+// CTAs that share a row: one where there are rows for all SMs; more where rows are few, as long as
+// shares have two chunks, or where a share's bits would not fit.
+int row_ranks(int64_t rows, int V, int es)
+{
+    int ranks = 1;
+    while (ranks < kMaxRanks &&
+           (V / ranks > kMostListed - 64 ||
+            (rows * ranks * 2 <= sm_count() && (int64_t)V * es / ranks >= 4 * kChunk)))
+        ranks *= 2;
+    return ranks;
+}
+
+// Clusters of `ranks` CTAs that the GPU holds at once.
+template <typename K>
+int resident(K kern, int ranks)
+{
+    if (ranks == 1)
+        return sm_count();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(sm_count() / ranks * ranks));
+    cfg.blockDim = dim3(kRingThreads);
+    cfg.dynamicSmemBytes = kRingSmem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim = {(unsigned)ranks, 1, 1};
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess || n < 1) {
+        cudaGetLastError();
+        n = sm_count() / ranks;
+    }
+    return n;
+}
+
+template <typename T, bool kSum, bool kGrad>
+cudaError_t launch_kind(const DistillArgs &a, cudaStream_t s)
+{
+    constexpr int es = sizeof(T);
+    if ((int64_t)a.V * es <= kSmallRow) {
+        auto *kern = distill_small_kernel<T, kSum, kGrad>;
+        const int64_t most = (int64_t)sm_count() * 16;
+        return launch(kern, dim3((unsigned)(a.rows < most ? a.rows : most)), dim3(kThreads),
+                      (size_t)((a.V + 31) / 32) * 4, s, true, a);
+    }
+    auto *kern = distill_ring_kernel<T, kSum, kGrad>;
     static PerDevice ready;
-    cudaError_t e = ready.once([] {
-        const int most = kMaxRowV / 8;
-        cudaError_t r = cudaFuncSetAttribute(distill_kernel<T, true, false>,
-                                             cudaFuncAttributeMaxDynamicSharedMemorySize, most);
-        if (r == cudaSuccess)
-            r = cudaFuncSetAttribute(distill_kernel<T, true, true>,
-                                     cudaFuncAttributeMaxDynamicSharedMemorySize, most);
-        if (r == cudaSuccess)
-            r = cudaFuncSetAttribute(distill_kernel<T, false, true>,
-                                     cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+    static std::atomic<int> held[kMaxCacheDevices][4];
+    cudaError_t e = ready.once([&] {
+        const cudaError_t r = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingSmem);
+        int dev = 0;
+        if (r == cudaSuccess && cudaGetDevice(&dev) == cudaSuccess)
+            for (int i = 0; i < 4; ++i)
+                held[dev][i] = resident(kern, 1 << i);
         return r;
     });
     if (e != cudaSuccess)
         return e;
-    const int64_t most = (int64_t)sm_count() * 2;
-    const dim3 grid((unsigned)(a.rows < most ? a.rows : most)), block(kThreads);
-    if (sum && grad)
-        return launch(distill_kernel<T, true, true>, grid, block, smem, s, true, a);
-    if (sum)
-        return launch(distill_kernel<T, true, false>, grid, block, smem, s, true, a);
-    return launch(distill_kernel<T, false, true>, grid, block, smem, s, true, a);
+    int dev = 0;
+    if ((e = cudaGetDevice(&dev)) != cudaSuccess)
+        return e;
+    const int ranks = row_ranks(a.rows, a.V, es);
+    const int most = held[dev][ranks == 1 ? 0 : ranks == 2 ? 1 : ranks == 4 ? 2 : 3];
+    const int clusters = (int)(a.rows < most ? a.rows : most);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(clusters * ranks));
+    cfg.blockDim = dim3(kRingThreads);
+    cfg.dynamicSmemBytes = kRingSmem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim = {(unsigned)ranks, 1, 1};
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = plain_launches ? 1 : 2;
+    return cudaLaunchKernelEx(&cfg, kern, DistillArgs(a), ranks);
+}
+
+template <typename T>
+cudaError_t launch_distill(const DistillArgs &a, bool sum, bool grad, cudaStream_t s)
+{
+    return sum && grad ? launch_kind<T, true, true>(a, s)
+           : sum       ? launch_kind<T, true, false>(a, s)
+                       : launch_kind<T, false, true>(a, s);
 }
 
 // What the three entry points check alike.
@@ -343,8 +1069,11 @@ fdllm_status check_distill(DistillArgs &a, const void *logits, int dtype, int B,
     return FDLLM_OK;
 }
 
-fdllm_status run_distill(const DistillArgs &a, int dtype, bool sum, bool grad, void *stream)
+fdllm_status run_distill(DistillArgs &a, int dtype, bool sum, bool grad, void *stream)
 {
+    a.status = cache_status_word();
+    if (!a.status)
+        return FDLLM_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const cudaError_t e = dtype == FDLLM_BF16   ? launch_distill<__nv_bfloat16>(a, sum, grad, s)
                           : dtype == FDLLM_FP16 ? launch_distill<__half>(a, sum, grad, s)

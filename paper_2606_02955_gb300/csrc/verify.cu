@@ -12,8 +12,6 @@
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
-#include "cache_tc.cuh"
-#include "ptx.cuh"
 #include "vocab_rows.cuh"
 
 namespace fdllm {
@@ -71,92 +69,6 @@ __device__ __forceinline__ RowAt row_at(const VerifyArgs &a, int b, int j, bool 
     r.p = static_cast<const uint8_t *>(of_draft ? a.draft : a.target) + at * a.V * (int64_t)sizeof(T);
     return r;
 }
-
-// The largest of a vector's values; NaN where one is.
-template <typename T>
-__device__ __forceinline__ float vector_most(const uint4 &r)
-{
-    if constexpr (sizeof(T) == 4) {
-        return fmax_nan(fmax_nan(__uint_as_float(r.x), __uint_as_float(r.y)),
-                        fmax_nan(__uint_as_float(r.z), __uint_as_float(r.w)));
-    } else {
-        using P = std::conditional_t<__is_same(T, __nv_bfloat16), __nv_bfloat162, __half2>;
-        auto as = [](const uint32_t &w) { return *reinterpret_cast<const P *>(&w); };
-        const P m = __hmax2_nan(__hmax2_nan(as(r.x), as(r.y)), __hmax2_nan(as(r.z), as(r.w)));
-        return fmax_nan(to_float(m.x), to_float(m.y));
-    }
-}
-
-template <typename T>
-__device__ __forceinline__ constexpr uint32_t no_values()  // a word of -inf
-{
-    return sizeof(T) == 4 ? 0xFF800000u : __is_same(T, __nv_bfloat16) ? 0xFF80FF80u : 0xFC00FC00u;
-}
-
-// A thread's sum of 2^((x - m) c) over its vectors.  m is a reference, not the maximum: it moves only
-// where a value exceeds it by kSlack, so that few vectors pay for that, and terms stay below 2^kSlack.
-// Below kFar the terms are 2^(x c - r), r = m c rounded, in one operation: the product is exact
-// there, and what r's rounding leaves, at most 2^-3 and the same for all terms, is taken out at the
-// end.  Beyond kFar, x less m comes first.
-constexpr float kSlack = 12.0f, kFar = 2097152.0f;
-
-struct Summed {
-    ExpSum z;
-    float r = 0.0f;
-    bool far = true;  // (so that a first value of -FLT_MAX, which moves nothing, counts 1)
-
-    template <typename T, int N>
-    __device__ __forceinline__ void add(const uint4 (&x)[N], float c)
-    {
-        constexpr int E = 16 / sizeof(T);
-        float top = vector_most<T>(x[0]);
-#pragma unroll
-        for (int n = 1; n < N; ++n)
-            top = fmax_nan(top, vector_most<T>(x[n]));
-        // (a NaN fails the test as well, and moves nothing: its term makes the sum NaN)
-        if (!((top - z.m) * c <= kSlack)) {
-            if (top > z.m) {
-                settle(c);
-                z.raise(top, c);
-                r = z.m * c;
-                far = !(fabsf(r) < kFar);
-                if (!far)
-                    z.z *= ex2_mufu(fmaf(z.m, c, -r));
-            }
-        }
-        uint64_t s2 = 0;
-        auto terms = [&](auto far_tag) {
-            constexpr bool kIsFar = decltype(far_tag)::value;
-            const uint64_t c2 = f2(c, c), n2 = kIsFar ? f2(-z.m, -z.m) : f2(-r, -r);
-#pragma unroll
-            for (int n = 0; n < N; ++n) {
-                float y[E];
-                widen<T>(x[n], y);
-#pragma unroll
-                for (int e = 0; e < E; e += 2) {
-                    float t0, t1;
-                    const uint64_t y2 = f2(y[e], y[e + 1]);
-                    un2(kIsFar ? mul2(add2(y2, n2), c2) : fma2(y2, c2, n2), t0, t1);
-                    s2 = add2(s2, f2(ex2_mufu(t0), ex2_mufu(t1)));
-                }
-            }
-        };
-        if (__builtin_expect(far, 0))
-            terms(std::true_type{});
-        else
-            terms(std::false_type{});
-        float s0, s1;
-        un2(s2, s0, s1);
-        z.z += s0 + s1;
-    }
-    // The sum relative to m itself.
-    __device__ __forceinline__ void settle(float c)
-    {
-        if (!far && z.z != 0.0f)
-            z.z *= ex2_mufu(-fmaf(z.m, c, -r));
-        far = true;
-    }
-};
 
 // A thread's largest value and its first index; `nan` where a value is one.
 struct Largest {
@@ -557,16 +469,6 @@ __device__ __forceinline__ int decide(const VerifyArgs &a, const Nodes &s, int c
         }
     }
     return kNone;
-}
-
-// The cluster's barrier, in its two halves.  A CTA may leave behind its last arrival.
-__device__ __forceinline__ void cluster_arrive()
-{
-    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
-}
-__device__ __forceinline__ void cluster_wait()
-{
-    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
 }
 
 // Clusters of CTAs, one to a sequence: the walk, in each CTA; then the draw, each CTA a slice of the

@@ -49,6 +49,7 @@ def check(fd, kw, weights):
         assert torch.equal(torch.isnan(got), nan)
         err = (got - exact).abs()[~nan]
         assert bool((err <= tol[~nan]).all()), float((err / tol[~nan].clamp_min(1e-40)).max())
+    assert fd.fdllm_cache_status() == 0
     out = kw["mask"] == 0
     assert bool((loss[out] == 0).all()) and bool((grad[out] == 0).all()) and bool((step[1][out] == 0).all())
     return step
