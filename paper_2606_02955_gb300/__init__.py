@@ -1037,11 +1037,12 @@ class _DistillLoss(torch.autograd.Function):
         return loss
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
     def backward(ctx, grad_loss):
+        if torch.is_grad_enabled():  # (create_graph: the kernels' gradient would be a constant)
+            raise RuntimeError("fdllm_distill_loss has no second derivative")
         logits, mask, top_index, top_logits, teacher_lse, stats = ctx.saved_tensors
-        grad = fdllm_distill_grad(logits, mask, top_index, top_logits, stats, grad_loss.contiguous(),
-                                  teacher_lse=teacher_lse, temperature=ctx.temperature)
+        grad = _distill_grad(logits, mask, top_index, top_logits, stats, grad_loss.contiguous(),
+                             teacher_lse, ctx.temperature, None, None)
         return grad, None, None, None, None, None
 
 
@@ -1094,6 +1095,12 @@ def fdllm_distill_grad(logits: torch.Tensor, mask: torch.Tensor, top_index: torc
                        teacher_lse=None, temperature: float = 1.0, out_grad=None, stream=None):
     """The gradient of fdllm_distill_loss with respect to ``logits`` from its ``out_stats`` and the
     gradient fp32 [B, L] of each position's loss.  ``out_grad`` may be ``logits``."""
+    return _distill_grad(logits, mask, top_index, top_logits, stats, grad_loss, teacher_lse,
+                         temperature, out_grad, stream)
+
+
+def _distill_grad(logits, mask, top_index, top_logits, stats, grad_loss, teacher_lse, temperature,
+                  out_grad, stream):
     dev = logits.device
     args = _distill_args(logits, mask, top_index, top_logits, teacher_lse, dev)
     B, L = args[2:4]

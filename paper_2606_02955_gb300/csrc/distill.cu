@@ -309,8 +309,8 @@ constexpr int kMathWarps = 16, kMath = 32 * kMathWarps;
 constexpr int kTeachers = 128;
 constexpr int kRingThreads = kMath + kTeachers + 64;
 constexpr int kChunk = 32768, kChunkVecs = kChunk / 16, kPer = kChunkVecs / kMath;
-constexpr int kStages = 6;
 constexpr int kMostListed = 1 << 17;  // tokens of a CTA's share of a row: their bits take 16 KB
+constexpr int kMarks = kMostListed / 8 + 16;
 constexpr int kZeros = 2048;
 constexpr int kMaxRanks = 8;
 enum { kBarMath = 1, kBarTeach };
@@ -404,7 +404,7 @@ struct Taught {
 };
 
 struct RingShared {
-    uint64_t full[kStages], empty[kStages];
+    uint64_t full[6], empty[6];
     uint64_t ready[2];    // of a row, by parity: its list is taught
     uint64_t swept[2];    // the first pass is done, its marks are not needed
     uint64_t written[2];  // the second is done, the listed tokens may be written
@@ -418,10 +418,18 @@ struct RingShared {
     uint32_t ends;
 };
 
-constexpr int kListedOff = kStages * kChunk, kZerosOff = kListedOff + kMostListed / 8 + 16;
-constexpr int kDupOff = kZerosOff + kZeros, kSharedOff = kDupOff + kMaxTop * 8;
-constexpr int kRingSmem = kSharedOff + (int)sizeof(RingShared);
-static_assert(kRingSmem <= 227 * 1024 && kSharedOff % 16 == 0 && kZerosOff % 16 == 0, "shared memory");
+// Shared memory.  The sum alone holds no row back: it does with a stage less, and marks the row to
+// come while the row before is still under way (with one set of marks, 1234 rows of 50021 logits in
+// fp32 take 64 us).
+template <bool kSum, bool kGrad>
+struct RingLayout {
+    static constexpr int sets = kSum && !kGrad ? 2 : 1;
+    static constexpr int stages = sets == 2 ? 5 : 6;
+    static constexpr int listed = stages * kChunk, zeros = listed + sets * kMarks;
+    static constexpr int dup = zeros + kZeros, shared = dup + kMaxTop * 8;
+    static constexpr int bytes = shared + (int)sizeof(RingShared);
+    static_assert(bytes <= 227 * 1024 && shared % 16 == 0 && zeros % 16 == 0, "shared memory");
+};
 
 // Eight bytes to another CTA of the cluster, counted by a barrier there.
 __device__ __forceinline__ void send_sum(const ExpSum *slot, const uint64_t *bar, int to, const ExpSum &v)
@@ -470,9 +478,13 @@ __global__ void __launch_bounds__(kRingThreads, 1)
     distill_ring_kernel(const __grid_constant__ DistillArgs a, int ranks)
 {
     constexpr int E = 16 / sizeof(T);
+    using Layout = RingLayout<kSum, kGrad>;
+    constexpr int kStages = Layout::stages;
+    constexpr bool kTwo = Layout::sets == 2;
     extern __shared__ __align__(128) uint8_t smem[];
-    uint8_t *const listed = smem + kListedOff;  // a bit for each value of the share's vectors
-    RingShared &sm = *reinterpret_cast<RingShared *>(smem + kSharedOff);
+    // a bit for each value of the share's vectors; with two sets, by the row's parity
+    uint8_t *const marks = smem + Layout::listed;
+    RingShared &sm = *reinterpret_cast<RingShared *>(smem + Layout::shared);
     const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31;
     const int rank = blockIdx.x % ranks, cluster = blockIdx.x / ranks, clusters = gridDim.x / ranks;
     const float c = a.inv_t * kLog2e;
@@ -489,10 +501,8 @@ __global__ void __launch_bounds__(kRingThreads, 1)
         }
         fence_mbar_init();
     }
-    for (int i = tid; i < (kMostListed / 8 + 16) / 4; i += kRingThreads)
-        reinterpret_cast<uint32_t *>(listed)[i] = 0;
-    for (int i = tid; i < kZeros / 4; i += kRingThreads)
-        reinterpret_cast<uint32_t *>(smem + kZerosOff)[i] = 0;
+    for (int i = tid; i < (Layout::sets * kMarks + kZeros) / 4; i += kRingThreads)
+        reinterpret_cast<uint32_t *>(marks)[i] = 0;
     fence_async_smem();
     __syncthreads();
     if (ranks > 1) {
@@ -527,6 +537,7 @@ __global__ void __launch_bounds__(kRingThreads, 1)
             ExpSum rest = of.rest;
             if constexpr (kSum) {
                 // ---- the tokens that are not listed
+                const uint8_t *const listed = marks + (kTwo ? par * kMarks : 0);
                 Summed sum;
                 for (int j = 0; j < chunks; ++j) {
                     const uint32_t k = kb + j, st = k % kStages;
@@ -567,7 +578,7 @@ __global__ void __launch_bounds__(kRingThreads, 1)
                 if (lane == 0)
                     sm.part[par][warp] = rest;
                 named_sync(kBarMath, kMath);
-                if (tid == 0)
+                if (kGrad && tid == 0)
                     mbar_arrive(&sm.swept[par]);
                 rest = sm.part[par][lane & 15];
 #pragma unroll
@@ -605,6 +616,8 @@ __global__ void __launch_bounds__(kRingThreads, 1)
                     if (a.stats_out)
                         a.stats_out[of.row] = make_float4(M, Z, rest.m, rest.z);
                 }
+                if (!kGrad && tid == 0)  // (what was taught of the row goes too)
+                    mbar_arrive(&sm.swept[par]);
             } else if (rest.z == 0.0f) {
                 R = 0.0f;
             }
@@ -670,15 +683,17 @@ __global__ void __launch_bounds__(kRingThreads, 1)
         // ------------------------------------------------------------ the teacher
         constexpr int kMine = kMaxTop / kTeachers;
         const int t = tid - kMath;
-        int *const idx = reinterpret_cast<int *>(smem + kDupOff);
+        int *const idx = reinterpret_cast<int *>(smem + Layout::dup);
         float *const mass = reinterpret_cast<float *>(idx + kMaxTop);
         RowWalk walk(a.mask, a.rows, true);
         int old[kMine];  // of the row before: its listed tokens, and what their gradients need
         float old_p[kMine], old_x[kMine];
         int64_t old_row = -1;
+        [[maybe_unused]] int older[kMine];  // and of the one before it
+        [[maybe_unused]] int64_t older_row = -1;
 #pragma unroll
         for (int j = 0; j < kMine; ++j)
-            old[j] = -1, old_p[j] = old_x[j] = 0.0f;
+            old[j] = older[j] = -1, old_p[j] = old_x[j] = 0.0f;
         for (uint32_t i = 0;; ++i) {
             const uint32_t par = i & 1;
             const int64_t row = walk.find(cluster + (int64_t)i * clusters);
@@ -727,9 +742,12 @@ __global__ void __launch_bounds__(kRingThreads, 1)
                     P = P == P ? 1.0f : P;
                 }
             }
-            // ---- the marks: the row before's go, this one's come
-            if (kSum && i > 0)
+            // ---- the marks: those of the row that had this set go, this one's come
+            if (kTwo && i > 1)
+                wait(&sm.swept[par], ((i - 2) >> 1) & 1);
+            if (kSum && kGrad && i > 0)
                 wait(&sm.swept[par ^ 1], ((i - 1) >> 1) & 1);
+            uint8_t *const listed = marks + (kTwo ? par * kMarks : 0);
             if (named_sync_or(kBarTeach, kTeachers, dead))
                 break;
             auto mark = [&](int64_t of_row, int at, bool set) -> bool {  // whether it was set before
@@ -753,11 +771,11 @@ __global__ void __launch_bounds__(kRingThreads, 1)
                 atomicAnd(word, ~(1u << bit));
                 return false;
             };
-            if (old_row >= 0)
+            if ((kTwo ? older_row : old_row) >= 0)
 #pragma unroll
                 for (int j = 0; j < kMine; ++j)
-                    if (old[j] >= 0)
-                        mark(old_row, old[j], false);
+                    if ((kTwo ? older[j] : old[j]) >= 0)
+                        mark(kTwo ? older_row : old_row, kTwo ? older[j] : old[j], false);
             if (t == 0) {
                 sm.ends = 0;
                 sm.twice = 0;
@@ -877,9 +895,11 @@ __global__ void __launch_bounds__(kRingThreads, 1)
             }
             if (row < 0)
                 break;
+            older_row = old_row;
             old_row = row;
 #pragma unroll
             for (int j = 0; j < kMine; ++j) {
+                older[j] = old[j];
                 old[j] = v[j];
                 old_p[j] = m[j];
                 old_x[j] = x[j];
@@ -941,7 +961,7 @@ __global__ void __launch_bounds__(kRingThreads, 1)
                 uint8_t *p = reinterpret_cast<uint8_t *>(grad + sh.r.head) + (int64_t)sh.v0 * 16;
                 for (int64_t o = (int64_t)lane * kZeros; o < bytes; o += 32 * kZeros)
                     asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(p + o),
-                                 "r"(smem_addr(smem + kZerosOff)), "r"((uint32_t)min((int64_t)kZeros, bytes - o))
+                                 "r"(smem_addr(smem + Layout::zeros)), "r"((uint32_t)min((int64_t)kZeros, bytes - o))
                                  : "memory");
                 asm volatile("cp.async.bulk.commit_group;" ::: "memory");
             }
@@ -970,14 +990,14 @@ int row_ranks(int64_t rows, int V, int es)
 
 // Clusters of `ranks` CTAs that the GPU holds at once.
 template <typename K>
-int resident(K kern, int ranks)
+int resident(K kern, int smem, int ranks)
 {
     if (ranks == 1)
         return sm_count();
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(sm_count() / ranks * ranks));
     cfg.blockDim = dim3(kRingThreads);
-    cfg.dynamicSmemBytes = kRingSmem;
+    cfg.dynamicSmemBytes = smem;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim = {(unsigned)ranks, 1, 1};
@@ -1002,14 +1022,15 @@ cudaError_t launch_kind(const DistillArgs &a, cudaStream_t s)
                       (size_t)((a.V + 31) / 32) * 4, s, true, a);
     }
     auto *kern = distill_ring_kernel<T, kSum, kGrad>;
+    constexpr int kSmem = RingLayout<kSum, kGrad>::bytes;
     static PerDevice ready;
     static std::atomic<int> held[kMaxCacheDevices][4];
     cudaError_t e = ready.once([&] {
-        const cudaError_t r = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingSmem);
+        const cudaError_t r = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
         int dev = 0;
         if (r == cudaSuccess && cudaGetDevice(&dev) == cudaSuccess)
             for (int i = 0; i < 4; ++i)
-                held[dev][i] = resident(kern, 1 << i);
+                held[dev][i] = resident(kern, kSmem, 1 << i);
         return r;
     });
     if (e != cudaSuccess)
@@ -1023,7 +1044,7 @@ cudaError_t launch_kind(const DistillArgs &a, cudaStream_t s)
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(clusters * ranks));
     cfg.blockDim = dim3(kRingThreads);
-    cfg.dynamicSmemBytes = kRingSmem;
+    cfg.dynamicSmemBytes = kSmem;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;

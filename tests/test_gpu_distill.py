@@ -215,6 +215,9 @@ def test_autograd_inside_a_graph_of_operations(fd):
     each = (torch.ones(2, 3, device="cuda") / count)
     dy = fd.fdllm_distill_step(y, kw["mask"], kw["top_index"], kw["top_logits"], each, kw["teacher_lse"])[1]
     assert torch.equal(w.grad, (x.flatten(0, 1).t() @ dy.flatten(0, 1)))
+    z = y.clone().requires_grad_()
+    with pytest.raises(RuntimeError):
+        torch.autograd.grad(fd.fdllm_distill_loss(**{**kw, "logits": z}).sum(), z, create_graph=True)
     with torch.no_grad():
         assert fd.fdllm_distill_loss(**{**kw, "logits": x @ w}).requires_grad is False
     with pytest.raises(ValueError):
