@@ -414,6 +414,7 @@ struct RingShared {
     ExpSum part[2][kMathWarps];
     ExpSum of_rank[2][kMaxRanks];
     float reduce[3][4];
+    uint32_t groups[2][kMostListed / 4 / 1024];  // a bit for each 32 vectors that hold a marked value
     int twice;
     uint32_t ends;
 };
@@ -440,6 +441,23 @@ __device__ __forceinline__ void send_sum(const ExpSum *slot, const uint64_t *bar
     asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.b32 [%0], {%1, %2}, [%3];" ::"r"(at),
                  "r"(__float_as_uint(v.m)), "r"(__float_as_uint(v.z)), "r"(b)
                  : "memory");
+}
+
+// This thread's vectors of a chunk of n; `pad` in the words of those that are not there.
+template <typename T>
+__device__ __forceinline__ void load_chunk(uint4 (&x)[kPer], const uint4 *buf, int n, uint32_t pad)
+{
+    if (n == kChunkVecs) {
+#pragma unroll
+        for (int q = 0; q < kPer; ++q)
+            x[q] = buf[threadIdx.x + q * kMath];
+    } else {
+#pragma unroll
+        for (int q = 0; q < kPer; ++q) {
+            const int v = threadIdx.x + q * kMath;
+            x[q] = v < n ? buf[v] : make_uint4(pad, pad, pad, pad);
+        }
+    }
 }
 
 // -inf in the place of the values whose bits are set.
@@ -538,6 +556,7 @@ __global__ void __launch_bounds__(kRingThreads, 1)
             if constexpr (kSum) {
                 // ---- the tokens that are not listed
                 const uint8_t *const listed = marks + (kTwo ? par * kMarks : 0);
+                const uint32_t *const groups = sm.groups[kTwo ? par : 0];
                 Summed sum;
                 for (int j = 0; j < chunks; ++j) {
                     const uint32_t k = kb + j, st = k % kStages;
@@ -545,29 +564,22 @@ __global__ void __launch_bounds__(kRingThreads, 1)
                     const uint4 *buf = reinterpret_cast<const uint4 *>(smem + st * kChunk);
                     const int n = sh.in_chunk(j);
                     uint4 x[kPer];
-                    uint32_t bits[kPer], any = 0;
-#pragma unroll
-                    for (int q = 0; q < kPer; ++q) {
-                        const int v = tid + q * kMath, at = j * kChunkVecs + v;
-                        constexpr uint32_t kPad = no_values<T>();
-                        x[q] = make_uint4(kPad, kPad, kPad, kPad);
-                        bits[q] = 0;
-                        if (v < n) {
-                            x[q] = buf[v];
-                            bits[q] = E == 8 ? listed[at] : (listed[at >> 1] >> (4 * (at & 1))) & 15u;
-                        }
-                        any |= bits[q];
-                    }
+                    load_chunk<T>(x, buf, n, no_values<T>());
+                    // (most groups of 32 vectors hold no listed token)
+                    const uint32_t some[2] = {groups[2 * j] >> warp & 0x10001u,
+                                              groups[2 * j + 1] >> warp & 0x10001u};
                     if (!kGrad || j < again) {
                         __syncwarp();
                         if (lane == 0)
                             mbar_arrive(&sm.empty[st]);
                     }
-                    if (any)
+                    if (some[0] | some[1])
 #pragma unroll
                         for (int q = 0; q < kPer; ++q)
-                            if (bits[q])
-                                leave_out<T>(x[q], bits[q]);
+                            if ((some[q >> 1] >> (16 * (q & 1))) & 1u) {
+                                const int at = j * kChunkVecs + tid + q * kMath;
+                                leave_out<T>(x[q], E == 8 ? listed[at] : listed[at >> 1] >> (4 * (at & 1)));
+                            }
                     sum.add<T, kPer>(x, c);
                 }
                 sum.settle(c);
@@ -647,20 +659,13 @@ __global__ void __launch_bounds__(kRingThreads, 1)
                     const uint4 *buf = reinterpret_cast<const uint4 *>(smem + st * kChunk);
                     const int n = sh.in_chunk(j);
                     uint4 x[kPer];
-#pragma unroll
-                    for (int p = 0; p < kPer; ++p) {
-                        const int v = tid + p * kMath;
-                        if (v < n)
-                            x[p] = buf[v];
-                    }
+                    load_chunk<T>(x, buf, n, 0u);
                     __syncwarp();
                     if (lane == 0)
                         mbar_arrive(&sm.empty[st]);
 #pragma unroll
                     for (int p = 0; p < kPer; ++p) {
                         const int v = tid + p * kMath;
-                        if (v >= n)
-                            continue;
                         float y[E];
                         widen<T>(x[p], y);
 #pragma unroll
@@ -670,7 +675,8 @@ __global__ void __launch_bounds__(kRingThreads, 1)
                             un2(far ? mul2(add2(y2, n2), c2) : fma2(y2, c2, n2), t0, t1);
                             un2(mul2(f2(ex2_mufu(t0), ex2_mufu(t1)), f2f), y[e], y[e + 1]);
                         }
-                        __stcs(out + j * kChunkVecs + v, narrow<T>(y));
+                        if (v < n)
+                            __stcs(out + j * kChunkVecs + v, narrow<T>(y));
                     }
                 }
                 __syncwarp();
@@ -748,6 +754,7 @@ __global__ void __launch_bounds__(kRingThreads, 1)
             if (kSum && kGrad && i > 0)
                 wait(&sm.swept[par ^ 1], ((i - 1) >> 1) & 1);
             uint8_t *const listed = marks + (kTwo ? par * kMarks : 0);
+            uint32_t *const groups = sm.groups[kTwo ? par : 0];
             if (named_sync_or(kBarTeach, kTeachers, dead))
                 break;
             auto mark = [&](int64_t of_row, int at, bool set) -> bool {  // whether it was set before
@@ -765,6 +772,8 @@ __global__ void __launch_bounds__(kRingThreads, 1)
                         return false;
                     word = reinterpret_cast<uint32_t *>(listed) + (b >> 5);
                     bit = b & 31;
+                    if (set)
+                        atomicOr(&groups[b / E >> 10], 1u << (b / E >> 5 & 31));
                 }
                 if (set)
                     return (atomicOr(word, 1u << bit) >> bit) & 1u;
@@ -780,6 +789,8 @@ __global__ void __launch_bounds__(kRingThreads, 1)
                 sm.ends = 0;
                 sm.twice = 0;
             }
+            if (t < kMostListed / 4 / 1024)
+                groups[t] = 0;
             named_sync(kBarTeach, kTeachers);
             if (row >= 0) {
                 bool again = false;
