@@ -578,10 +578,11 @@ size_t fdllm_verify_draft_workspace_bytes(int B, int M, int V, int dtype);
  *   can be drawn from that either, the next token is the argmax.
  * Probabilities and weights are fp32 (relative error within 1e-5), the tests of tokens 64-bit
  * products of them.
- *   target     [B, M, V] device, dtype as given, row j the logits after node j; base 16-byte
- *              aligned (FDLLM_ERR_ALIGN), V any from 1 to 2^20.
- *   draft      [B, M - 1, V] in the same dtype and alignment, row j the logits that node j + 1 was
- *              drawn from; or NULL.  Only with parents NULL and temperature > 0 (FDLLM_ERR_ARG).
+ *   target     [B, M, V] device, dtype as given, row j the logits after node j; V any from 1 to 2^20,
+ *              the values of a row contiguous, rows anywhere (FDLLM_ERR_ALIGN: a base that is not a
+ *              multiple of the value's size); target_strides {batch, row} in elements, host.
+ *   draft      [B, M - 1, V] in the same dtype, row j the logits that node j + 1 was drawn from, strides
+ *              as target's; or NULL.  Only with parents NULL and temperature > 0 (FDLLM_ERR_ARG).
  *   tokens     [B, M] int32 device: the nodes' tokens (node 0's is not read).  A token out of the
  *              vocabulary is never taken.
  *   parents    [B, M] int32 device, or NULL: a chain.  A node whose parent is not in 0 .. j - 1 is
@@ -590,9 +591,9 @@ size_t fdllm_verify_draft_workspace_bytes(int B, int M, int V, int dtype);
  *              read (a value out of 1 .. M counts as the nearer end).
  *   M          1 (no drafts: the next token is drawn from row 0) to FDLLM_MAX_L.
  *   temperature, draft_temperature   1e-6 to 1e6, or temperature 0.
- *   uniform    [B, M] fp32 device in [0, 1); entry 0 is not read.   noise  [B, V] fp32 device, > 0,
- *              base 16-byte aligned; a token whose noise is NaN, negative or infinite is not drawn.
- *              Both may be NULL where temperature is 0.
+ *   uniform    [B, M] fp32 device in [0, 1); entry 0 is not read.   noise  [B, V] fp32 device, > 0; a
+ *              token whose noise is NaN, negative or infinite is not drawn.  Both may be NULL where
+ *              temperature is 0.
  *   out_tokens [B, M] int32: the taken tokens, then the next token; -1 behind.
  *   out_nodes  [B, M] int32: the root (0), then the taken nodes: the rows whose keys and values
  *              enter the cache; -1 behind.
@@ -600,8 +601,9 @@ size_t fdllm_verify_draft_workspace_bytes(int B, int M, int V, int dtype);
  *              others) where a row on the way holds a NaN or its maximum is infinite.
  *   workspace  device, 256-byte aligned, fdllm_verify_draft_workspace_bytes() bytes of any content;
  *              calls that may overlap on the GPU need their own. */
-fdllm_status fdllm_verify_draft(const void *target, const void *draft, int dtype, int B, int M,
-                                int V, const int32_t *tokens, const int32_t *parents,
+fdllm_status fdllm_verify_draft(const void *target, const int64_t *target_strides,
+                                const void *draft, const int64_t *draft_strides, int dtype, int B,
+                                int M, int V, const int32_t *tokens, const int32_t *parents,
                                 const int32_t *lens, double temperature, double draft_temperature,
                                 const float *uniform, const float *noise, int32_t *out_tokens,
                                 int32_t *out_nodes, int32_t *out_n, void *workspace,

@@ -117,7 +117,7 @@ def _load():
     lib.fdllm_cache_tree_attention.argtypes = [p, p, i, i, i, i, p, p, i, p, p, p, p, p, i, p, p, d,
                                                p, p, p, sz, p]
     lib.fdllm_cache_tree_attention.restype = i
-    lib.fdllm_verify_draft.argtypes = [p, p, i, i, i, i, p, p, p, d, d, p, p, p, p, p, p, sz, p]
+    lib.fdllm_verify_draft.argtypes = [p, p, p, p, i, i, i, i, p, p, p, d, d, p, p, p, p, p, p, sz, p]
     lib.fdllm_verify_draft.restype = i
     lib.fdllm_verify_draft_workspace_bytes.argtypes = [i, i, i, i]
     lib.fdllm_verify_draft_workspace_bytes.restype = sz
@@ -976,16 +976,23 @@ def fdllm_verify_draft(target: torch.Tensor, tokens: torch.Tensor, parents=None,
     """Take drafted tokens by the target's probabilities and given random numbers.
 
     ``target`` [B, M, V] bf16/fp16/fp32, row j the target's logits after node j (node 0 the last
-    committed token); ``tokens`` int32 [B, M] the nodes' tokens; ``parents`` int32 [B, M] a tree
+    committed token; rows may lie anywhere, their values contiguous); ``tokens`` int32 [B, M] the nodes' tokens; ``parents`` int32 [B, M] a tree
     (None: a chain); ``lens`` int32 [B] the counts of nodes; ``draft`` [B, M - 1, V] the logits a
     chain was drawn from at ``draft_temperature`` (None: ``temperature``), or None where the tokens
     were chosen; ``uniform`` fp32 [B, M] in [0, 1) and ``noise`` fp32 [B, V] exponential variables
     (None at temperature 0, which is greedy).  Returns (tokens int32 [B, M]: the taken ones, then
     the next; nodes int32 [B, M]: the root, then the taken ones; -1 behind; n int32 [B])."""
     dev, dt = target.device, target.dtype
-    code, shape = _logits(target, "target", 3)
+    if target.dim() != 3 or dt not in _CODES:
+        raise TypeError("target must be [B, M, V] bfloat16, float16 or float32, got %s %s"
+                        % (dt, tuple(target.shape)))
+    code, shape = _CODES[dt], target.shape
     B, M, V = shape
     nodes = (B, M)
+    tp, ts = _rows(target, "target", dt, shape, dev, _Two)
+    dp = ds = None
+    if draft is not None:
+        dp, ds = _rows(draft, "draft", dt, (B, M - 1, V), dev, _Two)
     if out_tokens is None:
         out_tokens = _made(nodes, _I32, dev, stream)
     if out_nodes is None:
@@ -997,8 +1004,7 @@ def fdllm_verify_draft(target: torch.Tensor, tokens: torch.Tensor, parents=None,
         need = lib.fdllm_verify_draft_workspace_bytes(B, M, V, code)
         workspace = _made((need if need > 256 else 256,), _U8, dev, stream)
     st = lib.fdllm_verify_draft(
-        _ptr(target, "target", dt, shape, dev), _ptr(draft, "draft", dt, (B, M - 1, V), dev), code,
-        B, M, V, _ptr(tokens, "tokens", _I32, nodes, dev), _ptr(parents, "parents", _I32, nodes, dev),
+        tp, ts, dp, ds, code, B, M, V, _ptr(tokens, "tokens", _I32, nodes, dev), _ptr(parents, "parents", _I32, nodes, dev),
         _ptr(lens, "lens", _I32, (B,), dev), temperature,
         temperature if draft_temperature is None else draft_temperature,
         _ptr(uniform, "uniform", _F32, nodes, dev), _ptr(noise, "noise", _F32, (B, V), dev),

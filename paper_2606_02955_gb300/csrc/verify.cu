@@ -32,6 +32,7 @@ constexpr int kMaxRanks = 8;     // CTAs of a cluster of them
 struct VerifyArgs {
     const void *target;       // [B, M, V]
     const void *draft;        // [B, M - 1, V] or null
+    int64_t t_batch, t_row, d_batch, d_row;  // strides, in values
     int B, M, V;
     const int32_t *tokens;    // [B, M]
     const int32_t *parents;   // [B, M] or null: a chain
@@ -64,9 +65,9 @@ template <typename T>
 __device__ __forceinline__ RowAt row_at(const VerifyArgs &a, int b, int j, bool of_draft)
 {
     RowAt r;
-    const int64_t at = of_draft ? (int64_t)b * (a.M - 1) + j : (int64_t)b * a.M + j;
-    r.part = (of_draft ? (int64_t)a.B * a.M + at : at) * a.per;
-    r.p = static_cast<const uint8_t *>(of_draft ? a.draft : a.target) + at * a.V * (int64_t)sizeof(T);
+    r.part = (of_draft ? (int64_t)a.B * a.M + (int64_t)b * (a.M - 1) + j : (int64_t)b * a.M + j) * a.per;
+    const int64_t at = of_draft ? b * a.d_batch + j * a.d_row : b * a.t_batch + j * a.t_row;
+    r.p = static_cast<const uint8_t *>(of_draft ? a.draft : a.target) + at * (int64_t)sizeof(T);
     return r;
 }
 
@@ -594,7 +595,8 @@ __global__ void __launch_bounds__(kDraw, 2) verify_draw_kernel(const __grid_cons
                         top = best[w] > top ? best[w] : top;
                 return top;
             };
-            if (((int64_t)a.V * sizeof(T)) % 16 == 0) {
+            if (((reinterpret_cast<uintptr_t>(row) | reinterpret_cast<uintptr_t>(less) |
+                  reinterpret_cast<uintptr_t>(noise)) & 15u) == 0 && a.V % E == 0) {
                 constexpr int kTwo = 2;  // vectors of a thread in flight
                 for (int w = v0 + tid * E; w < v1; w += kTwo * kDraw * E) {
                     uint4 xr[kTwo], yr[kTwo];
@@ -800,8 +802,9 @@ size_t fdllm_verify_draft_workspace_bytes(int B, int M, int V, int dtype)
     return verify_sizes(B, M, V) && rows_dtype(dtype) ? verify_bytes(B, M, V, dtype) : 0;
 }
 
-fdllm_status fdllm_verify_draft(const void *target, const void *draft, int dtype, int B, int M,
-                                int V, const int32_t *tokens, const int32_t *parents,
+fdllm_status fdllm_verify_draft(const void *target, const int64_t *target_strides,
+                                const void *draft, const int64_t *draft_strides, int dtype, int B,
+                                int M, int V, const int32_t *tokens, const int32_t *parents,
                                 const int32_t *lens, double temperature, double draft_temperature,
                                 const float *uniform, const float *noise, int32_t *out_tokens,
                                 int32_t *out_nodes, int32_t *out_n, void *workspace,
@@ -809,12 +812,13 @@ fdllm_status fdllm_verify_draft(const void *target, const void *draft, int dtype
 {
     const bool greedy = temperature == 0.0;
     auto sane = [](double t) { return t >= 1e-6 && t <= 1e6; };
-    if (!verify_sizes(B, M, V) || !rows_dtype(dtype) || !target || !tokens || !out_tokens ||
+    if (!verify_sizes(B, M, V) || !rows_dtype(dtype) || !target || !target_strides ||
+        (draft && !draft_strides) || !tokens || !out_tokens ||
         !out_nodes || !out_n || (!greedy && (!sane(temperature) || !uniform || !noise)) ||
         (draft && (greedy || parents || !sane(draft_temperature))))
         return FDLLM_ERR_ARG;
-    if (((reinterpret_cast<uintptr_t>(target) | reinterpret_cast<uintptr_t>(draft) |
-          reinterpret_cast<uintptr_t>(noise)) & 15u) != 0)
+    if (((reinterpret_cast<uintptr_t>(target) | reinterpret_cast<uintptr_t>(draft)) &
+         (uintptr_t)(rows_esize(dtype) - 1)) != 0)
         return FDLLM_ERR_ALIGN;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 ||
         workspace_bytes < verify_bytes(B, M, V, dtype))
@@ -822,6 +826,12 @@ fdllm_status fdllm_verify_draft(const void *target, const void *draft, int dtype
     VerifyArgs a = {};
     a.target = target;
     a.draft = M > 1 ? draft : nullptr;
+    a.t_batch = target_strides[0];
+    a.t_row = target_strides[1];
+    if (a.draft) {
+        a.d_batch = draft_strides[0];
+        a.d_row = draft_strides[1];
+    }
     a.B = B;
     a.M = M;
     a.V = V;

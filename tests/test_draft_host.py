@@ -18,7 +18,7 @@ def lib(cuda_lib_path):
     lib = ctypes.CDLL(cuda_lib_path)
     lib.fdllm_tree_mask.argtypes = [P, P, I, I, P, P, P]
     lib.fdllm_cache_tree_attention.argtypes = [P, P, I, I, I, I, P, P, I, P, P, P, P, P, I, P, P, D, P, P, P, SZ, P]
-    lib.fdllm_verify_draft.argtypes = [P, P, I, I, I, I, P, P, P, D, D, P, P, P, P, P, P, SZ, P]
+    lib.fdllm_verify_draft.argtypes = [P, P, P, P, I, I, I, I, P, P, P, D, D, P, P, P, P, P, P, SZ, P]
     lib.fdllm_verify_draft_workspace_bytes.argtypes = [I, I, I, I]
     lib.fdllm_verify_draft_workspace_bytes.restype = SZ
     lib.fdllm_distill_loss.argtypes = [P, I, I, I, I, P, P, P, I, I, P, D, P, P, P]
@@ -36,8 +36,9 @@ def test_tree_mask_refuses(lib, change):
 
 def verify(lib, **change):
     a = {**dict(target=A16, draft=A16, dtype=0, B=2, M=3, V=100, tokens=A16, parents=None, t=1.0, td=1.0, u=A16,
-                e=A16, out=A16, nodes=A16, n=A16, ws=A16, size=1 << 20), **change}
-    return lib.fdllm_verify_draft(a["target"], a["draft"], a["dtype"], a["B"], a["M"], a["V"], a["tokens"],
+                e=A16, out=A16, nodes=A16, n=A16, ws=A16, size=1 << 20, ts=strides(300, 100),
+                ds=strides(200, 100)), **change}
+    return lib.fdllm_verify_draft(a["target"], a["ts"], a["draft"], a["ds"], a["dtype"], a["B"], a["M"], a["V"], a["tokens"],
                                   a["parents"], None, a["t"], a["td"], a["u"], a["e"], a["out"], a["nodes"],
                                   a["n"], a["ws"], a["size"], None)
 
@@ -48,8 +49,8 @@ def verify(lib, **change):
     (dict(tokens=None), ERR_ARG), (dict(parents=A16), ERR_ARG), (dict(t=0.0), ERR_ARG), (dict(t=-1.0), ERR_ARG),
     (dict(t=math.nan), ERR_ARG), (dict(t=math.inf), ERR_ARG), (dict(t=1e-7), ERR_ARG), (dict(td=0.0), ERR_ARG),
     (dict(td=math.nan), ERR_ARG), (dict(u=None), ERR_ARG), (dict(e=None), ERR_ARG), (dict(out=None), ERR_ARG),
-    (dict(nodes=None), ERR_ARG), (dict(n=None), ERR_ARG), (dict(target=A2), ERR_ALIGN), (dict(draft=A2), ERR_ALIGN),
-    (dict(e=A16 + 4), ERR_ALIGN), (dict(ws=None), ERR_WORKSPACE), (dict(ws=A16 + 16), ERR_WORKSPACE),
+    (dict(nodes=None), ERR_ARG), (dict(n=None), ERR_ARG), (dict(target=A16 + 1), ERR_ALIGN), (dict(draft=A16 + 1), ERR_ALIGN),
+    (dict(target=A2, dtype=1), ERR_ALIGN), (dict(ts=None), ERR_ARG), (dict(ds=None), ERR_ARG), (dict(ws=None), ERR_WORKSPACE), (dict(ws=A16 + 16), ERR_WORKSPACE),
     (dict(size=8), ERR_WORKSPACE)])
 def test_verify_refuses(lib, change, want):
     assert verify(lib, **change) == want
@@ -110,7 +111,7 @@ def test_tree_attention_refuses(lib, change, want):
 MORE = """
 lib.fdllm_tree_mask.argtypes = [p, p, i, i, p, p, p]
 lib.fdllm_cache_tree_attention.argtypes = [p, p, i, i, i, i, p, p, i, p, p, p, p, p, i, p, p, d, p, p, p, sz, p]
-lib.fdllm_verify_draft.argtypes = [p, p, i, i, i, i, p, p, p, d, d, p, p, p, p, p, p, sz, p]
+lib.fdllm_verify_draft.argtypes = [p, p, p, p, i, i, i, i, p, p, p, d, d, p, p, p, p, p, p, sz, p]
 lib.fdllm_distill_loss.argtypes = [p, i, i, i, i, p, p, p, i, i, p, d, p, p, p]
 lib.fdllm_distill_step.argtypes = [p, i, i, i, i, p, p, p, i, i, p, d, p, p, p, p]
 def mask(M):
@@ -121,7 +122,7 @@ def tree(M, D):
     return lib.fdllm_cache_tree_attention(A16, s, 0, 1, M, h, ctypes.byref(c), A16, 4, A16, A16, s, A16, s, M, None,
                                           A16, 1.0, A16, None, A16, 1 << 40, None)
 def verify(M, V, dtype, t=1.0):
-    return lib.fdllm_verify_draft(A16, None, dtype, 2, M, V, A16, None, None, t, 1.0, A16, A16, A16, A16, A16, A16,
+    return lib.fdllm_verify_draft(A16, strides(M * V, V), None, None, dtype, 2, M, V, A16, None, None, t, 1.0, A16, A16, A16, A16, A16, A16,
                                   1 << 40, None)
 def loss(V, dtype):
     return lib.fdllm_distill_loss(A16, dtype, 2, 3, V, A16, A16, A16, 1, 4, None, 1.0, A16, A16, None)

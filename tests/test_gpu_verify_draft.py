@@ -278,6 +278,26 @@ def test_deterministic_on_another_stream_in_a_graph_and_side_by_side(fd):
         assert all(torch.equal(a, b) for a, b in zip(outs, want))
 
 
+@pytest.mark.parametrize("dtype", [BF, HF, FP])
+@pytest.mark.parametrize("V", [512, 515, 50021])
+def test_rows_of_larger_tensors(fd, dtype, V):
+    """Rows that lie apart, at any alignment, in any order of batch and rows, or repeat."""
+    target, tokens, kw = inputs(3, 4, V, dtype, "draft", seed=18 + V)
+    want = check(fd, target, tokens, **kw)
+    g = torch.Generator().manual_seed(1)
+    wide = torch.randn(3, 9, V + 5, generator=g).to(dtype).cuda()
+    wide[:, 2:6, 3:V + 3] = target.cuda()
+    turned = torch.randn(5, 3, V + 1, generator=g).to(dtype).cuda().transpose(0, 1)
+    turned[:, 1:4, 1:] = kw["draft"].cuda()
+    more = {k: cuda(v) for k, v in kw.items() if k != "draft"}
+    got = fd.fdllm_verify_draft(wide[:, 2:6, 3:V + 3], tokens.cuda(), draft=turned[:, 1:4, 1:], **more)
+    assert all(torch.equal(a.cpu(), b) for a, b in zip(got, want))
+    one = target[:1, :1].cuda().expand(3, 4, V)
+    want = run(fd, one.contiguous().cpu(), tokens, **{k: v for k, v in kw.items() if k != "draft"})
+    got = fd.fdllm_verify_draft(one, tokens.cuda(), **more)
+    assert all(torch.equal(a.cpu(), b) for a, b in zip(got, want))
+
+
 def test_refusals(fd):
     target, tokens, kw = inputs(2, 3, 64, BF, "draft", seed=17)
     target, tokens, kw = cuda(target), cuda(tokens), {k: cuda(v) for k, v in kw.items()}
@@ -290,7 +310,8 @@ def test_refusals(fd):
         with pytest.raises(fd.FdllmError):
             call(**bad)
     for bad in (dict(draft=kw["draft"].float()), dict(draft=target), dict(tokens=tokens.long()),
-                dict(tokens=tokens[:, :2]), dict(uniform=kw["uniform"].cpu()), dict(target=target[:, :, ::2]),
+                dict(tokens=tokens[:, :2]), dict(uniform=kw["uniform"].cpu()),
+                dict(target=torch.cat((target, target), -1)[:, :, ::2]),
                 dict(target=target.double()), dict(target=target[0]), dict(lens=ints([1]))):
         with pytest.raises((TypeError, ValueError)):
             call(**bad)
