@@ -25,7 +25,8 @@ constexpr int kMath = 32 * kMathWarps;
 constexpr int kChunk = 65536;  // bytes of a stage
 constexpr int kStages = 3;
 constexpr int kChunkVecs = kChunk / 16;
-constexpr int kSmallRow = 8192;  // rows up to this many bytes: a warp each
+constexpr int kSmallRow = 32768;  // rows up to this many bytes: a few warps each, without the ring
+constexpr int kSmallVecs = 8;     // vectors of a lane in such a row, about
 constexpr int kDraw = 512;       // threads of a CTA of the walk and the draw
 constexpr int kMaxRanks = 8;     // CTAs of a cluster of them
 
@@ -163,7 +164,7 @@ struct Share {
     }
 };
 
-// ---- Rows of up to kSmallRow bytes: a warp each.
+// ---- Rows of up to kSmallRow bytes: a.per warps each, every one with a part of its own.
 template <typename T, bool kGreedy>
 __global__ void __launch_bounds__(256) verify_small_kernel(const __grid_constant__ VerifyArgs a)
 {
@@ -173,7 +174,10 @@ __global__ void __launch_bounds__(256) verify_small_kernel(const __grid_constant
         pdl_launch_dependents();
     const int lane = threadIdx.x & 31;
     const int64_t targets = (int64_t)a.B * a.M, rows = targets + (a.draft ? (int64_t)a.B * (a.M - 1) : 0);
-    for (int64_t row = blockIdx.x * 8ll + (threadIdx.x >> 5); row < rows; row += gridDim.x * 8ll) {
+    const int64_t step = (int64_t)gridDim.x * 8;
+    for (int64_t w = blockIdx.x * 8ll + (threadIdx.x >> 5); w < rows * a.per; w += step) {
+        const int64_t row = w / a.per;
+        const int share = (int)(w - row * a.per);
         const bool of_draft = row >= targets;
         const int64_t at = of_draft ? row - targets : row;
         const int per = of_draft ? a.M - 1 : a.M;
@@ -185,21 +189,22 @@ __global__ void __launch_bounds__(256) verify_small_kernel(const __grid_constant
         const RowSpan<T> r(reinterpret_cast<const T *>(where.p), a.V);
         Share<T, kGreedy> s;
         constexpr uint32_t kPad = no_values<T>();
-        for (int v = lane; v < r.vecs; v += 128) {
+        for (int v = 32 * share + lane; v < r.vecs; v += 128 * a.per) {
             uint4 x[4];
             int i[4];
 #pragma unroll
             for (int n = 0; n < 4; ++n) {
-                const int w = v + 32 * n;
-                x[n] = w < r.vecs ? r.vectors()[w] : make_uint4(kPad, kPad, kPad, kPad);
-                i[n] = r.head + w * E;
+                const int at = v + 32 * a.per * n;
+                x[n] = at < r.vecs ? r.vectors()[at] : make_uint4(kPad, kPad, kPad, kPad);
+                i[n] = r.head + at * E;
             }
             s.template add<4>(x, i, c);
         }
-        s.add_ends(r, c);
+        if (share == 0)
+            s.add_ends(r, c);
         const UnitPartial p = s.join(c);
         if (lane == 0)
-            a.parts[where.part] = p;
+            a.parts[where.part + share] = p;
     }
 }
 
@@ -341,41 +346,39 @@ __global__ void __launch_bounds__(kMath + 32, 1)
 }
 
 // ---- The walk.
-// A row's parts joined, by a warp.
+// A row's parts joined.
 struct RowSum {
     ExpSum z;
     uint32_t first = kNoIdx;
-};
 
-__device__ __forceinline__ RowSum row_sum(const VerifyArgs &a, int64_t part, float c)
-{
-    RowSum s;
-    for (int i = threadIdx.x & 31; i < a.per; i += 32) {
-        const int4 r = __ldcg(reinterpret_cast<const int4 *>(a.parts + part + i));
+    __device__ __forceinline__ void take(const int4 &r, bool greedy, float c)
+    {
         ExpSum o;
         o.m = __int_as_float(r.x);
         o.z = __int_as_float(r.y);
-        if (a.greedy) {
-            if (o.m > s.z.m || (o.m == s.z.m && (uint32_t)r.z < s.first))
-                s.first = (uint32_t)r.z;
-            s.z.m = fmaxf(s.z.m, o.m);
-            s.z.z += o.z;
+        if (greedy) {
+            if (o.m > z.m || (o.m == z.m && (uint32_t)r.z < first))
+                first = (uint32_t)r.z;
+            z.m = fmaxf(z.m, o.m);
+            z.z += o.z;
         } else {
-            s.z.merge(o, c);
+            z.merge(o, c);
         }
     }
-    if (a.greedy) {
-        const float top = warp_most(s.z.m);
-        s.first = __reduce_min_sync(0xFFFFFFFFu, s.z.m == top ? s.first : kNoIdx);
-        s.z.m = top;
+    __device__ __forceinline__ void join_warp(bool greedy, float c)
+    {
+        if (greedy) {
+            const float top = warp_most(z.m);
+            first = __reduce_min_sync(0xFFFFFFFFu, z.m == top ? first : kNoIdx);
+            z.m = top;
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1)
-            s.z.z += __shfl_xor_sync(0xFFFFFFFFu, s.z.z, o);
-    } else {
-        s.z = warp_sum(s.z, c);
+            for (int o = 16; o > 0; o >>= 1)
+                z.z += __shfl_xor_sync(0xFFFFFFFFu, z.z, o);
+        } else {
+            z = warp_sum(z, c);
+        }
     }
-    return s;
-}
+};
 
 __device__ __forceinline__ bool usable(const ExpSum &z)
 {
@@ -419,36 +422,111 @@ inline size_t draw_smem(int M, int V, int ranks, bool greedy)
            (greedy ? 0 : (size_t)((V + ranks - 1) / ranks + 31) / 32 * 4);
 }
 
-// Which child of node c is taken, by a warp; kNone, or kBad where a row of c is unusable.
-__device__ __forceinline__ int decide(const VerifyArgs &a, const Nodes &s, int c, int n, const RowSum &t,
-                                      const RowSum &q)
+// The sums of a sequence's rows, of the target's n and of the draft's n - 1: a thread a row where a row
+// is a few parts, else a warp, with the first parts of kAhead rows on their way at once.
+template <typename T>
+__device__ __forceinline__ void sum_rows(const VerifyArgs &a, const Nodes &s, int b, int n)
+{
+    constexpr int kAhead = 4;
+    const int rows = a.draft ? 2 * n - 1 : n;
+    auto keep = [&](int r, const RowSum &x) {
+        if (r < n) {
+            s.of[r] = x.z;
+            s.first[r] = x.first;
+        } else {
+            s.less[r - n] = x.z;
+        }
+    };
+    auto parts = [&](int r) {
+        return reinterpret_cast<const int4 *>(a.parts + (r < n ? row_at<T>(a, b, r, false).part
+                                                               : row_at<T>(a, b, r - n, true).part));
+    };
+    if (a.per <= 8) {
+        for (int r = threadIdx.x; r < rows; r += kDraw) {
+            RowSum x;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < a.per)
+                    x.take(__ldcg(parts(r) + i), a.greedy, r < n ? a.ct : a.cd);
+            keep(r, x);
+        }
+        return;
+    }
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    for (int r0 = warp; r0 < rows; r0 += kAhead * (kDraw / 32)) {
+        int4 p[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int r = r0 + k * (kDraw / 32);
+            if (r < rows && lane < a.per)
+                p[k] = __ldcg(parts(r) + lane);
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int r = r0 + k * (kDraw / 32);
+            if (r >= rows)
+                break;
+            const float c = r < n ? a.ct : a.cd;
+            RowSum x;
+            if (lane < a.per)
+                x.take(p[k], a.greedy, c);
+            for (int i = lane + 32; i < a.per; i += 32)
+                x.take(__ldcg(parts(r) + i), a.greedy, c);
+            x.join_warp(a.greedy, c);
+            if (lane == 0)
+                keep(r, x);
+        }
+    }
+}
+
+// p of node j's token after its parent c, q of it; 0 for a token out of the vocabulary.
+__device__ __forceinline__ float p_of_node(const VerifyArgs &a, const Nodes &s, int c, int j)
+{
+    const bool inside = s.token[j] >= 0 && s.token[j] < a.V;
+    return inside ? ex2_mufu((s.x[j] - s.of[c].m) * a.ct) / s.of[c].z : 0.0f;
+}
+__device__ __forceinline__ float q_of_node(const VerifyArgs &a, const Nodes &s, int c, int j)
+{
+    const bool inside = s.token[j] >= 0 && s.token[j] < a.V;
+    return inside ? ex2_mufu((s.y[j] - s.less[c].m) * a.cd) / s.less[c].z : 0.0f;
+}
+
+// Which child of node c is taken, kNone, or kBad where a row of c is unusable.  Of a chain, by a thread:
+__device__ __forceinline__ int decide_chain(const VerifyArgs &a, const Nodes &s, int c, int n)
+{
+    const int j = c + 1;
+    if (!usable(s.of[c]) || (a.draft && j < n && !usable(s.less[c])))
+        return kBad;
+    if (j >= n)
+        return kNone;
+    if (a.greedy)
+        return (uint32_t)s.token[j] == s.first[c] ? j : kNone;
+    const float p = p_of_node(a, s, c, j);
+    const double u = s.uniform[j];
+    return u * (a.draft ? (double)q_of_node(a, s, c, j) : 1.0) < (double)p ? j : kNone;
+}
+
+// Of a tree, by a warp:
+__device__ __forceinline__ int decide(const VerifyArgs &a, const Nodes &s, int c, int n)
 {
     const int lane = threadIdx.x & 31;
-    const bool drawn = a.draft && c + 1 < n;
-    if (!usable(t.z) || (drawn && !usable(q.z)))
+    if (!usable(s.of[c]))
         return kBad;
-    const int end = a.parents ? n : min(n, c + 2);
     double left = 1.0;
-    for (int j0 = c + 1; j0 < end; j0 += 32) {
+    for (int j0 = c + 1; j0 < n; j0 += 32) {
         const int j = j0 + lane;
-        const bool child = j < end && s.parent[j] == c;
+        const bool child = j < n && s.parent[j] == c;
         uint32_t kids = __ballot_sync(0xFFFFFFFFu, child);
         if (!kids)
             continue;
         const int d = child ? s.token[j] : -1;
-        const bool inside = d >= 0 && d < a.V;
         if (a.greedy) {
-            const uint32_t hit = __ballot_sync(0xFFFFFFFFu, inside && (uint32_t)d == t.first);
+            const uint32_t hit = __ballot_sync(0xFFFFFFFFu, child && (uint32_t)d == s.first[c]);
             if (hit)
                 return j0 + __ffs(hit) - 1;
             continue;
         }
-        float p = 0.0f, other = 0.0f;
-        if (inside) {
-            p = ex2_mufu((s.x[j] - t.z.m) * a.ct) / t.z.z;
-            if (drawn)
-                other = ex2_mufu((s.y[j] - q.z.m) * a.cd) / q.z.z;
-        }
+        float p = child ? p_of_node(a, s, c, j) : 0.0f;
         // a token that was tried before counts 0: among these 32, and among those before them
         if (__match_any_sync(0xFFFFFFFFu, d) & kids & ((1u << lane) - 1))
             p = 0.0f;
@@ -463,8 +541,7 @@ __device__ __forceinline__ int decide(const VerifyArgs &a, const Nodes &s, int c
         for (; kids; kids &= kids - 1) {
             const int k = __ffs(kids) - 1;
             const float pk = __shfl_sync(0xFFFFFFFFu, p, k), uk = __shfl_sync(0xFFFFFFFFu, u, k);
-            const float qk = __shfl_sync(0xFFFFFFFFu, other, k);
-            if ((double)uk * (drawn ? (double)qk : left) < (double)pk)
+            if ((double)uk * left < (double)pk)
                 return j0 + k;
             left -= pk;
         }
@@ -516,18 +593,17 @@ __global__ void __launch_bounds__(kDraw, 2) verify_draw_kernel(const __grid_cons
     pdl_wait();
     cluster_wait();  // every CTA of the cluster is there
     __syncthreads();
-    for (int c = warp; c < n; c += kDraw / 32) {
-        const RowSum t = row_sum(a, row_at<T>(a, b, c, false).part, a.ct);
-        RowSum q;
-        if (a.draft && c + 1 < n)
-            q = row_sum(a, row_at<T>(a, b, c, true).part, a.cd);
-        const int to = decide(a, s, c, n, t, q);
-        if (lane == 0) {
-            s.choice[c] = (short)to;
-            s.of[c] = t.z;
-            s.less[c] = q.z;
-            s.first[c] = t.first;
+    sum_rows<T>(a, s, b, n);
+    __syncthreads();
+    if (a.parents) {
+        for (int c = warp; c < n; c += kDraw / 32) {
+            const int to = decide(a, s, c, n);
+            if (lane == 0)
+                s.choice[c] = (short)to;
         }
+    } else {
+        for (int c = tid; c < n; c += kDraw)
+            s.choice[c] = (short)decide_chain(a, s, c, n);
     }
     __syncthreads();
     if (tid == 0) {
@@ -643,12 +719,27 @@ __global__ void __launch_bounds__(kDraw, 2) verify_draw_kernel(const __grid_cons
                     }
                 }
             } else {
-#pragma unroll 4
-                for (int v = v0 + tid; v < v1; v += kDraw) {
-                    float r = p_of(to_float(row[v]));
-                    if (rejected)
-                        r -= q_of(to_float(less[v]));
-                    weigh((gone[(v - v0) >> 5] >> ((v - v0) & 31)) & 1u ? 0.0f : r, noise[v], v);
+                constexpr int kMany = 8;  // values of a thread in flight
+                for (int w = v0 + tid; w < v1; w += kMany * kDraw) {
+                    T x[kMany], y[kMany];
+                    float e[kMany];
+#pragma unroll
+                    for (int k = 0; k < kMany; ++k) {
+                        const int v = min(w + k * kDraw, v1 - 1);
+                        x[k] = row[v];
+                        y[k] = less[v];
+                        e[k] = noise[v];
+                    }
+#pragma unroll
+                    for (int k = 0; k < kMany; ++k) {
+                        const int v = w + k * kDraw;
+                        if (v >= v1)
+                            break;
+                        float r = p_of(to_float(x[k]));
+                        if (rejected)
+                            r -= q_of(to_float(y[k]));
+                        weigh((gone[(v - v0) >> 5] >> ((v - v0) & 31)) & 1u ? 0.0f : r, e[k], v);
+                    }
                 }
             }
             unsigned long long top = best_of_cta();
@@ -724,7 +815,7 @@ cudaError_t launch_verify(const VerifyArgs &a, cudaStream_t s)
     auto small = a.greedy ? verify_small_kernel<T, true> : verify_small_kernel<T, false>;
     auto stream = a.greedy ? verify_stream_kernel<T, true> : verify_stream_kernel<T, false>;
     if ((int64_t)a.V * sizeof(T) <= kSmallRow) {
-        const int64_t want = (rows + 7) / 8, most = (int64_t)sm_count() * 8;
+        const int64_t want = (rows * a.per + 7) / 8, most = (int64_t)sm_count() * 8;
         e = launch(small, dim3((unsigned)(want < most ? want : most)), dim3(256), 0, s, true, a);
     } else {
         const int64_t units = rows * a.pieces, most = sm_count();
@@ -756,6 +847,8 @@ void cut_rows(int64_t rows, int V, int es, int &pieces, int &piece_vecs, int &pe
     if ((int64_t)V * es <= kSmallRow) {
         pieces = per = 1;
         piece_vecs = 0;
+        while (per < 8 && (int64_t)V * es / 16 > per * 32 * kSmallVecs)
+            per *= 2;
         return;
     }
     // vectors that a row has wherever it begins, so that no piece is empty
