@@ -557,7 +557,8 @@ __global__ void __launch_bounds__(kDraw, 2) verify_draw_kernel(const __grid_cons
 {
     constexpr int E = 16 / sizeof(T);
     __shared__ int taken, failed;
-    __shared__ unsigned long long best[kDraw / 32], of_cta[kMaxRanks];
+    __shared__ unsigned long long of_cta[kMaxRanks];
+    __shared__ uint2 best[kDraw / 32];
     extern __shared__ __align__(16) uint8_t dynamic[];
     const Nodes s(dynamic, a.M);
     uint32_t *const gone = s.gone;
@@ -568,7 +569,7 @@ __global__ void __launch_bounds__(kDraw, 2) verify_draw_kernel(const __grid_cons
     const int v0 = min(a.V, rank * slice), v1 = min(a.V, v0 + slice);
     const int64_t base = (int64_t)b * a.M;
     const float *noise = a.noise + (int64_t)b * a.V;
-    cluster_arrive();
+    cluster_arrive_relaxed();  // (that this CTA is there; waited for where another writes to it)
     if (!a.greedy) {
         for (int i = tid; i < slice / 32; i += kDraw)
             gone[i] = 0;
@@ -591,7 +592,6 @@ __global__ void __launch_bounds__(kDraw, 2) verify_draw_kernel(const __grid_cons
         }
     }
     pdl_wait();
-    cluster_wait();  // every CTA of the cluster is there
     __syncthreads();
     sum_rows<T>(a, s, b, n);
     __syncthreads();
@@ -621,6 +621,8 @@ __global__ void __launch_bounds__(kDraw, 2) verify_draw_kernel(const __grid_cons
     }
     __syncthreads();
     int extra = -1;
+    if (failed || a.greedy)
+        cluster_wait();
     if (!failed) {
         const int cur = s.path[taken];
         if (a.greedy) {
@@ -652,29 +654,47 @@ __global__ void __launch_bounds__(kDraw, 2) verify_draw_kernel(const __grid_cons
                     }
                 }
             };
+            // of all values of a vector, two at a time; the norm's reciprocal in the exponent
+            auto weights = [&](float (&x)[E], uint64_t m2, uint64_t c2, uint64_t l2) {
+#pragma unroll
+                for (int i = 0; i < E; i += 2) {
+                    float t0, t1;
+                    un2(fma2(add2(f2(x[i], x[i + 1]), m2), c2, l2), t0, t1);
+                    x[i] = ex2_mufu(t0);
+                    x[i + 1] = ex2_mufu(t1);
+                }
+            };
+            const float pl = -log2f(s.of[cur].z), ql = rejected ? -log2f(s.less[cur].z) : 0.0f;
+            const uint64_t pm2 = f2(-pm, -pm), pc2 = f2(a.ct, a.ct), pl2 = f2(pl, pl);
+            const uint64_t qm2 = f2(-qm, -qm), qc2 = f2(a.cd, a.cd), ql2 = f2(ql, ql);
+            float bar = 0.0f;
             auto p_of = [&](float x) { return ex2_mufu((x - pm) * a.ct) * pz; };
             auto q_of = [&](float y) { return ex2_mufu((y - qm) * a.cd) * qz; };
-            auto best_of_cta = [&]() -> unsigned long long {  // in thread 0
-                unsigned long long top =
-                    key > 0.0f ? ((unsigned long long)__float_as_uint(key) << 32) | (0xFFFFFFFFu - at) : 0;
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1) {
-                    const unsigned long long k = __shfl_xor_sync(0xFFFFFFFFu, top, o);
-                    top = k > top ? k : top;
-                }
-                __syncthreads();
+            // the largest key, the lowest token where there are several: in warp 0
+            auto best_of_warp = [&](uint32_t &k, uint32_t &v) {
+                const uint32_t top = __reduce_max_sync(0xFFFFFFFFu, k);
+                v = __reduce_min_sync(0xFFFFFFFFu, k == top ? v : kNoIdx);
+                k = top;
+            };
+            auto best_of_cta = [&]() -> unsigned long long {
+                uint32_t k = __float_as_uint(key), v = at;
+                best_of_warp(k, v);
                 if (lane == 0)
-                    best[warp] = top;
+                    best[warp] = make_uint2(k, v);
                 __syncthreads();
-                if (tid == 0)
-                    for (int w = 1; w < kDraw / 32; ++w)
-                        top = best[w] > top ? best[w] : top;
-                return top;
+                if (warp == 0) {
+                    const uint2 o = lane < kDraw / 32 ? best[lane] : make_uint2(0, kNoIdx);
+                    k = o.x;
+                    v = o.y;
+                    best_of_warp(k, v);
+                }
+                return k ? ((unsigned long long)k << 32) | (0xFFFFFFFFu - v) : 0;
             };
             if (((reinterpret_cast<uintptr_t>(row) | reinterpret_cast<uintptr_t>(less) |
                   reinterpret_cast<uintptr_t>(noise)) & 15u) == 0 && a.V % E == 0) {
                 constexpr int kTwo = 2;  // vectors of a thread in flight
-                for (int w = v0 + tid * E; w < v1; w += kTwo * kDraw * E) {
+                for (int w0 = v0 + warp * 32 * E; w0 < v1; w0 += kTwo * kDraw * E) {
+                    const int w = w0 + lane * E;
                     uint4 xr[kTwo], yr[kTwo];
                     float4 er[kTwo][E / 4];
 #pragma unroll
@@ -694,29 +714,37 @@ __global__ void __launch_bounds__(kDraw, 2) verify_draw_kernel(const __grid_cons
                         const int v = w + k * kDraw * E;
                         if (v >= v1)
                             continue;
-                        float x[E];
+                        float x[E], y[E];
                         widen<T>(xr[k], x);
-#pragma unroll
-                        for (int i = 0; i < E; ++i)
-                            x[i] = p_of(x[i]);
+                        weights(x, pm2, pc2, pl2);
                         if (rejected) {
-                            float y[E];
                             widen<T>(yr[k], y);
+                            weights(y, qm2, qc2, ql2);
 #pragma unroll
                             for (int i = 0; i < E; ++i)
-                                x[i] -= q_of(y[i]);
+                                x[i] -= y[i];
                         }
                         const uint32_t out = gone[(v - v0) >> 5] >> ((v - v0) & 31);
                         if (out & ((1u << E) - 1))
 #pragma unroll
                             for (int i = 0; i < E; ++i)
                                 x[i] = (out >> i) & 1u ? 0.0f : x[i];
+                        // whether one of them is more than the warp's best
+                        float most = -1.0f;
 #pragma unroll
-                        for (int i = 0; i < E; ++i) {
-                            const float4 f = er[k][i / 4];
-                            weigh(x[i], i % 4 == 0 ? f.x : i % 4 == 1 ? f.y : i % 4 == 2 ? f.z : f.w, v + i);
+                        for (int i = 0; i < E / 4; ++i) {
+                            const float4 f = er[k][i];
+                            most = max3(most, fmaf(-bar, f.x, x[4 * i]), fmaf(-bar, f.y, x[4 * i + 1]));
+                            most = max3(most, fmaf(-bar, f.z, x[4 * i + 2]), fmaf(-bar, f.w, x[4 * i + 3]));
                         }
+                        if (most > 0.0f)
+#pragma unroll
+                            for (int i = 0; i < E; ++i) {
+                                const float4 f = er[k][i / 4];
+                                weigh(x[i], i % 4 == 0 ? f.x : i % 4 == 1 ? f.y : i % 4 == 2 ? f.z : f.w, v + i);
+                            }
                     }
+                    bar = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(key)));
                 }
             } else {
                 constexpr int kMany = 8;  // values of a thread in flight
@@ -743,6 +771,7 @@ __global__ void __launch_bounds__(kDraw, 2) verify_draw_kernel(const __grid_cons
                 }
             }
             unsigned long long top = best_of_cta();
+            cluster_wait();
             if (tid == 0)
                 cluster.map_shared_rank(of_cta, 0)[rank] = top;
             cluster_arrive();

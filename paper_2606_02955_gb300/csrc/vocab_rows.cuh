@@ -207,6 +207,10 @@ struct Summed {
 };
 
 // The cluster's barrier, in its two halves.  A CTA may leave behind its last arrival.
+__device__ __forceinline__ void cluster_arrive_relaxed()  // (orders no memory)
+{
+    asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
+}
 __device__ __forceinline__ void cluster_arrive()
 {
     asm volatile("barrier.cluster.arrive.release;" ::: "memory");

@@ -82,6 +82,19 @@ def test_shapes(fd, kind, dtype, B, M, V):
     check(fd, target, tokens, **kw)
 
 
+@pytest.mark.parametrize("dtype", [BF, HF, FP])
+@pytest.mark.parametrize("kind", ["draft", "greedy"])
+@pytest.mark.parametrize("more", [-9, -8, -1, 0, 1, 7, 8, 9])
+def test_rows_of_about_whole_chunks(fd, dtype, kind, more):
+    """Rows that end a few values before or behind a chunk of 64 KB, at every place of a vector."""
+    V = (1 if dtype == FP else 2) * 16384 + more
+    target, tokens, kw = inputs(3, 3, V, dtype, kind, seed=more + 30)
+    target[:, :, -1] = 11.0  # the last values count
+    check(fd, target, tokens, **kw)
+    lens = torch.tensor([3, 1, 2], dtype=torch.int32)
+    check(fd, target, tokens, lens=lens, **kw)
+
+
 @pytest.mark.parametrize("seed", range(16))
 def test_many_sequences(fd, seed):
     kind = ("draft", "tree", "chosen", "greedy")[seed % 4]
