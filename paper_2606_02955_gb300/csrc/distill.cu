@@ -295,7 +295,7 @@ __global__ void __launch_bounds__(kThreads, 8) distill_small_kernel(const __grid
 // ---- Longer rows: a CTA, or a cluster of them, holds a row in shared memory from its sum to its
 // gradient.
 //
-// Roles.  Sixteen warps walk the row (the sum, then the gradient); four look after the teacher: for the
+// Roles.  Sixteen warps walk the row (the sum, then the gradient); eight look after the teacher: for the
 // row to come they read its list and the student's logits of it, make the probabilities and what
 // else is of the list alone, and mark the listed tokens, and for the row before they write the
 // listed tokens' gradients over what the sixteen wrote there; one lane copies rows into a ring of
@@ -306,7 +306,7 @@ __global__ void __launch_bounds__(kThreads, 8) distill_small_kernel(const __grid
 // row's last; the second pass starts with the oldest that is still there, and each chunk it gives back
 // makes room for one of the next row.
 constexpr int kMathWarps = 16, kMath = 32 * kMathWarps;
-constexpr int kTeachers = 128;
+constexpr int kTeachers = 256;
 constexpr int kRingThreads = kMath + kTeachers + 64;
 constexpr int kChunk = 32768, kChunkVecs = kChunk / 16, kPer = kChunkVecs / kMath;
 constexpr int kMostListed = 1 << 17;  // tokens of a CTA's share of a row: their bits take 16 KB
@@ -413,7 +413,7 @@ struct RingShared {
     float4 fix[2];        // for the listed tokens: M, Z, P + R, scale
     ExpSum part[2][kMathWarps];
     ExpSum of_rank[2][kMaxRanks];
-    float reduce[3][4];
+    float reduce[3][kTeachers / 32];
     uint32_t groups[2][kMostListed / 4 / 1024];  // a bit for each 32 vectors that hold a marked value
     int twice;
     uint32_t ends;
@@ -488,7 +488,11 @@ __device__ __forceinline__ float teach_reduce(float x, float *of_warp, F f)
     if ((threadIdx.x & 31) == 0)
         of_warp[(threadIdx.x - kMath) >> 5] = x;
     named_sync(kBarTeach, kTeachers);
-    return f(f(of_warp[0], of_warp[1]), f(of_warp[2], of_warp[3]));
+    x = of_warp[0];
+#pragma unroll
+    for (int i = 1; i < kTeachers / 32; ++i)
+        x = f(x, of_warp[i]);
+    return x;
 }
 
 template <typename T, bool kSum, bool kGrad>
@@ -692,6 +696,33 @@ __global__ void __launch_bounds__(kRingThreads, 1)
         int *const idx = reinterpret_cast<int *>(smem + Layout::dup);
         float *const mass = reinterpret_cast<float *>(idx + kMaxTop);
         RowWalk walk(a.mask, a.rows, true);
+        // The lists are read a row ahead: of the row to come, as they lie in memory.
+        int64_t next_row;
+        int next_v[kMine];
+        float next_s[kMine], next_lse = 0.0f, next_scale = 0.0f;
+        float4 next_given = make_float4(0, 0, 0, 0);
+        auto fetch = [&](uint32_t i) {
+            next_row = walk.find(cluster + (int64_t)i * clusters);
+#pragma unroll
+            for (int j = 0; j < kMine; ++j) {
+                const int k = t + j * kTeachers;
+                next_v[j] = -1;
+                next_s[j] = neg_inf_f();
+                if (next_row >= 0 && k < a.K) {
+                    next_v[j] = a.index[next_row * a.K + k];
+                    next_s[j] = top_value(a, next_row * a.K + k);
+                }
+            }
+            if (next_row >= 0) {
+                if (a.lse)
+                    next_lse = a.lse[next_row];
+                if (kGrad)
+                    next_scale = a.grad_loss[next_row] * a.inv_t;
+                if (!kSum)
+                    next_given = a.stats_in[next_row];
+            }
+        };
+        fetch(0);
         int old[kMine];  // of the row before: its listed tokens, and what their gradients need
         float old_p[kMine], old_x[kMine];
         int64_t old_row = -1;
@@ -702,51 +733,51 @@ __global__ void __launch_bounds__(kRingThreads, 1)
             old[j] = older[j] = -1, old_p[j] = old_x[j] = 0.0f;
         for (uint32_t i = 0;; ++i) {
             const uint32_t par = i & 1;
-            const int64_t row = walk.find(cluster + (int64_t)i * clusters);
+            const int64_t row = next_row;
             int v[kMine];
             float m[kMine], x[kMine];
-            float P = 0.0f, R = 0.0f, A = 0.0f, scale = 0.0f;
+            float P = 0.0f, R = 0.0f, A = 0.0f;
+            const float scale = next_scale;
+            const float4 given = next_given;
             ExpSum of_x;
-            float4 given = make_float4(0, 0, 0, 0);
             if (row >= 0) {
                 const T *logits = static_cast<const T *>(a.logits) + row * a.V;
                 float most = -FLT_MAX;
+                T raw[kMine];
 #pragma unroll
                 for (int j = 0; j < kMine; ++j) {
-                    const int k = t + j * kTeachers;
-                    v[j] = -1;
-                    m[j] = neg_inf_f();
-                    if (k < a.K) {
-                        const int at = a.index[row * a.K + k];
-                        if (at >= 0 && at < a.V) {
-                            v[j] = at;
-                            m[j] = __fdiv_rn(top_value(a, row * a.K + k), a.temperature);
-                        }
-                        most = Most()(most, m[j]);
-                    }
+                    v[j] = next_v[j] >= 0 && next_v[j] < a.V ? next_v[j] : -1;
+                    m[j] = v[j] >= 0 ? next_s[j] : neg_inf_f();
+                    raw[j] = logits[max(v[j], 0)];
                 }
+                const float lse = next_lse;
+                fetch(i + 1);
 #pragma unroll
                 for (int j = 0; j < kMine; ++j)
-                    x[j] = v[j] >= 0 ? to_float(logits[v[j]]) : neg_inf_f();
-                if (kGrad)
-                    scale = a.grad_loss[row] * a.inv_t;
-                if (!kSum)
-                    given = a.stats_in[row];
-                most = a.lse ? a.lse[row] : teach_reduce(most, sm.reduce[0], Most());
+                    if (j == 0 || j * kTeachers < a.K) {
+                        m[j] = __fdiv_rn(m[j], a.temperature);
+                        most = Most()(most, m[j]);
+                    }
+                most = a.lse ? lse : teach_reduce(most, sm.reduce[0], Most());
 #pragma unroll
-                for (int j = 0; j < kMine; ++j) {
-                    m[j] = v[j] >= 0 ? expf(m[j] - most) : 0.0f;
-                    P += m[j];
-                }
+                for (int j = 0; j < kMine; ++j)
+                    if (j == 0 || j * kTeachers < a.K) {
+                        m[j] = v[j] >= 0 ? expf(m[j] - most) : 0.0f;
+                        P += m[j];
+                    }
                 P = teach_reduce(P, sm.reduce[1], Add());
                 if (a.lse) {
                     R = fmaxf(1.0f - P, 0.0f);
                 } else if (P != 0.0f) {
 #pragma unroll
                     for (int j = 0; j < kMine; ++j)
-                        m[j] = __fdiv_rn(m[j], P);
+                        if (j == 0 || j * kTeachers < a.K)
+                            m[j] = __fdiv_rn(m[j], P);
                     P = P == P ? 1.0f : P;
                 }
+#pragma unroll
+                for (int j = 0; j < kMine; ++j)
+                    x[j] = v[j] >= 0 ? to_float(raw[j]) : neg_inf_f();
             }
             // ---- the marks: those of the row that had this set go, this one's come
             if (kTwo && i > 1)
@@ -757,8 +788,7 @@ __global__ void __launch_bounds__(kRingThreads, 1)
             uint32_t *const groups = sm.groups[kTwo ? par : 0];
             if (named_sync_or(kBarTeach, kTeachers, dead))
                 break;
-            auto mark = [&](int64_t of_row, int at, bool set) -> bool {  // whether it was set before
-                const RowShare<T> sh(a.logits, of_row, a.V, rank, ranks);
+            auto mark = [&](const RowShare<T> &sh, int at, bool set) -> bool {  // whether it was set before
                 uint32_t *word, bit;
                 if (at < sh.r.head) {
                     word = &sm.ends;
@@ -780,11 +810,13 @@ __global__ void __launch_bounds__(kRingThreads, 1)
                 atomicAnd(word, ~(1u << bit));
                 return false;
             };
-            if ((kTwo ? older_row : old_row) >= 0)
+            if ((kTwo ? older_row : old_row) >= 0) {
+                const RowShare<T> sh(a.logits, kTwo ? older_row : old_row, a.V, rank, ranks);
 #pragma unroll
                 for (int j = 0; j < kMine; ++j)
                     if ((kTwo ? older[j] : old[j]) >= 0)
-                        mark(kTwo ? older_row : old_row, kTwo ? older[j] : old[j], false);
+                        mark(sh, kTwo ? older[j] : old[j], false);
+            }
             if (t == 0) {
                 sm.ends = 0;
                 sm.twice = 0;
@@ -793,11 +825,12 @@ __global__ void __launch_bounds__(kRingThreads, 1)
                 groups[t] = 0;
             named_sync(kBarTeach, kTeachers);
             if (row >= 0) {
+                const RowShare<T> sh(a.logits, row, a.V, rank, ranks);
                 bool again = false;
 #pragma unroll
                 for (int j = 0; j < kMine; ++j)
                     if (v[j] >= 0)
-                        again |= mark(row, v[j], true);
+                        again |= mark(sh, v[j], true);
                 if (ranks > 1) {
                     // the marks are of this CTA's share: other tokens are looked up in a table
                     const int size = a.K <= 64 ? 128 : 2 << (32 - __clz(a.K - 1));
