@@ -598,7 +598,8 @@ size_t fdllm_verify_draft_workspace_bytes(int B, int M, int V, int dtype);
  *   out_nodes  [B, M] int32: the root (0), then the taken nodes: the rows whose keys and values
  *              enter the cache; -1 behind.
  *   out_n      [B] int32: taken tokens, 0 .. M - 1; FDLLM_ROW_NONFINITE (and -1 in the row of the
- *              others) where a row on the way holds a NaN or its maximum is infinite.
+ *              others) where a row on the way holds a NaN or its maximum is infinite;
+ *              FDLLM_ROW_DEVICE_ERROR where a kernel gave up a bounded wait (fdllm_cache_status).
  *   workspace  device, 256-byte aligned, fdllm_verify_draft_workspace_bytes() bytes of any content;
  *              calls that may overlap on the GPU need their own. */
 fdllm_status fdllm_verify_draft(const void *target, const int64_t *target_strides,
@@ -657,10 +658,11 @@ fdllm_status fdllm_distill_step(const void *logits, int dtype, int B, int L, int
                                 const float *grad_loss, float *out_loss, void *out_grad,
                                 void *stream);
 
-/* The sticky device error of fdllm_cache_attention and fdllm_cache_key_weights on the current
- * device: synchronises `stream`, returns FDLLM_ERR_DEVICE if one of their kernels gave up a
- * bounded wait since the last call (the results of the calls since then are unusable), FDLLM_OK
- * otherwise, and clears it. */
+/* The sticky device error of fdllm_cache_attention, fdllm_cache_tree_attention,
+ * fdllm_cache_key_weights, fdllm_verify_draft and the distillation calls on the current device:
+ * synchronises `stream`, returns FDLLM_ERR_DEVICE if one of their kernels gave up a bounded wait since
+ * the last call (the results of the calls since then are unusable; fdllm_verify_draft reports
+ * FDLLM_ROW_DEVICE_ERROR for every sequence until then), FDLLM_OK otherwise, and clears it. */
 fdllm_status fdllm_cache_status(void *stream);
 
 /* Health check of those kernels' bounded waits: enqueues a warp that waits on a barrier nobody

@@ -1017,6 +1017,12 @@ def fdllm_verify_draft(target: torch.Tensor, tokens: torch.Tensor, parents=None,
     return out_tokens, out_nodes, out_n
 
 
+def _overwritten(logits, out_grad):
+    """Tells autograd of a gradient written over its logits (a graph that saved them then says so)."""
+    if out_grad is logits and not logits.is_inference():
+        torch.autograd.graph.increment_version(logits)
+
+
 def _distill_args(logits, mask, top_index, top_logits, teacher_lse, dev):
     """The arguments that the distillation calls share, up to teacher_lse."""
     code, shape = _logits(logits, "logits", 3)
@@ -1028,6 +1034,14 @@ def _distill_args(logits, mask, top_index, top_logits, teacher_lse, dev):
             _ptr(mask, "mask", _U8, rows, dev), _ptr(top_index, "top_index", _I32, (B, L, K), dev),
             _ptr(top_logits, "top_logits", top_logits.dtype, (B, L, K), dev), top, K,
             _ptr(teacher_lse, "teacher_lse", _F32, rows, dev))
+
+
+def _not_captured():
+    # (autograd's engine may touch other streams than the captured one, where an error of its own
+    # thread would end the process)
+    if torch.cuda.is_current_stream_capturing():
+        raise RuntimeError("autograd of fdllm_distill_loss cannot be captured into a CUDA graph: capture "
+                           "fdllm_distill_step, or fdllm_distill_loss and fdllm_distill_grad")
 
 
 class _DistillLoss(torch.autograd.Function):
@@ -1044,6 +1058,7 @@ class _DistillLoss(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, grad_loss):
+        _not_captured()
         if torch.is_grad_enabled():  # (create_graph: the kernels' gradient would be a constant)
             raise RuntimeError("fdllm_distill_loss has no second derivative")
         logits, mask, top_index, top_logits, teacher_lse, stats = ctx.saved_tensors
@@ -1081,15 +1096,16 @@ def fdllm_distill_loss(logits: torch.Tensor, mask: torch.Tensor, top_index: torc
     teacher's probabilities are taken over its listed tokens).
 
     Differentiable with respect to ``logits`` where they require a gradient (the call then runs on
-    the current stream and makes its own outputs; the teacher's tensors get none).  In a CUDA graph
-    that holds the backward pass too, use fdllm_distill_step, or fdllm_distill_grad with
-    ``out_stats`` fp32 [B, L, 4]."""
+    the current stream and makes its own outputs; the teacher's tensors get none; there is no second
+    derivative).  It cannot be captured into a CUDA graph in that form: capture fdllm_distill_step, or
+    this call without a gradient, with ``out_stats`` fp32 [B, L, 4], and fdllm_distill_grad."""
     if logits.requires_grad and torch.is_grad_enabled():
         if out_loss is not None or out_stats is not None or stream is not None:
             raise ValueError("a loss for autograd makes its own outputs on the current stream: "
                              "out_loss, out_stats and stream must be None")
         if top_logits.requires_grad or (teacher_lse is not None and teacher_lse.requires_grad):
             raise ValueError("the teacher's tensors get no gradient: detach them")
+        _not_captured()
         return _DistillLoss.apply(logits, mask, top_index, top_logits, teacher_lse, temperature)
     return _distill_loss(logits, mask, top_index, top_logits, teacher_lse, temperature, out_loss,
                          out_stats, stream)
@@ -1119,6 +1135,7 @@ def _distill_grad(logits, mask, top_index, top_logits, stats, grad_loss, teacher
         _raw_stream(dev.index) if stream is None else _stream(stream))
     if st:
         _check(st, "fdllm_distill_grad")
+    _overwritten(logits, out_grad)
     return out_grad
 
 
@@ -1143,6 +1160,7 @@ def fdllm_distill_step(logits: torch.Tensor, mask: torch.Tensor, top_index: torc
         _raw_stream(dev.index) if stream is None else _stream(stream))
     if st:
         _check(st, "fdllm_distill_step")
+    _overwritten(logits, out_grad)
     return out_loss, out_grad
 
 

@@ -14,7 +14,10 @@ Tolerances of the distillation (fixed before the first run).  With u = 2^-24:
     rounding of what it is made of, 4 u (|log a| + |x - M| / temperature + log Z).  The rest's mass
     R is 1 less a sum, off by p absolutely.
   * A gradient: the formula's terms off by 2 (z + p) each, and half a step of the result's type
-    (2^-8, 2^-11, 2^-24; below the normal numbers half of the smallest subnormal).
+    (2^-8, 2^-11, 2^-24; below the normal numbers half of the smallest subnormal).  Its q_v and
+    q_v / r are single exponentials: the four roundings of an argument of t bits take 4 u ln 2 |t| of
+    them, whatever they weigh in the sum; and the exponential is 0 below 2^-126 (ex2.approx.ftz), so
+    2^-126 of the factor before it, |grad_loss| / temperature (P + 2 R), may be lost besides.
 """
 import math
 
@@ -207,6 +210,8 @@ def distill(logits, mask, index, top, lse=None, temperature=1.0, grad_loss=None)
             loss[b, t], loss_tol[b, t] = value, slack + 4 * U * abs(value) + 1e-30
             if g is not None:
                 grad[b, t] = dx * g / temperature
+                far = torch.nan_to_num(size, posinf=0.0) * 4 * U  # (t ln 2 = size)
+                off = off + far * (q * (P + R) + (R * s if R > 0 and some else 0.0)) + 2.0 ** -126 * (P + 2 * R)
                 grad_tol[b, t] = (off * abs(g) / temperature + EPS[logits.dtype] * grad[b, t].abs() * 1.001
                                   + TINY[logits.dtype])
     return loss, loss_tol, grad, grad_tol

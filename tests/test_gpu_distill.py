@@ -226,6 +226,47 @@ def test_autograd_inside_a_graph_of_operations(fd):
         fd.fdllm_distill_loss(**{**kw, "logits": x @ w, "top_logits": kw["top_logits"].requires_grad_()})
 
 
+def test_autograd_is_not_captured(fd):
+    """Neither pass: capture ends with an error of the call, and eager work goes on."""
+    kw, weights = inputs(2, 3, 200, 5, BF, 20, False)
+    x = kw["logits"].requires_grad_()
+    eager = fd.fdllm_distill_loss(**kw)
+    with pytest.raises(RuntimeError):
+        with torch.cuda.graph(torch.cuda.CUDAGraph()):
+            fd.fdllm_distill_loss(**kw)
+    grad, = torch.autograd.grad(eager, x, weights)
+    step = fd.fdllm_distill_step(x, kw["mask"], kw["top_index"], kw["top_logits"], weights)
+    assert torch.equal(grad, step[1])
+
+
+def test_a_gradient_over_saved_logits_is_seen(fd):
+    kw, weights = inputs(1, 3, 200, 5, FP, 21, False)
+    x = (kw["logits"] * 1.0).requires_grad_()
+    y = x * 2.0
+    loss = fd.fdllm_distill_loss(**{**kw, "logits": y})
+    fd.fdllm_distill_step(y, kw["mask"], kw["top_index"], kw["top_logits"], weights, out_grad=y)
+    with pytest.raises(RuntimeError):
+        loss.backward(weights)
+    with torch.inference_mode():
+        z = kw["logits"] * 1.0
+        fd.fdllm_distill_step(z, kw["mask"], kw["top_index"], kw["top_logits"], weights, out_grad=z)
+
+
+@pytest.mark.parametrize("temperature", [1e-3, 0.05, 30.0, 1e4])
+@pytest.mark.parametrize("V", [700, 20003])
+def test_temperatures_of_any_size(fd, temperature, V):
+    for dtype, rest in ((BF, True), (FP, False)):
+        kw, weights = inputs(2, 3, V, 9, dtype, 22, False, masked=1.1, temperature=temperature)
+        if rest:
+            kw["teacher_lse"] = torch.logsumexp(kw["top_logits"].double() / temperature, -1).float() + 0.7
+        if temperature < 0.01:  # scores of several thousand: the tolerance's 64 covers the logits' part only
+            kw["logits"] *= 0.01
+            kw["top_logits"] *= 0.01
+            if rest:
+                kw["teacher_lse"] = torch.logsumexp(kw["top_logits"].double() / temperature, -1).float() + 0.7
+        check(fd, kw, weights)
+
+
 def test_another_stream_and_a_graph(fd):
     kw, weights = inputs(3, 5, 4099, 20, BF, 17, True)
     args = (kw["logits"], kw["mask"], kw["top_index"], kw["top_logits"], weights, kw["teacher_lse"])
