@@ -95,6 +95,24 @@ def test_rows_of_about_whole_chunks(fd, dtype, kind, more):
     check(fd, target, tokens, lens=lens, **kw)
 
 
+@pytest.mark.parametrize("kind", ["draft", "tree", "chosen", "greedy"])
+@pytest.mark.parametrize("B,M,V,dtype", [(16, 9, 50021, FP), (5, 40, 70003, BF), (40, 5, 81920, HF),
+                                         (1, 120, 126464, BF), (70, 12, 17000, BF)])
+def test_rows_that_the_walk_cannot_reach(fd, kind, B, M, V, dtype):
+    """Large calls: NaN in the rows of nodes that are not on the way changes nothing."""
+    target, tokens, kw = inputs(B, M, V, dtype, kind, seed=B + M)
+    lens = (M - torch.arange(B) % 3 * (M // 3)).int()
+    got = check(fd, target, tokens, most_near=1, lens=lens, **kw)
+    on_path = torch.zeros(B, M, dtype=torch.bool)
+    for b in range(B):
+        on_path[b, got[1][b][got[1][b] >= 0].long()] = True
+    target[~on_path] = math.nan
+    if "draft" in kw:
+        kw["draft"][~on_path[:, :-1]] = math.nan
+    again = run(fd, target, tokens, lens=lens, **kw)
+    assert all(torch.equal(a, b) for a, b in zip(got, again))
+
+
 @pytest.mark.parametrize("seed", range(16))
 def test_many_sequences(fd, seed):
     kind = ("draft", "tree", "chosen", "greedy")[seed % 4]
