@@ -20,7 +20,11 @@ namespace {
 
 constexpr int kMaxTop = 1024;
 constexpr int kThreads = 128;      // of a CTA of the small form
-constexpr int kSmallRow = 16384;   // rows up to this many bytes take it
+// Rows up to kSmallRow bytes take it, and up to kManyRow where there are more rows than SMs: each
+// further row of a CTA costs the long form about 5 us whatever its length, for the latencies from list
+// to mark, which many CTAs to an SM hide.  Steps in bf16: 1024 rows of 12001 15 us (the long form 34), 256
+// of 17000 11 (15), 4096 of 32000 130 (150); but 152 of 32000 12.5 (10.5); 64 of 12001 alike, 8.
+constexpr int kSmallRow = 32768, kManyRow = 65536;
 
 struct DistillArgs {
     const void *logits;      // [rows, V]
@@ -51,23 +55,6 @@ __device__ __forceinline__ float top_value(const DistillArgs &a, int64_t i)
     return __half2float(static_cast<const __half *>(a.top)[i]);
 }
 
-// Sum (or maximum) over the CTA, the same bits in every thread.
-template <typename F>
-__device__ __forceinline__ float cta_reduce(float x, float *warps, F f)
-{
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-        x = f(x, __shfl_xor_sync(0xFFFFFFFFu, x, o));
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0)
-        warps[threadIdx.x >> 5] = x;
-    __syncthreads();
-    x = warps[0];
-    for (int i = 1; i < kThreads / 32; ++i)
-        x = f(x, warps[i]);
-    return x;
-}
-
 struct Add {
     __device__ float operator()(float a, float b) const { return a + b; }
 };
@@ -80,24 +67,78 @@ struct Most {  // a NaN stays
     }
 };
 
-// ---- Short rows: a CTA of kThreads to a row.
+// -inf in the place of the values whose bits are set.
+template <typename T>
+__device__ __forceinline__ void leave_out(uint4 &r, uint32_t bits)
+{
+    constexpr uint32_t kPad = no_values<T>();
+    uint32_t *w = reinterpret_cast<uint32_t *>(&r);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) {
+            w[i] = (bits >> i) & 1u ? kPad : w[i];
+        } else {
+            const uint32_t keep = ((bits >> (2 * i)) & 1u ? 0u : 0xFFFFu) |
+                                  ((bits >> (2 * i + 1)) & 1u ? 0u : 0xFFFF0000u);
+            w[i] = (w[i] & keep) | (kPad & ~keep);
+        }
+    }
+}
+
+// f 2^((x - m) c) of a vector's values: as Summed's terms are taken, what the rounding of m c leaves in f.
+struct RowTerms {
+    uint64_t f2f, c2, n2;
+    bool far;
+    __device__ __forceinline__ RowTerms(float m, float c, float f)
+    {
+        const float ref = m * c;
+        far = !(fabsf(ref) < kFar);
+        if (!far)
+            f *= ex2_mufu(-fmaf(m, c, -ref));
+        f2f = f2(f, f);
+        c2 = f2(c, c);
+        n2 = far ? f2(-m, -m) : f2(-ref, -ref);
+    }
+    template <typename T>
+    __device__ __forceinline__ uint4 of(const uint4 &x) const
+    {
+        constexpr int E = 16 / sizeof(T);
+        float y[E];
+        widen<T>(x, y);
+#pragma unroll
+        for (int e = 0; e < E; e += 2) {
+            const uint64_t y2 = f2(y[e], y[e + 1]);
+            float t0, t1;
+            un2(far ? mul2(add2(y2, n2), c2) : fma2(y2, c2, n2), t0, t1);
+            un2(mul2(f2(ex2_mufu(t0), ex2_mufu(t1)), f2f), y[e], y[e + 1]);
+        }
+        return narrow<T>(y);
+    }
+};
+
+// ---- Short rows: a CTA of kThreads to a row, many on an SM.
 // kSum: the row's sums are taken (else they are given); kGrad: the gradient is written.
 template <typename T, bool kSum, bool kGrad>
 __global__ void __launch_bounds__(kThreads, 8) distill_small_kernel(const __grid_constant__ DistillArgs a)
 {
     constexpr int E = 16 / sizeof(T);
     constexpr int kMine = kMaxTop / kThreads;  // listed tokens of a thread
-    extern __shared__ __align__(16) uint32_t listed[];  // a bit for each token
+    constexpr int kWarps = kThreads / 32;
+    constexpr int kFour = 4;  // vectors of a thread in flight
+    extern __shared__ __align__(16) uint32_t marks[];  // a bit for each value of the whole vectors
     __shared__ int idx[kMaxTop];
     __shared__ float p[kMaxTop];
-    __shared__ float warps[kThreads / 32];
-    __shared__ ExpSum sums[kThreads / 32];
+    __shared__ float of_most[kWarps], of_mass[kWarps];
+    __shared__ ExpSum of_rest[kWarps], of_listed[kWarps];
+    __shared__ float of_loss[kWarps], of_share[kWarps];
+    __shared__ uint32_t ends;  // of the values before the whole vectors (8 bits), and behind
     __shared__ int twice;
     pdl_wait();
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const float c = a.inv_t * kLog2e;
-    for (int i = tid; i < (a.V + 31) / 32; i += kThreads)
-        listed[i] = 0;
+    const uint8_t *const listed = reinterpret_cast<const uint8_t *>(marks);
+    for (int i = tid; i < a.V / 32 + 1; i += kThreads)
+        marks[i] = 0;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         T *grad = static_cast<T *>(a.grad) + row * a.V;
         if (!a.mask[row]) {
@@ -119,11 +160,11 @@ __global__ void __launch_bounds__(kThreads, 8) distill_small_kernel(const __grid
         }
         const RowSpan<T> s(static_cast<const T *>(a.logits) + row * a.V, a.V);
         // ---- the teacher's probabilities, and the student's logits of its tokens
+        if (tid == 0)
+            twice = 0, ends = 0;
+        __syncthreads();
         int v[kMine];
         float m[kMine], x[kMine];
-        if (tid == 0)
-            twice = 0;
-        __syncthreads();
         float most = -FLT_MAX;
 #pragma unroll
         for (int j = 0; j < kMine; ++j) {
@@ -136,30 +177,60 @@ __global__ void __launch_bounds__(kThreads, 8) distill_small_kernel(const __grid
                     v[j] = at;
                     m[j] = __fdiv_rn(top_value(a, row * a.K + k), a.temperature);
                     x[j] = to_float(s.row[at]);
-                    if ((atomicOr(&listed[at >> 5], 1u << (at & 31)) >> (at & 31)) & 1u)
-                        twice = 1;
                 }
                 idx[k] = v[j];
                 most = Most()(most, m[j]);
             }
         }
-        most = a.lse ? a.lse[row] : cta_reduce(most, warps, Most());
+        // its marks
+#pragma unroll
+        for (int j = 0; j < kMine; ++j)
+            if (v[j] >= 0) {
+                const int b = v[j] - s.head;
+                const bool end = v[j] < s.head || v[j] >= s.tail();
+                const int bit = v[j] < s.head ? v[j] : end ? 8 + v[j] - s.tail() : b & 31;
+                if ((atomicOr(end ? &ends : &marks[b >> 5], 1u << bit) >> bit) & 1u)
+                    twice = 1;
+            }
+        if (!a.lse) {
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1)
+                most = Most()(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
+            if (lane == 0)
+                of_most[warp] = most;
+        }
+        __syncthreads();
+        if (a.lse) {
+            most = a.lse[row];
+        } else {
+            most = of_most[0];
+            for (int w = 1; w < kWarps; ++w)
+                most = Most()(most, of_most[w]);
+        }
         float P = 0.0f, R = 0.0f;
 #pragma unroll
         for (int j = 0; j < kMine; ++j) {
             m[j] = v[j] >= 0 ? expf(m[j] - most) : 0.0f;
             P += m[j];
         }
-        P = cta_reduce(P, warps, Add());
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1)
+            P += __shfl_xor_sync(0xFFFFFFFFu, P, o);
+        if (lane == 0)
+            of_mass[warp] = P;
+        __syncthreads();
+        P = of_mass[0];
+        for (int w = 1; w < kWarps; ++w)
+            P += of_mass[w];
         if (a.lse) {
             R = fmaxf(1.0f - P, 0.0f);
         } else if (P != 0.0f) {
 #pragma unroll
             for (int j = 0; j < kMine; ++j)
-                m[j] = __fdiv_rn(m[j], P);
+                if (m[j] != 0.0f)
+                    m[j] = __fdiv_rn(m[j], P);
             P = P == P ? 1.0f : P;
         }
-        __syncthreads();
         if (twice) {  // a token listed more than once: its masses count together, in its first place
 #pragma unroll
             for (int j = 0; j < kMine; ++j)
@@ -183,70 +254,93 @@ __global__ void __launch_bounds__(kThreads, 8) distill_small_kernel(const __grid
                     }
             }
         }
-        float M, Z, r;
+        const int end = lane < 8 ? lane : s.tail() + lane - 8;  // warp 0: a value of the ends
+        const bool has_end = warp == 0 && lane < 16 && (lane < 8 ? end < s.head : end < a.V);
+        float M, Z;
         ExpSum rest;
         if (kSum) {
             // ---- the tokens that are not listed
-            auto value = [&](int i) {
-                return (listed[i >> 5] >> (i & 31)) & 1u ? neg_inf_f() : to_float(s.row[i]);
-            };
-            for (int i = tid; i < s.head; i += kThreads)
-                rest.add(value(i), c);
-            for (int i = s.tail() + tid; i < a.V; i += kThreads)
-                rest.add(value(i), c);
-            for (int i = tid; i < s.vecs; i += kThreads) {
-                float y[E];
-                widen<T>(s.vectors()[i], y);
-                const int at = s.head + i * E;
-                float top = -FLT_MAX;
+            Summed sum;
+            for (int i0 = tid; i0 < s.vecs; i0 += kFour * kThreads) {
+                constexpr uint32_t kPad = no_values<T>();
+                uint4 y[kFour];
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    y[e] = (listed[(at + e) >> 5] >> ((at + e) & 31)) & 1u ? neg_inf_f() : y[e];
-                    top = fmaxf(top, y[e]);
+                for (int q = 0; q < kFour; ++q) {
+                    const int i = i0 + q * kThreads;
+                    y[q] = i < s.vecs ? s.vectors()[i] : make_uint4(kPad, kPad, kPad, kPad);
                 }
-                rest.raise(top, c);
 #pragma unroll
-                for (int e = 0; e < E; ++e)
-                    rest.z += ex2_mufu((y[e] - rest.m) * c);
+                for (int q = 0; q < kFour; ++q) {
+                    const int i = i0 + q * kThreads;
+                    const uint32_t bits = i >= s.vecs ? 0u
+                                          : E == 8    ? listed[i]
+                                                      : (listed[i >> 1] >> (4 * (i & 1))) & 15u;
+                    if (bits)
+                        leave_out<T>(y[q], bits);
+                }
+                sum.add<T, kFour>(y, c);
             }
-            rest = warp_sum(rest, c);
-            __syncthreads();
-            if ((tid & 31) == 0)
-                sums[tid >> 5] = rest;
-            __syncthreads();
-            rest = sums[0];
-            for (int i = 1; i < kThreads / 32; ++i)
-                rest.merge(sums[i], c);
-            // ---- all tokens: the listed ones among them
-            M = rest.m;
-#pragma unroll
-            for (int j = 0; j < kMine; ++j)
-                M = fmaxf(M, x[j]);
-            M = cta_reduce(M, warps, Most());
-            Z = 0.0f;
+            sum.settle(c);
+            if (has_end && !((ends >> lane) & 1u))
+                sum.z.add(to_float(s.row[end]), c);
+            __syncwarp();
+            // ---- and the listed ones: each warp's, relative to their own maximum
+            ExpSum of_x;
+            float A = 0.0f, share = 0.0f;
 #pragma unroll
             for (int j = 0; j < kMine; ++j)
                 if (v[j] >= 0)
-                    Z += ex2_mufu((x[j] - M) * c);
-            Z = cta_reduce(Z, warps, Add());
-            Z += rest.z * ex2_mufu((rest.m - M) * c);
-            if (!(Z > 0.0f && Z <= FLT_MAX) || !finite_f(M))
-                Z = nan_f();
-            const float log_z = logf(Z);
-            float loss = 0.0f;
+                    of_x.m = Most()(of_x.m, x[j]);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1)
+                of_x.m = Most()(of_x.m, __shfl_xor_sync(0xFFFFFFFFu, of_x.m, o));
 #pragma unroll
             for (int j = 0; j < kMine; ++j)
-                if (v[j] >= 0 && m[j] != 0.0f)
-                    loss += m[j] * (logf(m[j]) - ((x[j] - M) * a.inv_t - log_z));
-            loss = cta_reduce(loss, warps, Add());
+                if (v[j] >= 0) {
+                    of_x.z += ex2_mufu((x[j] - of_x.m) * c);
+                    if (m[j] != 0.0f)
+                        A += m[j] * (logf(m[j]) - (x[j] - of_x.m) * a.inv_t);
+                    share += m[j];
+                }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+                of_x.z += __shfl_xor_sync(0xFFFFFFFFu, of_x.z, o);
+                A += __shfl_xor_sync(0xFFFFFFFFu, A, o);
+                share += __shfl_xor_sync(0xFFFFFFFFu, share, o);
+            }
+            rest = warp_sum(sum.z, c);
+            if (lane == 0) {
+                of_rest[warp] = rest;
+                of_listed[warp] = of_x;
+                of_loss[warp] = A;
+                of_share[warp] = share;
+            }
+            __syncthreads();
+            rest = of_rest[0];
+            M = of_listed[0].m;
+            for (int w = 1; w < kWarps; ++w) {
+                rest.merge(of_rest[w], c);
+                M = Most()(M, of_listed[w].m);
+            }
+            M = Most()(M, rest.m);
+            Z = rest.z * ex2_mufu((rest.m - M) * c);
+            for (int w = 0; w < kWarps; ++w)
+                Z += of_listed[w].z * ex2_mufu((of_listed[w].m - M) * c);
+            if (!(Z > 0.0f && Z <= FLT_MAX) || !finite_f(M))
+                Z = nan_f();
             if (rest.z == 0.0f)
                 R = 0.0f;
-            if (R > 0.0f)
-                loss += R * (logf(R) - ((rest.m - M) * a.inv_t + logf(rest.z) - log_z));
-            if (Z != Z)
-                loss = Z;
             if (tid == 0) {
-                a.loss[row] = loss;
+                const float log_z = logf(Z);
+                float loss = 0.0f;
+                for (int w = 0; w < kWarps; ++w) {
+                    loss += of_loss[w];
+                    if (of_share[w] != 0.0f)
+                        loss += of_share[w] * ((M - of_listed[w].m) * a.inv_t + log_z);
+                }
+                if (R > 0.0f)
+                    loss += R * (logf(R) - ((rest.m - M) * a.inv_t + logf(rest.z) - log_z));
+                a.loss[row] = Z == Z ? loss : Z;
                 if (a.stats_out)
                     a.stats_out[row] = make_float4(M, Z, rest.m, rest.z);
             }
@@ -261,22 +355,23 @@ __global__ void __launch_bounds__(kThreads, 8) distill_small_kernel(const __grid
         }
         if (kGrad) {
             const float scale = a.grad_loss[row] * a.inv_t;
-            r = rest.z * ex2_mufu((rest.m - M) * c) / Z;
-            // of s_v relative to the rest's maximum
-            const float f = rest.z == 0.0f ? (Z == Z ? 0.0f : Z)
-                                           : scale * (r * (P + R) - R) / rest.z;
-            auto of = [&](float y) { return ex2_mufu((y - rest.m) * c) * f; };
-            for (int i = tid; i < s.head; i += kThreads)
-                grad[i] = from_float<T>(of(to_float(s.row[i])));
-            for (int i = s.tail() + tid; i < a.V; i += kThreads)
-                grad[i] = from_float<T>(of(to_float(s.row[i])));
-            for (int i = tid; i < s.vecs; i += kThreads) {
-                float y[E];
-                widen<T>(s.vectors()[i], y);
+            const float r = rest.z * ex2_mufu((rest.m - M) * c) / Z;
+            // of s_v relative to the reference of the others
+            float f = rest.z == 0.0f ? (Z == Z ? 0.0f : Z) : scale * (r * (P + R) - R) / rest.z;
+            if (has_end)
+                grad[end] = from_float<T>(ex2_mufu((to_float(s.row[end]) - rest.m) * c) * f);
+            const RowTerms terms(rest.m, c, f);
+            uint4 *out = reinterpret_cast<uint4 *>(grad + s.head);
+            for (int i0 = tid; i0 < s.vecs; i0 += kFour * kThreads) {
+                uint4 y[kFour];
 #pragma unroll
-                for (int e = 0; e < E; ++e)
-                    y[e] = of(y[e]);
-                reinterpret_cast<uint4 *>(grad + s.head)[i] = narrow<T>(y);
+                for (int q = 0; q < kFour; ++q)
+                    if (i0 + q * kThreads < s.vecs)
+                        y[q] = s.vectors()[i0 + q * kThreads];
+#pragma unroll
+                for (int q = 0; q < kFour; ++q)
+                    if (i0 + q * kThreads < s.vecs)
+                        __stcs(out + i0 + q * kThreads, terms.template of<T>(y[q]));
             }
             __syncthreads();
 #pragma unroll
@@ -284,11 +379,13 @@ __global__ void __launch_bounds__(kThreads, 8) distill_small_kernel(const __grid
                 if (v[j] >= 0)
                     grad[v[j]] = from_float<T>(
                         scale * (ex2_mufu((x[j] - M) * c) / Z * (P + R) - m[j]));
+        } else {
+            __syncthreads();
         }
-        __syncthreads();
+        // (the marks of a token's other places go with its first)
         for (int k = tid; k < a.K; k += kThreads)
-            if (idx[k] >= 0)
-                listed[idx[k] >> 5] = 0;
+            if (idx[k] >= s.head && idx[k] < s.tail())
+                marks[(idx[k] - s.head) >> 5] = 0;
     }
 }
 
@@ -310,7 +407,7 @@ constexpr int kTeachers = 256;
 constexpr int kRingThreads = kMath + kTeachers + 64;
 constexpr int kChunk = 32768, kChunkVecs = kChunk / 16, kPer = kChunkVecs / kMath;
 constexpr int kMostListed = 1 << 17;  // tokens of a CTA's share of a row: their bits take 16 KB
-constexpr int kMarks = kMostListed / 8 + 16;
+constexpr int kMarks = kMostListed / 8 + 32;
 constexpr int kZeros = 2048;
 constexpr int kMaxRanks = 8;
 enum { kBarMath = 1, kBarTeach };
@@ -419,14 +516,16 @@ struct RingShared {
     uint32_t ends;
 };
 
-// Shared memory.  The sum alone holds no row back: it does with a stage less, and marks the row to
-// come while the row before is still under way (with one set of marks, 1234 rows of 50021 logits in
-// fp32 take 64 us).
+// Shared memory.  With two sets of marks the row to come is marked while the row before is still under
+// way (with one, 1234 rows of 50021 logits in fp32 took 64 us, not 53).  The sum alone holds no row
+// back and has room for them with a stage less; beside the gradient a set is half as long, and there
+// are two where a share fits that.
 template <bool kSum, bool kGrad>
 struct RingLayout {
-    static constexpr int sets = kSum && !kGrad ? 2 : 1;
-    static constexpr int stages = sets == 2 ? 5 : 6;
-    static constexpr int listed = stages * kChunk, zeros = listed + sets * kMarks;
+    static constexpr bool wide = kSum && !kGrad;
+    static constexpr int stages = wide ? 5 : 6;
+    static constexpr int set = wide ? kMarks : kMarks / 2;  // bytes of one of two sets
+    static constexpr int listed = stages * kChunk, zeros = listed + (wide ? 2 : 1) * kMarks;
     static constexpr int dup = zeros + kZeros, shared = dup + kMaxTop * 8;
     static constexpr int bytes = shared + (int)sizeof(RingShared);
     static_assert(bytes <= 227 * 1024 && shared % 16 == 0 && zeros % 16 == 0, "shared memory");
@@ -460,24 +559,6 @@ __device__ __forceinline__ void load_chunk(uint4 (&x)[kPer], const uint4 *buf, i
     }
 }
 
-// -inf in the place of the values whose bits are set.
-template <typename T>
-__device__ __forceinline__ void leave_out(uint4 &r, uint32_t bits)
-{
-    constexpr uint32_t kPad = no_values<T>();
-    uint32_t *w = reinterpret_cast<uint32_t *>(&r);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if constexpr (sizeof(T) == 4) {
-            w[i] = (bits >> i) & 1u ? kPad : w[i];
-        } else {
-            const uint32_t keep = ((bits >> (2 * i)) & 1u ? 0u : 0xFFFFu) |
-                                  ((bits >> (2 * i + 1)) & 1u ? 0u : 0xFFFF0000u);
-            w[i] = (w[i] & keep) | (kPad & ~keep);
-        }
-    }
-}
-
 // Sum (or maximum) over the teachers' warps, the same bits in every thread.
 template <typename F>
 __device__ __forceinline__ float teach_reduce(float x, float *of_warp, F f)
@@ -497,12 +578,11 @@ __device__ __forceinline__ float teach_reduce(float x, float *of_warp, F f)
 
 template <typename T, bool kSum, bool kGrad>
 __global__ void __launch_bounds__(kRingThreads, 1)
-    distill_ring_kernel(const __grid_constant__ DistillArgs a, int ranks)
+    distill_ring_kernel(const __grid_constant__ DistillArgs a, int ranks, int two)
 {
     constexpr int E = 16 / sizeof(T);
     using Layout = RingLayout<kSum, kGrad>;
     constexpr int kStages = Layout::stages;
-    constexpr bool kTwo = Layout::sets == 2;
     extern __shared__ __align__(128) uint8_t smem[];
     // a bit for each value of the share's vectors; with two sets, by the row's parity
     uint8_t *const marks = smem + Layout::listed;
@@ -523,7 +603,7 @@ __global__ void __launch_bounds__(kRingThreads, 1)
         }
         fence_mbar_init();
     }
-    for (int i = tid; i < (Layout::sets * kMarks + kZeros) / 4; i += kRingThreads)
+    for (int i = tid; i < (Layout::zeros - Layout::listed + kZeros) / 4; i += kRingThreads)
         reinterpret_cast<uint32_t *>(marks)[i] = 0;
     fence_async_smem();
     __syncthreads();
@@ -559,8 +639,8 @@ __global__ void __launch_bounds__(kRingThreads, 1)
             ExpSum rest = of.rest;
             if constexpr (kSum) {
                 // ---- the tokens that are not listed
-                const uint8_t *const listed = marks + (kTwo ? par * kMarks : 0);
-                const uint32_t *const groups = sm.groups[kTwo ? par : 0];
+                const uint8_t *const listed = marks + (two ? par * Layout::set : 0);
+                const uint32_t *const groups = sm.groups[two ? par : 0];
                 Summed sum;
                 for (int j = 0; j < chunks; ++j) {
                     const uint32_t k = kb + j, st = k % kStages;
@@ -643,17 +723,12 @@ __global__ void __launch_bounds__(kRingThreads, 1)
                 if (tid == 0)
                     sm.fix[par] = make_float4(M, Z, of.P + R, scale);
                 // of s_v relative to the reference of the others
-                float f = rest.z == 0.0f ? (Z == Z ? 0.0f : Z) : scale * (r * (of.P + R) - R) / rest.z;
+                const float f = rest.z == 0.0f ? (Z == Z ? 0.0f : Z) : scale * (r * (of.P + R) - R) / rest.z;
                 T *grad = static_cast<T *>(a.grad) + of.row * a.V;
                 if (has_end)
                     grad[end] = from_float<T>(ex2_mufu((to_float(sh.r.row[end]) - rest.m) * c) * f);
                 uint4 *out = reinterpret_cast<uint4 *>(grad + sh.r.head) + sh.v0;
-                const float ref = rest.m * c;
-                const bool far = !(fabsf(ref) < kFar);
-                if (!far)
-                    f *= ex2_mufu(-fmaf(rest.m, c, -ref));
-                const uint64_t f2f = f2(f, f), c2 = f2(c, c);
-                const uint64_t n2 = far ? f2(-rest.m, -rest.m) : f2(-ref, -ref);
+                const RowTerms terms(rest.m, c, f);
                 for (int q = 0; q < chunks; ++q) {
                     // the retained chunks, then those that came again
                     const int j = q < chunks - again ? q + again : q - (chunks - again);
@@ -670,17 +745,9 @@ __global__ void __launch_bounds__(kRingThreads, 1)
 #pragma unroll
                     for (int p = 0; p < kPer; ++p) {
                         const int v = tid + p * kMath;
-                        float y[E];
-                        widen<T>(x[p], y);
-#pragma unroll
-                        for (int e = 0; e < E; e += 2) {
-                            const uint64_t y2 = f2(y[e], y[e + 1]);
-                            float t0, t1;
-                            un2(far ? mul2(add2(y2, n2), c2) : fma2(y2, c2, n2), t0, t1);
-                            un2(mul2(f2(ex2_mufu(t0), ex2_mufu(t1)), f2f), y[e], y[e + 1]);
-                        }
+                        const uint4 y = terms.template of<T>(x[p]);
                         if (v < n)
-                            __stcs(out + j * kChunkVecs + v, narrow<T>(y));
+                            __stcs(out + j * kChunkVecs + v, y);
                     }
                 }
                 __syncwarp();
@@ -726,8 +793,8 @@ __global__ void __launch_bounds__(kRingThreads, 1)
         int old[kMine];  // of the row before: its listed tokens, and what their gradients need
         float old_p[kMine], old_x[kMine];
         int64_t old_row = -1;
-        [[maybe_unused]] int older[kMine];  // and of the one before it
-        [[maybe_unused]] int64_t older_row = -1;
+        int older[kMine];  // and of the one before it
+        int64_t older_row = -1;
 #pragma unroll
         for (int j = 0; j < kMine; ++j)
             old[j] = older[j] = -1, old_p[j] = old_x[j] = 0.0f;
@@ -780,12 +847,12 @@ __global__ void __launch_bounds__(kRingThreads, 1)
                     x[j] = v[j] >= 0 ? to_float(raw[j]) : neg_inf_f();
             }
             // ---- the marks: those of the row that had this set go, this one's come
-            if (kTwo && i > 1)
+            if (kSum && two && i > 1)
                 wait(&sm.swept[par], ((i - 2) >> 1) & 1);
-            if (kSum && kGrad && i > 0)
+            if (kSum && !two && i > 0)
                 wait(&sm.swept[par ^ 1], ((i - 1) >> 1) & 1);
-            uint8_t *const listed = marks + (kTwo ? par * kMarks : 0);
-            uint32_t *const groups = sm.groups[kTwo ? par : 0];
+            uint8_t *const listed = marks + (two ? par * Layout::set : 0);
+            uint32_t *const groups = sm.groups[two ? par : 0];
             if (named_sync_or(kBarTeach, kTeachers, dead))
                 break;
             auto mark = [&](const RowShare<T> &sh, int at, bool set) -> bool {  // whether it was set before
@@ -810,12 +877,12 @@ __global__ void __launch_bounds__(kRingThreads, 1)
                 atomicAnd(word, ~(1u << bit));
                 return false;
             };
-            if ((kTwo ? older_row : old_row) >= 0) {
-                const RowShare<T> sh(a.logits, kTwo ? older_row : old_row, a.V, rank, ranks);
+            if ((two ? older_row : old_row) >= 0) {
+                const RowShare<T> sh(a.logits, two ? older_row : old_row, a.V, rank, ranks);
 #pragma unroll
                 for (int j = 0; j < kMine; ++j)
-                    if ((kTwo ? older[j] : old[j]) >= 0)
-                        mark(sh, kTwo ? older[j] : old[j], false);
+                    if ((two ? older[j] : old[j]) >= 0)
+                        mark(sh, two ? older[j] : old[j], false);
             }
             if (t == 0) {
                 sm.ends = 0;
@@ -1021,13 +1088,14 @@ __global__ void __launch_bounds__(kRingThreads, 1)
 }
 
 // CTAs that share a row: one where there are rows for all SMs; more where rows are few, as long as
-// shares have two chunks, or where a share's bits would not fit.
+// shares have a chunk (a step of one row of 126464 tokens in bf16: 11 us, with two chunks 13), or where
+// a share's bits would not fit.
 int row_ranks(int64_t rows, int V, int es)
 {
     int ranks = 1;
     while (ranks < kMaxRanks &&
            (V / ranks > kMostListed - 64 ||
-            (rows * ranks * 2 <= sm_count() && (int64_t)V * es / ranks >= 4 * kChunk)))
+            (rows * ranks * 2 <= sm_count() && (int64_t)V * es / ranks >= 2 * kChunk)))
         ranks *= 2;
     return ranks;
 }
@@ -1059,11 +1127,11 @@ template <typename T, bool kSum, bool kGrad>
 cudaError_t launch_kind(const DistillArgs &a, cudaStream_t s)
 {
     constexpr int es = sizeof(T);
-    if ((int64_t)a.V * es <= kSmallRow) {
+    if ((int64_t)a.V * es <= (a.rows > sm_count() ? kManyRow : kSmallRow)) {
         auto *kern = distill_small_kernel<T, kSum, kGrad>;
         const int64_t most = (int64_t)sm_count() * 16;
         return launch(kern, dim3((unsigned)(a.rows < most ? a.rows : most)), dim3(kThreads),
-                      (size_t)((a.V + 31) / 32) * 4, s, true, a);
+                      (size_t)(a.V / 32 + 1) * 4, s, true, a);
     }
     auto *kern = distill_ring_kernel<T, kSum, kGrad>;
     constexpr int kSmem = RingLayout<kSum, kGrad>::bytes;
@@ -1097,7 +1165,8 @@ cudaError_t launch_kind(const DistillArgs &a, cudaStream_t s)
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = plain_launches ? 1 : 2;
-    return cudaLaunchKernelEx(&cfg, kern, DistillArgs(a), ranks);
+    const int two = RingLayout<kSum, kGrad>::wide || a.V / ranks <= kMostListed / 2 - 64;
+    return cudaLaunchKernelEx(&cfg, kern, DistillArgs(a), ranks, two);
 }
 
 template <typename T>

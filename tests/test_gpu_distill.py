@@ -312,6 +312,18 @@ def test_many_rows(fd, V):
         assert bool(((got.cpu().double() - exact).abs() <= tol).all())
 
 
+@pytest.mark.parametrize("dtype,rest,B,V", [(BF, True, 36, 20011), (HF, False, 12, 32767), (FP, True, 41, 16001),
+                                            (BF, False, 16, 70001), (FP, True, 25, 16411)])
+def test_many_long_rows(fd, dtype, rest, B, V):
+    """Several rows to a CTA, with one set of marks and with two, and the form of a CTA to each of many."""
+    kw, weights = inputs(B, 13, V, 33, dtype, 21 + B, rest, masked=0.9)
+    loss, grad = check(fd, kw, weights)
+    into = kw["logits"].clone()
+    again = fd.fdllm_distill_step(into, kw["mask"], kw["top_index"], kw["top_logits"], weights, kw["teacher_lse"],
+                                  kw["temperature"], out_grad=into)
+    assert torch.equal(again[0], loss) and torch.equal(into, grad)
+
+
 def test_refusals(fd):
     kw, weights = inputs(2, 3, 64, 4, BF, 19, True)
     loss = lambda **more: fd.fdllm_distill_loss(**{**kw, **more})
