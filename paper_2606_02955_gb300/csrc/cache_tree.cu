@@ -16,16 +16,17 @@ struct MaskArgs {
     int32_t *depth;          // [B, M] or null
 };
 
-// One CTA a sequence, a warp to a node's row of bits, lane l its word l.  Each turn a node's row
-// takes in the row of the node that its walk up has reached, and the walk doubles its length: as
-// many turns as the depth has bits.
+// One CTA a sequence, a thread to a word of a node's row of bits.  Each turn a node's row takes in the
+// row of the node that its walk up has reached, and the walk doubles its length: as many turns as
+// the depth has bits.  Bound by the turns' latencies: 32
+// trees of 48 nodes 2 to 3 us, two of 255 3 to 5 (a warp to a row 8 to 15), by the depth.
 __global__ void __launch_bounds__(1024) tree_mask_kernel(const __grid_constant__ MaskArgs a)
 {
     extern __shared__ uint32_t rows[];  // [M][words]
     __shared__ short up[2][kMaxNodes], dist[2][kMaxNodes];
     pdl_wait();
-    const int b = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int warps = blockDim.x >> 5;
+    const int b = blockIdx.x;
+    const int log = 32 - __clz(a.words - 1), all = 1 << log;  // words of a row, those not there too
     const int n = a.lens ? min(max(a.lens[b], 0), a.M) : a.M;
     for (int i = threadIdx.x; i < a.M; i += blockDim.x) {
         const int p = i > 0 && i < n ? a.parents[(int64_t)b * a.M + i] : -1;
@@ -33,17 +34,19 @@ __global__ void __launch_bounds__(1024) tree_mask_kernel(const __grid_constant__
         up[0][i] = hung ? p : -1;
         dist[0][i] = hung ? 1 : 0;
     }
-    for (int i = warp; i < a.M; i += warps)
-        if (lane < a.words)
-            rows[i * a.words + lane] = i < n && (i >> 5) == lane ? 1u << (i & 31) : 0u;
+    for (int x = threadIdx.x; x < a.M << log; x += blockDim.x) {
+        const int i = x >> log, w = x & (all - 1);
+        if (w < a.words)
+            rows[i * a.words + w] = i < n && (i >> 5) == w ? 1u << (i & 31) : 0u;
+    }
     int from = 0, more = 1;
     while (more) {
         __syncthreads();
         // (a row may be read while it takes bits in: they are ancestors' all the same)
-        for (int i = warp; i < n; i += warps) {
-            const int p = up[from][i];
-            if (p >= 0 && lane < a.words)
-                rows[i * a.words + lane] |= *(volatile uint32_t *)&rows[p * a.words + lane];
+        for (int x = threadIdx.x; x < n << log; x += blockDim.x) {
+            const int i = x >> log, w = x & (all - 1), p = up[from][i];
+            if (p >= 0 && w < a.words)
+                rows[i * a.words + w] |= *(volatile uint32_t *)&rows[p * a.words + w];
         }
         int on = 0;
         for (int i = threadIdx.x; i < n; i += blockDim.x) {
@@ -56,12 +59,11 @@ __global__ void __launch_bounds__(1024) tree_mask_kernel(const __grid_constant__
         more = __syncthreads_or(on);
     }
     __syncthreads();
-    for (int i = warp; i < a.M; i += warps) {
-        if (lane < a.words)
-            a.mask[((int64_t)b * a.M + i) * a.words + lane] = rows[i * a.words + lane];
-        if (a.depth && lane == 0)
+    for (int x = threadIdx.x; x < a.M * a.words; x += blockDim.x)
+        a.mask[(int64_t)b * a.M * a.words + x] = rows[x];
+    if (a.depth)
+        for (int i = threadIdx.x; i < a.M; i += blockDim.x)
             a.depth[(int64_t)b * a.M + i] = i < n ? dist[from][i] : -1;
-    }
 }
 
 }  // namespace
@@ -83,7 +85,7 @@ fdllm_status fdllm_tree_mask(const int32_t *parents, const int32_t *lens, int B,
                                         kMaxNodes * (kMaxNodes / 32) * 4);
         }) != cudaSuccess)
         return FDLLM_ERR_CUDA;
-    const int threads = M <= 32 ? 128 : M <= 256 ? 512 : 1024;
+    const int threads = M <= 32 ? 128 : M <= 128 ? 512 : 1024;
     const cudaError_t e = launch(tree_mask_kernel, dim3(B), dim3(threads), (size_t)M * a.words * 4,
                                  static_cast<cudaStream_t>(stream), true, a);
     return e == cudaSuccess ? FDLLM_OK : FDLLM_ERR_CUDA;

@@ -9,6 +9,17 @@
 //   is, the next token is drawn from p_c without the children's tokens.
 // A token is drawn from weights r(v) as argmax r(v) / E(v), E given (exponential variables): r needs
 // no norm, and no sum over the vocabulary has to be exact to the last token's share.
+//
+// Two kernels.  The first takes every row's maximum and sum (or its largest value) in one pass, in
+// parts that no CTA waits for; the second joins the parts, walks the nodes and draws the next token,
+// reading again only the one or two rows it is drawn from.  A kernel that walked as sums came and left out
+// the rows behind a rejection took 72 us and more where these take 57 (64 chains of nine): decisions
+// come 10 us and more behind the copies, and copies under way are not taken back.
+//
+// Bound by HBM where rows are many and long: 64 chains of up to nine rows of 126464 bf16 values and the
+// draft's rows, 57 us: 45 of the first kernel (243 MB, 5.4 TB/s, half of the issue slots taken), the
+// rest of the draw (63 MB), which the first does not hide.  By two launches and the draw's chain (parts, decisions, weights, the
+// cluster's best) where they are few: a chain of five rows of 32000 values 9 us.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
@@ -22,12 +33,14 @@ namespace cg = cooperative_groups;
 constexpr int kMaxNodes = FDLLM_MAX_L;
 constexpr int kMathWarps = 16;
 constexpr int kMath = 32 * kMathWarps;
-constexpr int kChunk = 65536;  // bytes of a stage
+constexpr int kChunk = 65536;  // bytes of a stage (six stages of half as many: 61 us for 59)
 constexpr int kStages = 3;
 constexpr int kChunkVecs = kChunk / 16;
-constexpr int kSmallRow = 32768;  // rows up to this many bytes: a few warps each, without the ring
+// Rows up to this many bytes: a few warps each, without the ring, whose beginning and end cost more than
+// their copies hide (14 trees of 53 rows of 23 KB, the whole call: 14.8 us, with the ring 24.8).
+constexpr int kSmallRow = 32768;
 constexpr int kSmallVecs = 8;     // vectors of a lane in such a row, about
-constexpr int kDraw = 512;       // threads of a CTA of the walk and the draw
+constexpr int kDraw = 512;       // threads of a CTA of the walk and the draw (256: 69 us for 58)
 constexpr int kMaxRanks = 8;     // CTAs of a cluster of them
 
 struct VerifyArgs {
@@ -209,7 +222,9 @@ __global__ void __launch_bounds__(256) verify_small_kernel(const __grid_constant
 }
 
 // ---- Longer rows: pieces of them stream through a ring of shared memory, filled by bulk copies.
-// Every warp leaves its own part of a piece: no warp waits for another but through the ring.
+// Every warp leaves its own part of a piece: no warp waits for another but through the ring.  Pieces go
+// to CTAs in turn; ranges of equal bytes, one to a CTA, end together, and took 64 us for 57: the
+// CTAs that end early leave their SMs to the draw's, which bring the noise in meanwhile.
 struct Stage {
     uint32_t n;     // vectors, 0: no more
     int32_t at;     // index in the row of their first value
@@ -811,7 +826,8 @@ __global__ void __launch_bounds__(kDraw, 2) verify_draw_kernel(const __grid_cons
         a.out_n[b] = dead ? FDLLM_ROW_DEVICE_ERROR : failed ? FDLLM_ROW_NONFINITE : taken;
 }
 
-// CTAs that share a sequence's draw: as many as fill the GPU once, where slices stay long enough.
+// CTAs that share a sequence's draw: as many as fill the GPU once (two to an SM), where a slice keeps
+// four values or so of a thread; and as many as a slice's bits of taken tokens need.
 int draw_ranks(const VerifyArgs &a)
 {
     if (a.greedy)
@@ -869,8 +885,8 @@ cudaError_t launch_verify(const VerifyArgs &a, cudaStream_t s)
     return cudaLaunchKernelEx(&cfg, verify_draw_kernel<T>, VerifyArgs(a));
 }
 
-// How rows are cut: whole, or in pieces of whole chunks so that every SM has some, and no piece is
-// longer than four chunks.
+// How rows are cut: whole, or in pieces of whole chunks so that every SM has two, and no piece is
+// longer than four chunks (where rows are many, pieces of one, two and four are alike within 2 %).
 void cut_rows(int64_t rows, int V, int es, int &pieces, int &piece_vecs, int &per)
 {
     if ((int64_t)V * es <= kSmallRow) {
