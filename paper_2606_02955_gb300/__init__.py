@@ -976,8 +976,8 @@ def fdllm_verify_draft(target: torch.Tensor, tokens: torch.Tensor, parents=None,
     """Take drafted tokens by the target's probabilities and given random numbers.
 
     ``target`` [B, M, V] bf16/fp16/fp32, row j the target's logits after node j (node 0 the last
-    committed token; rows may lie anywhere, their values contiguous); ``tokens`` int32 [B, M] the nodes' tokens; ``parents`` int32 [B, M] a tree
-    (None: a chain); ``lens`` int32 [B] the counts of nodes; ``draft`` [B, M - 1, V] the logits a
+    committed token; rows may lie anywhere, their values contiguous); ``tokens`` int32 [B, M] the
+    nodes' tokens; ``parents`` int32 [B, M] a tree (None: a chain); ``lens`` int32 [B] the counts of nodes; ``draft`` [B, M - 1, V] the logits a
     chain was drawn from at ``draft_temperature`` (None: ``temperature``), or None where the tokens
     were chosen; ``uniform`` fp32 [B, M] in [0, 1) and ``noise`` fp32 [B, V] exponential variables
     (None at temperature 0, which is greedy).  Returns (tokens int32 [B, M]: the taken ones, then
