@@ -1100,29 +1100,6 @@ int row_ranks(int64_t rows, int V, int es)
     return ranks;
 }
 
-// Clusters of `ranks` CTAs that the GPU holds at once.
-template <typename K>
-int resident(K kern, int smem, int ranks)
-{
-    if (ranks == 1)
-        return sm_count();
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(sm_count() / ranks * ranks));
-    cfg.blockDim = dim3(kRingThreads);
-    cfg.dynamicSmemBytes = smem;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim = {(unsigned)ranks, 1, 1};
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess || n < 1) {
-        cudaGetLastError();
-        n = sm_count() / ranks;
-    }
-    return n;
-}
-
 template <typename T, bool kSum, bool kGrad>
 cudaError_t launch_kind(const DistillArgs &a, cudaStream_t s)
 {
@@ -1142,7 +1119,7 @@ cudaError_t launch_kind(const DistillArgs &a, cudaStream_t s)
         int dev = 0;
         if (r == cudaSuccess && cudaGetDevice(&dev) == cudaSuccess)
             for (int i = 0; i < 4; ++i)
-                held[dev][i] = resident(kern, kSmem, 1 << i);
+                held[dev][i] = clusters_held(kern, kRingThreads, kSmem, 1 << i);
         return r;
     });
     if (e != cudaSuccess)

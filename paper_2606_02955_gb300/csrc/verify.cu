@@ -14,12 +14,15 @@
 // parts that no CTA waits for; the second joins the parts, walks the nodes and draws the next token,
 // reading again only the one or two rows it is drawn from.  A kernel that walked as sums came and left out
 // the rows behind a rejection took 72 us and more where these take 57 (64 chains of nine): decisions
-// come 10 us and more behind the copies, and copies under way are not taken back.
+// come 10 us and more behind the copies, and copies under way are not taken back.  Trees are another
+// matter where few of their many rows are on the path: there the second kernel comes alone, and its
+// clusters sum the rows as their walk comes to them.
 //
 // Bound by HBM where rows are many and long: 64 chains of up to nine rows of 126464 bf16 values and the
 // draft's rows, 57 us: 45 of the first kernel (243 MB, 5.4 TB/s, half of the issue slots taken), the
-// rest of the draw (63 MB), which the first does not hide.  By two launches and the draw's chain (parts, decisions, weights, the
-// cluster's best) where they are few: a chain of five rows of 32000 values 9 us.
+// rest of the draw (63 MB), which the first does not hide.  A walk by latencies, about 3 us a turn (8
+// trees of 48 nodes of 126464 values 14.6 us in all).  By two launches and the draw's chain (parts,
+// decisions, weights, the cluster's best) where they are few: a chain of five rows of 32000 values 9 us.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
@@ -61,6 +64,7 @@ struct VerifyArgs {
     UnitPartial *parts;       // [B, M] of the target's rows, [B, M - 1] of the draft's; each `per` long
     int per;                  // parts of a row
     int pieces, piece_vecs;   // pieces of a row, vectors of one
+    int turn, turn_most;      // rows of a turn of the walk at first, and at most
     uint32_t *status;         // sticky: a bounded wait gave up
 };
 
@@ -564,11 +568,138 @@ __device__ __forceinline__ int decide(const VerifyArgs &a, const Nodes &s, int c
     return kNone;
 }
 
+// ---- Trees of many nodes: the rows on the path alone are read, each by the whole cluster.
+constexpr int kTurn = 8;  // rows of a turn at most
+// Rows are read along the way where all of them are this many bytes: long ones (beyond kSmallRow), short
+// ones.  In bf16: 8 trees of 48 nodes of 126464 values 14.6 us (all rows first: 34.5), 16 of 60 of 32000
+// 13.5 (26.4), one of 48 of 126464 (12 MB) 11.2 (18.2), 64 of 40 of 11500 20 (30); but 8 of 16 of 32000 (8 MB) 13
+// (12), 14 of 53 of 11500 (17 MB) 16.8 (15.2).  Where paths are long the turns add up: 8 trees that are
+// chains of 48, every node taken, are 52 us (22), with two rows a turn throughout more.
+constexpr int64_t kWalkLong = 12000000, kWalkShort = 40000000;
+constexpr int kWalkShare = 8192;     // bytes of a row that a CTA is worth
+constexpr int kTurnBytes = 1 << 16;  // of a CTA's share of a turn's rows, and twice that where it went well
+
+struct WalkShared {
+    int4 part[kDraw / 32];                // of a warp's share of its row
+    int4 slot[2][kTurn][kMaxRanks];       // of a CTA's, by the turn's parity
+};
+
+// The first child of node c, -1: none.  By a warp.
+__device__ __forceinline__ int first_child(const Nodes &s, int c, int n)
+{
+    const int lane = threadIdx.x & 31;
+    for (int j0 = c + 1; j0 < n; j0 += 32) {
+        const uint32_t kids = __ballot_sync(0xFFFFFFFFu, j0 + lane < n && s.parent[j0 + lane] == c);
+        if (kids)
+            return j0 + __ffs(kids) - 1;
+    }
+    return -1;
+}
+
+// The walk by turns: the row of the node that it has come to and, on the way to a drafter's best guess,
+// those of its first child, that one's first child and so on, summed at once by warps of every CTA.
+// Where it went all the way down, the next turn takes twice as many.  A turn waits for its rows and for the
+// other CTAs' sums of them; nothing of a row is kept, the draw finds the last one in the L2.
+template <typename T, bool kGreedy>
+__device__ __forceinline__ void walk(const VerifyArgs &a, const Nodes &s, WalkShared &sm, int b, int n,
+                                     const cg::cluster_group &cluster, int &taken, int &failed)
+{
+    constexpr int E = 16 / sizeof(T), kWarps = kDraw / 32, kEight = 8;
+    const int ranks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    int at = 0, len = 0, most = a.turn;
+    for (uint32_t turn = 0;; ++turn) {
+        int node[kTurn], rows = 1, mine = at;
+        node[0] = at;
+#pragma unroll
+        for (int g = 1; g < kTurn; ++g) {
+            node[g] = g < most && node[g - 1] >= 0 ? first_child(s, node[g - 1], n) : -1;
+            rows += node[g] >= 0;
+        }
+        const int g = warp % rows;
+#pragma unroll
+        for (int i = 1; i < kTurn; ++i)
+            mine = g == i ? node[i] : mine;
+        const RowSpan<T> r(reinterpret_cast<const T *>(row_at<T>(a, b, mine, false).p), a.V);
+        const int per = (r.vecs + ranks - 1) / ranks, lo = min(r.vecs, rank * per), hi = min(r.vecs, lo + per);
+        const int wide = 32 * ((kWarps - g + rows - 1) / rows);  // threads of the row
+        Share<T, kGreedy> share;
+        for (int v = lo + (warp / rows) * 32 + lane; v < hi; v += kEight * wide) {
+            constexpr uint32_t kPad = no_values<T>();
+            uint4 x[kEight];
+            int i[kEight];
+#pragma unroll
+            for (int q = 0; q < kEight; ++q) {
+                const int w = v + q * wide;
+                x[q] = w < hi ? r.vectors()[w] : make_uint4(kPad, kPad, kPad, kPad);
+                i[q] = r.head + w * E;
+            }
+            share.template add<kEight>(x, i, a.ct);
+        }
+        if (rank == 0 && warp < rows)
+            share.add_ends(r, a.ct);
+        const UnitPartial p = share.join(a.ct);
+        if (lane == 0)
+            sm.part[warp] = make_int4(__float_as_int(p.M), __float_as_int(p.S), (int)p.idx, 0);
+        __syncthreads();
+        if (warp < rows) {
+            RowSum x;
+            if (warp + lane * rows < kWarps)
+                x.take(sm.part[warp + lane * rows], kGreedy, a.ct);
+            x.join_warp(kGreedy, a.ct);
+            if (lane < ranks)
+                *cluster.map_shared_rank(&sm.slot[turn & 1][warp][rank], lane) =
+                    make_int4(__float_as_int(x.z.m), __float_as_int(x.z.z), (int)x.first, 0);
+        }
+        cluster_arrive();
+        cluster_wait();
+        if (warp < rows) {
+            RowSum x;
+            if (lane < ranks)
+                x.take(sm.slot[turn & 1][warp][lane], kGreedy, a.ct);
+            x.join_warp(kGreedy, a.ct);
+            if (lane == 0) {
+                s.of[mine] = x.z;
+                s.first[mine] = x.first;
+            }
+            __syncwarp();
+            const int to = decide(a, s, mine, n);
+            if (lane == 0)
+                s.choice[mine] = (short)to;
+        }
+        __syncthreads();
+        most = min(a.turn_most, 2 * most);
+#pragma unroll
+        for (int i = 0; i < kTurn; ++i) {
+            if (i >= rows)
+                break;
+            if (node[i] != at) {
+                most = a.turn;
+                break;
+            }
+            if (threadIdx.x == 0)
+                s.path[len] = (short)at;
+            const int to = s.choice[at];
+            if (to <= 0) {
+                if (threadIdx.x == 0) {
+                    taken = len;
+                    failed = to == kBad;
+                }
+                return;
+            }
+            at = to;
+            ++len;
+        }
+    }
+}
+
 // Clusters of CTAs, one to a sequence: the walk, in each CTA; then the draw, each CTA a slice of the
 // vocabulary.  What the call was given is read, and the noise brought to the L2, while the rows'
-// sums are still under way: it was there before their kernel began.
-template <typename T>
-__global__ void __launch_bounds__(kDraw, 2) verify_draw_kernel(const __grid_constant__ VerifyArgs a)
+// sums are still under way: it was there before their kernel began.  kWalk: no kernel came before,
+// the rows are summed as the walk comes to them.
+template <typename T, bool kWalk>
+__global__ void __launch_bounds__(kDraw, kWalk ? 1 : 2)
+    verify_draw_kernel(const __grid_constant__ VerifyArgs a)
 {
     constexpr int E = 16 / sizeof(T);
     __shared__ int taken, failed;
@@ -585,6 +716,12 @@ __global__ void __launch_bounds__(kDraw, 2) verify_draw_kernel(const __grid_cons
     const int64_t base = (int64_t)b * a.M;
     const float *noise = a.noise + (int64_t)b * a.V;
     cluster_arrive_relaxed();  // (that this CTA is there; waited for where another writes to it)
+    if constexpr (kWalk) {
+        pdl_wait();
+        const uint8_t *root = row_at<T>(a, b, 0, false).p;
+        for (int v = v0 + tid * (128 / (int)sizeof(T)); v < v1; v += kDraw * (128 / (int)sizeof(T)))
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(root + (int64_t)v * sizeof(T)));
+    }
     if (!a.greedy) {
         for (int i = tid; i < slice / 32; i += kDraw)
             gone[i] = 0;
@@ -606,37 +743,47 @@ __global__ void __launch_bounds__(kDraw, 2) verify_draw_kernel(const __grid_cons
                 s.y[j] = to_float(reinterpret_cast<const T *>(row_at<T>(a, b, p, true).p)[d]);
         }
     }
-    pdl_wait();
-    __syncthreads();
-    sum_rows<T>(a, s, b, n);
-    __syncthreads();
-    if (a.parents) {
-        for (int c = warp; c < n; c += kDraw / 32) {
-            const int to = decide(a, s, c, n);
-            if (lane == 0)
-                s.choice[c] = (short)to;
-        }
+    if constexpr (kWalk) {
+        __shared__ WalkShared walked;
+        cluster_wait();
+        __syncthreads();
+        if (a.greedy)
+            walk<T, true>(a, s, walked, b, n, cluster, taken, failed);
+        else
+            walk<T, false>(a, s, walked, b, n, cluster, taken, failed);
     } else {
-        for (int c = tid; c < n; c += kDraw)
-            s.choice[c] = (short)decide_chain(a, s, c, n);
-    }
-    __syncthreads();
-    if (tid == 0) {
-        int at = 0, len = 0;
-        for (;; ++len) {
-            s.path[len] = (short)at;
-            const int to = s.choice[at];
-            if (to <= 0) {
-                failed = to == kBad;
-                break;
+        pdl_wait();
+        __syncthreads();
+        sum_rows<T>(a, s, b, n);
+        __syncthreads();
+        if (a.parents) {
+            for (int c = warp; c < n; c += kDraw / 32) {
+                const int to = decide(a, s, c, n);
+                if (lane == 0)
+                    s.choice[c] = (short)to;
             }
-            at = to;
+        } else {
+            for (int c = tid; c < n; c += kDraw)
+                s.choice[c] = (short)decide_chain(a, s, c, n);
         }
-        taken = len;
+        __syncthreads();
+        if (tid == 0) {
+            int at = 0, len = 0;
+            for (;; ++len) {
+                s.path[len] = (short)at;
+                const int to = s.choice[at];
+                if (to <= 0) {
+                    failed = to == kBad;
+                    break;
+                }
+                at = to;
+            }
+            taken = len;
+        }
     }
     __syncthreads();
     int extra = -1;
-    if (failed || a.greedy)
+    if (!kWalk && (failed || a.greedy))
         cluster_wait();
     if (!failed) {
         const int cur = s.path[taken];
@@ -786,7 +933,8 @@ __global__ void __launch_bounds__(kDraw, 2) verify_draw_kernel(const __grid_cons
                 }
             }
             unsigned long long top = best_of_cta();
-            cluster_wait();
+            if (!kWalk)
+                cluster_wait();
             if (tid == 0)
                 cluster.map_shared_rank(of_cta, 0)[rank] = top;
             cluster_arrive();
@@ -826,6 +974,23 @@ __global__ void __launch_bounds__(kDraw, 2) verify_draw_kernel(const __grid_cons
         a.out_n[b] = dead ? FDLLM_ROW_DEVICE_ERROR : failed ? FDLLM_ROW_NONFINITE : taken;
 }
 
+// Whether rows are read as the walk comes to them.
+bool walks(const VerifyArgs &a, int es)
+{
+    const int64_t row = (int64_t)a.V * es;
+    return a.parents && a.B * (a.M * row) >= (row > kSmallRow ? kWalkLong : kWalkShort);
+}
+
+// CTAs that share a sequence's rows then: a cluster of as many for each sequence at once, where there is room.
+// `held`: the clusters of 1, 2, 4 and 8 that the GPU holds.
+int walk_ranks(const VerifyArgs &a, int es, const std::atomic<int> *held)
+{
+    int i = 0;
+    while (i < 3 && a.B <= held[i + 1] && (int64_t)a.V * es >> i > kWalkShare)
+        ++i;
+    return 1 << i;
+}
+
 // CTAs that share a sequence's draw: as many as fill the GPU once (two to an SM), where a slice keeps
 // four values or so of a thread; and as many as a slice's bits of taken tokens need.
 int draw_ranks(const VerifyArgs &a)
@@ -842,7 +1007,9 @@ int draw_ranks(const VerifyArgs &a)
 template <typename T>
 cudaError_t launch_verify(const VerifyArgs &a, cudaStream_t s)
 {
+    constexpr int kMostDraw = kMaxNodes * Nodes::kBytes + kMaxRowV / 8;
     static PerDevice ready;
+    static std::atomic<int> held[kMaxCacheDevices][4];
     cudaError_t e = ready.once([] {
         cudaError_t r = cudaFuncSetAttribute(verify_stream_kernel<T, true>,
                                              cudaFuncAttributeMaxDynamicSharedMemorySize, kStreamSmem);
@@ -850,8 +1017,15 @@ cudaError_t launch_verify(const VerifyArgs &a, cudaStream_t s)
             r = cudaFuncSetAttribute(verify_stream_kernel<T, false>,
                                      cudaFuncAttributeMaxDynamicSharedMemorySize, kStreamSmem);
         if (r == cudaSuccess)
-            r = cudaFuncSetAttribute(verify_draw_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                     kMaxNodes * Nodes::kBytes + kMaxRowV / 8);
+            r = cudaFuncSetAttribute(verify_draw_kernel<T, false>,
+                                     cudaFuncAttributeMaxDynamicSharedMemorySize, kMostDraw);
+        if (r == cudaSuccess)
+            r = cudaFuncSetAttribute(verify_draw_kernel<T, true>,
+                                     cudaFuncAttributeMaxDynamicSharedMemorySize, kMostDraw);
+        int dev = 0;
+        if (r == cudaSuccess && (r = cudaGetDevice(&dev)) == cudaSuccess)
+            for (int i = 0; i < 4; ++i)
+                held[dev][i] = clusters_held(verify_draw_kernel<T, true>, kDraw, kMostDraw, 1 << i);
         return r;
     });
     if (e != cudaSuccess)
@@ -859,17 +1033,24 @@ cudaError_t launch_verify(const VerifyArgs &a, cudaStream_t s)
     const int64_t rows = (int64_t)a.B * (a.draft ? 2 * a.M - 1 : a.M);
     auto small = a.greedy ? verify_small_kernel<T, true> : verify_small_kernel<T, false>;
     auto stream = a.greedy ? verify_stream_kernel<T, true> : verify_stream_kernel<T, false>;
-    if ((int64_t)a.V * sizeof(T) <= kSmallRow) {
+    int walkers = 0;
+    if (walks(a, sizeof(T))) {
+        int dev = 0;
+        if ((e = cudaGetDevice(&dev)) != cudaSuccess)
+            return e;
+        walkers = walk_ranks(a, sizeof(T), held[dev]);
+    }
+    if (walkers == 0 && (int64_t)a.V * sizeof(T) <= kSmallRow) {
         const int64_t want = (rows * a.per + 7) / 8, most = (int64_t)sm_count() * 8;
         e = launch(small, dim3((unsigned)(want < most ? want : most)), dim3(256), 0, s, true, a);
-    } else {
+    } else if (walkers == 0) {
         const int64_t units = rows * a.pieces, most = sm_count();
         e = launch(stream, dim3((unsigned)(units < most ? units : most)), dim3(kMath + 32),
                    kStreamSmem, s, true, a);
     }
     if (e != cudaSuccess)
         return e;
-    const int ranks = draw_ranks(a);
+    const int ranks = walkers != 0 ? walkers : draw_ranks(a);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(a.B * ranks));
     cfg.blockDim = dim3(kDraw);
@@ -882,7 +1063,14 @@ cudaError_t launch_verify(const VerifyArgs &a, cudaStream_t s)
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = plain_launches ? 1 : 2;
-    return cudaLaunchKernelEx(&cfg, verify_draw_kernel<T>, VerifyArgs(a));
+    if (walkers == 0)
+        return cudaLaunchKernelEx(&cfg, verify_draw_kernel<T, false>, VerifyArgs(a));
+    VerifyArgs by_turns = a;
+    const int64_t share = (int64_t)a.V * (int)sizeof(T) / ranks;
+    auto rows_of = [&](int64_t bytes) { return (int)(bytes < share ? 1 : bytes / share < kTurn ? bytes / share : kTurn); };
+    by_turns.turn = rows_of(kTurnBytes);
+    by_turns.turn_most = rows_of(2 * kTurnBytes);
+    return cudaLaunchKernelEx(&cfg, verify_draw_kernel<T, true>, by_turns);
 }
 
 // How rows are cut: whole, or in pieces of whole chunks so that every SM has two, and no piece is

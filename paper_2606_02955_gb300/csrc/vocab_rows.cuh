@@ -222,6 +222,29 @@ __device__ __forceinline__ void cluster_wait()
 
 __device__ __forceinline__ bool finite_f(float x) { return fabsf(x) <= FLT_MAX; }
 
+// Clusters of `ranks` CTAs, one to an SM, that the GPU holds at once.
+template <typename K>
+int clusters_held(K kern, int threads, int smem, int ranks)
+{
+    if (ranks == 1)
+        return sm_count();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(sm_count() / ranks * ranks));
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim = {(unsigned)ranks, 1, 1};
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess || n < 1) {
+        cudaGetLastError();
+        n = sm_count() / ranks;
+    }
+    return n;
+}
+
 #endif  // __CUDACC__
 
 }  // namespace fdllm

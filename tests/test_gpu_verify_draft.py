@@ -113,6 +113,61 @@ def test_rows_that_the_walk_cannot_reach(fd, kind, B, M, V, dtype):
     assert all(torch.equal(a, b) for a, b in zip(got, again))
 
 
+@pytest.mark.parametrize("kind", ["tree", "greedy"])
+@pytest.mark.parametrize("B,M,V,dtype", [(3, 40, 60001, BF), (1, 1024, 17003, HF), (20, 24, 17003, FP),
+                                         (41, 128, 4999, HF), (160, 20, 8199, HF), (7, 4, 126464, FP)])
+def test_trees_read_along_the_way(fd, kind, B, M, V, dtype):
+    """Large calls with trees of every depth: rows of any alignment, more sequences than SMs; chains and
+    stars; a row that is no number in the middle of a path."""
+    target, tokens, kw = inputs(B, M, V, dtype, kind, seed=B + M + 1)
+    lens = (M + 1 - torch.arange(B) % 4 * (M // 3)).int()
+    check(fd, target, tokens, most_near=1, lens=lens, **kw)
+    # every node of a chain is taken, however deep; the first child's subtree or another's
+    chain = torch.arange(-1, M - 1).expand(B, M).int().contiguous()
+    if kind == "greedy":
+        tokens[:, 1:] = target[:, :-1].float().argmax(-1)
+    else:
+        kw["uniform"][:] = 0.0
+        tokens[:, 1:] = (7 * torch.arange(M - 1) + torch.arange(B)[:, None]) % V
+    kw["parents"] = chain
+    got = check(fd, target, tokens, **kw)
+    assert got[2].tolist() == [M - 1] * B and torch.equal(got[0][:, :-1], tokens[:, 1:])
+    at = M // 2
+    target[0, at, V // 2] = math.nan
+    got = check(fd, target, tokens, **kw)
+    assert got[2].tolist() == [-1] + [M - 1] * (B - 1)
+    kw["parents"] = chain.clone()
+    kw["parents"][:, at:] = 0  # one deep path, and leaves: the NaN is a leaf's
+    if kind == "tree":
+        kw["uniform"][:, at:] = 1.0 - 2.0 ** -24
+    got = check(fd, target, tokens, **kw)
+    assert int(got[2].min()) >= at - 1
+    kw["parents"][:] = 0
+    check(fd, target, tokens, lens=lens, **kw)
+
+
+def test_trees_read_along_the_way_replayed_and_apart(fd):
+    target, tokens, kw = inputs(6, 33, 40003, BF, "tree", seed=44)
+    want = check(fd, target, tokens, **kw)
+    wide = torch.zeros(7, 35, 40006, dtype=BF, device="cuda").transpose(0, 1)[:33].transpose(0, 1)[1:, :, 3:]
+    wide.copy_(target)
+    kw, tokens = {k: cuda(v) for k, v in kw.items()}, tokens.cuda()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for got in (fd.fdllm_verify_draft(wide, tokens, **kw), fd.fdllm_verify_draft(wide, tokens, stream=side, **kw)):
+        torch.cuda.synchronize()
+        assert all(torch.equal(a.cpu(), b) for a, b in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = [fd.fdllm_verify_draft(wide, tokens, **kw) for _ in range(2)]
+    for turn in range(3):
+        kw["uniform"].copy_(torch.rand(6, 33, generator=torch.Generator().manual_seed(turn)))
+        graph.replay()
+        again = fd.fdllm_verify_draft(wide, tokens, **kw)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) and torch.equal(a, c) for a, b, c in zip(again, *outs))
+
+
 @pytest.mark.parametrize("seed", range(16))
 def test_many_sequences(fd, seed):
     kind = ("draft", "tree", "chosen", "greedy")[seed % 4]
