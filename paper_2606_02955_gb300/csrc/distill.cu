@@ -22,9 +22,14 @@ constexpr int kMaxTop = 1024;
 constexpr int kThreads = 128;      // of a CTA of the small form
 // Rows up to kSmallRow bytes take it, and up to kManyRow where there are more rows than SMs: each
 // further row of a CTA costs the long form about 5 us whatever its length, for the latencies from list
-// to mark, which many CTAs to an SM hide.  Steps in bf16: 1024 rows of 12001 15 us (the long form 34), 256
-// of 17000 11 (15), 4096 of 32000 130 (150); but 152 of 32000 12.5 (10.5); 64 of 12001 alike, 8.
+// to mark, which many CTAs to an SM hide.  Steps in bf16: 1024 rows of 12001 13 us (the long form 34), 256
+// of 17000 8.7 (15), 4096 of 32000 116 (150), 300 of 32000 12.2 (15.4; half of them masked 12.3, 11.0); but
+// 64 of 32000 10.2 (9.5), 1024 of 45000, half of them masked, 36 (34), 2048 of 64000 131 (113): their
+// second read is no longer the L2's.  The loss alone has none, and rows of up to kLossV values take it
+// where there are more than kFull to an SM: 2056 of 50021 in fp32, 0.6 of them masked, 43 us (49), 4096
+// of 126464, half of them masked, 86 (95); but 256 of 126464 32 (19).
 constexpr int kSmallRow = 32768, kManyRow = 65536;
+constexpr int kLossV = 1 << 17, kFull = 8;
 
 struct DistillArgs {
     const void *logits;      // [rows, V]
@@ -117,17 +122,17 @@ struct RowTerms {
 };
 
 // ---- Short rows: a CTA of kThreads to a row, many on an SM.
-// kSum: the row's sums are taken (else they are given); kGrad: the gradient is written.
-template <typename T, bool kSum, bool kGrad>
-__global__ void __launch_bounds__(kThreads, 8) distill_small_kernel(const __grid_constant__ DistillArgs a)
+// kSum: the row's sums are taken (else they are given); kGrad: the gradient is written; kMine: listed
+// tokens of a thread.
+template <typename T, bool kSum, bool kGrad, int kMine>
+__global__ void __launch_bounds__(kThreads, kFull) distill_small_kernel(const __grid_constant__ DistillArgs a)
 {
     constexpr int E = 16 / sizeof(T);
-    constexpr int kMine = kMaxTop / kThreads;  // listed tokens of a thread
     constexpr int kWarps = kThreads / 32;
-    constexpr int kFour = 4;  // vectors of a thread in flight
+    constexpr int kFour = kGrad ? 4 : 8;  // vectors of a thread in flight
     extern __shared__ __align__(16) uint32_t marks[];  // a bit for each value of the whole vectors
-    __shared__ int idx[kMaxTop];
-    __shared__ float p[kMaxTop];
+    __shared__ int idx[kMine * kThreads];
+    __shared__ float p[kMine * kThreads];
     __shared__ float of_most[kWarps], of_mass[kWarps];
     __shared__ ExpSum of_rest[kWarps], of_listed[kWarps];
     __shared__ float of_loss[kWarps], of_share[kWarps];
@@ -137,8 +142,7 @@ __global__ void __launch_bounds__(kThreads, 8) distill_small_kernel(const __grid
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const float c = a.inv_t * kLog2e;
     const uint8_t *const listed = reinterpret_cast<const uint8_t *>(marks);
-    for (int i = tid; i < a.V / 32 + 1; i += kThreads)
-        marks[i] = 0;
+    bool clean = false;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         T *grad = static_cast<T *>(a.grad) + row * a.V;
         if (!a.mask[row]) {
@@ -160,6 +164,10 @@ __global__ void __launch_bounds__(kThreads, 8) distill_small_kernel(const __grid
         }
         const RowSpan<T> s(static_cast<const T *>(a.logits) + row * a.V, a.V);
         // ---- the teacher's probabilities, and the student's logits of its tokens
+        if (!clean)
+            for (int i = tid; i < a.V / 32 + 1; i += kThreads)
+                marks[i] = 0;
+        clean = true;
         if (tid == 0)
             twice = 0, ends = 0;
         __syncthreads();
@@ -1104,9 +1112,12 @@ template <typename T, bool kSum, bool kGrad>
 cudaError_t launch_kind(const DistillArgs &a, cudaStream_t s)
 {
     constexpr int es = sizeof(T);
-    if ((int64_t)a.V * es <= (a.rows > sm_count() ? kManyRow : kSmallRow)) {
-        auto *kern = distill_small_kernel<T, kSum, kGrad>;
-        const int64_t most = (int64_t)sm_count() * 16;
+    if ((int64_t)a.V * es <= (a.rows > sm_count() ? kManyRow : kSmallRow) ||
+        (kSum && !kGrad && a.V <= kLossV && a.rows > kFull * sm_count())) {
+        auto *kern = a.K <= kThreads ? distill_small_kernel<T, kSum, kGrad, 1>
+                                     : distill_small_kernel<T, kSum, kGrad, kMaxTop / kThreads>;
+        // (long rows a CTA each, as SMs have room for them)
+        const int64_t most = (int64_t)a.V * es > kSmallRow ? a.rows : (int64_t)sm_count() * 16;
         return launch(kern, dim3((unsigned)(a.rows < most ? a.rows : most)), dim3(kThreads),
                       (size_t)(a.V / 32 + 1) * 4, s, true, a);
     }

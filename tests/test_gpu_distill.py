@@ -324,6 +324,21 @@ def test_many_long_rows(fd, dtype, rest, B, V):
     assert torch.equal(again[0], loss) and torch.equal(into, grad)
 
 
+@pytest.mark.parametrize("dtype,V,K", [(BF, 50021, 40), (FP, 49999, 1024), (HF, 131072, 7)])
+def test_loss_of_many_long_rows(fd, dtype, V, K):
+    """A CTA to each of more rows than the GPU holds; the same thirteen again and again."""
+    kw, _ = inputs(1, 13, V, K, dtype, 31, True, masked=0.7, temperature=0.7)
+    want, tol, _, _ = ref.distill(kw["logits"], kw["mask"], kw["top_index"], kw["top_logits"], kw["teacher_lse"],
+                                  0.7, torch.ones(1, 13, device="cuda"))
+    big = {k: v.expand(100, *v.shape[1:]).contiguous() if isinstance(v, torch.Tensor) else v for k, v in kw.items()}
+    stats = torch.full((100, 13, 4), 7.0, device="cuda")
+    loss = fd.fdllm_distill_loss(out_stats=stats, **big)
+    assert bool(((loss.cpu().double() - want).abs() <= tol).all())
+    assert bool((stats[big["mask"] == 0] == 0).all())
+    assert torch.equal(loss, fd.fdllm_distill_loss(**big))
+    assert fd.fdllm_cache_status() == 0
+
+
 def test_refusals(fd):
     kw, weights = inputs(2, 3, 64, 4, BF, 19, True)
     loss = lambda **more: fd.fdllm_distill_loss(**{**kw, **more})
