@@ -578,6 +578,7 @@ size_t fdllm_verify_draft_workspace_bytes(int B, int M, int V, int dtype);
  *   can be drawn from that either, the next token is the argmax.
  * Probabilities and weights are fp32 (relative error within 1e-5), the tests of tokens 64-bit
  * products of them.
+ * Rows that are not on the way change nothing; of large trees they are not read.
  *   target     [B, M, V] device, dtype as given, row j the logits after node j; V any from 1 to 2^20,
  *              the values of a row contiguous, rows anywhere (FDLLM_ERR_ALIGN: a base that is not a
  *              multiple of the value's size); target_strides {batch, row} in elements, host.

@@ -1017,10 +1017,11 @@ def fdllm_verify_draft(target: torch.Tensor, tokens: torch.Tensor, parents=None,
     return out_tokens, out_nodes, out_n
 
 
-def _overwritten(logits, out_grad):
-    """Tells autograd of a gradient written over its logits (a graph that saved them then says so)."""
-    if out_grad is logits and not logits.is_inference():
-        torch.autograd.graph.increment_version(logits)
+def _overwritten(out_grad):
+    """Tells autograd of a gradient written over a caller's tensor (the logits themselves, for one): a
+    graph that saved it then says so."""
+    if not out_grad.is_inference():
+        torch.autograd.graph.increment_version(out_grad)
 
 
 def _distill_args(logits, mask, top_index, top_logits, teacher_lse, dev):
@@ -1126,7 +1127,8 @@ def _distill_grad(logits, mask, top_index, top_logits, stats, grad_loss, teacher
     dev = logits.device
     args = _distill_args(logits, mask, top_index, top_logits, teacher_lse, dev)
     B, L = args[2:4]
-    if out_grad is None:
+    made = out_grad is None
+    if made:
         out_grad = _made(logits.shape, logits.dtype, dev, stream)
     st = _load().fdllm_distill_grad(
         *args, temperature, _ptr(stats, "stats", _F32, (B, L, 4), dev),
@@ -1135,7 +1137,8 @@ def _distill_grad(logits, mask, top_index, top_logits, stats, grad_loss, teacher
         _raw_stream(dev.index) if stream is None else _stream(stream))
     if st:
         _check(st, "fdllm_distill_grad")
-    _overwritten(logits, out_grad)
+    if not made:
+        _overwritten(out_grad)
     return out_grad
 
 
@@ -1151,7 +1154,8 @@ def fdllm_distill_step(logits: torch.Tensor, mask: torch.Tensor, top_index: torc
     B, L = args[2:4]
     if out_loss is None:
         out_loss = _made((B, L), _F32, dev, stream)
-    if out_grad is None:
+    made = out_grad is None
+    if made:
         out_grad = _made(logits.shape, logits.dtype, dev, stream)
     st = _load().fdllm_distill_step(
         *args, temperature, _ptr(grad_loss, "grad_loss", _F32, (B, L), dev),
@@ -1160,13 +1164,14 @@ def fdllm_distill_step(logits: torch.Tensor, mask: torch.Tensor, top_index: torc
         _raw_stream(dev.index) if stream is None else _stream(stream))
     if st:
         _check(st, "fdllm_distill_step")
-    _overwritten(logits, out_grad)
+    if not made:
+        _overwritten(out_grad)
     return out_loss, out_grad
 
 
 def fdllm_cache_status(stream=None) -> int:
-    """Synchronises and returns (clearing it) the sticky device status of the cache's attention
-    and key-weight kernels on the current device."""
+    """Synchronises and returns (clearing it) the sticky device status of the cache's attention and
+    key-weight kernels, of the verification and of the distillation on the current device."""
     return _load().fdllm_cache_status(_stream(stream))
 
 

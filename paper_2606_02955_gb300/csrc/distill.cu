@@ -1112,29 +1112,34 @@ template <typename T, bool kSum, bool kGrad>
 cudaError_t launch_kind(const DistillArgs &a, cudaStream_t s)
 {
     constexpr int es = sizeof(T);
-    if ((int64_t)a.V * es <= (a.rows > sm_count() ? kManyRow : kSmallRow) ||
-        (kSum && !kGrad && a.V <= kLossV && a.rows > kFull * sm_count())) {
-        auto *kern = a.K <= kThreads ? distill_small_kernel<T, kSum, kGrad, 1>
-                                     : distill_small_kernel<T, kSum, kGrad, kMaxTop / kThreads>;
-        // (long rows a CTA each, as SMs have room for them)
-        const int64_t most = (int64_t)a.V * es > kSmallRow ? a.rows : (int64_t)sm_count() * 16;
-        return launch(kern, dim3((unsigned)(a.rows < most ? a.rows : most)), dim3(kThreads),
-                      (size_t)(a.V / 32 + 1) * 4, s, true, a);
-    }
-    auto *kern = distill_ring_kernel<T, kSum, kGrad>;
+    auto *few = distill_small_kernel<T, kSum, kGrad, 1>;
+    auto *many = distill_small_kernel<T, kSum, kGrad, kMaxTop / kThreads>;
+    auto *ring = distill_ring_kernel<T, kSum, kGrad>;
     constexpr int kSmem = RingLayout<kSum, kGrad>::bytes;
     static PerDevice ready;
     static std::atomic<int> held[kMaxCacheDevices][4];
     cudaError_t e = ready.once([&] {
-        const cudaError_t r = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        cudaFuncAttributes f;  // (asked for, a kernel is loaded: a capture may be next)
+        cudaError_t r = cudaFuncGetAttributes(&f, few);
+        if (r == cudaSuccess)
+            r = cudaFuncGetAttributes(&f, many);
+        if (r == cudaSuccess)
+            r = cudaFuncSetAttribute(ring, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
         int dev = 0;
         if (r == cudaSuccess && cudaGetDevice(&dev) == cudaSuccess)
             for (int i = 0; i < 4; ++i)
-                held[dev][i] = clusters_held(kern, kRingThreads, kSmem, 1 << i);
+                held[dev][i] = clusters_held(ring, kRingThreads, kSmem, 1 << i);
         return r;
     });
     if (e != cudaSuccess)
         return e;
+    if ((int64_t)a.V * es <= (a.rows > sm_count() ? kManyRow : kSmallRow) ||
+        (kSum && !kGrad && a.V <= kLossV && a.rows > kFull * sm_count())) {
+        // (long rows a CTA each, as SMs have room for them)
+        const int64_t most = (int64_t)a.V * es > kSmallRow ? a.rows : (int64_t)sm_count() * 16;
+        return launch(a.K <= kThreads ? few : many, dim3((unsigned)(a.rows < most ? a.rows : most)),
+                      dim3(kThreads), (size_t)(a.V / 32 + 1) * 4, s, true, a);
+    }
     int dev = 0;
     if ((e = cudaGetDevice(&dev)) != cudaSuccess)
         return e;
@@ -1154,7 +1159,7 @@ cudaError_t launch_kind(const DistillArgs &a, cudaStream_t s)
     cfg.attrs = attr;
     cfg.numAttrs = plain_launches ? 1 : 2;
     const int two = RingLayout<kSum, kGrad>::wide || a.V / ranks <= kMostListed / 2 - 64;
-    return cudaLaunchKernelEx(&cfg, kern, DistillArgs(a), ranks, two);
+    return cudaLaunchKernelEx(&cfg, ring, DistillArgs(a), ranks, two);
 }
 
 template <typename T>

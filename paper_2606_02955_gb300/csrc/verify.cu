@@ -1011,8 +1011,13 @@ cudaError_t launch_verify(const VerifyArgs &a, cudaStream_t s)
     static PerDevice ready;
     static std::atomic<int> held[kMaxCacheDevices][4];
     cudaError_t e = ready.once([] {
-        cudaError_t r = cudaFuncSetAttribute(verify_stream_kernel<T, true>,
-                                             cudaFuncAttributeMaxDynamicSharedMemorySize, kStreamSmem);
+        cudaFuncAttributes f;  // (asked for, a kernel is loaded: a capture may be next)
+        cudaError_t r = cudaFuncGetAttributes(&f, verify_small_kernel<T, true>);
+        if (r == cudaSuccess)
+            r = cudaFuncGetAttributes(&f, verify_small_kernel<T, false>);
+        if (r == cudaSuccess)
+            r = cudaFuncSetAttribute(verify_stream_kernel<T, true>,
+                                     cudaFuncAttributeMaxDynamicSharedMemorySize, kStreamSmem);
         if (r == cudaSuccess)
             r = cudaFuncSetAttribute(verify_stream_kernel<T, false>,
                                      cudaFuncAttributeMaxDynamicSharedMemorySize, kStreamSmem);

@@ -252,6 +252,39 @@ def test_a_gradient_over_saved_logits_is_seen(fd):
         fd.fdllm_distill_step(z, kw["mask"], kw["top_index"], kw["top_logits"], weights, out_grad=z)
 
 
+def test_a_gradient_over_another_view_of_saved_logits_is_seen(fd):
+    kw, weights = inputs(1, 3, 200, 5, FP, 22, False)
+    rest = (kw["mask"], kw["top_index"], kw["top_logits"])
+    stats = torch.empty(1, 3, 4, device="cuda")
+    for call in (lambda y: fd.fdllm_distill_step(y.detach(), *rest, weights, out_grad=y.detach()),
+                 lambda y: fd.fdllm_distill_grad(y.detach(), *rest, stats, weights, out_grad=y.detach())):
+        y = (kw["logits"] * 1.0).requires_grad_() * 2.0
+        loss = fd.fdllm_distill_loss(**{**kw, "logits": y})
+        fd.fdllm_distill_loss(out_stats=stats, **{**kw, "logits": y.detach()})
+        call(y)
+        with pytest.raises(RuntimeError):
+            loss.backward(weights)
+
+
+def test_every_form_may_be_captured_after_one_call(fd):
+    """A first call of few short rows sets up what long rows, long lists and clusters need too."""
+    calls = []
+    for B, L, V, K in ((1, 1, 33, 2), (2, 3, 40009, 200), (1, 200, 20000, 7), (1, 1, 126464, 9)):
+        kw, weights = inputs(B, L, V, K, HF, 51, True, masked=1.1)
+        calls.append((kw["logits"], kw["mask"], kw["top_index"], kw["top_logits"], weights, kw["teacher_lse"]))
+    for args in calls:
+        graph = torch.cuda.CUDAGraph()
+        if args is calls[0]:
+            fd.fdllm_distill_step(*args)
+            torch.cuda.synchronize()
+        with torch.cuda.graph(graph):
+            got = fd.fdllm_distill_step(*args)
+        graph.replay()
+        want = fd.fdllm_distill_step(*args)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 @pytest.mark.parametrize("temperature", [1e-3, 0.05, 30.0, 1e4])
 @pytest.mark.parametrize("V", [700, 20003])
 def test_temperatures_of_any_size(fd, temperature, V):
