@@ -492,6 +492,13 @@ struct RowShare {
         v0 = min(r.vecs, rank * per);
         v1 = min(r.vecs, v0 + per);
     }
+    // Whether value v of the row is the CTA's.
+    __device__ __forceinline__ bool holds(int v, int rank, int ranks) const
+    {
+        constexpr int E = RowSpan<T>::E;
+        const int b = v - r.head;
+        return v < r.head ? rank == 0 : v >= r.tail() ? rank == ranks - 1 : b >= v0 * E && b < v1 * E;
+    }
     __device__ __forceinline__ int chunks() const { return (v1 - v0 + kChunkVecs - 1) / kChunkVecs; }
     __device__ __forceinline__ int in_chunk(int j) const { return min(kChunkVecs, v1 - v0 - j * kChunkVecs); }
 };
@@ -817,13 +824,20 @@ __global__ void __launch_bounds__(kRingThreads, 1)
             ExpSum of_x;
             if (row >= 0) {
                 const T *logits = static_cast<const T *>(a.logits) + row * a.V;
+                const RowShare<T> sh(a.logits, row, a.V, rank, ranks);
                 float most = -FLT_MAX;
                 T raw[kMine];
 #pragma unroll
                 for (int j = 0; j < kMine; ++j) {
                     v[j] = next_v[j] >= 0 && next_v[j] < a.V ? next_v[j] : -1;
                     m[j] = v[j] >= 0 ? next_s[j] : neg_inf_f();
-                    raw[j] = logits[max(v[j], 0)];
+                    raw[j] = from_float<T>(0.0f);
+                    // In place the gradient takes the logits' place.  Where the row is summed no CTA
+                    // writes before all have sent their sums, which come behind these reads; where it
+                    // is not, the CTAs of a cluster do not wait for each other, and each reads what it
+                    // writes itself, its own share, and no more.
+                    if (v[j] >= 0 && (kSum || sh.holds(v[j], rank, ranks)))
+                        raw[j] = logits[v[j]];
                 }
                 const float lse = next_lse;
                 fetch(i + 1);
@@ -956,24 +970,26 @@ __global__ void __launch_bounds__(kRingThreads, 1)
                             }
                     }
                 }
-                // ---- what is of the listed tokens alone
-                float top = -FLT_MAX;
+                if constexpr (kSum) {
+                    // ---- what is of the listed tokens alone
+                    float top = -FLT_MAX;
 #pragma unroll
-                for (int j = 0; j < kMine; ++j)
-                    if (v[j] >= 0)
-                        top = Most()(top, x[j]);
-                top = teach_reduce(top, sm.reduce[0], Most());
-                of_x.m = top;
-                float z = 0.0f;
+                    for (int j = 0; j < kMine; ++j)
+                        if (v[j] >= 0)
+                            top = Most()(top, x[j]);
+                    top = teach_reduce(top, sm.reduce[0], Most());
+                    of_x.m = top;
+                    float z = 0.0f;
 #pragma unroll
-                for (int j = 0; j < kMine; ++j)
-                    if (v[j] >= 0) {
-                        z += ex2_mufu((x[j] - top) * c);
-                        if (m[j] != 0.0f)
-                            A += m[j] * (logf(m[j]) - (x[j] - top) * a.inv_t);
-                    }
-                of_x.z = teach_reduce(z, sm.reduce[1], Add());
-                A = teach_reduce(A, sm.reduce[2], Add());
+                    for (int j = 0; j < kMine; ++j)
+                        if (v[j] >= 0) {
+                            z += ex2_mufu((x[j] - top) * c);
+                            if (m[j] != 0.0f)
+                                A += m[j] * (logf(m[j]) - (x[j] - top) * a.inv_t);
+                        }
+                    of_x.z = teach_reduce(z, sm.reduce[1], Add());
+                    A = teach_reduce(A, sm.reduce[2], Add());
+                }
             }
             if (t == 0) {
                 Taught &of = sm.taught[par];
@@ -1002,11 +1018,7 @@ __global__ void __launch_bounds__(kRingThreads, 1)
                         const int at = old[j];
                         if (at < 0)
                             continue;
-                        const int b = at - sh.r.head;
-                        const bool mine = at < sh.r.head       ? rank == 0
-                                          : at >= sh.r.tail() ? rank == ranks - 1
-                                                              : b >= sh.v0 * E && b < sh.v1 * E;
-                        if (mine)
+                        if (sh.holds(at, rank, ranks))
                             grad[at] = from_float<T>(
                                 fix.w * (ex2_mufu((old_x[j] - fix.x) * c) / fix.y * fix.z - old_p[j]));
                     }

@@ -391,3 +391,32 @@ def test_refusals(fd):
         step(grad_loss=weights.bfloat16())
     with pytest.raises(ValueError):
         step(out_grad=torch.empty(2, 3, 65, dtype=BF, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype,B,L,V,K,masked", [(BF, 4, 80, 151937, 300, 0.7), (FP, 4, 60, 151937, 300, 0.7),
+                                                  (BF, 1, 3, 126464, 64, 1.1), (HF, 1, 9, 131072, 1024, 0.9),
+                                                  (FP, 2, 6, 126464, 33, 0.6), (BF, 2, 150, 50021, 200, 0.5),
+                                                  (HF, 3, 5, 4099, 40, 0.8), (FP, 3, 70, 301, 9, 0.8)])
+def test_gradient_in_place(fd, dtype, B, L, V, K, masked):
+    """fdllm_distill_grad over the logits themselves: one CTA to a row and clusters of two to eight, with
+    tokens listed in every share, several rows to each."""
+    g = torch.Generator().manual_seed(34)
+    logits = (1.5 * torch.randn(L, V, generator=g)).to(dtype).cuda().expand(B, L, V).contiguous()
+    index = torch.stack([torch.randperm(V, generator=g)[:K] for _ in range(B * L)]).view(B, L, K).int()
+    index[:, :, K // 2] = index[:, :, 0]  # (one twice)
+    top = (3 + 4 * torch.rand(B, L, K, generator=g)).cuda()
+    mask = (torch.rand(B, L, generator=g) < masked).to(torch.uint8).cuda()
+    lse = torch.logsumexp(top, -1) + 1.0
+    weights = torch.randn(B, L, generator=g).cuda()
+    rest = mask, index.cuda(), top
+    stats = torch.empty(B, L, 4, device="cuda")
+    fd.fdllm_distill_loss(logits, *rest, lse, out_stats=stats)
+    want = fd.fdllm_distill_grad(logits, *rest, stats, weights, lse)
+    step = fd.fdllm_distill_step(logits, *rest, weights, lse)[1]
+    assert bool((want[mask == 0] == 0).all()) and bool((want[mask != 0] != 0).any())
+    assert torch.equal(step[mask == 0], want[mask == 0])
+    for _ in range(3):
+        x = logits.clone()
+        got = fd.fdllm_distill_grad(x, *rest, stats, weights, lse, out_grad=x)
+        assert got.data_ptr() == x.data_ptr() and torch.equal(x, want)
+    assert fd.fdllm_cache_status() == 0
