@@ -420,3 +420,15 @@ def test_gradient_in_place(fd, dtype, B, L, V, K, masked):
         got = fd.fdllm_distill_grad(x, *rest, stats, weights, lse, out_grad=x)
         assert got.data_ptr() == x.data_ptr() and torch.equal(x, want)
     assert fd.fdllm_cache_status() == 0
+
+
+@pytest.mark.parametrize("V", [700, 20003])
+@pytest.mark.parametrize("temperature", [1e-6, 1e-3, 0.05])
+def test_a_teachers_gaps_at_low_temperatures(fd, temperature, V):
+    """Logits near 8 that differ by a few temperatures: the teacher's probabilities are of the gaps, which
+    fp32 holds, whatever logit / temperature is (8e6: a step of 0.5)."""
+    for dtype in (FP, BF):
+        kw, weights = inputs(2, 3, V, 9, FP, 32, False, masked=1.1, temperature=temperature)
+        kw["logits"] = (8.0 + temperature * kw["logits"]).to(dtype)
+        kw["top_logits"] = 8.0 + temperature * kw["top_logits"]
+        check(fd, kw, weights)
