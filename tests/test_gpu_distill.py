@@ -432,3 +432,25 @@ def test_a_teachers_gaps_at_low_temperatures(fd, temperature, V):
         kw["logits"] = (8.0 + temperature * kw["logits"]).to(dtype)
         kw["top_logits"] = 8.0 + temperature * kw["top_logits"]
         check(fd, kw, weights)
+
+
+@pytest.mark.parametrize("V", [700, 40009])
+def test_a_teachers_sum_that_is_nan(fd, V):
+    """Such a position's loss and gradient are NaN, whatever is listed: nothing, some tokens or all that
+    the student allows."""
+    kw, weights = inputs(1, 5, V, 9, FP, 33, True, masked=1.1)
+    kw["teacher_lse"][0, :3] = math.nan
+    kw["top_index"][0, 0] = -1
+    at = kw["top_index"][0, 2].long()
+    kept = kw["logits"][0, 2, at]
+    kw["logits"][0, 2] = -math.inf
+    kw["logits"][0, 2, at] = kept
+    stats = torch.empty(1, 5, 4, device="cuda")
+    loss = fd.fdllm_distill_loss(out_stats=stats, **kw)
+    args = kw["logits"], kw["mask"], kw["top_index"], kw["top_logits"]
+    grad = fd.fdllm_distill_grad(*args, stats, weights, kw["teacher_lse"])
+    step = fd.fdllm_distill_step(*args, weights, kw["teacher_lse"])
+    for x in (loss, step[0]):
+        assert torch.isnan(x).tolist() == [[True] * 3 + [False] * 2]
+    for x in (grad, step[1]):
+        assert bool(torch.isnan(x[0, :3]).all()) and not bool(torch.isnan(x[0, 3:]).any())
