@@ -88,8 +88,9 @@ def forward_nodes(model, prefix, tokens, parents):
     return rms(x) @ model.vocab_w.t(), state
 
 
-def step(model, drafter, prefix, root, nodes, tree, g, temperature=1.0):
-    """One pass: draft, run, take, keep.  `tree`: the nodes' parents, or None for a chain.  Returns
+def step(model, drafter, prefix, root, nodes, tree, g, temperature=1.0, live=None):
+    """One pass: draft, run, take, keep.  `tree`: the nodes' parents, or None for a chain; `live` [B]:
+    the sequences that go on (None: all), the others keep their cache and teach nothing.  Returns
     what was taken and what it was made of."""
     B = root.shape[0]
     if tree is None:
@@ -104,14 +105,17 @@ def step(model, drafter, prefix, root, nodes, tree, g, temperature=1.0):
     found, path, n = fd.fdllm_verify_draft(logits, tokens, parents=None if tree is None else parents,
                                            draft=drawn, temperature=temperature, uniform=uniform,
                                            noise=noise, draft_temperature=1.0)
+    kept = n + 1 if live is None else torch.where(live, n + 1, 0)
     rows = path.clamp(min=0).long()[:, :, None, None].expand(-1, -1, model.kv_heads, model.head_dim)
     for cache, s in zip(prefix.caches, state):
         fd.fdllm_cache_append(cache, prefix.table, prefix.lens, s["k"].gather(1, rows),
-                              s["v"].gather(1, rows), count=n + 1)
+                              s["v"].gather(1, rows), count=kept)
     on_path = torch.zeros(tokens.shape, dtype=torch.uint8, device="cuda")
     on_path.scatter_(1, path.clamp(min=0).long(), 1)
+    if live is not None:
+        on_path *= live[:, None]
     loss = drafter.learn(tokens, on_path, logits)
-    before, prefix.lens = prefix.lens, prefix.lens + n + 1
+    before, prefix.lens = prefix.lens, prefix.lens + kept
     return {"tokens": found, "path": path, "n": n, "loss": loss, "nodes": tokens, "parents": parents,
             "logits": logits, "drawn": drawn, "uniform": uniform, "noise": noise, "state": state,
             "lens": before}
@@ -122,22 +126,23 @@ def decode(model, drafter, prompt, generate, nodes=6, tree=None, seed=0):
     B, P = prompt.shape
     g = torch.Generator(device="cuda").manual_seed(seed)
     nodes = nodes if tree is None else len(tree)
-    prefix = PrefixCache(model, B, P + generate + 2 * nodes)
+    prefix = PrefixCache(model, B, P + generate + nodes)
     chain = torch.arange(-1, P - 2, dtype=torch.int32, device="cuda").expand(B, -1).contiguous()
     _, state = forward_nodes(model, prefix, prompt[:, :-1], chain)
     prefix.append(state)
     root, done, losses = prompt[:, -1], [[] for _ in range(B)], []
     while min(len(d) for d in done) < generate:
-        s = step(model, drafter, prefix, root, nodes, tree, g)
-        root = s["tokens"].gather(1, s["n"].long()[:, None])[:, 0]
+        # sequences that are done wait for the others
+        live = torch.tensor([len(d) < generate for d in done], device="cuda")
+        s = step(model, drafter, prefix, root, nodes, tree, g, live=live)
+        root = torch.where(live, s["tokens"].gather(1, s["n"].clamp(min=0).long()[:, None])[:, 0], root)
         for d, row, n in zip(done, s["tokens"].tolist(), s["n"].tolist()):
+            if len(d) >= generate:
+                continue
             if n < 0:
                 raise RuntimeError("a row of logits is not finite")
             d.extend(row[:n + 1])
         losses.append(float(s["loss"]))
-        # sequences that are done wait for the others: their cache must not run out of pages
-        if max(len(d) for d in done) + nodes > generate + 2 * nodes - 1:
-            break
     if fd.fdllm_cache_status() != 0:
         raise RuntimeError("a kernel reported an error")
     return done, losses, prefix

@@ -157,3 +157,14 @@ def test_a_pass_in_a_graph(example, fd):
         want = once()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("tree", [None, TREE])
+def test_slow_sequences_are_decoded_to_their_end(example, tree):
+    """Every sequence has its tokens, and none much more: those that are done wait for the others."""
+    prompt = torch.randint(0, 1023, (8, 21), generator=torch.Generator().manual_seed(14)).int().cuda()
+    model, drafter = example.Model(seed=15), example.Drafter(1024, seed=16)
+    done, _, prefix = example.decode(model, drafter, prompt, 120, tree=tree)
+    nodes = 6 if tree is None else len(TREE)
+    assert all(120 <= len(d) < 120 + nodes for d in done)
+    assert prefix.lens.tolist() == [20 + len(d) for d in done]
