@@ -600,7 +600,8 @@ size_t fdllm_verify_draft_workspace_bytes(int B, int M, int V, int dtype);
  *              enter the cache; -1 behind.
  *   out_n      [B] int32: taken tokens, 0 .. M - 1; FDLLM_ROW_NONFINITE (and -1 in the row of the
  *              others) where a row on the way holds a NaN or its maximum is infinite;
- *              FDLLM_ROW_DEVICE_ERROR where a kernel gave up a bounded wait (fdllm_cache_status).
+ *              FDLLM_ROW_DEVICE_ERROR where a kernel of this call gave up a bounded wait, or one of
+ *              another call did and fdllm_cache_status was not asked since.
  *   workspace  device, 256-byte aligned, fdllm_verify_draft_workspace_bytes() bytes of any content;
  *              calls that may overlap on the GPU need their own. */
 fdllm_status fdllm_verify_draft(const void *target, const int64_t *target_strides,

@@ -65,7 +65,9 @@ struct VerifyArgs {
     int per;                  // parts of a row
     int pieces, piece_vecs;   // pieces of a row, vectors of one
     int turn, turn_most;      // rows of a turn of the walk at first, and at most
-    uint32_t *status;         // sticky: a bounded wait gave up
+    uint32_t *status;         // sticky: a bounded wait gave up, in whatever call
+    uint32_t *gave_up;        // [streams] one did in that CTA of the first kernel
+    int streams;
 };
 
 __device__ __forceinline__ int nodes_of(const VerifyArgs &a, int b)
@@ -242,6 +244,7 @@ struct StreamShared {
     uint64_t full[kStages], empty[kStages];
     Stage stage[kStages];
 };
+constexpr int kMostStreams = 512;  // CTAs of it (the workspace's size does not ask for the GPU's)
 constexpr int kStreamSmem = kStages * kChunk + (int)sizeof(StreamShared);
 
 template <typename T, bool kGreedy>
@@ -260,10 +263,20 @@ __global__ void __launch_bounds__(kMath + 32, 1)
         }
         fence_mbar_init();
     }
-    __syncthreads();
     pdl_wait();
-    if (threadIdx.x == 0)
+    if (threadIdx.x == 0) {
+        a.gave_up[blockIdx.x] = 0;
         pdl_launch_dependents();
+    }
+    __syncthreads();
+    // What a wait that gave up leaves undone, the second kernel learns from the call's own word: the
+    // sticky one may have been asked for, and cleared, in between.
+    auto wait = [&](uint64_t *bar, uint32_t parity, uint64_t limit_ns) {
+        const bool done = mbar_wait(bar, parity, a.status, limit_ns);
+        if (!done)
+            a.gave_up[blockIdx.x] = 1;
+        return done;
+    };
     if (warp == kMathWarps) {
         // ------------------------------------------------------------ the copying lane
         if (lane != 0)
@@ -285,7 +298,7 @@ __global__ void __launch_bounds__(kMath + 32, 1)
             const int end = (int)piece + 1 < a.pieces ? (int)(piece + 1) * a.piece_vecs : r.vecs;
             for (int v = piece * a.piece_vecs; v < end; v += kChunkVecs, ++k) {
                 const uint32_t s = k % kStages;
-                if (k >= kStages && !mbar_wait(&sm.empty[s], (k / kStages - 1) & 1, a.status)) {
+                if (k >= kStages && !wait(&sm.empty[s], (k / kStages - 1) & 1, kWaitLimitNs)) {
                     alive = false;
                     break;
                 }
@@ -304,7 +317,7 @@ __global__ void __launch_bounds__(kMath + 32, 1)
         }
         if (alive) {
             const uint32_t s = k % kStages;
-            if (k < kStages || mbar_wait(&sm.empty[s], (k / kStages - 1) & 1, a.status)) {
+            if (k < kStages || wait(&sm.empty[s], (k / kStages - 1) & 1, kWaitLimitNs)) {
                 sm.stage[s].n = 0;
                 mbar_arrive(&sm.full[s]);
             } else {
@@ -315,7 +328,7 @@ __global__ void __launch_bounds__(kMath + 32, 1)
         // (the stage that holds the end had its last copy taken)
         const uint32_t most = alive ? kStages - 1 : kStages;
         for (uint32_t i = k > most ? k - most : 0; i < k; ++i)
-            mbar_wait(&sm.full[i % kStages], (i / kStages) & 1, a.status, kDrainLimitNs);
+            wait(&sm.full[i % kStages], (i / kStages) & 1, kDrainLimitNs);
         return;
     }
     // ---------------------------------------------------------------- the counting warps
@@ -323,7 +336,7 @@ __global__ void __launch_bounds__(kMath + 32, 1)
     Share<T, kGreedy> sum;
     for (uint32_t k = 0;; ++k) {
         const uint32_t s = k % kStages;
-        if (!mbar_wait(&sm.full[s], (k / kStages) & 1, a.status))
+        if (!wait(&sm.full[s], (k / kStages) & 1, kWaitLimitNs))
             return;
         const Stage &st = sm.stage[s];
         const uint32_t vecs = st.n, last = st.last;
@@ -702,7 +715,7 @@ __global__ void __launch_bounds__(kDraw, kWalk ? 1 : 2)
     verify_draw_kernel(const __grid_constant__ VerifyArgs a)
 {
     constexpr int E = 16 / sizeof(T);
-    __shared__ int taken, failed;
+    __shared__ int taken, failed, undone;
     __shared__ unsigned long long of_cta[kMaxRanks];
     __shared__ uint2 best[kDraw / 32];
     extern __shared__ __align__(16) uint8_t dynamic[];
@@ -754,8 +767,14 @@ __global__ void __launch_bounds__(kDraw, kWalk ? 1 : 2)
     } else {
         pdl_wait();
         __syncthreads();
+        if (tid == 0)
+            undone = 0;
+        static_assert(kMostStreams <= kDraw, "a thread to each CTA's word");
+        const uint32_t lost = tid < a.streams ? __ldcg(a.gave_up + tid) : 0;
         sum_rows<T>(a, s, b, n);
         __syncthreads();
+        if (lost)
+            undone = 1;
         if (a.parents) {
             for (int c = warp; c < n; c += kDraw / 32) {
                 const int to = decide(a, s, c, n);
@@ -960,7 +979,7 @@ __global__ void __launch_bounds__(kDraw, kWalk ? 1 : 2)
     }
     if (rank != 0)
         return;
-    const bool dead = (__ldcg(a.status) & kDevStatTimeout) != 0;
+    const bool dead = (!kWalk && undone) || (__ldcg(a.status) & kDevStatTimeout) != 0;
     for (int j = tid; j < a.M; j += kDraw) {
         int token = -1, node = -1;
         if (!failed && !dead && j <= taken) {
@@ -1038,6 +1057,7 @@ cudaError_t launch_verify(const VerifyArgs &a, cudaStream_t s)
     const int64_t rows = (int64_t)a.B * (a.draft ? 2 * a.M - 1 : a.M);
     auto small = a.greedy ? verify_small_kernel<T, true> : verify_small_kernel<T, false>;
     auto stream = a.greedy ? verify_stream_kernel<T, true> : verify_stream_kernel<T, false>;
+    VerifyArgs call = a;
     int walkers = 0;
     if (walks(a, sizeof(T))) {
         int dev = 0;
@@ -1049,9 +1069,9 @@ cudaError_t launch_verify(const VerifyArgs &a, cudaStream_t s)
         const int64_t want = (rows * a.per + 7) / 8, most = (int64_t)sm_count() * 8;
         e = launch(small, dim3((unsigned)(want < most ? want : most)), dim3(256), 0, s, true, a);
     } else if (walkers == 0) {
-        const int64_t units = rows * a.pieces, most = sm_count();
-        e = launch(stream, dim3((unsigned)(units < most ? units : most)), dim3(kMath + 32),
-                   kStreamSmem, s, true, a);
+        const int64_t units = rows * a.pieces, most = sm_count() < kMostStreams ? sm_count() : kMostStreams;
+        call.streams = (int)(units < most ? units : most);
+        e = launch(stream, dim3((unsigned)call.streams), dim3(kMath + 32), kStreamSmem, s, true, call);
     }
     if (e != cudaSuccess)
         return e;
@@ -1069,13 +1089,12 @@ cudaError_t launch_verify(const VerifyArgs &a, cudaStream_t s)
     cfg.attrs = attr;
     cfg.numAttrs = plain_launches ? 1 : 2;
     if (walkers == 0)
-        return cudaLaunchKernelEx(&cfg, verify_draw_kernel<T, false>, VerifyArgs(a));
-    VerifyArgs by_turns = a;
+        return cudaLaunchKernelEx(&cfg, verify_draw_kernel<T, false>, call);
     const int64_t share = (int64_t)a.V * (int)sizeof(T) / ranks;
     auto rows_of = [&](int64_t bytes) { return (int)(bytes < share ? 1 : bytes / share < kTurn ? bytes / share : kTurn); };
-    by_turns.turn = rows_of(kTurnBytes);
-    by_turns.turn_most = rows_of(2 * kTurnBytes);
-    return cudaLaunchKernelEx(&cfg, verify_draw_kernel<T, true>, by_turns);
+    call.turn = rows_of(kTurnBytes);
+    call.turn_most = rows_of(2 * kTurnBytes);
+    return cudaLaunchKernelEx(&cfg, verify_draw_kernel<T, true>, call);
 }
 
 // How rows are cut: whole, or in pieces of whole chunks so that every SM has two, and no piece is
@@ -1111,7 +1130,7 @@ size_t verify_bytes(int B, int M, int V, int dtype)
         cut_rows(rows, V, rows_esize(dtype), pieces, vecs, per);
         most = per > most ? per : most;
     }
-    return ((size_t)verify_rows(B, M) * most * sizeof(UnitPartial) + 255) / 256 * 256;
+    return kMostStreams * 4 + ((size_t)verify_rows(B, M) * most * sizeof(UnitPartial) + 255) / 256 * 256;
 }
 
 bool verify_sizes(int B, int M, int V)
@@ -1177,7 +1196,8 @@ fdllm_status fdllm_verify_draft(const void *target, const int64_t *target_stride
     a.out_tokens = out_tokens;
     a.out_nodes = out_nodes;
     a.out_n = out_n;
-    a.parts = static_cast<UnitPartial *>(workspace);
+    a.gave_up = static_cast<uint32_t *>(workspace);
+    a.parts = reinterpret_cast<UnitPartial *>(a.gave_up + kMostStreams);
     cut_rows((int64_t)B * (a.draft ? 2 * M - 1 : M), V, rows_esize(dtype), a.pieces, a.piece_vecs, a.per);
     a.status = cache_status_word();
     if (!a.status)

@@ -401,3 +401,25 @@ def test_refusals(fd):
                 dict(target=target.double()), dict(target=target[0]), dict(lens=ints([1]))):
         with pytest.raises((TypeError, ValueError)):
             call(**bad)
+
+
+@pytest.mark.parametrize("kind,M,V", [("draft", 4, 515), ("draft", 5, 50021), ("tree", 40, 50021)])
+def test_a_wait_that_ran_out_is_told_by_every_sequence(fd, kind, M, V):
+    """Short rows, long ones, and a tree that is read along the way: after a wait that ran out nothing
+    is reported as taken until the status was asked for; then all is as before, whatever the workspace
+    holds."""
+    target, tokens, kw = inputs(5, M, V, BF, kind, seed=41)
+    target, tokens, kw = cuda(target), cuda(tokens), {k: cuda(v) for k, v in kw.items()}
+    size = fd.fdllm_verify_draft_workspace_bytes(5, M, V)
+    call = lambda fill: fd.fdllm_verify_draft(
+        target, tokens, workspace=torch.full((size,), fill, dtype=torch.uint8, device="cuda"), **kw)
+    want = call(0)
+    assert bool((want[2] >= 0).all())
+    assert fd.fdllm_cache_status() == 0
+    assert fd.fdllm_cache_check_wait(1) == 0
+    out, nodes, n = call(0)
+    assert n.tolist() == [-2] * 5 and bool((out == -1).all()) and bool((nodes == -1).all())
+    assert fd.fdllm_cache_status() != 0
+    assert fd.fdllm_cache_status() == 0
+    for fill in (0, 1, 255):
+        assert all(torch.equal(a, b) for a, b in zip(call(fill), want))
