@@ -664,7 +664,8 @@ fdllm_status fdllm_distill_step(const void *logits, int dtype, int B, int L, int
  * fdllm_cache_key_weights, fdllm_verify_draft and the distillation calls on the current device:
  * synchronises `stream`, returns FDLLM_ERR_DEVICE if one of their kernels gave up a bounded wait since
  * the last call (the results of the calls since then are unusable; fdllm_verify_draft reports
- * FDLLM_ROW_DEVICE_ERROR for every sequence until then), FDLLM_OK otherwise, and clears it. */
+ * FDLLM_ROW_DEVICE_ERROR for every sequence until then), FDLLM_OK otherwise, and clears it.  The
+ * word is the device's, whichever thread's call it was: who asks, asks for all. */
 fdllm_status fdllm_cache_status(void *stream);
 
 /* Health check of those kernels' bounded waits: enqueues a warp that waits on a barrier nobody

@@ -977,9 +977,9 @@ def fdllm_verify_draft(target: torch.Tensor, tokens: torch.Tensor, parents=None,
 
     ``target`` [B, M, V] bf16/fp16/fp32, row j the target's logits after node j (node 0 the last
     committed token; rows may lie anywhere, their values contiguous); ``tokens`` int32 [B, M] the
-    nodes' tokens; ``parents`` int32 [B, M] a tree (None: a chain); ``lens`` int32 [B] the counts of nodes; ``draft`` [B, M - 1, V] the logits a
-    chain was drawn from at ``draft_temperature`` (None: ``temperature``), or None where the tokens
-    were chosen; ``uniform`` fp32 [B, M] in [0, 1) and ``noise`` fp32 [B, V] exponential variables
+    nodes' tokens; ``parents`` int32 [B, M] a tree (None: a chain); ``lens`` int32 [B] the counts of
+    nodes; ``draft`` [B, M - 1, V] the logits a chain was drawn from at ``draft_temperature`` (None:
+    ``temperature``), or None where the tokens were chosen; ``uniform`` fp32 [B, M] in [0, 1) and ``noise`` fp32 [B, V] exponential variables
     (None at temperature 0, which is greedy).  Returns (tokens int32 [B, M]: the taken ones, then
     the next; nodes int32 [B, M]: the root, then the taken ones; -1 behind; n int32 [B])."""
     dev, dt = target.device, target.dtype
@@ -1004,8 +1004,8 @@ def fdllm_verify_draft(target: torch.Tensor, tokens: torch.Tensor, parents=None,
         need = lib.fdllm_verify_draft_workspace_bytes(B, M, V, code)
         workspace = _made((need if need > 256 else 256,), _U8, dev, stream)
     st = lib.fdllm_verify_draft(
-        tp, ts, dp, ds, code, B, M, V, _ptr(tokens, "tokens", _I32, nodes, dev), _ptr(parents, "parents", _I32, nodes, dev),
-        _ptr(lens, "lens", _I32, (B,), dev), temperature,
+        tp, ts, dp, ds, code, B, M, V, _ptr(tokens, "tokens", _I32, nodes, dev),
+        _ptr(parents, "parents", _I32, nodes, dev), _ptr(lens, "lens", _I32, (B,), dev), temperature,
         temperature if draft_temperature is None else draft_temperature,
         _ptr(uniform, "uniform", _F32, nodes, dev), _ptr(noise, "noise", _F32, (B, V), dev),
         _ptr(out_tokens, "out_tokens", _I32, nodes, dev),

@@ -42,7 +42,9 @@ constexpr int kChunkVecs = kChunk / 16;
 // Rows up to this many bytes: a few warps each, without the ring, whose beginning and end cost more than
 // their copies hide (14 trees of 53 rows of 23 KB, the whole call: 14.8 us, with the ring 24.8).
 constexpr int kSmallRow = 32768;
-constexpr int kSmallVecs = 8;     // vectors of a lane in such a row, about
+// Vectors of a lane in such a row, about (33 chains of 51 rows of 2088 values 11.5 us, with four vectors
+// 13.5, with sixteen 10.8; 8 of nine of 8000 9.1, 9.2 and 9.9; 14 trees of 53 of 11500 16.7, 16.6 and 13.4).
+constexpr int kSmallVecs = 8;
 constexpr int kDraw = 512;       // threads of a CTA of the walk and the draw (256: 69 us for 58)
 constexpr int kMaxRanks = 8;     // CTAs of a cluster of them
 
@@ -585,12 +587,17 @@ __device__ __forceinline__ int decide(const VerifyArgs &a, const Nodes &s, int c
 constexpr int kTurn = 8;  // rows of a turn at most
 // Rows are read along the way where all of them are this many bytes: long ones (beyond kSmallRow), short
 // ones.  In bf16: 8 trees of 48 nodes of 126464 values 14.6 us (all rows first: 34.5), 16 of 60 of 32000
-// 13.5 (26.4), one of 48 of 126464 (12 MB) 11.2 (18.2), 64 of 40 of 11500 20 (30); but 8 of 16 of 32000 (8 MB) 13
-// (12), 14 of 53 of 11500 (17 MB) 16.8 (15.2).  Where paths are long the turns add up: 8 trees that are
-// chains of 48, every node taken, are 52 us (22), with two rows a turn throughout more.
+// 13.5 (26.4), one of 48 of 126464 (12 MB) 11.2 (18.2), 64 of 40 of 11500 20 (30); but 8 of 16 of 32000
+// (8 MB) 13 (12), 14 of 53 of 11500 (17 MB) 16.8 (15.2).  Where paths are long the turns add up: 8 trees
+// that are chains of 48, every node taken, are 52 us (22), with two rows a turn throughout more.
 constexpr int64_t kWalkLong = 12000000, kWalkShort = 40000000;
-constexpr int kWalkShare = 8192;     // bytes of a row that a CTA is worth
-constexpr int kTurnBytes = 1 << 16;  // of a CTA's share of a turn's rows, and twice that where it went well
+// Bytes of a row that a CTA is worth (half and twice as many are alike; four times: 16 trees of 60 of 32000
+// values 15.2 us for 13.8, 64 of 40 of 11500 19.1 for 18.1).
+constexpr int kWalkShare = 8192;
+// Of a CTA's share of a turn's rows, and twice that where it went well (half: one tree of 48 of 126464 20.6
+// us for 15.7, 64 of 60 of 19000 23.4 for 21.2, 64 of 40 of 11500 17.4 for 18.1; twice: 8 of 48 of 126464
+// 17.1 for 14.7).
+constexpr int kTurnBytes = 1 << 16;
 
 struct WalkShared {
     int4 part[kDraw / 32];                // of a warp's share of its row
@@ -634,7 +641,8 @@ __device__ __forceinline__ void walk(const VerifyArgs &a, const Nodes &s, WalkSh
         for (int i = 1; i < kTurn; ++i)
             mine = g == i ? node[i] : mine;
         const RowSpan<T> r(reinterpret_cast<const T *>(row_at<T>(a, b, mine, false).p), a.V);
-        const int per = (r.vecs + ranks - 1) / ranks, lo = min(r.vecs, rank * per), hi = min(r.vecs, lo + per);
+        const int per = (r.vecs + ranks - 1) / ranks;
+        const int lo = min(r.vecs, rank * per), hi = min(r.vecs, lo + per);
         const int wide = 32 * ((kWarps - g + rows - 1) / rows);  // threads of the row
         Share<T, kGreedy> share;
         for (int v = lo + (warp / rows) * 32 + lane; v < hi; v += kEight * wide) {
@@ -1000,7 +1008,8 @@ bool walks(const VerifyArgs &a, int es)
     return a.parents && a.B * (a.M * row) >= (row > kSmallRow ? kWalkLong : kWalkShort);
 }
 
-// CTAs that share a sequence's rows then: a cluster of as many for each sequence at once, where there is room.
+// CTAs that share a sequence's rows then: a cluster of as many for each sequence at once, where there is
+// room.
 // `held`: the clusters of 1, 2, 4 and 8 that the GPU holds.
 int walk_ranks(const VerifyArgs &a, int es, const std::atomic<int> *held)
 {
@@ -1091,14 +1100,19 @@ cudaError_t launch_verify(const VerifyArgs &a, cudaStream_t s)
     if (walkers == 0)
         return cudaLaunchKernelEx(&cfg, verify_draw_kernel<T, false>, call);
     const int64_t share = (int64_t)a.V * (int)sizeof(T) / ranks;
-    auto rows_of = [&](int64_t bytes) { return (int)(bytes < share ? 1 : bytes / share < kTurn ? bytes / share : kTurn); };
+    auto rows_of = [&](int64_t bytes) {
+        return (int)(bytes < share ? 1 : bytes / share < kTurn ? bytes / share : kTurn);
+    };
     call.turn = rows_of(kTurnBytes);
     call.turn_most = rows_of(2 * kTurnBytes);
     return cudaLaunchKernelEx(&cfg, verify_draw_kernel<T, true>, call);
 }
 
 // How rows are cut: whole, or in pieces of whole chunks so that every SM has two, and no piece is
-// longer than four chunks (where rows are many, pieces of one, two and four are alike within 2 %).
+// longer than four chunks (where rows are many, pieces of one, two and four are alike within 2 %).  The SMs
+// are counted as 152: the workspace's size goes by it, and that asks no GPU.  With one piece to an SM,
+// rows in the L2: 16 greedy chains of 17 of 50021 fp32 values 11.5 us for 13.0, 16 chains of nine of 126464
+// 22.8 for 25.4; with four 13.2 and 24.0; fewer rows are alike.
 void cut_rows(int64_t rows, int V, int es, int &pieces, int &piece_vecs, int &per)
 {
     if ((int64_t)V * es <= kSmallRow) {
